@@ -50,6 +50,9 @@ typedef enum {
                                               completed); the results of that call are not valid           */
 #define PODS_STATUS_INTERNAL         0x40u /* checked build only (-DPODS_BOUNDS_CHECK): an index computed inside a
                                               kernel left its extent; the access was skipped               */
+#define PODS_STATUS_NONFINITE_LOGIT  0x80u /* a row of logits held NaN or +inf                             */
+#define PODS_STATUS_EMPTY_ROW        0x100u /* every logit of a row was -inf                                */
+#define PODS_STATUS_PARAM_RANGE      0x200u /* pods_sample: a setting or random number of a row was out of range */
 #define PODS_STATUS_INDEX_RANGE      0x20u /* pods_compact: an entry of idx was outside [0,n); rollout 0 of the
                                               group was used instead                                        */
 
@@ -64,6 +67,18 @@ typedef enum {
 #define PODS_FLAG_ADV_BEFORE 0x1u  /* advantages from full-group statistics (Appendix A.3 "Before") */
 #define PODS_FLAG_STD_SAMPLE 0x2u  /* divide by (count-1) instead of count in the standard deviation  */
 #define PODS_FLAG_EXACT_TIES 0x4u  /* max-variance rule: settle near-equal split scores in ~106-bit arithmetic (see pods_select) */
+
+/* Element types of the calls that take logits of several types. */
+typedef enum {
+    PODS_DTYPE_BF16 = 0,
+    PODS_DTYPE_F16 = 1,
+    PODS_DTYPE_F32 = 2
+} pods_dtype;
+
+#define PODS_MAX_ROW_V 524288      /* longest row of pods_sample, pods_topk and pods_distill_chunk */
+#define PODS_MAX_TOPK 1024         /* longest list of pods_topk and pods_distill_chunk */
+
+#define PODS_DISTILL_REST 0x1u     /* pods_distill_chunk: add the term of the mass outside the list */
 
 #define PODS_MAX_N 1024            /* largest supported group size n */
 
@@ -259,6 +274,85 @@ int grpo_loss_from_hidden(const void* hidden, int64_t ldh, const void* W, int64_
                           int32_t V, int32_t d, float eps, float beta, float grad_scale, double* loss_acc,
                           float* logp, float* dhidden, int64_t lddh, float* dW, int64_t lddw, void* workspace,
                           size_t workspace_bytes, uint32_t* status, void* stream);
+
+/*
+ * pods_sample - one token per row drawn from the policy's logits, the step of a rollout that comes before its reward:
+ * the sampling policy pi_old of Sections 3.1 and 3.2, with the old_logp that grpo_loss_chunk takes.  Per row t, z its
+ * logits, d_v = (z_v - max z) / temperature, e_v = exp(d_v), and ids ordered by larger z, then lower id (-0 == +0):
+ *   top_k   keeps the first top_k ids (off where <= 0 or >= V)
+ *   top_p   of those, the shortest prefix whose sum of e is at least top_p times theirs, at least one id (off where >= 1)
+ *   min_p   keeps the ids with e_v >= min_p (off where <= 0; above 1 it is read as 1)
+ *   token = the first kept id, ids ascending, whose running sum of e exceeds u[t] times the kept sum
+ *   logp  = log softmax(z / temperature)[token], before any filter: old_logp of an objective on logits / temperature
+ *   logq  = the log-probability with which the token was drawn, after the filters
+ * A temperature below 2^-20 takes the first id of the order; logp is then that of temperature 1, logq 0.  Tokens are
+ * those of fp64 arithmetic: a draw or a border too close to call in fp32 is taken again in fp64.
+ *
+ *   logits [dev] [T, V] of dtype, row pitch ldl elements, any alignment of the element type
+ *   u      [dev] fp32 [T] uniform numbers in [0, 1)
+ *   temperature_row, top_p_row, min_p_row [dev] fp32 [T] and top_k_row [dev] int32 [T]: each row's own settings; where
+ *          one is NULL the scalar beside it holds for every row
+ *   mask   [dev] uint8 [T] or NULL: rows with mask 0 are not read and their outputs are left as they were
+ *   tokens [dev] int32 [T]    logp, logq [dev] fp32 [T], each may be NULL
+ * Row settings out of range (temperature negative, infinite or NaN: 1 is used; top_p or min_p NaN: off; u below 0 or NaN:
+ * 0; u of 1 or more: the largest number below 1) raise PODS_STATUS_PARAM_RANGE; a bad scalar temperature, top_p or min_p
+ * returns PODS_ERR_INVALID_ARG.  -inf marks an id that cannot be drawn.  A row of -inf alone gets token -1 and -inf log-
+ * probabilities (PODS_STATUS_EMPTY_ROW), one with NaN or +inf token -1 and NaN (PODS_STATUS_NONFINITE_LOGIT).
+ * V above PODS_MAX_ROW_V or an unknown dtype returns PODS_ERR_UNSUPPORTED.  No workspace.
+ */
+int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, const float* u,
+                const float* temperature_row, float temperature, const int32_t* top_k_row, int32_t top_k,
+                const float* top_p_row, float top_p, const float* min_p_row, float min_p, const uint8_t* mask,
+                int32_t* tokens, float* logp, float* logq, uint32_t* status, void* stream);
+
+/*
+ * pods_topk - the first K ids of each row (larger logit first, then lower id), their logits and the row's log-normaliser:
+ * what a teacher leaves behind for pods_distill_chunk instead of its [T,V] logits.
+ *   ids [dev] int32 [T,K]   values [dev] fp32 [T,K], the logits themselves   lse [dev] fp32 [T] or NULL:
+ *   log sum_v exp(z_v / temperature)
+ * Logits, mask and refusals as in pods_sample; 1 <= K <= min(V, PODS_MAX_TOPK); temperature > 0 and finite.  A row with NaN
+ * or +inf gets ids -1 and NaN values and lse (PODS_STATUS_NONFINITE_LOGIT).  -inf logits come last, by id; a row of nothing
+ * else has lse -inf (PODS_STATUS_EMPTY_ROW).
+ */
+int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int32_t K, float temperature,
+              const uint8_t* mask, int32_t* ids, float* values, float* lse, uint32_t* status, void* stream);
+
+/* Bytes of workspace pods_distill_chunk needs for a chunk of T rows. */
+size_t pods_distill_chunk_workspace_bytes(int64_t T);
+
+/*
+ * pods_distill_chunk - Kullback-Leibler divergence from a teacher's top logits to the policy's logits, and its gradient
+ * with respect to the logits, for rows [row0, row0 + T) of the packed tokens: the companion of grpo_loss_chunk where a
+ * policy is trained towards a teacher on the same rollouts, with the same weights.  (The paper has no counterpart.)
+ * Per row t of rollout i, z the policy's logits, p = softmax(z / temperature), and (id_j, y_j), j < K the teacher's list:
+ *   q_j = exp(y_j / temperature - L),  L = teacher_lse[t], or log sum_j exp(y_j / temperature) if teacher_lse is NULL
+ *   Q = sum_j q_j;  s = the sum of p over the listed ids;  r = max(0, 1 - Q) with PODS_DISTILL_REST, else 0
+ *   kl_t = sum_j q_j (log q_j - log p[id_j]) + r (log r - log(1 - s))
+ *   g_t  = grad_scale mask_t w_i / temperature
+ *   dlogits[t,v] = g_t ((Q + r) p_v - sum over the j with id_j == v of q_j)      listed v
+ *                = g_t ((Q + r) p_v - r p_v / (1 - s))                           every other v
+ * rounded to dtype (nearest even), and sum_t mask_t w_i kl_t is ADDED to *loss_acc (the caller zeroes it; fixed order).
+ * 1 - s is summed over the ids outside the list, never taken as a difference.  Where they have no mass at all (every such
+ * logit -inf, or none left) the rest's term is left out: r = 0.  A term with q_j = 0 is 0.  A listed id that the policy
+ * cannot produce (logit -inf, q_j > 0) makes kl_t +inf with a finite gradient.
+ *
+ *   logits [dev] [T, V] of dtype, row pitch ldl elements, any alignment of the element type
+ *   ids [dev] int32 [T, K], values [dev] fp32 [T, K], both of row pitch ldk; an id of -1 is an unused entry, another id
+ *          outside [0, V) raises PODS_STATUS_TOKEN_RANGE and is unused too; an id may stand in several entries
+ *   teacher_lse [dev] fp32 [T] or NULL (PODS_DISTILL_REST needs it)
+ *   seq_weight, cu_seqlens, M, row0, mask: as in grpo_loss_chunk (grpo_seq_weights makes the weights)
+ *   kl [dev] fp32 [T]: kl_t, 0 for rows whose mask or weight is 0 (those rows are not read)
+ *   dlogits [dev] [T, V] of dtype, pitch ldd, or NULL for the loss alone; may be the same buffer as logits (in place,
+ *          ldd == ldl), must not overlap it otherwise.  Rows whose mask or weight is 0 are zero.
+ *   loss_acc [dev] fp64 scalar; workspace [dev] of pods_distill_chunk_workspace_bytes(T), 16-byte aligned
+ * A row with NaN or +inf, or of -inf alone, has kl and gradient NaN and raises PODS_STATUS_NONFINITE_LOGIT or
+ * PODS_STATUS_EMPTY_ROW.  V above PODS_MAX_ROW_V, K above PODS_MAX_TOPK, an unknown dtype or flag: PODS_ERR_UNSUPPORTED.
+ */
+int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* ids, const float* values,
+                       int64_t ldk, int32_t K, const float* teacher_lse, const double* seq_weight,
+                       const int64_t* cu_seqlens, int64_t M, int64_t row0, const uint8_t* mask, int64_t T, int32_t V,
+                       float temperature, uint32_t flags, float grad_scale, double* loss_acc, float* kl, void* dlogits,
+                       int64_t ldd, void* workspace, size_t workspace_bytes, uint32_t* status, void* stream);
 
 /*
  * pods_set_loss_from_hidden_panel_bytes - tuning knob (the paper has no counterpart): the most bytes of workspace

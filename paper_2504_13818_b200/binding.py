@@ -19,7 +19,11 @@ RULE_MAXVAR, RULE_MAXREWARD, RULE_RANDOM, RULE_PERCENTILE = 0, 1, 2, 3
 FLAG_ADV_BEFORE, FLAG_STD_SAMPLE, FLAG_EXACT_TIES = 1, 2, 4
 STATUS_NONFINITE_REWARD, STATUS_TOKEN_RANGE, STATUS_CAPACITY, STATUS_NEG_LENGTH, STATUS_TIMEOUT = 1, 2, 4, 8, 16
 STATUS_INDEX_RANGE, STATUS_INTERNAL = 32, 64
+STATUS_NONFINITE_LOGIT, STATUS_EMPTY_ROW, STATUS_PARAM_RANGE = 128, 256, 512
 MAX_N = 1024
+MAX_ROW_V, MAX_TOPK = 524288, 1024
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+DISTILL_REST = 1
 
 # name -> (restype, argtypes); mirrors include/pods.h
 _p, _i64, _i32, _u64, _u32, _f32, _sz = (C.c_void_p, C.c_int64, C.c_int32, C.c_uint64, C.c_uint32,
@@ -47,6 +51,12 @@ SIGNATURES = {
     "pods_set_loss_from_hidden_panel_bytes": (_sz, [_sz]),
     "grpo_loss_from_hidden": (C.c_int, [_p, _i64, _p, _i64, _p, _p, _p, _p, _p, _p, _i64, _i64, _p, _i64, _i32, _i32,
                                         _f32, _f32, _f32, _p, _p, _p, _i64, _p, _i64, _p, _sz, _p, _p]),
+    "pods_sample": (C.c_int, [_p, _i64, _i32, _i64, _i32, _p, _p, _f32, _p, _i32, _p, _f32, _p, _f32, _p, _p, _p, _p,
+                              _p, _p]),
+    "pods_topk": (C.c_int, [_p, _i64, _i32, _i64, _i32, _i32, _f32, _p, _p, _p, _p, _p, _p]),
+    "pods_distill_chunk_workspace_bytes": (_sz, [_i64]),
+    "pods_distill_chunk": (C.c_int, [_p, _i64, _i32, _p, _p, _i64, _i32, _p, _p, _p, _i64, _i64, _p, _i64, _i32, _f32,
+                                     _u32, _f32, _p, _p, _p, _i64, _p, _sz, _p, _p]),
     "pods_selftest_bounded_wait": (C.c_int, [_u32, _p, _p]),
     "pods_set_loss_cluster_min_vocab": (_i32, [_i32]),
     "pods_host_step_create": (C.c_int, [_i64, _i32, _i32, _i64, _i64, _i32, _i64, _p]),
@@ -437,6 +447,150 @@ def grpo_loss_from_hidden(hidden, W, tokens, old_logp, ref_logp, adv, seq_weight
                                       workspace.numel(), _dev(status, torch.int32, "status", True), _stream())
     _check(rc, "grpo_loss_from_hidden")
     return logp, dhidden
+
+def _typed_rows(t, name):
+    """Pointer, row pitch and dtype code of a 2-D CUDA tensor of logits whose rows are contiguous."""
+    _require(isinstance(t, torch.Tensor) and t.dim() == 2, "%s must be [T,V]" % name)
+    _require(t.dtype in DTYPES, "%s must be bfloat16, float16 or float32, got %s" % (name, t.dtype))
+    _require(t.shape[1] <= MAX_ROW_V, "%s rows may hold at most %d entries, got %d" % (name, MAX_ROW_V, t.shape[1]))
+    _require(t.is_cuda, "%s must be a CUDA tensor" % name)
+    _require(t.stride(1) == 1 or t.shape[1] == 1, "%s rows must be contiguous" % name)
+    pitch = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    _require(pitch >= t.shape[1], "%s rows must not overlap" % name)
+    return C.c_void_p(t.data_ptr()), pitch, DTYPES[t.dtype]
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device's current stream: tensors of another device are refused."""
+    for t in tensors:
+        if t is not None:
+            _require(not t.is_cuda or t.device.index == torch.cuda.current_device(),
+                     "tensors must be on the current CUDA device, got %s" % t.device)
+
+
+def _setting(x, T, name):
+    """A sampling setting: one number for every row, or a tensor [T] of each row's own -> (tensor or None, scalar)."""
+    if isinstance(x, torch.Tensor):
+        _numel(x, T, name)
+        return x, 0
+    return None, x
+
+
+def pods_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask=None, tokens=None, logp=None, logq=None,
+                want_logq=False, status=None):
+    """Draw one token per row: logits [T,V] (bf16, fp16 or fp32), u [T] fp32 in [0,1) -> (tokens [T] int32, logp [T]
+    fp32, logq [T] fp32 or None).
+
+    temperature, top_k, top_p and min_p are numbers or tensors [T] (fp32; top_k int32).  logp is the log-probability
+    under softmax(logits / temperature), the old_logp of grpo_loss_chunk; logq the one the token was drawn with, after the
+    filters.  Rows with mask 0 are left alone: pass the outputs then (those made here start as -1, 0 and 0)."""
+    _require(isinstance(logits, torch.Tensor) and logits.dim() == 2, "logits must be [T,V]")
+    T, V = logits.shape
+    _require(V >= 1, "logits must have at least one column")
+    for t, name in ((u, "u"), (mask, "mask"), (tokens, "tokens"), (logp, "logp"), (logq, "logq")):
+        _numel(t, T, name)
+    tau_t, tau = _setting(temperature, T, "temperature")
+    k_t, k = _setting(top_k, T, "top_k")
+    p_t, p = _setting(top_p, T, "top_p")
+    m_t, m = _setting(min_p, T, "min_p")
+    lp, ldl, dtype = _typed_rows(logits, "logits")
+    _on_current_device(logits, u, mask, tokens, logp, logq, tau_t, k_t, p_t, m_t, status)
+    dev = logits.device
+    new = torch.empty if mask is None else torch.zeros
+    if tokens is None:
+        tokens = torch.empty(T, dtype=torch.int32, device=dev) if mask is None else torch.full((T,), -1, dtype=torch.int32, device=dev)
+    if logp is None:
+        logp = new(T, dtype=torch.float32, device=dev)
+    if logq is None and want_logq:
+        logq = new(T, dtype=torch.float32, device=dev)
+    rc = load().pods_sample(lp, ldl, dtype, T, V, _dev(u, torch.float32, "u"),
+                            _dev(tau_t, torch.float32, "temperature", True), tau, _dev(k_t, torch.int32, "top_k", True), k,
+                            _dev(p_t, torch.float32, "top_p", True), p, _dev(m_t, torch.float32, "min_p", True), m,
+                            _dev(mask, torch.uint8, "mask", True), _dev(tokens, torch.int32, "tokens"),
+                            _dev(logp, torch.float32, "logp"), _dev(logq, torch.float32, "logq", True),
+                            _dev(status, torch.int32, "status", True), _stream())
+    _check(rc, "pods_sample")
+    return tokens, logp, logq
+
+
+def pods_topk(logits, K, temperature=1.0, mask=None, ids=None, values=None, lse=None, status=None):
+    """The first K ids of each row (larger logit first, then lower id): logits [T,V] -> (ids [T,K] int32, values [T,K]
+    fp32, lse [T] fp32), lse being log sum exp(logits / temperature).
+
+    Rows with mask 0 are left alone: pass the outputs then (those made here start as -1, 0 and 0)."""
+    _require(isinstance(logits, torch.Tensor) and logits.dim() == 2, "logits must be [T,V]")
+    T, V = logits.shape
+    _require(1 <= K <= min(V, MAX_TOPK), "need 1 <= K <= min(V, %d), got K=%d V=%d" % (MAX_TOPK, K, V))
+    for t, name in ((ids, "ids"), (values, "values")):
+        _require(t is None or tuple(t.shape) == (T, K), "%s must have the shape [%d, %d]" % (name, T, K))
+    _numel(mask, T, "mask")
+    _numel(lse, T, "lse")
+    lp, ldl, dtype = _typed_rows(logits, "logits")
+    _on_current_device(logits, mask, ids, values, lse, status)
+    dev = logits.device
+    new = torch.empty if mask is None else torch.zeros
+    if ids is None:
+        ids = torch.empty((T, K), dtype=torch.int32, device=dev) if mask is None else torch.full((T, K), -1, dtype=torch.int32, device=dev)
+    if values is None:
+        values = new((T, K), dtype=torch.float32, device=dev)
+    if lse is None:
+        lse = new(T, dtype=torch.float32, device=dev)
+    rc = load().pods_topk(lp, ldl, dtype, T, V, K, temperature, _dev(mask, torch.uint8, "mask", True),
+                          _dev(ids, torch.int32, "ids"), _dev(values, torch.float32, "values"),
+                          _dev(lse, torch.float32, "lse"), _dev(status, torch.int32, "status", True), _stream())
+    _check(rc, "pods_topk")
+    return ids, values, lse
+
+
+def pods_distill_chunk_workspace_bytes(T) -> int:
+    return int(load().pods_distill_chunk_workspace_bytes(T))
+
+
+def pods_distill_chunk(logits, ids, values, teacher_lse, seq_weight, cu_seqlens, row0, mask, loss_acc, kl=None, dlogits=None,
+                       workspace=None, temperature=1.0, rest=False, want_grad=True, grad_scale=1.0, status=None):
+    """Rows [row0, row0+T) of the divergence from a teacher's lists (ids, values [T,K] as pods_topk writes them) to the
+    policy's logits [T,V] (bf16, fp16 or fp32), with its gradient.
+
+    teacher_lse [T] fp32 or None (the list is renormalised); rest: add the term of the mass outside the list.  loss_acc
+    [1] fp64 accumulates.  Returns (kl [T] fp32, dlogits like logits, or None without want_grad); ``dlogits`` may be
+    ``logits`` itself.  Missing outputs and the workspace are allocated here."""
+    _require(isinstance(logits, torch.Tensor) and logits.dim() == 2, "logits must be [T,V]")
+    T, V = logits.shape
+    _require(isinstance(ids, torch.Tensor) and ids.dim() == 2 and ids.shape[0] == T, "ids must be [T,K] with T = %d" % T)
+    K = ids.shape[1]
+    _require(1 <= K <= MAX_TOPK, "need 1 <= K <= %d, got K=%d" % (MAX_TOPK, K))
+    _require(isinstance(values, torch.Tensor) and tuple(values.shape) == (T, K), "values must have the shape [%d, %d]" % (T, K))
+    M = cu_seqlens.numel() - 1
+    _require(M >= 1, "cu_seqlens must hold M+1 >= 2 entries")
+    _require(not rest or teacher_lse is not None, "rest needs teacher_lse")
+    for t, name in ((teacher_lse, "teacher_lse"), (mask, "mask"), (kl, "kl")):
+        _numel(t, T, name)
+    _numel(seq_weight, M, "seq_weight")
+    _numel(loss_acc, 1, "loss_acc")
+    _require(dlogits is None or (tuple(dlogits.shape) == (T, V) and dlogits.dtype == logits.dtype),
+             "dlogits must have the shape and dtype of logits")
+    lp, ldl, dtype = _typed_rows(logits, "logits")
+    _on_current_device(logits, ids, values, teacher_lse, seq_weight, cu_seqlens, mask, loss_acc, kl, dlogits, workspace, status)
+    dev = logits.device
+    if kl is None:
+        kl = torch.empty(T, dtype=torch.float32, device=dev)
+    if dlogits is None and want_grad:
+        dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev)
+    need = pods_distill_chunk_workspace_bytes(T)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _require(workspace.numel() >= need, "workspace must hold %d bytes, got %d" % (need, workspace.numel()))
+    dp, ldd, _ = _typed_rows(dlogits, "dlogits") if dlogits is not None else (None, 0, 0)
+    rc = load().pods_distill_chunk(lp, ldl, dtype, _dev(ids, torch.int32, "ids"), _dev(values, torch.float32, "values"), K, K,
+                                   _dev(teacher_lse, torch.float32, "teacher_lse", True),
+                                   _dev(seq_weight, torch.float64, "seq_weight"), _dev(cu_seqlens, torch.int64, "cu_seqlens"),
+                                   M, row0, _dev(mask, torch.uint8, "mask", True), T, V, temperature,
+                                   DISTILL_REST if rest else 0, grad_scale, _dev(loss_acc, torch.float64, "loss_acc"),
+                                   _dev(kl, torch.float32, "kl"), dp, ldd, _dev(workspace, torch.uint8, "workspace"),
+                                   workspace.numel(), _dev(status, torch.int32, "status", True), _stream())
+    _check(rc, "pods_distill_chunk")
+    return kl, dlogits
+
 
 
 class HostStep:

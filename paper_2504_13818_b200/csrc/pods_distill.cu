@@ -1,0 +1,473 @@
+// pods_distill_chunk: divergence from a teacher's top-K list to the policy's logits, with its gradient.
+//
+// With z the row, zl its listed logits, the other logits are summed apart: m2 their maximum, S2 = sum exp((z - m2)/tau).
+// Then  Z = S2 e^{(m2-zmax)/tau} + sum_listed e^{(z-zmax)/tau},  1 - s = S2 e^{(m2-zmax)/tau} / Z  (no difference is ever
+// taken, so a policy that is sure of the list keeps its accuracy), and every id outside the list has the gradient
+//   e^{(z_v - m2)/tau} * g ((Q + r) e^{(m2-zmax)/tau} / Z - r / S2),
+// one factor for the row.  What concerns the list is fp64: K exponentials a CTA, against V / CL fp32 ones twice.
+//
+// A cluster of CTAs holds the row in shared memory (row_cluster.cuh): one read and one write per element.  The listed
+// logits are taken out first (their slots become -inf), so both sweeps run over the segment without asking about the
+// list; the first CTA-wide sweep is the maximum, the second the sum, and after one exchange over the cluster the third
+// writes the gradient, exponentials taken again (two on the special-function pipe per 4 bytes of traffic, where 2.8 would
+// be free).  The listed entries are then written over by the threads that hold them.
+
+#include "grpo_loss_common.cuh"
+#include "row_cluster.cuh"
+
+using namespace pods_row;
+
+namespace {
+
+constexpr int W = 8;
+constexpr int kThreads = W * 32;
+constexpr int kPer = PODS_MAX_TOPK / kThreads;         // list entries a thread holds at most
+
+struct DistillArgs {
+    const void* logits;
+    int64_t ldl;
+    const int32_t* ids;
+    const float* values;
+    int64_t ldk;
+    int K;
+    const float* teacher_lse;
+    const double* seq_weight;
+    const int64_t* cu_seqlens;
+    int64_t M, row0;
+    const uint8_t* mask;
+    int64_t T;
+    int V, seg;
+    float temperature;
+    int rest;
+    float grad_scale;
+    float* kl;
+    void* dlogits;
+    int64_t ldd;
+    double* row_loss;
+    uint32_t* status;
+};
+
+struct Xch {
+    double s_out, s_in, a;                             // sums outside and inside the list, sum of q z / tau
+    float m_out, m_in;
+};
+
+struct Ctrl {
+    unsigned long long full;
+    Xch x[2][kMaxCluster];
+    double dpart[W][3];
+    float fpart[W];
+    double weight;                                     // mask_t w_i of the row
+};
+constexpr int kCtrlBytes = (sizeof(Ctrl) + 127) & ~127;
+
+// N sums over the CTA in one go; every thread gets them.
+template <int N>
+__device__ __forceinline__ void block_sums(double (&v)[N], double (*part)[3]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) v[n] += __shfl_xor_sync(PODS_FULL_MASK, v[n], d);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int n = 0; n < N; ++n) part[threadIdx.x >> 5][n] = v[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        v[n] = part[0][n];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v[n] += part[w][n];
+    }
+}
+
+// Rollout of packed row r by a whole warp: 32 probes a step.
+__device__ __forceinline__ int64_t find_rollout_warp(const int64_t* cu, int64_t M, int64_t r) {
+    const int lane = threadIdx.x & 31;
+    int64_t lo = 0, hi = M;                            // cu[lo] <= r, answer in [lo, hi)
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 31) / 32;
+        const int64_t at = lo + lane * step;
+        const bool le = at < hi && cu[at] <= r;        // a prefix of the lanes, lane 0 always
+        const int n = __popc(__ballot_sync(PODS_FULL_MASK, le));
+        lo += (int64_t)(n > 0 ? n - 1 : 0) * step;
+        hi = hi < lo + step ? hi : lo + step;
+    }
+    return lo;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads)
+pods_distill_kernel(const DistillArgs a) {
+    using El = Elem<DT>;
+    using raw = typename El::raw;
+    constexpr int E = El::E;
+    extern __shared__ __align__(128) unsigned char smem[];
+    Ctrl& c = *reinterpret_cast<Ctrl*>(smem);
+    uint4* const buf = reinterpret_cast<uint4*>(smem + kCtrlBytes);
+    raw* const elems = reinterpret_cast<raw*>(buf);
+    cg::cluster_group cl = cg::this_cluster();
+    const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) {
+        mbar_init(&c.full, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    cl.sync();                                         // every CTA runs before its shared memory is written
+
+    const double tau_inv = 1.0 / (double)a.temperature;
+    const float cexp = (float)(1.4426950408889634 * tau_inv);
+    const int64_t n_clusters = gridDim.x / CL;
+    uint32_t phase = 0;
+    int parity = 0;
+    for (int64_t t = blockIdx.x / CL; t < a.T; t += n_clusters) {
+        const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+        const bool masked = a.mask != nullptr && a.mask[t] == 0;
+        if (!masked) {
+            if (tid == 0) start_load<DT>(s, a.V, buf, &c.full);
+            if (warp == 1) {
+                const int64_t i = find_rollout_warp(a.cu_seqlens, a.M, a.row0 + t);
+                if (lane == 0) c.weight = a.seq_weight[i];
+            }
+        } else if (tid == 0) {
+            c.weight = 0.0;
+        }
+
+        // ---- the teacher's list: every CTA holds all of it ------------------------------------------------------
+        int id[kPer];
+        float y[kPer];
+        double q[kPer];
+        double Q = 0.0, H = 0.0, L = 0.0;              // sum q, sum q log q, log-normaliser
+        if (!masked) {
+            const int32_t* ids = a.ids + t * a.ldk;
+            const float* vals = a.values + t * a.ldk;
+            bool odd = false;
+            float ymax = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const int j = tid + k * kThreads;
+                id[k] = -1;
+                y[k] = -INFINITY;
+                if (j < a.K) {
+                    const int v = ids[j];
+                    if (v >= 0 && v < a.V) {
+                        id[k] = v;
+                        y[k] = vals[j];
+                        ymax = max_nan(ymax, y[k]);
+                    } else if (v != -1) {
+                        odd = true;
+                    }
+                }
+            }
+            if (a.teacher_lse != nullptr) {
+                L = (double)a.teacher_lse[t];
+            } else {
+                ymax = block_reduce<W>(ymax, c.fpart, MaxNan());
+                const double ref = ymax == -INFINITY ? 0.0 : (double)ymax;     // no entry at all: every q is 0
+                double sum[1] = {0.0};
+#pragma unroll
+                for (int k = 0; k < kPer; ++k)
+                    if (id[k] >= 0) sum[0] += exp(((double)y[k] - ref) * tau_inv);
+                block_sums(sum, c.dpart);
+                L = ref * tau_inv + (sum[0] > 0.0 || sum[0] != sum[0] ? log(sum[0]) : 0.0);
+            }
+            double two[2] = {0.0, 0.0};
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                q[k] = 0.0;
+                if (id[k] >= 0) {
+                    const double lq = (double)y[k] * tau_inv - L;
+                    q[k] = exp(lq);
+                    two[0] += q[k];
+                    if (q[k] != 0.0) two[1] += q[k] * lq;
+                }
+            }
+            block_sums(two, c.dpart);
+            Q = two[0];
+            H = two[1];
+            if (odd && rank == 0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
+            if (!mbar_wait(&c.full, phase, kSpinLimit) && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
+            phase ^= 1u;
+        }
+        __syncthreads();
+        const double w = c.weight;
+
+        // the part of the gradient row that is mine
+        const int id_lo = max(0, s.id0), id_hi = min(a.V, s.id0 + s.cnt * E);
+        raw* const drow = a.dlogits != nullptr ? static_cast<raw*>(a.dlogits) + t * a.ldd : nullptr;
+        const int dlead = (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(raw));
+        // gradient vectors (16-byte boundaries of dlogits) whole inside [id_lo, id_hi): ids v * E - dlead ...
+        const int v_lo = (id_lo + dlead + E - 1) / E, v_hi = max(v_lo, (id_hi + dlead) / E);
+
+        if (w == 0.0) {                                // masked row, or one of an empty rollout
+            if (drow != nullptr && id_lo < id_hi) {
+                const raw zero = 0;
+                uint4* const dvec = reinterpret_cast<uint4*>(drow - dlead);
+                for (int v = v_lo + tid; v < v_hi; v += kThreads) dvec[v] = make_uint4(0u, 0u, 0u, 0u);
+                for (int i = id_lo + tid; i < min(id_hi, v_lo * E - dlead); i += kThreads) drow[i] = zero;
+                for (int i = max(id_lo, v_hi * E - dlead) + tid; i < id_hi; i += kThreads) drow[i] = zero;
+            }
+            if (rank == 0 && tid == 0) {
+                a.kl[t] = 0.0f;
+                a.row_loss[t] = 0.0;
+            }
+            fence_async_proxy();
+            __syncthreads();
+            continue;
+        }
+
+        // ---- the listed logits of my segment leave it -----------------------------------------------------------
+        float z[kPer];
+        int slot[kPer];                                // element of my segment, -1 where the entry is not mine
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int at = id[k] - s.id0;
+            slot[k] = id[k] >= 0 && at >= 0 && at < s.cnt * E ? at : -1;
+            z[k] = slot[k] >= 0 ? El::to_float(elems[slot[k]]) : -INFINITY;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (slot[k] >= 0) elems[slot[k]] = (raw)(tid + k * kThreads);      // one entry of an id stays visible
+        __syncthreads();
+        int twice = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (slot[k] >= 0 && elems[slot[k]] != (raw)(tid + k * kThreads)) twice = 1;
+        twice = __syncthreads_or(twice);
+        double qsum[kPer];                             // teacher mass of the entry's id
+        unsigned first = 0;                            // bit k: the entry speaks for its id
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            qsum[k] = q[k];
+            if (slot[k] >= 0) {
+                elems[slot[k]] = El::kNegInf;
+                first |= 1u << k;
+            }
+        }
+        if (twice) {
+            // an id in several entries: the first speaks for it, with their mass added in list order
+            const int32_t* ids = a.ids + t * a.ldk;
+            const float* vals = a.values + t * a.ldk;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (slot[k] >= 0) {
+                    const int j = tid + k * kThreads;
+                    for (int o = 0; o < a.K; ++o)
+                        if (o != j && ids[o] == id[k]) {
+                            if (o < j) first &= ~(1u << k);
+                            else qsum[k] += exp((double)vals[o] * tau_inv - L);
+                        }
+                }
+        }
+        __syncthreads();
+
+        // ---- maxima and sums -------------------------------------------------------------------------------------
+        float m_out = -INFINITY, m_in = -INFINITY;
+        for (int j = tid; j < s.cnt; j += kThreads) m_out = max_nan(m_out, El::vec_max(buf[j]));
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (first >> k & 1u) m_in = max_nan(m_in, z[k]);
+        Xch mine;
+        mine.m_out = block_reduce<W>(m_out, c.fpart, MaxNan());
+        mine.m_in = block_reduce<W>(m_in, c.fpart, MaxNan());
+        double three[3] = {0.0, 0.0, 0.0};
+        if (fabsf(mine.m_out) < INFINITY) {
+            const float ref = mine.m_out;
+            for (int j = tid; j < s.cnt; j += kThreads) {
+                float x[E];
+                El::unpack(buf[j], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = ex2_approx((x[e] - ref) * cexp);
+#pragma unroll
+                for (int d = E / 2; d > 0; d >>= 1)
+#pragma unroll
+                    for (int e = 0; e < d; ++e) x[e] += x[e + d];
+                three[0] += (double)x[0];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            if (first >> k & 1u)
+                if (mine.m_in > -INFINITY) three[1] += exp(((double)z[k] - (double)mine.m_in) * tau_inv);
+            if (slot[k] >= 0 && q[k] != 0.0) three[2] += q[k] * ((double)z[k] * tau_inv);
+        }
+        block_sums(three, c.dpart);
+        mine.s_out = three[0];
+        mine.s_in = three[1];
+        mine.a = three[2];
+        Xch* const xs = c.x[parity];
+        parity ^= 1;
+        if (tid < CL) *cl.map_shared_rank(xs + rank, tid) = mine;
+        cl.sync();
+
+        // ---- the row's scalars, in every thread ------------------------------------------------------------------
+        float m2 = -INFINITY, m1 = -INFINITY;
+        for (int r = 0; r < CL; ++r) {
+            m2 = max_nan(m2, xs[r].m_out);
+            m1 = max_nan(m1, xs[r].m_in);
+        }
+        const float zmax = max_nan(m1, m2);
+        const bool bad = !(fabsf(zmax) < INFINITY);
+        double S2 = 0.0, S1 = 0.0, A = 0.0;
+        if (!bad)
+            for (int r = 0; r < CL; ++r) {
+                if (xs[r].m_out > -INFINITY) S2 += xs[r].s_out * exp(((double)xs[r].m_out - (double)m2) * tau_inv);
+                if (xs[r].m_in > -INFINITY) S1 += xs[r].s_in * exp(((double)xs[r].m_in - (double)zmax) * tau_inv);
+                A += xs[r].a;
+            }
+        const double part = m2 > -INFINITY ? exp(((double)m2 - (double)zmax) * tau_inv) : 0.0;
+        const double Z = S2 * part + S1;
+        const double r = a.rest && m2 > -INFINITY ? fmax(0.0, 1.0 - Q) : 0.0;
+        const double g = (double)a.grad_scale * w * tau_inv;
+        if (rank == 0 && tid == 0) {
+            double kl = NAN;
+            if (!bad) {
+                const double lz = log(Z);
+                kl = H - A + Q * ((double)zmax * tau_inv + lz);
+                if (r > 0.0) kl += r * (log(r) - (((double)m2 - (double)zmax) * tau_inv + log(S2) - lz));
+            } else {
+                pods_raise(a.status, zmax == -INFINITY ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+            }
+            a.kl[t] = (float)kl;
+            a.row_loss[t] = w * kl;
+        }
+
+        // ---- the gradient ------------------------------------------------------------------------------------------
+        if (drow != nullptr && id_lo < id_hi) {
+            const float ref = m2 > -INFINITY ? m2 : 0.0f;
+            double f = bad ? (double)NAN : (Q + r) * part / Z;
+            if (r > 0.0) f -= r / S2;
+            const float coef = (float)(g * f);
+            uint4* const dvec = reinterpret_cast<uint4*>(drow - dlead);
+            const int shift = v_lo * E - dlead - s.id0 - (v_lo * E - dlead - s.id0) / E * E;
+            if (shift == 0) {
+                const int to_buf = -(dlead + s.id0) / E;                       // gradient vector v is vector v + to_buf here
+                for (int v = v_lo + tid; v < v_hi; v += kThreads)
+                    if (PODS_INDEX_OK(v + to_buf, s.cnt, a.status)) {
+                        float x[E];
+                        El::unpack(buf[v + to_buf], x);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] = coef * ex2_approx((x[e] - ref) * cexp);
+                        dvec[v] = El::pack(x);
+                    }
+            } else {
+                for (int v = v_lo + tid; v < v_hi; v += kThreads) {
+                    const int at = v * E - dlead - s.id0;
+                    if (PODS_INDEX_OK(at, s.cnt * E - E + 1, a.status)) {
+                        float x[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] = coef * ex2_approx((El::to_float(elems[at + e]) - ref) * cexp);
+                        dvec[v] = El::pack(x);
+                    }
+                }
+            }
+            for (int i = id_lo + tid; i < min(id_hi, v_lo * E - dlead); i += kThreads)
+                drow[i] = El::from_float(coef * ex2_approx((El::to_float(elems[i - s.id0]) - ref) * cexp));
+            for (int i = max(id_lo, v_hi * E - dlead) + tid; i < id_hi; i += kThreads)
+                drow[i] = El::from_float(coef * ex2_approx((El::to_float(elems[i - s.id0]) - ref) * cexp));
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (first >> k & 1u) {
+                    const double p = bad ? (double)NAN : exp(((double)z[k] - (double)zmax) * tau_inv) / Z;
+                    drow[id[k]] = El::from_float((float)(g * ((Q + r) * p - qsum[k])));
+                }
+        }
+        fence_async_proxy();                           // the buffer is refilled by bulk copies
+        __syncthreads();
+    }
+    cl.sync();                                         // no CTA leaves while a peer may still write its exchange words
+}
+
+size_t align_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
+
+constexpr size_t kMaxSmem = 227 * 1024;
+constexpr size_t kSegmentBytes = 40 * 1024;
+
+template <int DT>
+int launch_distill(DistillArgs& a, cudaStream_t stream) {
+    const int esize = DT == PODS_DTYPE_F32 ? 4 : 2;
+    int cl = 1;
+    while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
+    a.seg = segment_vectors(a.V, esize, cl);
+    const size_t smem = kCtrlBytes + (size_t)a.seg * 16;
+    if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
+    auto kernel = pods_distill_kernel<DT>;
+    PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (cl > 8) PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cl;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    const int64_t most = 1 << 20;
+    cfg.gridDim = dim3((unsigned)((a.T < most ? a.T : most) * cl), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, kernel, a));
+    return PODS_OK;
+}
+
+}  // namespace
+
+extern "C" size_t pods_distill_chunk_workspace_bytes(int64_t T) {
+    return T < 0 ? 0 : align_up((size_t)T * sizeof(double), 256) + 256;
+}
+
+extern "C" int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* ids,
+                                  const float* values, int64_t ldk, int32_t K, const float* teacher_lse,
+                                  const double* seq_weight, const int64_t* cu_seqlens, int64_t M, int64_t row0,
+                                  const uint8_t* mask, int64_t T, int32_t V, float temperature, uint32_t flags,
+                                  float grad_scale, double* loss_acc, float* kl, void* dlogits, int64_t ldd,
+                                  void* workspace, size_t workspace_bytes, uint32_t* status, void* stream) {
+    if (dtype != PODS_DTYPE_BF16 && dtype != PODS_DTYPE_F16 && dtype != PODS_DTYPE_F32) return PODS_ERR_UNSUPPORTED;
+    const size_t esize = dtype == PODS_DTYPE_F32 ? 4 : 2;
+    if (T < 0 || V < 1 || M < 1 || row0 < 0 || ldl < V || K < 1 || ldk < K) return PODS_ERR_INVALID_ARG;
+    if (V > PODS_MAX_ROW_V || K > PODS_MAX_TOPK || (flags & ~PODS_DISTILL_REST) != 0) return PODS_ERR_UNSUPPORTED;
+    if (!(temperature > 0.0f && temperature < INFINITY) || grad_scale != grad_scale) return PODS_ERR_INVALID_ARG;
+    if ((flags & PODS_DISTILL_REST) && teacher_lse == nullptr) return PODS_ERR_INVALID_ARG;
+    if (dlogits != nullptr && (ldd < V || !pods_aligned(dlogits, esize) || (dlogits == logits && ldd != ldl)))
+        return PODS_ERR_INVALID_ARG;
+    if (T == 0) return PODS_OK;
+    if (logits == nullptr || ids == nullptr || values == nullptr || seq_weight == nullptr || cu_seqlens == nullptr ||
+        loss_acc == nullptr || kl == nullptr)
+        return PODS_ERR_INVALID_ARG;
+    if (!pods_aligned(logits, esize) || !pods_aligned(loss_acc, 8)) return PODS_ERR_INVALID_ARG;
+    if (workspace == nullptr || workspace_bytes < pods_distill_chunk_workspace_bytes(T) || !pods_aligned(workspace, 16))
+        return PODS_ERR_WORKSPACE;
+    DistillArgs a = {};
+    a.logits = logits;
+    a.ldl = ldl;
+    a.ids = ids;
+    a.values = values;
+    a.ldk = ldk;
+    a.K = K;
+    a.teacher_lse = teacher_lse;
+    a.seq_weight = seq_weight;
+    a.cu_seqlens = cu_seqlens;
+    a.M = M;
+    a.row0 = row0;
+    a.mask = mask;
+    a.T = T;
+    a.V = V;
+    a.temperature = temperature;
+    a.rest = (flags & PODS_DISTILL_REST) ? 1 : 0;
+    a.grad_scale = grad_scale;
+    a.kl = kl;
+    a.dlogits = dlogits;
+    a.ldd = ldd;
+    a.row_loss = static_cast<double*>(workspace);
+    a.status = status;
+    cudaStream_t s = pods_stream(stream);
+    const int rc = dtype == PODS_DTYPE_BF16  ? launch_distill<PODS_DTYPE_BF16>(a, s)
+                   : dtype == PODS_DTYPE_F16 ? launch_distill<PODS_DTYPE_F16>(a, s)
+                                             : launch_distill<PODS_DTYPE_F32>(a, s);
+    if (rc != PODS_OK) return rc;
+    return pods_loss::launch_loss_reduce(a.row_loss, T, loss_acc, s);
+}

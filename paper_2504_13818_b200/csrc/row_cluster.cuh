@@ -1,0 +1,263 @@
+// A row of logits held by a thread-block cluster: helpers shared by the sampler, the top-K lists and the distillation
+// objective.
+//
+// CTA r of the cluster holds the r-th segment of the row in shared memory, so that the row crosses HBM once however often
+// it is looked at.  Rows may start at any element: the row is cut at the 16-byte boundaries of global memory.  Whole
+// vectors inside the row arrive by bulk asynchronous copies, the at most two vectors that the row covers only in part by
+// element loads, and every slot that is no logit of the row holds -inf, which adds nothing to a maximum or a sum of
+// exponentials.  Element i of CTA r's segment is the logit of id  r * seg * E + i - lead,  where E is the number of
+// elements of a vector and lead the number of elements between the boundary and the row's start.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cooperative_groups.h>
+#include <math.h>
+
+#include "pods_common.cuh"
+
+namespace pods_row {
+
+namespace cg = cooperative_groups;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kSpinLimit = 1u << 24;     // polls of the load barrier before giving up
+constexpr uint32_t kSuspendNs = 1000;         // upper bound of one poll
+constexpr int kMaxCluster = 16;
+
+template <int DT> struct Elem;
+
+template <> struct Elem<PODS_DTYPE_BF16> {
+    using raw = uint16_t;
+    static constexpr int E = 8;
+    static constexpr int kKeyBits = 16;
+    static constexpr raw kNegInf = 0xff80u;
+    __device__ static __forceinline__ float to_float(raw r) { return __uint_as_float((uint32_t)r << 16); }
+    __device__ static __forceinline__ raw from_float(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+    __device__ static __forceinline__ void unpack(const uint4& q, float (&x)[E]) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[E]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(x[2 * i + 1]), "f"(x[2 * i]));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // the largest element, NaN if one of them is
+    __device__ static __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static __forceinline__ float vec_max(const uint4& q) {
+        const uint32_t m = max2(max2(q.x, q.y), max2(q.z, q.w));
+        return to_float((raw)max2(m, m >> 16));
+    }
+    // keys whose unsigned order is the order of the values (-0 == +0)
+    __device__ static __forceinline__ uint32_t to_key(float v) {
+        const uint32_t u = __float_as_uint(v + 0.0f) >> 16;
+        return (u & 0x8000u) ? (~u & 0xffffu) : (u | 0x8000u);
+    }
+    __device__ static __forceinline__ float from_key(uint32_t k) {
+        return __uint_as_float(((k & 0x8000u) ? (k & 0x7fffu) : (~k & 0xffffu)) << 16);
+    }
+};
+
+template <> struct Elem<PODS_DTYPE_F16> {
+    using raw = uint16_t;
+    static constexpr int E = 8;
+    static constexpr int kKeyBits = 16;
+    static constexpr raw kNegInf = 0xfc00u;
+    __device__ static __forceinline__ float to_float(raw r) { return __half2float(__ushort_as_half(r)); }
+    __device__ static __forceinline__ raw from_float(float v) { return __half_as_ushort(__float2half_rn(v)); }
+    __device__ static __forceinline__ void unpack(const uint4& q, float (&x)[E]) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            x[2 * i] = f.x;
+            x[2 * i + 1] = f.y;
+        }
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[E]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ static __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static __forceinline__ float vec_max(const uint4& q) {
+        const uint32_t m = max2(max2(q.x, q.y), max2(q.z, q.w));
+        return to_float((raw)max2(m, m >> 16));
+    }
+    __device__ static __forceinline__ uint32_t to_key(float v) {
+        const uint32_t u = from_float(v + 0.0f);
+        return (u & 0x8000u) ? (~u & 0xffffu) : (u | 0x8000u);
+    }
+    __device__ static __forceinline__ float from_key(uint32_t k) {
+        return to_float((raw)((k & 0x8000u) ? (k & 0x7fffu) : (~k & 0xffffu)));
+    }
+};
+
+template <> struct Elem<PODS_DTYPE_F32> {
+    using raw = uint32_t;
+    static constexpr int E = 4;
+    static constexpr int kKeyBits = 32;
+    static constexpr raw kNegInf = 0xff800000u;
+    __device__ static __forceinline__ float to_float(raw r) { return __uint_as_float(r); }
+    __device__ static __forceinline__ raw from_float(float v) { return __float_as_uint(v); }
+    __device__ static __forceinline__ void unpack(const uint4& q, float (&x)[E]) {
+        x[0] = __uint_as_float(q.x);
+        x[1] = __uint_as_float(q.y);
+        x[2] = __uint_as_float(q.z);
+        x[3] = __uint_as_float(q.w);
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[E]) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+    __device__ static __forceinline__ float max_nan(float a, float b) {
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+        return r;
+    }
+    __device__ static __forceinline__ float vec_max(const uint4& q) {
+        return max_nan(max_nan(__uint_as_float(q.x), __uint_as_float(q.y)), max_nan(__uint_as_float(q.z), __uint_as_float(q.w)));
+    }
+    __device__ static __forceinline__ uint32_t to_key(float v) {
+        const uint32_t u = __float_as_uint(v + 0.0f);
+        return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    }
+    __device__ static __forceinline__ float from_key(uint32_t k) {
+        return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
+    }
+};
+
+// value -> 32-bit key in value order, for entries that leave their row (lists)
+__device__ __forceinline__ uint32_t order32(float v) { return Elem<PODS_DTYPE_F32>::to_key(v); }
+__device__ __forceinline__ float unorder32(uint32_t k) { return Elem<PODS_DTYPE_F32>::from_key(k); }
+
+__device__ __forceinline__ float max_nan(float a, float b) { return Elem<PODS_DTYPE_F32>::max_nan(a, b); }
+
+__device__ __forceinline__ float ex2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(unsigned long long* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t parity, uint32_t limit) {
+    for (uint32_t i = 0; i < limit; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+// Global -> this CTA's shared memory, completion counted on an mbarrier.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// This CTA's segment of a row.
+struct Segment {
+    int cnt;          // vectors of the row in the segment
+    int id0;          // id of the segment's element 0 (negative where the row starts inside the first vector)
+    int full0, full1; // local vectors [full0, full1) lie in the row whole
+    const uint4* src; // global address of local vector 0
+};
+
+template <int DT>
+__device__ __forceinline__ Segment make_segment(const void* base, int64_t pitch, int64_t t, int V, int rank, int seg) {
+    using El = Elem<DT>;
+    const typename El::raw* row = static_cast<const typename El::raw*>(base) + t * pitch;
+    const int lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(typename El::raw));
+    const uint4* aligned = reinterpret_cast<const uint4*>(row - lead);
+    const int nvec = (lead + V + El::E - 1) / El::E;
+    const int j0 = rank * seg;
+    Segment s;
+    s.cnt = max(0, min(seg, nvec - j0));
+    s.id0 = j0 * El::E - lead;
+    s.full0 = min(s.cnt, max(0, (lead ? 1 : 0) - j0));
+    s.full1 = max(s.full0, min(s.cnt, (lead + V) / El::E - j0));
+    s.src = aligned + j0;
+    return s;
+}
+
+// Starts the segment's copy (one thread) and fills the vectors at the row's two ends (that thread too: at most two).
+// The waiters see both after mbar_wait on `bar` and a CTA barrier.
+template <int DT>
+__device__ __forceinline__ void start_load(const Segment& s, int V, uint4* buf, unsigned long long* bar) {
+    using El = Elem<DT>;
+    constexpr int kPiece = 512;
+    const int n = s.full1 - s.full0;
+    mbar_expect_tx(bar, (uint32_t)n * 16u);
+    for (int v = 0; v < n; v += kPiece)
+        bulk_load(buf + s.full0 + v, s.src + s.full0 + v, (uint32_t)min(kPiece, n - v) * 16u, bar);
+    for (int j = 0; j < s.cnt; ++j) {
+        if (j == s.full0) j = s.full1;
+        if (j >= s.cnt) break;
+        typename El::raw* dst = reinterpret_cast<typename El::raw*>(buf + j);
+        const typename El::raw* src = reinterpret_cast<const typename El::raw*>(s.src + j);
+        for (int e = 0; e < El::E; ++e) {
+            const int id = s.id0 + j * El::E + e;
+            dst[e] = (id >= 0 && id < V) ? src[e] : El::kNegInf;
+        }
+    }
+}
+
+// ---- reductions over a CTA of W warps; `part` is scratch of W entries, every thread gets the result -------------------
+template <int W, typename T, typename Op>
+__device__ __forceinline__ T block_reduce(T v, T* part, Op op) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(PODS_FULL_MASK, v, d));
+    __syncthreads();                                   // an earlier use of `part` is over
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    T r = part[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) r = op(r, part[w]);
+    return r;
+}
+
+struct Plus {
+    template <typename T> __device__ T operator()(T a, T b) const { return a + b; }
+};
+struct MaxNan {
+    __device__ float operator()(float a, float b) const { return max_nan(a, b); }
+};
+struct Min {
+    template <typename T> __device__ T operator()(T a, T b) const { return a < b ? a : b; }
+};
+
+// Host: vectors per CTA for rows of V elements of `esize` bytes over `cl` CTAs (whole 128-byte lines).
+static inline int segment_vectors(int64_t V, int esize, int cl) {
+    const int64_t e = 16 / esize, nvec = (V + 2 * (e - 1)) / e + 1;
+    return (int)(((nvec + cl - 1) / cl + 7) & ~7ll);
+}
+
+}  // namespace pods_row

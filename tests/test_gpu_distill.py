@@ -1,0 +1,292 @@
+"""pods_distill_chunk against the fp64 oracle.
+
+Sums of exponentials carry SUM_RTOL (see test_gpu_sample.py).  kl = H - A + Q log Z + r (log r - log S2 + log Z): the two
+sums enter through logarithms with factors Q, r and r, then one rounding to fp32.  A gradient entry is a sum of terms (the
+oracle's `terms` is the sum of their absolute values): each carries SUM_RTOL, the exponent's own error of 9e-8 per unit of
+|z - max| / tau ((2^-24 + 2^-25), natural units), 2^-22.5 of the exponential and three fp32 roundings; the entry is then
+rounded to the logits' type, half a step: eps / 2 of the value, or half the smallest subnormal."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import rollout
+from paper_2504_13818_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+SUM_RTOL = 1.6e-6
+HALF_SUBNORMAL = {"bf16": 2.0 ** -127, "fp16": 2.0 ** -25, "fp32": 2.0 ** -126}   # fp32, bf16: the exponential flushes below 2^-126
+
+
+def make(T, V, K, dtype, seed, pad=0, offset=0, M=3, holes=False, sharp=False):
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn((T, V), generator=g) * 3.0
+    if sharp:
+        z[:, 0] += 60.0
+    if holes and V > 2:
+        z[torch.rand((T, V), generator=g) < 0.5] = -np.inf
+        z[:, V // 2] = 0.25
+    flat = torch.full((offset + T * (V + pad) + 16,), 6.0e4, dtype=DT[dtype]).cuda()
+    rows = flat[offset:offset + T * (V + pad)].view(T, V + pad)[:, :V]
+    rows.copy_(z.to(DT[dtype]))
+    teacher = torch.randn((T, V), generator=g) * 2.0 + torch.where(torch.isfinite(z), z, torch.zeros(())) * 0.7
+    values, ids = teacher.topk(K, dim=1)
+    cuts = np.linspace(0, T, M + 1).astype(np.int64)
+    mask = (torch.rand(T, generator=g) < 0.8).to(torch.uint8)
+    return dict(z=rows, teacher=teacher, ids=ids.to(torch.int32).cuda(), values=values.cuda(), cu=torch.from_numpy(cuts).cuda(),
+                mask=mask.cuda(), dtype=dtype)
+
+
+def run(b, tau=1.0, rest=False, lse=True, mask=True, grad_scale=1.0, want_grad=True, dlogits=None, expect_status=0):
+    L = torch.logsumexp(b["teacher"].double() / np.float32(tau), 1).float().cuda() if lse else None
+    m = b["mask"] if mask else None
+    weight = binding.grpo_seq_weights(m, b["cu"])
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    status = binding.new_status()
+    kl, dl = binding.pods_distill_chunk(b["z"], b["ids"], b["values"], L, weight, b["cu"], 0, m, acc, temperature=tau, rest=rest,
+                                        want_grad=want_grad, grad_scale=grad_scale, dlogits=dlogits, status=status)
+    torch.cuda.synchronize()
+    assert binding.read_status(status) == expect_status
+    return dict(kl=kl.cpu().numpy().astype(np.float64), dl=None if dl is None else dl, loss=float(acc.item()), L=L,
+                weight=weight.cpu().numpy(), mask=np.ones(b["z"].shape[0], np.uint8) if m is None else m.cpu().numpy())
+
+
+def check(b, got, tau=1.0, rest=False, grad_scale=1.0, z=None):
+    z = (b["z"] if z is None else z).double().cpu().numpy()
+    T = z.shape[0]
+    ids, values = b["ids"].cpu().numpy(), b["values"].cpu().numpy()
+    L = None if got["L"] is None else got["L"].cpu().numpy().astype(np.float64)
+    row = oracle.seq_of_rows(b["cu"].cpu().numpy())
+    tau = float(np.float32(tau))
+    dl = None if got["dl"] is None else got["dl"].double().cpu().numpy()
+    half = torch.finfo(DT[b["dtype"]]).eps / 2
+    loss, loss_tol = 0.0, 1e-12
+    for t in range(T):
+        w = got["weight"][row[t]] * (got["mask"][t] != 0)
+        if w == 0:
+            assert got["kl"][t] == 0 and (dl is None or (dl[t] == 0).all())
+            continue
+        want = rollout.distill_row(z[t], ids[t], values[t], None if L is None else L[t], tau, rest)
+        if not np.isfinite(want["kl"]):
+            assert np.isnan(got["kl"][t]) == np.isnan(want["kl"]) and (np.isnan(want["kl"]) or got["kl"][t] == want["kl"])
+            loss = np.nan
+        else:
+            tol = (want["Q"] + 2 * want["r"]) * SUM_RTOL + 1e-11          # 1e-11: fp64 sums of terms of up to 1e3
+            assert abs(got["kl"][t] - want["kl"]) <= tol + 2.0 ** -24 * abs(want["kl"]), (t, got["kl"][t], want["kl"], tol)
+            loss += w * want["kl"]
+            loss_tol += w * tol
+        if dl is not None:
+            if np.isnan(want["kl"]):
+                assert np.isnan(dl[t]).all()
+                continue
+            g = grad_scale * w / tau
+            depth = np.where(np.isfinite(z[t]), z[t].max() - z[t], 0.0) / tau
+            err = np.abs(dl[t] - g * want["grad"])
+            bar = g * want["terms"] * (SUM_RTOL + 9e-8 * depth + 2.0 ** -22.5 + 3 * 2.0 ** -24)
+            bar = bar * (1 + half) + half * np.abs(g * want["grad"]) + HALF_SUBNORMAL[b["dtype"]] * max(1.0, g)
+            assert (err <= bar).all(), (t, int(np.argmax(err - bar)), float((err - bar).max()))
+    if np.isfinite(loss):
+        assert abs(got["loss"] - loss) <= loss_tol
+    else:
+        assert not np.isfinite(got["loss"])
+
+
+MODES = [dict(rest=False, lse=False), dict(rest=False, lse=True), dict(rest=True, lse=True)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("V,K,pad,offset", [(1, 1, 0, 0), (7, 3, 2, 3), (9, 9, 0, 0), (255, 17, 1, 5), (1000, 300, 8, 0), (5003, 64, 0, 7), (32000, 1024, 0, 0)])
+def test_lengths_alignments_and_modes(dtype, V, K, pad, offset):
+    b = make(10, V, K, dtype, seed=V + K, pad=pad, offset=offset)
+    for i, mode in enumerate(MODES):
+        for tau in (1.0, 2.5, 0.4):
+            got = run(b, tau=tau, mask=i != 1, grad_scale=[1.0, 0.5, 64.0][i], **mode)
+            check(b, got, tau=tau, rest=mode["rest"], grad_scale=[1.0, 0.5, 64.0][i])
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 151936), ("fp32", 151936), ("fp16", 50257), ("bf16", 300001), ("fp32", 524288)])
+def test_long_rows(dtype, V):
+    b = make(5, V, 50, dtype, seed=V)
+    for mode in MODES:
+        check(b, run(b, tau=1.3, **mode), tau=1.3, rest=mode["rest"])
+
+
+@pytest.mark.parametrize("V", [9, 1000, 50257])
+def test_holes_and_sure_policies(V):
+    """-inf logits inside and outside the list (kl +inf, gradient finite); a policy with all but e^-60 on one id, where 1 - s
+    as a difference would be zero."""
+    b = make(6, V, 5, "fp32", seed=V, holes=True)
+    for mode in MODES:
+        check(b, run(b, **mode), rest=mode["rest"])
+    b = make(6, V, 5, "fp32", seed=V, sharp=True)
+    b["ids"][:, 4] = 0
+    b["ids"][:, :4] = torch.arange(1, 5, dtype=torch.int32)
+    for mode in MODES:
+        check(b, run(b, **mode), rest=mode["rest"])
+
+
+def test_ids_twice_unused_and_out_of_range():
+    b = make(8, 1000, 40, "fp32", seed=1)
+    for mode in MODES:
+        b["ids"][1, 7] = b["ids"][1, 30]
+        b["ids"][2, :] = 5
+        b["ids"][3, 10:] = -1
+        b["ids"][4, :] = -1
+        check(b, run(b, mask=False, **mode), rest=mode["rest"])
+        b["ids"][5, 0] = 1000
+        b["ids"][6, 3] = -7
+        check(b, run(b, mask=False, expect_status=binding.STATUS_TOKEN_RANGE, **mode), rest=mode["rest"])
+        b["ids"][5, 0], b["ids"][6, 3] = 1, 1
+
+
+def test_list_holding_the_whole_row():
+    b = make(4, 64, 64, "fp32", seed=2)
+    for mode in MODES:
+        check(b, run(b, mask=False, **mode), rest=mode["rest"])
+
+
+def test_rows_without_a_distribution():
+    b = make(6, 1000, 8, "bf16", seed=3)
+    b["mask"][:] = 1
+    b["z"][0] = -np.inf
+    b["z"][2, 999] = np.nan
+    b["z"][4, int(b["ids"][4, 0])] = np.inf
+    for mode in MODES:
+        check(b, run(b, expect_status=binding.STATUS_EMPTY_ROW | binding.STATUS_NONFINITE_LOGIT, **mode), rest=mode["rest"])
+    b["mask"][::2] = 0                                      # under the mask none of it counts
+    for mode in MODES:
+        got = run(b, **mode)
+        check(b, got, rest=mode["rest"])
+        assert np.isfinite(got["loss"])
+
+
+@pytest.mark.parametrize("pad", [0, 3, 8])
+def test_in_place_loss_alone_and_a_pitched_gradient(pad):
+    b = make(9, 5003, 20, "bf16", seed=4, pad=pad)
+    got = run(b, rest=True)
+    alone = run(b, rest=True, want_grad=False)
+    assert alone["dl"] is None and np.array_equal(alone["kl"], got["kl"]) and alone["loss"] == got["loss"]
+    wide = torch.full((9, 5003 + 13), 5.0, dtype=torch.bfloat16, device="cuda")
+    pitched = run(b, rest=True, dlogits=wide[:, 4:5007])
+    assert torch.equal(pitched["dl"], got["dl"]) and (wide[:, :4] == 5.0).all() and (wide[:, 5007:] == 5.0).all()
+    before = b["z"].clone()
+    behind = b["z"].as_strided((9, pad), b["z"].stride(), b["z"].storage_offset() + 5003).clone() if pad else None
+    inplace = run(b, rest=True, dlogits=b["z"])
+    assert torch.equal(b["z"], got["dl"]) and np.array_equal(inplace["kl"], got["kl"])
+    if pad:
+        assert torch.equal(b["z"].as_strided((9, pad), b["z"].stride(), b["z"].storage_offset() + 5003), behind)
+    check(b, got, rest=True, z=before)
+
+
+def test_chunks_add_up_and_weights_follow_the_rollouts():
+    b = make(40, 1000, 12, "bf16", seed=5, M=7)
+    whole = run(b, rest=True)
+    weight = binding.grpo_seq_weights(b["mask"], b["cu"])
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    for lo, hi in ((0, 13), (13, 14), (14, 40)):
+        kl, dl = binding.pods_distill_chunk(b["z"][lo:hi], b["ids"][lo:hi], b["values"][lo:hi], whole["L"][lo:hi], weight, b["cu"],
+                                            lo, b["mask"][lo:hi], acc, rest=True)
+        assert np.array_equal(kl.cpu().numpy(), whole["kl"][lo:hi].astype(np.float32)) and torch.equal(dl, whole["dl"][lo:hi])
+    assert abs(float(acc.item()) - whole["loss"]) <= 1e-12 * max(1.0, abs(whole["loss"]))
+
+
+def test_many_rollouts_find_their_weights():
+    """5000 rollouts of 0 to 3 tokens: the row-to-rollout search over more than two levels of 32."""
+    rng = np.random.default_rng(6)
+    lengths = rng.integers(0, 4, 5000)
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int64)
+    T = int(cu[-1])
+    g = torch.Generator().manual_seed(6)
+    z = torch.randn((T, 16), generator=g).cuda()
+    values, ids = torch.randn((T, 16), generator=g).topk(3, dim=1)
+    weight = torch.arange(1, 5001, dtype=torch.float64).cuda()
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    kl, _ = binding.pods_distill_chunk(z, ids.to(torch.int32).cuda(), values.cuda(), None, weight, torch.from_numpy(cu).cuda(), 0, None, acc)
+    want = (weight.cpu().numpy()[oracle.seq_of_rows(cu)] * kl.double().cpu().numpy()).sum()
+    assert abs(float(acc.item()) - want) <= 2.0 ** -23 * abs(want)      # kl is rounded to fp32, the sum is not
+
+
+def test_gradient_agrees_with_differences_of_the_loss():
+    V = 50
+    b = make(4, V, 6, "fp32", seed=7)
+    got = run(b, tau=1.5, rest=True, mask=False)
+    z0 = b["z"].clone()
+    h = 0.05
+    for t, v in ((0, int(b["ids"][0, 0])), (1, int(b["ids"][1, 5])), (2, 17), (3, 33)):
+        losses = []
+        for step in (h, -h):
+            b["z"].copy_(z0)
+            b["z"][t, v] += step
+            losses.append(run(b, tau=1.5, rest=True, mask=False)["loss"])
+        slope = (losses[0] - losses[1]) / (2 * h)
+        w = got["weight"][oracle.seq_of_rows(b["cu"].cpu().numpy())[t]]
+        # h^2 / 6 of a third derivative below 2 w, and the two losses' own errors of 4e-6 w over 2 h
+        assert abs(slope - float(got["dl"][t, v])) <= w * (2 * h * h / 6 + 4 * SUM_RTOL / (2 * h) * 2 + 1e-6)
+    b["z"].copy_(z0)
+
+
+def test_another_stream_a_captured_graph_and_the_same_bits_twice():
+    b = make(30, 50257, 33, "bf16", seed=8, M=4)
+    want = run(b, rest=True)
+    again = run(b, rest=True)
+    assert torch.equal(want["dl"], again["dl"]) and np.array_equal(want["kl"], again["kl"]) and want["loss"] == again["loss"]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = run(b, rest=True)
+    assert torch.equal(want["dl"], other["dl"]) and want["loss"] == other["loss"]
+    weight = binding.grpo_seq_weights(b["mask"], b["cu"])
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    kl, dl = torch.zeros(30, device="cuda"), torch.zeros_like(want["dl"])
+    ws = torch.empty(binding.pods_distill_chunk_workspace_bytes(30), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        acc.zero_()
+        binding.pods_distill_chunk(b["z"], b["ids"], b["values"], want["L"], weight, b["cu"], 0, b["mask"], acc, kl=kl, dlogits=dl,
+                                   workspace=ws, rest=True)
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dl, want["dl"]) and float(acc.item()) == want["loss"]
+
+
+def test_rollout_teacher_list_distillation_and_objective_in_one_run():
+    """As they are used: tokens drawn from the policy with their log-probs, the teacher's lists, the divergence's gradient and
+    the policy objective on the drawn tokens, whose ratio is 1 on the first step."""
+    T, V, K, M = 48, 32000, 32, 4
+    g = torch.Generator().manual_seed(9)
+    policy = (torch.randn((T, V), generator=g) * 2.5).to(torch.bfloat16).cuda()
+    teacher = (policy.float() + torch.randn((T, V), generator=g).cuda()).to(torch.bfloat16)
+    u = torch.rand(T, generator=g).cuda()
+    status = binding.new_status()
+    tokens, old_logp, _ = binding.pods_sample(policy, u, status=status)
+    ids, values, lse = binding.pods_topk(teacher, K, status=status)
+    cu = torch.arange(0, T + 1, T // M, dtype=torch.int64).cuda()
+    weight = binding.grpo_seq_weights(None, cu)
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    kl, dl = binding.pods_distill_chunk(policy, ids, values, lse, weight, cu, 0, None, acc, rest=True, status=status)
+    adv = torch.tensor([1.0, -1.0, 0.5, -0.5]).cuda()
+    loss, logp, dpolicy = binding.grpo_loss_fwd_bwd(policy, tokens, old_logp, None, adv, None, 0.2, 0.0, cu, status=status)
+    torch.cuda.synchronize()
+    assert binding.read_status(status) == 0
+    assert (logp - old_logp).abs().max() <= 1e-5             # both are log softmax(policy)[token], to 2 sums and 2 roundings at 16
+    z = policy.double().cpu().numpy()
+    teacher_rows = teacher.double().cpu().numpy()
+    for t in range(0, T, 7):
+        assert int(tokens[t]) == rollout.sample_row(z[t], float(u[t]))["token"]
+        want = rollout.topk_row(teacher_rows[t], K)
+        assert np.array_equal(ids[t].cpu().numpy(), want["ids"])
+        ref = rollout.distill_row(z[t], want["ids"], want["values"], float(lse[t]), rest=True)
+        assert abs(float(kl[t]) - ref["kl"]) <= 3 * SUM_RTOL + 2.0 ** -24 * ref["kl"]
+    assert torch.isfinite(dpolicy.float()).all() and torch.isfinite(dl.float()).all() and float(acc.item()) > 0
+
+
+def test_empty_chunk():
+    z = torch.zeros((0, 100), device="cuda")
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    kl, dl = binding.pods_distill_chunk(z, torch.zeros((0, 4), dtype=torch.int32, device="cuda"), torch.zeros((0, 4), device="cuda"), None,
+                                        torch.ones(1, dtype=torch.float64, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda"),
+                                        0, None, acc)
+    assert kl.numel() == 0 and dl.shape == (0, 100) and float(acc.item()) == 0.0
