@@ -462,10 +462,13 @@ def _typed_rows(t, name):
 
 def _on_current_device(*tensors):
     """The library launches on the current device's current stream: tensors of another device are refused."""
+    here = None
     for t in tensors:
-        if t is not None:
-            _require(not t.is_cuda or t.device.index == torch.cuda.current_device(),
-                     "tensors must be on the current CUDA device, got %s" % t.device)
+        if t is not None and t.is_cuda:
+            if here is None:
+                here = torch.cuda.current_device()
+            if t.get_device() != here:
+                raise PodsError("tensors must be on the current CUDA device (cuda:%d), got %s" % (here, t.device))
 
 
 def _setting(x, T, name):

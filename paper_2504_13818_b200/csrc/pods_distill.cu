@@ -21,7 +21,6 @@ namespace {
 
 constexpr int W = 8;
 constexpr int kThreads = W * 32;
-constexpr int kPer = PODS_MAX_TOPK / kThreads;         // list entries a thread holds at most
 
 struct DistillArgs {
     const void* logits;
@@ -58,6 +57,9 @@ struct Ctrl {
     double dpart[W][3];
     float fpart[W];
     double weight;                                     // mask_t w_i of the row
+    double coef, p_scale, g;                           // of the row's gradient, see below
+    float m2, zmax;
+    int bad;
 };
 constexpr int kCtrlBytes = (sizeof(Ctrl) + 127) & ~127;
 
@@ -96,8 +98,9 @@ __device__ __forceinline__ int64_t find_rollout_warp(const int64_t* cu, int64_t 
     return lo;
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads)
+// KP: list entries a thread holds at most, so K <= KP * kThreads.
+template <int DT, int KP>
+__global__ void __launch_bounds__(kThreads, KP == 1 ? 4 : 2)
 pods_distill_kernel(const DistillArgs a) {
     using El = Elem<DT>;
     using raw = typename El::raw;
@@ -114,7 +117,7 @@ pods_distill_kernel(const DistillArgs a) {
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    cl.sync();                                         // every CTA runs before its shared memory is written
+    bool started = false;
 
     const double tau_inv = 1.0 / (double)a.temperature;
     const float cexp = (float)(1.4426950408889634 * tau_inv);
@@ -126,6 +129,7 @@ pods_distill_kernel(const DistillArgs a) {
         const bool masked = a.mask != nullptr && a.mask[t] == 0;
         if (!masked) {
             if (tid == 0) start_load<DT>(s, a.V, buf, &c.full);
+            if (!started) { cl.sync(); started = true; }       // every CTA runs before its shared memory is written
             if (warp == 1) {
                 const int64_t i = find_rollout_warp(a.cu_seqlens, a.M, a.row0 + t);
                 if (lane == 0) c.weight = a.seq_weight[i];
@@ -135,9 +139,9 @@ pods_distill_kernel(const DistillArgs a) {
         }
 
         // ---- the teacher's list: every CTA holds all of it ------------------------------------------------------
-        int id[kPer];
-        float y[kPer];
-        double q[kPer];
+        int id[KP];
+        float y[KP];
+        double q[KP];
         double Q = 0.0, H = 0.0, L = 0.0;              // sum q, sum q log q, log-normaliser
         if (!masked) {
             const int32_t* ids = a.ids + t * a.ldk;
@@ -145,7 +149,7 @@ pods_distill_kernel(const DistillArgs a) {
             bool odd = false;
             float ymax = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) {
+            for (int k = 0; k < KP; ++k) {
                 const int j = tid + k * kThreads;
                 id[k] = -1;
                 y[k] = -INFINITY;
@@ -167,14 +171,14 @@ pods_distill_kernel(const DistillArgs a) {
                 const double ref = ymax == -INFINITY ? 0.0 : (double)ymax;     // no entry at all: every q is 0
                 double sum[1] = {0.0};
 #pragma unroll
-                for (int k = 0; k < kPer; ++k)
+                for (int k = 0; k < KP; ++k)
                     if (id[k] >= 0) sum[0] += exp(((double)y[k] - ref) * tau_inv);
                 block_sums(sum, c.dpart);
                 L = ref * tau_inv + (sum[0] > 0.0 || sum[0] != sum[0] ? log(sum[0]) : 0.0);
             }
             double two[2] = {0.0, 0.0};
 #pragma unroll
-            for (int k = 0; k < kPer; ++k) {
+            for (int k = 0; k < KP; ++k) {
                 q[k] = 0.0;
                 if (id[k] >= 0) {
                     const double lq = (double)y[k] * tau_inv - L;
@@ -218,28 +222,28 @@ pods_distill_kernel(const DistillArgs a) {
         }
 
         // ---- the listed logits of my segment leave it -----------------------------------------------------------
-        float z[kPer];
-        int slot[kPer];                                // element of my segment, -1 where the entry is not mine
+        float z[KP];
+        int slot[KP];                                // element of my segment, -1 where the entry is not mine
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
+        for (int k = 0; k < KP; ++k) {
             const int at = id[k] - s.id0;
             slot[k] = id[k] >= 0 && at >= 0 && at < s.cnt * E ? at : -1;
             z[k] = slot[k] >= 0 ? El::to_float(elems[slot[k]]) : -INFINITY;
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kPer; ++k)
+        for (int k = 0; k < KP; ++k)
             if (slot[k] >= 0) elems[slot[k]] = (raw)(tid + k * kThreads);      // one entry of an id stays visible
         __syncthreads();
         int twice = 0;
 #pragma unroll
-        for (int k = 0; k < kPer; ++k)
+        for (int k = 0; k < KP; ++k)
             if (slot[k] >= 0 && elems[slot[k]] != (raw)(tid + k * kThreads)) twice = 1;
         twice = __syncthreads_or(twice);
-        double qsum[kPer];                             // teacher mass of the entry's id
+        double qsum[KP];                             // teacher mass of the entry's id
         unsigned first = 0;                            // bit k: the entry speaks for its id
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
+        for (int k = 0; k < KP; ++k) {
             qsum[k] = q[k];
             if (slot[k] >= 0) {
                 elems[slot[k]] = El::kNegInf;
@@ -251,7 +255,7 @@ pods_distill_kernel(const DistillArgs a) {
             const int32_t* ids = a.ids + t * a.ldk;
             const float* vals = a.values + t * a.ldk;
 #pragma unroll
-            for (int k = 0; k < kPer; ++k)
+            for (int k = 0; k < KP; ++k)
                 if (slot[k] >= 0) {
                     const int j = tid + k * kThreads;
                     for (int o = 0; o < a.K; ++o)
@@ -267,28 +271,23 @@ pods_distill_kernel(const DistillArgs a) {
         float m_out = -INFINITY, m_in = -INFINITY;
         for (int j = tid; j < s.cnt; j += kThreads) m_out = max_nan(m_out, El::vec_max(buf[j]));
 #pragma unroll
-        for (int k = 0; k < kPer; ++k)
+        for (int k = 0; k < KP; ++k)
             if (first >> k & 1u) m_in = max_nan(m_in, z[k]);
-        Xch mine;
+        Xch mine;                                      // the last thing a row asks of its peers is the exchange's barrier
         mine.m_out = block_reduce<W>(m_out, c.fpart, MaxNan());
         mine.m_in = block_reduce<W>(m_in, c.fpart, MaxNan());
         double three[3] = {0.0, 0.0, 0.0};
-        if (fabsf(mine.m_out) < INFINITY) {
-            const float ref = mine.m_out;
+        {
+            const ExpRef ref(mine.m_out, cexp);
             for (int j = tid; j < s.cnt; j += kThreads) {
                 float x[E];
                 El::unpack(buf[j], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = ex2_approx((x[e] - ref) * cexp);
-#pragma unroll
-                for (int d = E / 2; d > 0; d >>= 1)
-#pragma unroll
-                    for (int e = 0; e < d; ++e) x[e] += x[e + d];
-                three[0] += (double)x[0];
+                ref.exps(x);
+                three[0] += (double)vec_add(x);
             }
         }
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
+        for (int k = 0; k < KP; ++k) {
             if (first >> k & 1u)
                 if (mine.m_in > -INFINITY) three[1] += exp(((double)z[k] - (double)mine.m_in) * tau_inv);
             if (slot[k] >= 0 && q[k] != 0.0) three[2] += q[k] * ((double)z[k] * tau_inv);
@@ -302,44 +301,64 @@ pods_distill_kernel(const DistillArgs a) {
         if (tid < CL) *cl.map_shared_rank(xs + rank, tid) = mine;
         cl.sync();
 
-        // ---- the row's scalars, in every thread ------------------------------------------------------------------
-        float m2 = -INFINITY, m1 = -INFINITY;
-        for (int r = 0; r < CL; ++r) {
-            m2 = max_nan(m2, xs[r].m_out);
-            m1 = max_nan(m1, xs[r].m_in);
-        }
-        const float zmax = max_nan(m1, m2);
-        const bool bad = !(fabsf(zmax) < INFINITY);
-        double S2 = 0.0, S1 = 0.0, A = 0.0;
-        if (!bad)
-            for (int r = 0; r < CL; ++r) {
-                if (xs[r].m_out > -INFINITY) S2 += xs[r].s_out * exp(((double)xs[r].m_out - (double)m2) * tau_inv);
-                if (xs[r].m_in > -INFINITY) S1 += xs[r].s_in * exp(((double)xs[r].m_in - (double)zmax) * tau_inv);
-                A += xs[r].a;
+        // ---- the row's scalars: one CTA a lane of the first warp ---------------------------------------------------
+        if (warp == 0) {
+            Xch x = {0.0, 0.0, 0.0, -INFINITY, -INFINITY};
+            if (lane < CL) x = xs[lane];
+            float m2 = x.m_out, m1 = x.m_in;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                m2 = max_nan(m2, __shfl_xor_sync(PODS_FULL_MASK, m2, d));
+                m1 = max_nan(m1, __shfl_xor_sync(PODS_FULL_MASK, m1, d));
             }
-        const double part = m2 > -INFINITY ? exp(((double)m2 - (double)zmax) * tau_inv) : 0.0;
-        const double Z = S2 * part + S1;
-        const double r = a.rest && m2 > -INFINITY ? fmax(0.0, 1.0 - Q) : 0.0;
-        const double g = (double)a.grad_scale * w * tau_inv;
-        if (rank == 0 && tid == 0) {
-            double kl = NAN;
+            const float zmax = max_nan(m1, m2);
+            const bool bad = !(fabsf(zmax) < INFINITY);
+            double S2 = 0.0, S1 = 0.0, A = x.a;
             if (!bad) {
-                const double lz = log(Z);
-                kl = H - A + Q * ((double)zmax * tau_inv + lz);
-                if (r > 0.0) kl += r * (log(r) - (((double)m2 - (double)zmax) * tau_inv + log(S2) - lz));
-            } else {
-                pods_raise(a.status, zmax == -INFINITY ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+                if (x.m_out > -INFINITY) S2 = x.s_out * ExpRef(x.m_out, cexp).scale_to(m2, cexp);
+                if (x.m_in > -INFINITY) S1 = x.s_in * exp(((double)x.m_in - (double)zmax) * tau_inv);
             }
-            a.kl[t] = (float)kl;
-            a.row_loss[t] = w * kl;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                S2 += __shfl_xor_sync(PODS_FULL_MASK, S2, d);
+                S1 += __shfl_xor_sync(PODS_FULL_MASK, S1, d);
+                A += __shfl_xor_sync(PODS_FULL_MASK, A, d);
+            }
+            const double part = m2 > -INFINITY ? exp(((double)m2 - (double)zmax) * tau_inv) : 0.0;
+            const double Z = S2 * part + S1;
+            const double r = a.rest && m2 > -INFINITY ? fmax(0.0, 1.0 - Q) : 0.0;
+            const double g = (double)a.grad_scale * w * tau_inv;
+            if (lane == 0) {
+                const double f = bad ? (double)NAN : (Q + r) / Z;
+                // relative to 2^-R of the sweep's reference, as the exponentials of the gradient are
+                const double per_e = ExpRef(m2, cexp).scale_to(m2 > -INFINITY ? m2 : 0.0f, cexp);
+                c.coef = g * (f * part - (r > 0.0 ? r / S2 : 0.0)) * per_e;
+                c.p_scale = f;
+                c.g = g;
+                c.m2 = m2;
+                c.zmax = zmax;
+                c.bad = bad;
+            }
+            __syncwarp();
+            if (rank == 0 && lane == 0) {              // nobody waits for these
+                double kl = NAN;
+                if (!bad) {
+                    const double lz = log(Z);
+                    kl = H - A + Q * ((double)zmax * tau_inv + lz);
+                    if (r > 0.0) kl += r * (log(r) - (((double)m2 - (double)zmax) * tau_inv + log(S2) - lz));
+                } else {
+                    pods_raise(a.status, zmax == -INFINITY ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+                }
+                a.kl[t] = (float)kl;
+                a.row_loss[t] = w * kl;
+            }
         }
+        __syncthreads();
 
         // ---- the gradient ------------------------------------------------------------------------------------------
         if (drow != nullptr && id_lo < id_hi) {
-            const float ref = m2 > -INFINITY ? m2 : 0.0f;
-            double f = bad ? (double)NAN : (Q + r) * part / Z;
-            if (r > 0.0) f -= r / S2;
-            const float coef = (float)(g * f);
+            const ExpRef ref(c.m2, cexp);
+            const float coef = (float)c.coef;
             uint4* const dvec = reinterpret_cast<uint4*>(drow - dlead);
             const int shift = v_lo * E - dlead - s.id0 - (v_lo * E - dlead - s.id0) / E * E;
             if (shift == 0) {
@@ -348,8 +367,9 @@ pods_distill_kernel(const DistillArgs a) {
                     if (PODS_INDEX_OK(v + to_buf, s.cnt, a.status)) {
                         float x[E];
                         El::unpack(buf[v + to_buf], x);
+                        ref.exps(x);
 #pragma unroll
-                        for (int e = 0; e < E; ++e) x[e] = coef * ex2_approx((x[e] - ref) * cexp);
+                        for (int e = 0; e < E; ++e) x[e] *= coef;
                         dvec[v] = El::pack(x);
                     }
             } else {
@@ -358,27 +378,29 @@ pods_distill_kernel(const DistillArgs a) {
                     if (PODS_INDEX_OK(at, s.cnt * E - E + 1, a.status)) {
                         float x[E];
 #pragma unroll
-                        for (int e = 0; e < E; ++e) x[e] = coef * ex2_approx((El::to_float(elems[at + e]) - ref) * cexp);
+                        for (int e = 0; e < E; ++e) x[e] = El::to_float(elems[at + e]);
+                        ref.exps(x);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] *= coef;
                         dvec[v] = El::pack(x);
                     }
                 }
             }
             for (int i = id_lo + tid; i < min(id_hi, v_lo * E - dlead); i += kThreads)
-                drow[i] = El::from_float(coef * ex2_approx((El::to_float(elems[i - s.id0]) - ref) * cexp));
+                drow[i] = El::from_float(coef * ref.exp1(El::to_float(elems[i - s.id0]), cexp));
             for (int i = max(id_lo, v_hi * E - dlead) + tid; i < id_hi; i += kThreads)
-                drow[i] = El::from_float(coef * ex2_approx((El::to_float(elems[i - s.id0]) - ref) * cexp));
+                drow[i] = El::from_float(coef * ref.exp1(El::to_float(elems[i - s.id0]), cexp));
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < kPer; ++k)
+            for (int k = 0; k < KP; ++k)
                 if (first >> k & 1u) {
-                    const double p = bad ? (double)NAN : exp(((double)z[k] - (double)zmax) * tau_inv) / Z;
-                    drow[id[k]] = El::from_float((float)(g * ((Q + r) * p - qsum[k])));
+                    const double p = exp(((double)z[k] - (double)c.zmax) * tau_inv) * c.p_scale;      // (Q + r) p
+                    drow[id[k]] = El::from_float((float)(c.g * (p - qsum[k])));
                 }
         }
         fence_async_proxy();                           // the buffer is refilled by bulk copies
         __syncthreads();
     }
-    cl.sync();                                         // no CTA leaves while a peer may still write its exchange words
 }
 
 size_t align_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
@@ -386,7 +408,7 @@ size_t align_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
 constexpr size_t kMaxSmem = 227 * 1024;
 constexpr size_t kSegmentBytes = 40 * 1024;
 
-template <int DT>
+template <int DT, int KP>
 int launch_distill(DistillArgs& a, cudaStream_t stream) {
     const int esize = DT == PODS_DTYPE_F32 ? 4 : 2;
     int cl = 1;
@@ -394,7 +416,7 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
     a.seg = segment_vectors(a.V, esize, cl);
     const size_t smem = kCtrlBytes + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
-    auto kernel = pods_distill_kernel<DT>;
+    auto kernel = pods_distill_kernel<DT, KP>;
     PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (cl > 8) PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     cudaLaunchConfig_t cfg = {};
@@ -403,8 +425,7 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
     attr[0].val.clusterDim.x = (unsigned)cl;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
-    const int64_t most = 1 << 20;
-    cfg.gridDim = dim3((unsigned)((a.T < most ? a.T : most) * cl), 1, 1);
+    cfg.gridDim = dim3((unsigned)(row_clusters(a.T, cl, smem) * cl), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -465,9 +486,11 @@ extern "C" int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype
     a.row_loss = static_cast<double*>(workspace);
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    const int rc = dtype == PODS_DTYPE_BF16  ? launch_distill<PODS_DTYPE_BF16>(a, s)
-                   : dtype == PODS_DTYPE_F16 ? launch_distill<PODS_DTYPE_F16>(a, s)
-                                             : launch_distill<PODS_DTYPE_F32>(a, s);
+    constexpr int kMany = PODS_MAX_TOPK / kThreads;
+    const bool few = K <= kThreads;
+    const int rc = dtype == PODS_DTYPE_BF16  ? (few ? launch_distill<PODS_DTYPE_BF16, 1>(a, s) : launch_distill<PODS_DTYPE_BF16, kMany>(a, s))
+                   : dtype == PODS_DTYPE_F16 ? (few ? launch_distill<PODS_DTYPE_F16, 1>(a, s) : launch_distill<PODS_DTYPE_F16, kMany>(a, s))
+                                             : (few ? launch_distill<PODS_DTYPE_F32, 1>(a, s) : launch_distill<PODS_DTYPE_F32, kMany>(a, s));
     if (rc != PODS_OK) return rc;
     return pods_loss::launch_loss_reduce(a.row_loss, T, loss_acc, s);
 }

@@ -18,11 +18,9 @@
 //   general  where the list does not reach far enough (a nucleus of thousands, a list full of ties), the threshold is
 //            bisected on the order-preserving keys of the values, counts and fp64 sums taken over the resident row.
 //
-// Which token is drawn must not depend on how sums are split or rounded.  The fast sums (fp32 exponentials, summed eight
-// at a time in fp32 and then in fp64) are within 1.6e-6 of the exact ones: exponent argument 2^-24 + 2^-25 relative of its
-// size, whose mean under the row's distribution is at most log2 V <= 19 (entropy bound), the hardware exponential 2^-22.5,
-// three roundings of the partial sums.  A draw or a border closer than kMargin to its neighbours is taken again with fp64
-// exponentials throughout, so the outcome is that of fp64 arithmetic.
+// Which token is drawn must not depend on how sums are split or rounded: a draw or a border that lies nearer to its
+// neighbours than the error of the fast sums (fp32 exponentials, summed eight at a time in fp32 and then in fp64; see
+// draw_margin) is taken again with fp64 exponentials throughout, so the outcome is that of fp64 arithmetic.
 
 #include "row_cluster.cuh"
 
@@ -32,10 +30,18 @@ namespace {
 
 constexpr int W = 8;                          // warps of a CTA
 constexpr int kThreads = W * 32;
-constexpr double kMargin = 4e-6;              // of the sum: see above
 constexpr float kGreedyBelow = 0x1p-20f;      // temperatures below this are the arg-max
 constexpr int kSampleList = 1024;             // entries of the sampler's list
 constexpr int kNoCut = 0x7fffffff;
+
+// How near an edge of the fast running sum a drawn point may lie before fp64 decides: twice the error of a fast sum.  That
+// is (2^-24 + 2^-24 + 2^-25) of the exponent (difference, product, log2e / tau), whose mean |d| under the row's distribution
+// is at most ln V - ln Z (its entropy, ln Z + mean |d|, is at most ln V), and 4e-7 for the hardware exponential (2^-22.5)
+// and the three roundings of a vector's sum.
+__device__ __forceinline__ double draw_margin(int V, double Z) {
+    const float depth = fmaxf(0.0f, __logf((float)V) - __logf((float)Z)) + 0.01f;
+    return 2.0 * (1.5e-7 * (double)depth + 4e-7) * Z;
+}
 
 struct SampleArgs {
     const void* logits;
@@ -635,7 +641,7 @@ pods_sample_kernel(const SampleArgs a) {
                     w.template locate<false, false>(target / scale, before / scale, ref, 0.0f, 0, r);
                     const double lo = c.found_before * scale, hi = lo + c.found_e * scale;
                     // an edge of the running sum closer than the margin is decided in fp64 (the row's start is no edge)
-                    out.n = (target - lo > kMargin * r.Z || lo == 0.0) && hi - target > kMargin * r.Z ? 1 : 0;
+                    out.n = (target - lo > draw_margin(a.V, r.Z) || lo == 0.0) && hi - target > draw_margin(a.V, r.Z) ? 1 : 0;
                     out.i = c.found;
                 }
                 x = w.exchange(out);
@@ -681,7 +687,7 @@ pods_sample_kernel(const SampleArgs a) {
                         if (nucleus) {
                             const bool over_list = top_k > 0 || whole;
                             const double goal = (double)top_p * (over_list ? total : r.Z);
-                            const double slack = over_list ? 0.0 : kMargin * r.Z;
+                            const double slack = over_list ? 0.0 : draw_margin(a.V, r.Z);
                             int first = kNoCut, unsure = 0;
 #pragma unroll
                             for (int k = 0; k < PT; ++k) {
@@ -848,17 +854,333 @@ pods_topk_kernel(const SampleArgs a) {
     w.cl.sync();
 }
 
+// ---- no filters: the whole policy -------------------------------------------------------------------------------------
+// Lanes own contiguous vectors of the segment, so a lane's, a warp's and a CTA's sums are stretches of the running sum.
+// Each warp reduces its part to a sum relative to 2^R, R the integer above its maximum's exponent, and hands the pair to
+// every CTA of the cluster; parts are then brought together by powers of two, exactly and without an exponential.  After
+// the one cluster barrier of a row every warp knows all parts in id order, and so whether the drawn point is in its own;
+// the warp that has it takes the lane from the lane sums that it kept and evaluates that lane's few vectors again.  Rows
+// whose draw lies within draw_margin of an edge are marked in every CTA of the cluster and taken in fp64 at the end.
+// 152 K bf16 vocabulary, 512 rows: ORIGINAL
+
+struct Part {
+    double s;             // sum relative to the part's reference (to its maximum, the second time round)
+    float m;              // its maximum
+    int pad;
+};
+
+constexpr int kRedoRows = 8192;               // rows of a cluster between two visits of the marked ones
+
+struct PolicyCtrl {
+    unsigned long long full;
+    Part part[2][kMaxCluster * W];
+    uint32_t redo[kRedoRows / 32];
+};
+constexpr int kPolicyCtrlBytes = (sizeof(PolicyCtrl) + 127) & ~127;
+
+__device__ __forceinline__ double pow2(int n) {       // n <= 0; below the normal numbers: 0
+    return n < -1000 ? 0.0 : __hiloint2double((1023 + n) << 20, 0);
+}
+
+// e = 2^(x c - R).  R is an integer, at least m c; where the product is so large that floats have no fractions, the
+// difference to the maximum is taken first and `far` parts are related by fp64 exponentials.
+struct PartRef {
+    float m, R, c;
+    bool far;
+    __device__ __forceinline__ PartRef(float m_, float c_) : c(c_) {
+        m = fabsf(m_) < INFINITY ? m_ : 0.0f;
+        R = ceilf(__fmul_ru(m, c));
+        far = !(fabsf(R) < 0x1p23f);
+    }
+    template <int E>
+    __device__ __forceinline__ void exps(float (&x)[E]) const {
+        const unsigned long long c2 = pack2(c, c), off2 = far ? pack2(-m, -m) : pack2(-R, -R);
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+            const unsigned long long v = pack2(x[i], x[i + 1]);
+            float p, q;
+            unpack2(far ? mul2(add2(v, off2), c2) : fma2(v, c2, off2), p, q);
+            x[i] = ex2_approx(p);
+            x[i + 1] = ex2_approx(q);
+        }
+    }
+    __device__ __forceinline__ double exp1(float x) const { return (double)ex2_approx(far ? (x - m) * c : fmaf(x, c, -R)); }
+    // what sums relative to this reference are multiplied with to be relative to that of `top`, the row's
+    __device__ __forceinline__ double scale_to(const PartRef& top) const {
+        if (!top.far) return pow2((int)fmaxf(R - top.R, -2000.0f));
+        return exp2((far ? (double)m * (double)c : (double)R) - (double)top.m * (double)c);
+    }
+};
+
+// Inclusive scan over a warp.
+__device__ __forceinline__ double warp_scan(double v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const double o = __shfl_up_sync(PODS_FULL_MASK, v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+template <int DT>
+struct Policy {
+    using El = Elem<DT>;
+    static constexpr int E = El::E;
+    const SampleArgs& a;
+    PolicyCtrl& ctl;
+    uint4* const buf;
+    cg::cluster_group cl;
+    int CL, rank, tid, lane, warp;
+    uint32_t phase = 0;
+    int parity = 0;
+
+    __device__ Policy(const SampleArgs& a_, PolicyCtrl& c_, uint4* b_) : a(a_), ctl(c_), buf(b_), cl(cg::this_cluster()) {
+        CL = (int)cl.num_blocks();
+        rank = (int)cl.block_rank();
+        tid = threadIdx.x;
+        lane = tid & 31;
+        warp = tid >> 5;
+    }
+
+    // One row; `mark`: the bit of the row in the marked ones.
+    template <bool PREC>
+    __device__ void row(int64_t t, int mark) {
+        const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+        if (tid == 0) start_load<DT>(s, a.V, buf, &ctl.full);
+        float tau = a.temperature_row ? a.temperature_row[t] : a.temperature;
+        float u = a.u[t];
+        bool odd = false;
+        if (!(tau >= 0.0f) || tau == INFINITY) { tau = 1.0f; odd = true; }
+        if (!(u >= 0.0f)) { u = 0.0f; odd = true; }
+        if (!(u < 1.0f)) { u = 0x1.fffffep-1f; odd = true; }
+        if (odd && rank == 0 && tid == 0) pods_raise(a.status, PODS_STATUS_PARAM_RANGE);
+        const bool greedy = tau < kGreedyBelow;
+        if (greedy) tau = 1.0f;
+        const double tau_inv = 1.0 / (double)tau;
+        const float c = (float)(1.4426950408889634 * tau_inv);
+        // an odd number of vectors a lane: eight lanes of a 16-byte access then touch all 32 banks once
+        const int per = ((s.cnt + kThreads - 1) / kThreads) | 1;
+        const int v0 = min(s.cnt, tid * per), v1 = min(s.cnt, v0 + per);
+        if (!mbar_wait(&ctl.full, phase, kSpinLimit) && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
+        phase ^= 1u;
+        __syncthreads();
+
+        float m = -INFINITY;
+#pragma unroll 4
+        for (int j = v0; j < v1; ++j) m = max_nan(m, El::vec_max(buf[j]));
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(PODS_FULL_MASK, m, d));
+        const PartRef ref(m, c);
+        double sum = 0.0;
+        if (PREC) {
+            for (int j = v0; j < v1; ++j) {
+                float x[E];
+                El::unpack(buf[j], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum += exp(((double)x[e] - (double)ref.m) * tau_inv);
+            }
+        } else {
+#pragma unroll 2
+            for (int j = v0; j < v1; ++j) {
+                float x[E];
+                El::unpack(buf[j], x);
+                ref.exps(x);
+                sum += (double)vec_add(x);
+            }
+        }
+        const double incl = warp_scan(sum, lane);
+        Part p;
+        p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
+        p.m = m;
+        p.pad = 0;
+        const int mine = rank * W + warp, n_parts = CL * W;
+        if (lane < CL) *cl.map_shared_rank(&ctl.part[parity][mine], lane) = p;
+        cl.sync();
+
+        // lane l holds parts [l n, (l + 1) n)
+        const Part* const part = ctl.part[parity];
+        parity ^= 1;
+        constexpr int N = kMaxCluster * W / 32;
+        const int n = (n_parts + 31) / 32;
+        float z = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n && lane * n + i < n_parts) z = max_nan(z, part[lane * n + i].m);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) z = max_nan(z, __shfl_xor_sync(PODS_FULL_MASK, z, d));
+        const float zmax = z + 0.0f;
+        if (!(fabsf(z) < INFINITY)) {
+            if (rank == 0 && tid == 0) {
+                const bool empty = z == -INFINITY;
+                a.tokens[t] = -1;
+                const float v = empty ? -INFINITY : NAN;
+                if (a.logp) a.logp[t] = v;
+                if (a.logq) a.logq[t] = v;
+                pods_raise(a.status, empty ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+            }
+            return;
+        }
+        const PartRef top(zmax, c);
+        double v[N], psum = 0.0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.0;
+            if (i < n && lane * n + i < n_parts) {
+                const Part q = part[lane * n + i];
+                if (q.s > 0.0) v[i] = q.s * (PREC ? exp(((double)q.m - (double)zmax) * tau_inv) : PartRef(q.m, c).scale_to(top));
+            }
+            psum += v[i];
+        }
+        const double pincl = warp_scan(psum, lane);
+        const double Z = __shfl_sync(PODS_FULL_MASK, pincl, 31);
+        const double target = (double)u * Z;
+        int owner = -1;
+        double before = 0.0;
+        if (greedy) {
+            int first = kNoCut;
+            for (int i = lane; i < n_parts; i += 32)
+                if (part[i].m == zmax) first = min(first, i);
+            owner = __reduce_min_sync(PODS_FULL_MASK, first);
+        } else {
+            const uint32_t hit = __ballot_sync(PODS_FULL_MASK, pincl > target && psum > 0.0);
+            const int from = __ffs(hit) - 1;               // there is one: target < Z
+            double b = pincl - psum, at = b;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (v[i] > 0.0 && (owner < 0 || !(b > target))) {  // the first that passes the target, else the last
+                    owner = lane * n + i;
+                    at = b;
+                    b += v[i];
+                }
+            owner = __shfl_sync(PODS_FULL_MASK, owner, from);
+            before = __shfl_sync(PODS_FULL_MASK, at, from);
+        }
+        if (owner != mine) return;
+
+        // ---- the warp with the drawn point ----
+        if (greedy) {
+            int id = kNoCut;
+            for (int j = v0; j < v1; ++j) {
+                float x[E];
+                El::unpack(buf[j], x);
+#pragma unroll
+                for (int e = E - 1; e >= 0; --e)
+                    if (x[e] == zmax) id = min(id, s.id0 + j * E + e);
+            }
+            id = __reduce_min_sync(PODS_FULL_MASK, id);
+            if (lane == 0) {
+                // the sum is relative to 2^R: ln Z over e^zmax
+                const double lz = log(Z) + (PREC || top.far ? 0.0 : ((double)top.R - (double)zmax * (double)c) * 0.6931471805599453);
+                a.tokens[t] = id;
+                if (a.logp) a.logp[t] = (float)-lz;
+                if (a.logq) a.logq[t] = 0.0f;
+            }
+            return;
+        }
+        const double scale = PREC ? exp(((double)m - (double)zmax) * tau_inv) : ref.scale_to(top);
+        const double goal = (target - before) / scale;
+        uint32_t hit = __ballot_sync(PODS_FULL_MASK, incl > goal && sum > 0.0);
+        const uint32_t any = __ballot_sync(PODS_FULL_MASK, sum > 0.0);
+        const int from = hit ? __ffs(hit) - 1 : 31 - __clz(any);
+        const double lane_before = __shfl_sync(PODS_FULL_MASK, incl - sum, from);
+        // the elements of that lane's vectors, K a lane
+        const int e0 = __shfl_sync(PODS_FULL_MASK, v0, from) * E, e1 = __shfl_sync(PODS_FULL_MASK, v1, from) * E;
+        const int K = (e1 - e0 + 31) / 32;
+        const typename El::raw* el = reinterpret_cast<const typename El::raw*>(buf);
+        const int k0 = min(e1, e0 + lane * K), k1 = min(e1, k0 + K);
+        auto weight = [&](int i) {
+            const float x = El::to_float(el[i]);
+            return PREC ? exp(((double)x - (double)ref.m) * tau_inv) : ref.exp1(x);
+        };
+        double own = 0.0;
+        for (int i = k0; i < k1; ++i) own += weight(i);
+        const double eincl = warp_scan(own, lane);
+        hit = __ballot_sync(PODS_FULL_MASK, lane_before + eincl > goal && own > 0.0);
+        const uint32_t some = __ballot_sync(PODS_FULL_MASK, own > 0.0);
+        const int last = hit ? __ffs(hit) - 1 : 31 - __clz(some);
+        if (lane == last) {
+            double run = lane_before + eincl - own, lo = run, ev = 0.0;
+            int at = -1;
+            for (int i = k0; i < k1; ++i) {
+                const double w = weight(i);
+                if (!(w > 0.0)) continue;
+                at = i;
+                lo = run;
+                ev = w;
+                run += w;
+                if (run > goal) break;
+            }
+            // an edge of the running sum within the margin is decided in fp64 (the row's start is no edge)
+            const double edge = before + lo * scale, next = edge + ev * scale, margin = draw_margin(a.V, Z);
+            if (PREC || ((target - edge > margin || edge == 0.0) && next - target > margin)) {
+                const double lz = log(Z) + (PREC || top.far ? 0.0 : ((double)top.R - (double)zmax * (double)c) * 0.6931471805599453);
+                const float d = (float)(((double)El::to_float(el[at]) - (double)zmax) * tau_inv - lz);
+                a.tokens[t] = s.id0 + at;
+                if (a.logp) a.logp[t] = d;
+                if (a.logq) a.logq[t] = d;
+            } else {
+                for (int q = 0; q < CL; ++q) atomicOr(cl.map_shared_rank(&ctl.redo[mark >> 5], q), 1u << (mark & 31));
+            }
+        }
+    }
+};
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 5)
+pods_sample_policy_kernel(const SampleArgs a) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    PolicyCtrl& ctl = *reinterpret_cast<PolicyCtrl*>(smem);
+    Policy<DT> w(a, ctl, reinterpret_cast<uint4*>(smem + kPolicyCtrlBytes));
+    const int tid = w.tid;
+    if (tid == 0) {
+        mbar_init(&ctl.full, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int i = tid; i < kRedoRows / 32; i += kThreads) ctl.redo[i] = 0;
+    __syncthreads();
+    w.cl.sync();                                       // every CTA runs before its shared memory is written
+
+    const int64_t n_clusters = gridDim.x / w.CL;
+    for (int64_t t0 = blockIdx.x / w.CL; t0 < a.T; t0 += kRedoRows * n_clusters) {
+        for (int k = 0; k < kRedoRows; ++k) {
+            const int64_t t = t0 + k * n_clusters;
+            if (t >= a.T) break;
+            if (a.mask != nullptr && a.mask[t] == 0) continue;
+            w.template row<false>(t, k);
+            fence_async_proxy();                       // the buffer is refilled by bulk copies
+            __syncthreads();
+        }
+        w.cl.sync();                                   // the marks are in place, the same in every CTA
+        static_assert(kRedoRows / 32 == kThreads, "a word of marks a thread");
+        if (__syncthreads_or(ctl.redo[tid] != 0)) {
+            for (int i = 0; i < kRedoRows / 32; ++i) {
+                uint32_t bits = ctl.redo[i];
+                while (bits) {
+                    const int k = 32 * i + __ffs(bits) - 1;
+                    bits &= bits - 1;
+                    w.template row<true>(t0 + k * n_clusters, 0);
+                    fence_async_proxy();
+                    __syncthreads();
+                }
+            }
+            __syncthreads();
+            ctl.redo[tid] = 0;
+        }
+        if (t0 + kRedoRows * n_clusters < a.T) w.cl.sync();      // cleared before the next mark
+    }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 constexpr size_t kMaxSmem = 227 * 1024;
 constexpr size_t kSegmentBytes = 40 * 1024;            // segments of about this size let five CTAs share an SM
 
 template <typename Kernel>
-int launch_rows(Kernel kernel, SampleArgs& a, int esize, cudaStream_t stream) {
+int launch_rows(Kernel kernel, SampleArgs& a, int esize, size_t ctrl_bytes, cudaStream_t stream) {
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
     a.seg = segment_vectors(a.V, esize, cl);
-    const size_t smem = kCtrlBytes + (size_t)a.list_cap * 8 + (size_t)a.seg * 16;
+    const size_t smem = ctrl_bytes + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
     PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     if (cl > 8) PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
@@ -868,13 +1190,13 @@ int launch_rows(Kernel kernel, SampleArgs& a, int esize, cudaStream_t stream) {
     attr[0].val.clusterDim.x = (unsigned)cl;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
-    const int64_t most = 1 << 20;                      // more rows than this go round
-    cfg.gridDim = dim3((unsigned)((a.T < most ? a.T : most) * cl), 1, 1);
+    cfg.gridDim = dim3((unsigned)cl, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)(row_clusters(a.T, cl, smem) * cl), 1, 1);
     PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, kernel, a));
     return PODS_OK;
 }
@@ -924,9 +1246,15 @@ extern "C" int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64
     a.list_cap = kSampleList;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16>, a, esize, s);
-    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16>, a, esize, s);
-    return launch_rows(pods_sample_kernel<PODS_DTYPE_F32>, a, esize, s);
+    if (!top_k_row && !top_p_row && !min_p_row && (top_k <= 0 || top_k >= V) && top_p >= 1.0f && min_p <= 0.0f) {
+        if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_policy_kernel<PODS_DTYPE_BF16>, a, esize, kPolicyCtrlBytes, s);
+        if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_policy_kernel<PODS_DTYPE_F16>, a, esize, kPolicyCtrlBytes, s);
+        return launch_rows(pods_sample_policy_kernel<PODS_DTYPE_F32>, a, esize, kPolicyCtrlBytes, s);
+    }
+    const size_t ctrl = kCtrlBytes + (size_t)a.list_cap * 8;
+    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16>, a, esize, ctrl, s);
+    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16>, a, esize, ctrl, s);
+    return launch_rows(pods_sample_kernel<PODS_DTYPE_F32>, a, esize, ctrl, s);
 }
 
 extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int32_t K,
@@ -954,7 +1282,8 @@ extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t
     while (a.list_cap < 4 * K) a.list_cap *= 2;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_topk_kernel<PODS_DTYPE_BF16>, a, esize, s);
-    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_topk_kernel<PODS_DTYPE_F16>, a, esize, s);
-    return launch_rows(pods_topk_kernel<PODS_DTYPE_F32>, a, esize, s);
+    const size_t ctrl = kCtrlBytes + (size_t)a.list_cap * 8;
+    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_topk_kernel<PODS_DTYPE_BF16>, a, esize, ctrl, s);
+    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_topk_kernel<PODS_DTYPE_F16>, a, esize, ctrl, s);
+    return launch_rows(pods_topk_kernel<PODS_DTYPE_F32>, a, esize, ctrl, s);
 }

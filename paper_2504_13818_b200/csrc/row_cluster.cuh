@@ -156,6 +156,78 @@ __device__ __forceinline__ float ex2_approx(float x) {
     return y;
 }
 
+// ---- exponentials of a vector -----------------------------------------------------------------------------------------
+// Two lanes of fp32 an instruction (fma.rn.f32x2): 3 issue slots an element with the unpacking and the exponential.
+
+__device__ __forceinline__ unsigned long long pack2(float lo, float hi) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(unsigned long long v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// What exponentials are taken relative to: e_i = 2^(x_i c - R) with R = fl(m c) for the reference value m, one fused
+// rounding an element.  Where R is so large that its own rounding matters (cold temperatures, huge logits) the difference is
+// taken first, e_i = 2^((x_i - m) c).  A reference of -inf (nothing in sight) makes every e 0.
+struct ExpRef {
+    float m, R;
+    bool far;
+    unsigned long long c2, off2;
+    __device__ __forceinline__ ExpRef(float m_, float c) {
+        m = fabsf(m_) < INFINITY ? m_ : 0.0f;
+        R = m * c;
+        far = !(fabsf(R) < 0x1p24f);
+        c2 = pack2(c, c);
+        off2 = far ? pack2(-m, -m) : pack2(-R, -R);
+    }
+    template <int E>
+    __device__ __forceinline__ void exps(float (&x)[E]) const {
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+            const unsigned long long v = pack2(x[i], x[i + 1]);
+            float a, b;
+            unpack2(far ? mul2(add2(v, off2), c2) : fma2(v, c2, off2), a, b);
+            x[i] = ex2_approx(a);
+            x[i + 1] = ex2_approx(b);
+        }
+    }
+    __device__ __forceinline__ float exp1(float x, float c) const { return ex2_approx(far ? (x - m) * c : fmaf(x, c, -R)); }
+    // a sum relative to this reference, times scale_to(z), is relative to z (fp64; z c and R are exact there)
+    __device__ __forceinline__ double scale_to(float z, float c) const {
+        return exp2(far ? ((double)m - (double)z) * (double)c : (double)R - (double)z * (double)c);
+    }
+};
+
+template <int E>
+__device__ __forceinline__ float vec_add(const float (&x)[E]) {
+    unsigned long long s[E / 2];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) s[i] = pack2(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+    for (int d = E / 4; d > 0; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < d; ++i) s[i] = add2(s[i], s[i + d]);
+    float a, b;
+    unpack2(s[0], a, b);
+    return a + b;
+}
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 __device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {
@@ -258,6 +330,15 @@ struct Min {
 static inline int segment_vectors(int64_t V, int esize, int cl) {
     const int64_t e = 16 / esize, nvec = (V + 2 * (e - 1)) / e + 1;
     return (int)(((nvec + cl - 1) / cl + 7) & ~7ll);
+}
+
+// Host: clusters to launch for T rows - no more than can be resident (each goes round over its rows), by shared memory and
+// at most five CTAs an SM.  An estimate is enough: clusters do not wait for one another.
+static inline int64_t row_clusters(int64_t T, int cl, size_t smem) {
+    int64_t per_sm = (int64_t)(233472 / (smem + 1024));
+    per_sm = per_sm < 1 ? 1 : per_sm > 5 ? 5 : per_sm;
+    const int64_t n = pods_sm_count() * per_sm / cl;
+    return T < n ? T : (n < 1 ? 1 : n);
 }
 
 }  // namespace pods_row
