@@ -6,21 +6,27 @@
 // exceeds u times the kept sum.
 //
 // A cluster of CL CTAs holds the row in shared memory (row_cluster.cuh): HBM is read once whatever the filters ask for.
+// Lanes own contiguous vectors of the CTA's segment, so a lane's, a warp's and a CTA's sums are stretches of the running sum.
 //
-//   pass 1   the segment's maximum; pass 2 its sum of exponentials relative to that maximum, one exponential an element;
-//            one exchange of (maximum, sum) over the cluster gives every CTA the row's maximum and normaliser.
-//   no filter  the CTA whose part of the running sum holds the target finds the token: warps own contiguous parts of the
-//            segment, so the search narrows from CTA to warp to 32 vectors to the element.
-//   filters  every warp takes the r-th largest of its lanes' maxima; the least of these over the cluster is a value that at
-//            least `want` logits reach, so the logits reaching it contain the first `want` of the order.  They are listed
-//            (in the typical row a few hundred), the cluster's first CTA sorts them, and the rest is arithmetic on the
-//            list in fp64.
-//   general  where the list does not reach far enough (a nucleus of thousands, a list full of ties), the threshold is
-//            bisected on the order-preserving keys of the values, counts and fp64 sums taken over the resident row.
+//   all rows  each warp reduces its part to a sum of exponentials relative to 2^R, R the integer above its maximum's exponent,
+//            and hands the pair to every CTA; parts are then brought together by powers of two, exactly and without an
+//            exponential.  After this one cluster barrier every warp knows all parts in id order.
+//   no filter  the warp whose part holds the drawn point takes the lane from the lane sums that it kept, and evaluates that
+//            lane's few vectors again; every other warp goes on to the next row.
+//   filters  every warp also finds the r-th largest of its lanes' maxima; the least of these over the cluster is a value that
+//            at least `want` logits reach, so the logits reaching it contain the first `want` of the order.  They are listed
+//            (in the typical row a few hundred), the cluster's first CTA sorts them, and the rest is fp64 arithmetic on the list.
+//   wide nucleus  where the list does not reach far enough, a histogram of the row's mass over 1024 stretches of logit
+//            brackets the border within a few stretches; one fp64 sweep takes the sums above the bracket and lists what lies in
+//            it, and the list settles the border.
+//   the rest  (a bracket full of ties, a top_k above the list) bisects the order-preserving keys of the values with counts and
+//            fp64 sums over the resident row.
 //
 // Which token is drawn must not depend on how sums are split or rounded: a draw or a border that lies nearer to its
 // neighbours than the error of the fast sums (fp32 exponentials, summed eight at a time in fp32 and then in fp64; see
 // draw_margin) is taken again with fp64 exponentials throughout, so the outcome is that of fp64 arithmetic.
+
+#include <stddef.h>
 
 #include "row_cluster.cuh"
 
@@ -28,19 +34,29 @@ using namespace pods_row;
 
 namespace {
 
-constexpr int W = 8;                          // warps of a CTA
+constexpr int W = 16;                         // warps of a CTA
 constexpr int kThreads = W * 32;
 constexpr float kGreedyBelow = 0x1p-20f;      // temperatures below this are the arg-max
-constexpr int kSampleList = 1024;             // entries of the sampler's list
+constexpr int kSampleList = 1024;             // entries that the sampler's first CTA orders
+constexpr int kBins = 1024;                   // stretches of the mass histogram
 constexpr int kNoCut = 0x7fffffff;
+constexpr int kRedoRows = 8192;               // rows of a cluster between two visits of the marked ones
+constexpr double kLn2 = 0.6931471805599453;
 
-// How near an edge of the fast running sum a drawn point may lie before fp64 decides: twice the error of a fast sum.  That
-// is (2^-24 + 2^-24 + 2^-25) of the exponent (difference, product, log2e / tau), whose mean |d| under the row's distribution
-// is at most ln V - ln Z (its entropy, ln Z + mean |d|, is at most ln V), and 4e-7 for the hardware exponential (2^-22.5)
-// and the three roundings of a vector's sum.
-__device__ __forceinline__ double draw_margin(int V, double Z) {
+// Errors of the fast sums, rigorously bounded.  An exponential e_v is off by at most (slope |d_v| + kFlat) of itself: the
+// rounding of the fused multiply-add (2^-24 of the exponent; `far` rows take a difference first, 2^-24 more) and of log2e / tau,
+// |d_v| deep; the hardware exponential (2^-22.5) and the three roundings of a vector's sum, flat.  The mean of |d| under the
+// row's distribution is at most ln V - ln Z (its entropy, ln Z + mean |d|, is at most ln V).
+constexpr double kFlat = 3.6e-7;
+__device__ __forceinline__ double deep_error(int V, double Z, float c, double tau_inv, bool far) {
     const float depth = fmaxf(0.0f, __logf((float)V) - __logf((float)Z)) + 0.01f;
-    return 2.0 * (1.5e-7 * (double)depth + 4e-7) * Z;
+    const double log2e = fabs((double)c / tau_inv * 0.6931471805599453 - 1.0);
+    return ((far ? 1.2e-7 : 6e-8) + log2e) * (double)depth;
+}
+// How near an edge C of the running sum a drawn point u Z may lie before fp64 decides: the error of u Z - C, which with
+// Z = C + rest is that of u rest - (1 - u) C where C is about u Z.
+__device__ __forceinline__ double draw_margin(double u, double Z, double deep) {
+    return (fmax(u, 1.0 - u) * deep + 2.1 * u * (1.0 - u) * kFlat + 1e-12) * Z;
 }
 
 struct SampleArgs {
@@ -59,824 +75,44 @@ struct SampleArgs {
     int K;
     int32_t* ids;
     float *values, *lse;
-    int list_cap;                             // entries of the list in shared memory (a power of two)
+    int list_cap, own_cap;                    // entries of one CTA: its share of all lists, its own list
     uint32_t* status;
+};
+
+struct Part {                                 // of one warp
+    double s;             // sum relative to the part's reference (to its maximum in fp64 rows)
+    float m;              // its maximum
+    float lim;            // a value that enough of its logits reach
 };
 
 struct Xch {                                  // one CTA's word in an exchange
     double a, b;
-    float m, lim;
+    float m;
     int i, n;
 };
 
-struct Ctrl {
+struct RowCtrl {
     unsigned long long full;                  // the segment's copy
-    Xch x[2][kMaxCluster];                    // exchanges alternate between the two, so that one barrier each is enough
-    double dpart[W], dwarp[W];
-    float fpart[W];
-    int ipart[W], iwarp[W];
-    int n_list;
-    int found;
-    double found_before;
-    double found_e;
-};
-constexpr int kCtrlBytes = (sizeof(Ctrl) + 127) & ~127;
-
-// Everything of a row that the steps share; the same in every thread of the cluster.
-struct Row {
-    double tau_inv;       // 1 / tau
-    float c;              // log2e / tau
-    float zmax;
-    double Z;             // fast sum of e over the row
-    int t_ok;
-};
-
-template <int DT>
-struct Worker {
-    using El = Elem<DT>;
-    static constexpr int E = El::E;
-    const SampleArgs& a;
-    Ctrl& c;
-    uint4* buf;
-    unsigned long long* list;
-    cg::cluster_group cl;
-    int CL, rank, tid, lane, warp;
-    int parity = 0;       // of the next exchange
-    Segment s;
-    int w0, w1;           // my warp's vectors
-
-    __device__ Worker(const SampleArgs& a_, Ctrl& c_, uint4* buf_, unsigned long long* list_)
-        : a(a_), c(c_), buf(buf_), list(list_), cl(cg::this_cluster()) {
-        CL = (int)cl.num_blocks();
-        rank = (int)cl.block_rank();
-        tid = threadIdx.x;
-        lane = tid & 31;
-        warp = tid >> 5;
-    }
-
-    // Hands `mine` to every CTA of the cluster; returns the CL words.  Call with the whole CTA.
-    __device__ const Xch* exchange(const Xch& mine) {
-        Xch* slot = c.x[parity];
-        parity ^= 1;
-        if (tid < CL) *cl.map_shared_rank(slot + rank, tid) = mine;
-        cl.sync();
-        return slot;
-    }
-
-    __device__ int id_of(int j, int e) const { return s.id0 + j * E + e; }
-    __device__ bool is_id(int id) const { return id >= 0 && id < a.V; }
-
-    // e of one value relative to `ref`, fast or in fp64
-    template <bool PREC>
-    __device__ static double weight(float x, float ref, const Row& r) {
-        if (PREC) return exp(((double)x - (double)ref) * r.tau_inv);
-        return (double)ex2_approx((x - ref) * r.c);
-    }
-
-    // sum of e over a vector, of the kept elements only if FILT
-    template <bool PREC, bool FILT>
-    __device__ double vec_sum(int j, float ref, float thr, int cut, const Row& r) const {
-        if constexpr (PREC) {
-            double sum = 0.0;
-#pragma unroll 1
-            for (int e = 0; e < E; ++e) {
-                const float v = El::to_float(reinterpret_cast<const typename El::raw*>(buf + j)[e]);
-                if (!FILT || v > thr || (v == thr && id_of(j, e) <= cut)) sum += weight<true>(v, ref, r);
-            }
-            return sum;
-        } else {
-            float x[E], p[E];
-            El::unpack(buf[j], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                p[e] = ex2_approx((x[e] - ref) * r.c);
-                if (FILT && !(x[e] > thr || (x[e] == thr && id_of(j, e) <= cut))) p[e] = 0.0f;
-            }
-#pragma unroll
-            for (int d = E / 2; d > 0; d >>= 1)
-#pragma unroll
-                for (int e = 0; e < d; ++e) p[e] += p[e + d];
-            return (double)p[0];
-        }
-    }
-
-    // per-warp sums of e into c.dwarp; returns the segment's sum
-    template <bool PREC, bool FILT>
-    __device__ double segment_sum(float ref, float thr, int cut, const Row& r) {
-        double sum = 0.0;
-        if (ref != -INFINITY)
-            for (int j = w0 + lane; j < w1; j += 32) sum += vec_sum<PREC, FILT>(j, ref, thr, cut, r);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
-        __syncthreads();
-        if (lane == 0) c.dwarp[warp] = sum;
-        __syncthreads();
-        double total = 0.0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) total += c.dwarp[w];
-        return total;
-    }
-
-    // cluster-wide sum of e over the kept elements, relative to zmax, in fp64
-    __device__ double row_sum_exact(float thr, int cut, const Row& r) {
-        Xch mine = {};
-        mine.a = segment_sum<true, true>(r.zmax, thr, cut, r);
-        const Xch* x = exchange(mine);
-        double total = 0.0;
-        for (int q = 0; q < CL; ++q) total += x[q].a;
-        return total;
-    }
-
-    // cluster-wide number of ids with value > thr and == thr
-    __device__ void row_count(float thr, long long* above, long long* equal) {
-        int n = 0, m = 0;
-        for (int j = w0 + lane; j < w1; j += 32) {
-            float x[E];
-            El::unpack(buf[j], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const bool ok = is_id(id_of(j, e));
-                n += (ok && x[e] > thr) ? 1 : 0;
-                m += (ok && x[e] == thr) ? 1 : 0;
-            }
-        }
-        Xch mine = {};
-        mine.n = block_reduce<W>(n, c.ipart, Plus());
-        mine.i = block_reduce<W>(m, c.ipart, Plus());
-        const Xch* x = exchange(mine);
-        *above = *equal = 0;
-        for (int q = 0; q < CL; ++q) { *above += x[q].n; *equal += x[q].i; }
-    }
-
-    // id of the nth (from 0) id, ascending, whose value is thr
-    __device__ int nth_equal(float thr, long long nth) {
-        int m = 0;
-        for (int j = w0 + lane; j < w1; j += 32) {
-            float x[E];
-            El::unpack(buf[j], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) m += (x[e] == thr && is_id(id_of(j, e))) ? 1 : 0;
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) m += __shfl_xor_sync(PODS_FULL_MASK, m, d);
-        __syncthreads();
-        if (lane == 0) c.iwarp[warp] = m;
-        if (tid == 0) c.found = -1;
-        __syncthreads();
-        Xch mine = {};
-        for (int w = 0; w < W; ++w) mine.n += c.iwarp[w];
-        const Xch* x = exchange(mine);
-        long long before = 0;
-        for (int q = 0; q < rank; ++q) before += x[q].n;
-        for (int w = 0; w < warp; ++w) before += c.iwarp[w];
-        if (nth >= before && nth < before + c.iwarp[warp]) {
-            for (int k = w0; k < w1; k += 32) {
-                const int j = k + lane;
-                int mine_n = 0;
-                float x[E];
-                if (j < w1) {
-                    El::unpack(buf[j], x);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) mine_n += (x[e] == thr && is_id(id_of(j, e))) ? 1 : 0;
-                }
-                int incl = mine_n;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int o = __shfl_up_sync(PODS_FULL_MASK, incl, d);
-                    if (lane >= d) incl += o;
-                }
-                const int total = __shfl_sync(PODS_FULL_MASK, incl, 31);
-                if (nth < before + total) {
-                    long long at = before + incl - mine_n;
-                    if (nth >= at && nth < at + mine_n)
-                        for (int e = 0; e < E; ++e) {
-                            const float v = El::to_float(reinterpret_cast<const typename El::raw*>(buf + j)[e]);
-                            if (v == thr && is_id(id_of(j, e))) {
-                                if (at == nth) c.found = id_of(j, e);
-                                ++at;
-                            }
-                        }
-                    break;
-                }
-                before += total;
-            }
-        }
-        __syncthreads();
-        Xch out = {};
-        out.i = c.found;
-        x = exchange(out);
-        int id = -1;
-        for (int q = 0; q < CL; ++q) id = max(id, x[q].i);
-        return id;
-    }
-
-    // Threshold of the first `count` ids of the order: value and highest id kept among the ids equal to it.
-    __device__ void count_threshold(long long count, float zmax, float* thr, int* cut) {
-        uint32_t lo = El::to_key(-INFINITY), hi = El::to_key(zmax) + 1;        // ids >= lo: all; >= hi: none
-        long long above, equal;
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            row_count(El::from_key(mid), &above, &equal);
-            if (above + equal >= count) lo = mid; else hi = mid;
-        }
-        *thr = El::from_key(lo);
-        row_count(*thr, &above, &equal);
-        const long long need = count - above;
-        *cut = need >= equal ? kNoCut : nth_equal(*thr, need - 1);
-    }
-
-    // Shrinks (thr, cut) to the smallest prefix whose sum of e reaches `mass`.
-    __device__ void mass_threshold(double mass, const Row& r, float* thr, int* cut) {
-        uint32_t lo = El::to_key(*thr), hi = El::to_key(r.zmax) + 1;
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (row_sum_exact(El::from_key(mid), kNoCut, r) >= mass) lo = mid; else hi = mid;
-        }
-        const float v = El::from_key(lo);
-        long long above, equal;
-        row_count(v, &above, &equal);
-        // everything above v: v itself with no id of its own
-        const double more = mass - row_sum_exact(v, -1, r);
-        const double ev = exp(((double)v - (double)r.zmax) * r.tau_inv);
-        double need = ev > 0.0 ? ceil(more / ev) : (double)equal;
-        if (need < 1.0) need = 1.0;
-        if (v > *thr) {
-            *thr = v;
-            *cut = need >= (double)equal ? kNoCut : nth_equal(v, (long long)need - 1);
-        } else if (need < (double)equal) {
-            const int id = nth_equal(v, (long long)need - 1);
-            *cut = min(*cut, id);
-        }
-    }
-
-    // The first kept id whose running sum exceeds `target`; warp sums in c.dwarp are relative to `ref`, `target` and
-    // `before` (the sum ahead of this segment) too.  Result in c.found (-1: not in this segment), with the sums around it.
-    template <bool PREC, bool FILT>
-    __device__ void locate(double target, double before, float ref, float thr, int cut, const Row& r) {
-        if (tid == 0) c.found = -1;
-        __syncthreads();
-        int last = -1;                                          // the last warp with any weight takes what rounding leaves
-        for (int w = 0; w < W; ++w)
-            if (c.dwarp[w] > 0.0) last = w;
-        double b = before;
-        int mine = -1;
-        for (int w = 0; w <= last; ++w) {
-            if (target < b + c.dwarp[w] || w == last) { mine = w; break; }
-            b += c.dwarp[w];
-        }
-        if (warp == mine) {
-            int best = -1;
-            double best_before = 0.0, best_e = 0.0;
-            bool done = false;
-            for (int k = w0; k < w1 && !done; k += 32) {
-                const int j = k + lane;
-                const double sum = j < w1 ? vec_sum<PREC, FILT>(j, ref, thr, cut, r) : 0.0;
-                double incl = sum;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const double o = __shfl_up_sync(PODS_FULL_MASK, incl, d);
-                    if (lane >= d) incl += o;
-                }
-                const double total = __shfl_sync(PODS_FULL_MASK, incl, 31);
-                const bool past = b + incl > target && sum > 0.0;
-                const uint32_t hit = __ballot_sync(PODS_FULL_MASK, past);
-                const uint32_t any = __ballot_sync(PODS_FULL_MASK, sum > 0.0);
-                // the vector that crosses the target; otherwise remember the last one with weight
-                const int from = hit ? __ffs(hit) - 1 : (any ? 31 - __clz(any) : -1);
-                if (from >= 0) {
-                    if (lane == from) {
-                        double run = b + incl - sum;
-                        for (int e = 0; e < E; ++e) {
-                            const float v = El::to_float(reinterpret_cast<const typename El::raw*>(buf + j)[e]);
-                            const int id = id_of(j, e);
-                            if (!is_id(id) || (FILT && !(v > thr || (v == thr && id <= cut)))) continue;
-                            const double ev = weight<PREC>(v, ref, r);
-                            if (!(ev > 0.0)) continue;
-                            best = id;
-                            best_before = run;
-                            best_e = ev;
-                            run += ev;
-                            if (run > target) break;
-                        }
-                    }
-                    best = __shfl_sync(PODS_FULL_MASK, best, from);
-                    best_before = __shfl_sync(PODS_FULL_MASK, best_before, from);
-                    best_e = __shfl_sync(PODS_FULL_MASK, best_e, from);
-                }
-                done = hit != 0;
-                b += total;
-            }
-            if (lane == 0) {
-                c.found = best;
-                c.found_before = best_before;
-                c.found_e = best_e;
-            }
-        }
-        __syncthreads();
-    }
-
-    // Draw over the kept set in fp64; every thread of the cluster gets the token and the kept sum.
-    __device__ int draw_exact(double u, float thr, int cut, const Row& r, double* kept) {
-        Xch mine = {};
-        mine.a = segment_sum<true, true>(r.zmax, thr, cut, r);
-        const Xch* x = exchange(mine);
-        double total = 0.0;
-        for (int q = 0; q < CL; ++q) total += x[q].a;
-        const double target = u * total;
-        double before = 0.0;
-        int last = -1, owner = -1;
-        for (int q = 0; q < CL; ++q)
-            if (x[q].a > 0.0) last = q;
-        for (int q = 0; q <= last; ++q) {
-            if (target < before + x[q].a || q == last) { owner = q; break; }
-            before += x[q].a;
-        }
-        if (rank == owner) locate<true, true>(target, before, r.zmax, thr, cut, r);
-        __syncthreads();
-        Xch out = {};
-        out.i = rank == owner ? c.found : -1;
-        x = exchange(out);
-        int id = -1;
-        for (int q = 0; q < CL; ++q) id = max(id, x[q].i);
-        *kept = total;
-        return id;
-    }
-
-    // Lists the kept (value, id) pairs of the segment: (order32(value) << 32) | ~id, larger first in the row's order.
-    // The count may exceed the room; only list_cap entries are stored.
-    __device__ void list_segment(float thr, int cut) {
-        __syncthreads();
-        if (tid == 0) c.n_list = 0;
-        __syncthreads();
-        for (int j = w0 + lane; j < w1; j += 32) {
-            const uint4 q = buf[j];
-            if (El::vec_max(q) < thr) continue;
-            float x[E];
-            El::unpack(q, x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int id = id_of(j, e);
-                if (is_id(id) && (x[e] > thr || (x[e] == thr && id <= cut))) {
-                    const int at = atomicAdd(&c.n_list, 1);
-                    if (at < a.list_cap) list[at] = ((unsigned long long)order32(x[e]) << 32) | (uint32_t)~id;
-                }
-            }
-        }
-        __syncthreads();
-    }
-
-    // The cluster's list in the first CTA, sorted in the row's order; returns its length, or -1 if it does not fit.
-    // Ends without a barrier after the first CTA's reads of its peers: an exchange has to follow.
-    __device__ int gather_sorted(float thr, int cut) {
-        list_segment(thr, cut);
-        Xch mine = {};
-        mine.n = c.n_list;
-        const Xch* x = exchange(mine);
-        long long total = 0;
-        for (int q = 0; q < CL; ++q) total += x[q].n;
-        if (total > a.list_cap) return -1;
-        if (rank == 0) {
-            int at = x[0].n;
-            for (int q = 1; q < CL; ++q) {
-                const unsigned long long* peer = cl.map_shared_rank(list, q);
-                for (int k = tid; k < x[q].n; k += kThreads) list[at + k] = peer[k];
-                at += x[q].n;
-            }
-            sort_list((int)total, true);
-        }
-        return (int)total;
-    }
-
-    // Bitonic sort of list[0, n), padded with the value that sorts last; the whole CTA.
-    __device__ void sort_list(int n, bool descending) {
-        int m = 1;
-        while (m < n) m <<= 1;
-        for (int k = n + tid; k < m; k += kThreads) list[k] = descending ? 0ull : ~0ull;
-        __syncthreads();
-        for (int size = 2; size <= m; size <<= 1)
-            for (int d = size >> 1; d > 0; d >>= 1) {
-                for (int k = tid; k < m / 2; k += kThreads) {
-                    const int i = 2 * k - (k & (d - 1)), p = i + d;
-                    const unsigned long long x = list[i], y = list[p];
-                    const bool up = ((i & size) == 0) != descending;
-                    if ((x > y) == up) { list[i] = y; list[p] = x; }
-                }
-                __syncthreads();
-            }
-    }
-
-    // The value that at least `want` ids of the row reach (over the CTAs' minimum): my CTA's part of it.
-    __device__ float reach(float lane_max, int want) {
-        const int r = min(32, (want + CL * W - 1) / (CL * W));
-        // lanes sorted by value, descending; lane r-1 holds the r-th largest
-        uint32_t k = order32(lane_max);
-#pragma unroll
-        for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-            for (int d = size >> 1; d > 0; d >>= 1) {
-                const uint32_t o = __shfl_xor_sync(PODS_FULL_MASK, k, d);
-                const bool keep_big = ((lane & size) == 0) == ((lane & d) == 0);
-                k = keep_big ? max(k, o) : min(k, o);
-            }
-        const float v = unorder32(__shfl_sync(PODS_FULL_MASK, k, r - 1));
-        return block_reduce<W>(want > CL * W * 32 ? -INFINITY : v, c.fpart, Min());
-    }
-};
-
-// ---- what both kernels begin with -------------------------------------------------------------------------------------
-
-template <int DT>
-__device__ __forceinline__ void load_row(Worker<DT>& w, int64_t t, uint32_t phase) {
-    w.s = make_segment<DT>(w.a.logits, w.a.ldl, t, w.a.V, w.rank, w.a.seg);
-    const int per = (w.s.cnt + W - 1) / W;
-    w.w0 = min(w.s.cnt, w.warp * per);
-    w.w1 = min(w.s.cnt, w.w0 + per);
-    if (w.tid == 0) start_load<DT>(w.s, w.a.V, w.buf, &w.c.full);
-    if (!mbar_wait(&w.c.full, phase, kSpinLimit) && w.lane == 0) pods_raise(w.a.status, PODS_STATUS_TIMEOUT);
-    __syncthreads();
-}
-
-template <int DT>
-__device__ __forceinline__ float lane_max(const Worker<DT>& w) {
-    float m = -INFINITY;
-    for (int j = w.w0 + w.lane; j < w.w1; j += 32) m = max_nan(m, Elem<DT>::vec_max(w.buf[j]));
-    return m;
-}
-
-// Cluster-wide maximum and fast sum from the CTAs' (maximum, sum relative to it).
-__device__ __forceinline__ void combine(const Xch* x, int CL, Row* r) {
-    float m = x[0].m;
-    for (int q = 1; q < CL; ++q) m = max_nan(m, x[q].m);
-    r->zmax = m + 0.0f;
-    double Z = 0.0;
-    if (fabsf(m) < INFINITY)
-        for (int q = 0; q < CL; ++q)
-            if (x[q].m > -INFINITY) Z += x[q].a * exp(((double)x[q].m - (double)r->zmax) * r->tau_inv);
-    r->Z = Z;
-}
-
-// Inclusive scan of v over the CTA in thread order; *total is the sum.
-__device__ __forceinline__ double block_scan(double v, double* part, double* total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const double o = __shfl_up_sync(PODS_FULL_MASK, v, d);
-        if (lane >= d) v += o;
-    }
-    __syncthreads();
-    if (lane == 31) part[warp] = v;
-    __syncthreads();
-    double before = 0.0, all = 0.0;
-    for (int w = 0; w < W; ++w) {
-        if (w < warp) before += part[w];
-        all += part[w];
-    }
-    *total = all;
-    return v + before;
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kThreads)
-pods_sample_kernel(const SampleArgs a) {
-    extern __shared__ __align__(128) unsigned char smem[];
-    Ctrl& c = *reinterpret_cast<Ctrl*>(smem);
-    unsigned long long* const list = reinterpret_cast<unsigned long long*>(smem + kCtrlBytes);
-    uint4* const buf = reinterpret_cast<uint4*>(smem + kCtrlBytes + (size_t)a.list_cap * 8);
-    Worker<DT> w(a, c, buf, list);
-    const int CL = w.CL, tid = w.tid;
-    if (tid == 0) {
-        mbar_init(&c.full, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-    w.cl.sync();                                       // every CTA of the cluster runs before its shared memory is written
-
-    const int64_t n_clusters = gridDim.x / CL;
-    uint32_t phase = 0;
-    for (int64_t t = blockIdx.x / CL; t < a.T; t += n_clusters) {
-        if (a.mask != nullptr && a.mask[t] == 0) continue;
-        load_row(w, t, phase);
-        phase ^= 1u;
-
-        // the row's settings
-        float tau = a.temperature_row ? a.temperature_row[t] : a.temperature;
-        float top_p = a.top_p_row ? a.top_p_row[t] : a.top_p;
-        float min_p = a.min_p_row ? a.min_p_row[t] : a.min_p;
-        const int top_k_in = a.top_k_row ? a.top_k_row[t] : a.top_k;
-        float u = a.u[t];
-        bool odd = false;
-        if (!(tau >= 0.0f) || tau == INFINITY) { tau = 1.0f; odd = true; }
-        if (top_p != top_p) { top_p = 1.0f; odd = true; }
-        if (min_p != min_p) { min_p = 0.0f; odd = true; }
-        if (!(u >= 0.0f)) { u = 0.0f; odd = true; }
-        if (!(u < 1.0f)) { u = 0x1.fffffep-1f; odd = true; }
-        if (odd && w.rank == 0 && tid == 0) pods_raise(a.status, PODS_STATUS_PARAM_RANGE);
-        const bool greedy = tau < kGreedyBelow;
-        if (greedy) tau = 1.0f;
-        const long long top_k = (top_k_in <= 0 || top_k_in >= a.V) ? 0 : top_k_in;
-        min_p = fminf(min_p, 1.0f);
-        const bool nucleus = top_p < 1.0f, floor = min_p > 0.0f;
-        const bool filtered = !greedy && (top_k > 0 || nucleus || floor);
-
-        Row r;
-        r.tau_inv = 1.0 / (double)tau;
-        r.c = (float)(1.4426950408889634 * r.tau_inv);
-
-        const float lm = lane_max(w);
-        Xch mine = {};
-        mine.m = block_reduce<W>(lm, c.fpart, MaxNan());
-        const float ref = fabsf(mine.m) < INFINITY ? mine.m : -INFINITY;     // no sums where they mean nothing
-        mine.a = w.template segment_sum<false, false>(ref, 0.0f, 0, r);
-        const int want = (int)(top_k > 0 ? (top_k < 512 ? top_k : 512) : 256);
-        mine.lim = filtered ? w.reach(lm, want) : 0.0f;
-        const Xch* x = w.exchange(mine);
-        combine(x, CL, &r);
-
-        int token = -1;
-        double logq = 0.0;
-        bool have = false;                             // token and logq are valid in the first CTA
-        if (!(r.zmax < INFINITY) || r.zmax == -INFINITY) {
-            const bool empty = r.zmax == -INFINITY;
-            if (w.rank == 0 && tid == 0) {
-                a.tokens[t] = -1;
-                const float v = empty ? -INFINITY : NAN;
-                if (a.logp) a.logp[t] = v;
-                if (a.logq) a.logq[t] = v;
-                pods_raise(a.status, empty ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
-            }
-        } else {
-            if (greedy) {
-                int id = kNoCut;
-                for (int j = w.w0 + w.lane; j < w.w1; j += 32) {
-                    if (Elem<DT>::vec_max(buf[j]) != r.zmax) continue;
-                    float v[Elem<DT>::E];
-                    Elem<DT>::unpack(buf[j], v);
-#pragma unroll
-                    for (int e = Elem<DT>::E - 1; e >= 0; --e)
-                        if (v[e] == r.zmax) id = min(id, w.id_of(j, e));
-                }
-                Xch out = {};
-                out.i = block_reduce<W>(id, c.ipart, Min());
-                x = w.exchange(out);
-                token = kNoCut;
-                for (int q = 0; q < CL; ++q) token = min(token, x[q].i);
-                logq = 0.0;
-                have = true;
-            } else if (!filtered) {
-                // the CTA that holds the target
-                const double target = (double)u * r.Z;
-                double before = 0.0, scale = 1.0;
-                int owner = -1, last = -1;
-                for (int q = 0; q < CL; ++q)
-                    if (x[q].a > 0.0) last = q;
-                for (int q = 0; q <= last; ++q) {
-                    scale = exp(((double)x[q].m - (double)r.zmax) * r.tau_inv);
-                    if (target < before + x[q].a * scale || q == last) { owner = q; break; }
-                    before += x[q].a * scale;
-                }
-                Xch out = {};
-                out.i = -1;
-                out.n = 0;
-                if (w.rank == owner) {
-                    w.template locate<false, false>(target / scale, before / scale, ref, 0.0f, 0, r);
-                    const double lo = c.found_before * scale, hi = lo + c.found_e * scale;
-                    // an edge of the running sum closer than the margin is decided in fp64 (the row's start is no edge)
-                    out.n = (target - lo > draw_margin(a.V, r.Z) || lo == 0.0) && hi - target > draw_margin(a.V, r.Z) ? 1 : 0;
-                    out.i = c.found;
-                }
-                x = w.exchange(out);
-                int sure = 0;
-                for (int q = 0; q < CL; ++q) { token = max(token, x[q].i); sure |= x[q].n; }
-                double kept = r.Z;
-                if (!sure) token = w.draw_exact((double)u, -INFINITY, kNoCut, r, &kept);
-                logq = -log(kept);
-                have = true;
-            } else {
-                float lim = x[0].lim;
-                for (int q = 1; q < CL; ++q) lim = fminf(lim, x[q].lim);
-                // the lowest value that min_p admits
-                const float zfloor = floor ? __double2float_ru((double)r.zmax + (double)tau * log((double)min_p)) : -INFINITY;
-                // top_p is a share of the whole top-k sum, so min_p may not shorten the list where both are set
-                if (floor && !(top_k > 0 && nucleus)) lim = (top_k > 0 || nucleus) ? fmaxf(lim, zfloor) : zfloor;
-                const int n = w.gather_sorted(lim, kNoCut);
-                const bool whole = n == a.V;                                 // the list is the row
-                const bool to_floor = floor && lim == zfloor;                // the list holds all that min_p admits
-                if (w.rank == 0) {
-                    if (tid == 0) c.found = -1;
-                    __syncthreads();
-                    // does the list settle the kept set?  (a nucleus that it does not reach is found out below)
-                    bool ok = n > 0 && (top_k == 0 || n >= top_k || whole || (to_floor && !nucleus));
-                    if (ok) {
-                        // prefix sums in the row's order, 4 entries a thread and step
-                        const int lim_n = top_k > 0 && top_k < n ? (int)top_k : n;
-                        constexpr int PT = kSampleList / kThreads;
-                        const int per = PT;
-                        double run[PT];
-                        double sum = 0.0;
-#pragma unroll
-                        for (int k = 0; k < PT; ++k) {
-                            const int i = tid * per + k;
-                            if (i < lim_n) sum += exp(((double)unorder32((uint32_t)(list[i] >> 32)) - (double)r.zmax) * r.tau_inv);
-                            run[k] = sum;
-                        }
-                        double total;
-                        const double incl = block_scan(sum, c.dpart, &total);
-                        const double base = incl - sum;
-                        // the nucleus: the first entry whose running sum reaches top_p of the (top-k) sum
-                        int count = lim_n;
-                        if (nucleus) {
-                            const bool over_list = top_k > 0 || whole;
-                            const double goal = (double)top_p * (over_list ? total : r.Z);
-                            const double slack = over_list ? 0.0 : draw_margin(a.V, r.Z);
-                            int first = kNoCut, unsure = 0;
-#pragma unroll
-                            for (int k = 0; k < PT; ++k) {
-                                const int i = tid * per + k;
-                                if (i < lim_n) {
-                                    const double at = base + run[k];
-                                    if (at >= goal && first == kNoCut) first = i;
-                                    if (slack > 0.0 && fabs(at - goal) <= slack) unsure = 1;
-                                }
-                            }
-                            first = block_reduce<W>(first, c.ipart, Min());
-                            unsure = block_reduce<W>(unsure, c.ipart, Plus());
-                            if (unsure) ok = false;
-                            if (first < kNoCut) count = first + 1;
-                            else if (!over_list && !to_floor) ok = false;    // the nucleus goes on below the list
-                        }
-                        // min_p: entries are sorted, so the admitted ones are a prefix
-                        if (floor) {
-                            int m = 0;
-#pragma unroll
-                            for (int k = 0; k < PT; ++k) {
-                                const int i = tid * per + k;
-                                if (i < count && unorder32((uint32_t)(list[i] >> 32)) >= zfloor) ++m;
-                            }
-                            m = block_reduce<W>(m, c.ipart, Plus());
-                            count = max(1, min(count, m));
-                        }
-                        if (ok) {
-                            // back into id order, and the draw
-                            __syncthreads();
-                            for (int i = tid; i < count; i += kThreads) {
-                                const unsigned long long k = list[i];
-                                list[i] = ((unsigned long long)~(uint32_t)k << 32) | (k >> 32);
-                            }
-                            w.sort_list(count, false);
-                            double s2 = 0.0;
-#pragma unroll
-                            for (int k = 0; k < PT; ++k) {
-                                const int i = tid * per + k;
-                                if (i < count) s2 += exp(((double)unorder32((uint32_t)list[i]) - (double)r.zmax) * r.tau_inv);
-                                run[k] = s2;
-                            }
-                            const double incl2 = block_scan(s2, c.dpart, &total);
-                            const double target = (double)u * total;
-                            int pick = kNoCut;
-#pragma unroll
-                            for (int k = 0; k < PT; ++k) {
-                                const int i = tid * per + k;
-                                if (i < count && pick == kNoCut && incl2 - s2 + run[k] > target) pick = i;
-                            }
-                            pick = block_reduce<W>(pick, c.ipart, Min());
-                            if (pick >= count) pick = count - 1;
-                            token = (int)(uint32_t)(list[pick] >> 32);
-                            logq = -log(total);
-                        }
-                    }
-                    if (tid == 0) c.found = ok ? token : -1;
-                    __syncthreads();
-                }
-                Xch out = {};
-                out.i = w.rank == 0 ? c.found : -1;
-                x = w.exchange(out);
-                if (x[0].i < 0) {
-                    float thr = -INFINITY;
-                    int cut = kNoCut;
-                    if (top_k > 0) w.count_threshold(top_k, r.zmax, &thr, &cut);
-                    if (nucleus) {
-                        const double total = w.row_sum_exact(thr, cut, r);
-                        w.mass_threshold((double)top_p * total, r, &thr, &cut);
-                    }
-                    if (zfloor > thr) { thr = zfloor; cut = kNoCut; }
-                    double kept;
-                    token = w.draw_exact((double)u, thr, cut, r, &kept);
-                    logq = -log(kept);
-                }
-                have = true;
-            }
-            // the owner of the token's logit writes the row's results
-            if (have && w.rank == 0 && tid == 0) {
-                a.tokens[t] = token;
-                const typename Elem<DT>::raw* row = static_cast<const typename Elem<DT>::raw*>(a.logits) + t * a.ldl;
-                const int safe = token < 0 ? 0 : token;
-                const double d = ((double)Elem<DT>::to_float(row[PODS_CLAMPED(safe, a.V, a.status)]) - (double)r.zmax) * r.tau_inv;
-                if (a.logp) a.logp[t] = (float)(d - log(r.Z));
-                if (a.logq) a.logq[t] = greedy ? 0.0f : (float)(d + logq);
-            }
-        }
-        fence_async_proxy();                           // the buffer is refilled by bulk copies
-        __syncthreads();
-    }
-    w.cl.sync();                                       // no CTA leaves while a peer may still reach its shared memory
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kThreads)
-pods_topk_kernel(const SampleArgs a) {
-    extern __shared__ __align__(128) unsigned char smem[];
-    Ctrl& c = *reinterpret_cast<Ctrl*>(smem);
-    unsigned long long* const list = reinterpret_cast<unsigned long long*>(smem + kCtrlBytes);
-    uint4* const buf = reinterpret_cast<uint4*>(smem + kCtrlBytes + (size_t)a.list_cap * 8);
-    Worker<DT> w(a, c, buf, list);
-    const int CL = w.CL, tid = w.tid;
-    if (tid == 0) {
-        mbar_init(&c.full, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-    w.cl.sync();
-
-    const int64_t n_clusters = gridDim.x / CL;
-    uint32_t phase = 0;
-    for (int64_t t = blockIdx.x / CL; t < a.T; t += n_clusters) {
-        if (a.mask != nullptr && a.mask[t] == 0) continue;
-        load_row(w, t, phase);
-        phase ^= 1u;
-        Row r;
-        r.tau_inv = 1.0 / (double)a.temperature;
-        r.c = (float)(1.4426950408889634 * r.tau_inv);
-        const float lm = lane_max(w);
-        Xch mine = {};
-        mine.m = block_reduce<W>(lm, c.fpart, MaxNan());
-        const float ref = fabsf(mine.m) < INFINITY ? mine.m : -INFINITY;
-        if (a.lse != nullptr) mine.a = w.template segment_sum<false, false>(ref, 0.0f, 0, r);
-        mine.lim = w.reach(lm, a.K);
-        const Xch* x = w.exchange(mine);
-        combine(x, CL, &r);
-        if (r.zmax != r.zmax || r.zmax == INFINITY) {
-            if (w.rank == 0) {
-                for (int i = tid; i < a.K; i += kThreads) {
-                    a.ids[t * a.K + i] = -1;
-                    a.values[t * a.K + i] = NAN;
-                }
-                if (tid == 0) {
-                    if (a.lse) a.lse[t] = NAN;
-                    pods_raise(a.status, PODS_STATUS_NONFINITE_LOGIT);
-                }
-            }
-        } else {
-            float lim = x[0].lim;
-            for (int q = 1; q < CL; ++q) lim = fminf(lim, x[q].lim);
-            int n = w.gather_sorted(lim, kNoCut);
-            if (n < a.K) {                             // too many reach it: the exact threshold
-                float thr;
-                int cut;
-                w.count_threshold(a.K, r.zmax, &thr, &cut);
-                n = w.gather_sorted(thr, cut);
-            }
-            if (w.rank == 0) {
-                for (int i = tid; i < a.K; i += kThreads) {
-                    const unsigned long long k = list[i];
-                    if (PODS_INDEX_OK(i, n, a.status)) {
-                        a.ids[t * a.K + i] = (int32_t)~(uint32_t)k;
-                        a.values[t * a.K + i] = unorder32((uint32_t)(k >> 32));
-                    }
-                }
-                if (tid == 0 && a.lse) a.lse[t] = r.zmax == -INFINITY ? -INFINITY : (float)((double)r.zmax * r.tau_inv + log(r.Z));
-                if (tid == 0 && r.zmax == -INFINITY) pods_raise(a.status, PODS_STATUS_EMPTY_ROW);
-            }
-            w.exchange(mine);                          // the first CTA has read its peers' lists
-        }
-        fence_async_proxy();
-        __syncthreads();
-    }
-    w.cl.sync();
-}
-
-// ---- no filters: the whole policy -------------------------------------------------------------------------------------
-// Lanes own contiguous vectors of the segment, so a lane's, a warp's and a CTA's sums are stretches of the running sum.
-// Each warp reduces its part to a sum relative to 2^R, R the integer above its maximum's exponent, and hands the pair to
-// every CTA of the cluster; parts are then brought together by powers of two, exactly and without an exponential.  After
-// the one cluster barrier of a row every warp knows all parts in id order, and so whether the drawn point is in its own;
-// the warp that has it takes the lane from the lane sums that it kept and evaluates that lane's few vectors again.  Rows
-// whose draw lies within draw_margin of an edge are marked in every CTA of the cluster and taken in fp64 at the end.
-// 152 K bf16 vocabulary, 512 rows: ORIGINAL
-
-struct Part {
-    double s;             // sum relative to the part's reference (to its maximum, the second time round)
-    float m;              // its maximum
-    int pad;
-};
-
-constexpr int kRedoRows = 8192;               // rows of a cluster between two visits of the marked ones
-
-struct PolicyCtrl {
-    unsigned long long full;
-    Part part[2][kMaxCluster * W];
+    Part part[2][kMaxCluster * W];            // exchanges alternate between two places, so that one barrier each is enough
     uint32_t redo[kRedoRows / 32];
+    uint32_t top[kThreads];                   // the lanes' maxima, as keys
 };
-constexpr int kPolicyCtrlBytes = (sizeof(PolicyCtrl) + 127) & ~127;
+struct FilterCtrl {
+    Xch x[2][kMaxCluster];
+    double dpart[W];
+    int ipart[W];
+    int n_list, found, sure;
+    int start[kMaxCluster], count[kMaxCluster];  // the CTAs' lists within `all`
+    double weight;
+};
+// Shared memory: RowCtrl, the row's segment, FilterCtrl, lists.  Reached through the array's name wherever it is used, so that
+// every access is known to be to shared memory.
+extern __shared__ __align__(128) unsigned char smem_[];
+constexpr int kRowCtrlBytes = (sizeof(RowCtrl) + 127) & ~127;
+__device__ __forceinline__ RowCtrl& row_ctrl() { return *reinterpret_cast<RowCtrl*>(smem_); }
+__device__ __forceinline__ uint4* row_buf() { return reinterpret_cast<uint4*>(smem_ + kRowCtrlBytes); }
+__device__ __forceinline__ FilterCtrl& filter_ctrl(const SampleArgs& a) { return *reinterpret_cast<FilterCtrl*>(smem_ + kRowCtrlBytes + a.seg * 16); }
+constexpr int kFilterCtrlBytes = (sizeof(FilterCtrl) + 127) & ~127;
 
 __device__ __forceinline__ double pow2(int n) {       // n <= 0; below the normal numbers: 0
     return n < -1000 ? 0.0 : __hiloint2double((1023 + n) << 20, 0);
@@ -910,235 +146,1037 @@ struct PartRef {
         if (!top.far) return pow2((int)fmaxf(R - top.R, -2000.0f));
         return exp2((far ? (double)m * (double)c : (double)R) - (double)top.m * (double)c);
     }
+    // ln of this reference's own weight over e^(m / tau): what log sums relative to it lack
+    __device__ __forceinline__ double log_offset() const { return far ? 0.0 : ((double)R - (double)m * (double)c) * kLn2; }
 };
 
 // Inclusive scan over a warp.
-__device__ __forceinline__ double warp_scan(double v, int lane) {
+template <typename T>
+__device__ __forceinline__ T warp_scan(T v, int lane) {
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const double o = __shfl_up_sync(PODS_FULL_MASK, v, d);
+        const T o = __shfl_up_sync(PODS_FULL_MASK, v, d);
         if (lane >= d) v += o;
     }
     return v;
 }
 
+// Inclusive scan over the CTA in thread order; *total is the sum.
+__device__ __forceinline__ double block_scan(double v, double* part, double* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    v = warp_scan(v, lane);
+    __syncthreads();
+    if (lane == 31) part[warp] = v;
+    __syncthreads();
+    double before = 0.0, all = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < warp) before += part[w];
+        all += part[w];
+    }
+    *total = all;
+    return v + before;
+}
+
+// Sorts list[0, n) ascending, n <= kSampleList; keys differ.  Few entries are ranked, each against all; many go through a
+// bitonic network in registers (four a thread), of which only the steps across warps need shared memory.
+__device__ __forceinline__ void sort_list(unsigned long long* list, int n) {
+    const int tid = threadIdx.x;
+    if (n <= kThreads) {
+        int P = 1;
+        while (P < 32 && n * P * 2 <= kThreads) P *= 2;
+        const int i = tid / P, sub = tid & (P - 1);
+        const unsigned long long key = i < n ? list[i] : 0ull;
+        int r = 0;
+#pragma unroll 4
+        for (int k = sub; k < n; k += P) r += list[k] < key ? 1 : 0;
+        for (int d = 1; d < P; d <<= 1) r += __shfl_xor_sync(PODS_FULL_MASK, r, d);
+        __syncthreads();
+        if (i < n && sub == 0) list[r] = key;
+        __syncthreads();
+        return;
+    }
+    constexpr int PT = kSampleList / kThreads;
+    int m = 1;
+    while (m < n) m <<= 1;
+    unsigned long long v[PT];
+#pragma unroll
+    for (int k = 0; k < PT; ++k) v[k] = tid * PT + k < n ? list[tid * PT + k] : ~0ull;
+    for (int size = 2; size <= m; size <<= 1) {
+        for (int d = size >> 1; d >= PT; d >>= 1) {
+            if (d >= 32 * PT) {
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < PT; ++k) list[tid * PT + k] = v[k];
+                __syncthreads();
+            }
+#pragma unroll
+            for (int k = 0; k < PT; ++k) {
+                const int i = tid * PT + k;
+                const unsigned long long o = d >= 32 * PT ? list[i ^ d] : __shfl_xor_sync(PODS_FULL_MASK, v[k], d / PT);
+                const bool small = ((i & d) == 0) == ((i & size) == 0);
+                v[k] = (o < v[k]) == small ? o : v[k];
+            }
+        }
+#pragma unroll
+        for (int d = PT / 2; d > 0; d >>= 1)
+            if (d < size) {
+#pragma unroll
+                for (int k = 0; k < PT; ++k)
+                    if ((k & d) == 0) {
+                        const bool up = ((tid * PT + k) & size) == 0;
+                        const unsigned long long x = v[k], y = v[k | d];
+                        if ((x > y) == up) { v[k] = y; v[k | d] = x; }
+                    }
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PT; ++k) list[tid * PT + k] = v[k];
+    __syncthreads();
+}
+
+// A row and its cluster.
 template <int DT>
-struct Policy {
+struct Rows {
     using El = Elem<DT>;
     static constexpr int E = El::E;
     const SampleArgs& a;
-    PolicyCtrl& ctl;
-    uint4* const buf;
     cg::cluster_group cl;
     int CL, rank, tid, lane, warp;
     uint32_t phase = 0;
-    int parity = 0;
+    int parity = 0;       // of the next exchange of parts
+    Segment s;
+    int v0, v1;           // my vectors
 
-    __device__ Policy(const SampleArgs& a_, PolicyCtrl& c_, uint4* b_) : a(a_), ctl(c_), buf(b_), cl(cg::this_cluster()) {
+    __device__ __forceinline__ explicit Rows(const SampleArgs& a_) : a(a_), cl(cg::this_cluster()) {
         CL = (int)cl.num_blocks();
         rank = (int)cl.block_rank();
         tid = threadIdx.x;
         lane = tid & 31;
         warp = tid >> 5;
+        if (tid == 0) {
+            mbar_init(&row_ctrl().full, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        for (int i = tid; i < kRedoRows / 32; i += kThreads) row_ctrl().redo[i] = 0;
+        __syncthreads();
+        cl.sync();                                     // every CTA runs before its shared memory is written
     }
 
-    // One row; `mark`: the bit of the row in the marked ones.
-    template <bool PREC>
-    __device__ void row(int64_t t, int mark) {
-        const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
-        if (tid == 0) start_load<DT>(s, a.V, buf, &ctl.full);
-        float tau = a.temperature_row ? a.temperature_row[t] : a.temperature;
-        float u = a.u[t];
-        bool odd = false;
-        if (!(tau >= 0.0f) || tau == INFINITY) { tau = 1.0f; odd = true; }
-        if (!(u >= 0.0f)) { u = 0.0f; odd = true; }
-        if (!(u < 1.0f)) { u = 0x1.fffffep-1f; odd = true; }
-        if (odd && rank == 0 && tid == 0) pods_raise(a.status, PODS_STATUS_PARAM_RANGE);
-        const bool greedy = tau < kGreedyBelow;
-        if (greedy) tau = 1.0f;
-        const double tau_inv = 1.0 / (double)tau;
-        const float c = (float)(1.4426950408889634 * tau_inv);
-        // an odd number of vectors a lane: eight lanes of a 16-byte access then touch all 32 banks once
-        const int per = ((s.cnt + kThreads - 1) / kThreads) | 1;
-        const int v0 = min(s.cnt, tid * per), v1 = min(s.cnt, v0 + per);
-        if (!mbar_wait(&ctl.full, phase, kSpinLimit) && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
+    __device__ __forceinline__ void start(int64_t t) {
+        s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+        if (tid == 0) start_load<DT>(s, a.V, row_buf(), &row_ctrl().full);
+        // a warp's share is contiguous, and so is a lane's: an odd number of vectors, so that eight lanes of a 16-byte access
+        // touch all 32 banks once
+        const int share = (s.cnt + W - 1) / W, per = ((share + 31) / 32) | 1;
+        const int end = min(s.cnt, (warp + 1) * share);
+        v0 = min(end, warp * share + lane * per);
+        v1 = min(end, v0 + per);
+    }
+    __device__ __forceinline__ void wait() {
+        if (!mbar_wait(&row_ctrl().full, phase, kSpinLimit) && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
         phase ^= 1u;
         __syncthreads();
+    }
+    __device__ __forceinline__ void done() {
+        fence_async_proxy();                           // the buffer is refilled by bulk copies
+        __syncthreads();
+    }
+    __device__ __forceinline__ int id_of(int j, int e) const { return s.id0 + j * E + e; }
+    __device__ __forceinline__ bool is_id(int id) const { return id >= 0 && id < a.V; }
 
+    __device__ __forceinline__ float lane_max() const {
         float m = -INFINITY;
 #pragma unroll 4
-        for (int j = v0; j < v1; ++j) m = max_nan(m, El::vec_max(buf[j]));
+        for (int j = v0; j < v1; ++j) m = max_nan(m, El::vec_max(row_buf()[j]));
+        return m;
+    }
+    static __device__ __forceinline__ float warp_max(float m) {
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(PODS_FULL_MASK, m, d));
-        const PartRef ref(m, c);
+        return m;
+    }
+
+    // e of one logit: fast relative to ref, or fp64 relative to ref's maximum
+    template <bool PREC>
+    __device__ __forceinline__ double weight(float x, const PartRef& ref, double tau_inv) const {
+        return PREC ? exp64(((double)x - (double)ref.m) * tau_inv) : ref.exp1(x);
+    }
+    static __device__ __forceinline__ bool kept(float x, int id, float thr, int cut) { return x > thr || (x == thr && id <= cut); }
+
+    // sum of e over my vectors, of the kept ids only if FILT
+    template <bool PREC, bool FILT>
+    __device__ __forceinline__ double lane_sum(const PartRef& ref, double tau_inv, float thr, int cut) const {
         double sum = 0.0;
-        if (PREC) {
+        if constexpr (PREC) {
+#pragma unroll 1
             for (int j = v0; j < v1; ++j) {
+                const uint4 q = row_buf()[j];
+                if (FILT && El::vec_max(q) < thr) continue;
                 float x[E];
-                El::unpack(buf[j], x);
+                El::unpack(q, x);
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum += exp(((double)x[e] - (double)ref.m) * tau_inv);
+                for (int h = 0; h < E; h += 4) {
+                    double d[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[i] = ((double)x[h + i] - (double)ref.m) * tau_inv;
+                    exp64x4(d);
+                    if (FILT)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) d[i] = kept(x[h + i], id_of(j, h + i), thr, cut) ? d[i] : 0.0;
+                    sum += (d[0] + d[1]) + (d[2] + d[3]);
+                }
             }
         } else {
 #pragma unroll 2
             for (int j = v0; j < v1; ++j) {
-                float x[E];
-                El::unpack(buf[j], x);
-                ref.exps(x);
-                sum += (double)vec_add(x);
+                float x[E], p[E];
+                El::unpack(row_buf()[j], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[e] = x[e];
+                ref.exps(p);
+                if (FILT)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) p[e] = kept(x[e], id_of(j, e), thr, cut) ? p[e] : 0.0f;
+                sum += (double)vec_add(p);
             }
         }
-        const double incl = warp_scan(sum, lane);
-        Part p;
-        p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
-        p.m = m;
-        p.pad = 0;
-        const int mine = rank * W + warp, n_parts = CL * W;
-        if (lane < CL) *cl.map_shared_rank(&ctl.part[parity][mine], lane) = p;
-        cl.sync();
+        return sum;
+    }
 
-        // lane l holds parts [l n, (l + 1) n)
-        const Part* const part = ctl.part[parity];
+    // Hands my warp's part to every CTA; returns the cluster's parts.
+    __device__ __forceinline__ const Part* publish(const Part& p) {
+        Part* const at = row_ctrl().part[parity];
         parity ^= 1;
-        constexpr int N = kMaxCluster * W / 32;
-        const int n = (n_parts + 31) / 32;
-        float z = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < n && lane * n + i < n_parts) z = max_nan(z, part[lane * n + i].m);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) z = max_nan(z, __shfl_xor_sync(PODS_FULL_MASK, z, d));
-        const float zmax = z + 0.0f;
-        if (!(fabsf(z) < INFINITY)) {
-            if (rank == 0 && tid == 0) {
-                const bool empty = z == -INFINITY;
-                a.tokens[t] = -1;
-                const float v = empty ? -INFINITY : NAN;
-                if (a.logp) a.logp[t] = v;
-                if (a.logq) a.logq[t] = v;
-                pods_raise(a.status, empty ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
-            }
-            return;
-        }
-        const PartRef top(zmax, c);
-        double v[N], psum = 0.0;
+        if (lane < CL) *cl.map_shared_rank(at + rank * W + warp, lane) = p;
+        cl.sync();
+        return at;
+    }
+
+    // All parts of a row; lane l of every warp holds parts [l n, (l + 1) n).
+    static constexpr int N = kMaxCluster * W / 32;
+    struct Sums {
+        double v[N], mine, incl, total;
+    };
+    // ONE_REF: the parts are relative to one reference already
+    template <bool PREC, bool ONE_REF>
+    __device__ __forceinline__ Sums sum_parts(const Part* part, const PartRef& top, double tau_inv) const {
+        const int n_parts = CL * W, n = (n_parts + 31) / 32;
+        Sums r;
+        r.mine = 0.0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            v[i] = 0.0;
+            r.v[i] = 0.0;
             if (i < n && lane * n + i < n_parts) {
                 const Part q = part[lane * n + i];
-                if (q.s > 0.0) v[i] = q.s * (PREC ? exp(((double)q.m - (double)zmax) * tau_inv) : PartRef(q.m, c).scale_to(top));
+                if (q.s > 0.0)
+                    r.v[i] = ONE_REF ? q.s
+                             : q.s * (PREC ? exp64(((double)q.m - (double)top.m) * tau_inv) : PartRef(q.m, top.c).scale_to(top));
             }
-            psum += v[i];
+            r.mine += r.v[i];
         }
-        const double pincl = warp_scan(psum, lane);
-        const double Z = __shfl_sync(PODS_FULL_MASK, pincl, 31);
-        const double target = (double)u * Z;
+        r.incl = warp_scan(r.mine, lane);
+        r.total = __shfl_sync(PODS_FULL_MASK, r.incl, 31);
+        return r;
+    }
+    // The part that holds `target` < total, and the sum ahead of it.
+    __device__ __forceinline__ int owner_of(const Sums& r, double target, double* before) const {
+        const int n = (CL * W + 31) / 32;
+        const uint32_t hit = __ballot_sync(PODS_FULL_MASK, r.incl > target && r.mine > 0.0);
+        const int from = hit ? __ffs(hit) - 1 : 0;
         int owner = -1;
-        double before = 0.0;
-        if (greedy) {
-            int first = kNoCut;
-            for (int i = lane; i < n_parts; i += 32)
-                if (part[i].m == zmax) first = min(first, i);
-            owner = __reduce_min_sync(PODS_FULL_MASK, first);
-        } else {
-            const uint32_t hit = __ballot_sync(PODS_FULL_MASK, pincl > target && psum > 0.0);
-            const int from = __ffs(hit) - 1;               // there is one: target < Z
-            double b = pincl - psum, at = b;
+        double b = r.incl - r.mine, at = b;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (v[i] > 0.0 && (owner < 0 || !(b > target))) {  // the first that passes the target, else the last
-                    owner = lane * n + i;
-                    at = b;
-                    b += v[i];
-                }
-            owner = __shfl_sync(PODS_FULL_MASK, owner, from);
-            before = __shfl_sync(PODS_FULL_MASK, at, from);
-        }
-        if (owner != mine) return;
-
-        // ---- the warp with the drawn point ----
-        if (greedy) {
-            int id = kNoCut;
-            for (int j = v0; j < v1; ++j) {
-                float x[E];
-                El::unpack(buf[j], x);
-#pragma unroll
-                for (int e = E - 1; e >= 0; --e)
-                    if (x[e] == zmax) id = min(id, s.id0 + j * E + e);
+        for (int i = 0; i < N; ++i)
+            if (r.v[i] > 0.0 && (owner < 0 || !(b > target))) {    // the first that passes the target, else the last
+                owner = lane * n + i;
+                at = b;
+                b += r.v[i];
             }
-            id = __reduce_min_sync(PODS_FULL_MASK, id);
-            if (lane == 0) {
-                // the sum is relative to 2^R: ln Z over e^zmax
-                const double lz = log(Z) + (PREC || top.far ? 0.0 : ((double)top.R - (double)zmax * (double)c) * 0.6931471805599453);
-                a.tokens[t] = id;
-                if (a.logp) a.logp[t] = (float)-lz;
-                if (a.logq) a.logq[t] = 0.0f;
-            }
-            return;
-        }
-        const double scale = PREC ? exp(((double)m - (double)zmax) * tau_inv) : ref.scale_to(top);
-        const double goal = (target - before) / scale;
+        *before = __shfl_sync(PODS_FULL_MASK, at, from);
+        return __shfl_sync(PODS_FULL_MASK, owner, from);
+    }
+    // Within my warp's part, whose lane sums are `sum` and their scan `incl`: the first id whose running sum exceeds `goal`
+    // (relative to ref).  One lane returns true, with the element, the sum ahead of it and its own e.
+    template <bool PREC, bool FILT>
+    __device__ __forceinline__ bool search(double goal, double sum, double incl, const PartRef& ref, double tau_inv, float thr, int cut,
+                                           int* element, double* lo, double* ev) const {
         uint32_t hit = __ballot_sync(PODS_FULL_MASK, incl > goal && sum > 0.0);
         const uint32_t any = __ballot_sync(PODS_FULL_MASK, sum > 0.0);
+        if (any == 0) return false;
         const int from = hit ? __ffs(hit) - 1 : 31 - __clz(any);
-        const double lane_before = __shfl_sync(PODS_FULL_MASK, incl - sum, from);
-        // the elements of that lane's vectors, K a lane
+        const double ahead = __shfl_sync(PODS_FULL_MASK, incl - sum, from);
+        // the elements of that lane's vectors, k a lane
         const int e0 = __shfl_sync(PODS_FULL_MASK, v0, from) * E, e1 = __shfl_sync(PODS_FULL_MASK, v1, from) * E;
-        const int K = (e1 - e0 + 31) / 32;
-        const typename El::raw* el = reinterpret_cast<const typename El::raw*>(buf);
-        const int k0 = min(e1, e0 + lane * K), k1 = min(e1, k0 + K);
-        auto weight = [&](int i) {
+        const int k = (e1 - e0 + 31) / 32;
+        const int k0 = min(e1, e0 + lane * k), k1 = min(e1, k0 + k);
+        const typename El::raw* el = reinterpret_cast<const typename El::raw*>(row_buf());
+        auto at = [&](int i) {
             const float x = El::to_float(el[i]);
-            return PREC ? exp(((double)x - (double)ref.m) * tau_inv) : ref.exp1(x);
+            return !FILT || kept(x, s.id0 + i, thr, cut) ? weight<PREC>(x, ref, tau_inv) : 0.0;
         };
         double own = 0.0;
-        for (int i = k0; i < k1; ++i) own += weight(i);
+        for (int i = k0; i < k1; ++i) own += at(i);
         const double eincl = warp_scan(own, lane);
-        hit = __ballot_sync(PODS_FULL_MASK, lane_before + eincl > goal && own > 0.0);
+        hit = __ballot_sync(PODS_FULL_MASK, ahead + eincl > goal && own > 0.0);
         const uint32_t some = __ballot_sync(PODS_FULL_MASK, own > 0.0);
-        const int last = hit ? __ffs(hit) - 1 : 31 - __clz(some);
-        if (lane == last) {
-            double run = lane_before + eincl - own, lo = run, ev = 0.0;
-            int at = -1;
-            for (int i = k0; i < k1; ++i) {
-                const double w = weight(i);
-                if (!(w > 0.0)) continue;
-                at = i;
-                lo = run;
-                ev = w;
-                run += w;
-                if (run > goal) break;
+        if (some == 0) return false;
+        if (lane != (hit ? __ffs(hit) - 1 : 31 - __clz(some))) return false;
+        double run = ahead + eincl - own;
+        for (int i = k0; i < k1; ++i) {
+            const double w = at(i);
+            if (!(w > 0.0)) continue;
+            *element = i;
+            *lo = run;
+            *ev = w;
+            run += w;
+            if (run > goal) break;
+        }
+        return true;
+    }
+    // An edge of the running sum nearer than the margin is decided in fp64 (the row's start is no edge).
+    __device__ __forceinline__ bool certain(double u, double target, double lo, double ev, double total, const PartRef& top, double tau_inv) const {
+        const double margin = draw_margin(u, total, deep_error(a.V, total, top.c, tau_inv, top.far));
+        return (target - lo > margin || lo == 0.0) && lo + ev - target > margin;
+    }
+
+    // A value that at least ceil(want / CL) logits of the segment reach, so the least one of the cluster is reached by `want`
+    // logits of the row: that many lanes' maxima reach it.  The first warp finds it among the lanes' maxima by bisection, on
+    // the upper half of the keys (a slightly lower value is as good); the other warps get +inf and go on.
+    __device__ __forceinline__ float reach(float lane_m, int want) const {
+        constexpr int M = kThreads / 32;
+        const int r = (want + CL - 1) / CL;
+        row_ctrl().top[tid] = order32(lane_m) >> 16;
+        __syncthreads();
+        if (warp != 0) return INFINITY;
+        if (r > kThreads) return -INFINITY;
+        uint32_t key[M];
+#pragma unroll
+        for (int k = 0; k < M; ++k) key[k] = row_ctrl().top[lane + 32 * k];
+        uint32_t lo = 0;                               // reached by r lanes (0: by all)
+#pragma unroll 1
+        for (int bit = 15; bit >= 0; --bit) {
+            const uint32_t mid = lo | (1u << bit);
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < M; ++k) n += (int)(key[k] >= mid);
+            if ((int)__reduce_add_sync(PODS_FULL_MASK, (unsigned)n) >= r) lo = mid;
+        }
+        const float v = unorder32(lo << 16);
+        return v >= -3.4028235e38f ? v : -INFINITY;    // below the finite numbers: every id
+    }
+    __device__ __forceinline__ float row_max(const Part* part) const {
+        float z = -INFINITY;
+        for (int i = lane; i < CL * W; i += 32) z = max_nan(z, part[i].m);
+        return warp_max(z) + 0.0f;
+    }
+    __device__ __forceinline__ float limit(const Part* part) const {
+        float l = INFINITY;
+        for (int i = lane; i < CL; i += 32) l = fminf(l, part[i * W].lim);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) l = fminf(l, __shfl_xor_sync(PODS_FULL_MASK, l, d));
+        return l;
+    }
+};
+
+// What is found by lists, counts and sums over the cluster.  Every method is called by the whole cluster.
+template <int DT>
+struct Finder {
+    using El = Elem<DT>;
+    static constexpr int E = El::E;
+    Rows<DT>& w;
+    int parity = 0;
+
+    __device__ __forceinline__ explicit Finder(Rows<DT>& w_) : w(w_) {}
+    __device__ __forceinline__ FilterCtrl& ctrl() const { return filter_ctrl(w.a); }
+    // the CTA's own list [own_cap]; all CTAs' lists [CL list_cap]; the sampler's ordered list or its histogram
+    __device__ __forceinline__ unsigned long long* own() const {
+        return reinterpret_cast<unsigned long long*>(smem_ + kRowCtrlBytes + w.a.seg * 16 + kFilterCtrlBytes);
+    }
+    __device__ __forceinline__ unsigned long long* all() const { return own() + w.a.own_cap; }
+    __device__ __forceinline__ unsigned long long* list() const { return all() + w.CL * w.a.list_cap; }
+    __device__ __forceinline__ uint32_t* hist() const { return reinterpret_cast<uint32_t*>(list()); }
+
+    // Hands `mine` to every CTA of the cluster; returns the CL words.
+    __device__ const Xch* exchange(const Xch& mine) {
+        Xch* const slot = ctrl().x[parity];
+        parity ^= 1;
+        if (w.tid < w.CL) *w.cl.map_shared_rank(slot + w.rank, w.tid) = mine;
+        w.cl.sync();
+        return slot;
+    }
+
+    // ids with value > thr and == thr
+    __device__ void row_count(float thr, long long* above, long long* equal) {
+        int n = 0, m = 0;
+        for (int j = w.v0; j < w.v1; ++j) {
+            const uint4 q = row_buf()[j];
+            if (El::vec_max(q) < thr) continue;
+            float x[E];
+            El::unpack(q, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool ok = w.is_id(w.id_of(j, e));
+                n += (ok && x[e] > thr) ? 1 : 0;
+                m += (ok && x[e] == thr) ? 1 : 0;
             }
-            // an edge of the running sum within the margin is decided in fp64 (the row's start is no edge)
-            const double edge = before + lo * scale, next = edge + ev * scale, margin = draw_margin(a.V, Z);
-            if (PREC || ((target - edge > margin || edge == 0.0) && next - target > margin)) {
-                const double lz = log(Z) + (PREC || top.far ? 0.0 : ((double)top.R - (double)zmax * (double)c) * 0.6931471805599453);
-                const float d = (float)(((double)El::to_float(el[at]) - (double)zmax) * tau_inv - lz);
-                a.tokens[t] = s.id0 + at;
-                if (a.logp) a.logp[t] = d;
-                if (a.logq) a.logq[t] = d;
-            } else {
-                for (int q = 0; q < CL; ++q) atomicOr(cl.map_shared_rank(&ctl.redo[mark >> 5], q), 1u << (mark & 31));
+        }
+        Xch mine = {};
+        mine.n = block_reduce<W>(n, ctrl().ipart, Plus());
+        mine.i = block_reduce<W>(m, ctrl().ipart, Plus());
+        const Xch* x = exchange(mine);
+        *above = *equal = 0;
+        for (int q = 0; q < w.CL; ++q) { *above += x[q].n; *equal += x[q].i; }
+    }
+
+    // id of the nth (from 0) id, ascending, whose value is thr
+    __device__ int nth_equal(float thr, long long nth) {
+        int m = 0;
+        for (int j = w.v0; j < w.v1; ++j) {
+            float x[E];
+            El::unpack(row_buf()[j], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) m += (x[e] == thr && w.is_id(w.id_of(j, e))) ? 1 : 0;
+        }
+        const int incl = warp_scan(m, w.lane);
+        __syncthreads();
+        if (w.lane == 31) ctrl().ipart[w.warp] = incl;
+        if (w.tid == 0) ctrl().found = -1;
+        __syncthreads();
+        Xch mine = {};
+        int before = incl - m;
+        for (int q = 0; q < W; ++q) {
+            mine.n += ctrl().ipart[q];
+            if (q < w.warp) before += ctrl().ipart[q];
+        }
+        const Xch* x = exchange(mine);
+        long long at = before;
+        for (int q = 0; q < w.rank; ++q) at += x[q].n;
+        if (nth >= at && nth < at + m) {
+            const typename El::raw* el = reinterpret_cast<const typename El::raw*>(row_buf());
+            for (int i = w.v0 * E; i < w.v1 * E; ++i)
+                if (El::to_float(el[i]) == thr && w.is_id(w.s.id0 + i)) {
+                    if (at == nth) ctrl().found = w.s.id0 + i;
+                    ++at;
+                }
+        }
+        __syncthreads();
+        Xch out = {};
+        out.i = ctrl().found;
+        x = exchange(out);
+        int id = -1;
+        for (int q = 0; q < w.CL; ++q) id = max(id, x[q].i);
+        return id;
+    }
+
+    // Threshold of the first `count` ids of the order: value and highest id kept among the ids equal to it.
+    __device__ void count_threshold(long long count, float zmax, float* thr, int* cut) {
+        uint32_t lo = El::to_key(-INFINITY), hi = El::to_key(zmax) + 1;        // ids >= lo: all; >= hi: none
+        long long above, equal;
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            row_count(El::from_key(mid), &above, &equal);
+            if (above + equal >= count) lo = mid; else hi = mid;
+        }
+        *thr = El::from_key(lo);
+        row_count(*thr, &above, &equal);
+        const long long need = count - above;
+        *cut = need >= equal ? kNoCut : nth_equal(*thr, need - 1);
+    }
+
+    // sum of e over the kept ids, relative to top's maximum, in fp64
+    __device__ double kept_sum(float thr, int cut, const PartRef& top, double tau_inv) {
+        double sum = w.template lane_sum<true, true>(top, tau_inv, thr, cut);
+        Xch mine = {};
+        mine.a = block_reduce<W>(sum, ctrl().dpart, Plus());
+        const Xch* x = exchange(mine);
+        double total = 0.0;
+        for (int q = 0; q < w.CL; ++q) total += x[q].a;
+        return total;
+    }
+
+    // Shrinks (thr, cut) to the smallest prefix of the kept ids whose sum of e reaches `mass`, by bisection.
+    __device__ void mass_threshold(double mass, const PartRef& top, double tau_inv, float* thr, int* cut) {
+        uint32_t lo = El::to_key(*thr), hi = El::to_key(top.m) + 1;
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (kept_sum(El::from_key(mid), kNoCut, top, tau_inv) >= mass) lo = mid; else hi = mid;
+        }
+        const float v = El::from_key(lo);
+        long long above, equal;
+        row_count(v, &above, &equal);
+        // everything above v: v itself with no id of its own
+        const double more = mass - kept_sum(v, -1, top, tau_inv);
+        const double ev = exp64(((double)v - (double)top.m) * tau_inv);
+        double need = ev > 0.0 ? ceil(more / ev) : (double)equal;
+        if (need < 1.0) need = 1.0;
+        if (v > *thr) {
+            *thr = v;
+            *cut = need >= (double)equal ? kNoCut : nth_equal(v, (long long)need - 1);
+        } else if (need < (double)equal) {
+            const int id = nth_equal(v, (long long)need - 1);
+            *cut = min(*cut, id);
+        }
+    }
+
+    // Lists hold (order32(value) << 32) | ~id: larger first is the row's order, and no two entries are equal.
+    __device__ __forceinline__ void list_add(float x, int id) {
+        const int at = atomicAdd(&ctrl().n_list, 1);
+        if (at < w.a.own_cap) own()[at] = ((unsigned long long)order32(x) << 32) | (uint32_t)~id;
+    }
+    // Hands my list to every CTA, with `mine`; returns the CL words and the lists' length together.  Each list has a room of
+    // list_cap; -1 if one is longer.  PACKED: the lengths are exchanged first and the lists laid end to end, for lists that are
+    // known to fit together but may all come from one CTA.
+    template <bool PACKED>
+    __device__ const Xch* share_list(Xch mine, int* total) {
+        __syncthreads();
+        mine.n = ctrl().n_list;
+        int at = w.rank * w.a.list_cap;
+        if (PACKED) {
+            const Xch* x = exchange(mine);
+            at = 0;
+            for (int q = 0; q < w.rank; ++q) at += x[q].n;
+        }
+        const int n = min(mine.n, PACKED ? w.a.own_cap : w.a.list_cap);
+        for (int q = w.warp; q < w.CL; q += W) {
+            unsigned long long* const peer = w.cl.map_shared_rank(all() + at, q);
+            for (int k = w.lane; k < n; k += 32)
+                if (PODS_INDEX_OK(at + k, w.CL * w.a.list_cap, w.a.status)) peer[k] = own()[k];
+        }
+        const Xch* x = exchange(mine);
+        int sum = 0;
+        bool fits = true;
+        for (int q = 0; q < w.CL; ++q) {
+            if (w.tid == 0) {
+                ctrl().start[q] = PACKED ? sum : q * w.a.list_cap;
+                ctrl().count[q] = x[q].n;
             }
+            sum += x[q].n;
+            fits = fits && (PACKED || x[q].n <= w.a.list_cap);
+        }
+        __syncthreads();
+        *total = fits ? sum : -1;
+        return x;
+    }
+    __device__ __forceinline__ void add_kept(float thr, int cut) {
+        __syncthreads();
+        if (w.tid == 0) ctrl().n_list = 0;
+        __syncthreads();
+        for (int j = w.v0; j < w.v1; ++j) {
+            const uint4 q = row_buf()[j];
+            if (El::vec_max(q) < thr) continue;
+            float x[E];
+            El::unpack(q, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (w.is_id(w.id_of(j, e)) && w.kept(x[e], w.id_of(j, e), thr, cut)) list_add(x[e], w.id_of(j, e));
+        }
+    }
+    // Lists the kept ids of the row; returns how many, -1 if they do not fit.
+    template <bool PACKED>
+    __device__ __forceinline__ int list_kept(float thr, int cut) {
+        add_kept(thr, cut);
+        const Xch none = {};
+        int total;
+        share_list<PACKED>(none, &total);
+        return total;
+    }
+    // The same for the sampler, with the sum of e over all lists, relative to top's maximum.
+    __device__ __forceinline__ int list_kept_mass(float thr, const PartRef& top, double tau_inv, double* mass) {
+        add_kept(thr, kNoCut);
+        __syncthreads();
+        Xch mine = {};
+        for (int i = w.tid; i < min(ctrl().n_list, w.a.own_cap); i += kThreads)
+            mine.a += exp64(((double)unorder32((uint32_t)(own()[i] >> 32)) - (double)top.m) * tau_inv);
+        mine.a = block_reduce<W>(mine.a, ctrl().dpart, Plus());
+        int total;
+        const Xch* x = share_list<false>(mine, &total);
+        *mass = 0.0;
+        for (int q = 0; q < w.CL; ++q) *mass += x[q].a;
+        return total;
+    }
+    // Calls put(rank, key) for the entries of CTAs [q0, q1), the rank being the number of entries of all lists ahead of it: the
+    // whole CTA.  Few entries are looked at by P neighbouring lanes each, many by a thread R at a time.
+    template <int R, typename Put>
+    __device__ __forceinline__ void rank_entries(int q0, int i0, int n, int P, Put put) const {
+        const int sub = w.tid & (P - 1);
+        unsigned long long key[R];
+        bool live[R];
+        int r[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            int i = i0 + w.tid / P + k * kThreads, q = q0;
+            live[k] = i < n;
+            if (live[k])
+                while (i >= ctrl().count[q]) i -= ctrl().count[q++];
+            key[k] = live[k] ? all()[ctrl().start[q] + i] : ~0ull;
+            r[k] = 0;
+        }
+        for (int q = 0; q < w.CL; ++q) {
+            const unsigned long long* const at = all() + ctrl().start[q];
+            const int m = ctrl().count[q];
+#pragma unroll 4
+            for (int j = sub; j < m; j += P) {
+                const unsigned long long o = at[j];
+#pragma unroll
+                for (int k = 0; k < R; ++k) r[k] += o > key[k] ? 1 : 0;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            for (int d = 1; d < P; d <<= 1) r[k] += __shfl_xor_sync(PODS_FULL_MASK, r[k], d);
+            if (live[k] && sub == 0) put(r[k], key[k]);
+        }
+    }
+    template <typename Put>
+    __device__ __forceinline__ void rank_lists(int q0, int q1, Put put) const {
+        int n = 0;
+        for (int q = q0; q < q1; ++q) n += ctrl().count[q];
+        if (n <= kThreads) {
+            int P = 1;
+            while (P < 32 && n * P * 2 <= kThreads) P *= 2;
+            rank_entries<1>(q0, 0, n, P, put);
+        } else {
+            for (int i0 = 0; i0 < n; i0 += 4 * kThreads) rank_entries<4>(q0, i0, n, 1, put);
+        }
+    }
+    // The sampler: all lists in the row's order in the first CTA's `list`, every CTA placing its own entries; n <= kSampleList.
+    __device__ __forceinline__ void order_lists() {
+        unsigned long long* const first = w.cl.map_shared_rank(list(), 0);
+        rank_lists(w.rank, w.rank + 1, [&](int r, unsigned long long key) { first[r] = key; });
+        w.cl.sync();
+    }
+
+    // Shrinks (thr, cut) to the smallest prefix of the kept ids whose sum of e reaches top_p of theirs, where the border is
+    // found in one bracket of the mass histogram; S: their sum, to a few parts in 1e6.  false: the bracket does not fit the list.
+    __device__ bool nucleus_threshold(float top_p, double S, const PartRef& top, double tau_inv, float* thr, int* cut) {
+        // logits below this have less than 1 - top_p of the mass together, so the border lies above
+        const double deep = log(fmax((1.0 - (double)top_p) * S, 1e-30) / (double)w.a.V) - 1e-3;
+        const float low = fmaxf(*thr, __double2float_rd((double)top.m + deep / tau_inv));
+        const float range = top.m - low;
+        const float scale = (float)kBins / range;      // stretches a unit of logit
+        if (!(range > 0.0f) || !(scale < INFINITY)) return false;
+        const float h2 = (float)(1.4426950408889634 * tau_inv * (double)range / kBins);     // exponent of two a stretch, < 0.05
+        const auto bin_of = [&](float x, float* pos) {
+            *pos = (top.m - x) * scale;
+            return min(kBins - 1, (int)*pos);
+        };
+        for (int i = w.tid; i < kBins; i += kThreads) hist()[i] = 0;
+        __syncthreads();
+        // mass in units of 2^-12 of the weight at the stretch's upper end: at most 2^19 ids make 2^31; each is off by 1.3e-4
+        for (int j = w.v0; j < w.v1; ++j) {
+            const uint4 q = row_buf()[j];
+            if (El::vec_max(q) < low) continue;
+            float x[E];
+            int b[E];
+            uint32_t mass[E];
+            El::unpack(q, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {              // no branch before the atomics: the eight chains overlap
+                float pos;
+                b[e] = bin_of(fmaxf(x[e], low), &pos);
+                mass[e] = __float2uint_rn(4096.0f * ex2_approx(((float)b[e] - pos) * h2));
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] >= low && w.kept(x[e], w.id_of(j, e), *thr, *cut)) atomicAdd(&hist()[b[e]], mass[e]);
+        }
+        w.cl.sync();
+        constexpr int PB = kBins / kThreads;
+        uint32_t n[PB] = {};
+        for (int q = 0; q < w.CL; ++q) {
+            const uint2 h = *reinterpret_cast<const uint2*>(w.cl.map_shared_rank(hist() + w.tid * PB, q));
+            n[0] += h.x;
+            n[1] += h.y;
+        }
+        static_assert(PB == 2, "one 8-byte read a thread and peer");
+        double run[PB], sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < PB; ++k) {
+            sum += (double)n[k] * (1.0 / 4096.0) * (double)ex2_approx(-(float)(w.tid * PB + k) * h2);
+            run[k] = sum;
+        }
+        double all;
+        const double base = block_scan(sum, ctrl().dpart, &all) - sum;
+        const double goal = (double)top_p * S, tol = 2e-4 * S;     // 1.3e-4 of rounding, the fast sum S, the exponentials here
+        int below = 0, first = kBins - 1;
+#pragma unroll
+        for (int k = 0; k < PB; ++k) {
+            if (base + run[k] <= goal - tol) ++below;              // a prefix of the stretches
+            if (base + run[k] >= goal + tol) first = min(first, w.tid * PB + k);
+        }
+        const int b1 = block_reduce<W>(below, ctrl().ipart, Plus()), b2 = block_reduce<W>(first, ctrl().ipart, Min());
+
+        // fp64 sums above the bracket and of all kept ids; the bracket's ids listed
+        if (w.tid == 0) ctrl().n_list = 0;
+        __syncthreads();
+        double above = 0.0, total = 0.0;
+#pragma unroll 1
+        for (int j = w.v0; j < w.v1; ++j) {
+            const uint4 q = row_buf()[j];
+            if (El::vec_max(q) < *thr) continue;
+            float x[E];
+            El::unpack(q, x);
+#pragma unroll
+            for (int h = 0; h < E; h += 4) {
+                double d[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[i] = ((double)x[h + i] - (double)top.m) * tau_inv;
+                exp64x4(d);
+                double high[4];
+                bool inside[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int id = w.id_of(j, h + i);
+                    const bool in = w.kept(x[h + i], id, *thr, *cut), far = x[h + i] < low;
+                    float pos;
+                    const int b = far ? kBins : bin_of(x[h + i], &pos);
+                    d[i] = in ? d[i] : 0.0;
+                    high[i] = b < b1 ? d[i] : 0.0;
+                    inside[i] = in && b >= b1 && b <= b2 && w.is_id(id);
+                }
+                if (inside[0] | inside[1] | inside[2] | inside[3])
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (inside[i]) list_add(x[h + i], w.id_of(j, h + i));
+                total += (d[0] + d[1]) + (d[2] + d[3]);
+                above += (high[0] + high[1]) + (high[2] + high[3]);
+            }
+        }
+        Xch mine = {};
+        mine.a = block_reduce<W>(above, ctrl().dpart, Plus());
+        mine.b = block_reduce<W>(total, ctrl().dpart, Plus());
+        int len;
+        const Xch* x = share_list<false>(mine, &len);  // past its barrier the histogram is read: its room is the list's again
+        double A = 0.0, Z = 0.0;
+        for (int q = 0; q < w.CL; ++q) { A += x[q].a; Z += x[q].b; }
+        Xch out = {};
+        out.n = 0;
+        const bool fits = len > 0 && len <= kSampleList;
+        if (fits) order_lists();
+        if (w.rank == 0 && fits) {
+            const int per = (len + kThreads - 1) / kThreads;
+            double own = 0.0;
+            for (int k = 0; k < per; ++k) {
+                const int i = w.tid * per + k;
+                if (i < len) own += exp64(((double)unorder32((uint32_t)(list()[i] >> 32)) - (double)top.m) * tau_inv);
+            }
+            double sum_all;
+            double at = A + block_scan(own, ctrl().dpart, &sum_all) - own;
+            int pick = kNoCut;
+            for (int k = 0; k < per; ++k) {
+                const int i = w.tid * per + k;
+                if (i < len) {
+                    at += exp64(((double)unorder32((uint32_t)(list()[i] >> 32)) - (double)top.m) * tau_inv);
+                    if (at >= (double)top_p * Z && pick == kNoCut) pick = i;
+                }
+            }
+            pick = block_reduce<W>(pick, ctrl().ipart, Min());
+            if (pick < len && (A < (double)top_p * Z || b1 == 0)) {
+                out.n = 1;
+                out.m = unorder32((uint32_t)(list()[pick] >> 32));
+                out.i = (int)~(uint32_t)list()[pick];
+            }
+        }
+        x = exchange(out);
+        if (x[0].n == 0) return false;
+        *thr = x[0].m;
+        *cut = x[0].i;
+        return true;
+    }
+
+    // Draws over the kept ids; the whole cluster gets the token, its logit and the kept sum relative to top's maximum.
+    template <bool PREC>
+    __device__ bool draw(double u, float thr, int cut, const PartRef& top, double tau_inv, int* token, float* logit, double* total) {
+        const double sum = w.template lane_sum<PREC, true>(top, tau_inv, thr, cut);
+        const double incl = warp_scan(sum, w.lane);
+        Part p;
+        p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
+        p.m = 0.0f;
+        p.lim = 0.0f;
+        if (w.tid == 0) ctrl().found = -1;
+        const Part* part = w.publish(p);
+        const typename Rows<DT>::Sums r = w.template sum_parts<PREC, true>(part, top, tau_inv);
+        const double target = u * r.total;
+        double before;
+        const int owner = w.owner_of(r, target, &before);
+        if (owner == w.rank * W + w.warp) {
+            int at = 0;
+            double lo = 0.0, ev = 0.0;
+            if (w.template search<PREC, true>(target - before, sum, incl, top, tau_inv, thr, cut, &at, &lo, &ev)) {
+                ctrl().found = w.s.id0 + at;
+                ctrl().sure = PREC || w.certain(u, target, before + lo, ev, r.total, top, tau_inv);
+                ctrl().weight = (double)El::to_float(reinterpret_cast<const typename El::raw*>(row_buf())[at]);
+            }
+        }
+        __syncthreads();
+        Xch out = {};
+        out.i = ctrl().found;
+        out.n = ctrl().found >= 0 ? ctrl().sure : 0;
+        out.m = ctrl().found >= 0 ? (float)ctrl().weight : 0.0f;
+        const Xch* x = exchange(out);
+        bool sure = false;
+        *token = -1;
+        for (int q = 0; q < w.CL; ++q)
+            if (x[q].i >= 0) { *token = x[q].i; *logit = x[q].m; sure = x[q].n != 0; }
+        *total = PREC ? r.total : r.total * exp2(top.far ? 0.0 : (double)top.R - (double)top.m * (double)top.c);
+        return sure;
+    }
+};
+
+// A row's settings, checked.
+struct Settings {
+    float tau, u, top_p, min_p;
+    long long top_k;
+    bool greedy, nucleus, floor, filtered, odd;
+    __device__ __forceinline__ Settings(const SampleArgs& a, int64_t t, bool filters) {
+        tau = a.temperature_row ? a.temperature_row[t] : a.temperature;
+        u = a.u[t];
+        odd = false;
+        if (!(tau >= 0.0f) || tau == INFINITY) { tau = 1.0f; odd = true; }
+        if (!(u >= 0.0f)) { u = 0.0f; odd = true; }
+        if (!(u < 1.0f)) { u = 0x1.fffffep-1f; odd = true; }
+        greedy = tau < kGreedyBelow;
+        if (greedy) tau = 1.0f;
+        top_k = 0;
+        nucleus = floor = filtered = false;
+        if (filters) {
+            top_p = a.top_p_row ? a.top_p_row[t] : a.top_p;
+            min_p = a.min_p_row ? a.min_p_row[t] : a.min_p;
+            const int k = a.top_k_row ? a.top_k_row[t] : a.top_k;
+            if (top_p != top_p) { top_p = 1.0f; odd = true; }
+            if (min_p != min_p) { min_p = 0.0f; odd = true; }
+            top_k = (k <= 0 || k >= a.V) ? 0 : k;
+            min_p = fminf(min_p, 1.0f);
+            nucleus = top_p < 1.0f;
+            floor = min_p > 0.0f;
+            filtered = !greedy && (top_k > 0 || nucleus || floor);
         }
     }
 };
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 5)
-pods_sample_policy_kernel(const SampleArgs a) {
-    extern __shared__ __align__(128) unsigned char smem[];
-    PolicyCtrl& ctl = *reinterpret_cast<PolicyCtrl*>(smem);
-    Policy<DT> w(a, ctl, reinterpret_cast<uint4*>(smem + kPolicyCtrlBytes));
-    const int tid = w.tid;
-    if (tid == 0) {
-        mbar_init(&ctl.full, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+// One row.  PREC: the second time, in fp64, for rows without filters.  `mark`: the row's bit among the marked ones.
+template <int DT, bool PREC, bool FILTERS>
+__device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t, int mark) {
+    using El = Elem<DT>;
+    const SampleArgs& a = w.a;
+    const int tid = w.tid, lane = w.lane, CL = w.CL;
+    w.start(t);
+    const Settings g(a, t, FILTERS);
+    if (g.odd && w.rank == 0 && tid == 0) pods_raise(a.status, PODS_STATUS_PARAM_RANGE);
+    const double tau_inv = 1.0 / (double)g.tau;
+    const float c = (float)(1.4426950408889634 * tau_inv);
+    w.wait();
+
+    const float lm = w.lane_max();
+    Part p;
+    p.m = w.warp_max(lm);
+    const PartRef ref(p.m, c);
+    const double sum = w.template lane_sum<PREC, false>(ref, tau_inv, 0.0f, 0);
+    const double incl = warp_scan(sum, lane);
+    p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
+    const int want = (int)(g.top_k > 0 ? (g.top_k < 512 ? g.top_k : 512) : 256);
+    p.lim = FILTERS && g.filtered ? w.reach(lm, want) : 0.0f;
+    const Part* const part = w.publish(p);
+    const float zmax = w.row_max(part);
+    if (!(fabsf(zmax) < INFINITY)) {
+        if (w.rank == 0 && tid == 0) {
+            const bool empty = zmax == -INFINITY;
+            a.tokens[t] = -1;
+            const float v = empty ? -INFINITY : NAN;
+            if (a.logp) a.logp[t] = v;
+            if (a.logq) a.logq[t] = v;
+            pods_raise(a.status, empty ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+        }
+        return;
     }
-    for (int i = tid; i < kRedoRows / 32; i += kThreads) ctl.redo[i] = 0;
-    __syncthreads();
-    w.cl.sync();                                       // every CTA runs before its shared memory is written
+    const PartRef top(zmax, c);
+    const typename Rows<DT>::Sums r = w.template sum_parts<PREC, false>(part, top, tau_inv);
+    const double Z = r.total;                          // relative to 2^R of top (to e^zmax in fp64 rows)
+
+    if (!FILTERS || !g.filtered) {
+        const int mine = w.rank * W + w.warp;
+        if (g.greedy) {
+            int first = kNoCut;
+            for (int i = lane; i < CL * W; i += 32)
+                if (part[i].m == zmax) first = min(first, i);
+            if ((int)__reduce_min_sync(PODS_FULL_MASK, first) != mine) return;
+            int id = kNoCut;
+            for (int j = w.v0; j < w.v1; ++j) {
+                float x[El::E];
+                El::unpack(row_buf()[j], x);
+#pragma unroll
+                for (int e = El::E - 1; e >= 0; --e)
+                    if (x[e] == zmax) id = min(id, w.id_of(j, e));
+            }
+            id = __reduce_min_sync(PODS_FULL_MASK, id);
+            if (lane == 0) {
+                a.tokens[t] = id;
+                if (a.logp) a.logp[t] = (float)-(log(Z) + (PREC ? 0.0 : top.log_offset()));
+                if (a.logq) a.logq[t] = 0.0f;
+            }
+            return;
+        }
+        const double target = (double)g.u * Z;
+        double before;
+        if (w.owner_of(r, target, &before) != mine) return;
+        const double scale = PREC ? exp64(((double)p.m - (double)zmax) * tau_inv) : ref.scale_to(top);
+        int at = 0;
+        double lo = 0.0, ev = 0.0;
+        if (w.template search<PREC, false>((target - before) / scale, sum, incl, ref, tau_inv, 0.0f, 0, &at, &lo, &ev)) {
+            if (PREC || w.certain((double)g.u, target, before + lo * scale, ev * scale, Z, top, tau_inv)) {
+                const float x = El::to_float(reinterpret_cast<const typename El::raw*>(row_buf())[at]);
+                const float d = (float)(((double)x - (double)zmax) * tau_inv - (log(Z) + (PREC ? 0.0 : top.log_offset())));
+                a.tokens[t] = w.s.id0 + at;
+                if (a.logp) a.logp[t] = d;
+                if (a.logq) a.logq[t] = d;
+            } else {
+                for (int q = 0; q < CL; ++q) atomicOr(w.cl.map_shared_rank(&row_ctrl().redo[mark >> 5], q), 1u << (mark & 31));
+            }
+        }
+        return;
+    }
+
+    if constexpr (FILTERS) {
+        unsigned long long* const list = f->list();
+        FilterCtrl& ctl = f->ctrl();
+        // relative to e^zmax, as everything below is
+        const double lz = log(Z) + top.log_offset(), Zm = Z * exp2(top.far ? 0.0 : (double)top.R - (double)top.m * (double)top.c);
+        // the lowest value that min_p admits
+        const float zfloor = g.floor ? __double2float_ru((double)zmax + (double)g.tau * log((double)g.min_p)) : -INFINITY;
+        float lim = w.limit(part);
+        // top_p is a share of the whole top-k sum, so min_p may not shorten the list where both are set
+        if (g.floor && !(g.top_k > 0 && g.nucleus)) lim = (g.top_k > 0 || g.nucleus) ? fmaxf(lim, zfloor) : zfloor;
+        double list_mass;
+        const int n = f->list_kept_mass(lim, top, tau_inv, &list_mass);
+        const bool whole = n == a.V;                   // the list is the row
+        const bool to_floor = g.floor && lim == zfloor;  // the list holds all that min_p admits
+        int token = -1;
+        float logit = 0.0f;
+        double kept_total = 1.0;
+        // can the list settle the kept set?  (a nucleus that ends at its very end is found out below)
+        const bool over_list = g.top_k > 0 || whole;   // what top_p is a share of
+        const double slack = over_list ? 0.0 : (deep_error(a.V, Zm, c, tau_inv, top.far) + kFlat) * (double)g.top_p * Zm + 1e-12 * Zm;
+        const bool listed = n > 0 && n <= kSampleList && (g.top_k == 0 || n >= g.top_k || whole || (to_floor && !g.nucleus)) &&
+                            (!g.nucleus || over_list || to_floor || list_mass > (double)g.top_p * Zm + slack);
+        if (listed) f->order_lists();
+        if (w.rank == 0 && listed) {
+            bool ok = true;
+            {
+                // running sums in the row's order
+                const int lim_n = g.top_k > 0 && g.top_k < n ? (int)g.top_k : n;
+                constexpr int PT = kSampleList / kThreads;
+                const int per = (lim_n + kThreads - 1) / kThreads;
+                double run[PT];
+                double own = 0.0;
+#pragma unroll
+                for (int k = 0; k < PT; ++k) {
+                    const int i = tid * per + k;
+                    if (k < per && i < lim_n) own += exp64(((double)unorder32((uint32_t)(list[i] >> 32)) - (double)zmax) * tau_inv);
+                    run[k] = own;
+                }
+                double total;
+                const double base = block_scan(own, ctl.dpart, &total) - own;
+                // the nucleus: the first entry whose running sum reaches top_p of the (top-k) sum
+                int count = lim_n;
+                if (g.nucleus) {
+                    const double goal = (double)g.top_p * (over_list ? total : Zm);
+                    int first = kNoCut, unsure = 0;
+#pragma unroll
+                    for (int k = 0; k < PT; ++k) {
+                        const int i = tid * per + k;
+                        if (k < per && i < lim_n) {
+                            const double at = base + run[k];
+                            if (at >= goal && first == kNoCut) first = i;
+                            if (slack > 0.0 && fabs(at - goal) <= slack) unsure = 1;
+                        }
+                    }
+                    first = block_reduce<W>(first, ctl.ipart, Min());
+                    unsure = block_reduce<W>(unsure, ctl.ipart, Plus());
+                    if (unsure) ok = false;
+                    if (first < kNoCut) count = first + 1;
+                    else if (!over_list && !to_floor) ok = false;    // the nucleus goes on below the list
+                }
+                // min_p: entries are sorted, so the admitted ones are a prefix
+                if (g.floor) {
+                    int m = 0;
+#pragma unroll
+                    for (int k = 0; k < PT; ++k) {
+                        const int i = tid * per + k;
+                        if (k < per && i < count && unorder32((uint32_t)(list[i] >> 32)) >= zfloor) ++m;
+                    }
+                    m = block_reduce<W>(m, ctl.ipart, Plus());
+                    count = max(1, min(count, m));
+                }
+                if (ok) {
+                    // back into id order, and the draw
+                    __syncthreads();
+                    for (int i = tid; i < count; i += kThreads) {
+                        const unsigned long long k = list[i];
+                        list[i] = ((unsigned long long)~(uint32_t)k << 32) | (k >> 32);
+                    }
+                    __syncthreads();
+                    if (count > 1) sort_list(list, count);
+                    const int per2 = (count + kThreads - 1) / kThreads;
+                    double s2 = 0.0;
+#pragma unroll
+                    for (int k = 0; k < PT; ++k) {
+                        const int i = tid * per2 + k;
+                        if (k < per2 && i < count) s2 += exp64(((double)unorder32((uint32_t)list[i]) - (double)zmax) * tau_inv);
+                        run[k] = s2;
+                    }
+                    const double base2 = block_scan(s2, ctl.dpart, &kept_total) - s2;
+                    const double target = (double)g.u * kept_total;
+                    int pick = kNoCut;
+#pragma unroll
+                    for (int k = 0; k < PT; ++k) {
+                        const int i = tid * per2 + k;
+                        if (k < per2 && i < count && pick == kNoCut && base2 + run[k] > target) pick = i;
+                    }
+                    pick = block_reduce<W>(pick, ctl.ipart, Min());
+                    if (pick >= count) pick = count - 1;
+                    token = (int)(uint32_t)(list[pick] >> 32);
+                    logit = unorder32((uint32_t)list[pick]);
+                }
+            }
+            if (!ok) token = -1;
+        }
+        bool settled = false;
+        if (listed) {
+            Xch out = {};
+            out.i = token;
+            settled = f->exchange(out)[0].i >= 0;
+        }
+        if (!settled) {
+            float thr = -INFINITY;
+            int cut = kNoCut;
+            if (g.top_k > 0) f->count_threshold(g.top_k, zmax, &thr, &cut);
+            if (g.nucleus) {
+                const double S = g.top_k > 0 ? f->kept_sum(thr, cut, top, tau_inv) : Zm;
+                if (!f->nucleus_threshold(g.top_p, S, top, tau_inv, &thr, &cut)) {
+                    const double total = f->kept_sum(thr, cut, top, tau_inv);
+                    f->mass_threshold((double)g.top_p * total, top, tau_inv, &thr, &cut);
+                }
+            }
+            if (zfloor > thr) { thr = zfloor; cut = kNoCut; }
+            if (!f->template draw<false>((double)g.u, thr, cut, top, tau_inv, &token, &logit, &kept_total))
+                f->template draw<true>((double)g.u, thr, cut, top, tau_inv, &token, &logit, &kept_total);
+        }
+        if (w.rank == 0 && tid == 0) {
+            const double d = ((double)logit - (double)zmax) * tau_inv;
+            a.tokens[t] = token;
+            if (a.logp) a.logp[t] = (float)(d - lz);
+            if (a.logq) a.logq[t] = (float)(d - log(kept_total));
+        }
+    }
+}
+
+template <int DT, bool FILTERS>
+__global__ void __launch_bounds__(kThreads, 2)
+pods_sample_kernel(const SampleArgs a) {
+    Rows<DT> w(a);
+    Finder<DT> f(w);
 
     const int64_t n_clusters = gridDim.x / w.CL;
     for (int64_t t0 = blockIdx.x / w.CL; t0 < a.T; t0 += kRedoRows * n_clusters) {
@@ -1146,59 +1184,113 @@ pods_sample_policy_kernel(const SampleArgs a) {
             const int64_t t = t0 + k * n_clusters;
             if (t >= a.T) break;
             if (a.mask != nullptr && a.mask[t] == 0) continue;
-            w.template row<false>(t, k);
-            fence_async_proxy();                       // the buffer is refilled by bulk copies
-            __syncthreads();
+            sample_row<DT, false, FILTERS>(w, &f, t, k);
+            w.done();
         }
         w.cl.sync();                                   // the marks are in place, the same in every CTA
-        static_assert(kRedoRows / 32 == kThreads, "a word of marks a thread");
-        if (__syncthreads_or(ctl.redo[tid] != 0)) {
+        static_assert(kRedoRows / 32 <= kThreads, "a word of marks a thread");
+        if (__syncthreads_or(w.tid < kRedoRows / 32 && row_ctrl().redo[w.tid] != 0)) {
             for (int i = 0; i < kRedoRows / 32; ++i) {
-                uint32_t bits = ctl.redo[i];
+                uint32_t bits = row_ctrl().redo[i];
                 while (bits) {
                     const int k = 32 * i + __ffs(bits) - 1;
                     bits &= bits - 1;
-                    w.template row<true>(t0 + k * n_clusters, 0);
-                    fence_async_proxy();
-                    __syncthreads();
+                    sample_row<DT, true, false>(w, nullptr, t0 + k * n_clusters, 0);
+                    w.done();
                 }
             }
             __syncthreads();
-            ctl.redo[tid] = 0;
+            if (w.tid < kRedoRows / 32) row_ctrl().redo[w.tid] = 0;
         }
         if (t0 + kRedoRows * n_clusters < a.T) w.cl.sync();      // cleared before the next mark
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 2)
+pods_topk_kernel(const SampleArgs a) {
+    Rows<DT> w(a);
+    Finder<DT> f(w);
+    const int tid = w.tid;
+
+    const double tau_inv = 1.0 / (double)a.temperature;
+    const float c = (float)(1.4426950408889634 * tau_inv);
+    const int64_t n_clusters = gridDim.x / w.CL;
+    for (int64_t t = blockIdx.x / w.CL; t < a.T; t += n_clusters) {
+        if (a.mask != nullptr && a.mask[t] == 0) continue;
+        w.start(t);
+        w.wait();
+        const float lm = w.lane_max();
+        Part p;
+        p.m = w.warp_max(lm);
+        p.s = 0.0;
+        if (a.lse != nullptr) {
+            const PartRef ref(p.m, c);
+            p.s = warp_scan(w.template lane_sum<false, false>(ref, tau_inv, 0.0f, 0), w.lane);
+            p.s = __shfl_sync(PODS_FULL_MASK, p.s, 31);
+        }
+        p.lim = w.reach(lm, a.K);
+        const Part* const part = w.publish(p);
+        const float zmax = w.row_max(part);
+        if (zmax != zmax || zmax == INFINITY) {
+            if (w.rank == 0) {
+                for (int i = tid; i < a.K; i += kThreads) {
+                    a.ids[t * a.K + i] = -1;
+                    a.values[t * a.K + i] = NAN;
+                }
+                if (tid == 0) {
+                    if (a.lse) a.lse[t] = NAN;
+                    pods_raise(a.status, PODS_STATUS_NONFINITE_LOGIT);
+                }
+            }
+        } else {
+            if (f.template list_kept<false>(w.limit(part), kNoCut) < a.K) {      // too many reach it: the exact threshold
+                float thr;
+                int cut;
+                f.count_threshold(a.K, zmax, &thr, &cut);
+                f.template list_kept<true>(thr, cut);
+            }
+            // every CTA ranks its own entries and writes those within K
+            f.rank_lists(w.rank, w.rank + 1, [&](int r, unsigned long long k) {
+                if (r < a.K) {
+                    a.ids[t * a.K + r] = (int32_t)~(uint32_t)k;
+                    a.values[t * a.K + r] = unorder32((uint32_t)(k >> 32));
+                }
+            });
+            if (w.rank == 0) {
+                if (w.warp == 0 && a.lse != nullptr) {
+                    const PartRef top(zmax, c);
+                    const double Z = w.template sum_parts<false, false>(part, top, tau_inv).total;
+                    if (tid == 0) a.lse[t] = zmax == -INFINITY ? -INFINITY : (float)((double)zmax * tau_inv + log(Z) + top.log_offset());
+                }
+                if (tid == 0 && zmax == -INFINITY) pods_raise(a.status, PODS_STATUS_EMPTY_ROW);
+            }
+        }
+        w.done();
     }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 constexpr size_t kMaxSmem = 227 * 1024;
-constexpr size_t kSegmentBytes = 40 * 1024;            // segments of about this size let five CTAs share an SM
+constexpr size_t kSegmentBytes = 80 * 1024;            // segments of at most this size let two CTAs share an SM
 
-template <typename Kernel>
-int launch_rows(Kernel kernel, SampleArgs& a, int esize, size_t ctrl_bytes, cudaStream_t stream) {
+// CTAs a row: segments of at most kSegmentBytes, and enough lanes for a list of K, whose bound comes from their maxima.
+int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
     int cl = 1;
-    while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
+    while (cl < kMaxCluster && ((size_t)segment_vectors(V, esize, cl) * 16 > kSegmentBytes || cl * kThreads < 2 * K)) cl *= 2;
+    // few rows: spread over idle SMs down to two vectors a lane
+    while (cl < kMaxCluster && 2 * cl * T <= 128 && segment_vectors(V, esize, 2 * cl) >= kThreads) cl *= 2;
+    return cl;
+}
+
+// room: bytes besides the segment
+template <typename Kernel>
+int launch_rows(Kernel kernel, SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stream) {
     a.seg = segment_vectors(a.V, esize, cl);
-    const size_t smem = ctrl_bytes + (size_t)a.seg * 16;
+    const size_t smem = room + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
-    PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    if (cl > 8) PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cl;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)cl, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)(row_clusters(a.T, cl, smem) * cl), 1, 1);
-    PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, kernel, a));
-    return PODS_OK;
+    return launch_row_clusters(kernel, a, a.T, cl, kThreads, smem, stream);
 }
 
 int check_rows(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int* esize) {
@@ -1243,18 +1335,20 @@ extern "C" int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64
     a.tokens = tokens;
     a.logp = logp;
     a.logq = logq;
-    a.list_cap = kSampleList;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
+    const int cl = row_cluster_size(V, T, esize, 0);
     if (!top_k_row && !top_p_row && !min_p_row && (top_k <= 0 || top_k >= V) && top_p >= 1.0f && min_p <= 0.0f) {
-        if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_policy_kernel<PODS_DTYPE_BF16>, a, esize, kPolicyCtrlBytes, s);
-        if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_policy_kernel<PODS_DTYPE_F16>, a, esize, kPolicyCtrlBytes, s);
-        return launch_rows(pods_sample_policy_kernel<PODS_DTYPE_F32>, a, esize, kPolicyCtrlBytes, s);
+        if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16, false>, a, esize, cl, kRowCtrlBytes, s);
+        if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16, false>, a, esize, cl, kRowCtrlBytes, s);
+        return launch_rows(pods_sample_kernel<PODS_DTYPE_F32, false>, a, esize, cl, kRowCtrlBytes, s);
     }
-    const size_t ctrl = kCtrlBytes + (size_t)a.list_cap * 8;
-    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16>, a, esize, ctrl, s);
-    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16>, a, esize, ctrl, s);
-    return launch_rows(pods_sample_kernel<PODS_DTYPE_F32>, a, esize, ctrl, s);
+    // a CTA may list more than its share of what is ordered: the ids of a row's top need not be spread evenly
+    a.list_cap = a.own_cap = cl <= 4 ? kSampleList / cl : 2 * kSampleList / cl;
+    const size_t ctrl = kRowCtrlBytes + kFilterCtrlBytes + (size_t)(1 + cl) * a.list_cap * 8 + (size_t)kSampleList * 8;
+    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16, true>, a, esize, cl, ctrl, s);
+    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16, true>, a, esize, cl, ctrl, s);
+    return launch_rows(pods_sample_kernel<PODS_DTYPE_F32, true>, a, esize, cl, ctrl, s);
 }
 
 extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int32_t K,
@@ -1278,12 +1372,15 @@ extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t
     a.ids = ids;
     a.values = values;
     a.lse = lse;
-    a.list_cap = 1024;
-    while (a.list_cap < 4 * K) a.list_cap *= 2;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    const size_t ctrl = kCtrlBytes + (size_t)a.list_cap * 8;
-    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_topk_kernel<PODS_DTYPE_BF16>, a, esize, ctrl, s);
-    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_topk_kernel<PODS_DTYPE_F16>, a, esize, ctrl, s);
-    return launch_rows(pods_topk_kernel<PODS_DTYPE_F32>, a, esize, ctrl, s);
+    const int cl = row_cluster_size(V, T, esize, K);
+    // the first bound leaves one to four times K entries, fewer the larger K is; the exact threshold K, maybe all in one CTA
+    a.list_cap = 128;
+    while (a.list_cap * cl < 4 * K || a.list_cap * cl < 1024) a.list_cap *= 2;
+    a.own_cap = a.list_cap > K ? a.list_cap : K;
+    const size_t ctrl = kRowCtrlBytes + kFilterCtrlBytes + ((size_t)a.own_cap + (size_t)cl * a.list_cap) * 8;
+    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_topk_kernel<PODS_DTYPE_BF16>, a, esize, cl, ctrl, s);
+    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_topk_kernel<PODS_DTYPE_F16>, a, esize, cl, ctrl, s);
+    return launch_rows(pods_topk_kernel<PODS_DTYPE_F32>, a, esize, cl, ctrl, s);
 }

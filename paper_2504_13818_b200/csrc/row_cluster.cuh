@@ -228,6 +228,48 @@ __device__ __forceinline__ float vec_add(const float (&x)[E]) {
     unpack2(s[0], a, b);
     return a + b;
 }
+// e^d for d <= 0 in fp64 without a branch, so that several run side by side: d log2 e = n + f with |f| <= 1/2, then the
+// Taylor polynomial of 2^f (the first term left out is 6.3e-15 of the sum).  Below e^-700: 0.
+template <int K> struct Exp2Term { static constexpr double value = Exp2Term<K - 1>::value * (0.69314718055994530942 / K); };
+template <> struct Exp2Term<0> { static constexpr double value = 1.0; };
+template <int K>
+__device__ __forceinline__ double exp2_poly(double p, double f) {
+    if constexpr (K < 0) return p;
+    else return exp2_poly<K - 1>(fma(p, f, Exp2Term<K>::value), f);
+}
+__device__ __forceinline__ double exp64(double d) {
+    const double y = d * 1.4426950408889634074;
+    const double t = y + 6755399441055744.0;           // 1.5 * 2^52: the integer part is in the low word
+    const double f = y - (t - 6755399441055744.0);
+    const double p = exp2_poly<10>(Exp2Term<11>::value, f);
+    const double e = __hiloint2double(__double2hiint(p) + (int)((unsigned)__double2loint(t) << 20), __double2loint(p));
+    return d > -700.0 ? e : 0.0;
+}
+// Four at a time, step by step, which hides the latency of the fp64 pipe: d becomes e^d.
+template <int K>
+__device__ __forceinline__ void exp2_poly4(double (&p)[4], const double (&f)[4]) {
+    if constexpr (K >= 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = fma(p[i], f[i], Exp2Term<K>::value);
+        exp2_poly4<K - 1>(p, f);
+    }
+}
+__device__ __forceinline__ void exp64x4(double (&d)[4]) {
+    double f[4], p[4];
+    int n[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const double y = d[i] * 1.4426950408889634074, t = y + 6755399441055744.0;
+        f[i] = y - (t - 6755399441055744.0);
+        n[i] = d[i] > -700.0 ? (int)((unsigned)__double2loint(t) << 20) : (int)0x80000000;
+        p[i] = Exp2Term<11>::value;
+    }
+    exp2_poly4<10>(p, f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        d[i] = n[i] != (int)0x80000000 ? __hiloint2double(__double2hiint(p[i]) + n[i], __double2loint(p[i])) : 0.0;
+}
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 __device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {
@@ -332,13 +374,34 @@ static inline int segment_vectors(int64_t V, int esize, int cl) {
     return (int)(((nvec + cl - 1) / cl + 7) & ~7ll);
 }
 
-// Host: clusters to launch for T rows - no more than can be resident (each goes round over its rows), by shared memory and
-// at most five CTAs an SM.  An estimate is enough: clusters do not wait for one another.
-static inline int64_t row_clusters(int64_t T, int cl, size_t smem) {
-    int64_t per_sm = (int64_t)(233472 / (smem + 1024));
-    per_sm = per_sm < 1 ? 1 : per_sm > 5 ? 5 : per_sm;
-    const int64_t n = pods_sm_count() * per_sm / cl;
-    return T < n ? T : (n < 1 ? 1 : n);
+// Host: launches `kernel` on clusters of cl CTAs that go round over T rows: as many clusters as are resident at once, since a
+// cluster that started late would leave its rows for a second round.  The query is left out where every row has its SMs.
+template <typename Kernel, typename Args>
+int launch_row_clusters(Kernel kernel, const Args& a, int64_t T, int cl, int threads, size_t smem, cudaStream_t stream) {
+    PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (cl > 8) PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cl;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)cl, 1, 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int64_t n = T;
+    if (T * cl > 128) {
+        int resident = 0;
+        PODS_RETURN_IF_CUDA_ERROR(cudaOccupancyMaxActiveClusters(&resident, kernel, &cfg));
+        if (resident < 1) return PODS_ERR_UNSUPPORTED;
+        if (n > resident) n = resident;
+    }
+    cfg.gridDim = dim3((unsigned)(n * cl), 1, 1);
+    PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, kernel, a));
+    return PODS_OK;
 }
 
 }  // namespace pods_row

@@ -176,7 +176,11 @@ def test_masked_rows_are_left_as_they_were():
     assert (tokens[~live] == 12345).all() and (logp[~live] == 3.5).all()
     assert (ids[~live] == -1).all() and (values[~live] == 0).all() and (lse[~live] == 0).all()
     alone = binding.pods_sample(z[live].contiguous(), u[live].contiguous(), top_p=0.9)
-    assert torch.equal(tokens[live], alone[0]) and torch.equal(logp[live], alone[1])
+    # V is odd: packed without the masked rows, a row starts at another 16-byte offset and its sum is grouped differently,
+    # so the two log-probs agree as two values that are each within log_tol of the exact one
+    assert torch.equal(tokens[live], alone[0])
+    both = logp[live].double().cpu().numpy(), alone[1].double().cpu().numpy()
+    assert (np.abs(both[0] - both[1]) <= 2 * log_tol(both[0])).all()
 
 
 def test_frequencies_follow_the_distribution():
