@@ -40,6 +40,7 @@ constexpr float kGreedyBelow = 0x1p-20f;      // temperatures below this are the
 constexpr int kSampleList = 1024;             // entries that the sampler's first CTA orders
 constexpr int kBins = 1024;                   // stretches of the mass histogram
 constexpr int kNoCut = 0x7fffffff;
+constexpr int kMarked = -2;                   // token of a row that the pipeline leaves to fp64
 constexpr int kRedoRows = 8192;               // rows of a cluster between two visits of the marked ones
 constexpr double kLn2 = 0.6931471805599453;
 
@@ -75,6 +76,7 @@ struct SampleArgs {
     int K;
     int32_t* ids;
     float *values, *lse;
+    int marked_only;                          // the rows whose token is kMarked, in fp64
     int list_cap, own_cap;                    // entries of one CTA: its share of all lists, its own list
     uint32_t* status;
 };
@@ -128,14 +130,14 @@ struct PartRef {
         R = ceilf(__fmul_ru(m, c));
         far = !(fabsf(R) < 0x1p23f);
     }
-    template <int E>
+    template <bool FAR, int E>
     __device__ __forceinline__ void exps(float (&x)[E]) const {
-        const unsigned long long c2 = pack2(c, c), off2 = far ? pack2(-m, -m) : pack2(-R, -R);
+        const unsigned long long c2 = pack2(c, c), off2 = FAR ? pack2(-m, -m) : pack2(-R, -R);
 #pragma unroll
         for (int i = 0; i < E; i += 2) {
             const unsigned long long v = pack2(x[i], x[i + 1]);
             float p, q;
-            unpack2(far ? mul2(add2(v, off2), c2) : fma2(v, c2, off2), p, q);
+            unpack2(FAR ? mul2(add2(v, off2), c2) : fma2(v, c2, off2), p, q);
             x[i] = ex2_approx(p);
             x[i + 1] = ex2_approx(q);
         }
@@ -236,6 +238,29 @@ __device__ __forceinline__ void sort_list(unsigned long long* list, int n) {
     __syncthreads();
 }
 
+// A lane's vectors of a segment dealt out to NW warps: a warp's share is contiguous, and so is a lane's - an odd number, so
+// that eight lanes of a 16-byte access touch all 32 banks once.
+template <int NW>
+__device__ __forceinline__ void lane_vectors(int cnt, int warp, int lane, int* v0, int* v1) {
+    const int share = (cnt + NW - 1) / NW, per = ((share + 31) / 32) | 1, end = min(cnt, (warp + 1) * share);
+    *v0 = min(end, warp * share + lane * per);
+    *v1 = min(end, *v0 + per);
+}
+
+// Fast sum of e over vectors [v0, v1).
+template <int DT, bool FAR>
+__device__ __forceinline__ double lane_exp_sum(const uint4* buf, int v0, int v1, const PartRef& ref) {
+    double sum = 0.0;
+#pragma unroll 2
+    for (int j = v0; j < v1; ++j) {
+        float x[Elem<DT>::E];
+        Elem<DT>::unpack(buf[j], x);
+        ref.template exps<FAR>(x);
+        sum += (double)vec_add(x);
+    }
+    return sum;
+}
+
 // A row and its cluster.
 template <int DT>
 struct Rows {
@@ -267,12 +292,7 @@ struct Rows {
     __device__ __forceinline__ void start(int64_t t) {
         s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
         if (tid == 0) start_load<DT>(s, a.V, row_buf(), &row_ctrl().full);
-        // a warp's share is contiguous, and so is a lane's: an odd number of vectors, so that eight lanes of a 16-byte access
-        // touch all 32 banks once
-        const int share = (s.cnt + W - 1) / W, per = ((share + 31) / 32) | 1;
-        const int end = min(s.cnt, (warp + 1) * share);
-        v0 = min(end, warp * share + lane * per);
-        v1 = min(end, v0 + per);
+        lane_vectors<W>(s.cnt, warp, lane, &v0, &v1);
     }
     __device__ __forceinline__ void wait() {
         if (!mbar_wait(&row_ctrl().full, phase, kSpinLimit) && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
@@ -328,17 +348,21 @@ struct Rows {
                     sum += (d[0] + d[1]) + (d[2] + d[3]);
                 }
             }
+        } else if constexpr (!FILT) {
+            sum = ref.far ? lane_exp_sum<DT, true>(row_buf(), v0, v1, ref) : lane_exp_sum<DT, false>(row_buf(), v0, v1, ref);
         } else {
-#pragma unroll 2
+#pragma unroll 1
             for (int j = v0; j < v1; ++j) {
+                const uint4 q = row_buf()[j];
+                if (El::vec_max(q) < thr) continue;
                 float x[E], p[E];
-                El::unpack(row_buf()[j], x);
+                El::unpack(q, x);
 #pragma unroll
                 for (int e = 0; e < E; ++e) p[e] = x[e];
-                ref.exps(p);
-                if (FILT)
+                if (ref.far) ref.template exps<true>(p);
+                else ref.template exps<false>(p);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) p[e] = kept(x[e], id_of(j, e), thr, cut) ? p[e] : 0.0f;
+                for (int e = 0; e < E; ++e) p[e] = kept(x[e], id_of(j, e), thr, cut) ? p[e] : 0.0f;
                 sum += (double)vec_add(p);
             }
         }
@@ -1180,7 +1204,15 @@ pods_sample_kernel(const SampleArgs a) {
 
     const int64_t n_clusters = gridDim.x / w.CL;
     for (int64_t t0 = blockIdx.x / w.CL; t0 < a.T; t0 += kRedoRows * n_clusters) {
-        for (int k = 0; k < kRedoRows; ++k) {
+        if (!FILTERS && a.marked_only) {
+            // rows that the pipeline marked: the marks are read before any of them is taken
+            for (int k = w.tid; k < kRedoRows; k += kThreads) {
+                const int64_t t = t0 + k * n_clusters;
+                const uint32_t bits = __ballot_sync(PODS_FULL_MASK, t < a.T && a.tokens[t] == kMarked);
+                if (w.lane == 0) row_ctrl().redo[k >> 5] = bits;
+                if (t0 + (k - w.tid + kThreads) * n_clusters >= a.T) break;
+            }
+        } else for (int k = 0; k < kRedoRows; ++k) {
             const int64_t t = t0 + k * n_clusters;
             if (t >= a.T) break;
             if (a.mask != nullptr && a.mask[t] == 0) continue;
@@ -1204,6 +1236,263 @@ pods_sample_kernel(const SampleArgs a) {
         }
         if (t0 + kRedoRows * n_clusters < a.T) w.cl.sync();      // cleared before the next mark
     }
+}
+
+// ---- many rows without filters: a pipeline -----------------------------------------------------------------------------
+// The same arithmetic where rows come by the hundred and every SM holds two CTAs: three kinds of warps that meet only at
+// mbarriers, so that no warp waits for the cluster with its hands full (with a cluster barrier a row, 512 rows of 151936 took
+// 135 us, two thirds of the instructions being every warp's own copy of what one needs to know).
+//   producer  one thread: the row's segment into one of two stages, as soon as the consumers have left it
+//   consumer  eight warps: maximum, sum, lane sums kept in a ring; the part goes to every CTA of the cluster by asynchronous
+//            stores that count on the receiver's mbarrier; then the stage is free - no consumer waits for the exchange
+//   exchange  one warp: all parts of the row, the owner of the drawn point, and, where that is a warp of this CTA, the search
+//            among the lane sums and of one lane's elements, read again from global memory
+// A row's slots are used again four rows later, when every exchange warp of the cluster has said that it is done with them.
+// Close draws are marked by a token of kMarked and taken by a launch of pods_sample_kernel in fp64.
+constexpr int PW = 8;                         // consumer warps
+constexpr int kPolicyThreads = (PW + 2) * 32;
+constexpr int kStages = 2, kRing = 4;
+
+struct PolicyCtrl {
+    unsigned long long full[kStages], empty[kStages];
+    unsigned long long parts[kRing];          // a row's parts have arrived
+    unsigned long long ready[kRing];          // this CTA's lane sums are there
+    unsigned long long done[kRing];           // every exchange warp is done with the slots
+    alignas(16) Part part[kRing][kMaxCluster * PW];
+    double lanes[kRing][PW][32];              // lane sums, scanned
+};
+constexpr int kPolicyCtrlBytes = (sizeof(PolicyCtrl) + 127) & ~127;
+
+__device__ __forceinline__ uint32_t mapa(const void* p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+// 16 bytes into a CTA of the cluster, counted on an mbarrier there.
+__device__ __forceinline__ void store_async(uint32_t at, uint32_t bar, double a, unsigned long long b) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];"
+                 ::"r"(at), "l"(__double_as_longlong(a)), "l"(b), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_local(unsigned long long* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool wait_cluster(unsigned long long* bar, uint32_t parity, uint32_t limit) {
+    for (uint32_t i = 0; i < limit; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kPolicyThreads, 2)
+pods_sample_policy_kernel(const SampleArgs a) {
+    using El = Elem<DT>;
+    constexpr int E = El::E;
+    PolicyCtrl& c = *reinterpret_cast<PolicyCtrl*>(smem_);
+    uint4* const stages = reinterpret_cast<uint4*>(smem_ + kPolicyCtrlBytes);
+    cg::cluster_group cl = cg::this_cluster();
+    const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
+    const int64_t n_rows = first < a.T ? (a.T - first + n_clusters - 1) / n_clusters : 0;
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&c.full[i], 1);
+            mbar_init(&c.empty[i], PW);
+        }
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&c.parts[i], 1);
+            mbar_init(&c.ready[i], PW);
+            mbar_init(&c.done[i], (uint32_t)CL);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    cl.sync();                                         // every CTA's barriers are there before anyone reaches for them
+
+    const float tau = a.temperature;
+    const double tau_inv = 1.0 / (double)tau;
+    const float cexp = (float)(1.4426950408889634 * tau_inv);
+    bool late = false;                                 // a wait ran out: no further one is worth its time
+    auto spins = [&]() { return late ? 1u : kSpinLimit; };
+
+    if (warp == PW) {
+        // ---- producer ----
+        if (lane == 0) {
+            for (int64_t i = 0; i < n_rows; ++i) {
+                const int st = (int)(i % kStages);
+                if (i >= kStages && !mbar_wait(&c.empty[st], (uint32_t)((i / kStages - 1) & 1), spins())) late = true;
+                const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
+                uint4* const buf = stages + (size_t)st * a.seg;
+                fill_edges<DT>(s, a.V, buf);
+                fence_async_proxy();                   // edges of an earlier row may lie where this row's copy goes
+                start_copy(s, buf, &c.full[st]);
+            }
+            // every copy has landed before the CTA ends, also one that a consumer gave up on
+            for (int64_t i = n_rows > kStages ? n_rows - kStages : 0; i < n_rows; ++i)
+                if (!mbar_wait(&c.full[i % kStages], (uint32_t)((i / kStages) & 1), kSpinLimit)) late = true;
+        }
+    } else if (warp < PW) {
+        // ---- consumers ----
+        for (int64_t i = 0; i < n_rows; ++i) {
+            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+            const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
+            int v0, v1;
+            lane_vectors<PW>(s.cnt, warp, lane, &v0, &v1);
+            const uint4* const buf = stages + (size_t)st * a.seg;
+            if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
+            float m = -INFINITY;
+#pragma unroll 4
+            for (int j = v0; j < v1; ++j) m = max_nan(m, El::vec_max(buf[j]));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(PODS_FULL_MASK, m, d));
+            const PartRef ref(m, cexp);
+            const double sum = ref.far ? lane_exp_sum<DT, true>(buf, v0, v1, ref) : lane_exp_sum<DT, false>(buf, v0, v1, ref);
+            __syncwarp();
+            if (lane == 0) arrive_local(&c.empty[st]);
+            const double incl = warp_scan(sum, lane);
+            const double total = __shfl_sync(PODS_FULL_MASK, incl, 31);
+            if (i >= kRing && !wait_cluster(&c.done[slot], (uint32_t)((i / kRing - 1) & 1), spins())) late = true;
+            c.lanes[slot][warp][lane] = incl;
+            __syncwarp();
+            if (lane == 0) arrive_local(&c.ready[slot]);
+            if (lane < CL)
+                store_async(mapa(&c.part[slot][rank * PW + warp], lane), mapa(&c.parts[slot], lane), total,
+                            (unsigned long long)__float_as_uint(m));
+        }
+    } else {
+        // ---- exchange ----
+        float u_next = n_rows > 0 ? a.u[first] : 0.0f;
+        for (int64_t i = 0; i < n_rows; ++i) {
+            const int slot = (int)(i % kRing);
+            const int64_t t = first + i * n_clusters;
+            float u = u_next;
+            if (i + 1 < n_rows) u_next = a.u[t + n_clusters];
+            bool odd = false;
+            if (!(u >= 0.0f)) { u = 0.0f; odd = true; }
+            if (!(u < 1.0f)) { u = 0x1.fffffep-1f; odd = true; }
+            if (lane == 0) {
+                mbar_expect_tx(&c.parts[slot], (uint32_t)(CL * PW * 16));
+                if (odd && rank == 0) pods_raise(a.status, PODS_STATUS_PARAM_RANGE);
+            }
+            if (!wait_cluster(&c.parts[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
+
+            // lane l holds parts [l n, (l + 1) n)
+            constexpr int N = kMaxCluster * PW / 32;
+            const int n_parts = CL * PW, n = (n_parts + 31) / 32;
+            double v[N], mine = 0.0;
+            float pm[N], z = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                v[k] = 0.0;
+                pm[k] = -INFINITY;
+                if (k < n && lane * n + k < n_parts) {
+                    v[k] = c.part[slot][lane * n + k].s;
+                    pm[k] = c.part[slot][lane * n + k].m;
+                }
+                z = max_nan(z, pm[k]);
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) z = max_nan(z, __shfl_xor_sync(PODS_FULL_MASK, z, d));
+            const float zmax = z + 0.0f;
+            if (fabsf(z) < INFINITY) {
+                const PartRef top(zmax, cexp);
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    if (v[k] > 0.0) v[k] *= PartRef(pm[k], cexp).scale_to(top);
+                    mine += v[k];
+                }
+                const double incl = warp_scan(mine, lane);
+                const double Z = __shfl_sync(PODS_FULL_MASK, incl, 31), target = (double)u * Z;
+                const uint32_t hit = __ballot_sync(PODS_FULL_MASK, incl > target && mine > 0.0);
+                const int from = hit ? __ffs(hit) - 1 : 0;
+                int owner = -1;
+                double b = incl - mine, before = b;
+                float om = 0.0f;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (v[k] > 0.0 && (owner < 0 || !(b > target))) {  // the first that passes the target, else the last
+                        owner = lane * n + k;
+                        om = pm[k];
+                        before = b;
+                        b += v[k];
+                    }
+                owner = __shfl_sync(PODS_FULL_MASK, owner, from);
+                before = __shfl_sync(PODS_FULL_MASK, before, from);
+                om = __shfl_sync(PODS_FULL_MASK, om, from);
+                if (owner / PW == rank) {
+                    const int w = owner % PW;
+                    const PartRef ref(om, cexp);
+                    const double scale = ref.scale_to(top), goal = (target - before) / scale;
+                    if (!mbar_wait(&c.ready[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
+                    const double lincl = c.lanes[slot][w][lane], up = __shfl_up_sync(PODS_FULL_MASK, lincl, 1);
+                    const double lsum = lincl - (lane ? up : 0.0);
+                    const uint32_t past = __ballot_sync(PODS_FULL_MASK, lincl > goal && lsum > 0.0);
+                    const uint32_t any = __ballot_sync(PODS_FULL_MASK, lsum > 0.0);
+                    const int l = past ? __ffs(past) - 1 : 31 - __clz(any | 1u);
+                    const double ahead = __shfl_sync(PODS_FULL_MASK, lane ? up : 0.0, l);
+                    const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+                    int v0, v1;
+                    lane_vectors<PW>(s.cnt, w, l, &v0, &v1);
+                    const int e0 = max(v0 * E, -s.id0), e1 = min(v1 * E, a.V - s.id0), K = (max(0, e1 - e0) + 31) / 32;
+                    const int k0 = min(e1, e0 + lane * K), k1 = min(e1, k0 + K);
+                    const typename El::raw* const row = static_cast<const typename El::raw*>(a.logits) + t * a.ldl + s.id0;
+                    double own = 0.0;
+                    for (int k = k0; k < k1; ++k) own += ref.exp1(El::to_float(row[k]));
+                    const double eincl = warp_scan(own, lane);
+                    const uint32_t over = __ballot_sync(PODS_FULL_MASK, ahead + eincl > goal && own > 0.0);
+                    const uint32_t some = __ballot_sync(PODS_FULL_MASK, own > 0.0);
+                    if (lane == (over ? __ffs(over) - 1 : 31 - __clz(some | 1u))) {
+                        double run = ahead + eincl - own, lo = run, ev = 0.0;
+                        int at = -1;
+                        float x = 0.0f;
+                        for (int k = k0; k < k1; ++k) {
+                            const float y = El::to_float(row[k]);
+                            const double wgt = ref.exp1(y);
+                            if (!(wgt > 0.0)) continue;
+                            at = s.id0 + k;
+                            x = y;
+                            lo = run;
+                            ev = wgt;
+                            run += wgt;
+                            if (run > goal) break;
+                        }
+                        const double edge = before + lo * scale, next = edge + ev * scale;
+                        const double margin = draw_margin((double)u, Z, deep_error(a.V, Z, cexp, tau_inv, top.far));
+                        if (at >= 0 && (target - edge > margin || edge == 0.0) && next - target > margin) {
+                            const float d = (float)(((double)x - (double)zmax) * tau_inv - (log(Z) + top.log_offset()));
+                            a.tokens[t] = at;
+                            if (a.logp) a.logp[t] = d;
+                            if (a.logq) a.logq[t] = d;
+                        } else {
+                            a.tokens[t] = kMarked;
+                        }
+                    }
+                }
+            } else if (rank == 0 && lane == 0) {
+                const bool empty = zmax == -INFINITY;
+                const float d = empty ? -INFINITY : NAN;
+                a.tokens[t] = -1;
+                if (a.logp) a.logp[t] = d;
+                if (a.logq) a.logq[t] = d;
+                pods_raise(a.status, empty ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+            }
+            __syncwarp();
+            if (lane < CL) arrive_remote(mapa(&c.done[slot], lane));
+        }
+    }
+    if (late && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
+    __syncwarp();
+    cl.sync();                                         // no CTA leaves while a peer may still reach its shared memory
 }
 
 template <int DT>
@@ -1275,6 +1564,8 @@ pods_topk_kernel(const SampleArgs a) {
 constexpr size_t kMaxSmem = 227 * 1024;
 constexpr size_t kSegmentBytes = 80 * 1024;            // segments of at most this size let two CTAs share an SM
 
+constexpr size_t kPolicySegmentBytes = 46 * 1024;      // two stages of it and the control block, twice on an SM
+
 // CTAs a row: segments of at most kSegmentBytes, and enough lanes for a list of K, whose bound comes from their maxima.
 int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
     int cl = 1;
@@ -1291,6 +1582,21 @@ int launch_rows(Kernel kernel, SampleArgs& a, int esize, int cl, size_t room, cu
     const size_t smem = room + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
     return launch_row_clusters(kernel, a, a.T, cl, kThreads, smem, stream);
+}
+
+// The pipeline where there are rows enough for it; sets marked_only if it ran.
+constexpr int64_t kPipelineMinBytes = 16 << 20;
+template <int DT>
+int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
+    if (a.T * a.V * esize < kPipelineMinBytes) return PODS_OK;
+    int cl = 1;
+    while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kPolicySegmentBytes) cl *= 2;
+    a.seg = segment_vectors(a.V, esize, cl);
+    const size_t smem = kPolicyCtrlBytes + (size_t)kStages * a.seg * 16;
+    if (smem > kMaxSmem) return PODS_OK;
+    const int rc = launch_row_clusters(pods_sample_policy_kernel<DT>, a, a.T, cl, kPolicyThreads, smem, stream);
+    if (rc == PODS_OK) a.marked_only = 1;
+    return rc;
 }
 
 int check_rows(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int* esize) {
@@ -1339,6 +1645,12 @@ extern "C" int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64
     cudaStream_t s = pods_stream(stream);
     const int cl = row_cluster_size(V, T, esize, 0);
     if (!top_k_row && !top_p_row && !min_p_row && (top_k <= 0 || top_k >= V) && top_p >= 1.0f && min_p <= 0.0f) {
+        if (mask == nullptr && temperature_row == nullptr && temperature >= kGreedyBelow) {
+            const int rc_pipe = dtype == PODS_DTYPE_BF16  ? launch_policy<PODS_DTYPE_BF16>(a, esize, s)
+                                : dtype == PODS_DTYPE_F16 ? launch_policy<PODS_DTYPE_F16>(a, esize, s)
+                                                          : launch_policy<PODS_DTYPE_F32>(a, esize, s);
+            if (rc_pipe != PODS_OK) return rc_pipe;
+        }
         if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16, false>, a, esize, cl, kRowCtrlBytes, s);
         if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16, false>, a, esize, cl, kRowCtrlBytes, s);
         return launch_rows(pods_sample_kernel<PODS_DTYPE_F32, false>, a, esize, cl, kRowCtrlBytes, s);

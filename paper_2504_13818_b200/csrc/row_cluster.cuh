@@ -322,16 +322,10 @@ __device__ __forceinline__ Segment make_segment(const void* base, int64_t pitch,
     return s;
 }
 
-// Starts the segment's copy (one thread) and fills the vectors at the row's two ends (that thread too: at most two).
-// The waiters see both after mbar_wait on `bar` and a CTA barrier.
+// The vectors at the row's two ends (one thread: at most two of them).
 template <int DT>
-__device__ __forceinline__ void start_load(const Segment& s, int V, uint4* buf, unsigned long long* bar) {
+__device__ __forceinline__ void fill_edges(const Segment& s, int V, uint4* buf) {
     using El = Elem<DT>;
-    constexpr int kPiece = 512;
-    const int n = s.full1 - s.full0;
-    mbar_expect_tx(bar, (uint32_t)n * 16u);
-    for (int v = 0; v < n; v += kPiece)
-        bulk_load(buf + s.full0 + v, s.src + s.full0 + v, (uint32_t)min(kPiece, n - v) * 16u, bar);
     for (int j = 0; j < s.cnt; ++j) {
         if (j == s.full0) j = s.full1;
         if (j >= s.cnt) break;
@@ -342,6 +336,20 @@ __device__ __forceinline__ void start_load(const Segment& s, int V, uint4* buf, 
             dst[e] = (id >= 0 && id < V) ? src[e] : El::kNegInf;
         }
     }
+}
+// Starts the copy of the others, counted on `bar` (one thread).
+__device__ __forceinline__ void start_copy(const Segment& s, uint4* buf, unsigned long long* bar) {
+    constexpr int kPiece = 512;
+    const int n = s.full1 - s.full0;
+    mbar_expect_tx(bar, (uint32_t)n * 16u);
+    for (int v = 0; v < n; v += kPiece)
+        bulk_load(buf + s.full0 + v, s.src + s.full0 + v, (uint32_t)min(kPiece, n - v) * 16u, bar);
+}
+// Both, the copy first: the waiters see the ends after mbar_wait on `bar` and a CTA barrier.
+template <int DT>
+__device__ __forceinline__ void start_load(const Segment& s, int V, uint4* buf, unsigned long long* bar) {
+    start_copy(s, buf, bar);
+    fill_edges<DT>(s, V, buf);
 }
 
 // ---- reductions over a CTA of W warps; `part` is scratch of W entries, every thread gets the result -------------------

@@ -280,3 +280,33 @@ def test_empty_batches():
     z = torch.zeros((0, 100), device="cuda")
     assert binding.pods_sample(z, torch.zeros(0, device="cuda"))[0].numel() == 0
     assert binding.pods_topk(z, 5)[0].shape == (0, 5)
+
+
+@pytest.mark.parametrize("dtype,T,V,pad", [("bf16", 700, 32001, 0), ("fp32", 900, 5003, 1), ("fp16", 90, 151936, 0), ("bf16", 30000, 1000, 8)])
+def test_many_rows_without_filters(dtype, T, V, pad):
+    """Enough rows that each cluster takes several in a row (slots of the ring used more than once), rows that fp64 decides,
+    rows without a distribution among them."""
+    z = make(T, V, dtype, seed=T, kind="normal", pad=pad)
+    z[5] = -np.inf
+    z[T // 2, V - 1] = np.nan
+    u = uniform(T, 13)
+    status = binding.new_status()
+    tokens, logp, logq = binding.pods_sample(z, u, temperature=1.5, want_logq=True, status=status)
+    again = binding.pods_sample(z, u, temperature=1.5, want_logq=True)
+    torch.cuda.synchronize()
+    assert binding.read_status(status) == binding.STATUS_EMPTY_ROW | binding.STATUS_NONFINITE_LOGIT
+    assert all(torch.equal(a, b) or (torch.isnan(a) == torch.isnan(b)).all() for a, b in zip((tokens, logp, logq), again))
+    rows = sorted({0, 1, 5, T // 2, T - 1} | set(range(0, T, max(1, T // 150))))
+    sub = z[rows].contiguous()
+    want_rows = sub.double().cpu().numpy()
+    tok, lp, un = tokens.cpu().numpy(), logp.cpu().numpy().astype(np.float64), u.cpu().numpy()
+    for k, t in enumerate(rows):
+        want = rollout.sample_row(want_rows[k], float(un[t]), 1.5)
+        if want["edge"] <= EDGE:
+            continue
+        assert tok[t] == want["token"], t
+        assert want["token"] < 0 or abs(lp[t] - want["logp"]) <= log_tol(want["logp"])
+    # every row against the way for few rows, which takes a mask
+    live = torch.ones(T, dtype=torch.uint8, device="cuda")
+    other = binding.pods_sample(z, u, temperature=1.5, mask=live)
+    assert torch.equal(tokens, other[0])
