@@ -76,7 +76,7 @@ struct SampleArgs {
     int K;
     int32_t* ids;
     float *values, *lse;
-    int marked_only;                          // the rows whose token is kMarked, in fp64
+    int marked;                               // rows are marked for fp64
     int list_cap, own_cap;                    // entries of one CTA: its share of all lists, its own list
     uint32_t* status;
 };
@@ -1204,15 +1204,7 @@ pods_sample_kernel(const SampleArgs a) {
 
     const int64_t n_clusters = gridDim.x / w.CL;
     for (int64_t t0 = blockIdx.x / w.CL; t0 < a.T; t0 += kRedoRows * n_clusters) {
-        if (!FILTERS && a.marked_only) {
-            // rows that the pipeline marked: the marks are read before any of them is taken
-            for (int k = w.tid; k < kRedoRows; k += kThreads) {
-                const int64_t t = t0 + k * n_clusters;
-                const uint32_t bits = __ballot_sync(PODS_FULL_MASK, t < a.T && a.tokens[t] == kMarked);
-                if (w.lane == 0) row_ctrl().redo[k >> 5] = bits;
-                if (t0 + (k - w.tid + kThreads) * n_clusters >= a.T) break;
-            }
-        } else for (int k = 0; k < kRedoRows; ++k) {
+        for (int k = 0; k < kRedoRows; ++k) {
             const int64_t t = t0 + k * n_clusters;
             if (t >= a.T) break;
             if (a.mask != nullptr && a.mask[t] == 0) continue;
@@ -1222,7 +1214,9 @@ pods_sample_kernel(const SampleArgs a) {
         w.cl.sync();                                   // the marks are in place, the same in every CTA
         static_assert(kRedoRows / 32 <= kThreads, "a word of marks a thread");
         if (__syncthreads_or(w.tid < kRedoRows / 32 && row_ctrl().redo[w.tid] != 0)) {
-            for (int i = 0; i < kRedoRows / 32; ++i) {
+            const int64_t left = (a.T - t0 + n_clusters - 1) / n_clusters;           // rows of this cluster from t0 on
+            const int words = (int)((left < kRedoRows ? left : kRedoRows) + 31) / 32;
+            for (int i = 0; i < words; ++i) {
                 uint32_t bits = row_ctrl().redo[i];
                 while (bits) {
                     const int k = 32 * i + __ffs(bits) - 1;
@@ -1242,26 +1236,29 @@ pods_sample_kernel(const SampleArgs a) {
 // The same arithmetic where rows come by the hundred and every SM holds two CTAs: three kinds of warps that meet only at
 // mbarriers, so that no warp waits for the cluster with its hands full (with a cluster barrier a row, 512 rows of 151936 took
 // 135 us, two thirds of the instructions being every warp's own copy of what one needs to know).
-//   producer  one thread: the row's segment into one of two stages, as soon as the consumers have left it
+//   producer  one thread: the row's segment into one of three stages, as soon as the consumers have left it
 //   consumer  eight warps: maximum, sum, lane sums kept in a ring; the part goes to every CTA of the cluster by asynchronous
 //            stores that count on the receiver's mbarrier; then the stage is free - no consumer waits for the exchange
 //   exchange  one warp: all parts of the row, the owner of the drawn point, and, where that is a warp of this CTA, the search
 //            among the lane sums and of one lane's elements, read again from global memory
 // A row's slots are used again four rows later, when every exchange warp of the cluster has said that it is done with them.
-// Close draws are marked by a token of kMarked and taken by a launch of pods_sample_kernel in fp64.
+// Close draws are marked by a token of kMarked; pods_sample_marked_kernel takes them in fp64.
 constexpr int PW = 8;                         // consumer warps
 constexpr int kPolicyThreads = (PW + 2) * 32;
-constexpr int kStages = 2, kRing = 4;
+constexpr int kStages = 3, kRing = 4;
 
 struct PolicyCtrl {
     unsigned long long full[kStages], empty[kStages];
     unsigned long long parts[kRing];          // a row's parts have arrived
     unsigned long long ready[kRing];          // this CTA's lane sums are there
     unsigned long long done[kRing];           // every exchange warp is done with the slots
-    alignas(16) Part part[kRing][kMaxCluster * PW];
     double lanes[kRing][PW][32];              // lane sums, scanned
+    alignas(16) Part part[1];                 // [kRing][CL PW]
 };
-constexpr int kPolicyCtrlBytes = (sizeof(PolicyCtrl) + 127) & ~127;
+// control block of a CTA in a cluster of cl
+__host__ __device__ constexpr int policy_ctrl_bytes(int cl) {
+    return ((int)offsetof(PolicyCtrl, part) + kRing * cl * PW * (int)sizeof(Part) + 127) & ~127;
+}
 
 __device__ __forceinline__ uint32_t mapa(const void* p, int rank) {
     uint32_t r;
@@ -1298,9 +1295,10 @@ pods_sample_policy_kernel(const SampleArgs a) {
     using El = Elem<DT>;
     constexpr int E = El::E;
     PolicyCtrl& c = *reinterpret_cast<PolicyCtrl*>(smem_);
-    uint4* const stages = reinterpret_cast<uint4*>(smem_ + kPolicyCtrlBytes);
     cg::cluster_group cl = cg::this_cluster();
-    const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+    const int CL = (int)cl.num_blocks();
+    uint4* const stages = reinterpret_cast<uint4*>(smem_ + policy_ctrl_bytes(CL));
+    const int rank = (int)cl.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
     const int64_t n_rows = first < a.T ? (a.T - first + n_clusters - 1) / n_clusters : 0;
@@ -1366,7 +1364,7 @@ pods_sample_policy_kernel(const SampleArgs a) {
             __syncwarp();
             if (lane == 0) arrive_local(&c.ready[slot]);
             if (lane < CL)
-                store_async(mapa(&c.part[slot][rank * PW + warp], lane), mapa(&c.parts[slot], lane), total,
+                store_async(mapa(c.part + slot * CL * PW + rank * PW + warp, lane), mapa(&c.parts[slot], lane), total,
                             (unsigned long long)__float_as_uint(m));
         }
     } else {
@@ -1396,8 +1394,9 @@ pods_sample_policy_kernel(const SampleArgs a) {
                 v[k] = 0.0;
                 pm[k] = -INFINITY;
                 if (k < n && lane * n + k < n_parts) {
-                    v[k] = c.part[slot][lane * n + k].s;
-                    pm[k] = c.part[slot][lane * n + k].m;
+                    const Part p = c.part[slot * n_parts + lane * n + k];
+                    v[k] = p.s;
+                    pm[k] = p.m;
                 }
                 z = max_nan(z, pm[k]);
             }
@@ -1495,6 +1494,63 @@ pods_sample_policy_kernel(const SampleArgs a) {
     cl.sync();                                         // no CTA leaves while a peer may still reach its shared memory
 }
 
+// Numbers the marked rows, so that they can be dealt out evenly: kMarked becomes kMarked - 1 - number.  One CTA.
+__global__ void __launch_bounds__(1024)
+number_marks_kernel(int32_t* tokens, int64_t T) {
+    __shared__ int part[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int count = 0;
+    for (int64_t t0 = 0; t0 < T; t0 += 1024) {
+        const int64_t t = t0 + threadIdx.x;
+        const bool marked = t < T && tokens[t] == kMarked;
+        if (!__syncthreads_or(marked)) continue;
+        const uint32_t bits = __ballot_sync(PODS_FULL_MASK, marked);
+        if (lane == 0) part[warp] = __popc(bits);
+        __syncthreads();
+        int before = count;
+        for (int w = 0; w < 32; ++w) {
+            if (w < warp) before += part[w];
+            count += part[w];
+        }
+        if (marked) tokens[t] = kMarked - 1 - (before + __popc(bits & ((1u << lane) - 1u)));
+        __syncthreads();
+    }
+}
+
+// The marked rows in fp64, each cluster the numbers that fall to it.  Other clusters put tokens in place of other numbers
+// meanwhile, which changes nothing for this one; its own rows are found before any of them is taken.
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 2)
+pods_sample_marked_kernel(const SampleArgs a) {
+    Rows<DT> w(a);
+    const int n_clusters = (int)(gridDim.x / w.CL), mine = (int)(blockIdx.x / w.CL);
+    uint32_t* const bits = row_ctrl().redo;
+    for (int64_t t0 = 0; t0 < a.T; t0 += kRedoRows) {
+        const int rows = (int)(a.T - t0 < kRedoRows ? a.T - t0 : kRedoRows), words = (rows + 31) / 32;
+        bool any = false;
+        for (int k0 = 0; k0 < rows; k0 += kThreads) {
+            const int k = k0 + w.tid;
+            const int token = k < rows ? a.tokens[t0 + k] : 0;
+            const bool hit = token < kMarked && (kMarked - 1 - token) % n_clusters == mine;
+            const uint32_t b = __ballot_sync(PODS_FULL_MASK, hit);
+            if (w.lane == 0 && (k >> 5) < words) bits[k >> 5] = b;
+            any |= hit;
+        }
+        w.cl.sync();
+        if (__syncthreads_or(any))
+            for (int i = 0; i < words; ++i) {
+                uint32_t b = bits[i];
+                while (b) {
+                    const int k = 32 * i + __ffs(b) - 1;
+                    b &= b - 1;
+                    sample_row<DT, true, false>(w, nullptr, t0 + k, 0);
+                    w.done();
+                }
+            }
+        __syncthreads();
+    }
+}
+
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 2)
 pods_topk_kernel(const SampleArgs a) {
@@ -1564,7 +1620,7 @@ pods_topk_kernel(const SampleArgs a) {
 constexpr size_t kMaxSmem = 227 * 1024;
 constexpr size_t kSegmentBytes = 80 * 1024;            // segments of at most this size let two CTAs share an SM
 
-constexpr size_t kPolicySegmentBytes = 46 * 1024;      // two stages of it and the control block, twice on an SM
+constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold for two of them to share an SM
 
 // CTAs a row: segments of at most kSegmentBytes, and enough lanes for a list of K, whose bound comes from their maxima.
 int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
@@ -1584,18 +1640,23 @@ int launch_rows(Kernel kernel, SampleArgs& a, int esize, int cl, size_t room, cu
     return launch_row_clusters(kernel, a, a.T, cl, kThreads, smem, stream);
 }
 
-// The pipeline where there are rows enough for it; sets marked_only if it ran.
+// The pipeline where there are rows enough for it; sets `marked` if it ran.
 constexpr int64_t kPipelineMinBytes = 16 << 20;
 template <int DT>
 int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
     if (a.T * a.V * esize < kPipelineMinBytes) return PODS_OK;
-    int cl = 1;
-    while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kPolicySegmentBytes) cl *= 2;
-    a.seg = segment_vectors(a.V, esize, cl);
-    const size_t smem = kPolicyCtrlBytes + (size_t)kStages * a.seg * 16;
-    if (smem > kMaxSmem) return PODS_OK;
+    // the smallest cluster whose stages fit twice on an SM: few partners, and few places of the GPU left empty by its size
+    static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
+    int cl = 0;
+    size_t smem = 0;
+    for (int size : kSizes) {
+        a.seg = segment_vectors(a.V, esize, size);
+        smem = policy_ctrl_bytes(size) + (size_t)kStages * a.seg * 16;
+        if (smem <= kHalfSmBytes) { cl = size; break; }
+    }
+    if (cl == 0) return PODS_OK;
     const int rc = launch_row_clusters(pods_sample_policy_kernel<DT>, a, a.T, cl, kPolicyThreads, smem, stream);
-    if (rc == PODS_OK) a.marked_only = 1;
+    if (rc == PODS_OK) a.marked = 1;
     return rc;
 }
 
@@ -1643,13 +1704,21 @@ extern "C" int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64
     a.logq = logq;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    const int cl = row_cluster_size(V, T, esize, 0);
+    int cl = row_cluster_size(V, T, esize, 0);
     if (!top_k_row && !top_p_row && !min_p_row && (top_k <= 0 || top_k >= V) && top_p >= 1.0f && min_p <= 0.0f) {
         if (mask == nullptr && temperature_row == nullptr && temperature >= kGreedyBelow) {
             const int rc_pipe = dtype == PODS_DTYPE_BF16  ? launch_policy<PODS_DTYPE_BF16>(a, esize, s)
                                 : dtype == PODS_DTYPE_F16 ? launch_policy<PODS_DTYPE_F16>(a, esize, s)
                                                           : launch_policy<PODS_DTYPE_F32>(a, esize, s);
             if (rc_pipe != PODS_OK) return rc_pipe;
+        }
+        if (a.marked) {
+            number_marks_kernel<<<1, 1024, 0, s>>>(tokens, T);
+            PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
+            if (cl < 8) cl *= 2;                       // marked rows are few: twice as many CTAs each
+            if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_marked_kernel<PODS_DTYPE_BF16>, a, esize, cl, kRowCtrlBytes, s);
+            if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_marked_kernel<PODS_DTYPE_F16>, a, esize, cl, kRowCtrlBytes, s);
+            return launch_rows(pods_sample_marked_kernel<PODS_DTYPE_F32>, a, esize, cl, kRowCtrlBytes, s);
         }
         if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16, false>, a, esize, cl, kRowCtrlBytes, s);
         if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16, false>, a, esize, cl, kRowCtrlBytes, s);
