@@ -95,7 +95,13 @@ def _check(rc, what):
         raise PodsError("%s failed: %s (status %d)" % (what, load().pods_status_string(rc).decode(), rc))
 
 
+# the current stream's handle without building a Stream object around it (3 us a call on the machine measured)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
+    if _raw_stream is not None:
+        return C.c_void_p(_raw_stream(torch.cuda.current_device()))
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
@@ -449,26 +455,44 @@ def grpo_loss_from_hidden(hidden, W, tokens, old_logp, ref_logp, adv, seq_weight
     return logp, dhidden
 
 def _typed_rows(t, name):
-    """Pointer, row pitch and dtype code of a 2-D CUDA tensor of logits whose rows are contiguous."""
+    """Address, row pitch and dtype code of a 2-D CUDA tensor of logits whose rows are contiguous."""
     _require(isinstance(t, torch.Tensor) and t.dim() == 2, "%s must be [T,V]" % name)
-    _require(t.dtype in DTYPES, "%s must be bfloat16, float16 or float32, got %s" % (name, t.dtype))
-    _require(t.shape[1] <= MAX_ROW_V, "%s rows may hold at most %d entries, got %d" % (name, MAX_ROW_V, t.shape[1]))
+    T, V = t.shape
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        raise PodsError("%s must be bfloat16, float16 or float32, got %s" % (name, t.dtype))
+    if V > MAX_ROW_V:
+        raise PodsError("%s rows may hold at most %d entries, got %d" % (name, MAX_ROW_V, V))
     _require(t.is_cuda, "%s must be a CUDA tensor" % name)
-    _require(t.stride(1) == 1 or t.shape[1] == 1, "%s rows must be contiguous" % name)
-    pitch = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    _require(pitch >= t.shape[1], "%s rows must not overlap" % name)
-    return C.c_void_p(t.data_ptr()), pitch, DTYPES[t.dtype]
+    pitch, step = t.stride()
+    _require(step == 1 or V == 1, "%s rows must be contiguous" % name)
+    if T <= 1 and pitch < V:
+        pitch = V
+    _require(pitch >= V, "%s rows must not overlap" % name)
+    return t.data_ptr(), pitch, code
 
 
-def _on_current_device(*tensors):
-    """The library launches on the current device's current stream: tensors of another device are refused."""
-    here = None
-    for t in tensors:
-        if t is not None and t.is_cuda:
-            if here is None:
-                here = torch.cuda.current_device()
-            if t.get_device() != here:
-                raise PodsError("tensors must be on the current CUDA device (cuda:%d), got %s" % (here, t.device))
+def _here():
+    """The current device: the library launches on its current stream, so tensors of another device are refused."""
+    return torch.cuda.current_device()
+
+
+def _vec(t, dtype, count, name, here, optional=False):
+    """Address of a contiguous tensor of `count` entries on the device `here`; None stays None."""
+    if t is None:
+        if optional:
+            return None
+        raise PodsError("%s is required" % name)
+    if t.dtype is dtype and t.is_cuda and t.numel() == count and t.is_contiguous() and t.get_device() == here:
+        return t.data_ptr()
+    _numel(t, count, name)
+    _dev(t, dtype, name)
+    raise PodsError("%s must be on the current CUDA device (cuda:%d), got %s" % (name, here, t.device))
+
+
+def _same_device(t, name, here):
+    if t.get_device() != here:
+        raise PodsError("%s must be on the current CUDA device (cuda:%d), got %s" % (name, here, t.device))
 
 
 def _setting(x, T, name):
@@ -489,30 +513,34 @@ def pods_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask=
     filters.  Rows with mask 0 are left alone: pass the outputs then (those made here start as -1, 0 and 0)."""
     _require(isinstance(logits, torch.Tensor) and logits.dim() == 2, "logits must be [T,V]")
     T, V = logits.shape
-    _require(V >= 1, "logits must have at least one column")
+    if V < 1:
+        raise PodsError("logits must have at least one column")
     for t, name in ((u, "u"), (mask, "mask"), (tokens, "tokens"), (logp, "logp"), (logq, "logq")):
-        _numel(t, T, name)
+        if t is not None and t.numel() != T:
+            _numel(t, T, name)
     tau_t, tau = _setting(temperature, T, "temperature")
     k_t, k = _setting(top_k, T, "top_k")
     p_t, p = _setting(top_p, T, "top_p")
     m_t, m = _setting(min_p, T, "min_p")
     lp, ldl, dtype = _typed_rows(logits, "logits")
-    _on_current_device(logits, u, mask, tokens, logp, logq, tau_t, k_t, p_t, m_t, status)
+    here = _here()
+    _same_device(logits, "logits", here)
     dev = logits.device
-    new = torch.empty if mask is None else torch.zeros
     if tokens is None:
         tokens = torch.empty(T, dtype=torch.int32, device=dev) if mask is None else torch.full((T,), -1, dtype=torch.int32, device=dev)
+    new = torch.empty if mask is None else torch.zeros
     if logp is None:
         logp = new(T, dtype=torch.float32, device=dev)
     if logq is None and want_logq:
         logq = new(T, dtype=torch.float32, device=dev)
-    rc = load().pods_sample(lp, ldl, dtype, T, V, _dev(u, torch.float32, "u"),
-                            _dev(tau_t, torch.float32, "temperature", True), tau, _dev(k_t, torch.int32, "top_k", True), k,
-                            _dev(p_t, torch.float32, "top_p", True), p, _dev(m_t, torch.float32, "min_p", True), m,
-                            _dev(mask, torch.uint8, "mask", True), _dev(tokens, torch.int32, "tokens"),
-                            _dev(logp, torch.float32, "logp"), _dev(logq, torch.float32, "logq", True),
-                            _dev(status, torch.int32, "status", True), _stream())
-    _check(rc, "pods_sample")
+    f32, i32 = torch.float32, torch.int32
+    rc = load().pods_sample(lp, ldl, dtype, T, V, _vec(u, f32, T, "u", here), _vec(tau_t, f32, T, "temperature", here, True), tau,
+                            _vec(k_t, i32, T, "top_k", here, True), k, _vec(p_t, f32, T, "top_p", here, True), p,
+                            _vec(m_t, f32, T, "min_p", here, True), m, _vec(mask, torch.uint8, T, "mask", here, True),
+                            _vec(tokens, i32, T, "tokens", here), _vec(logp, f32, T, "logp", here),
+                            _vec(logq, f32, T, "logq", here, True), _vec(status, i32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_sample")
     return tokens, logp, logq
 
 
@@ -529,7 +557,8 @@ def pods_topk(logits, K, temperature=1.0, mask=None, ids=None, values=None, lse=
     _numel(mask, T, "mask")
     _numel(lse, T, "lse")
     lp, ldl, dtype = _typed_rows(logits, "logits")
-    _on_current_device(logits, mask, ids, values, lse, status)
+    here = _here()
+    _same_device(logits, "logits", here)
     dev = logits.device
     new = torch.empty if mask is None else torch.zeros
     if ids is None:
@@ -538,10 +567,11 @@ def pods_topk(logits, K, temperature=1.0, mask=None, ids=None, values=None, lse=
         values = new((T, K), dtype=torch.float32, device=dev)
     if lse is None:
         lse = new(T, dtype=torch.float32, device=dev)
-    rc = load().pods_topk(lp, ldl, dtype, T, V, K, temperature, _dev(mask, torch.uint8, "mask", True),
-                          _dev(ids, torch.int32, "ids"), _dev(values, torch.float32, "values"),
-                          _dev(lse, torch.float32, "lse"), _dev(status, torch.int32, "status", True), _stream())
-    _check(rc, "pods_topk")
+    rc = load().pods_topk(lp, ldl, dtype, T, V, K, temperature, _vec(mask, torch.uint8, T, "mask", here, True),
+                          _vec(ids, torch.int32, T * K, "ids", here), _vec(values, torch.float32, T * K, "values", here),
+                          _vec(lse, torch.float32, T, "lse", here), _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_topk")
     return ids, values, lse
 
 
@@ -573,27 +603,33 @@ def pods_distill_chunk(logits, ids, values, teacher_lse, seq_weight, cu_seqlens,
     _require(dlogits is None or (tuple(dlogits.shape) == (T, V) and dlogits.dtype == logits.dtype),
              "dlogits must have the shape and dtype of logits")
     lp, ldl, dtype = _typed_rows(logits, "logits")
-    _on_current_device(logits, ids, values, teacher_lse, seq_weight, cu_seqlens, mask, loss_acc, kl, dlogits, workspace, status)
+    here = _here()
+    _same_device(logits, "logits", here)
     dev = logits.device
+    f32, f64, i32 = torch.float32, torch.float64, torch.int32
     if kl is None:
-        kl = torch.empty(T, dtype=torch.float32, device=dev)
+        kl = torch.empty(T, dtype=f32, device=dev)
     if dlogits is None and want_grad:
         dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev)
     need = pods_distill_chunk_workspace_bytes(T)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _require(workspace.numel() >= need, "workspace must hold %d bytes, got %d" % (need, workspace.numel()))
-    dp, ldd, _ = _typed_rows(dlogits, "dlogits") if dlogits is not None else (None, 0, 0)
-    rc = load().pods_distill_chunk(lp, ldl, dtype, _dev(ids, torch.int32, "ids"), _dev(values, torch.float32, "values"), K, K,
-                                   _dev(teacher_lse, torch.float32, "teacher_lse", True),
-                                   _dev(seq_weight, torch.float64, "seq_weight"), _dev(cu_seqlens, torch.int64, "cu_seqlens"),
-                                   M, row0, _dev(mask, torch.uint8, "mask", True), T, V, temperature,
-                                   DISTILL_REST if rest else 0, grad_scale, _dev(loss_acc, torch.float64, "loss_acc"),
-                                   _dev(kl, torch.float32, "kl"), dp, ldd, _dev(workspace, torch.uint8, "workspace"),
-                                   workspace.numel(), _dev(status, torch.int32, "status", True), _stream())
-    _check(rc, "pods_distill_chunk")
+    size = workspace.numel()
+    _require(size >= need, "workspace must hold %d bytes, got %d" % (need, size))
+    dp, ldd = None, 0
+    if dlogits is not None:
+        dp, ldd, _ = _typed_rows(dlogits, "dlogits")
+        _same_device(dlogits, "dlogits", here)
+    rc = load().pods_distill_chunk(lp, ldl, dtype, _vec(ids, i32, T * K, "ids", here), _vec(values, f32, T * K, "values", here), K, K,
+                                   _vec(teacher_lse, f32, T, "teacher_lse", here, True), _vec(seq_weight, f64, M, "seq_weight", here),
+                                   _vec(cu_seqlens, torch.int64, M + 1, "cu_seqlens", here), M, row0,
+                                   _vec(mask, torch.uint8, T, "mask", here, True), T, V, temperature,
+                                   DISTILL_REST if rest else 0, grad_scale, _vec(loss_acc, f64, 1, "loss_acc", here),
+                                   _vec(kl, f32, T, "kl", here), dp, ldd, _vec(workspace, torch.uint8, size, "workspace", here), size,
+                                   _vec(status, i32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_distill_chunk")
     return kl, dlogits
-
 
 
 class HostStep:

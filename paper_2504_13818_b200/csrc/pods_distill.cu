@@ -416,8 +416,7 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
     a.seg = segment_vectors(a.V, esize, cl);
     const size_t smem = kCtrlBytes + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
-    auto kernel = pods_distill_kernel<DT, KP>;
-    return launch_row_clusters(kernel, a, a.T, cl, kThreads, smem, stream);
+    return launch_row_clusters<pods_distill_kernel<DT, KP>>(a, a.T, cl, kThreads, smem, stream);
 }
 
 }  // namespace

@@ -1632,12 +1632,12 @@ int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
 }
 
 // room: bytes besides the segment
-template <typename Kernel>
-int launch_rows(Kernel kernel, SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stream) {
+template <auto KERNEL>
+int launch_rows(SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stream) {
     a.seg = segment_vectors(a.V, esize, cl);
     const size_t smem = room + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
-    return launch_row_clusters(kernel, a, a.T, cl, kThreads, smem, stream);
+    return launch_row_clusters<KERNEL>(a, a.T, cl, kThreads, smem, stream);
 }
 
 // The pipeline where there are rows enough for it; sets `marked` if it ran.
@@ -1655,7 +1655,7 @@ int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
         if (smem <= kHalfSmBytes) { cl = size; break; }
     }
     if (cl == 0) return PODS_OK;
-    const int rc = launch_row_clusters(pods_sample_policy_kernel<DT>, a, a.T, cl, kPolicyThreads, smem, stream);
+    const int rc = launch_row_clusters<pods_sample_policy_kernel<DT>>(a, a.T, cl, kPolicyThreads, smem, stream);
     if (rc == PODS_OK) a.marked = 1;
     return rc;
 }
@@ -1716,20 +1716,20 @@ extern "C" int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64
             number_marks_kernel<<<1, 1024, 0, s>>>(tokens, T);
             PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
             if (cl < 8) cl *= 2;                       // marked rows are few: twice as many CTAs each
-            if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_marked_kernel<PODS_DTYPE_BF16>, a, esize, cl, kRowCtrlBytes, s);
-            if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_marked_kernel<PODS_DTYPE_F16>, a, esize, cl, kRowCtrlBytes, s);
-            return launch_rows(pods_sample_marked_kernel<PODS_DTYPE_F32>, a, esize, cl, kRowCtrlBytes, s);
+            if (dtype == PODS_DTYPE_BF16) return launch_rows<pods_sample_marked_kernel<PODS_DTYPE_BF16>>(a, esize, cl, kRowCtrlBytes, s);
+            if (dtype == PODS_DTYPE_F16) return launch_rows<pods_sample_marked_kernel<PODS_DTYPE_F16>>(a, esize, cl, kRowCtrlBytes, s);
+            return launch_rows<pods_sample_marked_kernel<PODS_DTYPE_F32>>(a, esize, cl, kRowCtrlBytes, s);
         }
-        if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16, false>, a, esize, cl, kRowCtrlBytes, s);
-        if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16, false>, a, esize, cl, kRowCtrlBytes, s);
-        return launch_rows(pods_sample_kernel<PODS_DTYPE_F32, false>, a, esize, cl, kRowCtrlBytes, s);
+        if (dtype == PODS_DTYPE_BF16) return launch_rows<pods_sample_kernel<PODS_DTYPE_BF16, false>>(a, esize, cl, kRowCtrlBytes, s);
+        if (dtype == PODS_DTYPE_F16) return launch_rows<pods_sample_kernel<PODS_DTYPE_F16, false>>(a, esize, cl, kRowCtrlBytes, s);
+        return launch_rows<pods_sample_kernel<PODS_DTYPE_F32, false>>(a, esize, cl, kRowCtrlBytes, s);
     }
     // a CTA may list more than its share of what is ordered: the ids of a row's top need not be spread evenly
     a.list_cap = a.own_cap = cl <= 4 ? kSampleList / cl : 2 * kSampleList / cl;
     const size_t ctrl = kRowCtrlBytes + kFilterCtrlBytes + (size_t)(1 + cl) * a.list_cap * 8 + (size_t)kSampleList * 8;
-    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_sample_kernel<PODS_DTYPE_BF16, true>, a, esize, cl, ctrl, s);
-    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_sample_kernel<PODS_DTYPE_F16, true>, a, esize, cl, ctrl, s);
-    return launch_rows(pods_sample_kernel<PODS_DTYPE_F32, true>, a, esize, cl, ctrl, s);
+    if (dtype == PODS_DTYPE_BF16) return launch_rows<pods_sample_kernel<PODS_DTYPE_BF16, true>>(a, esize, cl, ctrl, s);
+    if (dtype == PODS_DTYPE_F16) return launch_rows<pods_sample_kernel<PODS_DTYPE_F16, true>>(a, esize, cl, ctrl, s);
+    return launch_rows<pods_sample_kernel<PODS_DTYPE_F32, true>>(a, esize, cl, ctrl, s);
 }
 
 extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int32_t K,
@@ -1761,7 +1761,7 @@ extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t
     while (a.list_cap * cl < 4 * K || a.list_cap * cl < 1024) a.list_cap *= 2;
     a.own_cap = a.list_cap > K ? a.list_cap : K;
     const size_t ctrl = kRowCtrlBytes + kFilterCtrlBytes + ((size_t)a.own_cap + (size_t)cl * a.list_cap) * 8;
-    if (dtype == PODS_DTYPE_BF16) return launch_rows(pods_topk_kernel<PODS_DTYPE_BF16>, a, esize, cl, ctrl, s);
-    if (dtype == PODS_DTYPE_F16) return launch_rows(pods_topk_kernel<PODS_DTYPE_F16>, a, esize, cl, ctrl, s);
-    return launch_rows(pods_topk_kernel<PODS_DTYPE_F32>, a, esize, cl, ctrl, s);
+    if (dtype == PODS_DTYPE_BF16) return launch_rows<pods_topk_kernel<PODS_DTYPE_BF16>>(a, esize, cl, ctrl, s);
+    if (dtype == PODS_DTYPE_F16) return launch_rows<pods_topk_kernel<PODS_DTYPE_F16>>(a, esize, cl, ctrl, s);
+    return launch_rows<pods_topk_kernel<PODS_DTYPE_F32>>(a, esize, cl, ctrl, s);
 }

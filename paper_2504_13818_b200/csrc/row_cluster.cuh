@@ -382,12 +382,21 @@ static inline int segment_vectors(int64_t V, int esize, int cl) {
     return (int)(((nvec + cl - 1) / cl + 7) & ~7ll);
 }
 
-// Host: launches `kernel` on clusters of cl CTAs that go round over T rows: as many clusters as are resident at once, since a
+// Host: launches KERNEL on clusters of cl CTAs that go round over T rows: as many clusters as are resident at once, since a
 // cluster that started late would leave its rows for a second round.  The query is left out where every row has its SMs.
-template <typename Kernel, typename Args>
-int launch_row_clusters(Kernel kernel, const Args& a, int64_t T, int cl, int threads, size_t smem, cudaStream_t stream) {
-    PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    if (cl > 8) PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+// The kernel's attributes are set once per device, and the last answer of the query is kept (both cost a small call more
+// than its launch: 5 us together).
+template <auto KERNEL, typename Args>
+int launch_row_clusters(const Args& a, int64_t T, int cl, int threads, size_t smem, cudaStream_t stream) {
+    static uint64_t prepared = 0, last = 0;            // devices as bits; device, cl, smem / 128 and the answer in 16 bits each
+    int dev = 0;
+    PODS_RETURN_IF_CUDA_ERROR(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return PODS_ERR_UNSUPPORTED;
+    if (!(__atomic_load_n(&prepared, __ATOMIC_ACQUIRE) >> dev & 1)) {
+        PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+        PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        __atomic_fetch_or(&prepared, 1ull << dev, __ATOMIC_RELEASE);
+    }
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -402,13 +411,18 @@ int launch_row_clusters(Kernel kernel, const Args& a, int64_t T, int cl, int thr
     cfg.numAttrs = 1;
     int64_t n = T;
     if (T * cl > 128) {
-        int resident = 0;
-        PODS_RETURN_IF_CUDA_ERROR(cudaOccupancyMaxActiveClusters(&resident, kernel, &cfg));
-        if (resident < 1) return PODS_ERR_UNSUPPORTED;
+        const uint64_t key = (uint64_t)dev << 48 | (uint64_t)cl << 32 | (uint64_t)(smem / 128) << 16;
+        const uint64_t kept = __atomic_load_n(&last, __ATOMIC_RELAXED);
+        int resident = (int)(kept & 0xffff);
+        if (kept >> 16 != key >> 16 || resident == 0) {
+            PODS_RETURN_IF_CUDA_ERROR(cudaOccupancyMaxActiveClusters(&resident, KERNEL, &cfg));
+            if (resident < 1) return PODS_ERR_UNSUPPORTED;
+            __atomic_store_n(&last, key | (uint64_t)(resident & 0xffff), __ATOMIC_RELAXED);
+        }
         if (n > resident) n = resident;
     }
     cfg.gridDim = dim3((unsigned)(n * cl), 1, 1);
-    PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, kernel, a));
+    PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, KERNEL, a));
     return PODS_OK;
 }
 
