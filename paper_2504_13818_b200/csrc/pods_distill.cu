@@ -12,6 +12,8 @@
 // writes the gradient, exponentials taken again (two on the special-function pipe per 4 bytes of traffic, where 2.8 would
 // be free).  The listed entries are then written over by the threads that hold them.
 
+#include <stddef.h>
+
 #include "grpo_loss_common.cuh"
 #include "row_cluster.cuh"
 
@@ -403,14 +405,490 @@ pods_distill_kernel(const DistillArgs a) {
     }
 }
 
+// ---- many rows: a pipeline ------------------------------------------------------------------------------------------------
+// The same arithmetic where rows come by the hundred and every SM holds two CTAs (lists of up to kPipeK entries): warps with one
+// task each that meet only at mbarriers.  With every warp doing everything and a dozen CTA barriers a row, 4096 rows of 151936
+// took 731 us, half the time waiting at barriers.
+//   producer  one thread: the row's segment into one of three stages, as soon as the consumers have left it
+//   list      one warp: the teacher's probabilities, the listed logits out of the stage (their slots become -inf), the list's
+//            sums to every CTA of the cluster; it works a row ahead of the others
+//   consumer  eight warps: front(i) maximum and sum of their slice, sent to every CTA; back(i - 1) the gradient of the row
+//            before, whose factors have had a whole sweep to arrive, and the listed entries of their slice
+//   exchange  one warp: all parts of a row into the row's factors, loss and status
+// Parts and factors have four slots each.  A part of row i is sent after its sender has seen the factors of row i - 2, which
+// took every CTA's parts of row i - 2, which were sent after the factors of row i - 4 were made: the slot of row i - 4 is free.
+constexpr int PW = 8;
+constexpr int kPipeThreads = (PW + 3) * 32;
+constexpr int kStages = 3, kRing = 4;
+constexpr int kPipeK = 128;                   // entries of a list: four a lane
+
+struct PipePart {                             // of one consumer warp
+    double s;
+    float m;
+    int pad;
+};
+struct PipeList {                             // of one CTA's part of the list
+    double s, a;
+    float m;
+    int pad;
+    double unused;
+};
+struct Entry {                                // a listed id of my segment
+    double q;                                 // its teacher mass
+    float z;
+    int id;
+};
+struct Factors {
+    double p_scale, g;                        // listed ids: g (p_scale e^((z - zmax)/tau) - q)
+    float coef, m2, zmax;                     // the others: coef 2^(x c - R(m2))
+    int mode;                                 // 0: a row of zeros
+};
+struct PipeCtrl {
+    unsigned long long full[kStages], done[kStages];   // the stage is loaded; its consumers have left it
+    unsigned long long listed[kRing];         // the listed logits are out of the stage
+    unsigned long long parts[kRing];          // all parts of the cluster have arrived
+    unsigned long long ready[kRing];          // the factors are there
+    Factors f[kRing];
+    double Q[kRing], H[kRing];                // sum q, sum q log q
+    int n_entry[kRing];
+    alignas(16) PipeList list[kRing][kMaxCluster];
+    alignas(16) Entry entry[1];               // [kRing][K], then PipePart [kRing][CL PW]
+};
+__host__ __device__ constexpr int pipe_part_offset(int K) { return (int)offsetof(PipeCtrl, entry) + kRing * K * (int)sizeof(Entry); }
+__host__ __device__ constexpr int pipe_ctrl_bytes(int cl, int K) {
+    return (pipe_part_offset(K) + kRing * cl * PW * (int)sizeof(PipePart) + 127) & ~127;
+}
+
+extern __shared__ __align__(128) unsigned char smem_[];
+
+template <int DT>
+__global__ void __launch_bounds__(kPipeThreads, 2)
+pods_distill_pipe_kernel(const DistillArgs a) {
+    using El = Elem<DT>;
+    using raw = typename El::raw;
+    constexpr int E = El::E;
+    PipeCtrl& c = *reinterpret_cast<PipeCtrl*>(smem_);
+    cg::cluster_group cl = cg::this_cluster();
+    const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+    PipePart* const part = reinterpret_cast<PipePart*>(smem_ + pipe_part_offset(a.K));
+    uint4* const stages = reinterpret_cast<uint4*>(smem_ + pipe_ctrl_bytes(CL, a.K));
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
+    const int64_t n_rows = first < a.T ? (a.T - first + n_clusters - 1) / n_clusters : 0;
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&c.full[i], 1);
+            mbar_init(&c.done[i], PW);
+        }
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&c.listed[i], 1);
+            mbar_init(&c.parts[i], 1);
+            mbar_init(&c.ready[i], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    cl.sync();                                         // every CTA's barriers are there before anyone reaches for them
+
+    const double tau_inv = 1.0 / (double)a.temperature;
+    const float cexp = (float)(1.4426950408889634 * tau_inv);
+    bool late = false;                                 // a wait ran out: no further one is worth its time
+    auto spins = [&]() { return late ? 1u : kSpinLimit; };
+    auto wait_ready = [&](int64_t i) {
+        if (!mbar_wait(&c.ready[i % kRing], (uint32_t)((i / kRing) & 1), spins())) late = true;
+    };
+
+    if (warp == PW) {
+        // ---- producer ----
+        if (lane == 0) {
+            for (int64_t i = 0; i < n_rows; ++i) {
+                const int st = (int)(i % kStages);
+                if (i >= kStages && !mbar_wait(&c.done[st], (uint32_t)((i / kStages - 1) & 1), spins())) late = true;
+                const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
+                uint4* const buf = stages + (size_t)st * a.seg;
+                fill_edges<DT>(s, a.V, buf);
+                fence_async_proxy();                   // edges of an earlier row may lie where this row's copy goes
+                start_copy(s, buf, &c.full[st]);
+            }
+            // every copy has landed before the CTA ends, also one that a consumer gave up on
+            for (int64_t i = n_rows > kStages ? n_rows - kStages : 0; i < n_rows; ++i)
+                if (!mbar_wait(&c.full[i % kStages], (uint32_t)((i / kStages) & 1), kSpinLimit)) late = true;
+        }
+    } else if (warp == PW + 1) {
+        // ---- list ----
+        constexpr int KP = kPipeK / 32;
+        int id_next[KP];
+        float y_next[KP], lse_next = 0.0f;
+        auto fetch = [&](int64_t t) {
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                const int j = lane + 32 * k;
+                id_next[k] = j < a.K ? a.ids[t * a.ldk + j] : -1;
+                y_next[k] = j < a.K ? a.values[t * a.ldk + j] : -INFINITY;
+            }
+            if (a.teacher_lse != nullptr) lse_next = a.teacher_lse[t];
+        };
+        if (n_rows > 0) fetch(first);
+        for (int64_t i = 0; i < n_rows; ++i) {
+            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+            const int64_t t = first + i * n_clusters;
+            const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+            raw* const elems = reinterpret_cast<raw*>(stages + (size_t)st * a.seg);
+            int id[KP], at[KP];
+            float y[KP], ymax = -INFINITY;
+            double q[KP], L = (double)lse_next;
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                id[k] = id_next[k];
+                y[k] = y_next[k];
+                if (id[k] < 0 || id[k] >= a.V) {
+                    odd |= id[k] != -1;
+                    id[k] = -1;
+                    y[k] = -INFINITY;
+                }
+                ymax = max_nan(ymax, y[k]);
+            }
+            if (i + 1 < n_rows) fetch(t + n_clusters);
+            if (a.teacher_lse == nullptr) {
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) ymax = max_nan(ymax, __shfl_xor_sync(PODS_FULL_MASK, ymax, d));
+                const double ref = ymax == -INFINITY ? 0.0 : (double)ymax;     // no entry at all: every q is 0
+                double sum = 0.0;
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+                    if (32 * k < a.K && id[k] >= 0) sum += exp(((double)y[k] - ref) * tau_inv);
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
+                L = ref * tau_inv + (sum > 0.0 || sum != sum ? log(sum) : 0.0);
+            }
+            double Q = 0.0, H = 0.0;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                q[k] = 0.0;
+                if (32 * k < a.K && id[k] >= 0) {
+                    const double lq = (double)y[k] * tau_inv - L;
+                    q[k] = exp(lq);
+                    Q += q[k];
+                    if (q[k] != 0.0) H += q[k] * lq;
+                }
+            }
+            if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
+            float z[KP], m_in = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                at[k] = id[k] - s.id0;
+                if (id[k] < 0 || at[k] < 0 || at[k] >= s.cnt * E) at[k] = -1;
+                z[k] = at[k] >= 0 ? El::to_float(elems[at[k]]) : -INFINITY;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < KP; ++k)
+                if (at[k] >= 0) elems[at[k]] = (raw)(lane + 32 * k);           // one entry of an id stays visible
+            __syncwarp();
+            bool twice = false;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) twice |= at[k] >= 0 && elems[at[k]] != (raw)(lane + 32 * k);
+            twice = __any_sync(PODS_FULL_MASK, twice);                         // (and everyone has looked)
+            double qsum[KP];
+            unsigned speaks = 0;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                qsum[k] = q[k];
+                if (at[k] >= 0) {
+                    elems[at[k]] = El::kNegInf;
+                    speaks |= 1u << k;
+                }
+            }
+            if (twice) {
+                // an id in several entries: the first speaks for it, with their mass added in list order
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+                    if (at[k] >= 0) {
+                        const int j = lane + 32 * k;
+                        for (int o = 0; o < a.K; ++o)
+                            if (o != j && a.ids[t * a.ldk + o] == id[k]) {
+                                if (o < j) speaks &= ~(1u << k);
+                                else qsum[k] += exp((double)a.values[t * a.ldk + o] * tau_inv - L);
+                            }
+                    }
+            }
+            fence_async_proxy();                       // what was written to the stage lies where a later copy goes
+            __syncwarp();
+            // entry slots of row i - 4 were read by back(i - 4), before the parts of row i - 2 that made its factors
+            if (i >= 2) wait_ready(i - 2);
+            int n = 0;
+            double A = 0.0, sum = 0.0;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                const bool mine = speaks >> k & 1u;
+                const uint32_t b = __ballot_sync(PODS_FULL_MASK, mine);
+                if (mine) {
+                    Entry e;
+                    e.q = qsum[k];
+                    e.z = z[k];
+                    e.id = id[k];
+                    c.entry[slot * a.K + n + __popc(b & ((1u << lane) - 1u))] = e;
+                    m_in = max_nan(m_in, z[k]);
+                }
+                n += __popc(b);
+                if (at[k] >= 0 && q[k] != 0.0) A += q[k] * ((double)z[k] * tau_inv);
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) m_in = max_nan(m_in, __shfl_xor_sync(PODS_FULL_MASK, m_in, d));
+#pragma unroll
+            for (int k = 0; k < KP; ++k)
+                if ((speaks >> k & 1u) && m_in > -INFINITY) sum += exp(((double)z[k] - (double)m_in) * tau_inv);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                Q += __shfl_xor_sync(PODS_FULL_MASK, Q, d);
+                H += __shfl_xor_sync(PODS_FULL_MASK, H, d);
+                A += __shfl_xor_sync(PODS_FULL_MASK, A, d);
+                sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
+            }
+            if (lane == 0) {
+                c.Q[slot] = Q;
+                c.H[slot] = H;
+                c.n_entry[slot] = n;
+            }
+            if (__any_sync(PODS_FULL_MASK, odd) && lane == 0 && rank == 0) {
+                const bool live = a.mask == nullptr || a.mask[t] != 0;
+                if (live) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
+            }
+            __syncwarp();
+            if (lane == 0) arrive_local(&c.listed[slot]);
+            if (lane < CL) {
+                const uint32_t to = mapa(&c.list[slot][rank], lane), bar = mapa(&c.parts[slot], lane);
+                store_async(to, bar, sum, (unsigned long long)__double_as_longlong(A));
+                store_async(to + 16, bar, __longlong_as_double((long long)__float_as_uint(m_in)), 0ull);
+            }
+        }
+    } else if (warp == PW + 2) {
+        // ---- exchange ----
+        for (int64_t i = 0; i < n_rows; ++i) {
+            const int slot = (int)(i % kRing);
+            const int64_t t = first + i * n_clusters;
+            if (lane == 0) mbar_expect_tx(&c.parts[slot], (uint32_t)(CL * (PW * 16 + 32)));
+            double w = 0.0;
+            if (a.mask == nullptr || a.mask[t] != 0) w = a.seq_weight[find_rollout_warp(a.cu_seqlens, a.M, a.row0 + t)];
+            if (!mbar_wait(&c.listed[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
+            const double Q = c.Q[slot], H = c.H[slot];
+            if (!wait_cluster(&c.parts[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
+            constexpr int N = kMaxCluster * PW / 32;
+            double v[N], S2 = 0.0, S1 = 0.0, A = 0.0;
+            float pm[N], m2 = -INFINITY, m1 = -INFINITY, lm = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                v[k] = 0.0;
+                pm[k] = -INFINITY;
+                if (lane + 32 * k < CL * PW) {
+                    const PipePart p = part[slot * CL * PW + lane + 32 * k];
+                    v[k] = p.s;
+                    pm[k] = p.m;
+                }
+                m2 = max_nan(m2, pm[k]);
+            }
+            if (lane < CL) {
+                const PipeList l = c.list[slot][lane];
+                S1 = l.s;
+                A = l.a;
+                m1 = lm = l.m;
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                m2 = max_nan(m2, __shfl_xor_sync(PODS_FULL_MASK, m2, d));
+                m1 = max_nan(m1, __shfl_xor_sync(PODS_FULL_MASK, m1, d));
+            }
+            const float zmax = max_nan(m1, m2);
+            const bool bad = !(fabsf(zmax) < INFINITY);
+            const PartRef top(m2, cexp);
+            if (!bad) {
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (v[k] > 0.0) S2 += v[k] * PartRef(pm[k], cexp).scale_to(top);
+                S1 = lm > -INFINITY ? S1 * exp(((double)lm - (double)zmax) * tau_inv) : 0.0;
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                S2 += __shfl_xor_sync(PODS_FULL_MASK, S2, d);
+                S1 += __shfl_xor_sync(PODS_FULL_MASK, S1, d);
+                A += __shfl_xor_sync(PODS_FULL_MASK, A, d);
+            }
+            // the reference's weight over e^(zmax / tau), and its logarithm
+            const double lpart = top.far ? ((double)m2 - (double)zmax) * (double)cexp * kLn2 : ((double)top.R - (double)zmax * (double)cexp) * kLn2;
+            const double pw = m2 > -INFINITY ? exp(lpart) : 0.0;
+            const double Z = S2 * pw + S1;
+            const double r = a.rest && m2 > -INFINITY ? fmax(0.0, 1.0 - Q) : 0.0;
+            const double g = (double)a.grad_scale * w * tau_inv;
+            if (lane == 0) {
+                Factors f;
+                f.p_scale = bad ? (double)NAN : (Q + r) / Z;
+                f.g = g;
+                f.coef = (float)(g * (f.p_scale * pw - (r > 0.0 ? r / S2 : 0.0)));
+                f.m2 = m2;
+                f.zmax = zmax;
+                f.mode = w != 0.0;
+                c.f[slot] = f;
+                arrive_local(&c.ready[slot]);
+                if (rank == 0) {                       // nobody waits for these
+                    double kl = 0.0;
+                    if (w != 0.0) {
+                        kl = NAN;
+                        if (!bad) {
+                            const double lz = log(Z);
+                            kl = H - A + Q * ((double)zmax * tau_inv + lz);
+                            if (r > 0.0) kl += r * (log(r) - (lpart + log(S2) - lz));
+                        } else {
+                            pods_raise(a.status, zmax == -INFINITY ? PODS_STATUS_EMPTY_ROW : PODS_STATUS_NONFINITE_LOGIT);
+                        }
+                    }
+                    a.kl[t] = (float)kl;
+                    a.row_loss[t] = w != 0.0 ? w * kl : 0.0;
+                }
+            }
+            __syncwarp();
+        }
+    } else {
+        // ---- consumers ----
+        auto back = [&](int64_t i) {
+            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+            const int64_t t = first + i * n_clusters;
+            wait_ready(i);
+            if (a.dlogits != nullptr) {
+                const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+                const uint4* const buf = stages + (size_t)st * a.seg;
+                const raw* const elems = reinterpret_cast<const raw*>(buf);
+                const Factors f = c.f[slot];
+                raw* const drow = static_cast<raw*>(a.dlogits) + t * a.ldd;
+                const int id_lo = max(0, s.id0), id_hi = min(a.V, s.id0 + s.cnt * E);
+                const int dlead = (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(raw));
+                // gradient vectors (16-byte boundaries of dlogits) whole inside [id_lo, id_hi), dealt out to the warps
+                const int v_lo = (id_lo + dlead + E - 1) / E, v_hi = max(v_lo, (id_hi + dlead) / E);
+                const int share = (v_hi - v_lo + PW - 1) / PW;
+                const int w_lo = min(v_hi, v_lo + warp * share), w_hi = min(v_hi, w_lo + share);
+                uint4* const dvec = reinterpret_cast<uint4*>(drow - dlead);
+                const PartRef ref(f.m2, cexp);
+                const unsigned long long coef2 = pack2(f.coef, f.coef);
+                auto edge = [&](int id) {
+                    return f.mode ? El::from_float(f.coef * (float)ref.exp1(El::to_float(elems[id - s.id0]))) : (raw)0;
+                };
+                if (id_lo < id_hi) {
+                    const int off = v_lo * E - dlead - s.id0, shift = off % E, to_buf = off / E - v_lo;
+                    if (f.mode == 0) {
+                        for (int v = w_lo + lane; v < w_hi; v += 32) dvec[v] = make_uint4(0u, 0u, 0u, 0u);
+                    } else if (shift == 0 && !ref.far) {
+#pragma unroll 2
+                        for (int v = w_lo + lane; v < w_hi; v += 32)
+                            if (PODS_INDEX_OK(v + to_buf, s.cnt, a.status)) {
+                                float x[E];
+                                El::unpack(buf[v + to_buf], x);
+                                ref.template exps<false>(x);
+#pragma unroll
+                                for (int e = 0; e < E; e += 2) unpack2(mul2(pack2(x[e], x[e + 1]), coef2), x[e], x[e + 1]);
+                                dvec[v] = El::pack(x);
+                            }
+                    } else {
+                        for (int v = w_lo + lane; v < w_hi; v += 32) {
+                            const int at = v * E - dlead - s.id0;
+                            if (PODS_INDEX_OK(at, s.cnt * E - E + 1, a.status)) {
+                                float x[E];
+#pragma unroll
+                                for (int e = 0; e < E; ++e) x[e] = El::to_float(elems[at + e]);
+                                if (ref.far) ref.template exps<true>(x);
+                                else ref.template exps<false>(x);
+#pragma unroll
+                                for (int e = 0; e < E; ++e) x[e] *= f.coef;
+                                dvec[v] = El::pack(x);
+                            }
+                        }
+                    }
+                    if (warp == 0) {                   // the ids outside whole vectors: less than 2 E
+                        const int head = min(id_hi, v_lo * E - dlead), tail = max(head, v_hi * E - dlead);
+                        if (id_lo + lane < head) drow[id_lo + lane] = edge(id_lo + lane);
+                        if (tail + lane < id_hi) drow[tail + lane] = edge(tail + lane);
+                    }
+                }
+                __syncwarp();                          // the listed ids of my slice over what was just stored there
+                if (f.mode)
+                    for (int k = lane; k < c.n_entry[slot]; k += 32) {
+                        const Entry e = c.entry[slot * a.K + k];
+                        const int v = (e.id + dlead) / E;
+                        const int owner = v < v_lo || v >= v_hi ? 0 : (v - v_lo) / share;
+                        if (owner == warp) {
+                            const double p = exp(((double)e.z - (double)f.zmax) * tau_inv) * f.p_scale;      // (Q + r) p
+                            drow[e.id] = El::from_float((float)(f.g * (p - e.q)));
+                        }
+                    }
+            }
+            fence_async_proxy();                       // the list warp wrote to the stage, and copies refill it
+            __syncwarp();
+            if (lane == 0) arrive_local(&c.done[st]);
+        };
+        for (int64_t i = 0; i < n_rows; ++i) {
+            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+            const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
+            const uint4* const buf = stages + (size_t)st * a.seg;
+            const int share = (s.cnt + PW - 1) / PW, lo = min(s.cnt, warp * share), hi = min(s.cnt, lo + share);
+            if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
+            if (!mbar_wait(&c.listed[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
+            float m = -INFINITY;
+#pragma unroll 4
+            for (int j = lo + lane; j < hi; j += 32) m = max_nan(m, El::vec_max(buf[j]));
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(PODS_FULL_MASK, m, d));
+            const PartRef ref(m, cexp);
+            double sum = 0.0;
+            if (!ref.far) {
+#pragma unroll 2
+                for (int j = lo + lane; j < hi; j += 32) {
+                    float x[E];
+                    El::unpack(buf[j], x);
+                    ref.template exps<false>(x);
+                    sum += (double)vec_add(x);
+                }
+            } else {
+                for (int j = lo + lane; j < hi; j += 32) {
+                    float x[E];
+                    El::unpack(buf[j], x);
+                    ref.template exps<true>(x);
+                    sum += (double)vec_add(x);
+                }
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
+            if (lane < CL)
+                store_async(mapa(part + slot * CL * PW + rank * PW + warp, lane), mapa(&c.parts[slot], lane), sum,
+                            (unsigned long long)__float_as_uint(m));
+            if (i > 0) back(i - 1);
+        }
+        if (n_rows > 0) back(n_rows - 1);
+    }
+    if (late && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
+    __syncwarp();
+    cl.sync();                                         // no CTA leaves while a peer may still write its parts
+}
+
 size_t align_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
 
 constexpr size_t kMaxSmem = 227 * 1024;
 constexpr size_t kSegmentBytes = 40 * 1024;
 
+constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold for two of them to share an SM
+constexpr int64_t kPipeMinBytes = 16 << 20;
+
 template <int DT, int KP>
 int launch_distill(DistillArgs& a, cudaStream_t stream) {
     const int esize = DT == PODS_DTYPE_F32 ? 4 : 2;
+    if (a.K <= kPipeK && a.T * a.V * esize >= kPipeMinBytes) {
+        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size
+        static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
+        for (int size : kSizes) {
+            a.seg = segment_vectors(a.V, esize, size);
+            const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)kStages * a.seg * 16;
+            if (smem <= kHalfSmBytes)
+                return launch_row_clusters<pods_distill_pipe_kernel<DT>>(a, a.T, size, kPipeThreads, smem, stream);
+        }
+    }
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
     a.seg = segment_vectors(a.V, esize, cl);

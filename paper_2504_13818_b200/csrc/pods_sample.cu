@@ -42,7 +42,6 @@ constexpr int kBins = 1024;                   // stretches of the mass histogram
 constexpr int kNoCut = 0x7fffffff;
 constexpr int kMarked = -2;                   // token of a row that the pipeline leaves to fp64
 constexpr int kRedoRows = 8192;               // rows of a cluster between two visits of the marked ones
-constexpr double kLn2 = 0.6931471805599453;
 
 // Errors of the fast sums, rigorously bounded.  An exponential e_v is off by at most (slope |d_v| + kFlat) of itself: the
 // rounding of the fused multiply-add (2^-24 of the exponent; `far` rows take a difference first, 2^-24 more) and of log2e / tau,
@@ -115,53 +114,6 @@ __device__ __forceinline__ RowCtrl& row_ctrl() { return *reinterpret_cast<RowCtr
 __device__ __forceinline__ uint4* row_buf() { return reinterpret_cast<uint4*>(smem_ + kRowCtrlBytes); }
 __device__ __forceinline__ FilterCtrl& filter_ctrl(const SampleArgs& a) { return *reinterpret_cast<FilterCtrl*>(smem_ + kRowCtrlBytes + a.seg * 16); }
 constexpr int kFilterCtrlBytes = (sizeof(FilterCtrl) + 127) & ~127;
-
-__device__ __forceinline__ double pow2(int n) {       // n <= 0; below the normal numbers: 0
-    return n < -1000 ? 0.0 : __hiloint2double((1023 + n) << 20, 0);
-}
-
-// e = 2^(x c - R).  R is an integer, at least m c; where the product is so large that floats have no fractions, the
-// difference to the maximum is taken first and `far` parts are related by fp64 exponentials.
-struct PartRef {
-    float m, R, c;
-    bool far;
-    __device__ __forceinline__ PartRef(float m_, float c_) : c(c_) {
-        m = fabsf(m_) < INFINITY ? m_ : 0.0f;
-        R = ceilf(__fmul_ru(m, c));
-        far = !(fabsf(R) < 0x1p23f);
-    }
-    template <bool FAR, int E>
-    __device__ __forceinline__ void exps(float (&x)[E]) const {
-        const unsigned long long c2 = pack2(c, c), off2 = FAR ? pack2(-m, -m) : pack2(-R, -R);
-#pragma unroll
-        for (int i = 0; i < E; i += 2) {
-            const unsigned long long v = pack2(x[i], x[i + 1]);
-            float p, q;
-            unpack2(FAR ? mul2(add2(v, off2), c2) : fma2(v, c2, off2), p, q);
-            x[i] = ex2_approx(p);
-            x[i + 1] = ex2_approx(q);
-        }
-    }
-    __device__ __forceinline__ double exp1(float x) const { return (double)ex2_approx(far ? (x - m) * c : fmaf(x, c, -R)); }
-    // what sums relative to this reference are multiplied with to be relative to that of `top`, the row's
-    __device__ __forceinline__ double scale_to(const PartRef& top) const {
-        if (!top.far) return pow2((int)fmaxf(R - top.R, -2000.0f));
-        return exp2((far ? (double)m * (double)c : (double)R) - (double)top.m * (double)c);
-    }
-    // ln of this reference's own weight over e^(m / tau): what log sums relative to it lack
-    __device__ __forceinline__ double log_offset() const { return far ? 0.0 : ((double)R - (double)m * (double)c) * kLn2; }
-};
-
-// Inclusive scan over a warp.
-template <typename T>
-__device__ __forceinline__ T warp_scan(T v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const T o = __shfl_up_sync(PODS_FULL_MASK, v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
-}
 
 // Inclusive scan over the CTA in thread order; *total is the sum.
 __device__ __forceinline__ double block_scan(double v, double* part, double* total) {
@@ -1258,35 +1210,6 @@ struct PolicyCtrl {
 // control block of a CTA in a cluster of cl
 __host__ __device__ constexpr int policy_ctrl_bytes(int cl) {
     return ((int)offsetof(PolicyCtrl, part) + kRing * cl * PW * (int)sizeof(Part) + 127) & ~127;
-}
-
-__device__ __forceinline__ uint32_t mapa(const void* p, int rank) {
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-    return r;
-}
-// 16 bytes into a CTA of the cluster, counted on an mbarrier there.
-__device__ __forceinline__ void store_async(uint32_t at, uint32_t bar, double a, unsigned long long b) {
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];"
-                 ::"r"(at), "l"(__double_as_longlong(a)), "l"(b), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void arrive_local(unsigned long long* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ bool wait_cluster(unsigned long long* bar, uint32_t parity, uint32_t limit) {
-    for (uint32_t i = 0; i < limit; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(kSuspendNs) : "memory");
-        if (ok) return true;
-    }
-    return false;
 }
 
 template <int DT>

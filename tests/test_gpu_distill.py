@@ -290,3 +290,35 @@ def test_empty_chunk():
                                         torch.ones(1, dtype=torch.float64, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda"),
                                         0, None, acc)
     assert kl.numel() == 0 and dl.shape == (0, 100) and float(acc.item()) == 0.0
+
+
+@pytest.mark.parametrize("dtype,T,V,K,pad,offset", [("bf16", 300, 32000, 64, 0, 0), ("fp32", 260, 17001, 128, 3, 1), ("fp16", 1800, 5003, 33, 8, 5),
+                                                    ("bf16", 66, 151936, 8, 0, 0), ("bf16", 9000, 1000, 5, 0, 0)])
+def test_many_rows(dtype, T, V, K, pad, offset):
+    """Enough rows that each cluster takes several in a row (every stage and slot used more than once), with masked rows, ids
+    twice, unused entries and rows without a distribution among them; in every mode, with the gradient at another alignment
+    than the logits and in place."""
+    b = make(T, V, K, dtype, seed=V, pad=pad, offset=offset, M=17)
+    b["ids"][3, K - 1] = b["ids"][3, 0]
+    b["ids"][T // 2, K // 2:] = -1
+    b["ids"][T - 1, :] = -1
+    b["mask"][3] = b["mask"][T // 2] = b["mask"][T - 1] = 1
+    for i, mode in enumerate(MODES):
+        got = run(b, tau=1.7, grad_scale=0.5, **mode)
+        check(b, got, tau=1.7, rest=mode["rest"], grad_scale=0.5)
+        alone = run(b, tau=1.7, want_grad=False, **mode)
+        assert np.array_equal(alone["kl"], got["kl"]) and alone["loss"] == got["loss"]
+    b["mask"][5] = b["mask"][7] = 1
+    b["mask"][8] = 0
+    b["z"][5] = -np.inf
+    b["z"][7, V - 1] = np.nan
+    b["z"][8, 0] = np.nan
+    bits = binding.STATUS_EMPTY_ROW | binding.STATUS_NONFINITE_LOGIT
+    got = run(b, rest=True, expect_status=bits)
+    check(b, got, rest=True)
+    wide = torch.full((T, V + 13), 5.0, dtype=DT[dtype], device="cuda")
+    pitched = run(b, rest=True, dlogits=wide[:, 4:V + 4], expect_status=bits)
+    same = lambda x, y: bool(((x == y) | (torch.isnan(x) & torch.isnan(y))).all())  # noqa: E731
+    assert same(pitched["dl"], got["dl"]) and (wide[:, :4] == 5.0).all() and (wide[:, V + 4:] == 5.0).all()
+    inplace = run(b, rest=True, dlogits=b["z"], expect_status=bits)
+    assert same(inplace["dl"], got["dl"]) and np.array_equal(inplace["kl"], got["kl"], equal_nan=True)
