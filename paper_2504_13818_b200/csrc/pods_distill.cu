@@ -45,7 +45,13 @@ struct DistillArgs {
     void* dlogits;
     int64_t ldd;
     double* row_loss;
+    struct RowPrep* prep;                              // workspace: what a row needs besides its logits (many rows)
     uint32_t* status;
+};
+
+struct alignas(16) RowPrep {
+    double w;                                          // mask_t w_i
+    double L, Q, H;                                    // the list's log-normaliser, sum q, sum q log q
 };
 
 struct Xch {
@@ -405,16 +411,66 @@ pods_distill_kernel(const DistillArgs a) {
     }
 }
 
+// One warp a row: its weight and what the teacher's list says by itself.
+__global__ void __launch_bounds__(256)
+distill_prep_kernel(const DistillArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (t >= a.T) return;
+    RowPrep p = {0.0, 0.0, 0.0, 0.0};
+    if (a.mask == nullptr || a.mask[t] != 0) {
+        p.w = a.seq_weight[find_rollout_warp(a.cu_seqlens, a.M, a.row0 + t)];
+        const double tau_inv = 1.0 / (double)a.temperature;
+        const int32_t* const ids = a.ids + t * a.ldk;
+        const float* const vals = a.values + t * a.ldk;
+        bool odd = false;
+        float ymax = -INFINITY;
+        for (int j = lane; j < a.K; j += 32) {
+            const int id = ids[j];
+            if (id >= 0 && id < a.V) ymax = max_nan(ymax, vals[j]);
+            else odd |= id != -1;
+        }
+        if (__any_sync(PODS_FULL_MASK, odd) && lane == 0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
+        if (a.teacher_lse != nullptr) {
+            p.L = (double)a.teacher_lse[t];
+        } else {
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) ymax = max_nan(ymax, __shfl_xor_sync(PODS_FULL_MASK, ymax, d));
+            const double ref = ymax == -INFINITY ? 0.0 : (double)ymax;         // no entry at all: every q is 0
+            double sum = 0.0;
+            for (int j = lane; j < a.K; j += 32)
+                if (ids[j] >= 0 && ids[j] < a.V) sum += exp(((double)vals[j] - ref) * tau_inv);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
+            p.L = ref * tau_inv + (sum > 0.0 || sum != sum ? log(sum) : 0.0);
+        }
+        for (int j = lane; j < a.K; j += 32)
+            if (ids[j] >= 0 && ids[j] < a.V) {
+                const double lq = (double)vals[j] * tau_inv - p.L, q = exp(lq);
+                p.Q += q;
+                if (q != 0.0) p.H += q * lq;
+            }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            p.Q += __shfl_xor_sync(PODS_FULL_MASK, p.Q, d);
+            p.H += __shfl_xor_sync(PODS_FULL_MASK, p.H, d);
+        }
+    }
+    if (lane == 0) a.prep[t] = p;
+}
+
 // ---- many rows: a pipeline ------------------------------------------------------------------------------------------------
 // The same arithmetic where rows come by the hundred and every SM holds two CTAs (lists of up to kPipeK entries): warps with one
 // task each that meet only at mbarriers.  With every warp doing everything and a dozen CTA barriers a row, 4096 rows of 151936
 // took 731 us, half the time waiting at barriers.
 //   producer  one thread: the row's segment into one of three stages, as soon as the consumers have left it
-//   list      one warp: the teacher's probabilities, the listed logits out of the stage (their slots become -inf), the list's
-//            sums to every CTA of the cluster; it works a row ahead of the others
+//   list      one warp: the listed logits out of the stage (their slots become -inf), their sums to every CTA of the cluster;
+//            it works a row ahead of the others
 //   consumer  eight warps: front(i) maximum and sum of their slice, sent to every CTA; back(i - 1) the gradient of the row
 //            before, whose factors have had a whole sweep to arrive, and the listed entries of their slice
 //   exchange  one warp: all parts of a row into the row's factors, loss and status
+// What the list says by itself (its normaliser, Q, sum q log q) and the row's weight are made beforehand, a warp a row: done by
+// the list warp of each CTA they took 7200 of a row's 9900 cycles, and every other warp waited for that one.
 // Parts and factors have four slots each.  A part of row i is sent after its sender has seen the factors of row i - 2, which
 // took every CTA's parts of row i - 2, which were sent after the factors of row i - 4 were made: the slot of row i - 4 is free.
 constexpr int PW = 8;
@@ -449,7 +505,6 @@ struct PipeCtrl {
     unsigned long long parts[kRing];          // all parts of the cluster have arrived
     unsigned long long ready[kRing];          // the factors are there
     Factors f[kRing];
-    double Q[kRing], H[kRing];                // sum q, sum q log q
     int n_entry[kRing];
     alignas(16) PipeList list[kRing][kMaxCluster];
     alignas(16) Entry entry[1];               // [kRing][K], then PipePart [kRing][CL PW]
@@ -518,7 +573,8 @@ pods_distill_pipe_kernel(const DistillArgs a) {
         // ---- list ----
         constexpr int KP = kPipeK / 32;
         int id_next[KP];
-        float y_next[KP], lse_next = 0.0f;
+        float y_next[KP];
+        double L_next = 0.0;
         auto fetch = [&](int64_t t) {
 #pragma unroll
             for (int k = 0; k < KP; ++k) {
@@ -526,7 +582,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                 id_next[k] = j < a.K ? a.ids[t * a.ldk + j] : -1;
                 y_next[k] = j < a.K ? a.values[t * a.ldk + j] : -INFINITY;
             }
-            if (a.teacher_lse != nullptr) lse_next = a.teacher_lse[t];
+            L_next = a.prep[t].L;
         };
         if (n_rows > 0) fetch(first);
         for (int64_t i = 0; i < n_rows; ++i) {
@@ -534,129 +590,94 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             const int64_t t = first + i * n_clusters;
             const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
             raw* const elems = reinterpret_cast<raw*>(stages + (size_t)st * a.seg);
-            int id[KP], at[KP];
-            float y[KP], ymax = -INFINITY;
-            double q[KP], L = (double)lse_next;
-            bool odd = false;
+            Entry* const entry = c.entry + slot * a.K;
+            const double L = L_next;
+            const int id_lo = max(0, s.id0), id_hi = min(a.V, s.id0 + s.cnt * E);
+            int id[KP];
+            float y[KP], z[KP];
 #pragma unroll
             for (int k = 0; k < KP; ++k) {
                 id[k] = id_next[k];
                 y[k] = y_next[k];
-                if (id[k] < 0 || id[k] >= a.V) {
-                    odd |= id[k] != -1;
-                    id[k] = -1;
-                    y[k] = -INFINITY;
-                }
-                ymax = max_nan(ymax, y[k]);
             }
             if (i + 1 < n_rows) fetch(t + n_clusters);
-            if (a.teacher_lse == nullptr) {
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) ymax = max_nan(ymax, __shfl_xor_sync(PODS_FULL_MASK, ymax, d));
-                const double ref = ymax == -INFINITY ? 0.0 : (double)ymax;     // no entry at all: every q is 0
-                double sum = 0.0;
-#pragma unroll
-                for (int k = 0; k < KP; ++k)
-                    if (32 * k < a.K && id[k] >= 0) sum += exp(((double)y[k] - ref) * tau_inv);
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
-                L = ref * tau_inv + (sum > 0.0 || sum != sum ? log(sum) : 0.0);
-            }
-            double Q = 0.0, H = 0.0;
-#pragma unroll
-            for (int k = 0; k < KP; ++k) {
-                q[k] = 0.0;
-                if (32 * k < a.K && id[k] >= 0) {
-                    const double lq = (double)y[k] * tau_inv - L;
-                    q[k] = exp(lq);
-                    Q += q[k];
-                    if (q[k] != 0.0) H += q[k] * lq;
-                }
-            }
             if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
-            float z[KP], m_in = -INFINITY;
+            float m_in = -INFINITY;
 #pragma unroll
             for (int k = 0; k < KP; ++k) {
-                at[k] = id[k] - s.id0;
-                if (id[k] < 0 || at[k] < 0 || at[k] >= s.cnt * E) at[k] = -1;
-                z[k] = at[k] >= 0 ? El::to_float(elems[at[k]]) : -INFINITY;
+                if (id[k] < id_lo || id[k] >= id_hi) id[k] = -1;
+                z[k] = id[k] >= 0 ? El::to_float(elems[id[k] - s.id0]) : -INFINITY;
+                m_in = max_nan(m_in, z[k]);
             }
             __syncwarp();
 #pragma unroll
             for (int k = 0; k < KP; ++k)
-                if (at[k] >= 0) elems[at[k]] = (raw)(lane + 32 * k);           // one entry of an id stays visible
+                if (id[k] >= 0) elems[id[k] - s.id0] = (raw)(lane + 32 * k);   // one entry of an id stays visible
             __syncwarp();
             bool twice = false;
 #pragma unroll
-            for (int k = 0; k < KP; ++k) twice |= at[k] >= 0 && elems[at[k]] != (raw)(lane + 32 * k);
+            for (int k = 0; k < KP; ++k) twice |= id[k] >= 0 && elems[id[k] - s.id0] != (raw)(lane + 32 * k);
             twice = __any_sync(PODS_FULL_MASK, twice);                         // (and everyone has looked)
-            double qsum[KP];
-            unsigned speaks = 0;
-#pragma unroll
-            for (int k = 0; k < KP; ++k) {
-                qsum[k] = q[k];
-                if (at[k] >= 0) {
-                    elems[at[k]] = El::kNegInf;
-                    speaks |= 1u << k;
-                }
-            }
-            if (twice) {
-                // an id in several entries: the first speaks for it, with their mass added in list order
-#pragma unroll
-                for (int k = 0; k < KP; ++k)
-                    if (at[k] >= 0) {
-                        const int j = lane + 32 * k;
-                        for (int o = 0; o < a.K; ++o)
-                            if (o != j && a.ids[t * a.ldk + o] == id[k]) {
-                                if (o < j) speaks &= ~(1u << k);
-                                else qsum[k] += exp((double)a.values[t * a.ldk + o] * tau_inv - L);
-                            }
-                    }
-            }
-            fence_async_proxy();                       // what was written to the stage lies where a later copy goes
-            __syncwarp();
-            // entry slots of row i - 4 were read by back(i - 4), before the parts of row i - 2 that made its factors
-            if (i >= 2) wait_ready(i - 2);
-            int n = 0;
-            double A = 0.0, sum = 0.0;
-#pragma unroll
-            for (int k = 0; k < KP; ++k) {
-                const bool mine = speaks >> k & 1u;
-                const uint32_t b = __ballot_sync(PODS_FULL_MASK, mine);
-                if (mine) {
-                    Entry e;
-                    e.q = qsum[k];
-                    e.z = z[k];
-                    e.id = id[k];
-                    c.entry[slot * a.K + n + __popc(b & ((1u << lane) - 1u))] = e;
-                    m_in = max_nan(m_in, z[k]);
-                }
-                n += __popc(b);
-                if (at[k] >= 0 && q[k] != 0.0) A += q[k] * ((double)z[k] * tau_inv);
-            }
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) m_in = max_nan(m_in, __shfl_xor_sync(PODS_FULL_MASK, m_in, d));
 #pragma unroll
             for (int k = 0; k < KP; ++k)
-                if ((speaks >> k & 1u) && m_in > -INFINITY) sum += exp(((double)z[k] - (double)m_in) * tau_inv);
+                if (id[k] >= 0) elems[id[k] - s.id0] = El::kNegInf;
+            fence_async_proxy();                       // what was written to the stage lies where a later copy goes
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) m_in = max_nan(m_in, __shfl_xor_sync(PODS_FULL_MASK, m_in, d));
+            // entry slots of row i - 4 were read by back(i - 4), before the parts of row i - 2 that made its factors
+            if (i >= 2) wait_ready(i - 2);
+            // the entries together, the teacher's value in place of its mass
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < KP; ++k) {
+                const uint32_t b = __ballot_sync(PODS_FULL_MASK, id[k] >= 0);
+                if (id[k] >= 0) {
+                    Entry e;
+                    e.q = (double)y[k];
+                    e.z = z[k];
+                    e.id = id[k];
+                    entry[n + __popc(b & ((1u << lane) - 1u))] = e;
+                }
+                n += __popc(b);
+            }
+            __syncwarp();
+            double A = 0.0, sum = 0.0;
+            for (int k = lane; k < n; k += 32) {
+                const Entry e = entry[k];
+                const double lq = e.q * tau_inv - L, q = exp(lq);
+                if (q != 0.0) A += q * ((double)e.z * tau_inv);
+                if (m_in > -INFINITY && !twice) sum += exp64(((double)e.z - (double)m_in) * tau_inv);
+                entry[k].q = q;
+            }
+            if (twice) {
+                // an id in several entries (kept in list order): the first speaks for it, with their mass added; the others are
+                // taken off the list of entries
+                __syncwarp();
+                if (lane == 0) {
+                    int kept = 0;
+                    for (int k = 0; k < n; ++k) {
+                        const Entry e = entry[k];
+                        int o = 0;
+                        while (o < kept && entry[o].id != e.id) ++o;
+                        if (o < kept) {
+                            entry[o].q += e.q;
+                        } else {
+                            entry[kept++] = e;
+                            if (m_in > -INFINITY) sum += exp64(((double)e.z - (double)m_in) * tau_inv);
+                        }
+                    }
+                    n = kept;
+                }
+                n = __shfl_sync(PODS_FULL_MASK, n, 0);
+            }
+            if (lane == 0) c.n_entry[slot] = n;
+            __syncwarp();
+            if (lane == 0) arrive_local(&c.listed[slot]);
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) {
-                Q += __shfl_xor_sync(PODS_FULL_MASK, Q, d);
-                H += __shfl_xor_sync(PODS_FULL_MASK, H, d);
                 A += __shfl_xor_sync(PODS_FULL_MASK, A, d);
                 sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
             }
-            if (lane == 0) {
-                c.Q[slot] = Q;
-                c.H[slot] = H;
-                c.n_entry[slot] = n;
-            }
-            if (__any_sync(PODS_FULL_MASK, odd) && lane == 0 && rank == 0) {
-                const bool live = a.mask == nullptr || a.mask[t] != 0;
-                if (live) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
-            }
-            __syncwarp();
-            if (lane == 0) arrive_local(&c.listed[slot]);
             if (lane < CL) {
                 const uint32_t to = mapa(&c.list[slot][rank], lane), bar = mapa(&c.parts[slot], lane);
                 store_async(to, bar, sum, (unsigned long long)__double_as_longlong(A));
@@ -665,14 +686,14 @@ pods_distill_pipe_kernel(const DistillArgs a) {
         }
     } else if (warp == PW + 2) {
         // ---- exchange ----
+        RowPrep next = {0.0, 0.0, 0.0, 0.0};
+        if (n_rows > 0) next = a.prep[first];
         for (int64_t i = 0; i < n_rows; ++i) {
             const int slot = (int)(i % kRing);
             const int64_t t = first + i * n_clusters;
             if (lane == 0) mbar_expect_tx(&c.parts[slot], (uint32_t)(CL * (PW * 16 + 32)));
-            double w = 0.0;
-            if (a.mask == nullptr || a.mask[t] != 0) w = a.seq_weight[find_rollout_warp(a.cu_seqlens, a.M, a.row0 + t)];
-            if (!mbar_wait(&c.listed[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
-            const double Q = c.Q[slot], H = c.H[slot];
+            const double w = next.w, Q = next.Q, H = next.H;
+            if (i + 1 < n_rows) next = a.prep[t + n_clusters];
             if (!wait_cluster(&c.parts[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
             constexpr int N = kMaxCluster * PW / 32;
             double v[N], S2 = 0.0, S1 = 0.0, A = 0.0;
@@ -706,7 +727,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
 #pragma unroll
                 for (int k = 0; k < N; ++k)
                     if (v[k] > 0.0) S2 += v[k] * PartRef(pm[k], cexp).scale_to(top);
-                S1 = lm > -INFINITY ? S1 * exp(((double)lm - (double)zmax) * tau_inv) : 0.0;
+                S1 = lm > -INFINITY ? S1 * exp64(((double)lm - (double)zmax) * tau_inv) : 0.0;
             }
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) {
@@ -716,7 +737,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             }
             // the reference's weight over e^(zmax / tau), and its logarithm
             const double lpart = top.far ? ((double)m2 - (double)zmax) * (double)cexp * kLn2 : ((double)top.R - (double)zmax * (double)cexp) * kLn2;
-            const double pw = m2 > -INFINITY ? exp(lpart) : 0.0;
+            const double pw = m2 > -INFINITY ? exp64(lpart) : 0.0;
             const double Z = S2 * pw + S1;
             const double r = a.rest && m2 > -INFINITY ? fmax(0.0, 1.0 - Q) : 0.0;
             const double g = (double)a.grad_scale * w * tau_inv;
@@ -750,7 +771,17 @@ pods_distill_pipe_kernel(const DistillArgs a) {
         }
     } else {
         // ---- consumers ----
-        auto back = [&](int64_t i) {
+        // Where the gradient's vectors lie on the logits' (shift 0) and the exponents are of ordinary size, the sweep of front()
+        // serves back() too: a bf16 row keeps bf16(e) in the stage and back() scales it with two-term bf16 factors.  That is a
+        // second rounding of the ids outside the list, half a step each time, as in grpo_loss_chunk's gradient; it saves the
+        // exponentials' second pass, which with the first fills half of the special-function pipe.  fp16 could not hold e.
+        constexpr bool kKeep = DT == PODS_DTYPE_BF16;
+        struct Slice { float R; bool kept; };
+        auto aligned = [&](const Segment& s, int64_t t) {
+            const int dlead = (int)((reinterpret_cast<uintptr_t>(static_cast<raw*>(a.dlogits) + t * a.ldd) & 15) / sizeof(raw));
+            return ((s.id0 + dlead) % E) == 0;
+        };
+        auto back = [&](int64_t i, const Slice& slice) {
             const int st = (int)(i % kStages), slot = (int)(i % kRing);
             const int64_t t = first + i * n_clusters;
             wait_ready(i);
@@ -760,74 +791,96 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                 const raw* const elems = reinterpret_cast<const raw*>(buf);
                 const Factors f = c.f[slot];
                 raw* const drow = static_cast<raw*>(a.dlogits) + t * a.ldd;
-                const int id_lo = max(0, s.id0), id_hi = min(a.V, s.id0 + s.cnt * E);
-                const int dlead = (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(raw));
-                // gradient vectors (16-byte boundaries of dlogits) whole inside [id_lo, id_hi), dealt out to the warps
-                const int v_lo = (id_lo + dlead + E - 1) / E, v_hi = max(v_lo, (id_hi + dlead) / E);
-                const int share = (v_hi - v_lo + PW - 1) / PW;
-                const int w_lo = min(v_hi, v_lo + warp * share), w_hi = min(v_hi, w_lo + share);
-                uint4* const dvec = reinterpret_cast<uint4*>(drow - dlead);
+                const int share = (s.cnt + PW - 1) / PW, lo = min(s.cnt, warp * share), hi = min(s.cnt, lo + share);
                 const PartRef ref(f.m2, cexp);
-                const unsigned long long coef2 = pack2(f.coef, f.coef);
-                auto edge = [&](int id) {
-                    return f.mode ? El::from_float(f.coef * (float)ref.exp1(El::to_float(elems[id - s.id0]))) : (raw)0;
+                // element k of the segment, alone
+                auto one = [&](int k) {
+                    if (f.mode == 0) return (raw)0;
+                    const float x = El::to_float(elems[k]);
+                    return El::from_float(f.coef * (kKeep && slice.kept ? x * (float)pow2_any(slice.R - ref.R) : (float)ref.exp1(x)));
                 };
-                if (id_lo < id_hi) {
-                    const int off = v_lo * E - dlead - s.id0, shift = off % E, to_buf = off / E - v_lo;
+                if (aligned(s, t)) {
+                    uint4* const dvec = reinterpret_cast<uint4*>(drow + s.id0);
+                    const unsigned long long coef2 = pack2(f.coef, f.coef);
+                    const int whole_lo = max(lo, s.full0), whole_hi = min(hi, s.full1);
                     if (f.mode == 0) {
-                        for (int v = w_lo + lane; v < w_hi; v += 32) dvec[v] = make_uint4(0u, 0u, 0u, 0u);
-                    } else if (shift == 0 && !ref.far) {
-#pragma unroll 2
-                        for (int v = w_lo + lane; v < w_hi; v += 32)
-                            if (PODS_INDEX_OK(v + to_buf, s.cnt, a.status)) {
-                                float x[E];
-                                El::unpack(buf[v + to_buf], x);
-                                ref.template exps<false>(x);
-#pragma unroll
-                                for (int e = 0; e < E; e += 2) unpack2(mul2(pack2(x[e], x[e + 1]), coef2), x[e], x[e + 1]);
-                                dvec[v] = El::pack(x);
-                            }
-                    } else {
-                        for (int v = w_lo + lane; v < w_hi; v += 32) {
-                            const int at = v * E - dlead - s.id0;
-                            if (PODS_INDEX_OK(at, s.cnt * E - E + 1, a.status)) {
-                                float x[E];
-#pragma unroll
-                                for (int e = 0; e < E; ++e) x[e] = El::to_float(elems[at + e]);
-                                if (ref.far) ref.template exps<true>(x);
-                                else ref.template exps<false>(x);
-#pragma unroll
-                                for (int e = 0; e < E; ++e) x[e] *= f.coef;
-                                dvec[v] = El::pack(x);
-                            }
+                        for (int j = whole_lo + lane; j < whole_hi; j += 32) dvec[j] = make_uint4(0u, 0u, 0u, 0u);
+                    } else if (kKeep && slice.kept) {
+                        const float coef = f.coef * (float)pow2_any(slice.R - ref.R);
+                        const uint16_t hi16 = pods_loss::to_bf16_bits(coef);
+                        const uint16_t lo16 = pods_loss::to_bf16_bits(coef - __uint_as_float((uint32_t)hi16 << 16));
+                        const uint32_t c_hi = (uint32_t)hi16 * 0x10001u, c_lo = (uint32_t)lo16 * 0x10001u;
+#pragma unroll 4
+                        for (int j = whole_lo + lane; j < whole_hi; j += 32) {
+                            uint4 q = buf[j];
+                            pods_loss::scale_vec(q, c_hi, c_lo);
+                            dvec[j] = q;
                         }
+                    } else {
+#pragma unroll 2
+                        for (int j = whole_lo + lane; j < whole_hi; j += 32) {
+                            float x[E];
+                            El::unpack(buf[j], x);
+                            if (ref.far) ref.template exps<true>(x);
+                            else ref.template exps<false>(x);
+#pragma unroll
+                            for (int e = 0; e < E; e += 2) unpack2(mul2(pack2(x[e], x[e + 1]), coef2), x[e], x[e + 1]);
+                            dvec[j] = El::pack(x);
+                        }
+                    }
+                    // the vectors that the row covers in part: its first and last
+                    for (int j = lo; j < hi; ++j) {
+                        if (j >= s.full0 && j < s.full1) { j = s.full1 - 1; continue; }
+                        const int id = s.id0 + j * E + lane;
+                        if (lane < E && id >= 0 && id < a.V) drow[id] = one(j * E + lane);
+                    }
+                    __syncwarp();                      // the listed ids of my slice over what was just stored there
+                } else {
+                    // gradient vectors (16-byte boundaries of dlogits) whole inside the segment's ids, dealt out anew
+                    const int id_lo = max(0, s.id0), id_hi = max(id_lo, min(a.V, s.id0 + s.cnt * E));
+                    const int dlead = (int)((reinterpret_cast<uintptr_t>(drow) & 15) / sizeof(raw));
+                    const int v_lo = (id_lo + dlead + E - 1) / E, v_hi = max(v_lo, (id_hi + dlead) / E);
+                    const int vshare = (v_hi - v_lo + PW - 1) / PW;
+                    const int w_lo = min(v_hi, v_lo + warp * vshare), w_hi = min(v_hi, w_lo + vshare);
+                    uint4* const dvec = reinterpret_cast<uint4*>(drow - dlead);
+                    for (int v = w_lo + lane; v < w_hi; v += 32) {
+                        const int at = v * E - dlead - s.id0;
+                        float x[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] = PODS_INDEX_OK(at + e, s.cnt * E, a.status) ? El::to_float(elems[at + e]) : 0.0f;
+                        if (ref.far) ref.template exps<true>(x);
+                        else ref.template exps<false>(x);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] = f.mode ? x[e] * f.coef : 0.0f;
+                        dvec[v] = El::pack(x);
                     }
                     if (warp == 0) {                   // the ids outside whole vectors: less than 2 E
                         const int head = min(id_hi, v_lo * E - dlead), tail = max(head, v_hi * E - dlead);
-                        if (id_lo + lane < head) drow[id_lo + lane] = edge(id_lo + lane);
-                        if (tail + lane < id_hi) drow[tail + lane] = edge(tail + lane);
+                        if (id_lo + lane < head) drow[id_lo + lane] = one(id_lo + lane - s.id0);
+                        if (tail + lane < id_hi) drow[tail + lane] = one(tail + lane - s.id0);
                     }
+                    // all warps of the CTA have stored before any listed id goes over it
+                    asm volatile("bar.sync 1, %0;" ::"n"(PW * 32) : "memory");
                 }
-                __syncwarp();                          // the listed ids of my slice over what was just stored there
                 if (f.mode)
                     for (int k = lane; k < c.n_entry[slot]; k += 32) {
                         const Entry e = c.entry[slot * a.K + k];
-                        const int v = (e.id + dlead) / E;
-                        const int owner = v < v_lo || v >= v_hi ? 0 : (v - v_lo) / share;
-                        if (owner == warp) {
-                            const double p = exp(((double)e.z - (double)f.zmax) * tau_inv) * f.p_scale;      // (Q + r) p
+                        if ((e.id - s.id0) / E / share == warp) {
+                            const double p = exp64(((double)e.z - (double)f.zmax) * tau_inv) * f.p_scale;    // (Q + r) p
                             drow[e.id] = El::from_float((float)(f.g * (p - e.q)));
                         }
                     }
             }
-            fence_async_proxy();                       // the list warp wrote to the stage, and copies refill it
+            fence_async_proxy();                       // the stage was written to, and copies refill it
             __syncwarp();
             if (lane == 0) arrive_local(&c.done[st]);
         };
+        Slice before = {0.0f, false};
         for (int64_t i = 0; i < n_rows; ++i) {
             const int st = (int)(i % kStages), slot = (int)(i % kRing);
-            const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
-            const uint4* const buf = stages + (size_t)st * a.seg;
+            const int64_t t = first + i * n_clusters;
+            const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
+            uint4* const buf = stages + (size_t)st * a.seg;
             const int share = (s.cnt + PW - 1) / PW, lo = min(s.cnt, warp * share), hi = min(s.cnt, lo + share);
             if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
             if (!mbar_wait(&c.listed[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
@@ -837,6 +890,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(PODS_FULL_MASK, m, d));
             const PartRef ref(m, cexp);
+            const Slice now = {ref.R, kKeep && !ref.far && a.dlogits != nullptr && aligned(s, t)};
             double sum = 0.0;
             if (!ref.far) {
 #pragma unroll 2
@@ -844,6 +898,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                     float x[E];
                     El::unpack(buf[j], x);
                     ref.template exps<false>(x);
+                    if (kKeep && now.kept) buf[j] = El::pack(x);
                     sum += (double)vec_add(x);
                 }
             } else {
@@ -859,9 +914,10 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             if (lane < CL)
                 store_async(mapa(part + slot * CL * PW + rank * PW + warp, lane), mapa(&c.parts[slot], lane), sum,
                             (unsigned long long)__float_as_uint(m));
-            if (i > 0) back(i - 1);
+            if (i > 0) back(i - 1, before);
+            before = now;
         }
-        if (n_rows > 0) back(n_rows - 1);
+        if (n_rows > 0) back(n_rows - 1, before);
     }
     if (late && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
     __syncwarp();
@@ -885,8 +941,11 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
         for (int size : kSizes) {
             a.seg = segment_vectors(a.V, esize, size);
             const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)kStages * a.seg * 16;
-            if (smem <= kHalfSmBytes)
+            if (smem <= kHalfSmBytes) {
+                distill_prep_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, stream>>>(a);
+                PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
                 return launch_row_clusters<pods_distill_pipe_kernel<DT>>(a, a.T, size, kPipeThreads, smem, stream);
+            }
         }
     }
     int cl = 1;
@@ -900,7 +959,7 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
 }  // namespace
 
 extern "C" size_t pods_distill_chunk_workspace_bytes(int64_t T) {
-    return T < 0 ? 0 : align_up((size_t)T * sizeof(double), 256) + 256;
+    return T < 0 ? 0 : align_up((size_t)T * sizeof(double), 256) + align_up((size_t)T * sizeof(RowPrep), 256) + 256;
 }
 
 extern "C" int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* ids,
@@ -946,6 +1005,7 @@ extern "C" int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype
     a.dlogits = dlogits;
     a.ldd = ldd;
     a.row_loss = static_cast<double*>(workspace);
+    a.prep = reinterpret_cast<RowPrep*>(static_cast<unsigned char*>(workspace) + align_up((size_t)T * sizeof(double), 256));
     a.status = status;
     cudaStream_t s = pods_stream(stream);
     constexpr int kMany = PODS_MAX_TOPK / kThreads;

@@ -276,6 +276,10 @@ __device__ __forceinline__ double pow2(int n) {       // n <= 0; below the norma
     return n < -1000 ? 0.0 : __hiloint2double((1023 + n) << 20, 0);
 }
 
+__device__ __forceinline__ float pow2_any(float n) {  // n an integer; outside the normal numbers: 0 or +inf
+    return n < -126.0f ? 0.0f : n > 127.0f ? INFINITY : __uint_as_float((uint32_t)(127 + (int)n) << 23);
+}
+
 // e = 2^(x c - R).  R is an integer, at least m c; where the product is so large that floats have no fractions, the
 // difference to the maximum is taken first and `far` parts are related by fp64 exponentials.
 struct PartRef {
@@ -317,6 +321,16 @@ __device__ __forceinline__ T warp_scan(T v, int lane) {
         if (lane >= d) v += o;
     }
     return v;
+}
+
+// The same for any d: NaN stays, what overflows is +inf.
+__device__ __forceinline__ void exp64x4_any(double (&d)[4]) {
+    double e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = fmin(d[i], 700.0);
+    exp64x4(e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] = d[i] > 700.0 ? (double)INFINITY : d[i] == d[i] ? e[i] : d[i];
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }

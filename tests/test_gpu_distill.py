@@ -4,7 +4,8 @@ Sums of exponentials carry SUM_RTOL (see test_gpu_sample.py).  kl = H - A + Q lo
 sums enter through logarithms with factors Q, r and r, then one rounding to fp32.  A gradient entry is a sum of terms (the
 oracle's `terms` is the sum of their absolute values): each carries SUM_RTOL, the exponent's own error of 9e-8 per unit of
 |z - max| / tau ((2^-24 + 2^-25), natural units), 2^-22.5 of the exponential and three fp32 roundings; the entry is then
-rounded to the logits' type, half a step: eps / 2 of the value, or half the smallest subnormal."""
+rounded to the logits' type, half a step: eps / 2 of the value, or half the smallest subnormal.  A bf16 entry outside the list
+may be the product of an exponential that was itself kept as bf16, half a step more."""
 import numpy as np
 import pytest
 import torch
@@ -85,7 +86,12 @@ def check(b, got, tau=1.0, rest=False, grad_scale=1.0, z=None):
             depth = np.where(np.isfinite(z[t]), z[t].max() - z[t], 0.0) / tau
             err = np.abs(dl[t] - g * want["grad"])
             bar = g * want["terms"] * (SUM_RTOL + 9e-8 * depth + 2.0 ** -22.5 + 3 * 2.0 ** -24)
-            bar = bar * (1 + half) + half * np.abs(g * want["grad"]) + HALF_SUBNORMAL[b["dtype"]] * max(1.0, g)
+            steps = np.ones(z.shape[1])
+            if b["dtype"] == "bf16":
+                # fl(fl(e) c): (1 + half)^2 - 1 of the value; a listed id's entry is computed apart and rounded once
+                steps[:] = 2 + half
+                steps[ids[t][(ids[t] >= 0) & (ids[t] < z.shape[1])]] = 1
+            bar = bar * (1 + half) + half * steps * np.abs(g * want["grad"]) + HALF_SUBNORMAL[b["dtype"]] * max(1.0, g)
             assert (err <= bar).all(), (t, int(np.argmax(err - bar)), float((err - bar).max()))
     if np.isfinite(loss):
         assert abs(got["loss"] - loss) <= loss_tol
@@ -319,6 +325,8 @@ def test_many_rows(dtype, T, V, K, pad, offset):
     wide = torch.full((T, V + 13), 5.0, dtype=DT[dtype], device="cuda")
     pitched = run(b, rest=True, dlogits=wide[:, 4:V + 4], expect_status=bits)
     same = lambda x, y: bool(((x == y) | (torch.isnan(x) & torch.isnan(y))).all())  # noqa: E731
-    assert same(pitched["dl"], got["dl"]) and (wide[:, :4] == 5.0).all() and (wide[:, V + 4:] == 5.0).all()
+    # at another alignment than the logits a bf16 entry is rounded once, not twice: held to the oracle, not to the bits of `got`
+    check(b, pitched, rest=True)
+    assert (dtype == "bf16" or same(pitched["dl"], got["dl"])) and (wide[:, :4] == 5.0).all() and (wide[:, V + 4:] == 5.0).all()
     inplace = run(b, rest=True, dlogits=b["z"], expect_status=bits)
     assert same(inplace["dl"], got["dl"]) and np.array_equal(inplace["kl"], got["kl"], equal_nan=True)
