@@ -37,7 +37,7 @@ struct DistillArgs {
     int64_t M, row0;
     const uint8_t* mask;
     int64_t T;
-    int V, seg;
+    int V, seg, n_stages;
     float temperature;
     int rest;
     float grad_scale;
@@ -475,7 +475,7 @@ distill_prep_kernel(const DistillArgs a) {
 // took every CTA's parts of row i - 2, which were sent after the factors of row i - 4 were made: the slot of row i - 4 is free.
 constexpr int PW = 8;
 constexpr int kPipeThreads = (PW + 3) * 32;
-constexpr int kStages = 3, kRing = 4;
+constexpr int kMaxStages = 3, kRing = 4;
 constexpr int kPipeK = 128;                   // entries of a list: four a lane
 
 struct PipePart {                             // of one consumer warp
@@ -500,7 +500,7 @@ struct Factors {
     int mode;                                 // 0: a row of zeros
 };
 struct PipeCtrl {
-    unsigned long long full[kStages], done[kStages];   // the stage is loaded; its consumers have left it
+    unsigned long long full[kMaxStages], done[kMaxStages];   // the stage is loaded; its consumers have left it
     unsigned long long listed[kRing];         // the listed logits are out of the stage
     unsigned long long parts[kRing];          // all parts of the cluster have arrived
     unsigned long long ready[kRing];          // the factors are there
@@ -519,6 +519,7 @@ extern __shared__ __align__(128) unsigned char smem_[];
 template <int DT>
 __global__ void __launch_bounds__(kPipeThreads, 2)
 pods_distill_pipe_kernel(const DistillArgs a) {
+    const int n_stages = a.n_stages;
     using El = Elem<DT>;
     using raw = typename El::raw;
     constexpr int E = El::E;
@@ -529,9 +530,9 @@ pods_distill_pipe_kernel(const DistillArgs a) {
     uint4* const stages = reinterpret_cast<uint4*>(smem_ + pipe_ctrl_bytes(CL, a.K));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
-    const int64_t n_rows = first < a.T ? (a.T - first + n_clusters - 1) / n_clusters : 0;
+    const int n_rows = first < a.T ? (int)((a.T - first + n_clusters - 1) / n_clusters) : 0;
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < kMaxStages; ++i) {
             mbar_init(&c.full[i], 1);
             mbar_init(&c.done[i], PW);
         }
@@ -549,25 +550,30 @@ pods_distill_pipe_kernel(const DistillArgs a) {
     const float cexp = (float)(1.4426950408889634 * tau_inv);
     bool late = false;                                 // a wait ran out: no further one is worth its time
     auto spins = [&]() { return late ? 1u : kSpinLimit; };
-    auto wait_ready = [&](int64_t i) {
+    auto wait_ready = [&](int i) {
         if (!mbar_wait(&c.ready[i % kRing], (uint32_t)((i / kRing) & 1), spins())) late = true;
     };
 
     if (warp == PW) {
         // ---- producer ----
         if (lane == 0) {
-            for (int64_t i = 0; i < n_rows; ++i) {
-                const int st = (int)(i % kStages);
-                if (i >= kStages && !mbar_wait(&c.done[st], (uint32_t)((i / kStages - 1) & 1), spins())) late = true;
+            StageRing ring;
+            for (int i = 0; i < n_rows; ++i) {
+                const int st = ring.st;
+                if (i >= n_stages && !mbar_wait(&c.done[st], ring.parity ^ 1u, spins())) late = true;
                 const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
                 uint4* const buf = stages + (size_t)st * a.seg;
                 fill_edges<DT>(s, a.V, buf);
                 fence_async_proxy();                   // edges of an earlier row may lie where this row's copy goes
                 start_copy(s, buf, &c.full[st]);
+                ring.next(n_stages);
             }
             // every copy has landed before the CTA ends, also one that a consumer gave up on
-            for (int64_t i = n_rows > kStages ? n_rows - kStages : 0; i < n_rows; ++i)
-                if (!mbar_wait(&c.full[i % kStages], (uint32_t)((i / kStages) & 1), kSpinLimit)) late = true;
+            for (int k = 0; k < n_stages && k < n_rows; ++k) {
+                ring.st = ring.st == 0 ? n_stages - 1 : ring.st - 1;           // from the last row back
+                if (ring.st == n_stages - 1) ring.parity ^= 1u;
+                if (!mbar_wait(&c.full[ring.st], ring.parity, kSpinLimit)) late = true;
+            }
         }
     } else if (warp == PW + 1) {
         // ---- list ----
@@ -585,8 +591,9 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             L_next = a.prep[t].L;
         };
         if (n_rows > 0) fetch(first);
-        for (int64_t i = 0; i < n_rows; ++i) {
-            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+        StageRing ring;
+        for (int i = 0; i < n_rows; ++i, ring.next(n_stages)) {
+            const int st = ring.st, slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
             raw* const elems = reinterpret_cast<raw*>(stages + (size_t)st * a.seg);
@@ -601,7 +608,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                 y[k] = y_next[k];
             }
             if (i + 1 < n_rows) fetch(t + n_clusters);
-            if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
+            if (!mbar_wait(&c.full[st], ring.parity, spins())) late = true;
             float m_in = -INFINITY;
 #pragma unroll
             for (int k = 0; k < KP; ++k) {
@@ -688,8 +695,8 @@ pods_distill_pipe_kernel(const DistillArgs a) {
         // ---- exchange ----
         RowPrep next = {0.0, 0.0, 0.0, 0.0};
         if (n_rows > 0) next = a.prep[first];
-        for (int64_t i = 0; i < n_rows; ++i) {
-            const int slot = (int)(i % kRing);
+        for (int i = 0; i < n_rows; ++i) {
+            const int slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             if (lane == 0) mbar_expect_tx(&c.parts[slot], (uint32_t)(CL * (PW * 16 + 32)));
             const double w = next.w, Q = next.Q, H = next.H;
@@ -781,8 +788,8 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             const int dlead = (int)((reinterpret_cast<uintptr_t>(static_cast<raw*>(a.dlogits) + t * a.ldd) & 15) / sizeof(raw));
             return ((s.id0 + dlead) % E) == 0;
         };
-        auto back = [&](int64_t i, const Slice& slice) {
-            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+        auto back = [&](int i, int st, const Slice& slice) {
+            const int slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             wait_ready(i);
             if (a.dlogits != nullptr) {
@@ -876,13 +883,15 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             if (lane == 0) arrive_local(&c.done[st]);
         };
         Slice before = {0.0f, false};
-        for (int64_t i = 0; i < n_rows; ++i) {
-            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+        int st_before = 0;
+        StageRing ring;
+        for (int i = 0; i < n_rows; ++i, ring.next(n_stages)) {
+            const int st = ring.st, slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
             uint4* const buf = stages + (size_t)st * a.seg;
             const int share = (s.cnt + PW - 1) / PW, lo = min(s.cnt, warp * share), hi = min(s.cnt, lo + share);
-            if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
+            if (!mbar_wait(&c.full[st], ring.parity, spins())) late = true;
             if (!mbar_wait(&c.listed[slot], (uint32_t)((i / kRing) & 1), spins())) late = true;
             float m = -INFINITY;
 #pragma unroll 4
@@ -914,10 +923,11 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             if (lane < CL)
                 store_async(mapa(part + slot * CL * PW + rank * PW + warp, lane), mapa(&c.parts[slot], lane), sum,
                             (unsigned long long)__float_as_uint(m));
-            if (i > 0) back(i - 1, before);
+            if (i > 0) back(i - 1, st_before, before);
             before = now;
+            st_before = st;
         }
-        if (n_rows > 0) back(n_rows - 1, before);
+        if (n_rows > 0) back(n_rows - 1, st_before, before);
     }
     if (late && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
     __syncwarp();
@@ -935,18 +945,19 @@ constexpr int64_t kPipeMinBytes = 16 << 20;
 template <int DT, int KP>
 int launch_distill(DistillArgs& a, cudaStream_t stream) {
     const int esize = DT == PODS_DTYPE_F32 ? 4 : 2;
-    if (a.K <= kPipeK && a.T * a.V * esize >= kPipeMinBytes) {
-        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size
+    if (a.K <= kPipeK && a.T * a.V * esize >= kPipeMinBytes && a.T <= 0x7fffffff) {
+        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size; the
+        // longest rows make do with two stages
         static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
-        for (int size : kSizes) {
-            a.seg = segment_vectors(a.V, esize, size);
-            const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)kStages * a.seg * 16;
-            if (smem <= kHalfSmBytes) {
+        for (a.n_stages = kMaxStages; a.n_stages >= 2; --a.n_stages)
+            for (int size : kSizes) {
+                a.seg = segment_vectors(a.V, esize, size);
+                const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)a.n_stages * a.seg * 16;
+                if (smem > kHalfSmBytes) continue;
                 distill_prep_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, stream>>>(a);
                 PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
                 return launch_row_clusters<pods_distill_pipe_kernel<DT>>(a, a.T, size, kPipeThreads, smem, stream);
             }
-        }
     }
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;

@@ -34,7 +34,7 @@ using namespace pods_row;
 
 namespace {
 
-constexpr int W = 16;                         // warps of a CTA
+constexpr int W = 8;                          // warps of a CTA
 constexpr int kThreads = W * 32;
 constexpr float kGreedyBelow = 0x1p-20f;      // temperatures below this are the arg-max
 constexpr int kSampleList = 1024;             // entries that the sampler's first CTA orders
@@ -62,7 +62,7 @@ __device__ __forceinline__ double draw_margin(double u, double Z, double deep) {
 struct SampleArgs {
     const void* logits;
     int64_t ldl, T;
-    int V, seg;
+    int V, seg, n_stages;
     const float* u;
     const float *temperature_row, *top_p_row, *min_p_row;
     const int32_t* top_k_row;
@@ -725,8 +725,9 @@ struct Finder {
     }
 
     // Shrinks (thr, cut) to the smallest prefix of the kept ids whose sum of e reaches top_p of theirs, where the border is
-    // found in one bracket of the mass histogram; S: their sum, to a few parts in 1e6.  false: the bracket does not fit the list.
-    __device__ bool nucleus_threshold(float top_p, double S, const PartRef& top, double tau_inv, float* thr, int* cut) {
+    // found in one bracket of the mass histogram; S: their sum, by fast exponentials or (exact_S) in fp64.  false: the bracket does not fit the lists.
+    // lane_above: see bracket_sum; negative where there is none.
+    __device__ bool nucleus_threshold(float top_p, double S, bool exact_S, const PartRef& top, double tau_inv, float* thr, int* cut, double* lane_above) {
         // logits below this have less than 1 - top_p of the mass together, so the border lies above
         const double deep = log(fmax((1.0 - (double)top_p) * S, 1e-30) / (double)w.a.V) - 1e-3;
         const float low = fmaxf(*thr, __double2float_rd((double)top.m + deep / tau_inv));
@@ -762,11 +763,15 @@ struct Finder {
         constexpr int PB = kBins / kThreads;
         uint32_t n[PB] = {};
         for (int q = 0; q < w.CL; ++q) {
-            const uint2 h = *reinterpret_cast<const uint2*>(w.cl.map_shared_rank(hist() + w.tid * PB, q));
-            n[0] += h.x;
-            n[1] += h.y;
+            const uint32_t* const peer = w.cl.map_shared_rank(hist() + w.tid * PB, q);
+#pragma unroll
+            for (int k = 0; k < PB; k += 2) {
+                const uint2 h = *reinterpret_cast<const uint2*>(peer + k);
+                n[k] += h.x;
+                n[k + 1] += h.y;
+            }
         }
-        static_assert(PB == 2, "one 8-byte read a thread and peer");
+        static_assert(PB % 2 == 0, "8 bytes a read");
         double run[PB], sum = 0.0;
 #pragma unroll
         for (int k = 0; k < PB; ++k) {
@@ -784,51 +789,87 @@ struct Finder {
         }
         const int b1 = block_reduce<W>(below, ctrl().ipart, Plus()), b2 = block_reduce<W>(first, ctrl().ipart, Min());
 
-        // fp64 sums above the bracket and of all kept ids; the bracket's ids listed
+        // the sums above the bracket, and the bracket's ids listed; fast first, then, where the border is too close to call, in fp64
+        *lane_above = 0.0;
+        int answer = bracket<false>(top_p, S, exact_S, low, scale, b1, b2, top, tau_inv, thr, cut, lane_above);
+        if (answer == 2) {
+            *lane_above = -1.0;
+            answer = bracket<true>(top_p, S, exact_S, low, scale, b1, b2, top, tau_inv, thr, cut, lane_above);
+        }
+        return answer == 1;
+    }
+
+    // One sweep for nucleus_threshold.  1: (thr, cut) is the border; 2: too close to call; 0: the bracket misses it or does not
+    // fit the lists.  The fast sweep leaves the lane's sum above the bracket (relative to top) in lane_above.
+    template <bool PREC>
+    __device__ __forceinline__ int bracket(float top_p, double S, bool exact_S, float low, float scale, int b1, int b2, const PartRef& top, double tau_inv,
+                                           float* thr, int* cut, double* lane_above) {
+        __syncthreads();
         if (w.tid == 0) ctrl().n_list = 0;
         __syncthreads();
         double above = 0.0, total = 0.0;
 #pragma unroll 1
         for (int j = w.v0; j < w.v1; ++j) {
             const uint4 q = row_buf()[j];
-            if (El::vec_max(q) < *thr) continue;
+            if (El::vec_max(q) < (PREC ? *thr : low)) continue;
             float x[E];
             El::unpack(q, x);
+            bool inside[E], high[E], in[E], any = false;
 #pragma unroll
-            for (int h = 0; h < E; h += 4) {
-                double d[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) d[i] = ((double)x[h + i] - (double)top.m) * tau_inv;
-                exp64x4(d);
-                double high[4];
-                bool inside[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int id = w.id_of(j, h + i);
-                    const bool in = w.kept(x[h + i], id, *thr, *cut), far = x[h + i] < low;
-                    float pos;
-                    const int b = far ? kBins : bin_of(x[h + i], &pos);
-                    d[i] = in ? d[i] : 0.0;
-                    high[i] = b < b1 ? d[i] : 0.0;
-                    inside[i] = in && b >= b1 && b <= b2 && w.is_id(id);
-                }
-                if (inside[0] | inside[1] | inside[2] | inside[3])
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (inside[i]) list_add(x[h + i], w.id_of(j, h + i));
-                total += (d[0] + d[1]) + (d[2] + d[3]);
-                above += (high[0] + high[1]) + (high[2] + high[3]);
+            for (int e = 0; e < E; ++e) {
+                const int id = w.id_of(j, e), b = min(kBins - 1, (int)((top.m - fmaxf(x[e], low)) * scale));
+                in[e] = w.kept(x[e], id, *thr, *cut);
+                const bool near = in[e] && x[e] >= low;
+                high[e] = near && b < b1;
+                inside[e] = near && b >= b1 && b <= b2 && w.is_id(id);
+                any |= inside[e];
             }
+            if (PREC) {
+#pragma unroll
+                for (int h = 0; h < E; h += 4) {
+                    double d[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[i] = ((double)x[h + i] - (double)top.m) * tau_inv;
+                    exp64x4(d);
+                    double a[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        a[i] = high[h + i] ? d[i] : 0.0;
+                        d[i] = in[h + i] ? d[i] : 0.0;
+                    }
+                    total += (d[0] + d[1]) + (d[2] + d[3]);
+                    above += (a[0] + a[1]) + (a[2] + a[3]);
+                }
+            } else {
+                float p[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[e] = x[e];
+                if (top.far) top.template exps<true>(p);
+                else top.template exps<false>(p);
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[e] = high[e] ? p[e] : 0.0f;
+                above += (double)vec_add(p);
+            }
+            if (any)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (inside[e]) list_add(x[e], w.id_of(j, e));
         }
+        if (!PREC) *lane_above = above;
+        // relative to e^zmax
+        const double unit = PREC || top.far ? 1.0 : exp2((double)top.R - (double)top.m * (double)top.c);
         Xch mine = {};
-        mine.a = block_reduce<W>(above, ctrl().dpart, Plus());
-        mine.b = block_reduce<W>(total, ctrl().dpart, Plus());
+        mine.a = block_reduce<W>(above, ctrl().dpart, Plus()) * unit;
+        if (PREC) mine.b = block_reduce<W>(total, ctrl().dpart, Plus());
         int len;
         const Xch* x = share_list<false>(mine, &len);  // past its barrier the histogram is read: its room is the list's again
         double A = 0.0, Z = 0.0;
         for (int q = 0; q < w.CL; ++q) { A += x[q].a; Z += x[q].b; }
+        if (!PREC) Z = S;
+        const double goal = (double)top_p * Z;
+        const double deep = deep_error(w.a.V, Z, top.c, tau_inv, top.far);
+        const double margin = PREC ? 0.0 : exact_S ? (deep + kFlat) * goal + 1e-12 * Z : draw_margin((double)top_p, Z, deep);
         Xch out = {};
-        out.n = 0;
         const bool fits = len > 0 && len <= kSampleList;
         if (fits) order_lists();
         if (w.rank == 0 && fits) {
@@ -840,32 +881,49 @@ struct Finder {
             }
             double sum_all;
             double at = A + block_scan(own, ctrl().dpart, &sum_all) - own;
-            int pick = kNoCut;
+            int pick = kNoCut, unsure = w.tid == 0 && b1 > 0 && fabs(A - goal) <= margin;
             for (int k = 0; k < per; ++k) {
                 const int i = w.tid * per + k;
                 if (i < len) {
                     at += exp64(((double)unorder32((uint32_t)(list()[i] >> 32)) - (double)top.m) * tau_inv);
-                    if (at >= (double)top_p * Z && pick == kNoCut) pick = i;
+                    if (at >= goal && pick == kNoCut) pick = i;
+                    if (fabs(at - goal) <= margin) unsure = 1;
                 }
             }
             pick = block_reduce<W>(pick, ctrl().ipart, Min());
-            if (pick < len && (A < (double)top_p * Z || b1 == 0)) {
+            unsure = block_reduce<W>(unsure, ctrl().ipart, Plus());
+            if (!PREC && unsure) {
+                out.n = 2;
+            } else if (pick < len && (A < goal || b1 == 0)) {
                 out.n = 1;
                 out.m = unorder32((uint32_t)(list()[pick] >> 32));
                 out.i = (int)~(uint32_t)list()[pick];
             }
         }
         x = exchange(out);
-        if (x[0].n == 0) return false;
-        *thr = x[0].m;
-        *cut = x[0].i;
-        return true;
+        if (x[0].n == 1) {
+            *thr = x[0].m;
+            *cut = x[0].i;
+        }
+        return x[0].n;
+    }
+    // The lane's fast sum over the kept ids, from its sum above the bracket and the bracket's entries.
+    __device__ __forceinline__ double bracket_sum(double lane_above, float thr, int cut, const PartRef& top) {
+        const int n = min(ctrl().n_list, w.a.own_cap);
+        for (int k = 0; k < n; ++k) {
+            const unsigned long long key = own()[k];
+            const float x = unorder32((uint32_t)(key >> 32));
+            const int id = (int)~(uint32_t)key, j = (id - w.s.id0) / E;
+            if (j >= w.v0 && j < w.v1 && w.kept(x, id, thr, cut)) lane_above += top.exp1(x);
+        }
+        return lane_above;
     }
 
     // Draws over the kept ids; the whole cluster gets the token, its logit and the kept sum relative to top's maximum.
     template <bool PREC>
-    __device__ bool draw(double u, float thr, int cut, const PartRef& top, double tau_inv, int* token, float* logit, double* total) {
-        const double sum = w.template lane_sum<PREC, true>(top, tau_inv, thr, cut);
+    __device__ bool draw(double u, float thr, int cut, const PartRef& top, double tau_inv, double lane_above, int* token, float* logit, double* total) {
+        const double sum = !PREC && lane_above >= 0.0 ? bracket_sum(lane_above, thr, cut, top)
+                                                      : w.template lane_sum<PREC, true>(top, tau_inv, thr, cut);
         const double incl = warp_scan(sum, w.lane);
         Part p;
         p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
@@ -1127,17 +1185,19 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
         if (!settled) {
             float thr = -INFINITY;
             int cut = kNoCut;
+            double lane_above = -1.0;
             if (g.top_k > 0) f->count_threshold(g.top_k, zmax, &thr, &cut);
             if (g.nucleus) {
                 const double S = g.top_k > 0 ? f->kept_sum(thr, cut, top, tau_inv) : Zm;
-                if (!f->nucleus_threshold(g.top_p, S, top, tau_inv, &thr, &cut)) {
+                if (!f->nucleus_threshold(g.top_p, S, g.top_k > 0, top, tau_inv, &thr, &cut, &lane_above)) {
+                    lane_above = -1.0;
                     const double total = f->kept_sum(thr, cut, top, tau_inv);
                     f->mass_threshold((double)g.top_p * total, top, tau_inv, &thr, &cut);
                 }
             }
-            if (zfloor > thr) { thr = zfloor; cut = kNoCut; }
-            if (!f->template draw<false>((double)g.u, thr, cut, top, tau_inv, &token, &logit, &kept_total))
-                f->template draw<true>((double)g.u, thr, cut, top, tau_inv, &token, &logit, &kept_total);
+            if (zfloor > thr) { thr = zfloor; cut = kNoCut; lane_above = -1.0; }
+            if (!f->template draw<false>((double)g.u, thr, cut, top, tau_inv, lane_above, &token, &logit, &kept_total))
+                f->template draw<true>((double)g.u, thr, cut, top, tau_inv, -1.0, &token, &logit, &kept_total);
         }
         if (w.rank == 0 && tid == 0) {
             const double d = ((double)logit - (double)zmax) * tau_inv;
@@ -1197,10 +1257,10 @@ pods_sample_kernel(const SampleArgs a) {
 // Close draws are marked by a token of kMarked; pods_sample_marked_kernel takes them in fp64.
 constexpr int PW = 8;                         // consumer warps
 constexpr int kPolicyThreads = (PW + 2) * 32;
-constexpr int kStages = 3, kRing = 4;
+constexpr int kMaxStages = 3, kRing = 4;
 
 struct PolicyCtrl {
-    unsigned long long full[kStages], empty[kStages];
+    unsigned long long full[kMaxStages], empty[kMaxStages];
     unsigned long long parts[kRing];          // a row's parts have arrived
     unsigned long long ready[kRing];          // this CTA's lane sums are there
     unsigned long long done[kRing];           // every exchange warp is done with the slots
@@ -1215,6 +1275,7 @@ __host__ __device__ constexpr int policy_ctrl_bytes(int cl) {
 template <int DT>
 __global__ void __launch_bounds__(kPolicyThreads, 2)
 pods_sample_policy_kernel(const SampleArgs a) {
+    const int n_stages = a.n_stages;
     using El = Elem<DT>;
     constexpr int E = El::E;
     PolicyCtrl& c = *reinterpret_cast<PolicyCtrl*>(smem_);
@@ -1224,9 +1285,9 @@ pods_sample_policy_kernel(const SampleArgs a) {
     const int rank = (int)cl.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
-    const int64_t n_rows = first < a.T ? (a.T - first + n_clusters - 1) / n_clusters : 0;
+    const int n_rows = first < a.T ? (int)((a.T - first + n_clusters - 1) / n_clusters) : 0;
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < kMaxStages; ++i) {
             mbar_init(&c.full[i], 1);
             mbar_init(&c.empty[i], PW);
         }
@@ -1249,28 +1310,34 @@ pods_sample_policy_kernel(const SampleArgs a) {
     if (warp == PW) {
         // ---- producer ----
         if (lane == 0) {
-            for (int64_t i = 0; i < n_rows; ++i) {
-                const int st = (int)(i % kStages);
-                if (i >= kStages && !mbar_wait(&c.empty[st], (uint32_t)((i / kStages - 1) & 1), spins())) late = true;
+            StageRing ring;
+            for (int i = 0; i < n_rows; ++i) {
+                const int st = ring.st;
+                if (i >= n_stages && !mbar_wait(&c.empty[st], ring.parity ^ 1u, spins())) late = true;
                 const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
                 uint4* const buf = stages + (size_t)st * a.seg;
                 fill_edges<DT>(s, a.V, buf);
                 fence_async_proxy();                   // edges of an earlier row may lie where this row's copy goes
                 start_copy(s, buf, &c.full[st]);
+                ring.next(n_stages);
             }
             // every copy has landed before the CTA ends, also one that a consumer gave up on
-            for (int64_t i = n_rows > kStages ? n_rows - kStages : 0; i < n_rows; ++i)
-                if (!mbar_wait(&c.full[i % kStages], (uint32_t)((i / kStages) & 1), kSpinLimit)) late = true;
+            for (int k = 0; k < n_stages && k < n_rows; ++k) {
+                ring.st = ring.st == 0 ? n_stages - 1 : ring.st - 1;           // from the last row back
+                if (ring.st == n_stages - 1) ring.parity ^= 1u;
+                if (!mbar_wait(&c.full[ring.st], ring.parity, kSpinLimit)) late = true;
+            }
         }
     } else if (warp < PW) {
         // ---- consumers ----
-        for (int64_t i = 0; i < n_rows; ++i) {
-            const int st = (int)(i % kStages), slot = (int)(i % kRing);
+        StageRing ring;
+        for (int i = 0; i < n_rows; ++i, ring.next(n_stages)) {
+            const int st = ring.st, slot = i % kRing;
             const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
             int v0, v1;
             lane_vectors<PW>(s.cnt, warp, lane, &v0, &v1);
             const uint4* const buf = stages + (size_t)st * a.seg;
-            if (!mbar_wait(&c.full[st], (uint32_t)((i / kStages) & 1), spins())) late = true;
+            if (!mbar_wait(&c.full[st], ring.parity, spins())) late = true;
             float m = -INFINITY;
 #pragma unroll 4
             for (int j = v0; j < v1; ++j) m = max_nan(m, El::vec_max(buf[j]));
@@ -1293,8 +1360,8 @@ pods_sample_policy_kernel(const SampleArgs a) {
     } else {
         // ---- exchange ----
         float u_next = n_rows > 0 ? a.u[first] : 0.0f;
-        for (int64_t i = 0; i < n_rows; ++i) {
-            const int slot = (int)(i % kRing);
+        for (int i = 0; i < n_rows; ++i) {
+            const int slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             float u = u_next;
             if (i + 1 < n_rows) u_next = a.u[t + n_clusters];
@@ -1548,7 +1615,7 @@ constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold fo
 // CTAs a row: segments of at most kSegmentBytes, and enough lanes for a list of K, whose bound comes from their maxima.
 int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
     int cl = 1;
-    while (cl < kMaxCluster && ((size_t)segment_vectors(V, esize, cl) * 16 > kSegmentBytes || cl * kThreads < 2 * K)) cl *= 2;
+    while (cl < kMaxCluster && ((size_t)segment_vectors(V, esize, cl) * 16 > kSegmentBytes || cl * kThreads < 4 * K)) cl *= 2;
     // few rows: spread over idle SMs down to two vectors a lane
     while (cl < kMaxCluster && 2 * cl * T <= 128 && segment_vectors(V, esize, 2 * cl) >= kThreads) cl *= 2;
     return cl;
@@ -1567,16 +1634,18 @@ int launch_rows(SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stre
 constexpr int64_t kPipelineMinBytes = 16 << 20;
 template <int DT>
 int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
-    if (a.T * a.V * esize < kPipelineMinBytes) return PODS_OK;
+    if (a.T * a.V * esize < kPipelineMinBytes || a.T > 0x7fffffff) return PODS_OK;
     // the smallest cluster whose stages fit twice on an SM: few partners, and few places of the GPU left empty by its size
     static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
     int cl = 0;
     size_t smem = 0;
-    for (int size : kSizes) {
-        a.seg = segment_vectors(a.V, esize, size);
-        smem = policy_ctrl_bytes(size) + (size_t)kStages * a.seg * 16;
-        if (smem <= kHalfSmBytes) { cl = size; break; }
-    }
+    for (a.n_stages = kMaxStages; a.n_stages >= 2 && cl == 0; --a.n_stages)    // the longest rows make do with two stages
+        for (int size : kSizes) {
+            a.seg = segment_vectors(a.V, esize, size);
+            smem = policy_ctrl_bytes(size) + (size_t)a.n_stages * a.seg * 16;
+            if (smem <= kHalfSmBytes) { cl = size; break; }
+        }
+    ++a.n_stages;
     if (cl == 0) return PODS_OK;
     const int rc = launch_row_clusters<pods_sample_policy_kernel<DT>>(a, a.T, cl, kPolicyThreads, smem, stream);
     if (rc == PODS_OK) a.marked = 1;

@@ -353,6 +353,18 @@ __device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t pari
     }
     return false;
 }
+// A pipeline's place in its ring of stages: the stage, and the parity of its barriers' current use.
+struct StageRing {
+    int st = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next(int n) {
+        if (++st == n) {
+            st = 0;
+            parity ^= 1u;
+        }
+    }
+};
+
 // ---- barriers and stores across the cluster -----------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t mapa(const void* p, int rank) {
     uint32_t r;
