@@ -37,7 +37,7 @@ struct DistillArgs {
     int64_t M, row0;
     const uint8_t* mask;
     int64_t T;
-    int V, seg, n_stages;
+    int V, seg;
     float temperature;
     int rest;
     float grad_scale;
@@ -475,7 +475,7 @@ distill_prep_kernel(const DistillArgs a) {
 // took every CTA's parts of row i - 2, which were sent after the factors of row i - 4 were made: the slot of row i - 4 is free.
 constexpr int PW = 8;
 constexpr int kPipeThreads = (PW + 3) * 32;
-constexpr int kMaxStages = 3, kRing = 4;
+constexpr int kStages = 3, kRing = 4;
 constexpr int kPipeK = 128;                   // entries of a list: four a lane
 
 struct PipePart {                             // of one consumer warp
@@ -500,7 +500,7 @@ struct Factors {
     int mode;                                 // 0: a row of zeros
 };
 struct PipeCtrl {
-    unsigned long long full[kMaxStages], done[kMaxStages];   // the stage is loaded; its consumers have left it
+    unsigned long long full[kStages], done[kStages];   // the stage is loaded; its consumers have left it
     unsigned long long listed[kRing];         // the listed logits are out of the stage
     unsigned long long parts[kRing];          // all parts of the cluster have arrived
     unsigned long long ready[kRing];          // the factors are there
@@ -519,7 +519,6 @@ extern __shared__ __align__(128) unsigned char smem_[];
 template <int DT>
 __global__ void __launch_bounds__(kPipeThreads, 2)
 pods_distill_pipe_kernel(const DistillArgs a) {
-    const int n_stages = a.n_stages;
     using El = Elem<DT>;
     using raw = typename El::raw;
     constexpr int E = El::E;
@@ -532,7 +531,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
     const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
     const int n_rows = first < a.T ? (int)((a.T - first + n_clusters - 1) / n_clusters) : 0;
     if (tid == 0) {
-        for (int i = 0; i < kMaxStages; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(&c.full[i], 1);
             mbar_init(&c.done[i], PW);
         }
@@ -560,18 +559,18 @@ pods_distill_pipe_kernel(const DistillArgs a) {
             StageRing ring;
             for (int i = 0; i < n_rows; ++i) {
                 const int st = ring.st;
-                if (i >= n_stages && !mbar_wait(&c.done[st], ring.parity ^ 1u, spins())) late = true;
+                if (i >= kStages && !mbar_wait(&c.done[st], ring.parity ^ 1u, spins())) late = true;
                 const Segment s = make_segment<DT>(a.logits, a.ldl, first + i * n_clusters, a.V, rank, a.seg);
                 uint4* const buf = stages + (size_t)st * a.seg;
                 fill_edges<DT>(s, a.V, buf);
                 fence_async_proxy();                   // edges of an earlier row may lie where this row's copy goes
                 start_copy(s, buf, &c.full[st]);
-                ring.next(n_stages);
+                ring.next(kStages);
             }
             // every copy has landed before the CTA ends, also one that a consumer gave up on
-            for (int k = 0; k < n_stages && k < n_rows; ++k) {
-                ring.st = ring.st == 0 ? n_stages - 1 : ring.st - 1;           // from the last row back
-                if (ring.st == n_stages - 1) ring.parity ^= 1u;
+            for (int k = 0; k < kStages && k < n_rows; ++k) {
+                ring.st = ring.st == 0 ? kStages - 1 : ring.st - 1;           // from the last row back
+                if (ring.st == kStages - 1) ring.parity ^= 1u;
                 if (!mbar_wait(&c.full[ring.st], ring.parity, kSpinLimit)) late = true;
             }
         }
@@ -592,7 +591,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
         };
         if (n_rows > 0) fetch(first);
         StageRing ring;
-        for (int i = 0; i < n_rows; ++i, ring.next(n_stages)) {
+        for (int i = 0; i < n_rows; ++i, ring.next(kStages)) {
             const int st = ring.st, slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
@@ -885,7 +884,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
         Slice before = {0.0f, false};
         int st_before = 0;
         StageRing ring;
-        for (int i = 0; i < n_rows; ++i, ring.next(n_stages)) {
+        for (int i = 0; i < n_rows; ++i, ring.next(kStages)) {
             const int st = ring.st, slot = i % kRing;
             const int64_t t = first + i * n_clusters;
             const Segment s = make_segment<DT>(a.logits, a.ldl, t, a.V, rank, a.seg);
@@ -946,18 +945,17 @@ template <int DT, int KP>
 int launch_distill(DistillArgs& a, cudaStream_t stream) {
     const int esize = DT == PODS_DTYPE_F32 ? 4 : 2;
     if (a.K <= kPipeK && a.T * a.V * esize >= kPipeMinBytes && a.T <= 0x7fffffff) {
-        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size; the
-        // longest rows make do with two stages
+        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size.
+        // (Rows too long for three stages stay with the kernel above: 203 us for 512 fp32 rows of 151936, 218 us with two stages.)
         static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
-        for (a.n_stages = kMaxStages; a.n_stages >= 2; --a.n_stages)
-            for (int size : kSizes) {
-                a.seg = segment_vectors(a.V, esize, size);
-                const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)a.n_stages * a.seg * 16;
-                if (smem > kHalfSmBytes) continue;
-                distill_prep_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, stream>>>(a);
-                PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
-                return launch_row_clusters<pods_distill_pipe_kernel<DT>>(a, a.T, size, kPipeThreads, smem, stream);
-            }
+        for (int size : kSizes) {
+            a.seg = segment_vectors(a.V, esize, size);
+            const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)kStages * a.seg * 16;
+            if (smem > kHalfSmBytes) continue;
+            distill_prep_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, stream>>>(a);
+            PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
+            return launch_row_clusters<pods_distill_pipe_kernel<DT>>(a, a.T, size, kPipeThreads, smem, stream);
+        }
     }
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;

@@ -84,6 +84,8 @@ struct Part {                                 // of one warp
     double s;             // sum relative to the part's reference (to its maximum in fp64 rows)
     float m;              // its maximum
     float lim;            // a value that enough of its logits reach
+    float near;           // mass of the lanes' maxima alone, relative to the part's reference
+    int pad;
 };
 
 struct Xch {                                  // one CTA's word in an exchange
@@ -430,14 +432,21 @@ struct Rows {
         uint32_t key[M];
 #pragma unroll
         for (int k = 0; k < M; ++k) key[k] = row_ctrl().top[lane + 32 * k];
-        uint32_t lo = 0;                               // reached by r lanes (0: by all)
+        uint32_t lo = key[0], hi = key[0];
+#pragma unroll
+        for (int k = 1; k < M; ++k) {
+            lo = min(lo, key[k]);
+            hi = max(hi, key[k]);
+        }
+        lo = __reduce_min_sync(PODS_FULL_MASK, lo);    // reached by all lanes, so by r
+        hi = __reduce_max_sync(PODS_FULL_MASK, hi) + 1;
 #pragma unroll 1
-        for (int bit = 15; bit >= 0; --bit) {
-            const uint32_t mid = lo | (1u << bit);
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
             int n = 0;
 #pragma unroll
             for (int k = 0; k < M; ++k) n += (int)(key[k] >= mid);
-            if ((int)__reduce_add_sync(PODS_FULL_MASK, (unsigned)n) >= r) lo = mid;
+            if ((int)__reduce_add_sync(PODS_FULL_MASK, (unsigned)n) >= r) lo = mid; else hi = mid;
         }
         const float v = unorder32(lo << 16);
         return v >= -3.4028235e38f ? v : -INFINITY;    // below the finite numbers: every id
@@ -735,10 +744,7 @@ struct Finder {
         const float scale = (float)kBins / range;      // stretches a unit of logit
         if (!(range > 0.0f) || !(scale < INFINITY)) return false;
         const float h2 = (float)(1.4426950408889634 * tau_inv * (double)range / kBins);     // exponent of two a stretch, < 0.05
-        const auto bin_of = [&](float x, float* pos) {
-            *pos = (top.m - x) * scale;
-            return min(kBins - 1, (int)*pos);
-        };
+        const bool all_ids = *thr == -INFINITY;        // no top_k in force
         for (int i = w.tid; i < kBins; i += kThreads) hist()[i] = 0;
         __syncthreads();
         // mass in units of 2^-12 of the weight at the stretch's upper end: at most 2^19 ids make 2^31; each is off by 1.3e-4
@@ -746,18 +752,20 @@ struct Finder {
             const uint4 q = row_buf()[j];
             if (El::vec_max(q) < low) continue;
             float x[E];
-            int b[E];
-            uint32_t mass[E];
+            uint32_t b[E], mass[E];
             El::unpack(q, x);
+            // the eight chains overlap, and rounding by a large addend keeps them off the pipe that converts and exponentiates:
+            // 2^-y for y <= 0.05 by its quadratic (the next term is 7e-6)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {              // no branch before the atomics: the eight chains overlap
-                float pos;
-                b[e] = bin_of(fmaxf(x[e], low), &pos);
-                mass[e] = __float2uint_rn(4096.0f * ex2_approx(((float)b[e] - pos) * h2));
+            for (int e = 0; e < E; ++e) {
+                const float pos = (top.m - fmaxf(x[e], low)) * scale;
+                const float t = (pos - 0.5f) + 12582912.0f, y = (pos - (t - 12582912.0f)) * (h2 * 0.6931472f);     // 1.5 * 2^23
+                b[e] = min((uint32_t)kBins - 1u, __float_as_uint(t) & 0x3fffffu);
+                mass[e] = __float_as_uint(fmaf(fmaf(y, 2048.0f, -4096.0f), y, 4096.0f + 8388608.0f)) & 0x7fffffu;
             }
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (x[e] >= low && w.kept(x[e], w.id_of(j, e), *thr, *cut)) atomicAdd(&hist()[b[e]], mass[e]);
+                if (x[e] >= low && (all_ids || w.kept(x[e], w.id_of(j, e), *thr, *cut))) atomicAdd(&hist()[b[e]], mass[e]);
         }
         w.cl.sync();
         constexpr int PB = kBins / kThreads;
@@ -780,7 +788,7 @@ struct Finder {
         }
         double all;
         const double base = block_scan(sum, ctrl().dpart, &all) - sum;
-        const double goal = (double)top_p * S, tol = 2e-4 * S;     // 1.3e-4 of rounding, the fast sum S, the exponentials here
+        const double goal = (double)top_p * S, tol = 2e-4 * S;     // 1.3e-4 of rounding, the quadratic, the fast sum S
         int below = 0, first = kBins - 1;
 #pragma unroll
         for (int k = 0; k < PB; ++k) {
@@ -791,10 +799,12 @@ struct Finder {
 
         // the sums above the bracket, and the bracket's ids listed; fast first, then, where the border is too close to call, in fp64
         *lane_above = 0.0;
-        int answer = bracket<false>(top_p, S, exact_S, low, scale, b1, b2, top, tau_inv, thr, cut, lane_above);
+        // its ends in logits, a hundredth of a stretch further out than the stretches, whose own ends are rounded
+        const float x_hi = top.m - ((float)b1 - 0.01f) / scale, x_lo = fmaxf(low, top.m - ((float)b2 + 1.01f) / scale);
+        int answer = bracket<false>(top_p, S, exact_S, x_hi, x_lo, b1 == 0, top, tau_inv, thr, cut, lane_above);
         if (answer == 2) {
             *lane_above = -1.0;
-            answer = bracket<true>(top_p, S, exact_S, low, scale, b1, b2, top, tau_inv, thr, cut, lane_above);
+            answer = bracket<true>(top_p, S, exact_S, x_hi, x_lo, b1 == 0, top, tau_inv, thr, cut, lane_above);
         }
         return answer == 1;
     }
@@ -802,28 +812,27 @@ struct Finder {
     // One sweep for nucleus_threshold.  1: (thr, cut) is the border; 2: too close to call; 0: the bracket misses it or does not
     // fit the lists.  The fast sweep leaves the lane's sum above the bracket (relative to top) in lane_above.
     template <bool PREC>
-    __device__ __forceinline__ int bracket(float top_p, double S, bool exact_S, float low, float scale, int b1, int b2, const PartRef& top, double tau_inv,
-                                           float* thr, int* cut, double* lane_above) {
+    __device__ __forceinline__ int bracket(float top_p, double S, bool exact_S, float x_hi, float x_lo, bool from_top, const PartRef& top,
+                                           double tau_inv, float* thr, int* cut, double* lane_above) {
         __syncthreads();
         if (w.tid == 0) ctrl().n_list = 0;
         __syncthreads();
         double above = 0.0, total = 0.0;
+        const bool all_ids = *thr == -INFINITY;
+        if (from_top) x_hi = INFINITY;                 // the bracket begins with the largest logit
 #pragma unroll 1
         for (int j = w.v0; j < w.v1; ++j) {
             const uint4 q = row_buf()[j];
-            if (El::vec_max(q) < (PREC ? *thr : low)) continue;
+            const float vmax = El::vec_max(q);
+            if (vmax < (PREC ? *thr : x_lo)) continue;
             float x[E];
             El::unpack(q, x);
-            bool inside[E], high[E], in[E], any = false;
+            if (!all_ids)                              // ids that top_k left out weigh nothing
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int id = w.id_of(j, e), b = min(kBins - 1, (int)((top.m - fmaxf(x[e], low)) * scale));
-                in[e] = w.kept(x[e], id, *thr, *cut);
-                const bool near = in[e] && x[e] >= low;
-                high[e] = near && b < b1;
-                inside[e] = near && b >= b1 && b <= b2 && w.is_id(id);
-                any |= inside[e];
-            }
+                for (int e = 0; e < E; ++e) x[e] = w.kept(x[e], w.id_of(j, e), *thr, *cut) ? x[e] : -INFINITY;
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < E; ++e) any |= x[e] >= x_lo && x[e] <= x_hi;
             if (PREC) {
 #pragma unroll
                 for (int h = 0; h < E; h += 4) {
@@ -834,8 +843,7 @@ struct Finder {
                     double a[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        a[i] = high[h + i] ? d[i] : 0.0;
-                        d[i] = in[h + i] ? d[i] : 0.0;
+                        a[i] = x[h + i] > x_hi ? d[i] : 0.0;
                     }
                     total += (d[0] + d[1]) + (d[2] + d[3]);
                     above += (a[0] + a[1]) + (a[2] + a[3]);
@@ -847,13 +855,13 @@ struct Finder {
                 if (top.far) top.template exps<true>(p);
                 else top.template exps<false>(p);
 #pragma unroll
-                for (int e = 0; e < E; ++e) p[e] = high[e] ? p[e] : 0.0f;
+                for (int e = 0; e < E; ++e) p[e] = x[e] > x_hi ? p[e] : 0.0f;
                 above += (double)vec_add(p);
             }
             if (any)
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (inside[e]) list_add(x[e], w.id_of(j, e));
+                    if (x[e] >= x_lo && x[e] <= x_hi && w.is_id(w.id_of(j, e))) list_add(x[e], w.id_of(j, e));
         }
         if (!PREC) *lane_above = above;
         // relative to e^zmax
@@ -881,7 +889,7 @@ struct Finder {
             }
             double sum_all;
             double at = A + block_scan(own, ctrl().dpart, &sum_all) - own;
-            int pick = kNoCut, unsure = w.tid == 0 && b1 > 0 && fabs(A - goal) <= margin;
+            int pick = kNoCut, unsure = w.tid == 0 && !from_top && fabs(A - goal) <= margin;
             for (int k = 0; k < per; ++k) {
                 const int i = w.tid * per + k;
                 if (i < len) {
@@ -894,7 +902,7 @@ struct Finder {
             unsure = block_reduce<W>(unsure, ctrl().ipart, Plus());
             if (!PREC && unsure) {
                 out.n = 2;
-            } else if (pick < len && (A < goal || b1 == 0)) {
+            } else if (pick < len && (A < goal || from_top)) {
                 out.n = 1;
                 out.m = unorder32((uint32_t)(list()[pick] >> 32));
                 out.i = (int)~(uint32_t)list()[pick];
@@ -925,10 +933,8 @@ struct Finder {
         const double sum = !PREC && lane_above >= 0.0 ? bracket_sum(lane_above, thr, cut, top)
                                                       : w.template lane_sum<PREC, true>(top, tau_inv, thr, cut);
         const double incl = warp_scan(sum, w.lane);
-        Part p;
+        Part p = {};
         p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
-        p.m = 0.0f;
-        p.lim = 0.0f;
         if (w.tid == 0) ctrl().found = -1;
         const Part* part = w.publish(p);
         const typename Rows<DT>::Sums r = w.template sum_parts<PREC, true>(part, top, tau_inv);
@@ -1012,6 +1018,13 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
     p.s = __shfl_sync(PODS_FULL_MASK, incl, 31);
     const int want = (int)(g.top_k > 0 ? (g.top_k < 512 ? g.top_k : 512) : 256);
     p.lim = FILTERS && g.filtered ? w.reach(lm, want) : 0.0f;
+    p.near = 0.0f;
+    p.pad = 0;
+    if (FILTERS && g.nucleus) {
+        p.near = lm > -INFINITY ? (float)ref.exp1(lm) : 0.0f;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) p.near += __shfl_xor_sync(PODS_FULL_MASK, p.near, d);
+    }
     const Part* const part = w.publish(p);
     const float zmax = w.row_max(part);
     if (!(fabsf(zmax) < INFINITY)) {
@@ -1082,8 +1095,19 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
         float lim = w.limit(part);
         // top_p is a share of the whole top-k sum, so min_p may not shorten the list where both are set
         if (g.floor && !(g.top_k > 0 && g.nucleus)) lim = (g.top_k > 0 || g.nucleus) ? fmaxf(lim, zfloor) : zfloor;
-        double list_mass;
-        const int n = f->list_kept_mass(lim, top, tau_inv, &list_mass);
+        // a nucleus of thousands shows in the maxima of the lanes: where they hold much less than top_p of the row, the list,
+        // which holds hardly more than they do, cannot reach the border
+        bool wide = false;
+        if (g.nucleus && g.top_k == 0) {
+            double near = 0.0;
+            for (int i = lane; i < CL * W; i += 32)
+                if (part[i].s > 0.0) near += (double)part[i].near * PartRef(part[i].m, c).scale_to(top);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) near += __shfl_xor_sync(PODS_FULL_MASK, near, d);
+            wide = near < 0.7 * (double)g.top_p * Z;
+        }
+        double list_mass = 0.0;
+        const int n = wide ? -1 : f->list_kept_mass(lim, top, tau_inv, &list_mass);
         const bool whole = n == a.V;                   // the list is the row
         const bool to_floor = g.floor && lim == zfloor;  // the list holds all that min_p admits
         int token = -1;
@@ -1259,17 +1283,23 @@ constexpr int PW = 8;                         // consumer warps
 constexpr int kPolicyThreads = (PW + 2) * 32;
 constexpr int kMaxStages = 3, kRing = 4;
 
+struct SumPart {                              // 16 bytes, sent as one store
+    double s;
+    float m;
+    int pad;
+};
+
 struct PolicyCtrl {
     unsigned long long full[kMaxStages], empty[kMaxStages];
     unsigned long long parts[kRing];          // a row's parts have arrived
     unsigned long long ready[kRing];          // this CTA's lane sums are there
     unsigned long long done[kRing];           // every exchange warp is done with the slots
     double lanes[kRing][PW][32];              // lane sums, scanned
-    alignas(16) Part part[1];                 // [kRing][CL PW]
+    alignas(16) SumPart part[1];              // [kRing][CL PW]
 };
 // control block of a CTA in a cluster of cl
 __host__ __device__ constexpr int policy_ctrl_bytes(int cl) {
-    return ((int)offsetof(PolicyCtrl, part) + kRing * cl * PW * (int)sizeof(Part) + 127) & ~127;
+    return ((int)offsetof(PolicyCtrl, part) + kRing * cl * PW * (int)sizeof(SumPart) + 127) & ~127;
 }
 
 template <int DT>
@@ -1384,7 +1414,7 @@ pods_sample_policy_kernel(const SampleArgs a) {
                 v[k] = 0.0;
                 pm[k] = -INFINITY;
                 if (k < n && lane * n + k < n_parts) {
-                    const Part p = c.part[slot * n_parts + lane * n + k];
+                    const SumPart p = c.part[slot * n_parts + lane * n + k];
                     v[k] = p.s;
                     pm[k] = p.m;
                 }
@@ -1542,7 +1572,7 @@ pods_sample_marked_kernel(const SampleArgs a) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 3)
 pods_topk_kernel(const SampleArgs a) {
     Rows<DT> w(a);
     Finder<DT> f(w);
@@ -1556,9 +1586,8 @@ pods_topk_kernel(const SampleArgs a) {
         w.start(t);
         w.wait();
         const float lm = w.lane_max();
-        Part p;
+        Part p = {};
         p.m = w.warp_max(lm);
-        p.s = 0.0;
         if (a.lse != nullptr) {
             const PartRef ref(p.m, c);
             p.s = warp_scan(w.template lane_sum<false, false>(ref, tau_inv, 0.0f, 0), w.lane);
@@ -1615,7 +1644,7 @@ constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold fo
 // CTAs a row: segments of at most kSegmentBytes, and enough lanes for a list of K, whose bound comes from their maxima.
 int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
     int cl = 1;
-    while (cl < kMaxCluster && ((size_t)segment_vectors(V, esize, cl) * 16 > kSegmentBytes || cl * kThreads < 4 * K)) cl *= 2;
+    while (cl < kMaxCluster && ((size_t)segment_vectors(V, esize, cl) * 16 > kSegmentBytes || cl * kThreads < 2 * K)) cl *= 2;
     // few rows: spread over idle SMs down to two vectors a lane
     while (cl < kMaxCluster && 2 * cl * T <= 128 && segment_vectors(V, esize, 2 * cl) >= kThreads) cl *= 2;
     return cl;
