@@ -589,19 +589,22 @@ def pods_distill_chunk(logits, ids, values, teacher_lse, seq_weight, cu_seqlens,
     ``logits`` itself.  Missing outputs and the workspace are allocated here."""
     _require(isinstance(logits, torch.Tensor) and logits.dim() == 2, "logits must be [T,V]")
     T, V = logits.shape
-    _require(isinstance(ids, torch.Tensor) and ids.dim() == 2 and ids.shape[0] == T, "ids must be [T,K] with T = %d" % T)
+    if not (isinstance(ids, torch.Tensor) and ids.dim() == 2 and ids.shape[0] == T):
+        raise PodsError("ids must be [T,K] with T = %d" % T)
     K = ids.shape[1]
-    _require(1 <= K <= MAX_TOPK, "need 1 <= K <= %d, got K=%d" % (MAX_TOPK, K))
-    _require(isinstance(values, torch.Tensor) and tuple(values.shape) == (T, K), "values must have the shape [%d, %d]" % (T, K))
+    if not 1 <= K <= MAX_TOPK:
+        raise PodsError("need 1 <= K <= %d, got K=%d" % (MAX_TOPK, K))
+    if not (isinstance(values, torch.Tensor) and values.shape == ids.shape):
+        raise PodsError("values must have the shape [%d, %d]" % (T, K))
     M = cu_seqlens.numel() - 1
     _require(M >= 1, "cu_seqlens must hold M+1 >= 2 entries")
     _require(not rest or teacher_lse is not None, "rest needs teacher_lse")
-    for t, name in ((teacher_lse, "teacher_lse"), (mask, "mask"), (kl, "kl")):
-        _numel(t, T, name)
-    _numel(seq_weight, M, "seq_weight")
-    _numel(loss_acc, 1, "loss_acc")
-    _require(dlogits is None or (tuple(dlogits.shape) == (T, V) and dlogits.dtype == logits.dtype),
-             "dlogits must have the shape and dtype of logits")
+    for t, count, name in ((teacher_lse, T, "teacher_lse"), (mask, T, "mask"), (kl, T, "kl"), (seq_weight, M, "seq_weight"),
+                           (loss_acc, 1, "loss_acc")):
+        if t is not None and t.numel() != count:
+            _numel(t, count, name)
+    if dlogits is not None and not (dlogits.shape == logits.shape and dlogits.dtype == logits.dtype):
+        raise PodsError("dlogits must have the shape and dtype of logits")
     lp, ldl, dtype = _typed_rows(logits, "logits")
     here = _here()
     _same_device(logits, "logits", here)
@@ -611,16 +614,18 @@ def pods_distill_chunk(logits, ids, values, teacher_lse, seq_weight, cu_seqlens,
         kl = torch.empty(T, dtype=f32, device=dev)
     if dlogits is None and want_grad:
         dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev)
-    need = pods_distill_chunk_workspace_bytes(T)
+    lib = load()
+    need = lib.pods_distill_chunk_workspace_bytes(T)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     size = workspace.numel()
-    _require(size >= need, "workspace must hold %d bytes, got %d" % (need, size))
+    if size < need:
+        raise PodsError("workspace must hold %d bytes, got %d" % (need, size))
     dp, ldd = None, 0
     if dlogits is not None:
         dp, ldd, _ = _typed_rows(dlogits, "dlogits")
         _same_device(dlogits, "dlogits", here)
-    rc = load().pods_distill_chunk(lp, ldl, dtype, _vec(ids, i32, T * K, "ids", here), _vec(values, f32, T * K, "values", here), K, K,
+    rc = lib.pods_distill_chunk(lp, ldl, dtype, _vec(ids, i32, T * K, "ids", here), _vec(values, f32, T * K, "values", here), K, K,
                                    _vec(teacher_lse, f32, T, "teacher_lse", here, True), _vec(seq_weight, f64, M, "seq_weight", here),
                                    _vec(cu_seqlens, torch.int64, M + 1, "cu_seqlens", here), M, row0,
                                    _vec(mask, torch.uint8, T, "mask", here, True), T, V, temperature,

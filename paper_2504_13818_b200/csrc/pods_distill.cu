@@ -939,7 +939,10 @@ constexpr size_t kMaxSmem = 227 * 1024;
 constexpr size_t kSegmentBytes = 40 * 1024;
 
 constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold for two of them to share an SM
-constexpr int64_t kPipeMinBytes = 16 << 20;
+// The pipeline from this much of logits on.  Measured, pipeline (with its preparation) against the kernel above, bf16:
+// V = 151936 20.7 : 20.7 us at 16 MB, 27.2 : 28.9 at 32 MB, 45.3 : 53.2 at 64 MB, 76.0 : 91.5 at 128 MB; V = 8000 24.0 : 23.8,
+// 37.1 : 39.1, 65.1 : 75.8; V = 1000 88 : 95, 166 : 180, 320 : 384.
+constexpr int64_t kPipeMinBytes = 32 << 20;
 
 template <int DT, int KP>
 int launch_distill(DistillArgs& a, cudaStream_t stream) {

@@ -1659,8 +1659,10 @@ int launch_rows(SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stre
     return launch_row_clusters<KERNEL>(a, a.T, cl, kThreads, smem, stream);
 }
 
-// The pipeline where there are rows enough for it; sets `marked` if it ran.
-constexpr int64_t kPipelineMinBytes = 16 << 20;
+// The pipeline where there are rows enough for it; sets `marked` if it ran.  Measured, pipeline (its three launches) against the
+// kernel for few rows, bf16: 27.0 : 22.9 us at 16 MB of logits of 151936, 30.9 : 37.0 at 32 MB, 41.2 : 45.3 at 64 MB, 71.3 : 78.2
+// at 128 MB; V = 32000 34.0 : 35.0 at 32 MB, 45.5 : 47.3 at 64 MB; V = 1000 213 : 209 at 32 MB, 394 : 409 at 64 MB.
+constexpr int64_t kPipelineMinBytes = 64 << 20;
 template <int DT>
 int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
     if (a.T * a.V * esize < kPipelineMinBytes || a.T > 0x7fffffff) return PODS_OK;

@@ -282,7 +282,8 @@ def test_empty_batches():
     assert binding.pods_topk(z, 5)[0].shape == (0, 5)
 
 
-@pytest.mark.parametrize("dtype,T,V,pad", [("bf16", 700, 32001, 0), ("fp32", 900, 5003, 1), ("fp16", 90, 151936, 0), ("bf16", 30000, 1000, 8), ("fp32", 130, 151936, 0)])
+@pytest.mark.parametrize("dtype,T,V,pad", [("bf16", 1100, 32001, 0), ("fp32", 3500, 5003, 1), ("fp16", 230, 151936, 0), ("bf16", 34000, 1000, 8),
+                                            ("fp32", 130, 151936, 0)])
 def test_many_rows_without_filters(dtype, T, V, pad):
     """Enough rows that each cluster takes several in a row (slots of the ring used more than once), rows that fp64 decides,
     rows without a distribution among them."""
