@@ -108,7 +108,7 @@ __device__ __forceinline__ int64_t find_rollout_warp(const int64_t* cu, int64_t 
 
 // KP: list entries a thread holds at most, so K <= KP * kThreads.
 template <int DT, int KP>
-__global__ void __launch_bounds__(kThreads, KP == 1 ? 4 : 2)
+__global__ void __launch_bounds__(kThreads, 2)
 pods_distill_kernel(const DistillArgs a) {
     using El = Elem<DT>;
     using raw = typename El::raw;
@@ -936,7 +936,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
 size_t align_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
 
 constexpr size_t kMaxSmem = 227 * 1024;
-constexpr size_t kSegmentBytes = 40 * 1024;
+constexpr size_t kSegmentBytes = 80 * 1024;            // segments of at most this size let two CTAs share an SM
 
 constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold for two of them to share an SM
 // The pipeline from this much of logits on.  Measured, pipeline (with its preparation) against the kernel above, bf16:
@@ -962,6 +962,8 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
     }
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
+    // few rows: spread over idle SMs down to a vector a thread
+    while (cl < kMaxCluster && 2 * cl * a.T <= 128 && segment_vectors(a.V, esize, 2 * cl) >= kThreads) cl *= 2;
     a.seg = segment_vectors(a.V, esize, cl);
     const size_t smem = kCtrlBytes + (size_t)a.seg * 16;
     if (smem > kMaxSmem) return PODS_ERR_UNSUPPORTED;
