@@ -282,7 +282,8 @@ int grpo_loss_from_hidden(const void* hidden, int64_t ldh, const void* W, int64_
  *   top_k   keeps the first top_k ids (off where <= 0 or >= V)
  *   top_p   of those, the shortest prefix whose sum of e is at least top_p times theirs, at least one id (off where >= 1)
  *   min_p   keeps the ids with e_v >= min_p (off where <= 0; above 1 it is read as 1)
- *   token = the first kept id, ids ascending, whose running sum of e exceeds u[t] times the kept sum
+ *   token = the first kept id, ids ascending, whose running sum of e exceeds u[t] times the kept sum (u = 0: the lowest kept
+ *           id whose logit is not -inf)
  *   logp  = log softmax(z / temperature)[token], before any filter: old_logp of an objective on logits / temperature
  *   logq  = the log-probability with which the token was drawn, after the filters
  * A temperature below 2^-20 takes the first id of the order; logp is then that of temperature 1, logq 0.  Tokens are
@@ -310,7 +311,7 @@ int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32
  * what a teacher leaves behind for pods_distill_chunk instead of its [T,V] logits.
  *   ids [dev] int32 [T,K]   values [dev] fp32 [T,K], the logits themselves   lse [dev] fp32 [T] or NULL:
  *   log sum_v exp(z_v / temperature)
- * Logits, mask and refusals as in pods_sample; 1 <= K <= min(V, PODS_MAX_TOPK); temperature > 0 and finite.  A row with NaN
+ * Logits, mask and refusals as in pods_sample; 1 <= K <= min(V, PODS_MAX_TOPK); temperature finite, at least FLT_MIN.  A row with NaN
  * or +inf gets ids -1 and NaN values and lse (PODS_STATUS_NONFINITE_LOGIT).  -inf logits come last, by id; a row of nothing
  * else has lse -inf (PODS_STATUS_EMPTY_ROW).
  */
@@ -328,10 +329,11 @@ size_t pods_distill_chunk_workspace_bytes(int64_t T);
  *   q_j = exp(y_j / temperature - L),  L = teacher_lse[t], or log sum_j exp(y_j / temperature) if teacher_lse is NULL
  *   Q = sum_j q_j;  s = the sum of p over the listed ids;  r = max(0, 1 - Q) with PODS_DISTILL_REST, else 0
  *   kl_t = sum_j q_j (log q_j - log p[id_j]) + r (log r - log(1 - s))
- *   g_t  = grad_scale mask_t w_i / temperature
+ *   g_t  = grad_scale mask_t w_i / temperature   (temperature finite, at least FLT_MIN)
  *   dlogits[t,v] = g_t ((Q + r) p_v - sum over the j with id_j == v of q_j)      listed v
  *                = g_t ((Q + r) p_v - r p_v / (1 - s))                           every other v
- * rounded to dtype (nearest even), and sum_t mask_t w_i kl_t is ADDED to *loss_acc (the caller zeroes it; fixed order).
+ * rounded to dtype (nearest even; bf16 entries outside the list may be the product of an exponential that was itself rounded to
+ * bf16, as in grpo_loss_chunk), and sum_t mask_t w_i kl_t is ADDED to *loss_acc (the caller zeroes it; fixed order).
  * 1 - s is summed over the ids outside the list, never taken as a difference.  Where they have no mass at all (every such
  * logit -inf, or none left) the rest's term is left out: r = 0.  A term with q_j = 0 is 0.  A listed id that the policy
  * cannot produce (logit -inf, q_j > 0) makes kl_t +inf with a finite gradient.
@@ -341,7 +343,7 @@ size_t pods_distill_chunk_workspace_bytes(int64_t T);
  *          outside [0, V) raises PODS_STATUS_TOKEN_RANGE and is unused too; an id may stand in several entries
  *   teacher_lse [dev] fp32 [T] or NULL (PODS_DISTILL_REST needs it)
  *   seq_weight, cu_seqlens, M, row0, mask: as in grpo_loss_chunk (grpo_seq_weights makes the weights)
- *   kl [dev] fp32 [T]: kl_t, 0 for rows whose mask or weight is 0 (those rows are not read)
+ *   kl [dev] fp32 [T]: kl_t, 0 for rows whose mask or weight is 0 (what their logits and lists hold is of no consequence)
  *   dlogits [dev] [T, V] of dtype, pitch ldd, or NULL for the loss alone; may be the same buffer as logits (in place,
  *          ldd == ldl), must not overlap it otherwise.  Rows whose mask or weight is 0 are zero.
  *   loss_acc [dev] fp64 scalar; workspace [dev] of pods_distill_chunk_workspace_bytes(T), 16-byte aligned

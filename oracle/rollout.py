@@ -43,12 +43,14 @@ def sample_row(row, u, tau=1.0, top_k=0, top_p=1.0, min_p=0.0):
         p_count = int(reach[0]) + 1 if len(reach) else count
     else:
         p_count = count
-    m_count = int((e >= min(min_p, 1.0)).sum()) if min_p > 0 else V
+    # e >= min_p, asked of the exponents: exp rounds to 1 what lies just below
+    m_count = int((d >= np.log(min(min_p, 1.0))).sum()) if min_p > 0 else V
     kept = ids[:max(1, min(count, p_count, m_count))]
     by_id = np.sort(kept)
     run = np.cumsum(e[by_id])
     target = u * run[-1]
-    at = int(np.nonzero(run > target)[0][0])
+    # at u = 0 every finite logit counts, also where fp64 has no weight left for it
+    at = int(np.nonzero(row[by_id] > -np.inf)[0][0]) if u == 0 else int(np.nonzero(run > target)[0][0])
     inner = run[:-1]
     if target > 0 and len(inner):
         edge = min(edge, float(np.abs(inner - target).min() / run[-1]))

@@ -12,6 +12,7 @@
 // writes the gradient, exponentials taken again (two on the special-function pipe per 4 bytes of traffic, where 2.8 would
 // be free).  The listed entries are then written over by the threads that hold them.
 
+#include <float.h>
 #include <stddef.h>
 
 #include "grpo_loss_common.cuh"
@@ -986,7 +987,7 @@ extern "C" int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype
     const size_t esize = dtype == PODS_DTYPE_F32 ? 4 : 2;
     if (T < 0 || V < 1 || M < 1 || row0 < 0 || ldl < V || K < 1 || ldk < K) return PODS_ERR_INVALID_ARG;
     if (V > PODS_MAX_ROW_V || K > PODS_MAX_TOPK || (flags & ~PODS_DISTILL_REST) != 0) return PODS_ERR_UNSUPPORTED;
-    if (!(temperature > 0.0f && temperature < INFINITY) || grad_scale != grad_scale) return PODS_ERR_INVALID_ARG;
+    if (!(temperature >= FLT_MIN && temperature < INFINITY) || grad_scale != grad_scale) return PODS_ERR_INVALID_ARG;
     if ((flags & PODS_DISTILL_REST) && teacher_lse == nullptr) return PODS_ERR_INVALID_ARG;
     if (dlogits != nullptr && (ldd < V || !pods_aligned(dlogits, esize) || (dlogits == logits && ldd != ldl)))
         return PODS_ERR_INVALID_ARG;

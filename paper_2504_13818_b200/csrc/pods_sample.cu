@@ -26,6 +26,7 @@
 // neighbours than the error of the fast sums (fp32 exponentials, summed eight at a time in fp32 and then in fp64; see
 // draw_margin) is taken again with fp64 exponentials throughout, so the outcome is that of fp64 arithmetic.
 
+#include <float.h>
 #include <stddef.h>
 
 #include "row_cluster.cuh"
@@ -45,11 +46,12 @@ constexpr int kRedoRows = 8192;               // rows of a cluster between two v
 
 // Errors of the fast sums, rigorously bounded.  An exponential e_v is off by at most (slope |d_v| + kFlat) of itself: the
 // rounding of the fused multiply-add (2^-24 of the exponent; `far` rows take a difference first, 2^-24 more) and of log2e / tau,
-// |d_v| deep; the hardware exponential (2^-22.5) and the three roundings of a vector's sum, flat.  The mean of |d| under the
-// row's distribution is at most ln V - ln Z (its entropy, ln Z + mean |d|, is at most ln V).
+// |d_v| deep (and ln 2 more, as R lies up to one above the maximum's exponent); the hardware exponential (2^-22.5) and the three
+// roundings of a vector's sum, flat.  The mean of |d| under the row's distribution is at most ln V - ln Z (its entropy,
+// ln Z + mean |d|, is at most ln V).
 constexpr double kFlat = 3.6e-7;
 __device__ __forceinline__ double deep_error(int V, double Z, float c, double tau_inv, bool far) {
-    const float depth = fmaxf(0.0f, __logf((float)V) - __logf((float)Z)) + 0.01f;
+    const float depth = fmaxf(0.0f, __logf((float)V) - __logf((float)Z)) + 0.7f;
     const double log2e = fabs((double)c / tau_inv * 0.6931471805599453 - 1.0);
     return ((far ? 1.2e-7 : 6e-8) + log2e) * (double)depth;
 }
@@ -941,7 +943,20 @@ struct Finder {
         const double target = u * r.total;
         double before;
         const int owner = w.owner_of(r, target, &before);
-        if (owner == w.rank * W + w.warp) {
+        if (u == 0.0) {                                // the lowest kept id, however little its weight
+            const typename El::raw* el = reinterpret_cast<const typename El::raw*>(row_buf());
+            int id = kNoCut;
+            for (int i = w.v0 * E; i < w.v1 * E && id == kNoCut; ++i) {
+                const float x = El::to_float(el[i]);
+                if (x > -INFINITY && w.kept(x, w.s.id0 + i, thr, cut)) id = w.s.id0 + i;
+            }
+            id = block_reduce<W>(id, ctrl().ipart, Min());
+            if (w.tid == 0 && id != kNoCut) {
+                ctrl().found = id;
+                ctrl().sure = 1;
+                ctrl().weight = (double)El::to_float(el[id - w.s.id0]);
+            }
+        } else if (owner == w.rank * W + w.warp) {
             int at = 0;
             double lo = 0.0, ev = 0.0;
             if (w.template search<PREC, true>(target - before, sum, incl, top, tau_inv, thr, cut, &at, &lo, &ev)) {
@@ -958,7 +973,7 @@ struct Finder {
         const Xch* x = exchange(out);
         bool sure = false;
         *token = -1;
-        for (int q = 0; q < w.CL; ++q)
+        for (int q = w.CL - 1; q >= 0; --q)
             if (x[q].i >= 0) { *token = x[q].i; *logit = x[q].m; sure = x[q].n != 0; }
         *total = PREC ? r.total : r.total * exp2(top.far ? 0.0 : (double)top.R - (double)top.m * (double)top.c);
         return sure;
@@ -1044,24 +1059,27 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
 
     if (!FILTERS || !g.filtered) {
         const int mine = w.rank * W + w.warp;
-        if (g.greedy) {
-            int first = kNoCut;
+        if (g.greedy || g.u == 0.0f) {
+            // the lowest id of the maximum; u = 0: the lowest id of all that can be drawn, however little its weight
+            int from = kNoCut, id = kNoCut;
             for (int i = lane; i < CL * W; i += 32)
-                if (part[i].m == zmax) first = min(first, i);
-            if ((int)__reduce_min_sync(PODS_FULL_MASK, first) != mine) return;
-            int id = kNoCut;
+                if (g.greedy ? part[i].m == zmax : part[i].m > -INFINITY) from = min(from, i);
+            if ((int)__reduce_min_sync(PODS_FULL_MASK, from) != mine) return;
+            const float least = g.greedy ? zmax : -FLT_MAX;
             for (int j = w.v0; j < w.v1; ++j) {
                 float x[El::E];
                 El::unpack(row_buf()[j], x);
 #pragma unroll
                 for (int e = El::E - 1; e >= 0; --e)
-                    if (x[e] == zmax) id = min(id, w.id_of(j, e));
+                    if (x[e] >= least) id = min(id, w.id_of(j, e));
             }
             id = __reduce_min_sync(PODS_FULL_MASK, id);
             if (lane == 0) {
+                const float x = El::to_float(reinterpret_cast<const typename El::raw*>(row_buf())[id - w.s.id0]);
+                const float d = (float)(((double)x - (double)zmax) * tau_inv - (log(Z) + (PREC ? 0.0 : top.log_offset())));
                 a.tokens[t] = id;
-                if (a.logp) a.logp[t] = (float)-(log(Z) + (PREC ? 0.0 : top.log_offset()));
-                if (a.logq) a.logq[t] = 0.0f;
+                if (a.logp) a.logp[t] = d;
+                if (a.logq) a.logq[t] = g.greedy ? 0.0f : d;
             }
             return;
         }
@@ -1190,7 +1208,9 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
 #pragma unroll
                     for (int k = 0; k < PT; ++k) {
                         const int i = tid * per2 + k;
-                        if (k < per2 && i < count && pick == kNoCut && base2 + run[k] > target) pick = i;
+                        if (k < per2 && i < count && pick == kNoCut &&
+                            (g.u == 0.0f ? unorder32((uint32_t)list[i]) > -INFINITY : base2 + run[k] > target))
+                            pick = i;
                     }
                     pick = block_reduce<W>(pick, ctl.ipart, Min());
                     if (pick >= count) pick = count - 1;
@@ -1448,7 +1468,9 @@ pods_sample_policy_kernel(const SampleArgs a) {
                 owner = __shfl_sync(PODS_FULL_MASK, owner, from);
                 before = __shfl_sync(PODS_FULL_MASK, before, from);
                 om = __shfl_sync(PODS_FULL_MASK, om, from);
-                if (owner / PW == rank) {
+                if (u == 0.0f) {                       // needs every id's own logit: left to the other kernel
+                    if (rank == 0 && lane == 0) a.tokens[t] = kMarked;
+                } else if (owner / PW == rank) {
                     const int w = owner % PW;
                     const PartRef ref(om, cexp);
                     const double scale = ref.scale_to(top), goal = (target - before) / scale;
@@ -1761,7 +1783,7 @@ extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t
     int esize = 0;
     const int rc = check_rows(logits, ldl, dtype, T, V, &esize);
     if (rc != PODS_OK) return rc;
-    if (K < 1 || K > V || !(temperature > 0.0f && temperature < INFINITY)) return PODS_ERR_INVALID_ARG;
+    if (K < 1 || K > V || !(temperature >= FLT_MIN && temperature < INFINITY)) return PODS_ERR_INVALID_ARG;
     if (K > PODS_MAX_TOPK) return PODS_ERR_UNSUPPORTED;
     if (T == 0) return PODS_OK;
     if (logits == nullptr || ids == nullptr || values == nullptr) return PODS_ERR_INVALID_ARG;

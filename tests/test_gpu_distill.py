@@ -18,7 +18,9 @@ pytestmark = pytest.mark.gpu
 
 DT = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
 SUM_RTOL = 1.6e-6
-HALF_SUBNORMAL = {"bf16": 2.0 ** -127, "fp16": 2.0 ** -25, "fp32": 2.0 ** -126}   # fp32, bf16: the exponential flushes below 2^-126
+# the smallest step that an entry can be off by: half the smallest fp16; where the type reaches as far as fp32, what the
+# exponential loses by giving 0 below 2^-126 (e <= 1 scales with a factor of at most g)
+HALF_SUBNORMAL = {"bf16": 2.0 ** -126, "fp16": 2.0 ** -25, "fp32": 2.0 ** -126}
 
 
 def make(T, V, K, dtype, seed, pad=0, offset=0, M=3, holes=False, sharp=False):

@@ -110,6 +110,19 @@ def test_first_and_last_random_number():
         check_sample(z, u, **f)
 
 
+@pytest.mark.parametrize("V", [1000, 20000, 143193])
+def test_zero_takes_the_lowest_kept_id_however_little_its_weight(V):
+    """Rows that rise with the id at a cold temperature: the first ids weigh e^-700 and less."""
+    z = (torch.randn((3, V), generator=torch.Generator().manual_seed(1)) * 10).sort(1).values.to(torch.bfloat16).cuda()
+    z[1, : V // 3] = -np.inf
+    u = torch.zeros(3).cuda()
+    for f in (dict(), dict(top_k=400), dict(top_k=700), dict(top_p=0.99999), dict(min_p=1e-30), dict(top_p=0.5)):
+        check_sample(z, u, tau=0.01, **f)
+    many = z[:1].expand(34 * 10 ** 6 // V, V).contiguous()      # rows enough for the pipeline
+    got = binding.pods_sample(many, torch.zeros(many.shape[0]).cuda(), temperature=0.01)
+    assert (got[0] == 0).all() and torch.isfinite(got[1]).all()
+
+
 @pytest.mark.parametrize("V,dtype", [(1000, "fp32"), (151936, "bf16")])
 def test_each_row_has_its_own_settings(V, dtype):
     T = 24

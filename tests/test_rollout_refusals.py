@@ -32,7 +32,7 @@ def topk(logits=fake, ldl=100, dtype=0, T=4, V=100, K=5, tau=1.0, ids=fake, valu
 def test_topk_refusals():
     assert topk(T=0) == 0
     assert topk(dtype=7) == 2 and topk(V=524289, ldl=524289) == 2 and topk(V=2000, ldl=2000, K=1025) == 2
-    for bad in (dict(K=0), dict(K=101), dict(tau=0.0), dict(tau=-1.0), dict(tau=NAN), dict(tau=INF), dict(ids=None), dict(values=None),
+    for bad in (dict(K=0), dict(K=101), dict(tau=0.0), dict(tau=-1.0), dict(tau=1e-39), dict(tau=NAN), dict(tau=INF), dict(ids=None), dict(values=None),
                 dict(logits=None), dict(ldl=5), dict(T=-3)):
         assert topk(**bad) == 1, bad
 
@@ -48,7 +48,7 @@ def test_distill_refusals():
     assert distill(dtype=3) == 2 and distill(V=524289, ldl=524289, ldd=524289) == 2 and distill(K=1025, ldk=1025) == 2
     assert distill(flags=2) == 2
     for bad in (dict(K=0), dict(ldk=7), dict(M=0), dict(row0=-1), dict(T=-1), dict(V=0), dict(ldl=99), dict(ldd=99), dict(tau=0.0),
-                dict(tau=NAN), dict(scale=NAN), dict(flags=1), dict(logits=None), dict(ids=None), dict(values=None), dict(loss=None),
+                dict(tau=1e-39), dict(tau=NAN), dict(scale=NAN), dict(flags=1), dict(logits=None), dict(ids=None), dict(values=None), dict(loss=None),
                 dict(kl=None), dict(dl=C.c_void_p(4097)), dict(dl=fake, ldd=104), dict(loss=C.c_void_p(260))):
         assert distill(**bad) == 1, bad
     need = binding.pods_distill_chunk_workspace_bytes(4)
