@@ -417,7 +417,7 @@ struct Rows {
     }
     // An edge of the running sum nearer than the margin is decided in fp64 (the row's start is no edge).
     __device__ __forceinline__ bool certain(double u, double target, double lo, double ev, double total, const PartRef& top, double tau_inv) const {
-        const double margin = draw_margin(u, total, deep_error(a.V, total, top.c, tau_inv, top.far));
+        const double margin = draw_margin(u, total, deep_error(a.V, total, top.c, tau_inv, top.near_far()));
         return (target - lo > margin || lo == 0.0) && lo + ev - target > margin;
     }
 
@@ -731,7 +731,9 @@ struct Finder {
     // The sampler: all lists in the row's order in the first CTA's `list`, every CTA placing its own entries; n <= kSampleList.
     __device__ __forceinline__ void order_lists() {
         unsigned long long* const first = w.cl.map_shared_rank(list(), 0);
-        rank_lists(w.rank, w.rank + 1, [&](int r, unsigned long long key) { first[r] = key; });
+        rank_lists(w.rank, w.rank + 1, [&](int r, unsigned long long key) {
+            if (PODS_INDEX_OK(r, kSampleList, w.a.status)) first[r] = key;
+        });
         w.cl.sync();
     }
 
@@ -877,7 +879,7 @@ struct Finder {
         for (int q = 0; q < w.CL; ++q) { A += x[q].a; Z += x[q].b; }
         if (!PREC) Z = S;
         const double goal = (double)top_p * Z;
-        const double deep = deep_error(w.a.V, Z, top.c, tau_inv, top.far);
+        const double deep = deep_error(w.a.V, Z, top.c, tau_inv, top.near_far());
         const double margin = PREC ? 0.0 : exact_S ? (deep + kFlat) * goal + 1e-12 * Z : draw_margin((double)top_p, Z, deep);
         Xch out = {};
         const bool fits = len > 0 && len <= kSampleList;
@@ -1133,7 +1135,7 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
         double kept_total = 1.0;
         // can the list settle the kept set?  (a nucleus that ends at its very end is found out below)
         const bool over_list = g.top_k > 0 || whole;   // what top_p is a share of
-        const double slack = over_list ? 0.0 : (deep_error(a.V, Zm, c, tau_inv, top.far) + kFlat) * (double)g.top_p * Zm + 1e-12 * Zm;
+        const double slack = over_list ? 0.0 : (deep_error(a.V, Zm, c, tau_inv, top.near_far()) + kFlat) * (double)g.top_p * Zm + 1e-12 * Zm;
         const bool listed = n > 0 && n <= kSampleList && (g.top_k == 0 || n >= g.top_k || whole || (to_floor && !g.nucleus)) &&
                             (!g.nucleus || over_list || to_floor || list_mass > (double)g.top_p * Zm + slack);
         if (listed) f->order_lists();
@@ -1508,7 +1510,7 @@ pods_sample_policy_kernel(const SampleArgs a) {
                             if (run > goal) break;
                         }
                         const double edge = before + lo * scale, next = edge + ev * scale;
-                        const double margin = draw_margin((double)u, Z, deep_error(a.V, Z, cexp, tau_inv, top.far));
+                        const double margin = draw_margin((double)u, Z, deep_error(a.V, Z, cexp, tau_inv, top.near_far()));
                         if (at >= 0 && (target - edge > margin || edge == 0.0) && next - target > margin) {
                             const float d = (float)(((double)x - (double)zmax) * tau_inv - (log(Z) + top.log_offset()));
                             a.tokens[t] = at;
@@ -1683,11 +1685,12 @@ int launch_rows(SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stre
 
 // The pipeline where there are rows enough for it; sets `marked` if it ran.  Measured, pipeline (its three launches) against the
 // kernel for few rows, bf16: 27.0 : 22.9 us at 16 MB of logits of 151936, 30.9 : 37.0 at 32 MB, 41.2 : 45.3 at 64 MB, 71.3 : 78.2
-// at 128 MB; V = 32000 34.0 : 35.0 at 32 MB, 45.5 : 47.3 at 64 MB; V = 1000 213 : 209 at 32 MB, 394 : 409 at 64 MB.
+// at 128 MB; V = 32000 34.0 : 35.0 at 32 MB, 45.5 : 47.3 at 64 MB; V = 1000 213 : 209 at 32 MB, 394 : 409 at 64 MB.  (The marks' numbers
+// fit 32 bits with kMarked for the rows that are admitted.)
 constexpr int64_t kPipelineMinBytes = 64 << 20;
 template <int DT>
 int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
-    if (a.T * a.V * esize < kPipelineMinBytes || a.T > 0x7fffffff) return PODS_OK;
+    if (a.T * a.V * esize < kPipelineMinBytes || a.T > 0x7ffffff0) return PODS_OK;
     // the smallest cluster whose stages fit twice on an SM: few partners, and few places of the GPU left empty by its size
     static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
     int cl = 0;

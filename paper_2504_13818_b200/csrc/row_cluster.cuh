@@ -30,7 +30,6 @@ template <int DT> struct Elem;
 template <> struct Elem<PODS_DTYPE_BF16> {
     using raw = uint16_t;
     static constexpr int E = 8;
-    static constexpr int kKeyBits = 16;
     static constexpr raw kNegInf = 0xff80u;
     __device__ static __forceinline__ float to_float(raw r) { return __uint_as_float((uint32_t)r << 16); }
     __device__ static __forceinline__ raw from_float(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
@@ -71,7 +70,6 @@ template <> struct Elem<PODS_DTYPE_BF16> {
 template <> struct Elem<PODS_DTYPE_F16> {
     using raw = uint16_t;
     static constexpr int E = 8;
-    static constexpr int kKeyBits = 16;
     static constexpr raw kNegInf = 0xfc00u;
     __device__ static __forceinline__ float to_float(raw r) { return __half2float(__ushort_as_half(r)); }
     __device__ static __forceinline__ raw from_float(float v) { return __half_as_ushort(__float2half_rn(v)); }
@@ -114,7 +112,6 @@ template <> struct Elem<PODS_DTYPE_F16> {
 template <> struct Elem<PODS_DTYPE_F32> {
     using raw = uint32_t;
     static constexpr int E = 4;
-    static constexpr int kKeyBits = 32;
     static constexpr raw kNegInf = 0xff800000u;
     __device__ static __forceinline__ float to_float(raw r) { return __uint_as_float(r); }
     __device__ static __forceinline__ raw from_float(float v) { return __float_as_uint(v); }
@@ -305,9 +302,12 @@ struct PartRef {
     __device__ __forceinline__ double exp1(float x) const { return (double)ex2_approx(far ? (x - m) * c : fmaf(x, c, -R)); }
     // what sums relative to this reference are multiplied with to be relative to that of `top`, the row's
     __device__ __forceinline__ double scale_to(const PartRef& top) const {
-        if (!top.far) return pow2((int)fmaxf(R - top.R, -2000.0f));
+        if (!top.far && !far) return pow2((int)fmaxf(R - top.R, -2000.0f));
+        if (!top.far) return exp2((double)m * (double)c - (double)top.R);
         return exp2((far ? (double)m * (double)c : (double)R) - (double)top.m * (double)c);
     }
+    // whether a part that counts beside this one may be far
+    __device__ __forceinline__ bool near_far() const { return !(fabsf(R) < 0x1p22f); }
     // ln of this reference's own weight over e^(m / tau): what log sums relative to it lack
     __device__ __forceinline__ double log_offset() const { return far ? 0.0 : ((double)R - (double)m * (double)c) * kLn2; }
 };
@@ -321,16 +321,6 @@ __device__ __forceinline__ T warp_scan(T v, int lane) {
         if (lane >= d) v += o;
     }
     return v;
-}
-
-// The same for any d: NaN stays, what overflows is +inf.
-__device__ __forceinline__ void exp64x4_any(double (&d)[4]) {
-    double e[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = fmin(d[i], 700.0);
-    exp64x4(e);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) d[i] = d[i] > 700.0 ? (double)INFINITY : d[i] == d[i] ? e[i] : d[i];
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }

@@ -123,6 +123,20 @@ def test_zero_takes_the_lowest_kept_id_however_little_its_weight(V):
     assert (got[0] == 0).all() and torch.isfinite(got[1]).all()
 
 
+@pytest.mark.parametrize("V", [4000, 60000])
+@pytest.mark.parametrize("tau", [1.0, 0.01])
+def test_logits_where_exponents_of_two_run_out_of_fractions(V, tau):
+    """Maxima of a row's parts lie on both sides of the exponent 2^23, where references change their form."""
+    at = -2.0 ** 23 * np.log(2.0) * tau
+    for seed in range(4):
+        z = torch.randn((8, V), generator=torch.Generator().manual_seed(seed), dtype=torch.float64) * (2 * tau)
+        z = (z - z.max(1, keepdim=True).values + at + 0.5 * tau * torch.arange(8)[:, None]).to(torch.float32).cuda()
+        u = torch.rand(8, generator=torch.Generator().manual_seed(100 + seed)).cuda()
+        check_sample(z, u, tau=tau)
+        check_sample(z, u, tau=tau, top_k=100)
+        check_sample(z, u, tau=tau, top_p=0.8)
+
+
 @pytest.mark.parametrize("V,dtype", [(1000, "fp32"), (151936, "bf16")])
 def test_each_row_has_its_own_settings(V, dtype):
     T = 24
