@@ -39,7 +39,7 @@ constexpr int W = 8;                          // warps of a CTA
 constexpr int kThreads = W * 32;
 constexpr float kGreedyBelow = 0x1p-20f;      // temperatures below this are the arg-max
 constexpr int kSampleList = 1024;             // entries that the sampler's first CTA orders
-constexpr int kBins = 1024;                   // stretches of the mass histogram
+constexpr int kBins = 2048;                   // stretches of the mass histogram, as many as fit the ordered list's place
 constexpr int kNoCut = 0x7fffffff;
 constexpr int kMarked = -2;                   // token of a row that the pipeline leaves to fp64
 constexpr int kRedoRows = 8192;               // rows of a cluster between two visits of the marked ones
@@ -612,6 +612,15 @@ struct Finder {
         const int at = atomicAdd(&ctrl().n_list, 1);
         if (at < w.a.own_cap) own()[at] = ((unsigned long long)order32(x) << 32) | (uint32_t)~id;
     }
+    // Lists those elements of vector j whose bit is set: as many steps as the warp's busiest lane has, not one an element.
+    __device__ __forceinline__ void list_hits(int j, uint32_t hits) {
+        const typename El::raw* const el = reinterpret_cast<const typename El::raw*>(row_buf());
+        while (hits) {
+            const int e = __ffs(hits) - 1;
+            hits &= hits - 1;
+            if (w.is_id(w.id_of(j, e))) list_add(El::to_float(el[j * E + e]), w.id_of(j, e));
+        }
+    }
     // Hands my list to every CTA, with `mine`; returns the CL words and the lists' length together.  Each list has a room of
     // list_cap; -1 if one is longer.  PACKED: the lengths are exchanged first and the lists laid end to end, for lists that are
     // known to fit together but may all come from one CTA.
@@ -655,9 +664,10 @@ struct Finder {
             if (El::vec_max(q) < thr) continue;
             float x[E];
             El::unpack(q, x);
+            uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (w.is_id(w.id_of(j, e)) && w.kept(x[e], w.id_of(j, e), thr, cut)) list_add(x[e], w.id_of(j, e));
+            for (int e = 0; e < E; ++e) hits |= w.kept(x[e], w.id_of(j, e), thr, cut) ? 1u << e : 0u;
+            list_hits(j, hits);
         }
     }
     // Lists the kept ids of the row; returns how many, -1 if they do not fit.
@@ -777,13 +787,16 @@ struct Finder {
         for (int q = 0; q < w.CL; ++q) {
             const uint32_t* const peer = w.cl.map_shared_rank(hist() + w.tid * PB, q);
 #pragma unroll
-            for (int k = 0; k < PB; k += 2) {
-                const uint2 h = *reinterpret_cast<const uint2*>(peer + k);
+            for (int k = 0; k < PB; k += 4) {
+                const uint4 h = *reinterpret_cast<const uint4*>(peer + k);
                 n[k] += h.x;
                 n[k + 1] += h.y;
+                n[k + 2] += h.z;
+                n[k + 3] += h.w;
             }
         }
-        static_assert(PB % 2 == 0, "8 bytes a read");
+        static_assert(PB % 4 == 0, "16 bytes a read");
+        static_assert(kBins * 4 <= kSampleList * 8, "the histogram lies where the list does");
         double run[PB], sum = 0.0;
 #pragma unroll
         for (int k = 0; k < PB; ++k) {
@@ -834,9 +847,9 @@ struct Finder {
             if (!all_ids)                              // ids that top_k left out weigh nothing
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[e] = w.kept(x[e], w.id_of(j, e), *thr, *cut) ? x[e] : -INFINITY;
-            bool any = false;
+            uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) any |= x[e] >= x_lo && x[e] <= x_hi;
+            for (int e = 0; e < E; ++e) hits |= x[e] >= x_lo && x[e] <= x_hi ? 1u << e : 0u;
             if (PREC) {
 #pragma unroll
                 for (int h = 0; h < E; h += 4) {
@@ -862,10 +875,7 @@ struct Finder {
                 for (int e = 0; e < E; ++e) p[e] = x[e] > x_hi ? p[e] : 0.0f;
                 above += (double)vec_add(p);
             }
-            if (any)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x[e] >= x_lo && x[e] <= x_hi && w.is_id(w.id_of(j, e))) list_add(x[e], w.id_of(j, e));
+            list_hits(j, hits);
         }
         if (!PREC) *lane_above = above;
         // relative to e^zmax
@@ -919,16 +929,22 @@ struct Finder {
         }
         return x[0].n;
     }
-    // The lane's fast sum over the kept ids, from its sum above the bracket and the bracket's entries.
+    // The lane's fast sum over the kept ids, from its sum above the bracket and the bracket's entries: a thread an entry, added
+    // to the lane that holds it in units of 2^-53, so that their order does not matter (each lane walking all entries took 5000
+    // cycles of a row's 80000).  e is at most 1 and the entries of the cluster at most 1024: no overflow, and 1.2e-13 of rounding.
     __device__ __forceinline__ double bracket_sum(double lane_above, float thr, int cut, const PartRef& top) {
-        const int n = min(ctrl().n_list, w.a.own_cap);
-        for (int k = 0; k < n; ++k) {
+        unsigned long long* const extra = reinterpret_cast<unsigned long long*>(hist());
+        extra[w.tid] = 0ull;
+        __syncthreads();
+        const int n = min(ctrl().n_list, w.a.own_cap), share = (w.s.cnt + W - 1) / W, per = ((share + 31) / 32) | 1;
+        for (int k = w.tid; k < n; k += kThreads) {
             const unsigned long long key = own()[k];
             const float x = unorder32((uint32_t)(key >> 32));
             const int id = (int)~(uint32_t)key, j = (id - w.s.id0) / E;
-            if (j >= w.v0 && j < w.v1 && w.kept(x, id, thr, cut)) lane_above += top.exp1(x);
+            if (w.kept(x, id, thr, cut)) atomicAdd(&extra[j / share * 32 + j % share / per], (unsigned long long)(top.exp1(x) * 0x1p53));
         }
-        return lane_above;
+        __syncthreads();
+        return lane_above + (double)extra[w.tid] * 0x1p-53;
     }
 
     // Draws over the kept ids; the whole cluster gets the token, its logit and the kept sum relative to top's maximum.
