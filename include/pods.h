@@ -294,7 +294,8 @@ int grpo_loss_from_hidden(const void* hidden, int64_t ldh, const void* W, int64_
  *   temperature_row, top_p_row, min_p_row [dev] fp32 [T] and top_k_row [dev] int32 [T]: each row's own settings; where
  *          one is NULL the scalar beside it holds for every row
  *   mask   [dev] uint8 [T] or NULL: rows with mask 0 are not read and their outputs are left as they were
- *   tokens [dev] int32 [T]    logp, logq [dev] fp32 [T], each may be NULL
+ *   tokens [dev] int32 [T] (while the call runs they may hold other negative numbers)
+ *   logp, logq [dev] fp32 [T], each may be NULL
  * Row settings out of range (temperature negative, infinite or NaN: 1 is used; top_p or min_p NaN: off; u below 0 or NaN:
  * 0; u of 1 or more: the largest number below 1) raise PODS_STATUS_PARAM_RANGE; a bad scalar temperature, top_p or min_p
  * returns PODS_ERR_INVALID_ARG.  -inf marks an id that cannot be drawn.  A row of -inf alone gets token -1 and -inf log-
@@ -311,9 +312,9 @@ int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32
  * what a teacher leaves behind for pods_distill_chunk instead of its [T,V] logits.
  *   ids [dev] int32 [T,K]   values [dev] fp32 [T,K], the logits themselves   lse [dev] fp32 [T] or NULL:
  *   log sum_v exp(z_v / temperature)
- * Logits, mask and refusals as in pods_sample; 1 <= K <= min(V, PODS_MAX_TOPK); temperature finite, at least FLT_MIN.  A row with NaN
- * or +inf gets ids -1 and NaN values and lse (PODS_STATUS_NONFINITE_LOGIT).  -inf logits come last, by id; a row of nothing
- * else has lse -inf (PODS_STATUS_EMPTY_ROW).
+ * Logits, mask and refusals as in pods_sample; 1 <= K <= min(V, PODS_MAX_TOPK); temperature finite, at least FLT_MIN.  A
+ * row with NaN or +inf gets ids -1 and NaN values and lse (PODS_STATUS_NONFINITE_LOGIT).  -inf logits come last, by id; a
+ * row of nothing else has lse -inf (PODS_STATUS_EMPTY_ROW).
  */
 int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, int32_t K, float temperature,
               const uint8_t* mask, int32_t* ids, float* values, float* lse, uint32_t* status, void* stream);

@@ -7,10 +7,15 @@
 // one factor for the row.  What concerns the list is fp64: K exponentials a CTA, against V / CL fp32 ones twice.
 //
 // A cluster of CTAs holds the row in shared memory (row_cluster.cuh): one read and one write per element.  The listed
-// logits are taken out first (their slots become -inf), so both sweeps run over the segment without asking about the
-// list; the first CTA-wide sweep is the maximum, the second the sum, and after one exchange over the cluster the third
-// writes the gradient, exponentials taken again (two on the special-function pipe per 4 bytes of traffic, where 2.8 would
-// be free).  The listed entries are then written over by the threads that hold them.
+// logits are taken out first (their slots become -inf), so the sweeps run over the segment without asking about the list:
+// maximum, sum, and after one exchange over the cluster the gradient; the listed entries are written over it.  Two kernels:
+//   many rows, K <= 128   pods_distill_pipe_kernel: every warp one task, rows overlap, only mbarriers.  4096 x 151936 bf16
+//             with K = 64: 549 us = 4.5 TB/s of one read and one write, 0.69 of the measured copy rate.  Bound by the
+//             consumers' issue slots (53 % of all) and the special-function pipe (one exponential an element, the sum's;
+//             the gradient scales what the sum's sweep kept).  512 x 151936 fp32 with K = 128: 144 us = 4.3 TB/s, 0.66.
+//   all others   pods_distill_kernel: every warp does everything, a dozen CTA barriers a row, which bound it, and two
+//             exponentials an element.  600 x 50257 fp16, the loss alone: 33 us = 1.8 TB/s; 37 rows of 1024: 13 us, four
+//             dependent launches of 2 to 5 us.
 
 #include <float.h>
 #include <stddef.h>
@@ -109,7 +114,7 @@ __device__ __forceinline__ int64_t find_rollout_warp(const int64_t* cu, int64_t 
 
 // KP: list entries a thread holds at most, so K <= KP * kThreads.
 template <int DT, int KP>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, KP == 1 ? 4 : 2)
 pods_distill_kernel(const DistillArgs a) {
     using El = Elem<DT>;
     using raw = typename El::raw;
@@ -474,8 +479,7 @@ distill_prep_kernel(const DistillArgs a) {
 // the list warp of each CTA they took 7200 of a row's 9900 cycles, and every other warp waited for that one.
 // Parts and factors have four slots each.  A part of row i is sent after its sender has seen the factors of row i - 2, which
 // took every CTA's parts of row i - 2, which were sent after the factors of row i - 4 were made: the slot of row i - 4 is free.
-constexpr int PW = 8;
-constexpr int kPipeThreads = (PW + 3) * 32;
+// PW: consumer warps, 8 where two CTAs share an SM, 16 where one has it alone.
 constexpr int kStages = 3, kRing = 4;
 constexpr int kPipeK = 128;                   // entries of a list: four a lane
 
@@ -511,14 +515,14 @@ struct PipeCtrl {
     alignas(16) Entry entry[1];               // [kRing][K], then PipePart [kRing][CL PW]
 };
 __host__ __device__ constexpr int pipe_part_offset(int K) { return (int)offsetof(PipeCtrl, entry) + kRing * K * (int)sizeof(Entry); }
-__host__ __device__ constexpr int pipe_ctrl_bytes(int cl, int K) {
-    return (pipe_part_offset(K) + kRing * cl * PW * (int)sizeof(PipePart) + 127) & ~127;
+__host__ __device__ constexpr int pipe_ctrl_bytes(int cl, int K, int pw) {
+    return (pipe_part_offset(K) + kRing * cl * pw * (int)sizeof(PipePart) + 127) & ~127;
 }
 
 extern __shared__ __align__(128) unsigned char smem_[];
 
-template <int DT>
-__global__ void __launch_bounds__(kPipeThreads, 2)
+template <int DT, int PW>
+__global__ void __launch_bounds__((PW + 3) * 32, 16 / PW)
 pods_distill_pipe_kernel(const DistillArgs a) {
     using El = Elem<DT>;
     using raw = typename El::raw;
@@ -527,7 +531,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
     cg::cluster_group cl = cg::this_cluster();
     const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
     PipePart* const part = reinterpret_cast<PipePart*>(smem_ + pipe_part_offset(a.K));
-    uint4* const stages = reinterpret_cast<uint4*>(smem_ + pipe_ctrl_bytes(CL, a.K));
+    uint4* const stages = reinterpret_cast<uint4*>(smem_ + pipe_ctrl_bytes(CL, a.K, PW));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t n_clusters = gridDim.x / CL, first = blockIdx.x / CL;
     const int n_rows = first < a.T ? (int)((a.T - first + n_clusters - 1) / n_clusters) : 0;
@@ -779,10 +783,11 @@ pods_distill_pipe_kernel(const DistillArgs a) {
     } else {
         // ---- consumers ----
         // Where the gradient's vectors lie on the logits' (shift 0) and the exponents are of ordinary size, the sweep of front()
-        // serves back() too: a bf16 row keeps bf16(e) in the stage and back() scales it with two-term bf16 factors.  That is a
-        // second rounding of the ids outside the list, half a step each time, as in grpo_loss_chunk's gradient; it saves the
-        // exponentials' second pass, which with the first fills half of the special-function pipe.  fp16 could not hold e.
-        constexpr bool kKeep = DT == PODS_DTYPE_BF16;
+        // serves back() too: an fp32 row keeps e in the stage, a bf16 row bf16(e), which back() scales with two-term bf16
+        // factors.  In bf16 that is a second rounding of the ids outside the list, half a step each time, as in
+        // grpo_loss_chunk's gradient; it saves the exponentials' second pass, which with the first fills half of the
+        // special-function pipe (4096 x 151936 bf16: 731 us without, with the preparation apart 564).  fp16 could not hold e.
+        constexpr bool kKeep = DT != PODS_DTYPE_F16;
         struct Slice { float R; bool kept; };
         auto aligned = [&](const Segment& s, int64_t t) {
             const int dlead = (int)((reinterpret_cast<uintptr_t>(static_cast<raw*>(a.dlogits) + t * a.ldd) & 15) / sizeof(raw));
@@ -814,14 +819,26 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                         for (int j = whole_lo + lane; j < whole_hi; j += 32) dvec[j] = make_uint4(0u, 0u, 0u, 0u);
                     } else if (kKeep && slice.kept) {
                         const float coef = f.coef * (float)pow2_any(slice.R - ref.R);
-                        const uint16_t hi16 = pods_loss::to_bf16_bits(coef);
-                        const uint16_t lo16 = pods_loss::to_bf16_bits(coef - __uint_as_float((uint32_t)hi16 << 16));
-                        const uint32_t c_hi = (uint32_t)hi16 * 0x10001u, c_lo = (uint32_t)lo16 * 0x10001u;
+                        if constexpr (DT == PODS_DTYPE_F32) {
+                            const unsigned long long c2 = pack2(coef, coef);
 #pragma unroll 4
-                        for (int j = whole_lo + lane; j < whole_hi; j += 32) {
-                            uint4 q = buf[j];
-                            pods_loss::scale_vec(q, c_hi, c_lo);
-                            dvec[j] = q;
+                            for (int j = whole_lo + lane; j < whole_hi; j += 32) {
+                                float x[E];
+                                El::unpack(buf[j], x);
+#pragma unroll
+                                for (int e = 0; e < E; e += 2) unpack2(mul2(pack2(x[e], x[e + 1]), c2), x[e], x[e + 1]);
+                                dvec[j] = El::pack(x);
+                            }
+                        } else {
+                            const uint16_t hi16 = pods_loss::to_bf16_bits(coef);
+                            const uint16_t lo16 = pods_loss::to_bf16_bits(coef - __uint_as_float((uint32_t)hi16 << 16));
+                            const uint32_t c_hi = (uint32_t)hi16 * 0x10001u, c_lo = (uint32_t)lo16 * 0x10001u;
+#pragma unroll 4
+                            for (int j = whole_lo + lane; j < whole_hi; j += 32) {
+                                uint4 q = buf[j];
+                                pods_loss::scale_vec(q, c_hi, c_lo);
+                                dvec[j] = q;
+                            }
                         }
                     } else {
 #pragma unroll 2
@@ -937,30 +954,36 @@ pods_distill_pipe_kernel(const DistillArgs a) {
 size_t align_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
 
 constexpr size_t kMaxSmem = 227 * 1024;
-constexpr size_t kSegmentBytes = 80 * 1024;            // segments of at most this size let two CTAs share an SM
-
 constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold for two of them to share an SM
-// The pipeline from this much of logits on.  Measured, pipeline (with its preparation) against the kernel above, bf16:
-// V = 151936 20.7 : 20.7 us at 16 MB, 27.2 : 28.9 at 32 MB, 45.3 : 53.2 at 64 MB, 76.0 : 91.5 at 128 MB; V = 8000 24.0 : 23.8,
-// 37.1 : 39.1, 65.1 : 75.8; V = 1000 88 : 95, 166 : 180, 320 : 384.
+// The pipeline from this much of logits on.  Measured, pipeline (with its preparation) against the kernel above, at 16, 32
+// and 64 MB: bf16 V = 1000 88 : 94, 162 : 180, 306 : 385 us; V = 8000 25 : 25, 37 : 39, 69 : 75; V = 32000 21 : 19, 29 : 31,
+// 49 : 57; V = 151936 19 : 21, 27 : 29, 46 : 54; fp32 V = 1000 47 : 53, 83 : 96, 150 : 198; V = 8000 18 : 17, 25 : 25, 43 : 53;
+// V = 32000 19 : 17, 25 : 25, 43 : 51; V = 151936 21 : 19, 26 : 27, 44 : 53.
 constexpr int64_t kPipeMinBytes = 32 << 20;
 
 template <int DT, int KP>
 int launch_distill(DistillArgs& a, cudaStream_t stream) {
     const int esize = DT == PODS_DTYPE_F32 ? 4 : 2;
     if (a.K <= kPipeK && a.T * a.V * esize >= kPipeMinBytes && a.T <= 0x7fffffff) {
-        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size.
-        // (Rows too long for three stages stay with the kernel above: 203 us for 512 fp32 rows of 151936, 218 us with two stages.)
+        // the smallest cluster whose stages fit twice on an SM: few partners, few places of the GPU left empty by its size;
+        // for rows too long for that the smallest that fits an SM once, with twice the consumers.  (512 fp32 rows of
+        // 151936: 144 us on clusters of 9, 178 of 10, 236 of 12, 226 of 16; 218 with two stages twice an SM; 198 by the kernel above.
+        // One CTA an SM where two fit: 602 us for 4096 bf16 rows of 151936 against 551.)
         static const int kSizes[] = {1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 16};
-        for (int size : kSizes) {
-            a.seg = segment_vectors(a.V, esize, size);
-            const size_t smem = pipe_ctrl_bytes(size, a.K) + (size_t)kStages * a.seg * 16;
-            if (smem > kHalfSmBytes) continue;
-            distill_prep_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, stream>>>(a);
-            PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
-            return launch_row_clusters<pods_distill_pipe_kernel<DT>>(a, a.T, size, kPipeThreads, smem, stream);
-        }
+        for (int pw = 8; pw <= 16; pw *= 2)
+            for (int size : kSizes) {
+                a.seg = segment_vectors(a.V, esize, size);
+                const size_t smem = pipe_ctrl_bytes(size, a.K, pw) + (size_t)kStages * a.seg * 16;
+                if (smem > (pw == 8 ? kHalfSmBytes : kMaxSmem)) continue;
+                distill_prep_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, stream>>>(a);
+                PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
+                return pw == 8 ? launch_row_clusters<pods_distill_pipe_kernel<DT, 8>>(a, a.T, size, 11 * 32, smem, stream)
+                               : launch_row_clusters<pods_distill_pipe_kernel<DT, 16>>(a, a.T, size, 19 * 32, smem, stream);
+            }
     }
+    // segments that let as many CTAs share an SM as registers allow: four, or two with long lists.  Four against two, bf16:
+    // 16 MB of V = 1000 94 : 154 us, of 8000 25 : 33, 64 MB of 151936 54 : 60; V = 32000 57 : 62; fp32 51 : 54.
+    constexpr size_t kSegmentBytes = (KP == 1 ? 55 : 80) * 1024;
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
     // few rows: spread over idle SMs down to a vector a thread

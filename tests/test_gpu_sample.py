@@ -259,6 +259,24 @@ def test_another_stream_and_a_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip((tokens, logp, ids, values, lse), want))
 
 
+def far_apart(rows, pitch):
+    """The rows in a storage of 9 GB: offsets past 2^32 elements."""
+    T, V = rows.shape
+    flat = torch.empty(T * pitch, dtype=rows.dtype, device="cuda")
+    out = flat.view(T, pitch)[:, :V]
+    out.copy_(rows)
+    return out
+
+
+def test_rows_far_apart():
+    z = far_apart(make(224, 151936, "bf16", seed=2), 20_000_003)         # rows enough for the pipeline
+    u = uniform(224, 4)
+    check_sample(z, u)
+    check_sample(z[200:], u[200:], top_k=40, top_p=0.9)
+    check_sample(z[200:], u[200:], top_p=0.95)
+    check_topk(z[200:], 100)
+
+
 # ---- pods_topk ------------------------------------------------------------------------------------------------------
 
 def check_topk(z, K, tau=1.0, expect_status=0):
