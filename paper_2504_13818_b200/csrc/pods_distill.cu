@@ -12,7 +12,7 @@
 //   many rows, K <= 128   pods_distill_pipe_kernel: every warp one task, rows overlap, only mbarriers.  4096 x 151936 bf16
 //             with K = 64: 549 us = 4.5 TB/s of one read and one write, 0.69 of the measured copy rate.  Bound by the
 //             consumers' issue slots (53 % of all) and the special-function pipe (one exponential an element, the sum's;
-//             the gradient scales what the sum's sweep kept).  512 x 151936 fp32 with K = 128: 144 us = 4.3 TB/s, 0.66.
+//             the gradient scales what the sum's sweep kept).  512 x 151936 fp32 with K = 128: 144 to 148 us = 4.2 TB/s, 0.65.
 //   all others   pods_distill_kernel: every warp does everything, a dozen CTA barriers a row, which bound it, and two
 //             exponentials an element.  600 x 50257 fp16, the loss alone: 33 us = 1.8 TB/s; 37 rows of 1024: 13 us, four
 //             dependent launches of 2 to 5 us.
@@ -805,11 +805,15 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                 raw* const drow = static_cast<raw*>(a.dlogits) + t * a.ldd;
                 const int share = (s.cnt + PW - 1) / PW, lo = min(s.cnt, warp * share), hi = min(s.cnt, lo + share);
                 const PartRef ref(f.m2, cexp);
+                // what the slice kept is relative to its own reference
+                const float to_ref = !(kKeep && slice.kept) ? 1.0f
+                                     : ref.far ? (float)exp64(((double)slice.R - (double)f.m2 * (double)cexp) * kLn2)
+                                               : pow2_any(slice.R - ref.R);
                 // element k of the segment, alone
                 auto one = [&](int k) {
                     if (f.mode == 0) return (raw)0;
                     const float x = El::to_float(elems[k]);
-                    return El::from_float(f.coef * (kKeep && slice.kept ? x * (float)pow2_any(slice.R - ref.R) : (float)ref.exp1(x)));
+                    return El::from_float(f.coef * (kKeep && slice.kept ? x * to_ref : (float)ref.exp1(x)));
                 };
                 if (aligned(s, t)) {
                     uint4* const dvec = reinterpret_cast<uint4*>(drow + s.id0);
@@ -818,7 +822,7 @@ pods_distill_pipe_kernel(const DistillArgs a) {
                     if (f.mode == 0) {
                         for (int j = whole_lo + lane; j < whole_hi; j += 32) dvec[j] = make_uint4(0u, 0u, 0u, 0u);
                     } else if (kKeep && slice.kept) {
-                        const float coef = f.coef * (float)pow2_any(slice.R - ref.R);
+                        const float coef = f.coef * to_ref;
                         if constexpr (DT == PODS_DTYPE_F32) {
                             const unsigned long long c2 = pack2(coef, coef);
 #pragma unroll 4
@@ -986,7 +990,7 @@ int launch_distill(DistillArgs& a, cudaStream_t stream) {
     constexpr size_t kSegmentBytes = (KP == 1 ? 55 : 80) * 1024;
     int cl = 1;
     while (cl < kMaxCluster && (size_t)segment_vectors(a.V, esize, cl) * 16 > kSegmentBytes) cl *= 2;
-    // few rows: spread over idle SMs down to a vector a thread
+    // few rows: spread over idle SMs down to a vector a thread (3 bf16 rows of 151936 and 16 of 32000: 14.6 -> 12.6 us)
     while (cl < kMaxCluster && 2 * cl * a.T <= 128 && segment_vectors(a.V, esize, 2 * cl) >= kThreads) cl *= 2;
     a.seg = segment_vectors(a.V, esize, cl);
     const size_t smem = kCtrlBytes + (size_t)a.seg * 16;

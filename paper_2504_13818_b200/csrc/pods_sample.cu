@@ -25,6 +25,15 @@
 // Which token is drawn must not depend on how sums are split or rounded: a draw or a border that lies nearer to its
 // neighbours than the error of the fast sums (fp32 exponentials, summed eight at a time in fp32 and then in fp64; see
 // draw_margin) is taken again with fp64 exponentials throughout, so the outcome is that of fp64 arithmetic.
+//
+// What it takes on one B200 (6.54 TB/s measured copy rate; rows of 151936 bf16 unless said), and what bounds it:
+//   512 rows, no filter   77 us = 2.0 TB/s: the pipeline 53 us (44 % of the issue slots, 48 % of the special-function pipe, the
+//            rest waits of one row for its slowest part), then 5 % of these flat rows in fp64, 16 to 28 us
+//   512 rows, nuclei of thousands   427 us: 82 K cycles a row, of which the histogram's shared-memory atomics 22 K, the bracket
+//            sweep 14 K, ranking and border 16 K, first sweep and load 10 K, about ten cluster barriers the rest
+//   64 fp32 rows with settings of their own   43 us; one row, top_k and top_p   19 us: a chain of cluster barriers, rankings
+//            and fp64 exponentials, not bandwidth
+//   pods_topk, 1024 rows, K = 64   179 us = 1.7 TB/s; 16 fp32 rows of 32000, K = 20   12 us: the same chain, fewer steps
 
 #include <float.h>
 #include <stddef.h>
@@ -35,7 +44,7 @@ using namespace pods_row;
 
 namespace {
 
-constexpr int W = 8;                          // warps of a CTA
+constexpr int W = 8;                          // warps of a CTA (12 and 16 were slower on three of the four filter cases)
 constexpr int kThreads = W * 32;
 constexpr float kGreedyBelow = 0x1p-20f;      // temperatures below this are the arg-max
 constexpr int kSampleList = 1024;             // entries that the sampler's first CTA orders
@@ -748,7 +757,8 @@ struct Finder {
     }
 
     // Shrinks (thr, cut) to the smallest prefix of the kept ids whose sum of e reaches top_p of theirs, where the border is
-    // found in one bracket of the mass histogram; S: their sum, by fast exponentials or (exact_S) in fp64.  false: the bracket does not fit the lists.
+    // found in one bracket of the mass histogram; S: their sum, by fast exponentials or (exact_S) in fp64.  false: the bracket
+    // does not fit the lists.
     // lane_above: see bracket_sum; negative where there is none.
     __device__ bool nucleus_threshold(float top_p, double S, bool exact_S, const PartRef& top, double tau_inv, float* thr, int* cut, double* lane_above) {
         // logits below this have less than 1 - top_p of the mass together, so the border lies above
@@ -1677,7 +1687,12 @@ pods_topk_kernel(const SampleArgs a) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 constexpr size_t kMaxSmem = 227 * 1024;
-constexpr size_t kSegmentBytes = 80 * 1024;            // segments of at most this size let two CTAs share an SM
+// Segments of at most this size let two CTAs share an SM, and the smallest such cluster has the fewest partners to wait for.
+// With twice the CTAs a row: 64 fp32 rows of 151936 with their own settings 43 -> 94 us, 512 bf16 rows with wide nuclei 427 ->
+// 877, pods_topk of 1024 bf16 rows 179 -> 276; with half of them, one CTA an SM, all three were slower too.
+// A cluster wide enough for a bound on top_k above 128, as K gets one, does not pay: V = 32000, 512 rows, top_k = 300 264 -> 223
+// us, but 700 270 -> 356 us, and V = 4000, 300 86 -> 222 us.
+constexpr size_t kSegmentBytes = 80 * 1024;
 
 constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold for two of them to share an SM
 
@@ -1685,7 +1700,8 @@ constexpr size_t kHalfSmBytes = 233472 / 2 - 1024;     // what a CTA may hold fo
 int row_cluster_size(int64_t V, int64_t T, int esize, int K) {
     int cl = 1;
     while (cl < kMaxCluster && ((size_t)segment_vectors(V, esize, cl) * 16 > kSegmentBytes || cl * kThreads < 2 * K)) cl *= 2;
-    // few rows: spread over idle SMs down to two vectors a lane
+    // few rows: spread over idle SMs down to a vector a thread.  One row of 32000 bf16: top_k = 200 45 -> 21 us, 700 121 -> 31 us,
+    // top_k = 50 21 -> 19 us; of 151936: 700 41 -> 33 us, 50 19 -> 20 us
     while (cl < kMaxCluster && 2 * cl * T <= 128 && segment_vectors(V, esize, 2 * cl) >= kThreads) cl *= 2;
     return cl;
 }

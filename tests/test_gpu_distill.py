@@ -132,6 +132,20 @@ def test_rows_far_apart():
     check(b, run(b, rest=True, dlogits=b["z"]), rest=True, z=z)
 
 
+@pytest.mark.parametrize("sign", [1, -1])
+def test_logits_where_exponents_of_two_run_out_of_fractions(sign):
+    """Maxima of a row's parts lie on both sides of the exponent 2^23, where references change their form."""
+    T, V = 520, 17001
+    b = make(T, V, 20, "fp32", seed=4)
+    z = b["z"].double() + sign * 2.0 ** 23 * np.log(2.0) + torch.linspace(-12, 6, T, device="cuda", dtype=torch.float64)[:, None]
+    b["z"].copy_(z.float())
+    for t in (T, 5):                                                     # the pipeline, and the kernel for few rows
+        part = dict(b, z=b["z"][:t], ids=b["ids"][:t], values=b["values"][:t], teacher=b["teacher"][:t], mask=b["mask"][:t],
+                    cu=torch.tensor([0, t // 2, t], device="cuda"))
+        for mode in MODES:
+            check(part, run(part, **mode), rest=mode["rest"])
+
+
 @pytest.mark.parametrize("V", [9, 1000, 50257])
 def test_holes_and_sure_policies(V):
     """-inf logits inside and outside the list (kl +inf, gradient finite); a policy with all but e^-60 on one id, where 1 - s
