@@ -157,10 +157,10 @@ pods_distill_kernel(const DistillArgs a) {
         float y[KP];
         double q[KP];
         double Q = 0.0, H = 0.0, L = 0.0;              // sum q, sum q log q, log-normaliser
+        bool odd = false;                              // an id out of range
         if (!masked) {
             const int32_t* ids = a.ids + t * a.ldk;
             const float* vals = a.values + t * a.ldk;
-            bool odd = false;
             float ymax = -INFINITY;
 #pragma unroll
             for (int k = 0; k < KP; ++k) {
@@ -204,12 +204,12 @@ pods_distill_kernel(const DistillArgs a) {
             block_sums(two, c.dpart);
             Q = two[0];
             H = two[1];
-            if (odd && rank == 0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
             if (!mbar_wait(&c.full, phase, kSpinLimit) && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
             phase ^= 1u;
         }
         __syncthreads();
         const double w = c.weight;
+        if (odd && rank == 0 && w != 0.0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
 
         // the part of the gradient row that is mine
         const int id_lo = max(0, s.id0), id_hi = min(a.V, s.id0 + s.cnt * E);
@@ -436,7 +436,7 @@ distill_prep_kernel(const DistillArgs a) {
             if (id >= 0 && id < a.V) ymax = max_nan(ymax, vals[j]);
             else odd |= id != -1;
         }
-        if (__any_sync(PODS_FULL_MASK, odd) && lane == 0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
+        if (__any_sync(PODS_FULL_MASK, odd) && lane == 0 && p.w != 0.0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
         if (a.teacher_lse != nullptr) {
             p.L = (double)a.teacher_lse[t];
         } else {

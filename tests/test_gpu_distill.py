@@ -363,3 +363,35 @@ def test_many_rows(dtype, T, V, K, pad, offset):
     # the bits of `got` where its rows lie as the logits' do; elsewhere see above
     assert (dtype != "fp16" and (pad, offset) != (0, 0)) or same(inplace["dl"], got["dl"])
     assert np.array_equal(inplace["kl"], got["kl"], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype,T,V,K", [("bf16", 12, 1000, 20), ("fp32", 12, 5003, 300), ("bf16", 120, 151936, 20), ("fp32", 520, 17001, 128)])
+def test_rollouts_of_weight_zero_leave_no_trace(dtype, T, V, K):
+    """Rows that are not masked but whose rollout weighs nothing: ids out of range, NaN in the lists and in the logits raise no
+    bit and leave a loss of 0 and a row of zeros; the other rows are as ever."""
+    b = make(T, V, K, dtype, seed=11, M=4)
+    mask = torch.ones(T, dtype=torch.uint8, device="cuda")
+    weight = torch.tensor([0.25, 0.0, 0.25, 0.0], dtype=torch.float64, device="cuda")
+    L = torch.logsumexp(b["teacher"].double(), 1).float().cuda()
+    of_row = oracle.seq_of_rows(b["cu"].cpu().numpy())
+    dead = torch.from_numpy(np.isin(of_row, (1, 3))).cuda()
+    want_acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    want_kl, want_dl = binding.pods_distill_chunk(b["z"], b["ids"], b["values"], L, weight, b["cu"], 0, mask, want_acc, rest=True)
+    b["ids"][dead, 0] = V
+    b["ids"][dead, K // 2] = -9
+    b["values"][dead, 1] = float("nan")
+    b["z"][dead, V - 1] = float("nan")
+    b["z"][dead, 0] = float("inf")
+    for m in (mask, None):
+        acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+        status = binding.new_status()
+        kl, dl = binding.pods_distill_chunk(b["z"], b["ids"], b["values"], L, weight, b["cu"], 0, m, acc, rest=True, status=status)
+        torch.cuda.synchronize()
+        assert binding.read_status(status) == 0
+        assert (kl[dead] == 0).all() and (dl[dead] == 0).all()
+        assert torch.equal(kl, want_kl) and torch.equal(dl, want_dl) and torch.equal(acc, want_acc)
+    # where a row weighs something, the same id counts
+    b["ids"][int((~dead).nonzero()[0]), 0] = V
+    status = binding.new_status()
+    binding.pods_distill_chunk(b["z"], b["ids"], b["values"], L, weight, b["cu"], 0, mask, acc, rest=True, status=status)
+    assert binding.read_status(status) == binding.STATUS_TOKEN_RANGE
