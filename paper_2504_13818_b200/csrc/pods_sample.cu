@@ -69,6 +69,14 @@ __device__ __forceinline__ double deep_error(int V, double Z, float c, double ta
 __device__ __forceinline__ double draw_margin(double u, double Z, double deep) {
     return (fmax(u, 1.0 - u) * deep + 2.1 * u * (1.0 - u) * kFlat + 1e-12) * Z;
 }
+// A point below this share of the kept sum is always fp64's: there a fast running sum of 0 need not be the row's start.  What
+// it may hide of the ids ahead: exponentials below 2^-126 of their part's reference, which become 0 (at most 2^19 2^-125 of
+// the sum), and what bracket_sum and fp64 additions round off (together below 3e-13).
+constexpr double kFastFrom = 1e-12;
+// Whether a drawn point `target` = u Z between the edges lo and hi of the fast running sum is sure to lie between the exact ones.
+__device__ __forceinline__ bool draw_is_sure(double u, double target, double lo, double hi, double margin) {
+    return u > kFastFrom && (target - lo > margin || lo == 0.0) && hi - target > margin;
+}
 
 struct SampleArgs {
     const void* logits;
@@ -424,10 +432,11 @@ struct Rows {
         }
         return true;
     }
-    // An edge of the running sum nearer than the margin is decided in fp64 (the row's start is no edge).
+    // An edge of the running sum nearer than the margin is decided in fp64 (the row's start is no edge where u is no smaller
+    // than the fast sums see).
     __device__ __forceinline__ bool certain(double u, double target, double lo, double ev, double total, const PartRef& top, double tau_inv) const {
         const double margin = draw_margin(u, total, deep_error(a.V, total, top.c, tau_inv, top.near_far()));
-        return (target - lo > margin || lo == 0.0) && lo + ev - target > margin;
+        return draw_is_sure(u, target, lo, lo + ev, margin);
     }
 
     // A value that at least ceil(want / CL) logits of the segment reach, so the least one of the cluster is reached by `want`
@@ -1537,7 +1546,7 @@ pods_sample_policy_kernel(const SampleArgs a) {
                         }
                         const double edge = before + lo * scale, next = edge + ev * scale;
                         const double margin = draw_margin((double)u, Z, deep_error(a.V, Z, cexp, tau_inv, top.near_far()));
-                        if (at >= 0 && (target - edge > margin || edge == 0.0) && next - target > margin) {
+                        if (at >= 0 && draw_is_sure((double)u, target, edge, next, margin)) {
                             const float d = (float)(((double)x - (double)zmax) * tau_inv - (log(Z) + top.log_offset()));
                             a.tokens[t] = at;
                             if (a.logp) a.logp[t] = d;

@@ -356,3 +356,42 @@ def test_many_rows_without_filters(dtype, T, V, pad):
     live = torch.ones(T, dtype=torch.uint8, device="cuda")
     other = binding.pods_sample(z, u, temperature=1.5, mask=live)
     assert torch.equal(tokens, other[0])
+
+
+# ---- random numbers far below the steps of the usual generators ------------------------------------------------------------
+
+def check_small_u(z, u, **settings):
+    """The oracle's tokens; that the draws are asked for fairly is a share of the drawn point itself: an fp64 sum of V <= 2^18
+    terms in any order is off by at most 2^18 * 2^-53 = 3e-11 of itself."""
+    status = binding.new_status()
+    tokens, logp, _ = binding.pods_sample(z, u, status=status, **settings)
+    torch.cuda.synchronize()
+    assert binding.read_status(status) == 0
+    rows, un = z.double().cpu().numpy(), u.cpu().numpy().astype(np.float64)
+    for t in range(z.shape[0]):
+        want = rollout.sample_row(rows[t], un[t], min_p=float(np.float32(settings.get("min_p", 0.0))), top_k=settings.get("top_k", 0))
+        run = np.cumsum(np.exp(rows[t] - rows[t].max())[np.sort(want["kept"])])
+        target = un[t] * run[-1]
+        assert np.abs(run[:-1] - target).min() > 1e-9 * target
+        assert int(tokens[t]) == want["token"], (t, un[t], int(tokens[t]), want["token"])
+        assert abs(float(logp[t]) - want["logp"]) <= log_tol(want["logp"])
+
+
+@pytest.mark.parametrize("V,dtype", [(600, "fp32"), (5003, "bf16"), (5003, "fp32"), (151936, "bf16")])
+def test_weights_that_fp32_flushes_can_be_drawn(V, dtype):
+    """The ids ahead of the maximum weigh 2 to 4e-39 of it, below the normal numbers of fp32: u = 1e-39 draws the first of them,
+    u = 1e-38 the fourth."""
+    z = torch.full((8, V), -30.0)
+    z[:, 0] = -88.5
+    z[:, 1:7] = -89.0
+    z[:, 7] = 0.0
+    z[:, V - 1] = -95.0                                    # what top_k = V - 1 leaves out
+    z = z.to(DT[dtype]).cuda()
+    u = torch.tensor([1e-39, 4.5e-39, 1e-38, 1e-20, 1.5e-13, 1e-7, 0.5, 1e-45]).cuda()
+    check_small_u(z, u)
+    check_small_u(z, u, min_p=1e-44)                       # a floor below every id: by list at V = 600, by threshold above
+    check_small_u(z, u, top_k=V - 1)
+    T = (64 << 20) // (V * z.element_size()) + 1           # rows enough for the pipeline
+    many = binding.pods_sample(z.repeat(T // 8 + 1, 1), u.repeat(T // 8 + 1))
+    few = binding.pods_sample(z, u)
+    assert (many[0].view(-1, 8) == few[0]).all()
