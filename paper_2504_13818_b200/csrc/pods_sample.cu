@@ -136,10 +136,12 @@ __device__ __forceinline__ uint4* row_buf() { return reinterpret_cast<uint4*>(sm
 __device__ __forceinline__ FilterCtrl& filter_ctrl(const SampleArgs& a) { return *reinterpret_cast<FilterCtrl*>(smem_ + kRowCtrlBytes + a.seg * 16); }
 constexpr int kFilterCtrlBytes = (sizeof(FilterCtrl) + 127) & ~127;
 
-// Inclusive scan over the CTA in thread order; *total is the sum.
-__device__ __forceinline__ double block_scan(double v, double* part, double* total) {
+// Sum of the threads ahead, in thread order; *total is the sum of all.  Never a difference of an inclusive sum and one's own
+// part: a large part would round off what lies ahead of it, which a small u may ask for.
+__device__ __forceinline__ double block_scan_ahead(double v, double* part, double* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     v = warp_scan(v, lane);
+    const double ahead = scan_ahead(v, lane);
     __syncthreads();
     if (lane == 31) part[warp] = v;
     __syncthreads();
@@ -150,7 +152,7 @@ __device__ __forceinline__ double block_scan(double v, double* part, double* tot
         all += part[w];
     }
     *total = all;
-    return v + before;
+    return ahead + before;
 }
 
 // Sorts list[0, n) ascending, n <= kSampleList; keys differ.  Few entries are ranked, each against all; many go through a
@@ -383,7 +385,7 @@ struct Rows {
         const uint32_t hit = __ballot_sync(PODS_FULL_MASK, r.incl > target && r.mine > 0.0);
         const int from = hit ? __ffs(hit) - 1 : 0;
         int owner = -1;
-        double b = r.incl - r.mine, at = b;
+        double b = scan_ahead(r.incl, lane), at = b;
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (r.v[i] > 0.0 && (owner < 0 || !(b > target))) {    // the first that passes the target, else the last
@@ -403,7 +405,7 @@ struct Rows {
         const uint32_t any = __ballot_sync(PODS_FULL_MASK, sum > 0.0);
         if (any == 0) return false;
         const int from = hit ? __ffs(hit) - 1 : 31 - __clz(any);
-        const double ahead = __shfl_sync(PODS_FULL_MASK, incl - sum, from);
+        const double ahead = __shfl_sync(PODS_FULL_MASK, scan_ahead(incl, lane), from);
         // the elements of that lane's vectors, k a lane
         const int e0 = __shfl_sync(PODS_FULL_MASK, v0, from) * E, e1 = __shfl_sync(PODS_FULL_MASK, v1, from) * E;
         const int k = (e1 - e0 + 31) / 32;
@@ -415,12 +417,12 @@ struct Rows {
         };
         double own = 0.0;
         for (int i = k0; i < k1; ++i) own += at(i);
-        const double eincl = warp_scan(own, lane);
+        const double eincl = warp_scan(own, lane), eahead = scan_ahead(eincl, lane);
         hit = __ballot_sync(PODS_FULL_MASK, ahead + eincl > goal && own > 0.0);
         const uint32_t some = __ballot_sync(PODS_FULL_MASK, own > 0.0);
         if (some == 0) return false;
         if (lane != (hit ? __ffs(hit) - 1 : 31 - __clz(some))) return false;
-        double run = ahead + eincl - own;
+        double run = ahead + eahead;
         for (int i = k0; i < k1; ++i) {
             const double w = at(i);
             if (!(w > 0.0)) continue;
@@ -823,7 +825,7 @@ struct Finder {
             run[k] = sum;
         }
         double all;
-        const double base = block_scan(sum, ctrl().dpart, &all) - sum;
+        const double base = block_scan_ahead(sum, ctrl().dpart, &all);
         const double goal = (double)top_p * S, tol = 2e-4 * S;     // 1.3e-4 of rounding, the quadratic, the fast sum S
         int below = 0, first = kBins - 1;
 #pragma unroll
@@ -921,7 +923,7 @@ struct Finder {
                 if (i < len) own += exp64(((double)unorder32((uint32_t)(list()[i] >> 32)) - (double)top.m) * tau_inv);
             }
             double sum_all;
-            double at = A + block_scan(own, ctrl().dpart, &sum_all) - own;
+            double at = A + block_scan_ahead(own, ctrl().dpart, &sum_all);
             int pick = kNoCut, unsure = w.tid == 0 && !from_top && fabs(A - goal) <= margin;
             for (int k = 0; k < per; ++k) {
                 const int i = w.tid * per + k;
@@ -1190,7 +1192,7 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
                     run[k] = own;
                 }
                 double total;
-                const double base = block_scan(own, ctl.dpart, &total) - own;
+                const double base = block_scan_ahead(own, ctl.dpart, &total);
                 // the nucleus: the first entry whose running sum reaches top_p of the (top-k) sum
                 int count = lim_n;
                 if (g.nucleus) {
@@ -1239,7 +1241,7 @@ __device__ __forceinline__ void sample_row(Rows<DT>& w, Finder<DT>* f, int64_t t
                         if (k < per2 && i < count) s2 += exp64(((double)unorder32((uint32_t)list[i]) - (double)zmax) * tau_inv);
                         run[k] = s2;
                     }
-                    const double base2 = block_scan(s2, ctl.dpart, &kept_total) - s2;
+                    const double base2 = block_scan_ahead(s2, ctl.dpart, &kept_total);
                     const double target = (double)g.u * kept_total;
                     int pick = kNoCut;
 #pragma unroll

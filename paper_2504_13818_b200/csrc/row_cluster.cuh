@@ -323,6 +323,13 @@ __device__ __forceinline__ T warp_scan(T v, int lane) {
     return v;
 }
 
+// Of a warp_scan's results: the sum of the lanes ahead.
+template <typename T>
+__device__ __forceinline__ T scan_ahead(T incl, int lane) {
+    const T o = __shfl_up_sync(PODS_FULL_MASK, incl, 1);
+    return lane > 0 ? o : T(0);
+}
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 __device__ __forceinline__ void mbar_init(unsigned long long* bar, uint32_t count) {

@@ -395,3 +395,27 @@ def test_weights_that_fp32_flushes_can_be_drawn(V, dtype):
     many = binding.pods_sample(z.repeat(T // 8 + 1, 1), u.repeat(T // 8 + 1))
     few = binding.pods_sample(z, u)
     assert (many[0].view(-1, 8) == few[0]).all()
+
+
+@pytest.mark.parametrize("V,dtype", [(600, "fp32"), (5003, "bf16"), (50257, "fp32"), (151936, "bf16")])
+def test_light_ids_ahead_of_a_heavy_one_are_told_apart(V, dtype):
+    """Ids of about 1e-20 of the row's mass, one that holds the rest somewhere behind them, and points drawn among the last of the
+    light ones: what lies ahead of the heavy id must not be rounded off by it (2^-53 of it is ten thousand of them)."""
+    heavy = sorted({4, 9, 40, 130, 333, 590, V // 3, V // 2 + 5, V - 300, V - 2})
+    T = 2 * len(heavy)
+    z = -46.0 + torch.randn((T, V), generator=torch.Generator().manual_seed(V))
+    for t in range(T):
+        z[t, heavy[t // 2]] = 0.0
+    z = z.to(DT[dtype])
+    e = np.exp(z.double().numpy())
+    u = torch.zeros(T)
+    for t in range(T):
+        last = heavy[t // 2] - 1 - t % 2                   # half way into the last light id ahead, or the one before it
+        u[t] = (e[t, :last].sum() + 0.5 * e[t, last]) / e[t].sum()
+    z, u = z.cuda(), u.cuda()
+    check_small_u(z, u)
+    check_small_u(z, u, min_p=1e-30)                       # a floor below every id: by list at V = 600, by threshold above
+    n = (64 << 20) // (T * V * z.element_size()) + 1       # rows enough for the pipeline
+    many = binding.pods_sample(z.repeat(n, 1), u.repeat(n))
+    few = binding.pods_sample(z, u)
+    assert (many[0].view(n, T) == few[0]).all()
