@@ -520,6 +520,8 @@ def pods_sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask=
             _numel(t, T, name)
     tau_t, tau = _setting(temperature, T, "temperature")
     k_t, k = _setting(top_k, T, "top_k")
+    if not -0x80000000 <= k <= 0x7fffffff:              # off, like any number below 1 or above V; the call would see its low 32 bits
+        k = 0
     p_t, p = _setting(top_p, T, "top_p")
     m_t, m = _setting(min_p, T, "min_p")
     lp, ldl, dtype = _typed_rows(logits, "logits")

@@ -419,3 +419,12 @@ def test_light_ids_ahead_of_a_heavy_one_are_told_apart(V, dtype):
     many = binding.pods_sample(z.repeat(n, 1), u.repeat(n))
     few = binding.pods_sample(z, u)
     assert (many[0].view(n, T) == few[0]).all()
+
+
+def test_top_k_of_any_size_is_off_above_the_row():
+    z = make(16, 1000, "fp32", seed=12)
+    u = uniform(16, 8)
+    want = binding.pods_sample(z, u, want_logq=True)
+    for k in (0, -1, 1000, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 40 + 3, -2 ** 31, -2 ** 32 + 2, np.int64(2 ** 33 + 1)):
+        got = binding.pods_sample(z, u, top_k=k, want_logq=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
