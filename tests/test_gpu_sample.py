@@ -428,3 +428,48 @@ def test_top_k_of_any_size_is_off_above_the_row():
     for k in (0, -1, 1000, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 40 + 3, -2 ** 31, -2 ** 32 + 2, np.int64(2 ** 33 + 1)):
         got = binding.pods_sample(z, u, top_k=k, want_logq=True)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+def same_bits(a, b):
+    return bool(((a == b) | (torch.isnan(a) & torch.isnan(b)) if a.is_floating_point() else a == b).all())
+
+
+@pytest.mark.parametrize("dtype,T,V,pad", [("bf16", 1100, 32001, 0), ("fp16", 230, 151936, 8), ("bf16", 34000, 1000, 0), ("fp32", 130, 151936, 1)])
+def test_many_rows_without_filters_the_same_bits_every_time_and_under_a_mask(dtype, T, V, pad):
+    """The pipeline's ring, marks and numbers leave nothing to the order in which its warps come: the same bits each time, rows
+    without a distribution among them.  Then half of the rows masked: those are left as they were, the others are as before."""
+    z = make(T, V, dtype, seed=T + 1, kind="normal", pad=pad)
+    z[3] = -np.inf
+    z[T // 3, 0] = np.nan
+    u = uniform(T, 14)
+    status = binding.new_status()
+    first = binding.pods_sample(z, u, temperature=1.3, want_logq=True, status=status)
+    assert binding.read_status(status) == binding.STATUS_EMPTY_ROW | binding.STATUS_NONFINITE_LOGIT
+    for _ in range(4):
+        again = binding.pods_sample(z, u, temperature=1.3, want_logq=True)
+        assert all(same_bits(a, b) for a, b in zip(first, again))
+    tok, lp, lq = (x.cpu().numpy().astype(np.float64) for x in first)
+    un = u.cpu().numpy()
+    for t in sorted({0, 1, 3, T // 3, T - 1} | set(range(0, T, max(1, T // 40)))):
+        want = rollout.sample_row(z[t].double().cpu().numpy(), float(un[t]), float(np.float32(1.3)))
+        if want["edge"] <= EDGE:
+            continue
+        assert tok[t] == want["token"], t
+        if want["token"] >= 0:
+            assert abs(lp[t] - want["logp"]) <= log_tol(want["logp"]) and abs(lq[t] - want["logq"]) <= log_tol(want["logq"])
+        else:
+            assert np.array_equal([lp[t], lq[t]], [want["logp"], want["logq"]], equal_nan=True)
+    mask = (torch.arange(T, device="cuda") % 7 < 4).to(torch.uint8)
+    live = mask.bool()
+    z[~live] = float("nan")                                # not read
+    z[3], z[T // 3] = 0.0, 0.0
+    given = [torch.full((T,), 77, dtype=torch.int32, device="cuda"), torch.full((T,), 2.5, device="cuda"), torch.full((T,), -3.5, device="cuda")]
+    status = binding.new_status()
+    binding.pods_sample(z, u, temperature=1.3, mask=mask, tokens=given[0], logp=given[1], logq=given[2], status=status)
+    assert binding.read_status(status) == 0
+    assert (given[0][~live] == 77).all() and (given[1][~live] == 2.5).all() and (given[2][~live] == -3.5).all()
+    live[3] = live[T // 3] = False                         # other rows now
+    assert torch.equal(given[0][live], first[0][live])
+    for x, y in zip(given[1:], first[1:]):                 # two kernels: each within log_tol of the exact value
+        x, y = x[live].double().cpu().numpy(), y[live].double().cpu().numpy()
+        assert (np.abs(x - y) <= 2 * log_tol(y)).all()
