@@ -395,3 +395,40 @@ def test_rollouts_of_weight_zero_leave_no_trace(dtype, T, V, K):
     status = binding.new_status()
     binding.pods_distill_chunk(b["z"], b["ids"], b["values"], L, weight, b["cu"], 0, mask, acc, rest=True, status=status)
     assert binding.read_status(status) == binding.STATUS_TOKEN_RANGE
+
+
+@pytest.mark.parametrize("dtype,T,V,K,pad,offset", [("bf16", 260, 100003, 200, 0, 0), ("fp32", 330, 50257, 300, 1, 3), ("fp16", 420, 60000, 129, 8, 5),
+                                                    ("bf16", 400, 70001, 1024, 0, 1), ("bf16", 180, 90001, 60, 3, 0)])
+def test_several_rows_a_cluster_without_the_pipeline(dtype, T, V, K, pad, offset):
+    """Lists above the pipeline's longest, and 32 MB of logits not reached: clusters of several CTAs that take more than one row,
+    so the segment, the load barrier and the exchange are used again; masked rows and rows without a distribution among them."""
+    b = make(T, V, K, dtype, seed=V, pad=pad, offset=offset, M=9)
+    b["mask"][[4, 6, T // 2]] = 1
+    b["mask"][[5, T // 2 + 1]] = 0
+    b["z"][4] = -np.inf
+    b["z"][5] = np.nan
+    b["z"][T // 2, V - 1] = np.nan
+    b["ids"][6, K - 1] = b["ids"][6, 0]
+    b["ids"][T - 1, K // 2:] = -1
+    bits = binding.STATUS_EMPTY_ROW | binding.STATUS_NONFINITE_LOGIT
+    got = run(b, tau=1.4, rest=True, expect_status=bits)
+    # some of the rows against the oracle, as if each were a rollout with the weight of its own
+    some = np.unique(np.r_[0:8, T // 2 - 1:T // 2 + 2, T - 2:T, np.arange(0, T, 23)])
+    at = torch.from_numpy(some).cuda()
+    row = oracle.seq_of_rows(b["cu"].cpu().numpy())
+    part = dict(b, z=b["z"][at], ids=b["ids"][at], values=b["values"][at], mask=b["mask"][at], cu=torch.arange(len(some) + 1, device="cuda"))
+    check(part, dict(kl=got["kl"][some], dl=got["dl"][at], loss=np.nan, L=got["L"][at], weight=got["weight"][row[some]], mask=got["mask"][some]),
+          tau=1.4, rest=True)
+    # every row against calls of so few rows that each has a cluster to itself: kl is within (Q + 2 r) SUM_RTOL and half a step of
+    # the exact value in both
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    weight = binding.grpo_seq_weights(b["mask"], b["cu"])
+    for lo in range(0, T, 40):
+        hi = min(T, lo + 40)
+        kl, dl = binding.pods_distill_chunk(b["z"][lo:hi], b["ids"][lo:hi], b["values"][lo:hi], got["L"][lo:hi], weight, b["cu"], lo,
+                                            b["mask"][lo:hi], acc, temperature=1.4, rest=True)
+        assert np.allclose(kl.cpu().numpy(), got["kl"][lo:hi], rtol=2.0 ** -23, atol=4 * SUM_RTOL, equal_nan=True)
+        assert ((kl == 0).cpu().numpy() == (got["kl"][lo:hi] == 0)).all()
+    again = run(b, tau=1.4, rest=True, expect_status=bits)
+    assert np.array_equal(again["kl"], got["kl"], equal_nan=True)
+    assert bool(((again["dl"] == got["dl"]) | (torch.isnan(again["dl"]) & torch.isnan(got["dl"]))).all())
