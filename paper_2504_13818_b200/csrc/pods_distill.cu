@@ -9,13 +9,17 @@
 // A cluster of CTAs holds the row in shared memory (row_cluster.cuh): one read and one write per element.  The listed
 // logits are taken out first (their slots become -inf), so the sweeps run over the segment without asking about the list:
 // maximum, sum, and after one exchange over the cluster the gradient; the listed entries are written over it.  Two kernels:
-//   many rows, K <= 128   pods_distill_pipe_kernel: every warp one task, rows overlap, only mbarriers.  4096 x 151936 bf16
-//             with K = 64: 549 us = 4.5 TB/s of one read and one write, 0.69 of the measured copy rate.  Bound by the
-//             consumers' issue slots (53 % of all) and the special-function pipe (one exponential an element, the sum's;
-//             the gradient scales what the sum's sweep kept).  512 x 151936 fp32 with K = 128: 144 to 148 us = 4.2 TB/s, 0.65.
+//   32 MB of logits and more, K <= 128   pods_distill_pipe_kernel: every warp one task, rows overlap, only mbarriers.
+//             4096 x 151936 bf16 with K = 64: 549 to 557 us = 4.5 TB/s of one read and one write, 0.69 of the measured copy rate;
+//             one exponential an element (the gradient scales what the sum's sweep kept).  Nothing is full (issue slots 53 %):
+//             its consumers sweep the stage for the maximum and again for the exponentials, and add to an fp64 sum once a vector,
+//             where the kernel of grpo_loss_cluster.cu holds its slice in registers and moves the same bytes at 0.95.
+//             512 x 151936 fp32 with K = 128: 144 to 148 us = 4.2 TB/s, 0.65, 9 % of it idle SMs.  1024 x 151936 with K = 64:
+//             bf16 153 us, fp16, which keeps nothing and takes two exponentials an element, 169.  600 x 50257 fp16, the loss
+//             alone: 33 us = 1.8 TB/s, six rows a cluster: filling and draining, and the launches around.
 //   all others   pods_distill_kernel: every warp does everything, a dozen CTA barriers a row, which bound it, and two
-//             exponentials an element.  600 x 50257 fp16, the loss alone: 33 us = 1.8 TB/s; 37 rows of 1024: 13 us, four
-//             dependent launches of 2 to 5 us.
+//             exponentials an element.  1024 x 151936 bf16 with K = 200: 199 us = 3.1 TB/s, K = 1024: 284; 37 rows of 1024:
+//             13 us, four dependent launches of 2 to 5 us.
 
 #include <float.h>
 #include <stddef.h>
@@ -481,7 +485,10 @@ distill_prep_kernel(const DistillArgs a) {
 // took every CTA's parts of row i - 2, which were sent after the factors of row i - 4 were made: the slot of row i - 4 is free.
 // PW: consumer warps, 8 where two CTAs share an SM, 16 where one has it alone.
 constexpr int kStages = 3, kRing = 4;
-constexpr int kPipeK = 128;                   // entries of a list: four a lane
+// Entries of a list: four a lane.  Pipeline against the other kernel at K = 128: 1024 rows of 151936 bf16 182 : 195 us, 2048 of
+// 32000 88 : 98, 512 fp32 rows of 151936 142 : 188.  With room for 256 (eight a lane) K = 129 took 200 : 196, 95 : 97 and 144 : 187 us,
+// K = 256 202 : 201, 126 : 101 and 150 : 190, and K = 64, which every list would pay, 166 instead of 153 (bf16, 1024 rows).
+constexpr int kPipeK = 128;
 
 struct PipePart {                             // of one consumer warp
     double s;

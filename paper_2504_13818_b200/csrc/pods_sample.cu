@@ -13,12 +13,14 @@
 //            exponential.  After this one cluster barrier every warp knows all parts in id order.
 //   no filter  the warp whose part holds the drawn point takes the lane from the lane sums that it kept, and evaluates that
 //            lane's few vectors again; every other warp goes on to the next row.
-//   filters  every warp also finds the r-th largest of its lanes' maxima; the least of these over the cluster is a value that
-//            at least `want` logits reach, so the logits reaching it contain the first `want` of the order.  They are listed
-//            (in the typical row a few hundred), the cluster's first CTA sorts them, and the rest is fp64 arithmetic on the list.
-//   wide nucleus  where the list does not reach far enough, a histogram of the row's mass over 1024 stretches of logit
-//            brackets the border within a few stretches; one fp64 sweep takes the sums above the bracket and lists what lies in
-//            it, and the list settles the border.
+//   filters  one warp of each CTA also finds the r-th largest of the CTA's lanes' maxima; the least of these over the cluster is
+//            a value that at least `want` logits reach, so the logits reaching it contain the first `want` of the order.  They are
+//            listed (in the typical row a few hundred), every CTA ranks its own among all of them into the first CTA's list, and
+//            the rest is fp64 arithmetic on that list.
+//   wide nucleus  where the list does not reach far enough, or the lanes' maxima hold so little of the row's mass that it cannot
+//            (then it is not made), a histogram of the row's mass over kBins stretches of logit brackets the border within a few
+//            stretches; one sweep takes the sums above the bracket and lists what lies in it, and the list settles the border.
+//            The sweep is fast at first, and in fp64 where the border is too close to call.
 //   the rest  (a bracket full of ties, a top_k above the list) bisects the order-preserving keys of the values with counts and
 //            fp64 sums over the resident row.
 //
@@ -31,9 +33,13 @@
 //            rest waits of one row for its slowest part), then 5 % of these flat rows in fp64, 16 to 28 us
 //   512 rows, nuclei of thousands   427 us: 82 K cycles a row, of which the histogram's shared-memory atomics 22 K, the bracket
 //            sweep 14 K, ranking and border 16 K, first sweep and load 10 K, about ten cluster barriers the rest
-//   64 fp32 rows with settings of their own   43 us; one row, top_k and top_p   19 us: a chain of cluster barriers, rankings
-//            and fp64 exponentials, not bandwidth
+//   512 rows, top_k 50 and top_p 0.95   139 us: the chain of one row, with its load ahead of it and nothing to overlap them
+//   512 rows of 32000, top_k 300   249 to 290 us, 700   294 us: the lanes' maxima bound so many ids that the list overflows, and
+//            the threshold is bisected with a sweep and a cluster barrier for each bit of the key
+//   one row, top_k and top_p   19 us: a chain of cluster barriers, rankings and fp64 exponentials, not bandwidth; 64 fp32 rows
+//            with settings of their own   43 us: two such chains, as clusters of eight hold only about 33 rows at a time
 //   pods_topk, 1024 rows, K = 64   179 us = 1.7 TB/s; 16 fp32 rows of 32000, K = 20   12 us: the same chain, fewer steps
+//   33554 rows of 1000, no filter   419 us = 0.16 TB/s: a CTA and its barriers for 2 KB
 
 #include <float.h>
 #include <stddef.h>
@@ -1728,8 +1734,10 @@ int launch_rows(SampleArgs& a, int esize, int cl, size_t room, cudaStream_t stre
 
 // The pipeline where there are rows enough for it; sets `marked` if it ran.  Measured, pipeline (its three launches) against the
 // kernel for few rows, bf16: 27.0 : 22.9 us at 16 MB of logits of 151936, 30.9 : 37.0 at 32 MB, 41.2 : 45.3 at 64 MB, 71.3 : 78.2
-// at 128 MB; V = 32000 34.0 : 35.0 at 32 MB, 45.5 : 47.3 at 64 MB; V = 1000 213 : 209 at 32 MB, 394 : 409 at 64 MB.  (The marks' numbers
-// fit 32 bits with kMarked for the rows that are admitted.)
+// at 128 MB; V = 32000 34.0 : 35.0 at 32 MB, 45.5 : 47.3 at 64 MB; V = 1000 213 : 209 at 32 MB, 394 : 409 at 64 MB.  One limit for all
+// V, where none loses: long rows would gain from 32 MB on.  Rows with a mask or temperatures of their own do not come here: 512
+// rows of 151936 102 us by the kernel for few rows against 71, half of them masked 56; V = 32000, 2048 rows 77 against 74, 512
+// rows 29 both.  (The marks' numbers fit 32 bits with kMarked for the rows that are admitted.)
 constexpr int64_t kPipelineMinBytes = 64 << 20;
 template <int DT>
 int launch_policy(SampleArgs& a, int esize, cudaStream_t stream) {
