@@ -334,7 +334,8 @@ size_t pods_distill_chunk_workspace_bytes(int64_t T);
  *   dlogits[t,v] = g_t ((Q + r) p_v - sum over the j with id_j == v of q_j)      listed v
  *                = g_t ((Q + r) p_v - r p_v / (1 - s))                           every other v
  * rounded to dtype (nearest even; bf16 entries outside the list may be the product of an exponential that was itself rounded to
- * bf16, as in grpo_loss_chunk: the same rows may differ by that rounding between chunks of other sizes, K or alignments), and sum_t mask_t w_i kl_t is ADDED to *loss_acc (the caller zeroes it; fixed order).
+ * bf16, as in grpo_loss_chunk: the same rows may differ by that rounding between chunks of other sizes, K or alignments), and
+ * sum_t mask_t w_i kl_t is ADDED to *loss_acc (the caller zeroes it; fixed order).
  * 1 - s is summed over the ids outside the list, never taken as a difference.  Where they have no mass at all (every such
  * logit -inf, or none left) the rest's term is left out: r = 0.  A term with q_j = 0 is 0.  A listed id that the policy
  * cannot produce (logit -inf, q_j > 0) makes kl_t +inf with a finite gradient.
