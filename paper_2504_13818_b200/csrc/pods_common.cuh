@@ -19,6 +19,10 @@ static inline cudaStream_t pods_stream(void* s) { return reinterpret_cast<cudaSt
 static inline bool pods_aligned(const void* p, size_t a) {
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }
+template <typename... P>
+static inline bool pods_all_aligned(size_t a, const P*... p) {
+    return (pods_aligned(p, a) && ...);
+}
 
 // Number of SMs of the current device (148 on B200); queried per call, it is cheap.
 static inline int pods_sm_count() {

@@ -1029,7 +1029,9 @@ extern "C" int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype
     if (logits == nullptr || ids == nullptr || values == nullptr || seq_weight == nullptr || cu_seqlens == nullptr ||
         loss_acc == nullptr || kl == nullptr)
         return PODS_ERR_INVALID_ARG;
-    if (!pods_aligned(logits, esize) || !pods_aligned(loss_acc, 8)) return PODS_ERR_INVALID_ARG;
+    if (!pods_aligned(logits, esize) || !pods_all_aligned(8, loss_acc, seq_weight, cu_seqlens) ||
+        !pods_all_aligned(4, ids, values, teacher_lse, kl, status))
+        return PODS_ERR_INVALID_ARG;
     if (workspace == nullptr || workspace_bytes < pods_distill_chunk_workspace_bytes(T) || !pods_aligned(workspace, 16))
         return PODS_ERR_WORKSPACE;
     DistillArgs a = {};

@@ -1783,6 +1783,7 @@ extern "C" int pods_sample(const void* logits, int64_t ldl, int32_t dtype, int64
     if (!min_p_row && !(min_p == min_p)) return PODS_ERR_INVALID_ARG;
     if (T == 0) return PODS_OK;
     if (logits == nullptr || u == nullptr || tokens == nullptr) return PODS_ERR_INVALID_ARG;
+    if (!pods_all_aligned(4, u, temperature_row, top_k_row, top_p_row, min_p_row, tokens, logp, logq, status)) return PODS_ERR_INVALID_ARG;
     SampleArgs a = {};
     a.logits = logits;
     a.ldl = ldl;
@@ -1841,6 +1842,7 @@ extern "C" int pods_topk(const void* logits, int64_t ldl, int32_t dtype, int64_t
     if (K > PODS_MAX_TOPK) return PODS_ERR_UNSUPPORTED;
     if (T == 0) return PODS_OK;
     if (logits == nullptr || ids == nullptr || values == nullptr) return PODS_ERR_INVALID_ARG;
+    if (!pods_all_aligned(4, ids, values, lse, status)) return PODS_ERR_INVALID_ARG;
     SampleArgs a = {};
     a.logits = logits;
     a.ldl = ldl;

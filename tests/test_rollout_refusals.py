@@ -100,3 +100,25 @@ def test_the_binding_checks_shapes_types_and_devices():
             binding.pods_distill_chunk(**args(**bad))
     with pytest.raises(binding.PodsError, match="CUDA"):
         binding.pods_distill_chunk(**args())
+
+
+def test_misaligned_pointers_are_refused():
+    """Every array, off its element's boundary by half an element or a byte: refused on the host, nothing is launched."""
+    lib = binding.load()
+    off = {1: None, 4: [C.c_void_p(256 + d) for d in (1, 2, 3)], 8: [C.c_void_p(256 + d) for d in (1, 4)]}
+
+    def refused(call, good, arrays):
+        for at, size in arrays.items():
+            for bad in off[size]:
+                args = list(good)
+                args[at] = bad
+                assert call(*args) == 1, (at, bad)
+
+    #            logits ldl dt T  V    u     tau_row tau  k_row k  p_row p    m_row m    mask  tokens logp logq status stream
+    refused(lib.pods_sample, (fake, 100, 2, 4, 100, fake, fake, 1.0, fake, 0, fake, 1.0, fake, 0.0, None, fake, fake, fake, fake, None),
+            {0: 4, 5: 4, 6: 4, 8: 4, 10: 4, 12: 4, 15: 4, 16: 4, 17: 4, 18: 4})
+    #          logits ldl dt T  V    K  tau  mask  ids   values lse status stream
+    refused(lib.pods_topk, (fake, 100, 2, 4, 100, 5, 1.0, None, fake, fake, fake, fake, None), {0: 4, 8: 4, 9: 4, 10: 4, 11: 4})
+    #                   logits ldl dt ids  values ldk K lse  weight  cu   M  row0 mask T  V   tau flags scale loss kl  dlogits ldd ws bytes status stream
+    refused(lib.pods_distill_chunk, (fake, 100, 2, fake, fake, 8, 8, fake, fake, fake, 1, 0, None, 4, 100, 1.0, 0, 1.0, fake, fake, C.c_void_p(4096), 100,
+                                     fake, 1 << 16, fake, None), {0: 4, 3: 4, 4: 4, 7: 4, 8: 8, 9: 8, 18: 8, 19: 4, 20: 4, 24: 4})
