@@ -432,3 +432,59 @@ def test_several_rows_a_cluster_without_the_pipeline(dtype, T, V, K, pad, offset
     again = run(b, tau=1.4, rest=True, expect_status=bits)
     assert np.array_equal(again["kl"], got["kl"], equal_nan=True)
     assert bool(((again["dl"] == got["dl"]) | (torch.isnan(again["dl"]) & torch.isnan(got["dl"]))).all())
+
+
+def test_pipelines_side_by_side_and_in_a_captured_graph():
+    """Sampling and distillation at sizes that take their pipelines, on two streams at once and replayed on new inputs: the bits of
+    the calls alone."""
+    T, V, K = 520, 70001, 40
+    b = make(T, V, K, "bf16", seed=21, M=6)
+    u = torch.rand(T, generator=torch.Generator().manual_seed(3)).cuda()
+    L = torch.logsumexp(b["teacher"].double(), 1).float().cuda()
+    weight = binding.grpo_seq_weights(b["mask"], b["cu"])
+    ws = [torch.empty(binding.pods_distill_chunk_workspace_bytes(T), dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def outputs():
+        return dict(tokens=torch.zeros(T, dtype=torch.int32, device="cuda"), logp=torch.zeros(T, device="cuda"), kl=torch.zeros(T, device="cuda"),
+                    dl=torch.zeros((T, V), dtype=torch.bfloat16, device="cuda"), acc=torch.zeros(1, dtype=torch.float64, device="cuda"))
+
+    def sample(o):
+        binding.pods_sample(b["z"], u, tokens=o["tokens"], logp=o["logp"])
+
+    def distill(o, w):
+        o["acc"].zero_()
+        binding.pods_distill_chunk(b["z"], b["ids"], b["values"], L, weight, b["cu"], 0, b["mask"], o["acc"], kl=o["kl"], dlogits=o["dl"],
+                                   workspace=w, rest=True)
+
+    def alone():
+        o = outputs()
+        sample(o)
+        distill(o, ws[0])
+        torch.cuda.synchronize()
+        return o
+
+    want = alone()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [outputs() for _ in streams]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                (sample(got[k]), distill(got[k], ws[k])) if k == 0 else (distill(got[k], ws[k]), sample(got[k]))
+    torch.cuda.synchronize()
+    for o in got:
+        assert all(torch.equal(o[n], want[n]) for n in want)
+    graph = torch.cuda.CUDAGraph()
+    o = outputs()
+    with torch.cuda.graph(graph):
+        sample(o)
+        distill(o, ws[1])
+    for seed in (22, 23):
+        b["z"].copy_(make(T, V, K, "bf16", seed=seed)["z"])
+        u.copy_(torch.rand(T, generator=torch.Generator().manual_seed(seed)))
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = alone()
+        assert all(torch.equal(o[n], want[n]) for n in want)
