@@ -53,8 +53,10 @@ typedef enum {
 #define PODS_STATUS_NONFINITE_LOGIT  0x80u /* a row of logits held NaN or +inf                             */
 #define PODS_STATUS_EMPTY_ROW        0x100u /* every logit of a row was -inf                                */
 #define PODS_STATUS_PARAM_RANGE      0x200u /* pods_sample: a setting or random number of a row was out of range */
+#define PODS_STATUS_NONFINITE_GRAD   0x400u /* a gradient norm was NaN or infinite; pods_adamw left everything as it was */
 #define PODS_STATUS_INDEX_RANGE      0x20u /* pods_compact: an entry of idx was outside [0,n); rollout 0 of the
-                                              group was used instead                                        */
+                                              group was used instead.  pods_preference: an id of a pair was
+                                              neither -1 nor in [0,M); the pair was left out                */
 
 /* Down-sampling rules D(o, r; m) of Section 3.2 / 3.3. */
 typedef enum {
@@ -79,6 +81,16 @@ typedef enum {
 #define PODS_MAX_TOPK 1024         /* longest list of pods_topk and pods_distill_chunk */
 
 #define PODS_DISTILL_REST 0x1u     /* pods_distill_chunk: add the term of the mass outside the list */
+
+/* Losses of a pair with margin h (pods_preference). */
+typedef enum {
+    PODS_PREFERENCE_SIGMOID = 0,   /* -(1 - s) log sigma(h) - s log sigma(-h), s the label smoothing */
+    PODS_PREFERENCE_HINGE = 1,     /* max(0, 1 - h)                                                  */
+    PODS_PREFERENCE_SQUARED = 2    /* ((h - 1/2) / beta)^2                                           */
+} pods_preference_kind;
+#define PODS_PREFERENCE_AVERAGE 0x1u /* scores are means over a rollout's tokens instead of sums */
+
+#define PODS_ADAMW_STOCHASTIC 0x1u /* bf16 parameters are rounded with random bits instead of to the nearest */
 
 #define PODS_MAX_N 1024            /* largest supported group size n */
 
@@ -357,6 +369,134 @@ int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype, const int
                        const int64_t* cu_seqlens, int64_t M, int64_t row0, const uint8_t* mask, int64_t T, int32_t V,
                        float temperature, uint32_t flags, float grad_scale, double* loss_acc, float* kl, void* dlogits,
                        int64_t ldd, void* workspace, size_t workspace_bytes, uint32_t* status, void* stream);
+
+/*
+ * pods_logp_chunk - log-probability of each row's token, from stored logits: what an objective on log-probabilities starts
+ * from (pods_preference, or the caller's own; old_logp and ref_logp of grpo_loss_chunk where the logits are at hand), with
+ * y_v = z_v / temperature:
+ *   lse[t] = log sum_v exp(y_v)    logp[t] = y[token] - lse    entropy[t] = lse - sum_v p_v y_v,  p = exp(y - lse)
+ *   logits [dev] [T, V] of dtype, row pitch ldl elements, any alignment of the element type
+ *   tokens [dev] int32 [T] (an id outside [0,V) raises PODS_STATUS_TOKEN_RANGE and is read as 0)
+ *   mask   [dev] uint8 [T] or NULL: rows with mask 0 are not read and their outputs are left as they were
+ *   logp   [dev] fp32 [T]    lse [dev] fp64 [T] or NULL (64 bits, so that pods_logp_grad_chunk loses nothing on logits far from
+ *          0; sums themselves are to fp32's precision)    entropy [dev] fp32 [T] or NULL
+ * -inf marks an id without probability.  A row with NaN or +inf gets NaN throughout (PODS_STATUS_NONFINITE_LOGIT), one of -inf
+ * alone lse -inf and NaN otherwise (PODS_STATUS_EMPTY_ROW).  temperature: finite, at least FLT_MIN.  V above PODS_MAX_ROW_V, T
+ * above 2^24 or an unknown dtype returns PODS_ERR_UNSUPPORTED.  No workspace.
+ */
+int pods_logp_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* tokens, const uint8_t* mask, int64_t T,
+                    int32_t V, float temperature, float* logp, double* lse, float* entropy, uint32_t* status, void* stream);
+
+/*
+ * pods_logp_grad_chunk - the gradient of any objective on pods_logp_chunk's outputs, carried back to the logits:
+ *   dlogits[t,v] = (dlogp_t ([v == token] - p_v) - dentropy_t p_v (log p_v + entropy_t)) / temperature   rounded to dtype
+ *   lse, entropy: as pods_logp_chunk left them (entropy is needed with dentropy only)
+ *   dlogp [dev] fp32 [T]    dentropy [dev] fp32 [T] or NULL
+ *   dlogits [dev] [T, V] of dtype, pitch ldd; may be the same buffer as logits (in place, ldd == ldl), must not overlap it
+ *           otherwise.  Rows whose dlogp and dentropy are 0 are zero, and what their logits hold is of no consequence.
+ * Other arguments and refusals as in pods_logp_chunk.
+ */
+int pods_logp_grad_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* tokens, const double* lse,
+                         const float* dlogp, const float* entropy, const float* dentropy, int64_t T, int32_t V,
+                         float temperature, void* dlogits, int64_t ldd, uint32_t* status, void* stream);
+
+/* Bytes of workspace pods_preference needs for M rollouts and P pairs. */
+size_t pods_preference_workspace_bytes(int64_t M, int64_t P);
+
+/*
+ * pods_preference - losses of pairs (better, worse) of the packed rollouts, and their derivative in every token's
+ * log-probability: the companion of grpo_loss_chunk where a policy is trained on which of two rollouts has the higher reward
+ * rather than on advantages.  (The paper has no counterpart.)  With |o_i| the tokens of rollout i whose mask is not 0:
+ *   s_i = sum_t mask_t (logp_t - ref_logp_t)           divided by |o_i| with PODS_PREFERENCE_AVERAGE; 0 for an empty rollout
+ *   h_p = beta (s_c - s_r) - margin_p                  (c, r) the pair's rollouts; loss_p(h) by kind, see pods_preference_kind
+ *   l_p = loss_p(h_p) + nll (1 / |o_c|) sum_t mask_t (-logp_t)                                       t of rollout c
+ * sum_p w_p l_p is ADDED to *loss_acc, w_p = pair_weight[p] or 1 / the number of pairs in use, and
+ *   dlogp[t] = grad_scale mask_t d(sum_p w_p l_p) / d logp_t        (0 for rows that belong to no rollout)
+ * A rollout may stand in any number of pairs.  A pair with an id of -1 is unused, one with another id outside [0,M) raises
+ * PODS_STATUS_INDEX_RANGE and is unused too: its pair_loss is 0.  A pair of weight 0 leaves nothing in the loss or in dlogp.  A
+ * log-probability of -inf makes scores and losses infinite or NaN as the formulas do; masked ones are not read.
+ *   logp, ref_logp (NULL: 0), mask (NULL: ones), dlogp: [dev] arrays of T (fp32, fp32, uint8, fp32 out)
+ *   cu_seqlens [dev] int64 [M+1]    pairs [dev] int32 [P,2]    pair_weight [dev] fp32 [P] or NULL
+ *   margin_pair [dev] fp32 [P], or NULL: margin holds for every pair    label_smoothing in [0, 1/2), sigmoid only
+ *   beta > 0, nll >= 0    reward [dev] fp32 [M] or NULL: beta s_i    pair_loss [dev] fp32 [P] or NULL: l_p
+ *   loss_acc [dev] fp64 scalar    workspace [dev] of pods_preference_workspace_bytes(M, P), 16-byte aligned
+ * Sums are fp64 in a fixed order.  An unknown kind or flag returns PODS_ERR_UNSUPPORTED.
+ */
+int pods_preference(const float* logp, const float* ref_logp, const uint8_t* mask, const int64_t* cu_seqlens, int64_t M,
+                    int64_t T, const int32_t* pairs, const float* pair_weight, int64_t P, int32_t kind, uint32_t flags,
+                    float beta, float label_smoothing, const float* margin_pair, float margin, float nll, float grad_scale,
+                    double* loss_acc, float* dlogp, float* reward, float* pair_loss, void* workspace, size_t workspace_bytes,
+                    uint32_t* status, void* stream);
+
+/* Bytes of workspace pods_preference_fwd_bwd needs. */
+size_t pods_preference_fwd_bwd_workspace_bytes(int64_t T, int64_t M, int64_t P);
+
+/*
+ * pods_preference_fwd_bwd - pods_logp_chunk, pods_preference and pods_logp_grad_chunk over a whole packed batch whose logits are
+ * at hand: loss [dev] fp32 scalar (written), logp [dev] fp32 [T] (0 where the mask is 0 and behind the last rollout), dlogits,
+ * reward, pair_loss.  Rows that weigh nothing (masked, behind the last rollout, of rollouts in no pair) get a zero gradient row.
+ * For logits that do not all exist at one time, make the three calls, the first and the last chunk by chunk.
+ */
+int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t dtype, const int32_t* tokens, const float* ref_logp,
+                            const uint8_t* mask, const int64_t* cu_seqlens, int64_t M, int64_t T, int32_t V,
+                            float temperature, const int32_t* pairs, const float* pair_weight, int64_t P, int32_t kind,
+                            uint32_t flags, float beta, float label_smoothing, const float* margin_pair, float margin,
+                            float nll, float grad_scale, float* loss, float* logp, void* dlogits, int64_t ldd, float* reward,
+                            float* pair_loss, void* workspace, size_t workspace_bytes, uint32_t* status, void* stream);
+
+/*
+ * One tensor of pods_grad_norm and pods_adamw.  The array of them is in HOST memory and is read during the call only; every
+ * pointer in it is [dev].  Tensors are dense; n elements, each pointer aligned to its element type (vectors are used where all of
+ * a tensor's pointers lie on four elements' boundaries).  No two may overlap.
+ *   state_bits 32: m, v fp32 [n], the first moment and the second.
+ *   state_bits 8:  m, v uint8 [n], e4m3 numbers; m_scale, v_scale uint8 [(n + 31) / 32], the exponent k of each block of 32
+ *                  elements: an element is its number times 2^(k - 127).  v holds the ROOT of the second moment.  All bytes 0 is
+ *                  the state before the first step.
+ *   copy: a copy of the parameter, written in copy_type (round to nearest of the fp32 result), or NULL.
+ */
+typedef struct {
+    void* param;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+    void* copy;
+    int64_t n;
+    int32_t param_type, grad_type, copy_type; /* pods_dtype */
+    int32_t state_bits;
+    float weight_decay, lr_scale;             /* of this tensor */
+} pods_adamw_tensor;
+
+/* Bytes of workspace pods_grad_norm needs for n tensors. */
+size_t pods_grad_norm_workspace_bytes(int32_t n);
+
+/*
+ * pods_grad_norm - norm [dev] fp32 scalar = |scale| sqrt(sum over all tensors of their squared gradients) (fp64 beyond a few
+ * terms, fixed order).  Reads grad, n and grad_type of each entry.  A norm that is NaN or infinite raises
+ * PODS_STATUS_NONFINITE_GRAD.  workspace [dev], 8-byte aligned.
+ */
+int pods_grad_norm(const pods_adamw_tensor* tensors /*host*/, int32_t n, float scale, float* norm, void* workspace,
+                   size_t workspace_bytes, uint32_t* status, void* stream);
+
+/*
+ * pods_adamw - step number `step` (1, 2, ...) of Adam with decoupled weight decay on all tensors at once: what takes the
+ * gradient of the objective (dW of grpo_loss_from_hidden, or a backward pass that consumed dlogits) to the weights.  (The paper
+ * names the optimiser only.)  Per element, all in fp32:
+ *   g = grad grad_scale min(1, max_norm / norm)          (the last factor where max_norm > 0)
+ *   m = beta1 m + (1 - beta1) g      v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - lr_t weight_decay) - lr_t / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),  lr_t = lr lr_scale
+ * then rounded to param_type: to the nearest, or, bf16 with PODS_ADAMW_STOCHASTIC, up or down with the probability that keeps the
+ * average (so that steps far below half a unit of the parameter are not lost).  8-bit states are rounded so in any case.  The
+ * random bits are a function of seed, step and the element's number among all tensors (each tensor begins at a multiple of 32).
+ *   step_dev [dev] int64, lr_dev [dev] fp32, or NULL: read on the device instead of step and lr, for captured graphs
+ *   norm [dev] fp32 or NULL, as pods_grad_norm left it with the same scale.  A norm that is NaN or infinite leaves every tensor
+ *          as it was and raises PODS_STATUS_NONFINITE_GRAD.
+ * Betas in [0, 1), eps >= 0.  A gradient that is no number makes its element no number, and its block's 8-bit states.
+ */
+int pods_adamw(const pods_adamw_tensor* tensors /*host*/, int32_t n, int64_t step, const int64_t* step_dev, float lr,
+               const float* lr_dev, float beta1, float beta2, float eps, float grad_scale, const float* norm, float max_norm,
+               uint32_t flags, uint64_t seed, uint32_t* status, void* stream);
 
 /*
  * pods_set_loss_from_hidden_panel_bytes - tuning knob (the paper has no counterpart): the most bytes of workspace

@@ -19,11 +19,14 @@ RULE_MAXVAR, RULE_MAXREWARD, RULE_RANDOM, RULE_PERCENTILE = 0, 1, 2, 3
 FLAG_ADV_BEFORE, FLAG_STD_SAMPLE, FLAG_EXACT_TIES = 1, 2, 4
 STATUS_NONFINITE_REWARD, STATUS_TOKEN_RANGE, STATUS_CAPACITY, STATUS_NEG_LENGTH, STATUS_TIMEOUT = 1, 2, 4, 8, 16
 STATUS_INDEX_RANGE, STATUS_INTERNAL = 32, 64
-STATUS_NONFINITE_LOGIT, STATUS_EMPTY_ROW, STATUS_PARAM_RANGE = 128, 256, 512
+STATUS_NONFINITE_LOGIT, STATUS_EMPTY_ROW, STATUS_PARAM_RANGE, STATUS_NONFINITE_GRAD = 128, 256, 512, 1024
 MAX_N = 1024
 MAX_ROW_V, MAX_TOPK = 524288, 1024
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 DISTILL_REST = 1
+PREFERENCE_KINDS = {"sigmoid": 0, "hinge": 1, "squared": 2}
+PREFERENCE_AVERAGE = 1
+ADAMW_STOCHASTIC = 1
 
 # name -> (restype, argtypes); mirrors include/pods.h
 _p, _i64, _i32, _u64, _u32, _f32, _sz = (C.c_void_p, C.c_int64, C.c_int32, C.c_uint64, C.c_uint32,
@@ -57,6 +60,17 @@ SIGNATURES = {
     "pods_distill_chunk_workspace_bytes": (_sz, [_i64]),
     "pods_distill_chunk": (C.c_int, [_p, _i64, _i32, _p, _p, _i64, _i32, _p, _p, _p, _i64, _i64, _p, _i64, _i32, _f32,
                                      _u32, _f32, _p, _p, _p, _i64, _p, _sz, _p, _p]),
+    "pods_logp_chunk": (C.c_int, [_p, _i64, _i32, _p, _p, _i64, _i32, _f32, _p, _p, _p, _p, _p]),
+    "pods_logp_grad_chunk": (C.c_int, [_p, _i64, _i32, _p, _p, _p, _p, _p, _i64, _i32, _f32, _p, _i64, _p, _p]),
+    "pods_preference_workspace_bytes": (_sz, [_i64, _i64]),
+    "pods_preference": (C.c_int, [_p, _p, _p, _p, _i64, _i64, _p, _p, _i64, _i32, _u32, _f32, _f32, _p, _f32, _f32, _f32,
+                                  _p, _p, _p, _p, _p, _sz, _p, _p]),
+    "pods_preference_fwd_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "pods_preference_fwd_bwd": (C.c_int, [_p, _i64, _i32, _p, _p, _p, _p, _i64, _i64, _i32, _f32, _p, _p, _i64, _i32, _u32,
+                                          _f32, _f32, _p, _f32, _f32, _f32, _p, _p, _p, _i64, _p, _p, _p, _sz, _p, _p]),
+    "pods_grad_norm_workspace_bytes": (_sz, [_i32]),
+    "pods_grad_norm": (C.c_int, [_p, _i32, _f32, _p, _p, _sz, _p, _p]),
+    "pods_adamw": (C.c_int, [_p, _i32, _i64, _p, _f32, _p, _f32, _f32, _f32, _f32, _p, _f32, _u32, _u64, _p, _p]),
     "pods_selftest_bounded_wait": (C.c_int, [_u32, _p, _p]),
     "pods_set_loss_cluster_min_vocab": (_i32, [_i32]),
     "pods_host_step_create": (C.c_int, [_i64, _i32, _i32, _i64, _i64, _i32, _i64, _p]),
@@ -711,3 +725,291 @@ class HostStep:
             self.close()
         except Exception:
             pass
+
+
+def _token_rows(logits, tokens):
+    """Checks shared by the calls on stored logits and their tokens -> (T, V, address, pitch, dtype code, current device)."""
+    _require(isinstance(logits, torch.Tensor) and logits.dim() == 2, "logits must be [T,V]")
+    T, V = logits.shape
+    if V < 1:
+        raise PodsError("logits must have at least one column")
+    _numel(tokens, T, "tokens")
+    lp, ldl, dtype = _typed_rows(logits, "logits")
+    here = _here()
+    _same_device(logits, "logits", here)
+    return T, V, lp, ldl, dtype, here
+
+
+def _gradient_rows(logits, dlogits, ldl, here):
+    """dlogits (made here if None) -> (tensor, address, pitch)."""
+    if dlogits is None:
+        T, V = logits.shape
+        dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        return dlogits, dlogits.data_ptr(), V
+    if not (isinstance(dlogits, torch.Tensor) and dlogits.shape == logits.shape and dlogits.dtype == logits.dtype):
+        raise PodsError("dlogits must have the shape and dtype of logits")
+    dp, ldd, _ = _typed_rows(dlogits, "dlogits")
+    _same_device(dlogits, "dlogits", here)
+    _require(dp != logits.data_ptr() or ldd == ldl or logits.shape[0] <= 1, "dlogits in place needs the row pitch of logits")
+    return dlogits, dp, ldl if dp == logits.data_ptr() else ldd
+
+
+def pods_logp_chunk(logits, tokens, temperature=1.0, mask=None, logp=None, lse=None, entropy=None, want_lse=False,
+                    want_entropy=False, status=None):
+    """Log-probability of each row's token under softmax(logits / temperature): logits [T,V] (bf16, fp16 or fp32), tokens [T]
+    int32 -> (logp [T] fp32, lse [T] fp64 or None, entropy [T] fp32 or None).
+
+    pods_logp_grad_chunk takes lse (and entropy) back.  Rows with mask 0 are left alone: pass the outputs then (those made
+    here start as 0)."""
+    T, V, lp, ldl, dtype, here = _token_rows(logits, tokens)
+    dev = logits.device
+    new = torch.empty if mask is None else torch.zeros
+    if logp is None:
+        logp = new(T, dtype=torch.float32, device=dev)
+    if lse is None and want_lse:
+        lse = new(T, dtype=torch.float64, device=dev)
+    if entropy is None and want_entropy:
+        entropy = new(T, dtype=torch.float32, device=dev)
+    f32 = torch.float32
+    rc = load().pods_logp_chunk(lp, ldl, dtype, _vec(tokens, torch.int32, T, "tokens", here), _vec(mask, torch.uint8, T, "mask", here, True),
+                                T, V, temperature, _vec(logp, f32, T, "logp", here), _vec(lse, torch.float64, T, "lse", here, True),
+                                _vec(entropy, f32, T, "entropy", here, True), _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_logp_chunk")
+    return logp, lse, entropy
+
+
+def pods_logp_grad_chunk(logits, tokens, lse, dlogp, entropy=None, dentropy=None, temperature=1.0, dlogits=None, status=None):
+    """Gradient of an objective on pods_logp_chunk's outputs with respect to the logits: dlogp [T] fp32 and, for entropy
+    terms, entropy and dentropy [T] fp32 -> dlogits like logits (``dlogits`` may be ``logits`` itself)."""
+    T, V, lp, ldl, dtype, here = _token_rows(logits, tokens)
+    _require(dentropy is None or entropy is not None, "dentropy needs entropy")
+    f32 = torch.float32
+    lse_p, dlogp_p = _vec(lse, torch.float64, T, "lse", here), _vec(dlogp, f32, T, "dlogp", here)
+    entropy_p, dentropy_p = _vec(entropy, f32, T, "entropy", here, True), _vec(dentropy, f32, T, "dentropy", here, True)
+    dlogits, dp, ldd = _gradient_rows(logits, dlogits, ldl, here)
+    rc = load().pods_logp_grad_chunk(lp, ldl, dtype, _vec(tokens, torch.int32, T, "tokens", here), lse_p, dlogp_p, entropy_p, dentropy_p,
+                                     T, V, temperature, dp, ldd, _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_logp_grad_chunk")
+    return dlogits
+
+
+def _pair_args(ref_logp, mask, cu_seqlens, pairs, kind, margin, pair_weight, T, here):
+    """Checks shared by the calls on pairs -> (M, P, kind code, margins' address, scalar margin, other addresses)."""
+    M = cu_seqlens.numel() - 1
+    _require(M >= 1, "cu_seqlens must hold M+1 >= 2 entries")
+    if not (isinstance(pairs, torch.Tensor) and pairs.dim() == 2 and pairs.shape[1] == 2):
+        raise PodsError("pairs must be [P,2]")
+    P = pairs.shape[0]
+    code = PREFERENCE_KINDS.get(kind)
+    if code is None:
+        raise PodsError("kind must be one of %s, got %r" % (", ".join(PREFERENCE_KINDS), kind))
+    margin_t, margin = _setting(margin, P, "margin")
+    f32 = torch.float32
+    return (M, P, code, _vec(margin_t, f32, P, "margin", here, True), margin, _vec(ref_logp, f32, T, "ref_logp", here, True),
+            _vec(mask, torch.uint8, T, "mask", here, True), _vec(cu_seqlens, torch.int64, M + 1, "cu_seqlens", here),
+            _vec(pairs, torch.int32, 2 * P, "pairs", here), _vec(pair_weight, f32, P, "pair_weight", here, True))
+
+
+def _scratch(workspace, need, dev):
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    _require(workspace.numel() >= need, "workspace must hold %d bytes, got %d" % (need, workspace.numel()))
+    return workspace
+
+
+def pods_preference(logp, ref_logp, mask, cu_seqlens, pairs, beta, loss_acc, kind="sigmoid", label_smoothing=0.0, margin=0.0,
+                    pair_weight=None, average=False, nll=0.0, grad_scale=1.0, dlogp=None, reward=None, pair_loss=None,
+                    workspace=None, status=None):
+    """Losses of pairs (better, worse) of rollouts, pairs [P,2] int32, from the packed tokens' log-probabilities [T] fp32, with
+    the derivative in every one of them.
+
+    kind: "sigmoid", "hinge" or "squared"; margin: a number or a tensor [P]; average: scores are means over tokens; nll:
+    weight of the better rollout's mean negative log-probability.  loss_acc [1] fp64 accumulates.  Returns (dlogp [T],
+    reward [M] = beta times the scores, pair_loss [P]), fp32; missing ones and the workspace are allocated here."""
+    _require(isinstance(logp, torch.Tensor) and logp.dim() == 1, "logp must be [T]")
+    T, dev, here, f32 = logp.numel(), logp.device, _here(), torch.float32
+    logp_p = _vec(logp, f32, T, "logp", here)
+    M, P, code, margin_p, margin_all, ref_p, mask_p, cu_p, pairs_p, weight_p = _pair_args(ref_logp, mask, cu_seqlens, pairs, kind, margin,
+                                                                                      pair_weight, T, here)
+    if dlogp is None:
+        dlogp = torch.empty(T, dtype=f32, device=dev)
+    if reward is None:
+        reward = torch.empty(M, dtype=f32, device=dev)
+    if pair_loss is None:
+        pair_loss = torch.empty(P, dtype=f32, device=dev)
+    lib = load()
+    workspace = _scratch(workspace, lib.pods_preference_workspace_bytes(M, P), dev)
+    rc = lib.pods_preference(logp_p, ref_p, mask_p, cu_p, M, T, pairs_p, weight_p, P, code, PREFERENCE_AVERAGE if average else 0, beta,
+                             label_smoothing, margin_p, margin_all, nll, grad_scale, _vec(loss_acc, torch.float64, 1, "loss_acc", here),
+                             _vec(dlogp, f32, T, "dlogp", here), _vec(reward, f32, M, "reward", here),
+                             _vec(pair_loss, f32, P, "pair_loss", here),
+                             _vec(workspace, torch.uint8, workspace.numel(), "workspace", here), workspace.numel(),
+                             _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_preference")
+    return dlogp, reward, pair_loss
+
+
+def pods_preference_fwd_bwd(logits, tokens, ref_logp, mask, cu_seqlens, pairs, beta, kind="sigmoid", label_smoothing=0.0, margin=0.0,
+                            pair_weight=None, average=False, nll=0.0, grad_scale=1.0, temperature=1.0, loss=None, logp=None,
+                            dlogits=None, reward=None, pair_loss=None, workspace=None, status=None):
+    """pods_logp_chunk, pods_preference and pods_logp_grad_chunk over a whole packed batch of logits [T,V] ->
+    (loss [1], logp [T], dlogits like logits, reward [M], pair_loss [P]); ``dlogits`` may be ``logits`` itself.  Arguments as
+    theirs.  Missing outputs and the workspace are allocated here."""
+    T, V, lp, ldl, dtype, here = _token_rows(logits, tokens)
+    dev, f32 = logits.device, torch.float32
+    M, P, code, margin_p, margin_all, ref_p, mask_p, cu_p, pairs_p, weight_p = _pair_args(ref_logp, mask, cu_seqlens, pairs, kind, margin,
+                                                                                      pair_weight, T, here)
+    if loss is None:
+        loss = torch.empty(1, dtype=f32, device=dev)
+    if logp is None:
+        logp = torch.empty(T, dtype=f32, device=dev)
+    if reward is None:
+        reward = torch.empty(M, dtype=f32, device=dev)
+    if pair_loss is None:
+        pair_loss = torch.empty(P, dtype=f32, device=dev)
+    dlogits, dp, ldd = _gradient_rows(logits, dlogits, ldl, here)
+    lib = load()
+    workspace = _scratch(workspace, lib.pods_preference_fwd_bwd_workspace_bytes(T, M, P), dev)
+    rc = lib.pods_preference_fwd_bwd(lp, ldl, dtype, _vec(tokens, torch.int32, T, "tokens", here), ref_p, mask_p, cu_p, M, T, V,
+                                     temperature, pairs_p, weight_p, P, code, PREFERENCE_AVERAGE if average else 0, beta,
+                                     label_smoothing, margin_p, margin_all, nll, grad_scale, _vec(loss, f32, 1, "loss", here),
+                                     _vec(logp, f32, T, "logp", here), dp, ldd, _vec(reward, f32, M, "reward", here),
+                                     _vec(pair_loss, f32, P, "pair_loss", here),
+                                     _vec(workspace, torch.uint8, workspace.numel(), "workspace", here), workspace.numel(),
+                                     _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_preference_fwd_bwd")
+    return loss, logp, dlogits, reward, pair_loss
+
+
+class _AdamWEntry(C.Structure):
+    """pods_adamw_tensor of include/pods.h."""
+    _fields_ = [("param", _p), ("grad", _p), ("m", _p), ("v", _p), ("m_scale", _p), ("v_scale", _p), ("copy", _p), ("n", _i64),
+                ("param_type", _i32), ("grad_type", _i32), ("copy_type", _i32), ("state_bits", _i32), ("weight_decay", _f32),
+                ("lr_scale", _f32)]
+
+
+def _dense(t, name, here, n=None, dtypes=None):
+    """Address and dtype code of a dense CUDA tensor of n elements on the device `here`."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise PodsError("%s must be a CUDA tensor" % name)
+    _same_device(t, name, here)
+    if n is not None:
+        _numel(t, n, name)
+    code = DTYPES.get(t.dtype) if dtypes is None else (0 if t.dtype in dtypes else None)
+    if code is None:
+        raise PodsError("%s must be %s, got %s" % (name, "bfloat16, float16 or float32" if dtypes is None else " or ".join(map(str, dtypes)), t.dtype))
+    if not t.is_contiguous():
+        raise PodsError("%s must be contiguous" % name)
+    return t.data_ptr(), code
+
+
+def new_adamw_state(param, bits=32):
+    """The state of one tensor before its first step: (m, v) fp32, or with bits=8 (m, m_scale, v, v_scale) uint8."""
+    _require(bits in (8, 32), "bits must be 8 or 32, got %r" % (bits,))
+    n, dev = param.numel(), param.device
+    if bits == 32:
+        return tuple(torch.zeros(n, dtype=torch.float32, device=dev) for _ in range(2))
+    return tuple(torch.zeros(k, dtype=torch.uint8, device=dev) for k in (n, (n + 31) // 32, n, (n + 31) // 32))
+
+
+class AdamWTable:
+    """The tensors of pods_adamw and pods_grad_norm, checked and laid out once.  It holds them: their storage must stay theirs
+    (a tensor moved elsewhere needs a new table; gradients that change places each step go through set_grads)."""
+
+    def __init__(self, params, grads, states, copies, weight_decay, lr_scale):
+        n = len(params)
+        each = lambda x, name: list(x) if isinstance(x, (list, tuple)) else [x] * n  # noqa: E731
+        decay, scale = each(weight_decay, "weight_decay"), each(lr_scale, "lr_scale")
+        copies = list(copies) if copies is not None else [None] * n
+        for x, name in ((grads, "grads"), (states, "states"), (copies, "copies"), (decay, "weight_decay"), (scale, "lr_scale")):
+            _require(len(x) == n, "%s must have one entry a parameter, %d, got %d" % (name, n, len(x)))
+        here = self.device = _here() if torch.cuda.is_available() else -1
+        self.params, self.states, self.copies = list(params), [tuple(s) for s in states], copies
+        self.entries = (_AdamWEntry * max(n, 1))()
+        self.count = n
+        seen = set()
+        for i, (p, s, c) in enumerate(zip(params, self.states, copies)):
+            e = self.entries[i]
+            e.param, e.param_type = _dense(p, "params[%d]" % i, here)
+            e.n = k = p.numel()
+            _require(len(s) in (2, 4), "states[%d] must be (m, v) or (m, m_scale, v, v_scale)" % i)
+            if len(s) == 2:
+                e.state_bits = 32
+                (e.m, _), (e.v, _) = (_dense(t, "states[%d]" % i, here, k, (torch.float32,)) for t in s)
+            else:
+                e.state_bits = 8
+                blocks = (k + 31) // 32
+                (e.m, _), (e.m_scale, _), (e.v, _), (e.v_scale, _) = (_dense(t, "states[%d]" % i, here, w, (torch.uint8,))
+                                                                     for t, w in zip(s, (k, blocks, k, blocks)))
+            if c is not None:
+                e.copy, e.copy_type = _dense(c, "copies[%d]" % i, here, k)
+            e.weight_decay, e.lr_scale = decay[i], scale[i]
+            for t in (p, c) + s:
+                if t is not None and k:
+                    _require(t.data_ptr() not in seen, "params[%d] shares memory with an earlier entry" % i)
+                    seen.add(t.data_ptr())
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        """Takes other gradient tensors, one a parameter, of the same numbers of elements."""
+        _require(len(grads) == self.count, "grads must have one entry a parameter, %d, got %d" % (self.count, len(grads)))
+        got = [_dense(g, "grads[%d]" % i, self.device, self.entries[i].n) for i, g in enumerate(grads)]
+        for e, (at, code) in zip(self.entries, got):
+            e.grad, e.grad_type = at, code
+        self.grads = list(grads)
+
+
+def pods_adamw_table(params, grads, states, copies=None, weight_decay=0.0, lr_scale=1.0):
+    """Lists of parameters (bf16, fp16 or fp32), their gradients (any of these types), their states (new_adamw_state) and, where
+    wanted, copies (a tensor or None each) -> the table that pods_adamw and pods_grad_norm take.  weight_decay and lr_scale: a
+    number, or one a parameter."""
+    return AdamWTable(params, grads, states, copies, weight_decay, lr_scale)
+
+
+def pods_grad_norm(tensors, scale=1.0, norm=None, workspace=None, status=None):
+    """|scale| times the 2-norm over all gradients of an AdamWTable, or over a list of dense CUDA tensors -> norm [1] fp32."""
+    here = _here()
+    if isinstance(tensors, AdamWTable):
+        entries, n = tensors.entries, tensors.count
+        _require(tensors.device == here, "the table's tensors must be on the current CUDA device (cuda:%d), they are on cuda:%d" % (here, tensors.device))
+    else:
+        n = len(tensors)
+        entries = (_AdamWEntry * max(n, 1))()
+        for i, t in enumerate(tensors):
+            entries[i].grad, entries[i].grad_type = _dense(t, "tensors[%d]" % i, here)
+            entries[i].n = t.numel()
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device="cuda:%d" % here)
+    lib = load()
+    workspace = _scratch(workspace, lib.pods_grad_norm_workspace_bytes(n), norm.device)
+    rc = lib.pods_grad_norm(entries, n, scale, _vec(norm, torch.float32, 1, "norm", here),
+                            _vec(workspace, torch.uint8, workspace.numel(), "workspace", here), workspace.numel(),
+                            _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_grad_norm")
+    return norm
+
+
+def pods_adamw(table, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, norm=None, max_norm=0.0, grad_scale=1.0, stochastic=False, seed=0,
+               status=None):
+    """Step number `step` (1, 2, ...) of AdamW on the tensors of an AdamWTable, in place.
+
+    step and lr are numbers, or CUDA tensors [1] (int64, fp32) that captured graphs read anew.  norm: what pods_grad_norm
+    returned with scale=grad_scale; gradients are scaled down to max_norm (0: not), and a norm that is no finite number leaves
+    everything as it was.  stochastic: bf16 parameters are rounded with random bits, a function of seed, step and place."""
+    _require(isinstance(table, AdamWTable), "table must be made by pods_adamw_table")
+    here = _here()
+    _require(table.device == here, "the table's tensors must be on the current CUDA device (cuda:%d), they are on cuda:%d" % (here, table.device))
+    step_t, step = (step, 0) if isinstance(step, torch.Tensor) else (None, step)
+    lr_t, lr = (lr, 0.0) if isinstance(lr, torch.Tensor) else (None, lr)
+    _require(max_norm == 0.0 or norm is not None, "max_norm needs norm")
+    rc = load().pods_adamw(table.entries, table.count, step, _vec(step_t, torch.int64, 1, "step", here, True), lr,
+                           _vec(lr_t, torch.float32, 1, "lr", here, True), beta1, beta2, eps, grad_scale,
+                           _vec(norm, torch.float32, 1, "norm", here, True), max_norm, ADAMW_STOCHASTIC if stochastic else 0,
+                           seed & 0xffffffffffffffff, _vec(status, torch.int32, 1, "status", here, True), _stream())
+    if rc:
+        _check(rc, "pods_adamw")

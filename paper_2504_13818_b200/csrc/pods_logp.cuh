@@ -1,0 +1,55 @@
+// Arguments of the token log-probability kernels, for the calls that launch them between others.
+#pragma once
+
+#include "row_cluster.cuh"
+
+namespace pods_logp {
+
+constexpr int64_t kMaxRows = 1 << 24;  // rows of one call: with at most 64 stretches a row, block numbers stay within 31 bits
+
+struct FwdArgs {
+    const void* logits;
+    int64_t ldl;
+    const int32_t* tokens;
+    const uint8_t* mask;
+    const int64_t* rows_end;           // rows from *rows_end on are left out like masked ones; NULL: none
+    int64_t T;
+    int32_t V;
+    int32_t fill;                      // rows left out get logp 0 (otherwise they stay as they were)
+    double inv_tau;
+    float c;
+    float* logp;
+    double* lse;
+    float* entropy;
+    uint32_t* status;
+};
+
+struct GradArgs {
+    const void* logits;
+    int64_t ldl;
+    const int32_t* tokens;
+    const double* lse;
+    const float* dlogp;
+    const float* entropy;
+    const float* dentropy;
+    int64_t T;
+    int32_t V;
+    int32_t n_seg, seg;
+    double inv_tau;
+    float c;
+    void* dlogits;
+    int64_t ldd;
+    uint32_t* status;
+};
+
+// log2 e / temperature; exponents of temperatures so cold that it overflows are taken in fp64 as those of huge logits are
+inline float exponent_scale(float temperature) {
+    const double c = 1.4426950408889634074 / (double)temperature;
+    return c > 3e38 ? 3e38f : (float)c;
+}
+
+int check_rows(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, float temperature);
+int launch_forward(const FwdArgs& a, int dtype, cudaStream_t s);
+int launch_gradient(GradArgs& a, int dtype, cudaStream_t s);
+
+}  // namespace pods_logp

@@ -1,0 +1,247 @@
+"""pods_preference and pods_preference_fwd_bwd against the fp64 oracle.
+
+pods_preference works in fp64 from fp32 inputs: what it returns is rounded once, 2^-24 relative, and sums of n terms add
+n 2^-53 of their magnitudes.  pods_preference_fwd_bwd starts from log-probabilities that are off by up to TOL a token (derived in
+test_gpu_logp.py), so scores move by |o_i| TOL and coefficients by the slope's change."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import preference
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -23
+TOL = 2.0 ** -18
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2504_13818_b200 import binding as b
+    b.load()
+    return b
+
+
+def batch(M, mean, P, seed=0, masked=0.1, far=0):
+    """Ragged rollouts, one of them empty, and pairs among them with repeats, unused ones and one against itself."""
+    rng = np.random.default_rng(seed)
+    lengths = rng.integers(0, 2 * mean + 1, M)
+    if M > 2:
+        lengths[1] = 0
+    cu = np.concatenate([[0], np.cumsum(lengths)])
+    T = int(cu[-1]) + far
+    logp, ref = -rng.random(T) * 4, -rng.random(T) * 4
+    mask = rng.random(T) >= masked
+    pairs = rng.integers(0, M, (P, 2))
+    if P > 3:
+        pairs[1] = (-1, 0)
+        pairs[2] = pairs[0]
+        pairs[3] = (0, 0)
+    return logp.astype(np.float32), ref.astype(np.float32), mask.astype(np.uint8), cu, pairs.astype(np.int32)
+
+
+def dev(x, dtype=None):
+    return None if x is None else torch.as_tensor(np.asarray(x), dtype=dtype).cuda()
+
+
+def close(got, want, scale=1.0):
+    got = got.double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= EPS * np.abs(want) + 1e-12 * scale), np.abs(got - want).max()
+
+
+KINDS = [("sigmoid", 0.0), ("sigmoid", 0.2), ("hinge", 0.0), ("squared", 0.0)]
+
+
+@pytest.mark.parametrize("kind,smoothing", KINDS)
+@pytest.mark.parametrize("average", [False, True])
+@pytest.mark.parametrize("M,mean,P", [(2, 3, 1), (5, 40, 9), (130, 70, 700), (33, 300, 5000)])
+def test_pairs(binding, kind, smoothing, average, M, mean, P):
+    logp, ref, mask, cu, pairs = batch(M, mean, P, seed=M, far=3)
+    for k, (r, m, nll, weight, margin) in enumerate([(ref, mask, 0.0, None, 0.25), (None, None, 0.5, "some", "each"), (ref, mask, 0.1, None, 0.0)]):
+        rng = np.random.default_rng(k)
+        weight = rng.random(P).astype(np.float32) * (rng.random(P) < 0.8) if weight else None
+        margin = rng.random(P).astype(np.float32) if margin == "each" else margin
+        acc = torch.full((1,), 2.0, dtype=torch.float64, device="cuda")
+        status = binding.new_status()
+        dlogp, reward, losses = binding.pods_preference(
+            dev(logp), dev(r), dev(m), dev(cu), dev(pairs), 0.3, acc, kind=kind, label_smoothing=smoothing,
+            margin=dev(margin) if isinstance(margin, np.ndarray) else margin, pair_weight=dev(weight, torch.float32), average=average,
+            nll=nll, grad_scale=1.5, status=status)
+        assert binding.read_status(status) == 0
+        s, n = float(np.float32(smoothing)), float(np.float32(nll))
+        want = preference.preference(logp, r, m, cu, pairs.tolist(), float(np.float32(0.3)), kind=kind, smoothing=s, margin=margin,
+                                     pair_weight=weight, average=average, nll=n, grad_scale=1.5)
+        size = max(1.0, np.abs(want[3]).max())
+        assert abs(acc.item() - 2.0 - want[0]) <= 1e-11 * size * (1 + abs(want[0]))
+        close(dlogp, want[1], size)
+        close(reward, want[2], size)
+        close(losses, want[3], size)
+        assert (dlogp[int(cu[-1]):] == 0).all()
+
+
+def test_ids_out_of_range_and_no_pairs(binding):
+    logp, ref, mask, cu, pairs = batch(6, 20, 8, seed=2)
+    pairs[5], pairs[6], pairs[7] = (6, 0), (0, -2), (2 ** 31 - 1, -2 ** 31)
+    acc, status = torch.zeros(1, dtype=torch.float64, device="cuda"), binding.new_status()
+    got = binding.pods_preference(dev(logp), dev(ref), dev(mask), dev(cu), dev(pairs), 0.5, acc, status=status)
+    assert binding.read_status(status) == binding.STATUS_INDEX_RANGE
+    want = preference.preference(logp, ref, mask, cu, [(c, r) if 0 <= c < 6 and 0 <= r < 6 else (-1, -1) for c, r in pairs.tolist()], 0.5)
+    close(got[0], want[1])
+    close(got[2], want[3])
+    assert abs(acc.item() - want[0]) < 1e-11
+    acc.zero_()
+    got = binding.pods_preference(dev(logp), dev(ref), dev(mask), dev(cu), dev(pairs[:0]), 0.5, acc)
+    assert acc.item() == 0 and (got[0] == 0).all() and got[2].numel() == 0
+    close(got[1], want[2])
+    none = torch.full((4, 2), -1, dtype=torch.int32, device="cuda")
+    got = binding.pods_preference(dev(logp), dev(ref), dev(mask), dev(cu), none, 0.5, acc)
+    assert acc.item() == 0 and (got[0] == 0).all() and (got[2] == 0).all()
+
+
+def test_masked_and_weightless_log_probabilities_are_of_no_consequence(binding):
+    logp, ref, mask, cu, pairs = batch(8, 30, 6, seed=3)
+    pairs[:] = [(0, 2), (3, 4), (4, 0), (2, 3), (5, 6), (6, 7)]
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    weight = torch.tensor([1.0, 0.5, 0.25, 1.0, 0.0, 0.0], device="cuda")
+    want = binding.pods_preference(dev(logp), dev(ref), dev(mask), dev(cu), dev(pairs), 0.5, acc, pair_weight=weight, nll=0.1)
+    first = acc.item()
+    bad = logp.copy()
+    bad[mask == 0] = np.nan
+    bad[cu[6]:cu[7]] = -np.inf                         # rollout 6 stands in pairs of weight 0 only
+    acc.zero_()
+    got = binding.pods_preference(dev(bad), dev(ref), dev(mask), dev(cu), dev(pairs), 0.5, acc, pair_weight=weight, nll=0.1)
+    assert torch.equal(got[0], want[0]) and acc.item() == first
+
+
+def test_log_probability_of_minus_infinity(binding):
+    """A worse rollout that cannot happen: loss 0 and slope 0.  A better one: loss infinite, the full slope."""
+    cu, pairs = torch.tensor([0, 2, 4], device="cuda"), torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+    lp = torch.tensor([-1.0, -1.0, -torch.inf, -1.0], device="cuda")
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    d, _, l = binding.pods_preference(lp, None, None, cu, pairs, 0.5, acc)
+    assert l.item() == 0 and (d == 0).all() and acc.item() == 0
+    d, _, l = binding.pods_preference(lp, None, None, cu, pairs.flip(1).contiguous(), 0.5, acc)
+    assert l.item() == float("inf") and d.tolist() == [0.5, 0.5, -0.5, -0.5]
+
+
+def test_a_rollout_that_stands_in_every_pair(binding):
+    M, P = 40, 3000
+    logp, ref, mask, cu, pairs = batch(M, 10, P, seed=6)
+    pairs[:, 0] = 7
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    got = binding.pods_preference(dev(logp), dev(ref), dev(mask), dev(cu), dev(pairs), 0.1, acc)
+    want = preference.preference(logp, ref, mask, cu, pairs.tolist(), float(np.float32(0.1)))
+    close(got[0], want[1])
+    again = binding.pods_preference(dev(logp), dev(ref), dev(mask), dev(cu), dev(pairs), 0.1, acc)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+def logits_of(T, V, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    z = (torch.randn((T, V), generator=g) * 2).to(TYPES[dtype]).cuda()
+    return z, torch.randint(0, V, (T,), generator=g, dtype=torch.int32).cuda()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("kind,average,nll", [("sigmoid", False, 0.0), ("squared", True, 0.2), ("hinge", False, 0.1)])
+@pytest.mark.parametrize("M,mean,V", [(4, 9, 515), (6, 20, 20000), (40, 12, 1024)])
+def test_from_logits(binding, dtype, kind, average, nll, M, mean, V):
+    _, _, mask, cu, pairs = batch(M, mean, max(1, M // 2), seed=M + V, far=2)
+    T = len(mask)
+    z, tok = logits_of(T, V, dtype, seed=V)
+    zn, tn = z.double().cpu().numpy(), tok.cpu().numpy()
+    exact = np.array([preference.logp_row(zn[t], tn[t], 1.0)[0] for t in range(T)])
+    ref = (exact + 0.1 * np.random.default_rng(1).normal(size=T)).astype(np.float32)
+    tok[int(cu[-1]):] = -5                             # rows behind the last rollout are not looked at
+    z[mask == 0] = torch.nan
+    status = binding.new_status()
+    loss, logp, dlogits, reward, losses = binding.pods_preference_fwd_bwd(z, tok, dev(ref), dev(mask), dev(cu), dev(pairs), 0.2, kind=kind,
+                                                                          average=average, nll=nll, status=status)
+    assert binding.read_status(status) == 0
+    live = mask.astype(bool) & (np.arange(T) < cu[-1])
+    assert (logp[dev(~live)] == 0).all()
+    beta = float(np.float32(0.2))
+    want = preference.preference(exact, ref, mask, cu, pairs.tolist(), beta, kind=kind, average=average, nll=float(np.float32(nll)))
+    moved = TOL * max(1, int(np.diff(cu).max()))       # of a score
+    steep = 2 * (np.abs(want[3]).max() ** 0.5 + moved) / beta * beta + 2 * moved if kind == "squared" else 1.0
+    got_lp = logp.double().cpu().numpy()
+    assert np.all(np.abs(got_lp - exact)[live] <= TOL + EPS * np.abs(exact[live]))
+    assert np.all(np.abs(reward.double().cpu().numpy() - want[2]) <= beta * moved + EPS * np.abs(want[2]))
+    assert np.all(np.abs(losses.double().cpu().numpy() - want[3]) <= 2 * moved * (steep + 1) + EPS * np.abs(want[3]))
+    assert abs(loss.item() - want[0]) <= 2 * moved * (steep + 1) + EPS * abs(want[0])
+    # the gradient, from the call's own slopes: those of pods_preference on the log-probabilities it returned
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    dlogp = binding.pods_preference(logp, dev(ref), dev(mask), dev(cu), dev(pairs), 0.2, acc, kind=kind, average=average, nll=nll)[0]
+    d = dlogp.double().cpu().numpy()
+    out = dlogits.double().cpu().numpy()
+    half = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11, "fp32": 2.0 ** -24}[dtype]
+    for t in range(T):
+        if d[t] == 0:
+            assert (out[t] == 0).all()
+            continue
+        g = preference.logp_grad_row(zn[t], tn[t], 1.0, d[t])
+        tol = half * np.abs(g) + TOL * np.abs(g) + 2.0 ** -25 * (dtype == "fp16")
+        tol[tn[t]] += EPS * abs(d[t])
+        assert np.all(np.abs(out[t] - g) <= 1.001 * tol), t
+    # in place, chunk by chunk, and with everything handed in: the same bits
+    parts = torch.empty(T, device="cuda"), torch.empty(T, dtype=torch.float64, device="cuda")
+    keep = dev(live.astype(np.uint8))
+    parts[0].zero_()
+    cut = T // 3
+    for a, b in ((0, cut), (cut, T)):
+        binding.pods_logp_chunk(z[a:b], tok[a:b], mask=keep[a:b], logp=parts[0][a:b], lse=parts[1][a:b])
+    chunked = torch.empty_like(z)
+    for a, b in ((0, cut), (cut, T)):
+        binding.pods_logp_grad_chunk(z[a:b], tok[a:b], parts[1][a:b], dlogp[a:b], dlogits=chunked[a:b])
+    assert torch.allclose(parts[0], logp, rtol=0, atol=TOL)
+    assert torch.allclose(chunked.float(), dlogits.float(), rtol=2 * half + TOL, atol=1e-9 + 2.0 ** -24 * (dtype == "fp16"))
+    ws = torch.empty(binding.load().pods_preference_fwd_bwd_workspace_bytes(T, M, len(pairs)), dtype=torch.uint8, device="cuda")
+    again = binding.pods_preference_fwd_bwd(z, tok, dev(ref), dev(mask), dev(cu), dev(pairs), 0.2, kind=kind, average=average, nll=nll,
+                                            dlogits=z, workspace=ws)
+    assert again[2] is z and all(torch.equal(a, b) for a, b in zip(again, (loss, logp, dlogits, reward, losses)))
+
+
+def test_gradient_in_the_logits_is_that_of_differences(binding):
+    _, _, mask, cu, pairs = batch(4, 5, 2, seed=11, masked=0.2)
+    pairs[:] = [(0, 2), (3, 2)]
+    T, V = len(mask), 24
+    z, tok = logits_of(T, V, "fp32", seed=4)
+    call = lambda x: binding.pods_preference_fwd_bwd(x, tok, None, dev(mask), dev(cu), dev(pairs), 0.5, nll=0.2, temperature=1.5)  # noqa: E731
+    g = call(z)[2]
+    lp = lambda x: np.array([preference.logp_row(x[t], int(tok[t]), 1.5)[0] for t in range(T)])  # noqa: E731
+    f = lambda x: preference.preference(lp(x), None, mask, cu, pairs.tolist(), 0.5, nll=float(np.float32(0.2)))[0]  # noqa: E731
+    zn = z.double().cpu().numpy()
+    rng = np.random.default_rng(0)
+    for _ in range(40):
+        t, v = rng.integers(T), rng.integers(V)
+        up, down = zn.copy(), zn.copy()
+        up[t, v] += 1e-5
+        down[t, v] -= 1e-5
+        assert abs((f(up) - f(down)) / 2e-5 - g[t, v].item()) < 1e-6
+
+
+def test_captured_and_replayed_beside_an_eager_call(binding):
+    _, ref, mask, cu, pairs = batch(6, 30, 5, seed=21)
+    T = len(mask)
+    args = [dev(ref), dev(mask), dev(cu), dev(pairs)]
+    z, tok = logits_of(T, 9000, "bf16", seed=1)
+    z2, _ = logits_of(T, 9000, "bf16", seed=2)
+    eager = binding.pods_preference_fwd_bwd(z, tok, *args, 0.2)
+    other = binding.pods_preference_fwd_bwd(z2, tok, *args, 0.2)
+    held = z.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = binding.pods_preference_fwd_bwd(held, tok, *args, 0.2)
+    graph.replay()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        beside = binding.pods_preference_fwd_bwd(z2, tok, *args, 0.2)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, eager)) and all(torch.equal(a, b) for a, b in zip(beside, other))
+    held.copy_(z2)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, other))
