@@ -22,8 +22,8 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
-constexpr int kTile = kThreads * 4 * kUnroll;          // elements; a multiple of 32
+constexpr int kTile = kThreads * 8;                    // elements, eight a thread; a multiple of 32
+constexpr int kMostCtas = 148 * 6;                     // of a launch; each takes one run of consecutive tiles
 
 struct Tensor {
     void* p;
@@ -35,19 +35,23 @@ struct Tensor {
     void* copy;
     int64_t n, first;                  // elements; the number of the first one among all of the call
     uint32_t tile0;                    // tiles of this launch ahead of it
-    uint8_t p_type, g_type, copy_type, bits, aligned;
+    uint8_t p_type, g_type, copy_type;
+    uint8_t vectors;                   // 2: eight elements of every buffer lie on their boundary (32 bytes of fp32), 1: 16 bytes, 0: neither
     float decay, lr_scale;
 };
 
+// The launch's tensors, and the tensor in which each CTA's run of tiles begins: a search in a table of this size would cost a CTA
+// several misses of the constant cache, one after the other (a norm over 217 tensors: 183 us with it).
 template <int N>
 struct Table {
     int count;
     uint32_t tiles;
+    uint16_t start[kMostCtas];
     Tensor t[N];
 };
 
 // A kernel argument may hold 32764 bytes; most sets of tensors need few entries, and an argument costs its upload.
-constexpr int kFew = 40, kMany = 320;
+constexpr int kFew = 24, kMany = 320;
 static_assert(sizeof(Table<kMany>) < 32000, "a kernel argument");
 
 struct Step {
@@ -72,247 +76,290 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
     return x ^ (x >> 16);
 }
 
-template <int N>
-__device__ __forceinline__ const Tensor& tensor_of(const Table<N>& tab, uint32_t tile) {
-    int lo = 0, hi = tab.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tab.t[mid].tile0 <= tile) lo = mid;
-        else hi = mid - 1;
-    }
-    return tab.t[lo];
-}
-
-// Four elements as they lie in memory.
-struct Raw4 {
-    uint4 w;
+// Eight elements as they lie in memory; 16-bit types use the first half.
+struct Raw8 {
+    uint32_t w[8];
 };
-__device__ __forceinline__ Raw4 load4(const void* base, int type, int64_t i) {
-    Raw4 r;
+__device__ __forceinline__ Raw8 load8(const void* base, int type, int64_t i, int vectors) {
+    Raw8 r = {};
     if (type == PODS_DTYPE_F32) {
-        r.w = *reinterpret_cast<const uint4*>(static_cast<const float*>(base) + i);
+        const float* at = static_cast<const float*>(base) + i;
+        if (vectors == 2) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "l"(at));
+        } else {
+            const uint4 a = reinterpret_cast<const uint4*>(at)[0], b = reinterpret_cast<const uint4*>(at)[1];
+            r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+            r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+        }
     } else {
-        const uint2 h = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + i);
-        r.w = make_uint4(h.x, h.y, 0, 0);
+        const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + i);
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
     }
     return r;
-}
-__device__ __forceinline__ float one(uint32_t bits, int type) {
-    return type == PODS_DTYPE_BF16 ? __uint_as_float(bits << 16) : __half2float(__ushort_as_half((unsigned short)bits));
-}
-__device__ __forceinline__ void to_floats(const Raw4& r, int type, float (&x)[4]) {
-    if (type == PODS_DTYPE_F32) {
-        x[0] = __uint_as_float(r.w.x);
-        x[1] = __uint_as_float(r.w.y);
-        x[2] = __uint_as_float(r.w.z);
-        x[3] = __uint_as_float(r.w.w);
-    } else {
-        x[0] = one(r.w.x & 0xffffu, type);
-        x[1] = one(r.w.x >> 16, type);
-        x[2] = one(r.w.y & 0xffffu, type);
-        x[3] = one(r.w.y >> 16, type);
-    }
 }
 // Element by element: ends of a tensor, and tensors that do not lie on the vectors' boundaries.
-__device__ __forceinline__ Raw4 gather4(const void* base, int type, int64_t i, int64_t n) {
-    uint32_t x[4] = {0, 0, 0, 0};
+__device__ __forceinline__ Raw8 gather8(const void* base, int type, int64_t i, int64_t n) {
+    Raw8 r = {};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (i + k < n) x[k] = type == PODS_DTYPE_F32 ? static_cast<const uint32_t*>(base)[i + k] : static_cast<const uint16_t*>(base)[i + k];
-    Raw4 r;
-    r.w = type == PODS_DTYPE_F32 ? make_uint4(x[0], x[1], x[2], x[3]) : make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, 0, 0);
+    for (int k = 0; k < 8; ++k)
+        if (i + k < n) {
+            if (type == PODS_DTYPE_F32) r.w[k] = static_cast<const uint32_t*>(base)[i + k];
+            else r.w[k >> 1] |= (uint32_t) static_cast<const uint16_t*>(base)[i + k] << (16 * (k & 1));
+        }
     return r;
 }
-__device__ __forceinline__ Raw4 from_floats(const float (&x)[4], int type) {
-    Raw4 r;
+__device__ __forceinline__ void to_floats(const Raw8& r, int type, float (&x)[8]) {
     if (type == PODS_DTYPE_F32) {
-        r.w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(r.w[k]);
     } else if (type == PODS_DTYPE_BF16) {
-        uint32_t a, b;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(a) : "f"(x[1]), "f"(x[0]));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(x[3]), "f"(x[2]));
-        r.w = make_uint4(a, b, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[2 * k] = __uint_as_float(r.w[k] << 16);
+            x[2 * k + 1] = __uint_as_float(r.w[k] & 0xffff0000u);
+        }
     } else {
-        const __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
-        r.w = make_uint4(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b), 0, 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r.w[k]));
+            x[2 * k] = f.x;
+            x[2 * k + 1] = f.y;
+        }
+    }
+}
+__device__ __forceinline__ Raw8 from_floats(const float (&x)[8], int type) {
+    Raw8 r = {};
+    if (type == PODS_DTYPE_F32) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r.w[k] = __float_as_uint(x[k]);
+    } else if (type == PODS_DTYPE_BF16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w[k]) : "f"(x[2 * k + 1]), "f"(x[2 * k]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __half2 h = __floats2half2_rn(x[2 * k], x[2 * k + 1]);
+            r.w[k] = *reinterpret_cast<const uint32_t*>(&h);
+        }
     }
     return r;
 }
-__device__ __forceinline__ void store4(void* base, int type, int64_t i, int64_t n, bool whole, const Raw4& r) {
-    if (whole) {
-        if (type == PODS_DTYPE_F32) *reinterpret_cast<uint4*>(static_cast<float*>(base) + i) = r.w;
-        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + i) = make_uint2(r.w.x, r.w.y);
+__device__ __forceinline__ void store8(void* base, int type, int64_t i, int64_t n, int vectors, const Raw8& r) {
+    if (vectors) {
+        if (type == PODS_DTYPE_F32) {
+            float* at = static_cast<float*>(base) + i;
+            if (vectors == 2) {
+                asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                             ::"r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]), "r"(r.w[6]), "r"(r.w[7]), "l"(at) : "memory");
+            } else {
+                reinterpret_cast<uint4*>(at)[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+                reinterpret_cast<uint4*>(at)[1] = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+            }
+        } else {
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + i) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        }
         return;
     }
-    const uint32_t x[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 8; ++k)
         if (i + k < n) {
-            if (type == PODS_DTYPE_F32) static_cast<uint32_t*>(base)[i + k] = x[k];
-            else static_cast<uint16_t*>(base)[i + k] = (uint16_t)(x[k >> 1] >> (16 * (k & 1)));
+            if (type == PODS_DTYPE_F32) static_cast<uint32_t*>(base)[i + k] = r.w[k];
+            else static_cast<uint16_t*>(base)[i + k] = (uint16_t)(r.w[k >> 1] >> (16 * (k & 1)));
         }
 }
 
-// ---- e4m3 blocks ------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void codes_to_floats(uint32_t codes, uint32_t scale, float (&x)[4]) {
+// ---- e4m3 blocks: a block of 32 is held by four lanes -----------------------------------------------------------------------
+__device__ __forceinline__ uint2 load_codes(const void* base, int64_t i, int64_t n, bool fast) {
+    const uint8_t* at = static_cast<const uint8_t*>(base) + i;
+    if (fast) return *reinterpret_cast<const uint2*>(at);
+    uint2 r = make_uint2(0, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (i + k < n) (k < 4 ? r.x : r.y) |= (uint32_t)at[k] << (8 * (k & 3));
+    return r;
+}
+__device__ __forceinline__ void store_codes(void* base, int64_t i, int64_t n, bool fast, uint2 c) {
+    uint8_t* at = static_cast<uint8_t*>(base) + i;
+    if (fast) {
+        *reinterpret_cast<uint2*>(at) = c;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (i + k < n) at[k] = (uint8_t)((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
+}
+__device__ __forceinline__ void codes_to_floats(uint2 codes, uint32_t scale, float (&x)[8]) {
     const float s = __uint_as_float(scale << 23);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const __half2 h = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * k)), __NV_E4M3));
-        const float2 f = __half22float2(h);
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t two = (k < 2 ? codes.x : codes.y) >> (16 * (k & 1));
+        const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3)));
         x[2 * k] = f.x * s;
         x[2 * k + 1] = f.y * s;
     }
 }
-// The smallest power of two 2^(k - 127), k >= 1, with top / 2^(k - 127) <= 448 = 1.75 * 2^8; 255 where top is no number.
-__device__ __forceinline__ uint32_t block_scale(float top) {
-    if (!(top <= FLT_MAX)) return 255u;
-    return (uint32_t)max(1, (int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8);
+// The largest |x| of eight, NaN if one of them is.
+__device__ __forceinline__ float largest8(const float (&x)[8]) {
+    float a, b;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(b), "f"(b));
+    return a;
 }
-// |x| / 2^(k - 127) on e4m3's grid: numbers below 2^-6 gain 2^-6, after which 20 bits lie below the grid for all.
-__device__ __forceinline__ uint32_t round_code(float y, uint32_t word) {
-    const bool low = y < 0.015625f;
-    const uint32_t b = __float_as_uint(low ? y + 0.015625f : y);
-    return ((b + (word << 4) + 8u) >> 20) - (low ? 968u : 960u);
+// The smallest k >= 1 with top / 2^(k - 127) <= 448 = 1.75 * 2^8; 255 where top is no number.
+__device__ __forceinline__ uint32_t block_scale(float top) {
+    const uint32_t b = __float_as_uint(top) & 0x7fffffffu;
+    return b >= 0x7f800000u ? 255u : (uint32_t)max(1, (int)((b + 0x1fffffu) >> 23) - 8);
+}
+// Codes of eight numbers in a block of scale k.  A number times 2^(127 - k) 2^-120 has e4m3's exponent where fp32 keeps its
+// own, and e4m3's smallest numbers are fp32's: for all of them the code lies above the lowest 20 bits, and 16 random bits and a
+// half (a number that is on the grid stays) added there carry into it with the probability that keeps the average.
+template <bool ROOT>
+__device__ __forceinline__ uint2 to_codes(const float (&x)[8], uint32_t k, const uint32_t (&word)[8]) {
+    uint32_t c[8];
+    float pre = 1.0f, f = __uint_as_float((134u - k) << 23);
+    if (k > 133u) {                                    // 2^(7 - k) is no normal number: blocks above 28672, in two factors; NaN
+        pre = 0x1p-120f;
+        f = __uint_as_float((254u - min(k, 253u)) << 23);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t random = ROOT ? (word[i] * 0x9e3779b1u) >> 12 : word[i] >> 12;
+        uint32_t b = __float_as_uint((k > 133u ? fabsf(x[i]) * pre : fabsf(x[i])) * f) + ((random & 0xffff0u) | 8u);
+        if (ROOT && x[i] > 0.0f) b = max(b, 1u << 20);
+        c[i] = b >> 20;
+    }
+    uint2 r;
+    r.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+    r.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
+    if (!ROOT) {
+        const uint32_t a = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0073),
+                                       __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
+        const uint32_t b = __byte_perm(__byte_perm(__float_as_uint(x[4]), __float_as_uint(x[5]), 0x0073),
+                                       __byte_perm(__float_as_uint(x[6]), __float_as_uint(x[7]), 0x0073), 0x5410);
+        r.x |= a & 0x80808080u;
+        r.y |= b & 0x80808080u;
+    }
+    if (k == 255u) r = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+    return r;
+}
+
+__device__ __forceinline__ float sqrt_approx(float x) {    // off by 2^-23 at most
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {     // off by 2^-23 at most
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 struct Coefs {
     float g, beta1, beta2, keep1, keep2, lr, step, root, eps;
 };
 
-// One element: m, v (or its root r) and p move on.
-__device__ __forceinline__ void advance(const Coefs& c, float decay, float g, float& m, float& v, float& r, float& p) {
-    g *= c.g;
-    m = c.beta1 * m + c.keep1 * g;
-    v = c.beta2 * v + c.keep2 * (g * g);
-    r = sqrtf(v);
-    p = p * decay - c.step * (m / (r * c.root + c.eps));
-}
-
 template <int BITS>
-__device__ __forceinline__ void adamw_tile(const Tensor& t, uint32_t tile, const Step& a, const Coefs& c0, uint32_t key) {
-    const int64_t base = (int64_t)(tile - t.tile0) * kTile;
-    Coefs c = c0;
-    c.step *= t.lr_scale;
-    const float decay = 1.0f - c.lr * t.lr_scale * t.decay;
-    Raw4 p[kUnroll], g[kUnroll], m[kUnroll], v[kUnroll];
-    uint32_t ms[kUnroll], vs[kUnroll];
-    const bool fast = t.aligned && base + kTile <= t.n;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int64_t i = base + (int64_t)(u * kThreads + threadIdx.x) * 4;
-        if (fast) {
-            g[u] = load4(t.g, t.g_type, i);
-            p[u] = load4(t.p, t.p_type, i);
-            if (BITS == 32) {
-                m[u] = load4(t.m, PODS_DTYPE_F32, i);
-                v[u] = load4(t.v, PODS_DTYPE_F32, i);
-            } else {
-                m[u].w.x = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.m) + i);
-                v[u].w.x = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(t.v) + i);
-                ms[u] = t.m_scale[i >> 5];
-                vs[u] = t.v_scale[i >> 5];
-            }
-        } else {
-            g[u] = gather4(t.g, t.g_type, i, t.n);
-            p[u] = gather4(t.p, t.p_type, i, t.n);
-            if (BITS == 32) {
-                m[u] = gather4(t.m, PODS_DTYPE_F32, i, t.n);
-                v[u] = gather4(t.v, PODS_DTYPE_F32, i, t.n);
-            } else {
-                m[u].w.x = v[u].w.x = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (i + k < t.n) {
-                        m[u].w.x |= (uint32_t) static_cast<const uint8_t*>(t.m)[i + k] << (8 * k);
-                        v[u].w.x |= (uint32_t) static_cast<const uint8_t*>(t.v)[i + k] << (8 * k);
-                    }
-                ms[u] = i < t.n ? t.m_scale[i >> 5] : 0;
-                vs[u] = i < t.n ? t.v_scale[i >> 5] : 0;
-            }
-        }
+__device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const Step& a, const Coefs& c, uint32_t key) {
+    const float decay = 1.0f - c.lr * t.lr_scale * t.decay, rate = c.step * t.lr_scale;
+    const int64_t i = base + (int64_t)threadIdx.x * 8, n = t.n;
+    const int vectors = base + kTile <= n ? t.vectors : 0;
+    const bool fast = vectors != 0;
+    Raw8 g, p, m, v;
+    uint2 mc, vc;
+    uint32_t ms, vs;
+    if (fast) {
+        g = load8(t.g, t.g_type, i, vectors);
+        p = load8(t.p, t.p_type, i, vectors);
+    } else {
+        g = gather8(t.g, t.g_type, i, n);
+        p = gather8(t.p, t.p_type, i, n);
     }
+    if (BITS == 32) {
+        m = fast ? load8(t.m, PODS_DTYPE_F32, i, vectors) : gather8(t.m, PODS_DTYPE_F32, i, n);
+        v = fast ? load8(t.v, PODS_DTYPE_F32, i, vectors) : gather8(t.v, PODS_DTYPE_F32, i, n);
+    } else {
+        mc = load_codes(t.m, i, n, fast);
+        vc = load_codes(t.v, i, n, fast);
+        ms = i < n ? t.m_scale[i >> 5] : 0;
+        vs = i < n ? t.v_scale[i >> 5] : 0;
+    }
+    uint32_t word[8];
+    if (BITS == 8 || a.stochastic) {
+        const uint64_t number = (uint64_t)(t.first + i);   // a multiple of 8: the eight share the high word
+        const uint32_t high = (uint32_t)(number >> 32), k32 = mix(key + high);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int64_t i = base + (int64_t)(u * kThreads + threadIdx.x) * 4;
-        float pf[4], gf[4], mf[4], vf[4], rf[4];
-        to_floats(g[u], t.g_type, gf);
-        to_floats(p[u], t.p_type, pf);
-        if (BITS == 32) {
-            to_floats(m[u], PODS_DTYPE_F32, mf);
-            to_floats(v[u], PODS_DTYPE_F32, vf);
-        } else {
-            codes_to_floats(m[u].w.x, ms[u], mf);
-            codes_to_floats(v[u].w.x, vs[u], vf);
+        for (int k = 0; k < 8; ++k) word[k] = mix(((uint32_t)number + k) ^ k32);
+    }
+    float pf[8], gf[8], mf[8], vf[8];
+    to_floats(g, t.g_type, gf);
+    to_floats(p, t.p_type, pf);
+    if (BITS == 32) {
+        to_floats(m, PODS_DTYPE_F32, mf);
+        to_floats(v, PODS_DTYPE_F32, vf);
+    } else {
+        codes_to_floats(mc, ms, mf);
+        codes_to_floats(vc, vs, vf);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) vf[k] *= vf[k];
-        }
+        for (int k = 0; k < 8; ++k) vf[k] *= vf[k];
+    }
+    float rf[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) advance(c, decay, gf[k], mf[k], vf[k], rf[k], pf[k]);
-        uint32_t word[4];
-        if (BITS == 8 || a.stochastic) {
-            const uint64_t number = (uint64_t)(t.first + i);   // a multiple of 4: the four share the high word
-            const uint32_t k32 = (uint32_t)(number >> 32) == 0 ? mix(key) : mix(key + (uint32_t)(number >> 32));
+    for (int k = 0; k < 8; ++k) {
+        const float x = gf[k] * c.g;
+        mf[k] = c.beta1 * mf[k] + c.keep1 * x;
+        vf[k] = c.beta2 * vf[k] + c.keep2 * (x * x);
+        rf[k] = sqrt_approx(vf[k]);
+        pf[k] = pf[k] * decay - rate * (mf[k] * rcp_approx(rf[k] * c.root + c.eps));
+    }
+    if (t.copy != nullptr) store8(t.copy, t.copy_type, i, n, vectors, from_floats(pf, t.copy_type));
+    if (a.stochastic && t.p_type == PODS_DTYPE_BF16) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) word[k] = mix(((uint32_t)number + k) ^ k32);
-        }
-        if (t.copy != nullptr) store4(t.copy, t.copy_type, i, t.n, fast, from_floats(pf, t.copy_type));
-        if (a.stochastic && t.p_type == PODS_DTYPE_BF16) {
+        for (int k = 0; k < 8; ++k)
+            if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + (word[k] & 0xffffu)) & 0xffff0000u);
+    }
+    store8(t.p, t.p_type, i, n, vectors, from_floats(pf, t.p_type));
+    if (BITS == 32) {
+        store8(t.m, PODS_DTYPE_F32, i, n, vectors, from_floats(mf, PODS_DTYPE_F32));
+        store8(t.v, PODS_DTYPE_F32, i, n, vectors, from_floats(vf, PODS_DTYPE_F32));
+        return;
+    }
+    if (!fast) {                                       // what lies behind the tensor's end counts nothing
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + (word[k] & 0xffffu)) & 0xffff0000u);
-        }
-        store4(t.p, t.p_type, i, t.n, fast, from_floats(pf, t.p_type));
-        if (BITS == 32) {
-            store4(t.m, PODS_DTYPE_F32, i, t.n, fast, from_floats(mf, PODS_DTYPE_F32));
-            store4(t.v, PODS_DTYPE_F32, i, t.n, fast, from_floats(vf, PODS_DTYPE_F32));
-        } else {
-            // the block's largest, over the eight lanes that hold it; a NaN stays one
-            float mt = 0.0f, rt = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool in = i + k < t.n;
-                mt = in ? (fabsf(mf[k]) > mt || mf[k] != mf[k] ? fabsf(mf[k]) : mt) : mt;
-                rt = in ? (rf[k] > rt || rf[k] != rf[k] ? rf[k] : rt) : rt;
-            }
-            uint32_t mb = __float_as_uint(mt), rb = __float_as_uint(rt);        // of numbers >= 0 and NaN the order is that of the bits
-#pragma unroll
-            for (int d = 4; d > 0; d >>= 1) {
-                mb = max(mb, __shfl_xor_sync(PODS_FULL_MASK, mb, d));
-                rb = max(rb, __shfl_xor_sync(PODS_FULL_MASK, rb, d));
-            }
-            const uint32_t mk = block_scale(__uint_as_float(mb)), rk = block_scale(__uint_as_float(rb));
-            const float mi = __uint_as_float((254u - min(mk, 253u)) << 23), ri = __uint_as_float((254u - min(rk, 253u)) << 23);
-            uint32_t mc = 0, rc = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t sign = (__float_as_uint(mf[k]) >> 24) & 0x80u;
-                const uint32_t a8 = mk == 255u ? 0x7fu : round_code(fabsf(mf[k]) * mi, word[k] >> 16);
-                uint32_t b8 = rk == 255u ? 0x7fu : round_code(rf[k] * ri, (word[k] * 0x9e3779b1u) >> 16);
-                if (b8 == 0 && rf[k] > 0.0f) b8 = 1;
-                mc |= (a8 | sign) << (8 * k);
-                rc |= b8 << (8 * k);
-            }
-            if (fast) {
-                *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.m) + i) = mc;
-                *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.v) + i) = rc;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (i + k < t.n) {
-                        static_cast<uint8_t*>(t.m)[i + k] = (uint8_t)(mc >> (8 * k));
-                        static_cast<uint8_t*>(t.v)[i + k] = (uint8_t)(rc >> (8 * k));
-                    }
-            }
-            if ((i & 31) == 0 && i < t.n) {
-                t.m_scale[i >> 5] = (uint8_t)mk;
-                t.v_scale[i >> 5] = (uint8_t)rk;
-            }
-        }
+        for (int k = 0; k < 8; ++k)
+            if (i + k >= n) mf[k] = rf[k] = 0.0f;
+    }
+    uint32_t scales = block_scale(largest8(mf)) | block_scale(largest8(rf)) << 16;     // larger numbers have larger scales
+    scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 1));
+    scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 2));
+    const uint32_t mk = scales & 0xffffu, rk = scales >> 16;
+    store_codes(t.m, i, n, fast, to_codes<false>(mf, mk, word));
+    store_codes(t.v, i, n, fast, to_codes<true>(rf, rk, word));
+    if ((threadIdx.x & 3) == 0 && i < n) {
+        t.m_scale[i >> 5] = (uint8_t)mk;
+        t.v_scale[i >> 5] = (uint8_t)rk;
     }
 }
 
-template <int N>
+// The run of tiles [lo, hi) of this CTA
+template <int N, typename F>
+__device__ __forceinline__ void each_tile(const Table<N>& tab, F f) {
+    const uint32_t lo = (uint32_t)((uint64_t)tab.tiles * blockIdx.x / gridDim.x);
+    const uint32_t hi = (uint32_t)((uint64_t)tab.tiles * (blockIdx.x + 1) / gridDim.x);
+    int i = tab.start[blockIdx.x];
+    uint32_t next = i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles;
+    for (uint32_t tile = lo; tile < hi; ++tile) {
+        while (tile >= next) {
+            ++i;
+            next = i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles;
+        }
+        f(tab.t[i], (int64_t)(tile - tab.t[i].tile0) * kTile);
+    }
+}
+
+template <int N, int BITS>
 __global__ void __launch_bounds__(kThreads) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
     __shared__ double bias[2];
     __shared__ int64_t step_now;
@@ -350,11 +397,7 @@ __global__ void __launch_bounds__(kThreads) pods_adamw_kernel(const __grid_const
     c.root = (float)(1.0 / sqrt(b2));
     c.eps = a.eps;
     const uint32_t key = mix(mix(mix((uint32_t)a.seed + 0x9e3779b9u) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
-    for (uint32_t tile = blockIdx.x; tile < tab.tiles; tile += gridDim.x) {
-        const Tensor& t = tensor_of(tab, tile);
-        if (t.bits == 32) adamw_tile<32>(t, tile, a, c, key);
-        else adamw_tile<8>(t, tile, a, c, key);
-    }
+    each_tile(tab, [&](const Tensor& t, int64_t base) { adamw_tile<BITS>(t, base, a, c, key); });
 }
 
 // ---- norm -------------------------------------------------------------------------------------------------------------
@@ -363,27 +406,21 @@ __global__ void __launch_bounds__(kThreads) pods_adamw_kernel(const __grid_const
 template <int N>
 __global__ void __launch_bounds__(kThreads) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
     double sum = 0.0;
-    for (uint32_t tile = blockIdx.x; tile < tab.tiles; tile += gridDim.x) {
-        const Tensor& t = tensor_of(tab, tile);
-        const int64_t base = (int64_t)(tile - t.tile0) * kTile;
-        Raw4 g[kUnroll];
-        const bool fast = t.aligned && base + kTile <= t.n;
+    each_tile(tab, [&](const Tensor& t, int64_t base) {
+        const int64_t i = base + (int64_t)threadIdx.x * 8;
+        const int vectors = base + kTile <= t.n ? t.vectors : 0;
+        const Raw8 g = vectors ? load8(t.g, t.g_type, i, vectors) : gather8(t.g, t.g_type, i, t.n);
+        float x[8];
+        to_floats(g, t.g_type, x);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int64_t i = base + (int64_t)(u * kThreads + threadIdx.x) * 4;
-            g[u] = fast ? load4(t.g, t.g_type, i) : gather4(t.g, t.g_type, i, t.n);
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            float x[4];
-            to_floats(g[u], t.g_type, x);
-            const float q = (x[0] * x[0] + x[1] * x[1]) + (x[2] * x[2] + x[3] * x[3]);
+        for (int h = 0; h < 8; h += 4) {
+            const float q = (x[h] * x[h] + x[h + 1] * x[h + 1]) + (x[h + 2] * x[h + 2] + x[h + 3] * x[h + 3]);
             if (q > 1e-24f && q < 1e38f) sum += (double)q;
             else
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum += (double)x[k] * (double)x[k];
+                for (int k = h; k < h + 4; ++k) sum += (double)x[k] * (double)x[k];
         }
-    }
+    });
     __shared__ double scratch[kThreads / 32];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
@@ -414,7 +451,7 @@ __global__ void __launch_bounds__(1024) norm_finish_kernel(const double* parts, 
 size_t esize(int type) { return type == PODS_DTYPE_F32 ? 4 : 2; }
 bool known(int type) { return type == PODS_DTYPE_BF16 || type == PODS_DTYPE_F16 || type == PODS_DTYPE_F32; }
 
-constexpr int64_t kMostElements = (int64_t)1 << 42;   // of a call: 2^30 tiles
+constexpr int64_t kMostElements = (int64_t)1 << 42;   // of a call: 2^31 tiles
 
 int check_table(const pods_adamw_tensor* t, int32_t n, bool all) {
     if (n < 0 || (n > 0 && t == nullptr)) return PODS_ERR_INVALID_ARG;
@@ -438,41 +475,51 @@ int check_table(const pods_adamw_tensor* t, int32_t n, bool all) {
     return PODS_OK;
 }
 
-// Tiles of tensors [from, ...) into the table until it is full; returns the first tensor left, and the element count ahead of it.
+// Tensors [from, ...) of states of `bits` (0: of any) into the table until it is full; returns the first tensor left.  The runs of
+// tiles are for a grid of at most `most` CTAs, which is returned in `grid`.  `first`: elements ahead of tensor `from` in the call.
 template <int N>
-int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, int64_t& first) {
+int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, int bits, int most, int64_t& first, unsigned& grid) {
     tab.count = 0;
-    uint64_t tiles = 0;
+    uint32_t tiles = 0;
     int i = from;
     for (; i < n && tab.count < N; ++i) {
         const pods_adamw_tensor& x = t[i];
-        if (x.n == 0) continue;
-        const uint64_t mine = (uint64_t)((x.n + kTile - 1) / kTile);
-        Tensor& d = tab.t[tab.count++];
-        d = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n, first, (uint32_t)tiles,
-             (uint8_t)x.param_type, (uint8_t)x.grad_type, (uint8_t)x.copy_type, (uint8_t)x.state_bits, 0, x.weight_decay, x.lr_scale};
-        const size_t state = x.state_bits == 32 ? 16 : 4;
-        d.aligned = pods_aligned(x.grad, 4 * esize(x.grad_type)) &&
-                    (x.param == nullptr || (pods_aligned(x.param, 4 * esize(x.param_type)) && pods_all_aligned(state, x.m, x.v) &&
-                                            pods_aligned(x.copy, x.copy == nullptr ? 1 : 4 * esize(x.copy_type))));
-        tiles += mine;
+        if (x.n != 0 && (bits == 0 || x.state_bits == bits)) {
+            Tensor& d = tab.t[tab.count++];
+            d = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n, first, tiles,
+                 (uint8_t)x.param_type, (uint8_t)x.grad_type, (uint8_t)x.copy_type, 0, x.weight_decay, x.lr_scale};
+            for (int level = 1; level <= 2; ++level) {
+                const size_t f = 16 * level;
+                bool on = pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? f : 16);
+                if (bits != 0)
+                    on = on && pods_aligned(x.param, x.param_type == PODS_DTYPE_F32 ? f : 16) && pods_all_aligned(bits == 32 ? f : 8, x.m, x.v) &&
+                         (x.copy == nullptr || pods_aligned(x.copy, x.copy_type == PODS_DTYPE_F32 ? f : 16));
+                if (on) d.vectors = (uint8_t)level;
+            }
+            tiles += (uint32_t)((x.n + kTile - 1) / kTile);
+        }
         first += (x.n + 31) / 32 * 32;
     }
-    tab.tiles = (uint32_t)tiles;
+    tab.tiles = tiles;
+    grid = tiles < (uint32_t)most ? tiles : (unsigned)most;
+    for (unsigned b = 0, at = 0; b < grid; ++b) {
+        const uint32_t lo = (uint32_t)((uint64_t)tiles * b / grid);
+        while ((int)at + 1 < tab.count && tab.t[at + 1].tile0 <= lo) ++at;
+        tab.start[b] = (uint16_t)at;
+    }
     return i;
 }
 
-constexpr int kNormParts = 148 * 8;    // CTAs of the norm at most; their sums are joined by one
+constexpr int kNormCtas = 148 * 6;     // of a launch at most; their sums are joined by one more
 
 template <int N>
 int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& used, cudaStream_t s) {
-    static Table<N> zero;                              // entries that stay unused are copied too
     int64_t first = 0;
     for (int from = 0; from < n;) {
-        Table<N> tab = zero;
-        from = fill(tab, t, from, n, first);
+        Table<N> tab;
+        unsigned grid;
+        from = fill(tab, t, from, n, 0, kNormCtas, first, grid);
         if (tab.count == 0) continue;
-        const unsigned grid = tab.tiles < (uint32_t)kNormParts ? tab.tiles : (uint32_t)kNormParts;
         pods_grad_norm_kernel<N><<<grid, kThreads, 0, s>>>(tab, parts + used);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
         used += (int)grid;
@@ -480,15 +527,15 @@ int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& use
     return PODS_OK;
 }
 
-template <int N>
+template <int N, int BITS>
 int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Step& a, cudaStream_t s) {
-    static Table<N> zero;
     int64_t first = 0;
     for (int from = 0; from < n;) {
-        Table<N> tab = zero;
-        from = fill(tab, t, from, n, first);
+        Table<N> tab;
+        unsigned grid;
+        from = fill(tab, t, from, n, BITS, 148 * 4, first, grid);
         if (tab.count == 0) continue;
-        pods_adamw_kernel<N><<<tab.tiles, kThreads, 0, s>>>(tab, a);
+        pods_adamw_kernel<N, BITS><<<grid, kThreads, 0, s>>>(tab, a);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
     }
     return PODS_OK;
@@ -497,7 +544,7 @@ int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Step& a, cudaStr
 }  // namespace
 
 extern "C" size_t pods_grad_norm_workspace_bytes(int32_t n) {
-    return n < 0 ? 0 : (size_t)(n / kMany + 2) * kNormParts * sizeof(double);
+    return n < 0 ? 0 : (size_t)(n / kMany + 2) * kNormCtas * sizeof(double);
 }
 
 extern "C" int pods_grad_norm(const pods_adamw_tensor* tensors, int32_t n, float scale, float* norm, void* workspace,
@@ -546,5 +593,10 @@ extern "C" int pods_adamw(const pods_adamw_tensor* tensors, int32_t n, int64_t s
     a.stochastic = (flags & PODS_ADAMW_STOCHASTIC) ? 1 : 0;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    return n <= kFew ? adamw_launches<kFew>(tensors, n, a, s) : adamw_launches<kMany>(tensors, n, a, s);
+    int kinds = 0;
+    for (int i = 0; i < n; ++i) kinds |= tensors[i].state_bits;
+    int e = PODS_OK;
+    if (kinds & 32) e = n <= kFew ? adamw_launches<kFew, 32>(tensors, n, a, s) : adamw_launches<kMany, 32>(tensors, n, a, s);
+    if (e == PODS_OK && (kinds & 8)) e = n <= kFew ? adamw_launches<kFew, 8>(tensors, n, a, s) : adamw_launches<kMany, 8>(tensors, n, a, s);
+    return e;
 }
