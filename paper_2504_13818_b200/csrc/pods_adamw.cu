@@ -215,46 +215,66 @@ __device__ __forceinline__ uint32_t block_scale(float top) {
 }
 // Codes of eight numbers in a block of scale k.  A number times 2^(127 - k) 2^-120 has e4m3's exponent where fp32 keeps its
 // own, and e4m3's smallest numbers are fp32's: for all of them the code lies above the lowest 20 bits, and 16 random bits and a
-// half (a number that is on the grid stays) added there carry into it with the probability that keeps the average.
+// half (a number that is on the grid stays) added there carry into it with the probability that keeps the average.  Four bits
+// further up the code is the highest byte: one multiply-add makes it, and bytes are picked, so that the integer pipe, which is
+// the busiest, has little to do.  random: the 16 bits in bytes 1 and 2, 0x80 in byte 0.
 template <bool ROOT>
-__device__ __forceinline__ uint2 to_codes(const float (&x)[8], uint32_t k, const uint32_t (&word)[8]) {
-    uint32_t c[8];
-    float pre = 1.0f, f = __uint_as_float((134u - k) << 23);
+__device__ __forceinline__ uint2 to_codes(float (&x)[8], uint32_t k, const uint32_t (&random)[8]) {
+    float f = __uint_as_float((134u - k) << 23);
     if (k > 133u) {                                    // 2^(7 - k) is no normal number: blocks above 28672, in two factors; NaN
-        pre = 0x1p-120f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= 0x1p-120f;
         f = __uint_as_float((254u - min(k, 253u)) << 23);
     }
+    uint32_t c[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t random = ROOT ? (word[i] * 0x9e3779b1u) >> 12 : word[i] >> 12;
-        uint32_t b = __float_as_uint((k > 133u ? fabsf(x[i]) * pre : fabsf(x[i])) * f) + ((random & 0xffff0u) | 8u);
-        if (ROOT && x[i] > 0.0f) b = max(b, 1u << 20);
-        c[i] = b >> 20;
+        float y = x[i] * f;
+        if (ROOT) y = fmaxf(y, 0x1p-129f);             // the smallest code; a root of 0 is put right by the caller
+        c[i] = __float_as_uint(y) * 16u + random[i];
+        if (!ROOT) c[i] |= __float_as_uint(y) & 0x80000000u;
     }
     uint2 r;
-    r.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
-    r.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
-    if (!ROOT) {
-        const uint32_t a = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0073),
-                                       __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
-        const uint32_t b = __byte_perm(__byte_perm(__float_as_uint(x[4]), __float_as_uint(x[5]), 0x0073),
-                                       __byte_perm(__float_as_uint(x[6]), __float_as_uint(x[7]), 0x0073), 0x5410);
-        r.x |= a & 0x80808080u;
-        r.y |= b & 0x80808080u;
-    }
+    r.x = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
+    r.y = __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410);
     if (k == 255u) r = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
     return r;
 }
 
-__device__ __forceinline__ float sqrt_approx(float x) {    // off by 2^-23 at most
+// Two fp32 numbers an instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+__device__ __forceinline__ float sqrt_fast(float x) {      // off by 2^-23 at most; numbers below FLT_MIN are 0
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float rcp_approx(float x) {     // off by 2^-23 at most
+__device__ __forceinline__ float rcp_fast(float x) {       // off by 2^-23 at most
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float least8(const float (&x)[8]) {
+    float a, b;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
+    return fminf(a, b);
 }
 
 struct Coefs {
@@ -286,14 +306,23 @@ __device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const 
         ms = i < n ? t.m_scale[i >> 5] : 0;
         vs = i < n ? t.v_scale[i >> 5] : 0;
     }
-    uint32_t word[8];
+    // words = mix(number ^ k32), number a multiple of 8 for the first: the eight share the high word and the mix's first step
+    uint32_t low[8], for_m[8], for_r[8];
     if (BITS == 8 || a.stochastic) {
-        const uint64_t number = (uint64_t)(t.first + i);   // a multiple of 8: the eight share the high word
-        const uint32_t high = (uint32_t)(number >> 32), k32 = mix(key + high);
+        const uint64_t number = (uint64_t)(t.first + i);
+        uint32_t x0 = (uint32_t)number ^ mix(key + (uint32_t)(number >> 32));
+        x0 ^= x0 >> 16;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) word[k] = mix(((uint32_t)number + k) ^ k32);
+        for (int k = 0; k < 8; ++k) {
+            uint32_t x = (x0 ^ k) * 0x888ec647u;
+            x = (x ^ (x >> 15)) * 0x246ce511u;
+            const uint32_t word = x ^ (x >> 16);
+            low[k] = word & 0xffffu;
+            for_m[k] = __byte_perm(word, 0x80u, 0x7324);
+            for_r[k] = __byte_perm(word * 0x9e3779b1u, 0x80u, 0x7324);
+        }
     }
-    float pf[8], gf[8], mf[8], vf[8];
+    float pf[8], gf[8], mf[8], vf[8], rf[8];
     to_floats(g, t.g_type, gf);
     to_floats(p, t.p_type, pf);
     if (BITS == 32) {
@@ -302,25 +331,50 @@ __device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const 
     } else {
         codes_to_floats(mc, ms, mf);
         codes_to_floats(vc, vs, vf);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) vf[k] *= vf[k];
     }
-    float rf[8];
+    const uint64_t c_g = pair(c.g, c.g), beta1 = pair(c.beta1, c.beta1), keep1 = pair(c.keep1, c.keep1), beta2 = pair(c.beta2, c.beta2),
+                   keep2 = pair(c.keep2, c.keep2), root = pair(c.root, c.root), eps = pair(c.eps, c.eps), shrink = pair(decay, decay),
+                   minus = pair(-rate, -rate);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float x = gf[k] * c.g;
-        mf[k] = c.beta1 * mf[k] + c.keep1 * x;
-        vf[k] = c.beta2 * vf[k] + c.keep2 * (x * x);
-        rf[k] = sqrt_approx(vf[k]);
-        pf[k] = pf[k] * decay - rate * (mf[k] * rcp_approx(rf[k] * c.root + c.eps));
+    for (int k = 0; k < 8; k += 2) {
+        const uint64_t x = mul2(pair(gf[k], gf[k + 1]), c_g), m2 = fma2(keep1, x, mul2(beta1, pair(mf[k], mf[k + 1])));
+        uint64_t v2 = pair(vf[k], vf[k + 1]);
+        if (BITS == 8) v2 = mul2(v2, v2);
+        v2 = fma2(keep2, mul2(x, x), mul2(beta2, v2));
+        unpair(m2, mf[k], mf[k + 1]);
+        unpair(v2, vf[k], vf[k + 1]);
+        rf[k] = sqrt_fast(vf[k]);
+        rf[k + 1] = sqrt_fast(vf[k + 1]);
+    }
+    const bool tiny = least8(vf) < FLT_MIN;            // zeros mostly, of elements that never had a gradient
+    if (tiny) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) rf[k] = sqrtf(vf[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        float d0, d1;
+        unpair(fma2(pair(rf[k], rf[k + 1]), root, eps), d0, d1);
+        const uint64_t u = mul2(pair(mf[k], mf[k + 1]), pair(rcp_fast(d0), rcp_fast(d1)));
+        unpair(fma2(minus, u, mul2(pair(pf[k], pf[k + 1]), shrink)), pf[k], pf[k + 1]);
     }
     if (t.copy != nullptr) store8(t.copy, t.copy_type, i, n, vectors, from_floats(pf, t.copy_type));
     if (a.stochastic && t.p_type == PODS_DTYPE_BF16) {
+        if (largest8(pf) <= FLT_MAX) {
+            Raw8 r = {};
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + (word[k] & 0xffffu)) & 0xffff0000u);
+            for (int k = 0; k < 4; ++k)
+                r.w[k] = __byte_perm(__float_as_uint(pf[2 * k]) + low[2 * k], __float_as_uint(pf[2 * k + 1]) + low[2 * k + 1], 0x7632);
+            store8(t.p, PODS_DTYPE_BF16, i, n, vectors, r);
+        } else {                                       // what is no number stays none
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + low[k]) & 0xffff0000u);
+            store8(t.p, PODS_DTYPE_BF16, i, n, vectors, from_floats(pf, PODS_DTYPE_BF16));
+        }
+    } else {
+        store8(t.p, t.p_type, i, n, vectors, from_floats(pf, t.p_type));
     }
-    store8(t.p, t.p_type, i, n, vectors, from_floats(pf, t.p_type));
     if (BITS == 32) {
         store8(t.m, PODS_DTYPE_F32, i, n, vectors, from_floats(mf, PODS_DTYPE_F32));
         store8(t.v, PODS_DTYPE_F32, i, n, vectors, from_floats(vf, PODS_DTYPE_F32));
@@ -335,32 +389,43 @@ __device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const 
     scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 1));
     scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 2));
     const uint32_t mk = scales & 0xffffu, rk = scales >> 16;
-    store_codes(t.m, i, n, fast, to_codes<false>(mf, mk, word));
-    store_codes(t.v, i, n, fast, to_codes<true>(rf, rk, word));
+    uint32_t zero_x = 0, zero_y = 0;                   // bytes of the roots that are 0
+    if (tiny || !fast) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            zero_x |= rf[k] == 0.0f ? 0xffu << (8 * k) : 0u;
+            zero_y |= rf[k + 4] == 0.0f ? 0xffu << (8 * k) : 0u;
+        }
+    }
+    store_codes(t.m, i, n, fast, to_codes<false>(mf, mk, for_m));
+    uint2 rc = to_codes<true>(rf, rk, for_r);
+    if (tiny || !fast) {
+        rc.x &= ~zero_x;
+        rc.y &= ~zero_y;
+    }
+    store_codes(t.v, i, n, fast, rc);
     if ((threadIdx.x & 3) == 0 && i < n) {
         t.m_scale[i >> 5] = (uint8_t)mk;
         t.v_scale[i >> 5] = (uint8_t)rk;
     }
 }
 
-// The run of tiles [lo, hi) of this CTA
+// This CTA's run of tiles, a stretch of each tensor at a time: f(tensor, first element, tiles)
 template <int N, typename F>
-__device__ __forceinline__ void each_tile(const Table<N>& tab, F f) {
+__device__ __forceinline__ void each_stretch(const Table<N>& tab, F f) {
     const uint32_t lo = (uint32_t)((uint64_t)tab.tiles * blockIdx.x / gridDim.x);
     const uint32_t hi = (uint32_t)((uint64_t)tab.tiles * (blockIdx.x + 1) / gridDim.x);
     int i = tab.start[blockIdx.x];
-    uint32_t next = i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles;
-    for (uint32_t tile = lo; tile < hi; ++tile) {
-        while (tile >= next) {
-            ++i;
-            next = i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles;
-        }
-        f(tab.t[i], (int64_t)(tile - tab.t[i].tile0) * kTile);
+    for (uint32_t tile = lo; tile < hi; ++i) {
+        const Tensor& t = tab.t[i];
+        const uint32_t end = min(hi, i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles);
+        f(t, (int64_t)(tile - t.tile0) * kTile, (int)(end - tile));
+        tile = end;
     }
 }
 
 template <int N, int BITS>
-__global__ void __launch_bounds__(kThreads) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
+__global__ void __launch_bounds__(kThreads, 4) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
     __shared__ double bias[2];
     __shared__ int64_t step_now;
     float clip = a.grad_scale;
@@ -397,7 +462,9 @@ __global__ void __launch_bounds__(kThreads) pods_adamw_kernel(const __grid_const
     c.root = (float)(1.0 / sqrt(b2));
     c.eps = a.eps;
     const uint32_t key = mix(mix(mix((uint32_t)a.seed + 0x9e3779b9u) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
-    each_tile(tab, [&](const Tensor& t, int64_t base) { adamw_tile<BITS>(t, base, a, c, key); });
+    each_stretch(tab, [&](const Tensor& t, int64_t base, int tiles) {
+        for (int k = 0; k < tiles; ++k) adamw_tile<BITS>(t, base + (int64_t)k * kTile, a, c, key);
+    });
 }
 
 // ---- norm -------------------------------------------------------------------------------------------------------------
@@ -406,12 +473,9 @@ __global__ void __launch_bounds__(kThreads) pods_adamw_kernel(const __grid_const
 template <int N>
 __global__ void __launch_bounds__(kThreads) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
     double sum = 0.0;
-    each_tile(tab, [&](const Tensor& t, int64_t base) {
-        const int64_t i = base + (int64_t)threadIdx.x * 8;
-        const int vectors = base + kTile <= t.n ? t.vectors : 0;
-        const Raw8 g = vectors ? load8(t.g, t.g_type, i, vectors) : gather8(t.g, t.g_type, i, t.n);
+    auto add = [&](const Raw8& g, int type) {
         float x[8];
-        to_floats(g, t.g_type, x);
+        to_floats(g, type, x);
 #pragma unroll
         for (int h = 0; h < 8; h += 4) {
             const float q = (x[h] * x[h] + x[h + 1] * x[h + 1]) + (x[h + 2] * x[h + 2] + x[h + 3] * x[h + 3]);
@@ -420,6 +484,21 @@ __global__ void __launch_bounds__(kThreads) pods_grad_norm_kernel(const __grid_c
 #pragma unroll
                 for (int k = h; k < h + 4; ++k) sum += (double)x[k] * (double)x[k];
         }
+    };
+    each_stretch(tab, [&](const Tensor& t, int64_t base, int tiles) {
+        const int type = t.g_type;
+        int64_t i = base + (int64_t)threadIdx.x * 8;
+        const int whole = t.vectors ? (int)min((int64_t)tiles, (t.n - base) / kTile) : 0;
+        int k = 0;
+        for (; k + 4 <= whole; k += 4, i += 4 * kTile) {
+            Raw8 g[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) g[u] = load8(t.g, type, i + u * kTile, t.vectors);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) add(g[u], type);
+        }
+        for (; k < whole; ++k, i += kTile) add(load8(t.g, type, i, t.vectors), type);
+        for (; k < tiles; ++k, i += kTile) add(gather8(t.g, type, i, t.n), type);
     });
     __shared__ double scratch[kThreads / 32];
 #pragma unroll
@@ -533,7 +612,7 @@ int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Step& a, cudaStr
     for (int from = 0; from < n;) {
         Table<N> tab;
         unsigned grid;
-        from = fill(tab, t, from, n, BITS, 148 * 4, first, grid);
+        from = fill(tab, t, from, n, BITS, pods_sm_count() * 4, first, grid);
         if (tab.count == 0) continue;
         pods_adamw_kernel<N, BITS><<<grid, kThreads, 0, s>>>(tab, a);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
