@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTile = kThreads * 8;                    // elements, eight a thread; a multiple of 32
-constexpr int kMostCtas = 148 * 6;                     // of a launch; each takes one run of consecutive tiles
+constexpr int kMostCtas = 148 * 4;                     // of a launch; each takes one run of consecutive tiles
 
 struct Tensor {
     void* p;
@@ -35,7 +35,7 @@ struct Tensor {
     void* copy;
     int64_t n, first;                  // elements; the number of the first one among all of the call
     uint32_t tile0;                    // tiles of this launch ahead of it
-    uint8_t p_type, g_type, copy_type;
+    uint8_t g_type, copy_type;
     uint8_t vectors;                   // 2: eight elements of every buffer lie on their boundary (32 bytes of fp32), 1: 16 bytes, 0: neither
     float decay, lr_scale;
 };
@@ -80,7 +80,7 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 struct Raw8 {
     uint32_t w[8];
 };
-__device__ __forceinline__ Raw8 load8(const void* base, int type, int64_t i, int vectors) {
+__device__ __forceinline__ Raw8 load8(const void* base, int type, uint32_t i, int vectors) {
     Raw8 r = {};
     if (type == PODS_DTYPE_F32) {
         const float* at = static_cast<const float*>(base) + i;
@@ -98,12 +98,12 @@ __device__ __forceinline__ Raw8 load8(const void* base, int type, int64_t i, int
     }
     return r;
 }
-// Element by element: ends of a tensor, and tensors that do not lie on the vectors' boundaries.
-__device__ __forceinline__ Raw8 gather8(const void* base, int type, int64_t i, int64_t n) {
+// Element by element, the first n of eight: ends of a tensor, and tensors that do not lie on the vectors' boundaries.
+__device__ __forceinline__ Raw8 gather8(const void* base, int type, uint32_t i, int n) {
     Raw8 r = {};
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (i + k < n) {
+        if (k < n) {
             if (type == PODS_DTYPE_F32) r.w[k] = static_cast<const uint32_t*>(base)[i + k];
             else r.w[k >> 1] |= (uint32_t) static_cast<const uint16_t*>(base)[i + k] << (16 * (k & 1));
         }
@@ -145,7 +145,7 @@ __device__ __forceinline__ Raw8 from_floats(const float (&x)[8], int type) {
     }
     return r;
 }
-__device__ __forceinline__ void store8(void* base, int type, int64_t i, int64_t n, int vectors, const Raw8& r) {
+__device__ __forceinline__ void store8(void* base, int type, uint32_t i, int n, int vectors, const Raw8& r) {
     if (vectors) {
         if (type == PODS_DTYPE_F32) {
             float* at = static_cast<float*>(base) + i;
@@ -163,23 +163,23 @@ __device__ __forceinline__ void store8(void* base, int type, int64_t i, int64_t 
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (i + k < n) {
+        if (k < n) {
             if (type == PODS_DTYPE_F32) static_cast<uint32_t*>(base)[i + k] = r.w[k];
             else static_cast<uint16_t*>(base)[i + k] = (uint16_t)(r.w[k >> 1] >> (16 * (k & 1)));
         }
 }
 
 // ---- e4m3 blocks: a block of 32 is held by four lanes -----------------------------------------------------------------------
-__device__ __forceinline__ uint2 load_codes(const void* base, int64_t i, int64_t n, bool fast) {
+__device__ __forceinline__ uint2 load_codes(const void* base, uint32_t i, int n, bool fast) {
     const uint8_t* at = static_cast<const uint8_t*>(base) + i;
     if (fast) return *reinterpret_cast<const uint2*>(at);
     uint2 r = make_uint2(0, 0);
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (i + k < n) (k < 4 ? r.x : r.y) |= (uint32_t)at[k] << (8 * (k & 3));
+        if (k < n) (k < 4 ? r.x : r.y) |= (uint32_t)at[k] << (8 * (k & 3));
     return r;
 }
-__device__ __forceinline__ void store_codes(void* base, int64_t i, int64_t n, bool fast, uint2 c) {
+__device__ __forceinline__ void store_codes(void* base, uint32_t i, int n, bool fast, uint2 c) {
     uint8_t* at = static_cast<uint8_t*>(base) + i;
     if (fast) {
         *reinterpret_cast<uint2*>(at) = c;
@@ -187,7 +187,7 @@ __device__ __forceinline__ void store_codes(void* base, int64_t i, int64_t n, bo
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (i + k < n) at[k] = (uint8_t)((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
+        if (k < n) at[k] = (uint8_t)((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
 }
 __device__ __forceinline__ void codes_to_floats(uint2 codes, uint32_t scale, float (&x)[8]) {
     const float s = __uint_as_float(scale << 23);
@@ -281,35 +281,48 @@ struct Coefs {
     float g, beta1, beta2, keep1, keep2, lr, step, root, eps;
 };
 
+// A thread's eight elements of a tile, and what they are stored with.
 template <int BITS>
-__device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const Step& a, const Coefs& c, uint32_t key) {
-    const float decay = 1.0f - c.lr * t.lr_scale * t.decay, rate = c.step * t.lr_scale;
-    const int64_t i = base + (int64_t)threadIdx.x * 8, n = t.n;
-    const int vectors = base + kTile <= n ? t.vectors : 0;
-    const bool fast = vectors != 0;
+struct Loaded {
     Raw8 g, p, m, v;
     uint2 mc, vc;
     uint32_t ms, vs;
+};
+
+// `off`: elements into the stretch; left: elements of the tensor from the tile's first on.  PT, GT: types of parameter and gradient.
+// FAST: whole tiles of tensors on the vectors' boundaries.
+template <int PT, int GT, int BITS, bool FAST>
+__device__ __forceinline__ void load_tile(Loaded<BITS>& d, const Tensor& at, int vectors, uint32_t off, int left) {
+    const int n = FAST ? 8 : left - (int)threadIdx.x * 8;         // the thread's elements and those behind
+    constexpr bool fast = FAST;
     if (fast) {
-        g = load8(t.g, t.g_type, i, vectors);
-        p = load8(t.p, t.p_type, i, vectors);
+        d.g = load8(at.g, GT, off, vectors);
+        d.p = load8(at.p, PT, off, vectors);
     } else {
-        g = gather8(t.g, t.g_type, i, n);
-        p = gather8(t.p, t.p_type, i, n);
+        d.g = gather8(at.g, GT, off, n);
+        d.p = gather8(at.p, PT, off, n);
     }
     if (BITS == 32) {
-        m = fast ? load8(t.m, PODS_DTYPE_F32, i, vectors) : gather8(t.m, PODS_DTYPE_F32, i, n);
-        v = fast ? load8(t.v, PODS_DTYPE_F32, i, vectors) : gather8(t.v, PODS_DTYPE_F32, i, n);
+        d.m = fast ? load8(at.m, PODS_DTYPE_F32, off, vectors) : gather8(at.m, PODS_DTYPE_F32, off, n);
+        d.v = fast ? load8(at.v, PODS_DTYPE_F32, off, vectors) : gather8(at.v, PODS_DTYPE_F32, off, n);
     } else {
-        mc = load_codes(t.m, i, n, fast);
-        vc = load_codes(t.v, i, n, fast);
-        ms = i < n ? t.m_scale[i >> 5] : 0;
-        vs = i < n ? t.v_scale[i >> 5] : 0;
+        d.mc = load_codes(at.m, off, n, fast);
+        d.vc = load_codes(at.v, off, n, fast);
+        d.ms = n > 0 ? at.m_scale[off >> 5] : 0;
+        d.vs = n > 0 ? at.v_scale[off >> 5] : 0;
     }
+}
+
+template <int PT, int GT, int BITS, bool FAST>
+__device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& t, const Tensor& at, uint32_t off, int left, const Step& a,
+                                           const Coefs& c, float decay, float rate, uint64_t first, uint32_t key) {
+    const int vectors = FAST ? t.vectors : 0;
+    constexpr bool fast = FAST;
+    const int n = FAST ? 8 : left - (int)threadIdx.x * 8;
     // words = mix(number ^ k32), number a multiple of 8 for the first: the eight share the high word and the mix's first step
     uint32_t low[8], for_m[8], for_r[8];
     if (BITS == 8 || a.stochastic) {
-        const uint64_t number = (uint64_t)(t.first + i);
+        const uint64_t number = first + off;
         uint32_t x0 = (uint32_t)number ^ mix(key + (uint32_t)(number >> 32));
         x0 ^= x0 >> 16;
 #pragma unroll
@@ -323,14 +336,14 @@ __device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const 
         }
     }
     float pf[8], gf[8], mf[8], vf[8], rf[8];
-    to_floats(g, t.g_type, gf);
-    to_floats(p, t.p_type, pf);
+    to_floats(d.g, GT, gf);
+    to_floats(d.p, PT, pf);
     if (BITS == 32) {
-        to_floats(m, PODS_DTYPE_F32, mf);
-        to_floats(v, PODS_DTYPE_F32, vf);
+        to_floats(d.m, PODS_DTYPE_F32, mf);
+        to_floats(d.v, PODS_DTYPE_F32, vf);
     } else {
-        codes_to_floats(mc, ms, mf);
-        codes_to_floats(vc, vs, vf);
+        codes_to_floats(d.mc, d.ms, mf);
+        codes_to_floats(d.vc, d.vs, vf);
     }
     const uint64_t c_g = pair(c.g, c.g), beta1 = pair(c.beta1, c.beta1), keep1 = pair(c.keep1, c.keep1), beta2 = pair(c.beta2, c.beta2),
                    keep2 = pair(c.keep2, c.keep2), root = pair(c.root, c.root), eps = pair(c.eps, c.eps), shrink = pair(decay, decay),
@@ -358,32 +371,32 @@ __device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const 
         const uint64_t u = mul2(pair(mf[k], mf[k + 1]), pair(rcp_fast(d0), rcp_fast(d1)));
         unpair(fma2(minus, u, mul2(pair(pf[k], pf[k + 1]), shrink)), pf[k], pf[k + 1]);
     }
-    if (t.copy != nullptr) store8(t.copy, t.copy_type, i, n, vectors, from_floats(pf, t.copy_type));
-    if (a.stochastic && t.p_type == PODS_DTYPE_BF16) {
+    if (at.copy != nullptr) store8(at.copy, t.copy_type, off, n, vectors, from_floats(pf, t.copy_type));
+    if (PT == PODS_DTYPE_BF16 && a.stochastic) {
         if (largest8(pf) <= FLT_MAX) {
             Raw8 r = {};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 r.w[k] = __byte_perm(__float_as_uint(pf[2 * k]) + low[2 * k], __float_as_uint(pf[2 * k + 1]) + low[2 * k + 1], 0x7632);
-            store8(t.p, PODS_DTYPE_BF16, i, n, vectors, r);
+            store8(at.p, PODS_DTYPE_BF16, off, n, vectors, r);
         } else {                                       // what is no number stays none
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + low[k]) & 0xffff0000u);
-            store8(t.p, PODS_DTYPE_BF16, i, n, vectors, from_floats(pf, PODS_DTYPE_BF16));
+            store8(at.p, PODS_DTYPE_BF16, off, n, vectors, from_floats(pf, PODS_DTYPE_BF16));
         }
     } else {
-        store8(t.p, t.p_type, i, n, vectors, from_floats(pf, t.p_type));
+        store8(at.p, PT, off, n, vectors, from_floats(pf, PT));
     }
     if (BITS == 32) {
-        store8(t.m, PODS_DTYPE_F32, i, n, vectors, from_floats(mf, PODS_DTYPE_F32));
-        store8(t.v, PODS_DTYPE_F32, i, n, vectors, from_floats(vf, PODS_DTYPE_F32));
+        store8(at.m, PODS_DTYPE_F32, off, n, vectors, from_floats(mf, PODS_DTYPE_F32));
+        store8(at.v, PODS_DTYPE_F32, off, n, vectors, from_floats(vf, PODS_DTYPE_F32));
         return;
     }
     if (!fast) {                                       // what lies behind the tensor's end counts nothing
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (i + k >= n) mf[k] = rf[k] = 0.0f;
+            if (k >= n) mf[k] = rf[k] = 0.0f;
     }
     uint32_t scales = block_scale(largest8(mf)) | block_scale(largest8(rf)) << 16;     // larger numbers have larger scales
     scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 1));
@@ -397,16 +410,16 @@ __device__ __forceinline__ void adamw_tile(const Tensor& t, int64_t base, const 
             zero_y |= rf[k + 4] == 0.0f ? 0xffu << (8 * k) : 0u;
         }
     }
-    store_codes(t.m, i, n, fast, to_codes<false>(mf, mk, for_m));
+    store_codes(at.m, off, n, fast, to_codes<false>(mf, mk, for_m));
     uint2 rc = to_codes<true>(rf, rk, for_r);
     if (tiny || !fast) {
         rc.x &= ~zero_x;
         rc.y &= ~zero_y;
     }
-    store_codes(t.v, i, n, fast, rc);
-    if ((threadIdx.x & 3) == 0 && i < n) {
-        t.m_scale[i >> 5] = (uint8_t)mk;
-        t.v_scale[i >> 5] = (uint8_t)rk;
+    store_codes(at.v, off, n, fast, rc);
+    if ((threadIdx.x & 3) == 0 && n > 0) {
+        at.m_scale[off >> 5] = (uint8_t)mk;
+        at.v_scale[off >> 5] = (uint8_t)rk;
     }
 }
 
@@ -424,8 +437,12 @@ __device__ __forceinline__ void each_stretch(const Table<N>& tab, F f) {
     }
 }
 
-template <int N, int BITS>
-__global__ void __launch_bounds__(kThreads, 4) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
+__device__ __forceinline__ size_t bytes_of(int type) { return type == PODS_DTYPE_F32 ? 4 : 2; }
+
+constexpr int kCtas8 = 3, kCtas32 = 4;                 // an SM
+
+template <int N, int PT, int GT, int BITS>
+__global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
     __shared__ double bias[2];
     __shared__ int64_t step_now;
     float clip = a.grad_scale;
@@ -463,7 +480,52 @@ __global__ void __launch_bounds__(kThreads, 4) pods_adamw_kernel(const __grid_co
     c.eps = a.eps;
     const uint32_t key = mix(mix(mix((uint32_t)a.seed + 0x9e3779b9u) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
     each_stretch(tab, [&](const Tensor& t, int64_t base, int tiles) {
-        for (int k = 0; k < tiles; ++k) adamw_tile<BITS>(t, base + (int64_t)k * kTile, a, c, key);
+        // the stretch's own addresses, so that offsets in it have 32 bits (at most 2^40 elements over the CTAs of a full grid)
+        Tensor at;
+        at.g = static_cast<const char*>(t.g) + base * bytes_of(GT);
+        at.p = static_cast<char*>(t.p) + base * bytes_of(PT);
+        at.m = static_cast<char*>(t.m) + base * (BITS == 32 ? 4 : 1);
+        at.v = static_cast<char*>(t.v) + base * (BITS == 32 ? 4 : 1);
+        at.m_scale = t.m_scale + (base >> 5);
+        at.v_scale = t.v_scale + (base >> 5);
+        at.copy = t.copy == nullptr ? nullptr : static_cast<char*>(t.copy) + base * bytes_of(t.copy_type);
+        const float decay = 1.0f - c.lr * t.lr_scale * t.decay, rate = c.step * t.lr_scale;
+        // in registers: read from the table again for each tile they cost more than the arithmetic of an element
+        asm volatile("" : "+l"(at.g), "+l"(at.p), "+l"(at.m), "+l"(at.v));
+        if (BITS == 8) asm volatile("" : "+l"(at.m_scale), "+l"(at.v_scale));
+        const int64_t behind = t.n - base;
+        const int whole = t.vectors ? (int)min((int64_t)tiles, behind / kTile) : 0;
+        const uint64_t first = (uint64_t)(t.first + base);
+        uint32_t off = threadIdx.x * 8;
+        int k = 0;
+        if (BITS == 8) {                               // two tiles in turn, each loaded while the other is worked on
+            Loaded<BITS> x, y;
+            if (whole > 0) load_tile<PT, GT, BITS, true>(x, at, t.vectors, off, 0);
+#pragma unroll 1
+            for (; k < whole; k += 2, off += 2 * kTile) {
+                if (k + 1 < whole) load_tile<PT, GT, BITS, true>(y, at, t.vectors, off + kTile, 0);
+                adamw_tile<PT, GT, BITS, true>(x, t, at, off, 0, a, c, decay, rate, first, key);
+                if (k + 1 >= whole) break;
+                if (k + 2 < whole) load_tile<PT, GT, BITS, true>(x, at, t.vectors, off + 2 * kTile, 0);
+                adamw_tile<PT, GT, BITS, true>(y, t, at, off + kTile, 0, a, c, decay, rate, first, key);
+            }
+            k = whole;
+            off = threadIdx.x * 8 + whole * kTile;
+        } else {
+#pragma unroll 1
+            for (; k < whole; ++k, off += kTile) {
+                Loaded<BITS> x;
+                load_tile<PT, GT, BITS, true>(x, at, t.vectors, off, 0);
+                adamw_tile<PT, GT, BITS, true>(x, t, at, off, 0, a, c, decay, rate, first, key);
+            }
+        }
+#pragma unroll 1
+        for (; k < tiles; ++k, off += kTile) {
+            const int left = (int)min((int64_t)kTile, behind - (int64_t)k * kTile);
+            Loaded<BITS> x;
+            load_tile<PT, GT, BITS, false>(x, at, 0, off, left);
+            adamw_tile<PT, GT, BITS, false>(x, t, at, off, left, a, c, decay, rate, first, key);
+        }
     });
 }
 
@@ -471,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 4) pods_adamw_kernel(const __grid_co
 // Squares of four in fp32, everything beyond in fp64; where a sum of four leaves the middle of fp32's range its squares are
 // taken again in fp64, so that neither large nor small gradients are lost.
 template <int N>
-__global__ void __launch_bounds__(kThreads) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
+__global__ void __launch_bounds__(kThreads, 4) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
     double sum = 0.0;
     auto add = [&](const Raw8& g, int type) {
         float x[8];
@@ -487,18 +549,19 @@ __global__ void __launch_bounds__(kThreads) pods_grad_norm_kernel(const __grid_c
     };
     each_stretch(tab, [&](const Tensor& t, int64_t base, int tiles) {
         const int type = t.g_type;
-        int64_t i = base + (int64_t)threadIdx.x * 8;
+        const char* const at = static_cast<const char*>(t.g) + base * bytes_of(type);
+        uint32_t i = threadIdx.x * 8;
         const int whole = t.vectors ? (int)min((int64_t)tiles, (t.n - base) / kTile) : 0;
         int k = 0;
         for (; k + 4 <= whole; k += 4, i += 4 * kTile) {
             Raw8 g[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) g[u] = load8(t.g, type, i + u * kTile, t.vectors);
+            for (int u = 0; u < 4; ++u) g[u] = load8(at, type, i + u * kTile, t.vectors);
 #pragma unroll
             for (int u = 0; u < 4; ++u) add(g[u], type);
         }
-        for (; k < whole; ++k, i += kTile) add(load8(t.g, type, i, t.vectors), type);
-        for (; k < tiles; ++k, i += kTile) add(gather8(t.g, type, i, t.n), type);
+        for (; k < whole; ++k, i += kTile) add(load8(at, type, i, t.vectors), type);
+        for (; k < tiles; ++k, i += kTile) add(gather8(at, type, i, (int)max((int64_t)0, min((int64_t)8, t.n - base - i))), type);
     });
     __shared__ double scratch[kThreads / 32];
 #pragma unroll
@@ -530,7 +593,7 @@ __global__ void __launch_bounds__(1024) norm_finish_kernel(const double* parts, 
 size_t esize(int type) { return type == PODS_DTYPE_F32 ? 4 : 2; }
 bool known(int type) { return type == PODS_DTYPE_BF16 || type == PODS_DTYPE_F16 || type == PODS_DTYPE_F32; }
 
-constexpr int64_t kMostElements = (int64_t)1 << 42;   // of a call: 2^31 tiles
+constexpr int64_t kMostElements = (int64_t)1 << 40;   // of a call
 
 int check_table(const pods_adamw_tensor* t, int32_t n, bool all) {
     if (n < 0 || (n > 0 && t == nullptr)) return PODS_ERR_INVALID_ARG;
@@ -554,24 +617,31 @@ int check_table(const pods_adamw_tensor* t, int32_t n, bool all) {
     return PODS_OK;
 }
 
-// Tensors [from, ...) of states of `bits` (0: of any) into the table until it is full; returns the first tensor left.  The runs of
-// tiles are for a grid of at most `most` CTAs, which is returned in `grid`.  `first`: elements ahead of tensor `from` in the call.
+// What a kernel is made for: the types of parameter and gradient, and the states' bits.
+struct Kind {
+    int p, g, bits;
+    bool operator==(const Kind& o) const { return p == o.p && g == o.g && bits == o.bits; }
+};
+Kind kind_of(const pods_adamw_tensor& x) { return {x.param_type, x.grad_type, x.state_bits}; }
+
+// Tensors [from, ...) of a kind (of any, where none is given) into the table until it is full; returns the first tensor left.
+// `first`: elements ahead of tensor `from` in the call.  The runs of tiles are for `grid` CTAs.
 template <int N>
-int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, int bits, int most, int64_t& first, unsigned& grid) {
+int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, const Kind* kind, int most, int64_t& first, unsigned& grid) {
     tab.count = 0;
     uint32_t tiles = 0;
     int i = from;
     for (; i < n && tab.count < N; ++i) {
         const pods_adamw_tensor& x = t[i];
-        if (x.n != 0 && (bits == 0 || x.state_bits == bits)) {
+        if (x.n != 0 && (kind == nullptr || kind_of(x) == *kind)) {
             Tensor& d = tab.t[tab.count++];
-            d = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n, first, tiles,
-                 (uint8_t)x.param_type, (uint8_t)x.grad_type, (uint8_t)x.copy_type, 0, x.weight_decay, x.lr_scale};
+            d = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n, first, tiles, (uint8_t)x.grad_type, (uint8_t)x.copy_type, 0,
+                 x.weight_decay, x.lr_scale};
             for (int level = 1; level <= 2; ++level) {
                 const size_t f = 16 * level;
                 bool on = pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? f : 16);
-                if (bits != 0)
-                    on = on && pods_aligned(x.param, x.param_type == PODS_DTYPE_F32 ? f : 16) && pods_all_aligned(bits == 32 ? f : 8, x.m, x.v) &&
+                if (kind != nullptr)
+                    on = on && pods_aligned(x.param, x.param_type == PODS_DTYPE_F32 ? f : 16) && pods_all_aligned(x.state_bits == 32 ? f : 8, x.m, x.v) &&
                          (x.copy == nullptr || pods_aligned(x.copy, x.copy_type == PODS_DTYPE_F32 ? f : 16));
                 if (on) d.vectors = (uint8_t)level;
             }
@@ -589,7 +659,10 @@ int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, int bits, i
     return i;
 }
 
-constexpr int kNormCtas = 148 * 6;     // of a launch at most; their sums are joined by one more
+int most_ctas(int per_sm) {
+    const int n = pods_sm_count() * per_sm;
+    return n < kMostCtas ? n : kMostCtas;
+}
 
 template <int N>
 int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& used, cudaStream_t s) {
@@ -597,7 +670,7 @@ int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& use
     for (int from = 0; from < n;) {
         Table<N> tab;
         unsigned grid;
-        from = fill(tab, t, from, n, 0, kNormCtas, first, grid);
+        from = fill(tab, t, from, n, nullptr, most_ctas(4), first, grid);
         if (tab.count == 0) continue;
         pods_grad_norm_kernel<N><<<grid, kThreads, 0, s>>>(tab, parts + used);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
@@ -606,15 +679,35 @@ int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& use
     return PODS_OK;
 }
 
-template <int N, int BITS>
-int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Step& a, cudaStream_t s) {
+template <int N, int PT, int GT, int BITS>
+void launch_kind(const Table<N>& tab, const Step& a, unsigned grid, cudaStream_t s) {
+    pods_adamw_kernel<N, PT, GT, BITS><<<grid, kThreads, 0, s>>>(tab, a);
+}
+template <int N, int PT>
+void launch_kind(const Table<N>& tab, const Step& a, unsigned grid, cudaStream_t s, const Kind& k) {
+    constexpr int B = PODS_DTYPE_BF16, H = PODS_DTYPE_F16, F = PODS_DTYPE_F32;
+    if (k.bits == 32) {
+        if (k.g == B) launch_kind<N, PT, B, 32>(tab, a, grid, s);
+        else if (k.g == H) launch_kind<N, PT, H, 32>(tab, a, grid, s);
+        else launch_kind<N, PT, F, 32>(tab, a, grid, s);
+    } else {
+        if (k.g == B) launch_kind<N, PT, B, 8>(tab, a, grid, s);
+        else if (k.g == H) launch_kind<N, PT, H, 8>(tab, a, grid, s);
+        else launch_kind<N, PT, F, 8>(tab, a, grid, s);
+    }
+}
+
+template <int N>
+int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Kind& k, const Step& a, cudaStream_t s) {
     int64_t first = 0;
     for (int from = 0; from < n;) {
         Table<N> tab;
         unsigned grid;
-        from = fill(tab, t, from, n, BITS, pods_sm_count() * 4, first, grid);
+        from = fill(tab, t, from, n, &k, most_ctas(k.bits == 8 ? kCtas8 : kCtas32), first, grid);
         if (tab.count == 0) continue;
-        pods_adamw_kernel<N, BITS><<<grid, kThreads, 0, s>>>(tab, a);
+        if (k.p == PODS_DTYPE_BF16) launch_kind<N, PODS_DTYPE_BF16>(tab, a, grid, s, k);
+        else if (k.p == PODS_DTYPE_F16) launch_kind<N, PODS_DTYPE_F16>(tab, a, grid, s, k);
+        else launch_kind<N, PODS_DTYPE_F32>(tab, a, grid, s, k);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
     }
     return PODS_OK;
@@ -623,7 +716,7 @@ int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Step& a, cudaStr
 }  // namespace
 
 extern "C" size_t pods_grad_norm_workspace_bytes(int32_t n) {
-    return n < 0 ? 0 : (size_t)(n / kMany + 2) * kNormCtas * sizeof(double);
+    return n < 0 ? 0 : (size_t)(n / kMany + 2) * kMostCtas * sizeof(double);
 }
 
 extern "C" int pods_grad_norm(const pods_adamw_tensor* tensors, int32_t n, float scale, float* norm, void* workspace,
@@ -672,10 +765,16 @@ extern "C" int pods_adamw(const pods_adamw_tensor* tensors, int32_t n, int64_t s
     a.stochastic = (flags & PODS_ADAMW_STOCHASTIC) ? 1 : 0;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
-    int kinds = 0;
-    for (int i = 0; i < n; ++i) kinds |= tensors[i].state_bits;
+    // a launch for each kind of tensor; sets have one or two
     int e = PODS_OK;
-    if (kinds & 32) e = n <= kFew ? adamw_launches<kFew, 32>(tensors, n, a, s) : adamw_launches<kMany, 32>(tensors, n, a, s);
-    if (e == PODS_OK && (kinds & 8)) e = n <= kFew ? adamw_launches<kFew, 8>(tensors, n, a, s) : adamw_launches<kMany, 8>(tensors, n, a, s);
+    uint32_t done = 0;
+    for (int i = 0; i < n && e == PODS_OK; ++i) {
+        if (tensors[i].n == 0) continue;
+        const Kind k = kind_of(tensors[i]);
+        const uint32_t bit = 1u << (k.p * 6 + k.g * 2 + (k.bits == 8 ? 1 : 0));
+        if (done & bit) continue;
+        done |= bit;
+        e = n <= kFew ? adamw_launches<kFew>(tensors, n, k, a, s) : adamw_launches<kMany>(tensors, n, k, a, s);
+    }
     return e;
 }
