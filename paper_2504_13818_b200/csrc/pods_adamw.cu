@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTile = kThreads * 8;                    // elements, eight a thread; a multiple of 32
-constexpr int kMostCtas = 148 * 4;                     // of a launch; each takes one run of consecutive tiles
+constexpr int kMostCtas = 148 * 8;                     // of a launch; each takes one run of consecutive tiles
 
 struct Tensor {
     void* p;
@@ -439,7 +439,7 @@ __device__ __forceinline__ void each_stretch(const Table<N>& tab, F f) {
 
 __device__ __forceinline__ size_t bytes_of(int type) { return type == PODS_DTYPE_F32 ? 4 : 2; }
 
-constexpr int kCtas8 = 3, kCtas32 = 4;                 // an SM
+constexpr int kCtas8 = 3, kCtas32 = 3;                 // an SM
 
 template <int N, int PT, int GT, int BITS>
 __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
         at.copy = t.copy == nullptr ? nullptr : static_cast<char*>(t.copy) + base * bytes_of(t.copy_type);
         const float decay = 1.0f - c.lr * t.lr_scale * t.decay, rate = c.step * t.lr_scale;
         // in registers: read from the table again for each tile they cost more than the arithmetic of an element
-        asm volatile("" : "+l"(at.g), "+l"(at.p), "+l"(at.m), "+l"(at.v));
+        if (BITS == 8) asm volatile("" : "+l"(at.g), "+l"(at.p), "+l"(at.m), "+l"(at.v));
         if (BITS == 8) asm volatile("" : "+l"(at.m_scale), "+l"(at.v_scale));
         const int64_t behind = t.n - base;
         const int whole = t.vectors ? (int)min((int64_t)tiles, behind / kTile) : 0;
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
 // Squares of four in fp32, everything beyond in fp64; where a sum of four leaves the middle of fp32's range its squares are
 // taken again in fp64, so that neither large nor small gradients are lost.
 template <int N>
-__global__ void __launch_bounds__(kThreads, 4) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
+__global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
     double sum = 0.0;
     auto add = [&](const Raw8& g, int type) {
         float x[8];
@@ -553,12 +553,12 @@ __global__ void __launch_bounds__(kThreads, 4) pods_grad_norm_kernel(const __gri
         uint32_t i = threadIdx.x * 8;
         const int whole = t.vectors ? (int)min((int64_t)tiles, (t.n - base) / kTile) : 0;
         int k = 0;
-        for (; k + 4 <= whole; k += 4, i += 4 * kTile) {
-            Raw8 g[4];
+        for (; k + 2 <= whole; k += 2, i += 2 * kTile) {
+            Raw8 g[2];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) g[u] = load8(at, type, i + u * kTile, t.vectors);
+            for (int u = 0; u < 2; ++u) g[u] = load8(at, type, i + u * kTile, t.vectors);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) add(g[u], type);
+            for (int u = 0; u < 2; ++u) add(g[u], type);
         }
         for (; k < whole; ++k, i += kTile) add(load8(at, type, i, t.vectors), type);
         for (; k < tiles; ++k, i += kTile) add(gather8(at, type, i, (int)max((int64_t)0, min((int64_t)8, t.n - base - i))), type);
@@ -670,7 +670,7 @@ int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& use
     for (int from = 0; from < n;) {
         Table<N> tab;
         unsigned grid;
-        from = fill(tab, t, from, n, nullptr, most_ctas(4), first, grid);
+        from = fill(tab, t, from, n, nullptr, most_ctas(8), first, grid);
         if (tab.count == 0) continue;
         pods_grad_norm_kernel<N><<<grid, kThreads, 0, s>>>(tab, parts + used);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
