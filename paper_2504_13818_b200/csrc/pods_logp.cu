@@ -35,16 +35,27 @@ __device__ __forceinline__ double pow2_int(int n) {    // n <= 0
     return n < -1000 ? 0.0 : __hiloint2double((1023 + n) << 20, 0);
 }
 
-__device__ __forceinline__ Part join(const Part& a, const Part& b) {
-    Part r;
-    r.R = max(a.R, b.R);
-    r.bad = a.bad | b.bad;
-    const int da = a.R - r.R, db = b.R - r.R;
-    const double fa = pow2_int(da), fb = pow2_int(db);
-    r.s = a.s * fa + b.s * fb;
-    // 2^(y - R) (y - R) = 2^(y - Ra) 2^(Ra - R) (y - Ra + Ra - R); an empty part (s = 0) adds nothing however far its reference
-    r.u = (a.u + (a.s != 0.0 ? a.s * (double)da : 0.0)) * fa + (b.u + (b.s != 0.0 ? b.s * (double)db : 0.0)) * fb;
-    return r;
+// Makes `p` relative to 2^R, R its own or a larger one.
+template <bool ENT>
+__device__ __forceinline__ void move_to(Part& p, int R) {
+    const int d = p.R - R;
+    const double f = pow2_int(d);
+    // 2^(y - R) (y - R) = 2^(y - Rp) 2^(Rp - R) (y - Rp + Rp - R); an empty part adds nothing however far its reference
+    if (ENT) p.u = p.s != 0.0 ? (p.u + p.s * (double)d) * f : 0.0;
+    p.s *= f;
+    p.R = R;
+}
+
+// The parts of a warp's lanes as one, in every lane.
+template <bool ENT>
+__device__ __forceinline__ void join_warp(Part& p) {
+    move_to<ENT>(p, __reduce_max_sync(PODS_FULL_MASK, p.R));
+    p.bad = (int)__reduce_or_sync(PODS_FULL_MASK, (unsigned)p.bad);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        p.s += __shfl_xor_sync(PODS_FULL_MASK, p.s, d);
+        if (ENT) p.u += __shfl_xor_sync(PODS_FULL_MASK, p.u, d);
+    }
 }
 
 // What a thread holds while it goes through its elements.
@@ -56,14 +67,14 @@ struct Sums {
     int R = kNoRef, bad = 0;
 
     // e = 2^(x c - R) of a vector, added up; with ENT also e (x c - R)
-    __device__ __forceinline__ void add(const uint4& q, float c, float R_, float& bs, float& bu) const {
+    __device__ __forceinline__ void add(const uint4& q, float c, float c_lo, float R_, float& bs, float& bu) const {
         float x[E];
         El::unpack(q, x);
-        const unsigned long long c2 = pack2(c, c), off2 = pack2(-R_, -R_);
+        const unsigned long long c2 = pack2(c, c), lo2 = pack2(c_lo, c_lo), off2 = pack2(-R_, -R_);
         unsigned long long acc = 0ull, accu = 0ull;
 #pragma unroll
         for (int i = 0; i < E; i += 2) {
-            const unsigned long long d2 = fma2(pack2(x[i], x[i + 1]), c2, off2);
+            const unsigned long long x2 = pack2(x[i], x[i + 1]), d2 = fma2(x2, lo2, fma2(x2, c2, off2));
             float d0, d1;
             unpack2(d2, d0, d1);
             const unsigned long long e2 = pack2(ex2_approx(d0), ex2_approx(d1));
@@ -79,11 +90,11 @@ struct Sums {
         }
     }
     template <int N>
-    __device__ __forceinline__ void take(const uint4 (&q)[N], float c) {
+    __device__ __forceinline__ void take(const uint4 (&q)[N], float c, float c_lo) {
         float bs = 0.0f, bu = 0.0f;
         const float ref = (float)R;
 #pragma unroll
-        for (int k = 0; k < N; ++k) add(q[k], c, ref, bs, bu);
+        for (int k = 0; k < N; ++k) add(q[k], c, c_lo, ref, bs, bu);
         if (!(bs < kSumLimit)) {                       // rare: the first block, a block far above all before it, NaN, +inf
             float m = -INFINITY;
 #pragma unroll
@@ -103,7 +114,7 @@ struct Sums {
                     }
                     const float now = (float)R;
 #pragma unroll
-                    for (int k = 0; k < N; ++k) add(q[k], c, now, bs, bu);
+                    for (int k = 0; k < N; ++k) add(q[k], c, c_lo, now, bs, bu);
                 }
             }
         }
@@ -120,131 +131,54 @@ __device__ __forceinline__ T warp_reduce(T v, Op op) {
     return v;
 }
 
-// the row in fp64, by one group of `n` threads: what is left where fp32 has no fractional bits for the exponents
+// A row in fp64 by one warp: what is left where fp32 has no fractional bits for the exponents.  top: the largest logit.
 template <int DT>
-__device__ Part row_fp64(const typename Elem<DT>::raw* row, int V, double inv_tau, float top, int at, int n) {
-    Part r = {0.0, 0.0, 0, 0};
-    for (int v = at; v < V; v += n) {
-        const double d = ((double)Elem<DT>::to_float(row[v]) - (double)top) * inv_tau, e = exp64(d);
-        r.s += e;
-        if (e != 0.0) r.u += e * d;
+__device__ __noinline__ Part far_row(const typename Elem<DT>::raw* row, int V, double inv_tau, int lane, float& top) {
+    using El = Elem<DT>;
+    float m = -INFINITY;
+    for (int i = lane; i < V; i += 32) m = max_nan(m, El::to_float(row[i]));
+    m = warp_reduce(m, MaxNan());
+    top = m;
+    Part p = {0.0, 0.0, 0, m < INFINITY ? 0 : 1};
+    if (!(fabsf(m) < INFINITY)) return p;
+    for (int i = lane; i < V; i += 32) {
+        const double d = ((double)El::to_float(row[i]) - (double)m) * inv_tau, e = exp64(d);
+        p.s += e;
+        if (e != 0.0) p.u += e * d;
     }
-    return r;
+    p.s = warp_reduce(p.s, Plus());
+    p.u = warp_reduce(p.u, Plus());
+    return p;
 }
 
-// G threads a row: a warp (eight rows a CTA), or the CTAs of a cluster.  Rows are cut at 16-byte boundaries of memory.
-template <int DT, bool ENT, bool WARP>
-__global__ void __launch_bounds__(kThreads) pods_logp_kernel(const FwdArgs a) {
-    using El = Elem<DT>;
-    using raw = typename El::raw;
-    constexpr int E = El::E;
-    __shared__ Part parts[kMaxCluster * (kThreads / 32)];
-    __shared__ float tops[kThreads / 32];
-    cg::cluster_group cl = cg::this_cluster();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int CL = WARP ? 1 : (int)cl.num_blocks(), rank = WARP ? 0 : (int)cl.block_rank();
-    const int64_t t = WARP ? (int64_t)blockIdx.x * (kThreads / 32) + warp : (int64_t)(blockIdx.x / CL);
-    if (WARP && t >= a.T) return;
-    if (CL > 1) cl.barrier_arrive();                   // met before the first store into another CTA
-    if ((a.mask != nullptr && a.mask[t] == 0) || (a.rows_end != nullptr && t >= *a.rows_end)) {    // the same for the whole cluster
-        if (a.fill && (WARP ? lane : (int)threadIdx.x) == 0 && rank == 0) a.logp[t] = 0.0f;
-        if (CL > 1) cl.barrier_wait();
-        return;
-    }
-    const raw* const row = static_cast<const raw*>(a.logits) + t * a.ldl;
-    const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw));
-    const int head = min(lead, a.V), nvec = (a.V - head) / E, tail = head + nvec * E;
-    const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
-    const int G = WARP ? 32 : kThreads, me = WARP ? lane : (int)threadIdx.x;
-    const int share = (nvec + CL - 1) / CL, lo = min(nvec, rank * share), hi = min(nvec, lo + share);
-    Sums<DT, ENT> sums;
-    int v = lo + me;
-    for (; v + (kBlockVecs - 1) * G < hi; v += kBlockVecs * G) {
-        uint4 q[kBlockVecs];
-#pragma unroll
-        for (int k = 0; k < kBlockVecs; ++k) q[k] = __ldg(vec + v + k * G);
-        sums.take(q, a.c);
-    }
-    for (; v < hi; v += G) {
-        const uint4 q[1] = {__ldg(vec + v)};
-        sums.take(q, a.c);
-    }
-    if (rank == 0) {                                   // the ends: less than 2 E elements
-        const int i = me < head ? me : tail + me - head;
-        if (me < head + a.V - tail && PODS_INDEX_OK(i, a.V, a.status)) {
-            raw e[16 / sizeof(raw)];
-#pragma unroll
-            for (int k = 0; k < E; ++k) e[k] = k == 0 ? row[i] : El::kNegInf;
-            const uint4 q[1] = {*reinterpret_cast<const uint4*>(e)};
-            sums.take(q, a.c);
-        }
-    }
-    Part p = sums.part();
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        Part o;
-        o.s = __shfl_xor_sync(PODS_FULL_MASK, p.s, d);
-        o.u = ENT ? __shfl_xor_sync(PODS_FULL_MASK, p.u, d) : 0.0;
-        o.R = __shfl_xor_sync(PODS_FULL_MASK, p.R, d);
-        o.bad = __shfl_xor_sync(PODS_FULL_MASK, p.bad, d);
-        p = join(p, o);
-    }
-    if (!WARP) {
-        if (CL == 1) {
-            if (lane == 0) parts[warp] = p;
-            __syncthreads();
-        } else {
-            cl.barrier_wait();
-            if (lane == 0) *cl.map_shared_rank(&parts[rank * (kThreads / 32) + warp], 0) = p;
-            cl.sync();
-        }
-        if (rank != 0) return;
-        p = parts[0];
-        for (int i = 1; i < CL * (kThreads / 32); ++i) p = join(p, parts[i]);
-    }
-    // far, or nothing above 2^kNoRef: fp64 tells huge negative logits from a row of -inf
-    const bool far = p.bad == 2 || (p.bad == 0 && p.R == kNoRef);
-    float top = 0.0f;
-    if (far) {
-        float m = -INFINITY;
-        for (int i = me; i < a.V; i += G) m = max_nan(m, El::to_float(row[i]));
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) m = max_nan(m, __shfl_xor_sync(PODS_FULL_MASK, m, d));
-        if (!WARP) {
-            if (lane == 0) tops[warp] = m;
-            __syncthreads();
-            for (int w = 0; w < kThreads / 32; ++w) m = max_nan(m, tops[w]);
-        }
-        top = m;
-        p = {0.0, 0.0, 0, top < INFINITY ? 0 : 1};
-        if (fabsf(top) < INFINITY) {
-            Part q = row_fp64<DT>(row, a.V, a.inv_tau, top, me, G);
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) {
-                q.s += __shfl_xor_sync(PODS_FULL_MASK, q.s, d);
-                q.u += __shfl_xor_sync(PODS_FULL_MASK, q.u, d);
-            }
-            if (!WARP) {
-                __syncthreads();
-                if (lane == 0) parts[warp] = q;
-                __syncthreads();
-                q = parts[0];
-                for (int w = 1; w < kThreads / 32; ++w) {
-                    q.s += parts[w].s;
-                    q.u += parts[w].u;
-                }
-            }
-            p.s = q.s;
-            p.u = q.u;
-        }
-    }
-    if (me != 0) return;
+// What a lane knows of its row's token: its logit.
+template <int DT>
+__device__ __forceinline__ float token_logit(const FwdArgs& a, int64_t t) {
     int token = a.tokens[t];
     if ((unsigned)token >= (unsigned)a.V) {
         pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
         token = 0;
     }
-    const double z = (double)El::to_float(row[token]);
+    return Elem<DT>::to_float((static_cast<const typename Elem<DT>::raw*>(a.logits) + t * a.ldl)[token]);
+}
+
+// A warp's lanes each hold the sums of a row of their own (t < 0: none), and its token's logit: writes the rows' outputs.
+template <int DT, bool ENT>
+__device__ __forceinline__ void finish_rows(const FwdArgs& a, int64_t t, Part p, float z, int lane) {
+    // far, or nothing above 2^kNoRef: fp64 tells huge negative logits from a row of -inf
+    const bool far = t >= 0 && (p.bad == 2 || (p.bad == 0 && p.R == kNoRef));
+    float top = 0.0f;
+    for (unsigned todo = __ballot_sync(PODS_FULL_MASK, far); todo != 0; todo &= todo - 1) {
+        const int who = __ffs(todo) - 1;
+        const int64_t at = __shfl_sync(PODS_FULL_MASK, t, who);
+        float m;
+        const Part q = far_row<DT>(static_cast<const typename Elem<DT>::raw*>(a.logits) + at * a.ldl, a.V, a.inv_tau, lane, m);
+        if (lane == who) {
+            p = q;
+            top = m;
+        }
+    }
+    if (t < 0) return;
     double lse, logp, H;
     if (p.bad & 1) {
         pods_raise(a.status, PODS_STATUS_NONFINITE_LOGIT);
@@ -256,18 +190,262 @@ __global__ void __launch_bounds__(kThreads) pods_logp_kernel(const FwdArgs a) {
     } else if (far) {
         const double ls = log(p.s);
         lse = (double)top * a.inv_tau + ls;
-        logp = (z - (double)top) * a.inv_tau - ls;
+        logp = ((double)z - (double)top) * a.inv_tau - ls;
         H = ls - p.u / p.s;
     } else {
         const double ls = log2(p.s);
         lse = ((double)p.R + ls) * kLn2;
-        logp = ((z * (double)a.c - (double)p.R) - ls) * kLn2;
+        logp = (((double)z * a.c64 - (double)p.R) - ls) * kLn2;
         H = (ls - p.u / p.s) * kLn2;
     }
-    a.logp[t] = (float)fmin(logp, 0.0);
-    if (logp != logp) a.logp[t] = NAN;
+    a.logp[t] = logp == logp ? (float)fmin(logp, 0.0) : NAN;
     if (a.lse != nullptr) a.lse[t] = lse;
     if (ENT) a.entropy[t] = H == H ? (float)fmax(H, 0.0) : NAN;
+}
+
+// Whether row t is to be read; one that is not gets its 0 where the call fills.
+__device__ __forceinline__ bool live_row(const FwdArgs& a, int64_t t, bool fill) {
+    if (t >= a.T) return false;
+    const bool live = (a.mask == nullptr || a.mask[t] != 0) && (a.rows_end == nullptr || t < *a.rows_end);
+    if (!live && fill && a.fill) a.logp[t] = 0.0f;
+    return live;
+}
+
+// The elements of a row outside its whole 16-byte vectors, less than 2 E: one a lane.
+template <int DT, bool ENT>
+__device__ __forceinline__ void take_edges(const FwdArgs& a, const typename Elem<DT>::raw* row, int head, int tail, int lane, Sums<DT, ENT>& sums) {
+    using El = Elem<DT>;
+    const int i = lane < head ? lane : tail + lane - head;
+    if (head + a.V - tail == 0) return;
+    typename El::raw e[El::E];
+#pragma unroll
+    for (int k = 0; k < El::E; ++k) e[k] = El::kNegInf;
+    if (lane < head + a.V - tail && PODS_INDEX_OK(i, a.V, a.status)) e[0] = row[i];
+    uint4 q[1];
+    memcpy(q, e, sizeof q);
+    sums.take(q, a.c, a.c_lo);
+}
+
+template <int DT>
+__device__ __forceinline__ uint4 nothing() {           // a vector of -inf
+    const uint32_t w = DT == PODS_DTYPE_F32 ? (uint32_t)Elem<DT>::kNegInf : (uint32_t)Elem<DT>::kNegInf * 0x10001u;
+    return make_uint4(w, w, w, w);
+}
+
+// Short rows: a warp takes `batch` rows one after the other and finishes them together, a lane each, since a row's logarithms
+// and the chain to its token's logit cost a warp more than 1000 logits.
+template <int DT, bool ENT>
+__global__ void __launch_bounds__(kThreads) pods_logp_rows_kernel(const FwdArgs a, int batch) {
+    using El = Elem<DT>;
+    using raw = typename El::raw;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * batch;
+    if (first >= a.T) return;
+    const int64_t mine = lane < batch && live_row(a, first + lane, true) ? first + lane : -1;
+    const float z = mine >= 0 ? token_logit<DT>(a, mine) : 0.0f;
+    Part kept = {0.0, 0.0, kNoRef, 0};
+    for (unsigned todo = __ballot_sync(PODS_FULL_MASK, mine >= 0); todo != 0; todo &= todo - 1) {
+        const int j = __ffs(todo) - 1;
+        const raw* const row = static_cast<const raw*>(a.logits) + (first + j) * a.ldl;
+        const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw));
+        const int head = min(lead, a.V), nvec = (a.V - head) / El::E, tail = head + nvec * El::E;
+        const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
+        Sums<DT, ENT> sums;
+        for (int v = lane; v - lane < nvec; v += kBlockVecs * 32) {
+            uint4 q[kBlockVecs];
+#pragma unroll
+            for (int k = 0; k < kBlockVecs; ++k) q[k] = v + k * 32 < nvec ? __ldg(vec + v + k * 32) : nothing<DT>();
+            sums.take(q, a.c, a.c_lo);
+        }
+        take_edges(a, row, head, tail, lane, sums);
+        Part p = sums.part();
+        join_warp<ENT>(p);
+        if (lane == j) kept = p;
+    }
+    finish_rows<DT, ENT>(a, mine, kept, z, lane);
+}
+
+// Long rows: a cluster of CTAs holds a share of the row each and goes round over the rows; a CTA is a producer warp that keeps
+// kStages copies of 32 KB in flight, consumer warps that add up what has arrived, and a warp that finishes the rows, 32 at
+// once.  They meet at mbarriers only, so the copies never wait for a row's end.
+constexpr int kConsumers = 16;
+constexpr int kStageVecs = kConsumers * 32 * kBlockVecs;
+constexpr int kStages = 6;
+constexpr int kRing = 4;               // rows whose parts may be waiting to be finished
+
+struct PipePart {                      // a consumer warp's part, as it travels: 16 bytes, with ENT 32
+    double s;
+    unsigned long long ref;            // R above, bad below
+    double u;
+    unsigned long long unused;
+};
+
+struct PipeCtrl {
+    unsigned long long full[kStages], empty[kStages], parts[kRing], free_slot[kRing];
+    alignas(16) PipePart part[kRing][8 * kConsumers];
+};
+
+// Rows of a cluster, a mask of 32 at a time
+struct RowWalk {
+    int64_t first, step;
+    int n;
+    unsigned bits;
+    __device__ __forceinline__ bool live(const FwdArgs& a, int i, int lane, bool fill) {
+        if ((i & 31) == 0) {
+            const bool plain = a.mask == nullptr && a.rows_end == nullptr;
+            bits = plain ? PODS_FULL_MASK : __ballot_sync(PODS_FULL_MASK, i + lane < n && live_row(a, first + (int64_t)(i + lane) * step, fill));
+        }
+        return bits >> (i & 31) & 1;
+    }
+};
+
+template <int DT, bool ENT>
+__global__ void __launch_bounds__((kConsumers + 2) * 32, 1) pods_logp_pipe_kernel(const FwdArgs a) {
+    using El = Elem<DT>;
+    using raw = typename El::raw;
+    extern __shared__ __align__(128) unsigned char smem[];
+    uint4* const stages = reinterpret_cast<uint4*>(smem);
+    PipeCtrl& c = *reinterpret_cast<PipeCtrl*>(smem + (size_t)kStages * kStageVecs * 16);
+    cg::cluster_group cl = cg::this_cluster();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+    RowWalk walk;
+    walk.first = blockIdx.x / CL;
+    walk.step = gridDim.x / CL;
+    walk.n = walk.first < a.T ? (int)((a.T - walk.first + walk.step - 1) / walk.step) : 0;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&c.full[i], 1);
+            mbar_init(&c.empty[i], kConsumers);
+        }
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(&c.parts[i], 1);
+            mbar_init(&c.free_slot[i], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cl.sync();
+    bool late = false;                                 // a wait ran out: no further one is made
+    auto spins = [&] { return late ? 1u : kSpinLimit; };
+    // this CTA's share [lo, hi) of a row's whole vectors
+    auto share = [&](const raw* row, int& head, int& nvec, int& lo, int& hi) {
+        const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw));
+        head = min(lead, a.V);
+        nvec = (a.V - head) / El::E;
+        const int per = ((nvec + CL - 1) / CL + 7) & ~7;
+        lo = min(nvec, rank * per);
+        hi = min(nvec, lo + per);
+    };
+    if (warp == kConsumers) {
+        // ---- producer ----
+        StageRing ring;
+        int64_t issued = 0;
+        for (int i = 0; i < walk.n; ++i) {
+            if (!walk.live(a, i, lane, false)) continue;
+            const raw* const row = static_cast<const raw*>(a.logits) + (walk.first + (int64_t)i * walk.step) * a.ldl;
+            int head, nvec, lo, hi;
+            share(row, head, nvec, lo, hi);
+            const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
+            for (int v = lo; v < hi; v += kStageVecs, ++issued, ring.next(kStages)) {
+                if (issued >= kStages && !mbar_wait(&c.empty[ring.st], ring.parity ^ 1u, spins())) late = true;
+                if (lane == 0) {
+                    const int n = min(kStageVecs, hi - v);
+                    mbar_expect_tx(&c.full[ring.st], (uint32_t)n * 16u);
+                    for (int k = 0; k < n; k += 512)
+                        bulk_load(stages + (size_t)ring.st * kStageVecs + k, vec + v + k, (uint32_t)min(512, n - k) * 16u, &c.full[ring.st]);
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp < kConsumers) {
+        // ---- consumers ----
+        StageRing ring;
+        int rows = 0;
+        const int tid = threadIdx.x;
+        for (int i = 0; i < walk.n; ++i) {
+            if (!walk.live(a, i, lane, false)) continue;
+            const raw* const row = static_cast<const raw*>(a.logits) + (walk.first + (int64_t)i * walk.step) * a.ldl;
+            int head, nvec, lo, hi;
+            share(row, head, nvec, lo, hi);
+            Sums<DT, ENT> sums;
+            for (int v = lo; v < hi; v += kStageVecs, ring.next(kStages)) {
+                if (!mbar_wait(&c.full[ring.st], ring.parity, spins())) late = true;
+                const uint4* const buf = stages + (size_t)ring.st * kStageVecs;
+                const int n = hi - v;
+                uint4 q[kBlockVecs];
+#pragma unroll
+                for (int k = 0; k < kBlockVecs; ++k) q[k] = tid + k * kConsumers * 32 < n ? buf[tid + k * kConsumers * 32] : nothing<DT>();
+                __syncwarp();
+                if (lane == 0) arrive_local(&c.empty[ring.st]);
+                sums.take(q, a.c, a.c_lo);
+            }
+            if (rank == 0 && warp == 0) take_edges(a, row, head, head + nvec * El::E, lane, sums);
+            Part p = sums.part();
+            join_warp<ENT>(p);
+            if (lane == 0) {
+                const int slot = rows % kRing;
+                if (rows >= kRing && !wait_cluster(&c.free_slot[slot], (uint32_t)((rows / kRing - 1) & 1), spins())) late = true;
+                const uint32_t to = mapa(&c.part[slot][rank * kConsumers + warp], 0), bar = mapa(&c.parts[slot], 0);
+                store_async(to, bar, p.s, (unsigned long long)(uint32_t)p.R << 32 | (uint32_t)p.bad);
+                if (ENT) store_async(to + 16, bar, p.u, 0ull);
+            }
+            ++rows;
+            __syncwarp();
+        }
+    } else if (rank == 0) {
+        // ---- finisher ----
+        int rows = 0;
+        int64_t mine = -1;
+        float z = 0.0f;
+        Part kept = {0.0, 0.0, kNoRef, 0};
+        for (int i = 0; i < walk.n; ++i) {
+            const bool live = walk.live(a, i, lane, true);
+            if ((i & 31) == 0) {
+                mine = i + lane < walk.n && (walk.bits >> lane & 1) ? walk.first + (int64_t)(i + lane) * walk.step : -1;
+                z = mine >= 0 ? token_logit<DT>(a, mine) : 0.0f;
+            }
+            if (live) {
+                const int slot = rows % kRing;
+                if (lane == 0) mbar_expect_tx(&c.parts[slot], (uint32_t)(CL * kConsumers * (ENT ? 32 : 16)));
+                __syncwarp();
+                if (!wait_cluster(&c.parts[slot], (uint32_t)((rows / kRing) & 1), spins())) late = true;
+                Part p[8 * kConsumers / 32];
+                int R = kNoRef;
+#pragma unroll
+                for (int k = 0; k < 8 * kConsumers / 32; ++k) {
+                    p[k] = {0.0, 0.0, kNoRef, 0};
+                    if (lane + 32 * k < CL * kConsumers) {
+                        const PipePart& q = c.part[slot][lane + 32 * k];
+                        p[k].s = q.s;
+                        p[k].R = (int)(q.ref >> 32);
+                        p[k].bad = (int)(uint32_t)q.ref;
+                        if (ENT) p[k].u = q.u;
+                    }
+                    R = max(R, p[k].R);
+                }
+                __syncwarp();
+                if (lane < CL) arrive_remote(mapa(&c.free_slot[slot], lane));
+                Part sum = {0.0, 0.0, R, 0};
+#pragma unroll
+                for (int k = 0; k < 8 * kConsumers / 32; ++k) {
+                    move_to<ENT>(p[k], R);
+                    sum.s += p[k].s;
+                    sum.u += p[k].u;
+                    sum.bad |= p[k].bad;
+                }
+                join_warp<ENT>(sum);
+                if (lane == (i & 31)) kept = sum;
+                ++rows;
+            }
+            if ((i & 31) == 31 || i + 1 == walk.n) {
+                finish_rows<DT, ENT>(a, mine, kept, z, lane);
+                kept = {0.0, 0.0, kNoRef, 0};
+            }
+        }
+    }
+    if (late && lane == 0) pods_raise(a.status, PODS_STATUS_TIMEOUT);
+    __syncwarp();
+    cl.sync();                                         // no CTA leaves while a peer may still write to it
 }
 
 // d objective / d logits.  A CTA takes a stretch of `seg` vectors of one row (WARP: a warp a whole row).
@@ -339,17 +517,18 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
     const float A = (float)(-back * (g64 + (ENT ? b64 * (H - kLn2 * f64) : 0.0))), B = (float)(-back * b64 * kLn2);
     const int tok_vec = token >= head && token < tail ? (token - head) / E : -1, tok_at = (token - head) - tok_vec * E;
     auto one = [&](float z) {
-        const float d = fmaf(z, a.c, -n), p = ex2_approx(d);
+        const float d = fmaf(z, a.c_lo, fmaf(z, a.c, -n)), p = ex2_approx(d);
         return ENT ? p * fmaf(B, fmaxf(d, -1e4f), A) : p * A;
     };
     auto vector = [&](const uint4& q, int v) {
         float x[E];
         El::unpack(q, x);
-        const unsigned long long c2 = pack2(a.c, a.c), off2 = pack2(-n, -n);
+        const unsigned long long c2 = pack2(a.c, a.c), lo2 = pack2(a.c_lo, a.c_lo), off2 = pack2(-n, -n);
 #pragma unroll
         for (int i = 0; i < E; i += 2) {
+            const unsigned long long x2 = pack2(x[i], x[i + 1]);
             float d0, d1;
-            unpack2(fma2(pack2(x[i], x[i + 1]), c2, off2), d0, d1);
+            unpack2(fma2(x2, lo2, fma2(x2, c2, off2)), d0, d1);
             const float p0 = ex2_approx(d0), p1 = ex2_approx(d1);
             x[i] = ENT ? p0 * fmaf(B, fmaxf(d0, -1e4f), A) : p0 * A;
             x[i + 1] = ENT ? p1 * fmaf(B, fmaxf(d1, -1e4f), A) : p1 * A;
@@ -389,30 +568,33 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
     }
 }
 
-constexpr int kWarpVecs = 32 * 16;     // rows of up to this many vectors are taken a warp each
+constexpr int kWarpVecs = 32 * 16;     // gradient: rows of up to this many vectors are taken a warp each
+constexpr int kRowsVecs = 1024;        // log-probabilities: the same
 
 template <int DT, bool ENT>
 int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
-    const int nvec = a.V / Elem<DT>::E;
-    if (nvec <= kWarpVecs) {
-        pods_logp_kernel<DT, ENT, true><<<(unsigned)((a.T + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, stream>>>(a);
+    const int64_t nvec = a.V / Elem<DT>::E;
+    const int sms = pods_sm_count();
+    if (nvec <= kRowsVecs) {
+        const int64_t per = a.T / ((int64_t)sms * 32);
+        const int batch = (int)(per < 1 ? 1 : per > 32 ? 32 : per);
+        const int64_t warps = (a.T + batch - 1) / batch;
+        pods_logp_rows_kernel<DT, ENT><<<(unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, stream>>>(a, batch);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
         return PODS_OK;
     }
-    int cl = 1;                                        // few rows: spread over idle SMs
-    while (cl < 8 && 2 * cl * a.T <= 4 * pods_sm_count() && nvec >= 2 * cl * kThreads) cl *= 2;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cl;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(a.T * cl));
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    PODS_RETURN_IF_CUDA_ERROR(cudaLaunchKernelEx(&cfg, pods_logp_kernel<DT, ENT, false>, a));
-    return PODS_OK;
+    // the cluster size with the shortest longest share: rounds of rows times the vectors of a share and what a row costs beside
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int cl = 1; cl <= 8; cl *= 2) {
+        const int64_t n = cl == 1 ? sms : cl == 2 ? sms / 2 : (sms - 16) / cl;         // clusters at once; larger ones leave SMs empty
+        const int64_t cost = (a.T + n - 1) / n * (nvec / cl + (cl == 1 ? 256 : 512));
+        if (cost < least) {
+            least = cost;
+            best = cl;
+        }
+    }
+    return launch_row_clusters<pods_logp_pipe_kernel<DT, ENT>>(a, a.T, best, (kConsumers + 2) * 32, (size_t)kStages * kStageVecs * 16 + sizeof(PipeCtrl), stream);
 }
 
 template <int DT, bool ENT>
@@ -468,8 +650,7 @@ extern "C" int pods_logp_chunk(const void* logits, int64_t ldl, int32_t dtype, c
     a.mask = mask;
     a.T = T;
     a.V = V;
-    a.inv_tau = 1.0 / (double)temperature;
-    a.c = pods_logp::exponent_scale(temperature);
+    pods_logp::set_temperature(a, temperature);
     a.logp = logp;
     a.lse = lse;
     a.entropy = entropy;
@@ -498,8 +679,7 @@ extern "C" int pods_logp_grad_chunk(const void* logits, int64_t ldl, int32_t dty
     a.dentropy = dentropy;
     a.T = T;
     a.V = V;
-    a.inv_tau = 1.0 / (double)temperature;
-    a.c = pods_logp::exponent_scale(temperature);
+    pods_logp::set_temperature(a, temperature);
     a.dlogits = dlogits;
     a.ldd = ldd;
     a.status = status;

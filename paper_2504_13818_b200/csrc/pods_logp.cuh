@@ -16,8 +16,8 @@ struct FwdArgs {
     int64_t T;
     int32_t V;
     int32_t fill;                      // rows left out get logp 0 (otherwise they stay as they were)
-    double inv_tau;
-    float c;
+    double inv_tau, c64;               // c64 = log2 e / temperature, c + c_lo the same in two fp32 numbers
+    float c, c_lo;
     float* logp;
     double* lse;
     float* entropy;
@@ -35,17 +35,24 @@ struct GradArgs {
     int64_t T;
     int32_t V;
     int32_t n_seg, seg;
-    double inv_tau;
-    float c;
+    double inv_tau, c64;               // c64 = log2 e / temperature, c + c_lo the same in two fp32 numbers
+    float c, c_lo;
     void* dlogits;
     int64_t ldd;
     uint32_t* status;
 };
 
-// log2 e / temperature; exponents of temperatures so cold that it overflows are taken in fp64 as those of huge logits are
-inline float exponent_scale(float temperature) {
+// Exponents of temperatures so cold that the scale overflows are taken in fp64, as those of huge logits are.
+template <typename Args>
+void set_temperature(Args& a, float temperature) {
+    a.inv_tau = 1.0 / (double)temperature;
     const double c = 1.4426950408889634074 / (double)temperature;
-    return c > 3e38 ? 3e38f : (float)c;
+    a.c64 = c;
+    a.c = c > 3e38 ? 3e38f : (float)c;
+    if ((double)a.c > c) a.c = nextafterf(a.c, 0.0f);
+    // above 0, so that -inf times it is -inf as -inf times c is
+    const float lo = c > 3e38 ? 0.0f : (float)(c - (double)a.c), least = a.c * 0x1p-48f;
+    a.c_lo = lo > least ? lo : least > 1e-45f ? least : 1e-45f;
 }
 
 int check_rows(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, float temperature);

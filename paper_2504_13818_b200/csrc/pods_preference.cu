@@ -338,8 +338,7 @@ extern "C" int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t 
         f.T = T;
         f.V = V;
         f.fill = 1;
-        f.inv_tau = 1.0 / (double)temperature;
-        f.c = pods_logp::exponent_scale(temperature);
+        pods_logp::set_temperature(f, temperature);
         f.logp = logp;
         f.lse = lse;
         f.status = status;
@@ -359,8 +358,7 @@ extern "C" int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t 
     g.dlogp = dlogp;
     g.T = T;
     g.V = V;
-    g.inv_tau = 1.0 / (double)temperature;
-    g.c = pods_logp::exponent_scale(temperature);
+    pods_logp::set_temperature(g, temperature);
     g.dlogits = dlogits;
     g.ldd = ldd;
     g.status = status;
