@@ -58,20 +58,26 @@ __device__ __forceinline__ void join_warp(Part& p) {
     }
 }
 
-// What a thread holds while it goes through its elements.
+// What a thread holds while it goes through its elements of a row.  R starts as the row before left it, and is looked at once
+// more if the first block shows it far from this row's logits: a reference of the row's own would cost each row a block twice.
 template <int DT, bool ENT>
 struct Sums {
     using El = Elem<DT>;
     static constexpr int E = El::E;
-    float s = 0.0f, u = 0.0f;
-    int R = kNoRef, bad = 0;
+    float s, u;
+    int R = kNoRef, bad;
+    bool fresh;                        // nothing has been added yet
 
-    // e = 2^(x c - R) of a vector, added up; with ENT also e (x c - R)
-    __device__ __forceinline__ void add(const uint4& q, float c, float c_lo, float R_, float& bs, float& bu) const {
+    __device__ __forceinline__ void start() {
+        s = u = 0.0f;
+        bad = 0;
+        fresh = true;
+    }
+    // e = 2^(x c - R) of a vector, added to the pairs of sums; with ENT also e (x c - R)
+    __device__ __forceinline__ void add(const uint4& q, float c, float c_lo, float ref, unsigned long long& acc, unsigned long long& accu) const {
         float x[E];
         El::unpack(q, x);
-        const unsigned long long c2 = pack2(c, c), lo2 = pack2(c_lo, c_lo), off2 = pack2(-R_, -R_);
-        unsigned long long acc = 0ull, accu = 0ull;
+        const unsigned long long c2 = pack2(c, c), lo2 = pack2(c_lo, c_lo), off2 = pack2(-ref, -ref);
 #pragma unroll
         for (int i = 0; i < E; i += 2) {
             const unsigned long long x2 = pack2(x[i], x[i + 1]), d2 = fma2(x2, lo2, fma2(x2, c2, off2));
@@ -81,25 +87,33 @@ struct Sums {
             acc = add2(acc, e2);
             if (ENT) accu = fma2(e2, pack2(fmaxf(d0, -1e4f), fmaxf(d1, -1e4f)), accu);   // 2^-inf (-inf) counts 0
         }
+    }
+    template <int N>
+    __device__ __forceinline__ void add_all(const uint4 (&q)[N], float c, float c_lo, float& bs, float& bu) const {
+        const float ref = (float)R;
+        unsigned long long acc = 0ull, accu = 0ull;
+#pragma unroll
+        for (int k = 0; k < N; ++k) add(q[k], c, c_lo, ref, acc, accu);
         float a, b;
         unpack2(acc, a, b);
-        bs += a + b;
+        bs = a + b;
+        bu = 0.0f;
         if (ENT) {
             unpack2(accu, a, b);
-            bu += a + b;
+            bu = a + b;
         }
     }
     template <int N>
     __device__ __forceinline__ void take(const uint4 (&q)[N], float c, float c_lo) {
-        float bs = 0.0f, bu = 0.0f;
-        const float ref = (float)R;
-#pragma unroll
-        for (int k = 0; k < N; ++k) add(q[k], c, c_lo, ref, bs, bu);
-        if (!(bs < kSumLimit)) {                       // rare: the first block, a block far above all before it, NaN, +inf
+        float bs, bu;
+        add_all(q, c, c_lo, bs, bu);
+        if (!(bs < kSumLimit) || (fresh && !(bs > 1.0f / kSumLimit))) {
+            // rare: the reference lies far from the first block or below a later one; NaN, +inf, nothing but -inf
             float m = -INFINITY;
 #pragma unroll
             for (int k = 0; k < N; ++k) m = max_nan(m, El::vec_max(q[k]));
             bs = bu = 0.0f;
+            if (fresh) R = kNoRef;
             if (!(m < INFINITY)) bad |= 1;
             else if (m > -INFINITY) {
                 const float top = ceilf(m * c);
@@ -112,16 +126,17 @@ struct Sums {
                         s *= f;
                         R = to;
                     }
-                    const float now = (float)R;
-#pragma unroll
-                    for (int k = 0; k < N; ++k) add(q[k], c, c_lo, now, bs, bu);
+                    add_all(q, c, c_lo, bs, bu);
                 }
             }
+            if (R == kNoRef && !bad) return;           // still nothing
         }
+        fresh = false;
         s += bs;
         if (ENT) u += bu;
     }
-    __device__ __forceinline__ Part part() const { return {(double)s, (double)u, R, bad}; }
+    // nothing of the row so far: a row whose reference is still that of the row before
+    __device__ __forceinline__ Part part() const { return {(double)s, (double)u, fresh ? kNoRef : R, bad}; }
 };
 
 template <typename T, typename Op>
@@ -244,13 +259,14 @@ __global__ void __launch_bounds__(kThreads) pods_logp_rows_kernel(const FwdArgs 
     const int64_t mine = lane < batch && live_row(a, first + lane, true) ? first + lane : -1;
     const float z = mine >= 0 ? token_logit<DT>(a, mine) : 0.0f;
     Part kept = {0.0, 0.0, kNoRef, 0};
+    Sums<DT, ENT> sums;
     for (unsigned todo = __ballot_sync(PODS_FULL_MASK, mine >= 0); todo != 0; todo &= todo - 1) {
         const int j = __ffs(todo) - 1;
         const raw* const row = static_cast<const raw*>(a.logits) + (first + j) * a.ldl;
         const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw));
         const int head = min(lead, a.V), nvec = (a.V - head) / El::E, tail = head + nvec * El::E;
         const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
-        Sums<DT, ENT> sums;
+        sums.start();
         for (int v = lane; v - lane < nvec; v += kBlockVecs * 32) {
             uint4 q[kBlockVecs];
 #pragma unroll
@@ -362,22 +378,33 @@ __global__ void __launch_bounds__((kConsumers + 2) * 32, 1) pods_logp_pipe_kerne
         StageRing ring;
         int rows = 0;
         const int tid = threadIdx.x;
+        Sums<DT, ENT> sums;
         for (int i = 0; i < walk.n; ++i) {
             if (!walk.live(a, i, lane, false)) continue;
             const raw* const row = static_cast<const raw*>(a.logits) + (walk.first + (int64_t)i * walk.step) * a.ldl;
             int head, nvec, lo, hi;
             share(row, head, nvec, lo, hi);
-            Sums<DT, ENT> sums;
+            sums.start();
             for (int v = lo; v < hi; v += kStageVecs, ring.next(kStages)) {
                 if (!mbar_wait(&c.full[ring.st], ring.parity, spins())) late = true;
                 const uint4* const buf = stages + (size_t)ring.st * kStageVecs;
                 const int n = hi - v;
-                uint4 q[kBlockVecs];
+                if (n >= kStageVecs) {
+                    uint4 q[kBlockVecs];
 #pragma unroll
-                for (int k = 0; k < kBlockVecs; ++k) q[k] = tid + k * kConsumers * 32 < n ? buf[tid + k * kConsumers * 32] : nothing<DT>();
-                __syncwarp();
-                if (lane == 0) arrive_local(&c.empty[ring.st]);
-                sums.take(q, a.c, a.c_lo);
+                    for (int k = 0; k < kBlockVecs; ++k) q[k] = buf[tid + k * kConsumers * 32];
+                    __syncwarp();
+                    if (lane == 0) arrive_local(&c.empty[ring.st]);
+                    sums.take(q, a.c, a.c_lo);
+                } else {
+#pragma unroll 1
+                    for (int k = tid; k < n; k += kConsumers * 32) {
+                        const uint4 q[1] = {buf[k]};
+                        sums.take(q, a.c, a.c_lo);
+                    }
+                    __syncwarp();
+                    if (lane == 0) arrive_local(&c.empty[ring.st]);
+                }
             }
             if (rank == 0 && warp == 0) take_edges(a, row, head, head + nvec * El::E, lane, sums);
             Part p = sums.part();
