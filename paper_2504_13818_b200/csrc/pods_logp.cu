@@ -10,6 +10,8 @@
 // Bound: HBM; a read of the logits (forward), a read and a write (gradient).
 #include <float.h>
 
+#include <type_traits>
+
 #include "pods_logp.cuh"
 
 namespace {
@@ -21,7 +23,7 @@ using pods_logp::GradArgs;
 constexpr int kThreads = 256;
 constexpr int kBlockVecs = 4;          // vectors a thread takes at once
 constexpr float kSumLimit = 1024.0f;   // a block's sum above this moves the reference
-constexpr int kNoRef = -(1 << 30);
+constexpr int kNoRef = -(1 << 28);
 constexpr int kFar = 1 << 22;          // references from here on leave fp32 too few fractional bits: the row is taken in fp64
 
 // A part of a row: S and U relative to 2^R.  R == kNoRef: nothing but -inf so far.
@@ -35,28 +37,18 @@ __device__ __forceinline__ double pow2_int(int n) {    // n <= 0
     return n < -1000 ? 0.0 : __hiloint2double((1023 + n) << 20, 0);
 }
 
-// Makes `p` relative to 2^R, R its own or a larger one.
+// Adds what a lane left of a row to `p`, whose reference is at least the lane's: a product with a power of two, then fp64.
 template <bool ENT>
-__device__ __forceinline__ void move_to(Part& p, int R) {
-    const int d = p.R - R;
+__device__ __forceinline__ void add_left(Part& p, uint2 l, float lu) {
+    const float s = __uint_as_float(l.x);
+    const int d = ((int)l.y >> 2) - p.R;
     const double f = pow2_int(d);
-    // 2^(y - R) (y - R) = 2^(y - Rp) 2^(Rp - R) (y - Rp + Rp - R); an empty part adds nothing however far its reference
-    if (ENT) p.u = p.s != 0.0 ? (p.u + p.s * (double)d) * f : 0.0;
-    p.s *= f;
-    p.R = R;
+    // 2^(y - R) (y - R) = 2^(y - Rl) 2^(Rl - R) (y - Rl + Rl - R); a lane without anything adds nothing
+    if (ENT) p.u += s != 0.0f ? ((double)lu + (double)s * (double)d) * f : 0.0;
+    p.s += (double)s * f;
+    p.bad |= (int)(l.y & 3u);
 }
-
-// The parts of a warp's lanes as one, in every lane.
-template <bool ENT>
-__device__ __forceinline__ void join_warp(Part& p) {
-    move_to<ENT>(p, __reduce_max_sync(PODS_FULL_MASK, p.R));
-    p.bad = (int)__reduce_or_sync(PODS_FULL_MASK, (unsigned)p.bad);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        p.s += __shfl_xor_sync(PODS_FULL_MASK, p.s, d);
-        if (ENT) p.u += __shfl_xor_sync(PODS_FULL_MASK, p.u, d);
-    }
-}
+__device__ __forceinline__ int ref_of(uint2 l) { return (int)l.y >> 2; }
 
 // What a thread holds while it goes through its elements of a row.  R starts as the row before left it, and is looked at once
 // more if the first block shows it far from this row's logits: a reference of the row's own would cost each row a block twice.
@@ -135,8 +127,10 @@ struct Sums {
         s += bs;
         if (ENT) u += bu;
     }
-    // nothing of the row so far: a row whose reference is still that of the row before
-    __device__ __forceinline__ Part part() const { return {(double)s, (double)u, fresh ? kNoRef : R, bad}; }
+    // What a lane leaves of a row, 8 bytes and with ENT 8 more.  Nothing so far: the reference is still that of the row before.
+    __device__ __forceinline__ uint2 left() const {
+        return make_uint2(__float_as_uint(s), (uint32_t)(fresh ? kNoRef : R) << 2 | (uint32_t)bad);
+    }
 };
 
 template <typename T, typename Op>
@@ -247,58 +241,163 @@ __device__ __forceinline__ uint4 nothing() {           // a vector of -inf
     return make_uint4(w, w, w, w);
 }
 
-// Short rows: a warp takes `batch` rows one after the other and finishes them together, a lane each, since a row's logarithms
-// and the chain to its token's logit cost a warp more than 1000 logits.
+// Short rows: a warp takes `batch` rows one after the other, with two blocks of 2 KB on their way to its own shared memory while
+// it works on a third, and finishes the rows together.  What its lanes have of each row goes to shared memory too, and then four
+// lanes sum a row: a reduction over the warp for each row, its logarithms and the chain to its token's logit would cost more
+// than 1000 logits do.
+constexpr int kBatch = 8;
+constexpr int kAhead = 3;              // blocks a warp holds
+
+template <bool ENT>
+struct RowsWarp {
+    uint4 block[kAhead][kBlockVecs * 32];
+    uint2 left[kBatch][33];
+    float left_u[ENT ? kBatch : 1][33];
+};
+
+__device__ __forceinline__ void copy16(uint4* dst, const uint4* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+
+// Where a warp is in its rows: blocks of the rows whose bits are set, in order.
+template <int DT>
+struct Cursor {
+    const uint4* vec;
+    int nvec, v;                       // the row's whole vectors; the block's first
+    unsigned todo;                     // rows from this one on
+    __device__ __forceinline__ void open(const FwdArgs& a, int64_t first) {
+        using raw = typename Elem<DT>::raw;
+        const raw* const row = static_cast<const raw*>(a.logits) + (first + __ffs(todo) - 1) * a.ldl;
+        const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw)), head = min(lead, a.V);
+        nvec = (a.V - head) / Elem<DT>::E;
+        vec = reinterpret_cast<const uint4*>(row + head);
+        v = 0;
+    }
+};
+
 template <int DT, bool ENT>
-__global__ void __launch_bounds__(kThreads) pods_logp_rows_kernel(const FwdArgs a, int batch) {
+__global__ void __launch_bounds__(kThreads, 3) pods_logp_rows_kernel(const FwdArgs a, int batch) {
     using El = Elem<DT>;
     using raw = typename El::raw;
+    extern __shared__ __align__(128) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * batch;
-    if (first >= a.T) return;
-    const int64_t mine = lane < batch && live_row(a, first + lane, true) ? first + lane : -1;
-    const float z = mine >= 0 ? token_logit<DT>(a, mine) : 0.0f;
-    Part kept = {0.0, 0.0, kNoRef, 0};
+    RowsWarp<ENT>& w = reinterpret_cast<RowsWarp<ENT>*>(smem)[warp];
     Sums<DT, ENT> sums;
-    for (unsigned todo = __ballot_sync(PODS_FULL_MASK, mine >= 0); todo != 0; todo &= todo - 1) {
-        const int j = __ffs(todo) - 1;
-        const raw* const row = static_cast<const raw*>(a.logits) + (first + j) * a.ldl;
-        const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw));
-        const int head = min(lead, a.V), nvec = (a.V - head) / El::E, tail = head + nvec * El::E;
-        const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
-        sums.start();
-        for (int v = lane; v - lane < nvec; v += kBlockVecs * 32) {
-            uint4 q[kBlockVecs];
+    for (int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + warp) * batch; first < a.T; first += (int64_t)gridDim.x * (kThreads / 32) * batch) {
+        const int64_t mine = lane < batch && live_row(a, first + lane, true) ? first + lane : -1;
+        const unsigned rows = __ballot_sync(PODS_FULL_MASK, mine >= 0);
+        if (rows == 0) continue;
+        Cursor<DT> load, use;
+        load.todo = use.todo = rows;
+        load.open(a, first);
+        int to = 0;
+        auto issue = [&] {
+            if (load.todo != 0) {
+                const int v = load.v + lane;
 #pragma unroll
-            for (int k = 0; k < kBlockVecs; ++k) q[k] = v + k * 32 < nvec ? __ldg(vec + v + k * 32) : nothing<DT>();
-            sums.take(q, a.c, a.c_lo);
+                for (int k = 0; k < kBlockVecs; ++k)
+                    if (v + k * 32 < load.nvec) copy16(&w.block[to][k * 32 + lane], load.vec + v + k * 32);
+                load.v += kBlockVecs * 32;
+                if (load.v >= load.nvec) {
+                    load.todo &= load.todo - 1;
+                    if (load.todo != 0) load.open(a, first);
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            to = to + 1 == kAhead ? 0 : to + 1;
+        };
+#pragma unroll
+        for (int k = 0; k < kAhead - 1; ++k) issue();
+        const float z = mine >= 0 ? token_logit<DT>(a, mine) : 0.0f;
+        int from = 0;
+        for (; use.todo != 0; use.todo &= use.todo - 1) {
+            const int j = __ffs(use.todo) - 1;
+            use.open(a, first);
+            sums.start();
+            for (; use.v < use.nvec || use.v == 0; use.v += kBlockVecs * 32) {
+                issue();
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+                uint4 q[kBlockVecs];                   // a lane's own copies: nobody else's are waited for
+                const int v = use.v + lane;
+                if (use.v + kBlockVecs * 32 <= use.nvec) {
+#pragma unroll
+                    for (int k = 0; k < kBlockVecs; ++k) q[k] = w.block[from][k * 32 + lane];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kBlockVecs; ++k) q[k] = v + k * 32 < use.nvec ? w.block[from][k * 32 + lane] : nothing<DT>();
+                }
+                from = from + 1 == kAhead ? 0 : from + 1;
+                sums.take(q, a.c, a.c_lo);
+            }
+            const raw* const row = static_cast<const raw*>(a.logits) + (first + j) * a.ldl;
+            const int head = (int)(reinterpret_cast<const raw*>(use.vec) - row);
+            take_edges(a, row, head, head + use.nvec * El::E, lane, sums);
+            w.left[j][lane] = sums.left();
+            if (ENT) w.left_u[j][lane] = sums.u;
         }
-        take_edges(a, row, head, tail, lane, sums);
-        Part p = sums.part();
-        join_warp<ENT>(p);
-        if (lane == j) kept = p;
+        __syncwarp();
+        // four lanes a row: lane l sums row l / 4
+        const int j = lane >> 2;
+        Part p = {0.0, 0.0, kNoRef, 0};
+        if (rows >> j & 1) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) p.R = max(p.R, ref_of(w.left[j][(lane & 3) + 4 * k]));
+        }
+        p.R = max(p.R, __shfl_xor_sync(PODS_FULL_MASK, p.R, 1));
+        p.R = max(p.R, __shfl_xor_sync(PODS_FULL_MASK, p.R, 2));
+        if (rows >> j & 1) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) add_left<ENT>(p, w.left[j][(lane & 3) + 4 * k], ENT ? w.left_u[j][(lane & 3) + 4 * k] : 0.0f);
+        }
+#pragma unroll
+        for (int d = 1; d <= 2; d <<= 1) {
+            p.s += __shfl_xor_sync(PODS_FULL_MASK, p.s, d);
+            if (ENT) p.u += __shfl_xor_sync(PODS_FULL_MASK, p.u, d);
+            p.bad |= __shfl_xor_sync(PODS_FULL_MASK, p.bad, d);
+        }
+        // back to a lane a row
+        const int at = (lane & 7) * 4;
+        Part q;
+        q.s = __shfl_sync(PODS_FULL_MASK, p.s, at);
+        q.u = ENT ? __shfl_sync(PODS_FULL_MASK, p.u, at) : 0.0;
+        q.R = __shfl_sync(PODS_FULL_MASK, p.R, at);
+        q.bad = __shfl_sync(PODS_FULL_MASK, p.bad, at);
+        finish_rows<DT, ENT>(a, mine, q, z, lane);
+        __syncwarp();
     }
-    finish_rows<DT, ENT>(a, mine, kept, z, lane);
 }
 
 // Long rows: a cluster of CTAs holds a share of the row each and goes round over the rows; a CTA is a producer warp that keeps
-// kStages copies of 32 KB in flight, consumer warps that add up what has arrived, and a warp that finishes the rows, 32 at
-// once.  They meet at mbarriers only, so the copies never wait for a row's end.
+// 192 KB of copies in flight, consumer warps that add up what has arrived, and a warp that finishes the rows, 32 at once.  They
+// meet at mbarriers only, so the copies never wait for a row's end.  Consumers work in groups of W warps, each on a row of its
+// own and with a producer and stages of its own (a group that waited for a stage which another one uses first could be two uses
+// ahead of it, which a barrier's parity does not tell apart): at a row's end one group leaves the exponentials' pipe to the others.
 constexpr int kConsumers = 16;
-constexpr int kStageVecs = kConsumers * 32 * kBlockVecs;
-constexpr int kStages = 6;
-constexpr int kRing = 4;               // rows whose parts may be waiting to be finished
+constexpr int kStageBytes = 196608;
 
-struct PipePart {                      // a consumer warp's part, as it travels: 16 bytes, with ENT 32
+template <int W>
+struct Pipe {
+    static constexpr int groups = kConsumers / W;
+    static constexpr int stage_vecs = W * 32 * kBlockVecs;
+    static constexpr int stages = kStageBytes / (stage_vecs * 16 * groups);          // of a group
+    static constexpr int threads = (kConsumers + groups + 1) * 32;
+    static constexpr int ring = 2 * groups < 4 ? 4 : 2 * groups;       // rows whose sums may be waiting to be finished
+};
+
+struct PipePart {                      // a CTA's sums of a row, as they travel to the cluster's first CTA
     double s;
     unsigned long long ref;            // R above, bad below
     double u;
     unsigned long long unused;
 };
 
+template <int W>
 struct PipeCtrl {
-    unsigned long long full[kStages], empty[kStages], parts[kRing], free_slot[kRing];
-    alignas(16) PipePart part[kRing][8 * kConsumers];
+    using P = Pipe<W>;
+    unsigned long long full[P::groups][P::stages], empty[P::groups][P::stages], summed[P::ring], free_slot[P::ring], parts[P::ring], free_part[P::ring];
+    alignas(16) PipePart part[P::ring][8];
+    uint2 left[P::ring][W * 32];
+    float left_u[P::ring][W * 32];
 };
 
 // Rows of a cluster, a mask of 32 at a time
@@ -315,13 +414,14 @@ struct RowWalk {
     }
 };
 
-template <int DT, bool ENT>
-__global__ void __launch_bounds__((kConsumers + 2) * 32, 1) pods_logp_pipe_kernel(const FwdArgs a) {
+template <int DT, bool ENT, int W>
+__global__ void __launch_bounds__(Pipe<W>::threads, 1) pods_logp_pipe_kernel(const FwdArgs a) {
     using El = Elem<DT>;
     using raw = typename El::raw;
     extern __shared__ __align__(128) unsigned char smem[];
     uint4* const stages = reinterpret_cast<uint4*>(smem);
-    PipeCtrl& c = *reinterpret_cast<PipeCtrl*>(smem + (size_t)kStages * kStageVecs * 16);
+    constexpr int kStages = Pipe<W>::stages, kStageVecs = Pipe<W>::stage_vecs, kRing = Pipe<W>::ring, kGroups = Pipe<W>::groups;
+    PipeCtrl<W>& c = *reinterpret_cast<PipeCtrl<W>*>(smem + kStageBytes);
     cg::cluster_group cl = cg::this_cluster();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int CL = (int)cl.num_blocks(), rank = (int)cl.block_rank();
@@ -330,13 +430,16 @@ __global__ void __launch_bounds__((kConsumers + 2) * 32, 1) pods_logp_pipe_kerne
     walk.step = gridDim.x / CL;
     walk.n = walk.first < a.T ? (int)((a.T - walk.first + walk.step - 1) / walk.step) : 0;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(&c.full[i], 1);
-            mbar_init(&c.empty[i], kConsumers);
-        }
+        for (int g = 0; g < kGroups; ++g)
+            for (int i = 0; i < kStages; ++i) {
+                mbar_init(&c.full[g][i], 1);
+                mbar_init(&c.empty[g][i], W);
+            }
         for (int i = 0; i < kRing; ++i) {
-            mbar_init(&c.parts[i], 1);
+            mbar_init(&c.summed[i], W);
             mbar_init(&c.free_slot[i], 1);
+            mbar_init(&c.parts[i], 1);
+            mbar_init(&c.free_part[i], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -352,23 +455,27 @@ __global__ void __launch_bounds__((kConsumers + 2) * 32, 1) pods_logp_pipe_kerne
         lo = min(nvec, rank * per);
         hi = min(nvec, lo + per);
     };
-    if (warp == kConsumers) {
-        // ---- producer ----
+    if (warp >= kConsumers && warp < kConsumers + kGroups) {
+        // ---- a group's producer ----
+        const int group = warp - kConsumers;
+        uint4* const mine = stages + (size_t)group * kStages * kStageVecs;
         StageRing ring;
         int64_t issued = 0;
+        int rows = 0;
         for (int i = 0; i < walk.n; ++i) {
             if (!walk.live(a, i, lane, false)) continue;
+            if (rows++ % kGroups != group) continue;
             const raw* const row = static_cast<const raw*>(a.logits) + (walk.first + (int64_t)i * walk.step) * a.ldl;
             int head, nvec, lo, hi;
             share(row, head, nvec, lo, hi);
             const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
             for (int v = lo; v < hi; v += kStageVecs, ++issued, ring.next(kStages)) {
-                if (issued >= kStages && !mbar_wait(&c.empty[ring.st], ring.parity ^ 1u, spins())) late = true;
+                if (issued >= kStages && !mbar_wait(&c.empty[group][ring.st], ring.parity ^ 1u, spins())) late = true;
                 if (lane == 0) {
                     const int n = min(kStageVecs, hi - v);
-                    mbar_expect_tx(&c.full[ring.st], (uint32_t)n * 16u);
+                    mbar_expect_tx(&c.full[group][ring.st], (uint32_t)n * 16u);
                     for (int k = 0; k < n; k += 512)
-                        bulk_load(stages + (size_t)ring.st * kStageVecs + k, vec + v + k, (uint32_t)min(512, n - k) * 16u, &c.full[ring.st]);
+                        bulk_load(mine + (size_t)ring.st * kStageVecs + k, vec + v + k, (uint32_t)min(512, n - k) * 16u, &c.full[group][ring.st]);
                 }
                 __syncwarp();
             }
@@ -377,94 +484,110 @@ __global__ void __launch_bounds__((kConsumers + 2) * 32, 1) pods_logp_pipe_kerne
         // ---- consumers ----
         StageRing ring;
         int rows = 0;
-        const int tid = threadIdx.x;
+        const int group = warp / W, tid = threadIdx.x % (W * 32);
         Sums<DT, ENT> sums;
         for (int i = 0; i < walk.n; ++i) {
             if (!walk.live(a, i, lane, false)) continue;
             const raw* const row = static_cast<const raw*>(a.logits) + (walk.first + (int64_t)i * walk.step) * a.ldl;
+            if (rows % kGroups != group) {
+                ++rows;
+                continue;
+            }
             int head, nvec, lo, hi;
             share(row, head, nvec, lo, hi);
             sums.start();
             for (int v = lo; v < hi; v += kStageVecs, ring.next(kStages)) {
-                if (!mbar_wait(&c.full[ring.st], ring.parity, spins())) late = true;
-                const uint4* const buf = stages + (size_t)ring.st * kStageVecs;
+                if (!mbar_wait(&c.full[group][ring.st], ring.parity, spins())) late = true;
+                const uint4* const buf = stages + (size_t)(group * kStages + ring.st) * kStageVecs;
                 const int n = hi - v;
-                if (n >= kStageVecs) {
-                    uint4 q[kBlockVecs];
+                // as many vectors a thread as the chunk has, the last ones padded
+                auto some = [&](auto count) {
+                    constexpr int N = decltype(count)::value;
+                    uint4 q[N];
 #pragma unroll
-                    for (int k = 0; k < kBlockVecs; ++k) q[k] = buf[tid + k * kConsumers * 32];
-                    __syncwarp();
-                    if (lane == 0) arrive_local(&c.empty[ring.st]);
-                    sums.take(q, a.c, a.c_lo);
-                } else {
-#pragma unroll 1
-                    for (int k = tid; k < n; k += kConsumers * 32) {
-                        const uint4 q[1] = {buf[k]};
-                        sums.take(q, a.c, a.c_lo);
+                    for (int k = 0; k < N; ++k) {
+                        const int at = tid + k * W * 32;
+                        q[k] = k + 1 < N || at < n ? buf[at] : nothing<DT>();
                     }
                     __syncwarp();
-                    if (lane == 0) arrive_local(&c.empty[ring.st]);
-                }
+                    if (lane == 0) arrive_local(&c.empty[group][ring.st]);
+                    sums.take(q, a.c, a.c_lo);
+                };
+                if (n > 3 * W * 32) some(std::integral_constant<int, 4>());
+                else if (n > 2 * W * 32) some(std::integral_constant<int, 3>());
+                else if (n > W * 32) some(std::integral_constant<int, 2>());
+                else some(std::integral_constant<int, 1>());
             }
-            if (rank == 0 && warp == 0) take_edges(a, row, head, head + nvec * El::E, lane, sums);
-            Part p = sums.part();
-            join_warp<ENT>(p);
-            if (lane == 0) {
-                const int slot = rows % kRing;
-                if (rows >= kRing && !wait_cluster(&c.free_slot[slot], (uint32_t)((rows / kRing - 1) & 1), spins())) late = true;
-                const uint32_t to = mapa(&c.part[slot][rank * kConsumers + warp], 0), bar = mapa(&c.parts[slot], 0);
-                store_async(to, bar, p.s, (unsigned long long)(uint32_t)p.R << 32 | (uint32_t)p.bad);
-                if (ENT) store_async(to + 16, bar, p.u, 0ull);
-            }
-            ++rows;
+            if (rank == 0 && warp % W == 0) take_edges(a, row, head, head + nvec * El::E, lane, sums);
+            const int slot = rows % kRing;
+            if (rows >= kRing && !mbar_wait(&c.free_slot[slot], (uint32_t)((rows / kRing - 1) & 1), spins())) late = true;
+            c.left[slot][tid] = sums.left();
+            if (ENT) c.left_u[slot][tid] = sums.u;
             __syncwarp();
+            if (lane == 0) arrive_local(&c.summed[slot]);
+            ++rows;
         }
-    } else if (rank == 0) {
-        // ---- finisher ----
+    } else {
+        // ---- finisher: this CTA's sums of a row, then, in the cluster's first CTA, the row ----
         int rows = 0;
         int64_t mine = -1;
         float z = 0.0f;
         Part kept = {0.0, 0.0, kNoRef, 0};
         for (int i = 0; i < walk.n; ++i) {
-            const bool live = walk.live(a, i, lane, true);
-            if ((i & 31) == 0) {
+            const bool live = walk.live(a, i, lane, rank == 0);
+            if ((i & 31) == 0 && rank == 0) {
                 mine = i + lane < walk.n && (walk.bits >> lane & 1) ? walk.first + (int64_t)(i + lane) * walk.step : -1;
                 z = mine >= 0 ? token_logit<DT>(a, mine) : 0.0f;
             }
             if (live) {
                 const int slot = rows % kRing;
-                if (lane == 0) mbar_expect_tx(&c.parts[slot], (uint32_t)(CL * kConsumers * (ENT ? 32 : 16)));
-                __syncwarp();
-                if (!wait_cluster(&c.parts[slot], (uint32_t)((rows / kRing) & 1), spins())) late = true;
-                Part p[8 * kConsumers / 32];
-                int R = kNoRef;
+                const uint32_t use = (uint32_t)(rows / kRing);
+                if (CL > 1 && rank == 0 && lane == 0) mbar_expect_tx(&c.parts[slot], (uint32_t)((CL - 1) * (ENT ? 32 : 16)));
+                if (!mbar_wait(&c.summed[slot], use & 1u, spins())) late = true;
+                Part sum = {0.0, 0.0, kNoRef, 0};
+                uint2 l[W];
 #pragma unroll
-                for (int k = 0; k < 8 * kConsumers / 32; ++k) {
-                    p[k] = {0.0, 0.0, kNoRef, 0};
-                    if (lane + 32 * k < CL * kConsumers) {
-                        const PipePart& q = c.part[slot][lane + 32 * k];
-                        p[k].s = q.s;
-                        p[k].R = (int)(q.ref >> 32);
-                        p[k].bad = (int)(uint32_t)q.ref;
-                        if (ENT) p[k].u = q.u;
+                for (int k = 0; k < W; ++k) {
+                    l[k] = c.left[slot][k * 32 + lane];
+                    sum.R = max(sum.R, ref_of(l[k]));
+                }
+                sum.R = __reduce_max_sync(PODS_FULL_MASK, sum.R);
+#pragma unroll
+                for (int k = 0; k < W; ++k) add_left<ENT>(sum, l[k], ENT ? c.left_u[slot][k * 32 + lane] : 0.0f);
+                __syncwarp();
+                if (lane == 0) arrive_local(&c.free_slot[slot]);
+                sum.s = warp_reduce(sum.s, Plus());
+                if (ENT) sum.u = warp_reduce(sum.u, Plus());
+                sum.bad = (int)__reduce_or_sync(PODS_FULL_MASK, (unsigned)sum.bad);
+                if (CL > 1 && rank != 0) {
+                    if (lane == 0) {
+                        if (rows >= kRing && !wait_cluster(&c.free_part[slot], (use - 1u) & 1u, spins())) late = true;
+                        const uint32_t to = mapa(&c.part[slot][rank], 0), bar = mapa(&c.parts[slot], 0);
+                        store_async(to, bar, sum.s, (unsigned long long)(uint32_t)sum.R << 32 | (uint32_t)sum.bad);
+                        if (ENT) store_async(to + 16, bar, sum.u, 0ull);
                     }
-                    R = max(R, p[k].R);
+                    __syncwarp();
+                } else if (CL > 1) {
+                    if (!wait_cluster(&c.parts[slot], use & 1u, spins())) late = true;
+                    Part p = {0.0, 0.0, kNoRef, 0};
+                    if (lane == 0) p = sum;
+                    else if (lane < CL) {
+                        const PipePart& q = c.part[slot][lane];
+                        p = {q.s, ENT ? q.u : 0.0, (int)(q.ref >> 32), (int)(uint32_t)q.ref};
+                    }
+                    __syncwarp();
+                    if (lane > 0 && lane < CL) arrive_remote(mapa(&c.free_part[slot], lane));
+                    const int R = __reduce_max_sync(PODS_FULL_MASK, p.R);
+                    const double f = pow2_int(p.R - R);
+                    if (ENT) sum.u = warp_reduce(p.s != 0.0 ? (p.u + p.s * (double)(p.R - R)) * f : 0.0, Plus());
+                    sum.s = warp_reduce(p.s * f, Plus());
+                    sum.R = R;
+                    sum.bad = (int)__reduce_or_sync(PODS_FULL_MASK, (unsigned)p.bad);
                 }
-                __syncwarp();
-                if (lane < CL) arrive_remote(mapa(&c.free_slot[slot], lane));
-                Part sum = {0.0, 0.0, R, 0};
-#pragma unroll
-                for (int k = 0; k < 8 * kConsumers / 32; ++k) {
-                    move_to<ENT>(p[k], R);
-                    sum.s += p[k].s;
-                    sum.u += p[k].u;
-                    sum.bad |= p[k].bad;
-                }
-                join_warp<ENT>(sum);
                 if (lane == (i & 31)) kept = sum;
                 ++rows;
             }
-            if ((i & 31) == 31 || i + 1 == walk.n) {
+            if (rank == 0 && ((i & 31) == 31 || i + 1 == walk.n)) {
                 finish_rows<DT, ENT>(a, mine, kept, z, lane);
                 kept = {0.0, 0.0, kNoRef, 0};
             }
@@ -597,31 +720,48 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
 
 constexpr int kWarpVecs = 32 * 16;     // gradient: rows of up to this many vectors are taken a warp each
 constexpr int kRowsVecs = 1024;        // log-probabilities: the same
+constexpr int kGroupVecs = 8192;       // shares of up to this many vectors are taken by groups of four warps
+
+template <int DT, bool ENT>
+int launch_rows(const FwdArgs& a, int batch, int grid, cudaStream_t stream) {
+    static uint64_t prepared = 0;                      // devices as bits
+    constexpr size_t smem = sizeof(RowsWarp<ENT>) * (kThreads / 32);
+    int dev = 0;
+    PODS_RETURN_IF_CUDA_ERROR(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return PODS_ERR_UNSUPPORTED;
+    if (!(__atomic_load_n(&prepared, __ATOMIC_ACQUIRE) >> dev & 1)) {
+        PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(pods_logp_rows_kernel<DT, ENT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        __atomic_fetch_or(&prepared, 1ull << dev, __ATOMIC_RELEASE);
+    }
+    pods_logp_rows_kernel<DT, ENT><<<grid, kThreads, smem, stream>>>(a, batch);
+    PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
+    return PODS_OK;
+}
 
 template <int DT, bool ENT>
 int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
     const int64_t nvec = a.V / Elem<DT>::E;
     const int sms = pods_sm_count();
     if (nvec <= kRowsVecs) {
-        const int64_t per = a.T / ((int64_t)sms * 32);
-        const int batch = (int)(per < 1 ? 1 : per > 32 ? 32 : per);
-        const int64_t warps = (a.T + batch - 1) / batch;
-        pods_logp_rows_kernel<DT, ENT><<<(unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, stream>>>(a, batch);
-        PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
-        return PODS_OK;
+        const int64_t per = a.T / ((int64_t)sms * 24);
+        const int batch = (int)(per < 1 ? 1 : per > kBatch ? kBatch : per);
+        const int64_t ctas = (a.T + (int64_t)batch * (kThreads / 32) - 1) / ((int64_t)batch * (kThreads / 32));
+        return launch_rows<DT, ENT>(a, batch, ctas < 3 * sms ? (int)ctas : 3 * sms, stream);
     }
     // the cluster size with the shortest longest share: rounds of rows times the vectors of a share and what a row costs beside
     int best = 1;
     int64_t least = INT64_MAX;
     for (int cl = 1; cl <= 8; cl *= 2) {
         const int64_t n = cl == 1 ? sms : cl == 2 ? sms / 2 : (sms - 16) / cl;         // clusters at once; larger ones leave SMs empty
-        const int64_t cost = (a.T + n - 1) / n * (nvec / cl + (cl == 1 ? 256 : 512));
+        const int64_t cost = (a.T + n - 1) / n * (nvec / cl + (cl == 1 ? 1000 : 1250));
         if (cost < least) {
             least = cost;
             best = cl;
         }
     }
-    return launch_row_clusters<pods_logp_pipe_kernel<DT, ENT>>(a, a.T, best, (kConsumers + 2) * 32, (size_t)kStages * kStageVecs * 16 + sizeof(PipeCtrl), stream);
+    // groups of four warps want several rows each
+    return nvec / best <= kGroupVecs && a.T * best >= 16 * (int64_t)sms ? launch_row_clusters<pods_logp_pipe_kernel<DT, ENT, 4>>(a, a.T, best, Pipe<4>::threads, kStageBytes + sizeof(PipeCtrl<4>), stream)
+                                     : launch_row_clusters<pods_logp_pipe_kernel<DT, ENT, 16>>(a, a.T, best, Pipe<16>::threads, kStageBytes + sizeof(PipeCtrl<16>), stream);
 }
 
 template <int DT, bool ENT>
