@@ -433,7 +433,7 @@ size_t pods_preference_fwd_bwd_workspace_bytes(int64_t T, int64_t M, int64_t P);
 
 /*
  * pods_preference_fwd_bwd - pods_logp_chunk, pods_preference and pods_logp_grad_chunk over a whole packed batch whose logits are
- * at hand: loss [dev] fp32 scalar (written), logp [dev] fp32 [T] (0 where the mask is 0 and behind the last rollout), dlogits,
+ * at hand (scores are sums of the log-probabilities before they are rounded to logp): loss [dev] fp32 scalar (written), logp [dev] fp32 [T] (0 where the mask is 0 and behind the last rollout), dlogits,
  * reward, pair_loss.  Rows that weigh nothing (masked, behind the last rollout, of rollouts in no pair) get a zero gradient row.
  * For logits that do not all exist at one time, make the three calls, the first and the last chunk by chunk.
  */

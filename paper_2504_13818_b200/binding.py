@@ -862,6 +862,8 @@ def pods_preference_fwd_bwd(logits, tokens, ref_logp, mask, cu_seqlens, pairs, b
     dev, f32 = logits.device, torch.float32
     M, P, code, margin_p, margin_all, ref_p, mask_p, cu_p, pairs_p, weight_p = _pair_args(ref_logp, mask, cu_seqlens, pairs, kind, margin,
                                                                                       pair_weight, T, here)
+    if loss is None and logp is None and reward is None and pair_loss is None:      # one allocation for all four
+        loss, logp, reward, pair_loss = torch.empty(1 + T + M + P, dtype=f32, device=dev).split((1, T, M, P))
     if loss is None:
         loss = torch.empty(1, dtype=f32, device=dev)
     if logp is None:
@@ -983,11 +985,11 @@ def pods_grad_norm(tensors, scale=1.0, norm=None, workspace=None, status=None):
             entries[i].grad, entries[i].grad_type = _dense(t, "tensors[%d]" % i, here)
             entries[i].n = t.numel()
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device="cuda:%d" % here)
+        norm = torch.empty(1, dtype=torch.float32, device="cuda")
     lib = load()
     workspace = _scratch(workspace, lib.pods_grad_norm_workspace_bytes(n), norm.device)
-    rc = lib.pods_grad_norm(entries, n, scale, _vec(norm, torch.float32, 1, "norm", here),
-                            _vec(workspace, torch.uint8, workspace.numel(), "workspace", here), workspace.numel(),
+    size = workspace.numel()
+    rc = lib.pods_grad_norm(entries, n, scale, _vec(norm, torch.float32, 1, "norm", here), _vec(workspace, torch.uint8, size, "workspace", here), size,
                             _vec(status, torch.int32, 1, "status", here, True), _stream())
     if rc:
         _check(rc, "pods_grad_norm")

@@ -19,6 +19,7 @@ struct FwdArgs {
     double inv_tau, c64;               // c64 = log2 e / temperature, c + c_lo the same in two fp32 numbers
     float c, c_lo;
     float* logp;
+    double* logp64;                    // the same before it is rounded; NULL: not wanted
     double* lse;
     float* entropy;
     uint32_t* status;

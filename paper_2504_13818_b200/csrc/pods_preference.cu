@@ -14,10 +14,12 @@ namespace {
 using namespace pods_row;
 
 constexpr int kThreads = 512;
-constexpr int kCluster = 8;
+constexpr int kCluster = 8;            // CTAs at most
+constexpr int kAtOnce = 8;             // tokens a lane has on their way
 
 struct PrefArgs {
     const float* logp;
+    const double* logp64;              // used instead of logp where there is one
     const float* ref_logp;
     const uint8_t* mask;
     const int64_t* cu;
@@ -77,7 +79,12 @@ __device__ __forceinline__ void pair_terms(const PrefArgs& a, double h, double& 
 __global__ void __launch_bounds__(kThreads) pods_preference_kernel(const PrefArgs a) {
     cg::cluster_group cl = cg::this_cluster();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int n_warps = kCluster * (kThreads / 32), gw = (int)cl.block_rank() * (kThreads / 32) + warp;
+    const int CL = (int)cl.num_blocks(), all = CL * kThreads;
+    auto meet = [&] {                                  // after it everybody sees what anybody wrote
+        if (CL == 1) __syncthreads();
+        else cl.sync();
+    };
+    const int n_warps = CL * (kThreads / 32), gw = (int)cl.block_rank() * (kThreads / 32) + warp;
     const int64_t gt = (int64_t)cl.block_rank() * kThreads + threadIdx.x;
     __shared__ double scratch[2][kThreads / 32];
 
@@ -86,12 +93,24 @@ __global__ void __launch_bounds__(kThreads) pods_preference_kernel(const PrefArg
         const int64_t lo = max((int64_t)0, min(a.T, a.cu[i])), hi = max(lo, min(a.T, a.cu[i + 1]));
         double sum = 0.0, like = 0.0;
         int64_t n = 0;
-        for (int64_t t = lo + lane; t < hi; t += 32) {
-            if (a.mask != nullptr && a.mask[t] == 0) continue;
-            const double lp = (double)a.logp[t];
-            sum += a.ref_logp != nullptr ? lp - (double)a.ref_logp[t] : lp;
-            like -= lp;
-            ++n;
+        for (int64_t t = lo + lane; t < hi; t += 32 * kAtOnce) {
+            double lp[kAtOnce];
+            float ref[kAtOnce];
+            bool on[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int64_t at = t + 32 * k;
+                on[k] = at < hi && (a.mask == nullptr || a.mask[at] != 0);
+                lp[k] = at < hi ? (a.logp64 != nullptr ? a.logp64[at] : (double)a.logp[at]) : 0.0;
+                ref[k] = at < hi && a.ref_logp != nullptr ? a.ref_logp[at] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (on[k]) {
+                    sum += lp[k] - (double)ref[k];
+                    like -= lp[k];
+                    ++n;
+                }
         }
         sum = warp_sum(sum);
         like = warp_sum(like);
@@ -116,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) pods_preference_kernel(const PrefArg
         return c_ok && r_ok;
     };
     double count = 0.0;
-    for (int64_t p = gt; p < a.P; p += kCluster * kThreads) {
+    for (int64_t p = gt; p < a.P; p += all) {
         int c, r;
         count += used(p, c, r) ? 1.0 : 0.0;
     }
@@ -127,14 +146,14 @@ __global__ void __launch_bounds__(kThreads) pods_preference_kernel(const PrefArg
         for (int w = 1; w < kThreads / 32; ++w) count += scratch[0][w];
         a.parts[cl.block_rank()] = count;
     }
-    cl.sync();
+    meet();
 
     // 2. every pair's slope and loss
     count = 0.0;
-    for (int b = 0; b < kCluster; ++b) count += a.parts[b];
+    for (int b = 0; b < CL; ++b) count += a.parts[b];
     const double even = count > 0.0 ? 1.0 / count : 0.0;
     double total = 0.0;
-    for (int64_t p = gt; p < a.P; p += kCluster * kThreads) {
+    for (int64_t p = gt; p < a.P; p += all) {
         int c, r;
         double loss = 0.0, slope = 0.0, w = 0.0;
         if (used(p, c, r)) {
@@ -161,12 +180,12 @@ __global__ void __launch_bounds__(kThreads) pods_preference_kernel(const PrefArg
         for (int w = 1; w < kThreads / 32; ++w) total += scratch[1][w];
         a.parts[kCluster + cl.block_rank()] = total;
     }
-    cl.sync();
+    meet();
 
     // 3. the loss, and every token's coefficient
     if (gt == 0) {
         total = 0.0;
-        for (int b = 0; b < kCluster; ++b) total += a.parts[kCluster + b];
+        for (int b = 0; b < CL; ++b) total += a.parts[kCluster + b];
         if (a.loss_acc != nullptr) *a.loss_acc += total;
         else *a.loss32 = (float)total;
     }
@@ -189,17 +208,19 @@ __global__ void __launch_bounds__(kThreads) pods_preference_kernel(const PrefArg
     }
     // rows ahead of the first and behind the last rollout
     const int64_t first = max((int64_t)0, min(a.T, a.cu[0])), last = max(first, min(a.T, a.cu[a.M]));
-    for (int64_t t = gt; t < first; t += kCluster * kThreads) a.dlogp[t] = 0.0f;
-    for (int64_t t = last + gt; t < a.T; t += kCluster * kThreads) a.dlogp[t] = 0.0f;
+    for (int64_t t = gt; t < first; t += all) a.dlogp[t] = 0.0f;
+    for (int64_t t = last + gt; t < a.T; t += all) a.dlogp[t] = 0.0f;
 }
 
 int launch_preference(const PrefArgs& a, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCluster;
+    // one CTA where it has warps and tokens enough for itself: its barriers cost less than a cluster's
+    const int size = a.M <= kThreads / 32 && a.P <= kThreads && a.T <= 16384 ? 1 : kCluster;
+    attr[0].val.clusterDim.x = (unsigned)size;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3(kCluster);
+    cfg.gridDim = dim3((unsigned)size);
     cfg.blockDim = dim3(kThreads);
     cfg.stream = stream;
     cfg.attrs = attr;
@@ -300,7 +321,7 @@ extern "C" int pods_preference(const float* logp, const float* ref_logp, const u
 }
 
 extern "C" size_t pods_preference_fwd_bwd_workspace_bytes(int64_t T, int64_t M, int64_t P) {
-    return T < 0 || M < 0 || P < 0 ? 0 : up((size_t)T * 8) + up((size_t)T * 4) + lay_out(nullptr, nullptr, M, P);
+    return T < 0 || M < 0 || P < 0 ? 0 : 2 * up((size_t)T * 8) + up((size_t)T * 4) + lay_out(nullptr, nullptr, M, P);
 }
 
 extern "C" int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t dtype, const int32_t* tokens,
@@ -325,8 +346,9 @@ extern "C" int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t 
         return PODS_ERR_WORKSPACE;
     unsigned char* const base = static_cast<unsigned char*>(workspace);
     double* const lse = reinterpret_cast<double*>(base);
-    float* const dlogp = reinterpret_cast<float*>(base + up((size_t)T * 8));
-    lay_out(&a, base + up((size_t)T * 8) + up((size_t)T * 4), M, P);
+    double* const logp64 = reinterpret_cast<double*>(base + up((size_t)T * 8));
+    float* const dlogp = reinterpret_cast<float*>(base + 2 * up((size_t)T * 8));
+    lay_out(&a, base + 2 * up((size_t)T * 8) + up((size_t)T * 4), M, P);
     cudaStream_t s = pods_stream(stream);
     if (T > 0) {
         pods_logp::FwdArgs f = {};
@@ -340,12 +362,14 @@ extern "C" int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t 
         f.fill = 1;
         pods_logp::set_temperature(f, temperature);
         f.logp = logp;
+        f.logp64 = logp64;
         f.lse = lse;
         f.status = status;
         rc = pods_logp::launch_forward(f, dtype, s);
         if (rc != PODS_OK) return rc;
     }
     a.logp = logp;
+    a.logp64 = logp64;
     a.dlogp = dlogp;
     a.loss32 = loss;
     rc = launch_preference(a, s);
