@@ -728,12 +728,9 @@ constexpr int kRowsVecs = 1024;        // log-probabilities: the same
 constexpr int kGroupVecs = 8192;       // shares of up to this many vectors are taken by groups of four warps
 
 template <int DT, bool ENT>
-int launch_rows(const FwdArgs& a, int batch, int grid, cudaStream_t stream) {
+int launch_rows(const FwdArgs& a, int dev, int batch, int grid, cudaStream_t stream) {
     static uint64_t prepared = 0;                      // devices as bits
     constexpr size_t smem = sizeof(RowsWarp<ENT>) * (kThreads / 32);
-    int dev = 0;
-    PODS_RETURN_IF_CUDA_ERROR(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return PODS_ERR_UNSUPPORTED;
     if (!(__atomic_load_n(&prepared, __ATOMIC_ACQUIRE) >> dev & 1)) {
         PODS_RETURN_IF_CUDA_ERROR(cudaFuncSetAttribute(pods_logp_rows_kernel<DT, ENT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         __atomic_fetch_or(&prepared, 1ull << dev, __ATOMIC_RELEASE);
@@ -746,12 +743,14 @@ int launch_rows(const FwdArgs& a, int batch, int grid, cudaStream_t stream) {
 template <int DT, bool ENT>
 int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
     const int64_t nvec = a.V / Elem<DT>::E;
-    const int sms = pods_sm_count();
+    int dev;
+    const int sms = pods_logp::device_sms(dev);
+    if (dev < 0) return PODS_ERR_UNSUPPORTED;
     if (nvec <= kRowsVecs) {
         const int64_t per = a.T / ((int64_t)sms * 24);
         const int batch = (int)(per < 1 ? 1 : per > kBatch ? kBatch : per);
         const int64_t ctas = (a.T + (int64_t)batch * (kThreads / 32) - 1) / ((int64_t)batch * (kThreads / 32));
-        return launch_rows<DT, ENT>(a, batch, ctas < 3 * sms ? (int)ctas : 3 * sms, stream);
+        return launch_rows<DT, ENT>(a, dev, batch, ctas < 3 * sms ? (int)ctas : 3 * sms, stream);
     }
     // the cluster size with the shortest longest share: rounds of rows times the vectors of a share and what a row costs beside
     int best = 1;

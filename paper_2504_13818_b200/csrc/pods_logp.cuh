@@ -56,6 +56,21 @@ void set_temperature(Args& a, float temperature) {
     a.c_lo = lo > least ? lo : least > 1e-45f ? least : 1e-45f;
 }
 
+// The current device and its SMs (asked once a device).
+inline int device_sms(int& dev) {
+    static int known[64];
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        dev = -1;
+        return 0;
+    }
+    int n = __atomic_load_n(&known[dev], __ATOMIC_RELAXED);
+    if (n == 0) {
+        n = pods_sm_count();
+        __atomic_store_n(&known[dev], n, __ATOMIC_RELAXED);
+    }
+    return n;
+}
+
 int check_rows(const void* logits, int64_t ldl, int32_t dtype, int64_t T, int32_t V, float temperature);
 int launch_forward(const FwdArgs& a, int dtype, cudaStream_t s);
 int launch_gradient(GradArgs& a, int dtype, cudaStream_t s);
