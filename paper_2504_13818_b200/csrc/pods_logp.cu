@@ -372,6 +372,45 @@ __global__ void __launch_bounds__(kThreads, 3) pods_logp_rows_kernel(const FwdAr
     }
 }
 
+// Few rows, not long: a CTA each, a row's vectors loaded at once, for the time of a small call is a chain of latencies.
+template <int DT, bool ENT>
+__global__ void __launch_bounds__(kThreads) pods_logp_row_kernel(const FwdArgs a) {
+    using El = Elem<DT>;
+    using raw = typename El::raw;
+    __shared__ uint2 left[kThreads];
+    __shared__ float left_u[ENT ? kThreads : 1];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int64_t t = blockIdx.x;
+    if (!live_row(a, t, tid == 0)) return;
+    const float z = tid == 0 ? token_logit<DT>(a, t) : 0.0f;
+    const raw* const row = static_cast<const raw*>(a.logits) + t * a.ldl;
+    const int lead = (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(raw));
+    const int head = min(lead, a.V), nvec = (a.V - head) / El::E;
+    const uint4* const vec = reinterpret_cast<const uint4*>(row + head);
+    const int threads = blockDim.x;
+    Sums<DT, ENT> sums;
+    sums.start();
+    for (int v = tid; v - tid < nvec; v += kBlockVecs * threads) {
+        uint4 q[kBlockVecs];
+#pragma unroll
+        for (int k = 0; k < kBlockVecs; ++k) q[k] = v + k * threads < nvec ? __ldg(vec + v + k * threads) : nothing<DT>();
+        sums.take(q, a.c, a.c_lo);
+    }
+    if (tid < 32) take_edges(a, row, head, head + nvec * El::E, lane, sums);
+    left[tid] = sums.left();
+    if (ENT) left_u[tid] = sums.u;
+    __syncthreads();
+    if (tid >= 32) return;
+    Part p = {0.0, 0.0, kNoRef, 0};
+    for (int k = lane; k < threads; k += 32) p.R = max(p.R, ref_of(left[k]));
+    p.R = __reduce_max_sync(PODS_FULL_MASK, p.R);
+    for (int k = lane; k < threads; k += 32) add_left<ENT>(p, left[k], ENT ? left_u[k] : 0.0f);
+    p.s = warp_reduce(p.s, Plus());
+    if (ENT) p.u = warp_reduce(p.u, Plus());
+    p.bad = (int)__reduce_or_sync(PODS_FULL_MASK, (unsigned)p.bad);
+    finish_rows<DT, ENT>(a, lane == 0 ? t : -1, p, z, lane);
+}
+
 // Long rows: a cluster of CTAs holds a share of the row each and goes round over the rows; a CTA is a producer warp that keeps
 // 192 KB of copies in flight, consumer warps that add up what has arrived, and a warp that finishes the rows, 32 at once.  They
 // meet at mbarriers only, so the copies never wait for a row's end.  Consumers work in groups of W warps, each on a row of its
@@ -725,6 +764,10 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
 
 constexpr int kWarpVecs = 32 * 16;     // gradient: rows of up to this many vectors are taken a warp each
 constexpr int kRowsVecs = 1024;        // log-probabilities: the same
+// Rows of up to kCtaVecs vectors, up to kFewRows of them an SM, get a CTA each.  Measured, a CTA each against what takes more of
+// them: bf16 V = 1000 3.5 : 4.1 us (37 rows), 4.5 : 5.3 (1200), 20.8 : 17.2 (20000); V = 8000 3.7 : 7.7, 11.9 : 11.6, 116 : 64;
+// V = 32000 5.4 : 6.2, 21.3 : 21.0, 67 : 59 (5000).
+constexpr int kFewRows = 8, kCtaVecs = 4096;
 constexpr int kGroupVecs = 8192;       // shares of up to this many vectors are taken by groups of four warps
 
 template <int DT, bool ENT>
@@ -746,6 +789,12 @@ int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
     int dev;
     const int sms = pods_logp::device_sms(dev);
     if (dev < 0) return PODS_ERR_UNSUPPORTED;
+    if (nvec <= kCtaVecs && a.T <= kFewRows * sms) {
+        const int threads = nvec <= 128 ? 32 : nvec <= 256 ? 64 : nvec <= 512 ? 128 : kThreads;
+        pods_logp_row_kernel<DT, ENT><<<(unsigned)a.T, threads, 0, stream>>>(a);
+        PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
+        return PODS_OK;
+    }
     if (nvec <= kRowsVecs) {
         const int64_t per = a.T / ((int64_t)sms * 24);
         const int batch = (int)(per < 1 ? 1 : per > kBatch ? kBatch : per);
