@@ -14,6 +14,10 @@ in general NOT the one a single n -> m selection would keep; everything after th
     and advantages (`row0` = the range's first row): the gradient rows of a step already carry the batch-wide
     factor, and the steps' loss terms add up in the one fp64 accumulator.  No 1/steps factor is needed anywhere.
 
+  * pair losses on the same batch (`pods_preference`; no counterpart in the paper): `logp_step` per step, the pairs of the
+    whole batch, then `logp_grad_step` per step on the logits formed again;
+  * the weights: `update` after the last step, the clipped step of AdamW on the gradients that the steps accumulated.
+
 Host logic only (index arithmetic and calls of the binding); the kernels are the single-batch ones."""
 from dataclasses import dataclass
 
@@ -102,3 +106,35 @@ def loss_step(step, ranges, logits_step, tokens, old_logp, ref_logp, adv, seq_we
                                 None if ref_logp is None else ref_logp[lo:hi], adv, seq_weight, cu_seqlens, lo,
                                 None if mask is None else mask[lo:hi], eps, beta, loss_acc, logp[lo:hi],
                                 dlogits_step[lo - row_lo:hi - row_lo], workspace, status=status)
+
+
+def _step_rows(step, ranges, logits_step):
+    _, _, row_lo, row_hi = ranges[step]
+    if logits_step.shape[0] != row_hi - row_lo:
+        raise ValueError("step %d has %d rows, logits_step has %d" % (step, row_hi - row_lo, logits_step.shape[0]))
+    return row_lo, row_hi
+
+
+def logp_step(step, ranges, logits_step, tokens, mask, logp, lse, temperature=1.0, status=None):
+    """Accumulation step `step` of an objective on log-probabilities: `pods_logp_chunk` over the step's rows, into the
+    batch-wide logp [T] and lse [T] (fp64).  After the last step `pods_preference` takes logp as it is."""
+    lo, hi = _step_rows(step, ranges, logits_step)
+    binding.pods_logp_chunk(logits_step, tokens[lo:hi], temperature=temperature, mask=None if mask is None else mask[lo:hi],
+                            logp=logp[lo:hi], lse=lse[lo:hi], status=status)
+
+
+def logp_grad_step(step, ranges, logits_step, tokens, lse, dlogp, dlogits_step, temperature=1.0, status=None):
+    """The step's logits once more (its forward pass made them again, or kept them): `pods_logp_grad_chunk` with the
+    batch-wide lse and dlogp; ``dlogits_step`` may be ``logits_step``."""
+    lo, hi = _step_rows(step, ranges, logits_step)
+    return binding.pods_logp_grad_chunk(logits_step, tokens[lo:hi], lse[lo:hi], dlogp[lo:hi], temperature=temperature,
+                                        dlogits=dlogits_step, status=status)
+
+
+def update(table, step, lr, max_norm=1.0, grad_scale=1.0, status=None, **settings):
+    """The optimiser's step on the gradients that the accumulation steps added up (`dW` of grpo_loss_from_hidden among
+    them): their norm over all tensors of the table, then AdamW with the gradients scaled down to ``max_norm`` (0: not).
+    A norm that is no finite number leaves the weights as they were.  Returns the norm [1].  ``settings``: as pods_adamw's."""
+    norm = binding.pods_grad_norm(table, scale=grad_scale, status=status)
+    binding.pods_adamw(table, step, lr, norm=norm, max_norm=max_norm, grad_scale=grad_scale, status=status, **settings)
+    return norm

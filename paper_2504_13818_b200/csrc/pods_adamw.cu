@@ -425,14 +425,15 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& 
 
 // This CTA's run of tiles, a stretch of each tensor at a time: f(tensor, first element, tiles)
 template <int N, typename F>
-__device__ __forceinline__ void each_stretch(const Table<N>& tab, F f) {
+__device__ __forceinline__ void each_stretch(const Table<N>& tab, uint32_t* status, F f) {
     const uint32_t lo = (uint32_t)((uint64_t)tab.tiles * blockIdx.x / gridDim.x);
     const uint32_t hi = (uint32_t)((uint64_t)tab.tiles * (blockIdx.x + 1) / gridDim.x);
     int i = tab.start[blockIdx.x];
     for (uint32_t tile = lo; tile < hi; ++i) {
+        if (!PODS_INDEX_OK(i, tab.count, status)) return;
         const Tensor& t = tab.t[i];
         const uint32_t end = min(hi, i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles);
-        f(t, (int64_t)(tile - t.tile0) * kTile, (int)(end - tile));
+        if (PODS_INDEX_OK((int64_t)(end - 1 - t.tile0) * kTile, t.n, status)) f(t, (int64_t)(tile - t.tile0) * kTile, (int)(end - tile));
         tile = end;
     }
 }
@@ -479,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
     c.root = (float)(1.0 / sqrt(b2));
     c.eps = a.eps;
     const uint32_t key = mix(mix(mix((uint32_t)a.seed + 0x9e3779b9u) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
-    each_stretch(tab, [&](const Tensor& t, int64_t base, int tiles) {
+    each_stretch(tab, a.status, [&](const Tensor& t, int64_t base, int tiles) {
         // the stretch's own addresses, so that offsets in it have 32 bits (at most 2^40 elements over the CTAs of a full grid)
         Tensor at;
         at.g = static_cast<const char*>(t.g) + base * bytes_of(GT);
@@ -533,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
 // Squares of four in fp32, everything beyond in fp64; where a sum of four leaves the middle of fp32's range its squares are
 // taken again in fp64, so that neither large nor small gradients are lost.
 template <int N>
-__global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts) {
+__global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts, uint32_t* status) {
     double sum = 0.0;
     auto add = [&](const Raw8& g, int type) {
         float x[8];
@@ -547,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __gri
                 for (int k = h; k < h + 4; ++k) sum += (double)x[k] * (double)x[k];
         }
     };
-    each_stretch(tab, [&](const Tensor& t, int64_t base, int tiles) {
+    each_stretch(tab, status, [&](const Tensor& t, int64_t base, int tiles) {
         const int type = t.g_type;
         const char* const at = static_cast<const char*>(t.g) + base * bytes_of(type);
         uint32_t i = threadIdx.x * 8;
@@ -665,14 +666,14 @@ int most_ctas(int per_sm) {
 }
 
 template <int N>
-int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& used, cudaStream_t s) {
+int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& used, uint32_t* status, cudaStream_t s) {
     int64_t first = 0;
     for (int from = 0; from < n;) {
         Table<N> tab;
         unsigned grid;
         from = fill(tab, t, from, n, nullptr, most_ctas(8), first, grid);
         if (tab.count == 0) continue;
-        pods_grad_norm_kernel<N><<<grid, kThreads, 0, s>>>(tab, parts + used);
+        pods_grad_norm_kernel<N><<<grid, kThreads, 0, s>>>(tab, parts + used, status);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
         used += (int)grid;
     }
@@ -728,7 +729,7 @@ extern "C" int pods_grad_norm(const pods_adamw_tensor* tensors, int32_t n, float
     cudaStream_t s = pods_stream(stream);
     double* const parts = static_cast<double*>(workspace);
     int used = 0;
-    const int e = n <= kFew ? norm_launches<kFew>(tensors, n, parts, used, s) : norm_launches<kMany>(tensors, n, parts, used, s);
+    const int e = n <= kFew ? norm_launches<kFew>(tensors, n, parts, used, status, s) : norm_launches<kMany>(tensors, n, parts, used, status, s);
     if (e != PODS_OK) return e;
     norm_finish_kernel<<<1, 1024, 0, s>>>(parts, used, scale, norm, status);
     PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());

@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(Pipe<W>::threads, 1) pods_logp_pipe_kernel(con
             for (int v = lo; v < hi; v += kStageVecs, ++issued, ring.next(kStages)) {
                 if (issued >= kStages && !mbar_wait(&c.empty[group][ring.st], ring.parity ^ 1u, spins())) late = true;
                 if (lane == 0) {
-                    const int n = min(kStageVecs, hi - v);
+                    const int n = PODS_INDEX_OK(head + min(v + kStageVecs, hi) * El::E - 1, a.V, a.status) ? min(kStageVecs, hi - v) : 0;
                     mbar_expect_tx(&c.full[group][ring.st], (uint32_t)n * 16u);
                     for (int k = 0; k < n; k += 512)
                         bulk_load(mine + (size_t)ring.st * kStageVecs + k, vec + v + k, (uint32_t)min(512, n - k) * 16u, &c.full[group][ring.st]);

@@ -135,6 +135,24 @@ def test_a_rollout_that_stands_in_every_pair(binding):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+def test_no_tokens_and_nothing_but_masked_ones(binding):
+    pairs = torch.tensor([[0, 1], [1, 0]], dtype=torch.int32, device="cuda")
+    none, cu0 = torch.zeros(0, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    acc = torch.zeros(1, dtype=torch.float64, device="cuda")
+    d, reward, losses = binding.pods_preference(none, none, None, cu0, pairs, 0.5, acc, margin=0.25, nll=0.5)
+    want = [preference.pair_loss(-0.25, "sigmoid", 0.0, 0.5)[0]] * 2
+    assert d.numel() == 0 and (reward == 0).all() and np.allclose(losses.tolist(), want, rtol=2.0 ** -23) and abs(acc.item() - want[0]) < 1e-12
+    z, tok = torch.zeros((0, 100), dtype=torch.bfloat16, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    loss, logp, dz, reward, losses = binding.pods_preference_fwd_bwd(z, tok, None, None, cu0, pairs, 0.5, margin=0.25)
+    assert abs(loss.item() - want[0]) <= 2.0 ** -23 and logp.numel() == 0 and dz.shape == (0, 100)
+    z = torch.full((6, 20000), torch.nan, dtype=torch.float16, device="cuda")
+    tok = torch.full((6,), -9, dtype=torch.int32, device="cuda")
+    cu, off = torch.tensor([0, 2, 6], device="cuda"), torch.zeros(6, dtype=torch.uint8, device="cuda")
+    status = binding.new_status()
+    loss, logp, dz, reward, losses = binding.pods_preference_fwd_bwd(z, tok, None, off, cu, pairs, 0.5, average=True, nll=0.5, status=status)
+    assert abs(loss.item() - np.log(2)) <= 2.0 ** -23 and (logp == 0).all() and (dz == 0).all() and binding.read_status(status) == 0
+
+
 TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
 
 
