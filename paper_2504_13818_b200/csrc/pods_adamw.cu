@@ -189,14 +189,14 @@ __device__ __forceinline__ void store_codes(void* base, uint32_t i, int n, bool 
     for (int k = 0; k < 8; ++k)
         if (k < n) at[k] = (uint8_t)((k < 4 ? c.x : c.y) >> (8 * (k & 3)));
 }
-__device__ __forceinline__ void codes_to_floats(uint2 codes, uint32_t scale, float (&x)[8]) {
-    const float s = __uint_as_float(scale << 23);
+// Eight codes as numbers, without their block's scale.
+__device__ __forceinline__ void codes_to_floats(uint2 codes, float (&x)[8]) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t two = (k < 2 ? codes.x : codes.y) >> (16 * (k & 1));
         const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3)));
-        x[2 * k] = f.x * s;
-        x[2 * k + 1] = f.y * s;
+        x[2 * k] = f.x;
+        x[2 * k + 1] = f.y;
     }
 }
 // The largest |x| of eight, NaN if one of them is.
@@ -213,34 +213,6 @@ __device__ __forceinline__ uint32_t block_scale(float top) {
     const uint32_t b = __float_as_uint(top) & 0x7fffffffu;
     return b >= 0x7f800000u ? 255u : (uint32_t)max(1, (int)((b + 0x1fffffu) >> 23) - 8);
 }
-// Codes of eight numbers in a block of scale k.  A number times 2^(127 - k) 2^-120 has e4m3's exponent where fp32 keeps its
-// own, and e4m3's smallest numbers are fp32's: for all of them the code lies above the lowest 20 bits, and 16 random bits and a
-// half (a number that is on the grid stays) added there carry into it with the probability that keeps the average.  Four bits
-// further up the code is the highest byte: one multiply-add makes it, and bytes are picked, so that the integer pipe, which is
-// the busiest, has little to do.  random: the 16 bits in bytes 1 and 2, 0x80 in byte 0.
-template <bool ROOT>
-__device__ __forceinline__ uint2 to_codes(float (&x)[8], uint32_t k, const uint32_t (&random)[8]) {
-    float f = __uint_as_float((134u - k) << 23);
-    if (k > 133u) {                                    // 2^(7 - k) is no normal number: blocks above 28672, in two factors; NaN
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= 0x1p-120f;
-        f = __uint_as_float((254u - min(k, 253u)) << 23);
-    }
-    uint32_t c[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float y = x[i] * f;
-        if (ROOT) y = fmaxf(y, 0x1p-129f);             // the smallest code; a root of 0 is put right by the caller
-        c[i] = __float_as_uint(y) * 16u + random[i];
-        if (!ROOT) c[i] |= __float_as_uint(y) & 0x80000000u;
-    }
-    uint2 r;
-    r.x = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
-    r.y = __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410);
-    if (k == 255u) r = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
-    return r;
-}
-
 // Two fp32 numbers an instruction.
 __device__ __forceinline__ uint64_t pair(float lo, float hi) {
     uint64_t r;
@@ -256,6 +228,41 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Codes of eight numbers in a block of scale k.  A number times 2^(127 - k) 2^-120 has e4m3's exponent where fp32 keeps its
+// own, and e4m3's smallest numbers are fp32's: for all of them the code lies above the lowest 20 bits, and 16 random bits and a
+// half (a number that is on the grid stays) added there carry into it with the probability that keeps the average.  Four bits
+// further up the code is the highest byte: one multiply-add makes it, and bytes are picked, so that the integer pipe, which is
+// the busiest, has little to do.   The 16 random
+// bits go to bytes 1 and 2, the half to byte 0.
+template <bool ROOT>
+__device__ __forceinline__ uint2 to_codes(float (&x)[8], uint32_t k, const uint32_t (&word)[8]) {
+    float f = __uint_as_float((134u - k) << 23);
+    if (k > 133u) {                                    // 2^(7 - k) is no normal number: blocks above 28672, in two factors; NaN
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= 0x1p-120f;
+        f = __uint_as_float((254u - min(k, 253u)) << 23);
+    }
+    uint32_t c[8];
+    const uint64_t f2 = pair(f, f);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        float y[2];
+        unpair(mul2(pair(x[i], x[i + 1]), f2), y[0], y[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (ROOT) y[h] = fmaxf(y[h], 0x1p-129f);   // the smallest code; a root of 0 is put right by the caller
+            const uint32_t w = ROOT ? word[i + h] * 0x9e3779b1u : word[i + h];
+            c[i + h] = __float_as_uint(y[h]) * 16u + __byte_perm(w, 0x80u, 0x7324);
+            if (!ROOT) c[i + h] |= __float_as_uint(y[h]) & 0x80000000u;
+        }
+    }
+    uint2 r;
+    r.x = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
+    r.y = __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410);
+    if (k == 255u) r = make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
     return r;
 }
 
@@ -313,28 +320,50 @@ __device__ __forceinline__ void load_tile(Loaded<BITS>& d, const Tensor& at, int
     }
 }
 
+// What the threads of a CTA have on its way to shared memory for a whole tile; each thread reads only what it asked for itself.
+template <int PT, int GT>
+struct Ahead {
+    static constexpr int gv = GT == PODS_DTYPE_F32 ? 2 : 1, pv = PT == PODS_DTYPE_F32 ? 2 : 1;
+    uint4 g[gv][kThreads], p[pv][kThreads];
+    uint2 m[kThreads], v[kThreads];
+};
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "n"(BYTES) : "memory");
+}
+template <int PT, int GT>
+__device__ __forceinline__ void ask_tile(Ahead<PT, GT>& d, const Tensor& at, uint32_t off) {
+    const char* const g = static_cast<const char*>(at.g) + (size_t)off * (GT == PODS_DTYPE_F32 ? 4 : 2);
+    const char* const p = static_cast<const char*>(at.p) + (size_t)off * (PT == PODS_DTYPE_F32 ? 4 : 2);
+#pragma unroll
+    for (int k = 0; k < Ahead<PT, GT>::gv; ++k) copy_async<16>(&d.g[k][threadIdx.x], g + 16 * k);
+#pragma unroll
+    for (int k = 0; k < Ahead<PT, GT>::pv; ++k) copy_async<16>(&d.p[k][threadIdx.x], p + 16 * k);
+    copy_async<8>(&d.m[threadIdx.x], static_cast<const uint8_t*>(at.m) + off);
+    copy_async<8>(&d.v[threadIdx.x], static_cast<const uint8_t*>(at.v) + off);
+}
+template <int PT, int GT>
+__device__ __forceinline__ void take_tile(Loaded<8>& x, const Ahead<PT, GT>& d) {
+#pragma unroll
+    for (int k = 0; k < Ahead<PT, GT>::gv; ++k) {
+        const uint4 q = d.g[k][threadIdx.x];
+        x.g.w[4 * k] = q.x; x.g.w[4 * k + 1] = q.y; x.g.w[4 * k + 2] = q.z; x.g.w[4 * k + 3] = q.w;
+    }
+#pragma unroll
+    for (int k = 0; k < Ahead<PT, GT>::pv; ++k) {
+        const uint4 q = d.p[k][threadIdx.x];
+        x.p.w[4 * k] = q.x; x.p.w[4 * k + 1] = q.y; x.p.w[4 * k + 2] = q.z; x.p.w[4 * k + 3] = q.w;
+    }
+    x.mc = d.m[threadIdx.x];
+    x.vc = d.v[threadIdx.x];
+}
+
 template <int PT, int GT, int BITS, bool FAST>
 __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& t, const Tensor& at, uint32_t off, int left, const Step& a,
                                            const Coefs& c, float decay, float rate, uint64_t first, uint32_t key) {
     const int vectors = FAST ? t.vectors : 0;
     constexpr bool fast = FAST;
     const int n = FAST ? 8 : left - (int)threadIdx.x * 8;
-    // words = mix(number ^ k32), number a multiple of 8 for the first: the eight share the high word and the mix's first step
-    uint32_t low[8], for_m[8], for_r[8];
-    if (BITS == 8 || a.stochastic) {
-        const uint64_t number = first + off;
-        uint32_t x0 = (uint32_t)number ^ mix(key + (uint32_t)(number >> 32));
-        x0 ^= x0 >> 16;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            uint32_t x = (x0 ^ k) * 0x888ec647u;
-            x = (x ^ (x >> 15)) * 0x246ce511u;
-            const uint32_t word = x ^ (x >> 16);
-            low[k] = word & 0xffffu;
-            for_m[k] = __byte_perm(word, 0x80u, 0x7324);
-            for_r[k] = __byte_perm(word * 0x9e3779b1u, 0x80u, 0x7324);
-        }
-    }
     float pf[8], gf[8], mf[8], vf[8], rf[8];
     to_floats(d.g, GT, gf);
     to_floats(d.p, PT, pf);
@@ -342,10 +371,23 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& 
         to_floats(d.m, PODS_DTYPE_F32, mf);
         to_floats(d.v, PODS_DTYPE_F32, vf);
     } else {
-        codes_to_floats(d.mc, d.ms, mf);
-        codes_to_floats(d.vc, d.vs, vf);
+        codes_to_floats(d.mc, mf);
+        codes_to_floats(d.vc, vf);
     }
-    const uint64_t c_g = pair(c.g, c.g), beta1 = pair(c.beta1, c.beta1), keep1 = pair(c.keep1, c.keep1), beta2 = pair(c.beta2, c.beta2),
+    // the blocks' scales, powers of two, go into the betas: the same numbers as if they had gone into the codes, as long as their
+    // square is a normal number
+    float b1 = c.beta1, b2 = c.beta2;
+    if (BITS == 8) {
+        const float s = __uint_as_float(d.vs << 23);
+        b1 *= __uint_as_float(d.ms << 23);
+        if (d.vs - 65u < 125u) {
+            b2 *= s * s;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) vf[k] *= s;
+        }
+    }
+    const uint64_t c_g = pair(c.g, c.g), beta1 = pair(b1, b1), keep1 = pair(c.keep1, c.keep1), beta2 = pair(b2, b2),
                    keep2 = pair(c.keep2, c.keep2), root = pair(c.root, c.root), eps = pair(c.eps, c.eps), shrink = pair(decay, decay),
                    minus = pair(-rate, -rate);
 #pragma unroll
@@ -371,18 +413,31 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& 
         const uint64_t u = mul2(pair(mf[k], mf[k + 1]), pair(rcp_fast(d0), rcp_fast(d1)));
         unpair(fma2(minus, u, mul2(pair(pf[k], pf[k + 1]), shrink)), pf[k], pf[k + 1]);
     }
+    // words = mix(number ^ k32), number a multiple of 8 for the first: the eight share the high word and the mix's first step
+    uint32_t word[8];
+    if (BITS == 8 || a.stochastic) {
+        const uint64_t number = first + off;
+        uint32_t x0 = (uint32_t)number ^ mix(key + (uint32_t)(number >> 32));
+        x0 ^= x0 >> 16;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            uint32_t x = (x0 ^ k) * 0x888ec647u;
+            x = (x ^ (x >> 15)) * 0x246ce511u;
+            word[k] = x ^ (x >> 16);
+        }
+    }
     if (at.copy != nullptr) store8(at.copy, t.copy_type, off, n, vectors, from_floats(pf, t.copy_type));
     if (PT == PODS_DTYPE_BF16 && a.stochastic) {
         if (largest8(pf) <= FLT_MAX) {
             Raw8 r = {};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                r.w[k] = __byte_perm(__float_as_uint(pf[2 * k]) + low[2 * k], __float_as_uint(pf[2 * k + 1]) + low[2 * k + 1], 0x7632);
+                r.w[k] = __byte_perm(__float_as_uint(pf[2 * k]) + (word[2 * k] & 0xffffu), __float_as_uint(pf[2 * k + 1]) + (word[2 * k + 1] & 0xffffu), 0x7632);
             store8(at.p, PODS_DTYPE_BF16, off, n, vectors, r);
         } else {                                       // what is no number stays none
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + low[k]) & 0xffff0000u);
+                if (fabsf(pf[k]) <= FLT_MAX) pf[k] = __uint_as_float((__float_as_uint(pf[k]) + (word[k] & 0xffffu)) & 0xffff0000u);
             store8(at.p, PODS_DTYPE_BF16, off, n, vectors, from_floats(pf, PODS_DTYPE_BF16));
         }
     } else {
@@ -410,8 +465,8 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& 
             zero_y |= rf[k + 4] == 0.0f ? 0xffu << (8 * k) : 0u;
         }
     }
-    store_codes(at.m, off, n, fast, to_codes<false>(mf, mk, for_m));
-    uint2 rc = to_codes<true>(rf, rk, for_r);
+    store_codes(at.m, off, n, fast, to_codes<false>(mf, mk, word));
+    uint2 rc = to_codes<true>(rf, rk, word);
     if (tiny || !fast) {
         rc.x &= ~zero_x;
         rc.y &= ~zero_y;
@@ -440,7 +495,7 @@ __device__ __forceinline__ void each_stretch(const Table<N>& tab, uint32_t* stat
 
 __device__ __forceinline__ size_t bytes_of(int type) { return type == PODS_DTYPE_F32 ? 4 : 2; }
 
-constexpr int kCtas8 = 3, kCtas32 = 3;                 // an SM
+constexpr int kCtas8 = 4, kCtas32 = 3;                 // an SM
 
 template <int N, int PT, int GT, int BITS>
 __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
@@ -499,19 +554,30 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
         const uint64_t first = (uint64_t)(t.first + base);
         uint32_t off = threadIdx.x * 8;
         int k = 0;
-        if (BITS == 8) {                               // two tiles in turn, each loaded while the other is worked on
-            Loaded<BITS> x, y;
-            if (whole > 0) load_tile<PT, GT, BITS, true>(x, at, t.vectors, off, 0);
-#pragma unroll 1
-            for (; k < whole; k += 2, off += 2 * kTile) {
-                if (k + 1 < whole) load_tile<PT, GT, BITS, true>(y, at, t.vectors, off + kTile, 0);
-                adamw_tile<PT, GT, BITS, true>(x, t, at, off, 0, a, c, decay, rate, first, key);
-                if (k + 1 >= whole) break;
-                if (k + 2 < whole) load_tile<PT, GT, BITS, true>(x, at, t.vectors, off + 2 * kTile, 0);
-                adamw_tile<PT, GT, BITS, true>(y, t, at, off + kTile, 0, a, c, decay, rate, first, key);
+        if (BITS == 8) {                               // the next tile is on its way while one is worked on
+            extern __shared__ __align__(16) unsigned char smem[];
+            Ahead<PT, GT>* const ahead = reinterpret_cast<Ahead<PT, GT>*>(smem);
+            uint32_t ms = 0, vs = 0;
+            if (whole > 0) {
+                ask_tile(ahead[0], at, off);
+                ms = at.m_scale[off >> 5];
+                vs = at.v_scale[off >> 5];
             }
-            k = whole;
-            off = threadIdx.x * 8 + whole * kTile;
+            asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll 1
+            for (; k < whole; ++k, off += kTile) {
+                Loaded<8> x;
+                x.ms = ms;
+                x.vs = vs;
+                if (k + 1 < whole) {
+                    ask_tile(ahead[(k + 1) & 1], at, off + kTile);
+                    ms = at.m_scale[(off + kTile) >> 5];
+                    vs = at.v_scale[(off + kTile) >> 5];
+                }
+                asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
+                take_tile(x, ahead[k & 1]);
+                adamw_tile<PT, GT, 8, true>(x, t, at, off, 0, a, c, decay, rate, first, key);
+            }
         } else {
 #pragma unroll 1
             for (; k < whole; ++k, off += kTile) {
@@ -682,7 +748,7 @@ int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& use
 
 template <int N, int PT, int GT, int BITS>
 void launch_kind(const Table<N>& tab, const Step& a, unsigned grid, cudaStream_t s) {
-    pods_adamw_kernel<N, PT, GT, BITS><<<grid, kThreads, 0, s>>>(tab, a);
+    pods_adamw_kernel<N, PT, GT, BITS><<<grid, kThreads, BITS == 8 ? 2 * sizeof(Ahead<PT, GT>) : 0, s>>>(tab, a);
 }
 template <int N, int PT>
 void launch_kind(const Table<N>& tab, const Step& a, unsigned grid, cudaStream_t s, const Kind& k) {
