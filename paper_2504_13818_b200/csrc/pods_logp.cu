@@ -642,6 +642,23 @@ __global__ void __launch_bounds__(Pipe<W>::threads, 1) pods_logp_pipe_kernel(con
     cl.sync();                                         // no CTA leaves while a peer may still write to it
 }
 
+// 16 bytes from `bytes` (a multiple of the element's) behind a 16-byte boundary, of the 32 that follow it.
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int bytes) {
+    const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const int sub = (bytes & 3) * 8;
+    auto from = [&](auto first) {
+        constexpr int W = decltype(first)::value;
+        return make_uint4(__funnelshift_r(x[W], x[W + 1], sub), __funnelshift_r(x[W + 1], x[W + 2], sub), __funnelshift_r(x[W + 2], x[W + 3], sub),
+                          __funnelshift_r(x[W + 3], W + 4 < 8 ? x[W + 4 < 8 ? W + 4 : 7] : 0u, sub));
+    };
+    switch (bytes >> 2) {                              // the same for the whole row
+        case 0: return from(std::integral_constant<int, 0>());
+        case 1: return from(std::integral_constant<int, 1>());
+        case 2: return from(std::integral_constant<int, 2>());
+        default: return from(std::integral_constant<int, 3>());
+    }
+}
+
 // d objective / d logits.  A CTA takes a stretch of `seg` vectors of one row (WARP: a warp a whole row).
 //   p = 2^(z c - n) 2^-f,  n + f = lse log2 e, n an integer;   out = p (A + B (z c - n)),  + g at the token
 //   A = -2^-f (g + (dH / tau) (H - ln 2 f)),  B = -2^-f (dH / tau) ln 2,  g = dlogp / tau
@@ -679,6 +696,24 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
         if (has_edge) out[edge] = 0;
         return;
     }
+    // the first block is on its way while the row's coefficients are made.  Logits that do not lie on the output's boundaries are
+    // taken from the two vectors of their own that hold them, but for those at the row's ends, whose neighbours may not be the row's.
+    const int apart = (int)(reinterpret_cast<uintptr_t>(row + head) & 15);
+    const uint4* const src = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(row + head) - apart);
+    auto fetch = [&](int v) {
+        if (apart == 0) return src[v];
+        if (v > 0 && v + 1 < nvec) return shifted(src[v], src[v + 1], apart);
+        raw e[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) e[i] = row[head + v * E + i];
+        uint4 q;
+        memcpy(&q, e, sizeof q);
+        return q;
+    };
+    uint4 ahead[kBlockVecs];
+#pragma unroll
+    for (int k = 0; k < kBlockVecs; ++k)
+        if (lo + me + k * G < hi) ahead[k] = fetch(lo + me + k * G);
     int token = a.tokens[t];
     if ((unsigned)token >= (unsigned)a.V) {
         if (me == 0 && seg == 0) pods_raise(a.status, PODS_STATUS_TOKEN_RANGE);
@@ -734,27 +769,18 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
         }
         dst[v] = El::pack(x);
     };
-    if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0) {
-        const uint4* const src = reinterpret_cast<const uint4*>(row + head);
-        int v = lo + me;
-        for (; v + (kBlockVecs - 1) * G < hi; v += kBlockVecs * G) {
-            uint4 q[kBlockVecs];
 #pragma unroll
-            for (int k = 0; k < kBlockVecs; ++k) q[k] = src[v + k * G];
+    for (int k = 0; k < kBlockVecs; ++k)
+        if (lo + me + k * G < hi) vector(ahead[k], lo + me + k * G);
+    int v = lo + me + kBlockVecs * G;
+    for (; v + (kBlockVecs - 1) * G < hi; v += kBlockVecs * G) {
+        uint4 q[kBlockVecs];
 #pragma unroll
-            for (int k = 0; k < kBlockVecs; ++k) vector(q[k], v + k * G);
-        }
-        for (; v < hi; v += G) vector(src[v], v);
-    } else {
-        for (int v = lo + me; v < hi; v += G) {
-            raw e[E];
+        for (int k = 0; k < kBlockVecs; ++k) q[k] = fetch(v + k * G);
 #pragma unroll
-            for (int i = 0; i < E; ++i) e[i] = row[head + v * E + i];
-            uint4 q;
-            memcpy(&q, e, sizeof q);
-            vector(q, v);
-        }
+        for (int k = 0; k < kBlockVecs; ++k) vector(q[k], v + k * G);
     }
+    for (; v < hi; v += G) vector(fetch(v), v);
     if (has_edge) {
         float x = one(El::to_float(row[edge]));
         if (edge == token) x += g;
