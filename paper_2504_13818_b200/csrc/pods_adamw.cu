@@ -23,15 +23,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTile = kThreads * 8;                    // elements, eight a thread; a multiple of 32
-constexpr int kMostCtas = 148 * 8;                     // of a launch; each takes one run of consecutive tiles
+constexpr int kMostCtas = 148 * 4;                     // of a launch; each takes one run of consecutive tiles
+constexpr int kMostNormCtas = 148 * 8;
 
-struct Tensor {
+struct Tensor32 {
     void* p;
     const void* g;
     void* m;
     void* v;
-    uint8_t* m_scale;
-    uint8_t* v_scale;
     void* copy;
     int64_t n, first;                  // elements; the number of the first one among all of the call
     uint32_t tile0;                    // tiles of this launch ahead of it
@@ -39,20 +38,38 @@ struct Tensor {
     uint8_t vectors;                   // 2: eight elements of every buffer lie on their boundary (32 bytes of fp32), 1: 16 bytes, 0: neither
     float decay, lr_scale;
 };
+struct Tensor8 : Tensor32 {
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+};
+struct TensorG {                       // of the norm
+    const void* g;
+    int64_t n;
+    uint32_t tile0;
+    uint8_t g_type, vectors;
+};
 
 // The launch's tensors, and the tensor in which each CTA's run of tiles begins: a search in a table of this size would cost a CTA
 // several misses of the constant cache, one after the other (a norm over 217 tensors: 183 us with it).
-template <int N>
+template <typename E, int N, int CTAS>
 struct Table {
+    using Entry = E;
+    static constexpr int most = N;
     int count;
     uint32_t tiles;
-    uint16_t start[kMostCtas];
-    Tensor t[N];
+    uint16_t start[CTAS];
+    E t[N];
 };
 
 // A kernel argument may hold 32764 bytes; most sets of tensors need few entries, and an argument costs its upload.
-constexpr int kFew = 24, kMany = 320;
-static_assert(sizeof(Table<kMany>) < 32000, "a kernel argument");
+constexpr int kFew = 24;
+using Few8 = Table<Tensor8, kFew, kMostCtas>;
+using Many8 = Table<Tensor8, 352, kMostCtas>;
+using Few32 = Table<Tensor32, kFew, kMostCtas>;
+using Many32 = Table<Tensor32, 432, kMostCtas>;
+using FewG = Table<TensorG, kFew, kMostNormCtas>;
+using ManyG = Table<TensorG, 1248, kMostNormCtas>;
+static_assert(sizeof(Many8) < 32500 && sizeof(Many32) < 32500 && sizeof(ManyG) < 32700, "a kernel argument");
 
 struct Step {
     float lr, beta1, beta2, eps, grad_scale, max_norm;
@@ -299,7 +316,7 @@ struct Loaded {
 // `off`: elements into the stretch; left: elements of the tensor from the tile's first on.  PT, GT: types of parameter and gradient.
 // FAST: whole tiles of tensors on the vectors' boundaries.
 template <int PT, int GT, int BITS, bool FAST>
-__device__ __forceinline__ void load_tile(Loaded<BITS>& d, const Tensor& at, int vectors, uint32_t off, int left) {
+__device__ __forceinline__ void load_tile(Loaded<BITS>& d, const Tensor8& at, int vectors, uint32_t off, int left) {
     const int n = FAST ? 8 : left - (int)threadIdx.x * 8;         // the thread's elements and those behind
     constexpr bool fast = FAST;
     if (fast) {
@@ -332,7 +349,7 @@ __device__ __forceinline__ void copy_async(void* dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "n"(BYTES) : "memory");
 }
 template <int PT, int GT>
-__device__ __forceinline__ void ask_tile(Ahead<PT, GT>& d, const Tensor& at, uint32_t off) {
+__device__ __forceinline__ void ask_tile(Ahead<PT, GT>& d, const Tensor8& at, uint32_t off) {
     const char* const g = static_cast<const char*>(at.g) + (size_t)off * (GT == PODS_DTYPE_F32 ? 4 : 2);
     const char* const p = static_cast<const char*>(at.p) + (size_t)off * (PT == PODS_DTYPE_F32 ? 4 : 2);
 #pragma unroll
@@ -359,7 +376,7 @@ __device__ __forceinline__ void take_tile(Loaded<8>& x, const Ahead<PT, GT>& d) 
 }
 
 template <int PT, int GT, int BITS, bool FAST>
-__device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& t, const Tensor& at, uint32_t off, int left, const Step& a,
+__device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32& t, const Tensor8& at, uint32_t off, int left, const Step& a,
                                            const Coefs& c, float decay, float rate, uint64_t first, uint32_t key) {
     const int vectors = FAST ? t.vectors : 0;
     constexpr bool fast = FAST;
@@ -479,14 +496,14 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor& 
 }
 
 // This CTA's run of tiles, a stretch of each tensor at a time: f(tensor, first element, tiles)
-template <int N, typename F>
-__device__ __forceinline__ void each_stretch(const Table<N>& tab, uint32_t* status, F f) {
+template <typename T, typename F>
+__device__ __forceinline__ void each_stretch(const T& tab, uint32_t* status, F f) {
     const uint32_t lo = (uint32_t)((uint64_t)tab.tiles * blockIdx.x / gridDim.x);
     const uint32_t hi = (uint32_t)((uint64_t)tab.tiles * (blockIdx.x + 1) / gridDim.x);
     int i = tab.start[blockIdx.x];
     for (uint32_t tile = lo; tile < hi; ++i) {
         if (!PODS_INDEX_OK(i, tab.count, status)) return;
-        const Tensor& t = tab.t[i];
+        const auto& t = tab.t[i];
         const uint32_t end = min(hi, i + 1 < tab.count ? tab.t[i + 1].tile0 : tab.tiles);
         if (PODS_INDEX_OK((int64_t)(end - 1 - t.tile0) * kTile, t.n, status)) f(t, (int64_t)(tile - t.tile0) * kTile, (int)(end - tile));
         tile = end;
@@ -497,8 +514,8 @@ __device__ __forceinline__ size_t bytes_of(int type) { return type == PODS_DTYPE
 
 constexpr int kCtas8 = 4, kCtas32 = 3;                 // an SM
 
-template <int N, int PT, int GT, int BITS>
-__global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_adamw_kernel(const __grid_constant__ Table<N> tab, const Step a) {
+template <typename T, int PT, int GT, int BITS>
+__global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_adamw_kernel(const __grid_constant__ T tab, const Step a) {
     __shared__ double bias[2];
     __shared__ int64_t step_now;
     float clip = a.grad_scale;
@@ -535,15 +552,17 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
     c.root = (float)(1.0 / sqrt(b2));
     c.eps = a.eps;
     const uint32_t key = mix(mix(mix((uint32_t)a.seed + 0x9e3779b9u) ^ (uint32_t)(a.seed >> 32)) ^ (uint32_t)step);
-    each_stretch(tab, a.status, [&](const Tensor& t, int64_t base, int tiles) {
+    each_stretch(tab, a.status, [&](const typename T::Entry& t, int64_t base, int tiles) {
         // the stretch's own addresses, so that offsets in it have 32 bits (at most 2^40 elements over the CTAs of a full grid)
-        Tensor at;
+        Tensor8 at;
         at.g = static_cast<const char*>(t.g) + base * bytes_of(GT);
         at.p = static_cast<char*>(t.p) + base * bytes_of(PT);
         at.m = static_cast<char*>(t.m) + base * (BITS == 32 ? 4 : 1);
         at.v = static_cast<char*>(t.v) + base * (BITS == 32 ? 4 : 1);
-        at.m_scale = t.m_scale + (base >> 5);
-        at.v_scale = t.v_scale + (base >> 5);
+        if constexpr (BITS == 8) {
+            at.m_scale = t.m_scale + (base >> 5);
+            at.v_scale = t.v_scale + (base >> 5);
+        }
         at.copy = t.copy == nullptr ? nullptr : static_cast<char*>(t.copy) + base * bytes_of(t.copy_type);
         const float decay = 1.0f - c.lr * t.lr_scale * t.decay, rate = c.step * t.lr_scale;
         // in registers: read from the table again for each tile they cost more than the arithmetic of an element
@@ -599,8 +618,8 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
 // ---- norm -------------------------------------------------------------------------------------------------------------
 // Squares of four in fp32, everything beyond in fp64; where a sum of four leaves the middle of fp32's range its squares are
 // taken again in fp64, so that neither large nor small gradients are lost.
-template <int N>
-__global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __grid_constant__ Table<N> tab, double* parts, uint32_t* status) {
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __grid_constant__ T tab, double* parts, uint32_t* status) {
     double sum = 0.0;
     auto add = [&](const Raw8& g, int type) {
         float x[8];
@@ -614,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __gri
                 for (int k = h; k < h + 4; ++k) sum += (double)x[k] * (double)x[k];
         }
     };
-    each_stretch(tab, status, [&](const Tensor& t, int64_t base, int tiles) {
+    each_stretch(tab, status, [&](const TensorG& t, int64_t base, int tiles) {
         const int type = t.g_type;
         const char* const at = static_cast<const char*>(t.g) + base * bytes_of(type);
         uint32_t i = threadIdx.x * 8;
@@ -691,27 +710,41 @@ struct Kind {
 };
 Kind kind_of(const pods_adamw_tensor& x) { return {x.param_type, x.grad_type, x.state_bits}; }
 
+// The entry of a tensor but for its place in the table.
+void enter(TensorG& d, const pods_adamw_tensor& x, int64_t) {
+    d = {x.grad, x.n, 0, (uint8_t)x.grad_type, 0};
+    for (int level = 1; level <= 2; ++level)
+        if (pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? 16 * level : 16)) d.vectors = (uint8_t)level;
+}
+void enter(Tensor32& d, const pods_adamw_tensor& x, int64_t first) {
+    d = {x.param, x.grad, x.m, x.v, x.copy, x.n, first, 0, (uint8_t)x.grad_type, (uint8_t)x.copy_type, 0, x.weight_decay, x.lr_scale};
+    for (int level = 1; level <= 2; ++level) {
+        const size_t f = 16 * level;
+        if (pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? f : 16) && pods_aligned(x.param, x.param_type == PODS_DTYPE_F32 ? f : 16) &&
+            pods_all_aligned(x.state_bits == 32 ? f : 8, x.m, x.v) &&
+            (x.copy == nullptr || pods_aligned(x.copy, x.copy_type == PODS_DTYPE_F32 ? f : 16)))
+            d.vectors = (uint8_t)level;
+    }
+}
+void enter(Tensor8& d, const pods_adamw_tensor& x, int64_t first) {
+    enter(static_cast<Tensor32&>(d), x, first);
+    d.m_scale = x.m_scale;
+    d.v_scale = x.v_scale;
+}
+
 // Tensors [from, ...) of a kind (of any, where none is given) into the table until it is full; returns the first tensor left.
 // `first`: elements ahead of tensor `from` in the call.  The runs of tiles are for `grid` CTAs.
-template <int N>
-int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, const Kind* kind, int most, int64_t& first, unsigned& grid) {
+template <typename T>
+int fill(T& tab, const pods_adamw_tensor* t, int from, int n, const Kind* kind, int most, int64_t& first, unsigned& grid) {
     tab.count = 0;
     uint32_t tiles = 0;
     int i = from;
-    for (; i < n && tab.count < N; ++i) {
+    for (; i < n && tab.count < T::most; ++i) {
         const pods_adamw_tensor& x = t[i];
         if (x.n != 0 && (kind == nullptr || kind_of(x) == *kind)) {
-            Tensor& d = tab.t[tab.count++];
-            d = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n, first, tiles, (uint8_t)x.grad_type, (uint8_t)x.copy_type, 0,
-                 x.weight_decay, x.lr_scale};
-            for (int level = 1; level <= 2; ++level) {
-                const size_t f = 16 * level;
-                bool on = pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? f : 16);
-                if (kind != nullptr)
-                    on = on && pods_aligned(x.param, x.param_type == PODS_DTYPE_F32 ? f : 16) && pods_all_aligned(x.state_bits == 32 ? f : 8, x.m, x.v) &&
-                         (x.copy == nullptr || pods_aligned(x.copy, x.copy_type == PODS_DTYPE_F32 ? f : 16));
-                if (on) d.vectors = (uint8_t)level;
-            }
+            auto& d = tab.t[tab.count++];
+            enter(d, x, first);
+            d.tile0 = tiles;
             tiles += (uint32_t)((x.n + kTile - 1) / kTile);
         }
         first += (x.n + 31) / 32 * 32;
@@ -726,55 +759,48 @@ int fill(Table<N>& tab, const pods_adamw_tensor* t, int from, int n, const Kind*
     return i;
 }
 
-int most_ctas(int per_sm) {
+int most_ctas(int per_sm, int most) {
     const int n = pods_sm_count() * per_sm;
-    return n < kMostCtas ? n : kMostCtas;
+    return n < most ? n : most;
 }
 
-template <int N>
+template <typename T>
 int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& used, uint32_t* status, cudaStream_t s) {
     int64_t first = 0;
     for (int from = 0; from < n;) {
-        Table<N> tab;
+        T tab;
         unsigned grid;
-        from = fill(tab, t, from, n, nullptr, most_ctas(8), first, grid);
+        from = fill(tab, t, from, n, nullptr, most_ctas(8, kMostNormCtas), first, grid);
         if (tab.count == 0) continue;
-        pods_grad_norm_kernel<N><<<grid, kThreads, 0, s>>>(tab, parts + used, status);
+        pods_grad_norm_kernel<<<grid, kThreads, 0, s>>>(tab, parts + used, status);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
         used += (int)grid;
     }
     return PODS_OK;
 }
 
-template <int N, int PT, int GT, int BITS>
-void launch_kind(const Table<N>& tab, const Step& a, unsigned grid, cudaStream_t s) {
-    pods_adamw_kernel<N, PT, GT, BITS><<<grid, kThreads, BITS == 8 ? 2 * sizeof(Ahead<PT, GT>) : 0, s>>>(tab, a);
+template <typename T, int PT, int GT, int BITS>
+void launch_kind(const T& tab, const Step& a, unsigned grid, cudaStream_t s) {
+    pods_adamw_kernel<T, PT, GT, BITS><<<grid, kThreads, BITS == 8 ? 2 * sizeof(Ahead<PT, GT>) : 0, s>>>(tab, a);
 }
-template <int N, int PT>
-void launch_kind(const Table<N>& tab, const Step& a, unsigned grid, cudaStream_t s, const Kind& k) {
-    constexpr int B = PODS_DTYPE_BF16, H = PODS_DTYPE_F16, F = PODS_DTYPE_F32;
-    if (k.bits == 32) {
-        if (k.g == B) launch_kind<N, PT, B, 32>(tab, a, grid, s);
-        else if (k.g == H) launch_kind<N, PT, H, 32>(tab, a, grid, s);
-        else launch_kind<N, PT, F, 32>(tab, a, grid, s);
-    } else {
-        if (k.g == B) launch_kind<N, PT, B, 8>(tab, a, grid, s);
-        else if (k.g == H) launch_kind<N, PT, H, 8>(tab, a, grid, s);
-        else launch_kind<N, PT, F, 8>(tab, a, grid, s);
-    }
+template <typename T, int PT, int BITS>
+void launch_kind(const T& tab, const Step& a, unsigned grid, cudaStream_t s, int g) {
+    if (g == PODS_DTYPE_BF16) launch_kind<T, PT, PODS_DTYPE_BF16, BITS>(tab, a, grid, s);
+    else if (g == PODS_DTYPE_F16) launch_kind<T, PT, PODS_DTYPE_F16, BITS>(tab, a, grid, s);
+    else launch_kind<T, PT, PODS_DTYPE_F32, BITS>(tab, a, grid, s);
 }
 
-template <int N>
+template <typename T, int BITS>
 int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Kind& k, const Step& a, cudaStream_t s) {
     int64_t first = 0;
     for (int from = 0; from < n;) {
-        Table<N> tab;
+        T tab;
         unsigned grid;
-        from = fill(tab, t, from, n, &k, most_ctas(k.bits == 8 ? kCtas8 : kCtas32), first, grid);
+        from = fill(tab, t, from, n, &k, most_ctas(BITS == 8 ? kCtas8 : kCtas32, kMostCtas), first, grid);
         if (tab.count == 0) continue;
-        if (k.p == PODS_DTYPE_BF16) launch_kind<N, PODS_DTYPE_BF16>(tab, a, grid, s, k);
-        else if (k.p == PODS_DTYPE_F16) launch_kind<N, PODS_DTYPE_F16>(tab, a, grid, s, k);
-        else launch_kind<N, PODS_DTYPE_F32>(tab, a, grid, s, k);
+        if (k.p == PODS_DTYPE_BF16) launch_kind<T, PODS_DTYPE_BF16, BITS>(tab, a, grid, s, k.g);
+        else if (k.p == PODS_DTYPE_F16) launch_kind<T, PODS_DTYPE_F16, BITS>(tab, a, grid, s, k.g);
+        else launch_kind<T, PODS_DTYPE_F32, BITS>(tab, a, grid, s, k.g);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
     }
     return PODS_OK;
@@ -783,7 +809,7 @@ int adamw_launches(const pods_adamw_tensor* t, int32_t n, const Kind& k, const S
 }  // namespace
 
 extern "C" size_t pods_grad_norm_workspace_bytes(int32_t n) {
-    return n < 0 ? 0 : (size_t)(n / kMany + 2) * kMostCtas * sizeof(double);
+    return n < 0 ? 0 : (size_t)(n / ManyG::most + 2) * kMostNormCtas * sizeof(double);
 }
 
 extern "C" int pods_grad_norm(const pods_adamw_tensor* tensors, int32_t n, float scale, float* norm, void* workspace,
@@ -795,7 +821,7 @@ extern "C" int pods_grad_norm(const pods_adamw_tensor* tensors, int32_t n, float
     cudaStream_t s = pods_stream(stream);
     double* const parts = static_cast<double*>(workspace);
     int used = 0;
-    const int e = n <= kFew ? norm_launches<kFew>(tensors, n, parts, used, status, s) : norm_launches<kMany>(tensors, n, parts, used, status, s);
+    const int e = n <= kFew ? norm_launches<FewG>(tensors, n, parts, used, status, s) : norm_launches<ManyG>(tensors, n, parts, used, status, s);
     if (e != PODS_OK) return e;
     norm_finish_kernel<<<1, 1024, 0, s>>>(parts, used, scale, norm, status);
     PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
@@ -841,7 +867,8 @@ extern "C" int pods_adamw(const pods_adamw_tensor* tensors, int32_t n, int64_t s
         const uint32_t bit = 1u << (k.p * 6 + k.g * 2 + (k.bits == 8 ? 1 : 0));
         if (done & bit) continue;
         done |= bit;
-        e = n <= kFew ? adamw_launches<kFew>(tensors, n, k, a, s) : adamw_launches<kMany>(tensors, n, k, a, s);
+        if (k.bits == 8) e = n <= kFew ? adamw_launches<Few8, 8>(tensors, n, k, a, s) : adamw_launches<Many8, 8>(tensors, n, k, a, s);
+        else e = n <= kFew ? adamw_launches<Few32, 32>(tensors, n, k, a, s) : adamw_launches<Many32, 32>(tensors, n, k, a, s);
     }
     return e;
 }

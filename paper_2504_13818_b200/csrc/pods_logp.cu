@@ -788,7 +788,9 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
     }
 }
 
-constexpr int kWarpVecs = 32 * 16;     // gradient: rows of up to this many vectors are taken a warp each
+// Gradient: rows of up to this many vectors are taken a warp each, unless there are few of them.  Measured, a warp each against a
+// CTA each: bf16 V = 1000 81 : 310 us (100000 rows), V = 4000 116 : 157 us (40000), 6.0 : 3.3 us (300); V = 8000 115 : 111 us (20000).
+constexpr int kWarpVecs = 512;
 constexpr int kRowsVecs = 1024;        // log-probabilities: the same
 // Rows of up to kCtaVecs vectors, up to kFewRows of them an SM, get a CTA each.  Measured, a CTA each against what takes more of
 // them: bf16 V = 1000 3.5 : 4.1 us (37 rows), 4.5 : 5.3 (1200), 20.8 : 17.2 (20000); V = 8000 3.7 : 7.7, 11.9 : 11.6, 116 : 64;
@@ -846,7 +848,7 @@ int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
 template <int DT, bool ENT>
 int launch_grad(GradArgs& a, cudaStream_t stream) {
     const int nvec = a.V / Elem<DT>::E;
-    if (nvec <= kWarpVecs) {
+    if (nvec <= kWarpVecs && (nvec <= 128 || a.T > kFewRows * (int64_t)pods_sm_count())) {
         pods_logp_grad_kernel<DT, ENT, true><<<(unsigned)((a.T + kThreads / 32 - 1) / (kThreads / 32)), kThreads, 0, stream>>>(a);
     } else {
         a.n_seg = max(1, (nvec + 4 * kThreads) / (8 * kThreads));

@@ -175,7 +175,7 @@ def test_tensors_off_the_vectors_boundaries(binding, bits, offset):
         assert abs(norm - total) <= 4 * U * total
 
 
-@pytest.mark.parametrize("count", [39, 40, 41, 320, 321, 700])
+@pytest.mark.parametrize("count", [24, 25, 352, 353, 433, 700, 1300])
 def test_many_tensors(binding, count):
     """Sets that fill one table of either size exactly, and more."""
     rng = np.random.default_rng(count)
