@@ -482,7 +482,7 @@ int pods_grad_norm(const pods_adamw_tensor* tensors /*host*/, int32_t n, float s
 /*
  * pods_adamw - step number `step` (1, 2, ...) of Adam with decoupled weight decay on all tensors at once: what takes the
  * gradient of the objective (dW of grpo_loss_from_hidden, or a backward pass that consumed dlogits) to the weights.  (The paper
- * names the optimiser only.)  Per element, all in fp32:
+ * names the optimiser only.)  Per element, in fp32, the operations of g, m and v each rounded by themselves:
  *   g = grad grad_scale min(1, max_norm / norm)          (the last factor where max_norm > 0)
  *   m = beta1 m + (1 - beta1) g      v = beta2 v + (1 - beta2) g^2
  *   param = param (1 - lr_t weight_decay) - lr_t / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),  lr_t = lr lr_scale

@@ -24,7 +24,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = kThreads * 8;                    // elements, eight a thread; a multiple of 32
 constexpr int kMostCtas = 148 * 4;                     // of a launch; each takes one run of consecutive tiles
-constexpr int kMostNormCtas = 148 * 8;
+constexpr int kMostNormCtas = 148 * 6;
 
 struct Tensor32 {
     void* p;
@@ -263,7 +263,7 @@ __device__ __forceinline__ uint2 to_codes(float (&x)[8], uint32_t k, const uint3
         f = __uint_as_float((254u - min(k, 253u)) << 23);
     }
     uint32_t c[8];
-    const uint64_t f2 = pair(f, f);
+    const uint64_t f2 = ROOT ? pair(-f, -f) : pair(f, f);                               // roots come with their sign turned
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
         float y[2];
@@ -283,22 +283,31 @@ __device__ __forceinline__ uint2 to_codes(float (&x)[8], uint32_t k, const uint3
     return r;
 }
 
-__device__ __forceinline__ float sqrt_fast(float x) {      // off by 2^-23 at most; numbers below FLT_MIN are 0
+__device__ __forceinline__ float rsqrt_fast(float x) {
     float y;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// a + b, two numbers at a time but one by one: ptxas makes a fused product and sum of mul.rn.f32x2 and add.rn.f32x2, though both
+// name their rounding (a quarter of the sums differed in the last bit).
+__device__ __forceinline__ void sums(uint64_t a, uint64_t b, float& lo, float& hi) {
+    float al, ah, bl, bh;
+    unpair(a, al, ah);
+    unpair(b, bl, bh);
+    lo = __fadd_rn(al, bl);
+    hi = __fadd_rn(ah, bh);
 }
 __device__ __forceinline__ float rcp_fast(float x) {       // off by 2^-23 at most
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float least8(const float (&x)[8]) {
+__device__ __forceinline__ float largest8s(const float (&x)[8]) {
     float a, b;
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
-    return fminf(a, b);
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
+    return fmaxf(a, b);
 }
 
 struct Coefs {
@@ -404,29 +413,33 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
             for (int k = 0; k < 8; ++k) vf[k] *= s;
         }
     }
-    const uint64_t c_g = pair(c.g, c.g), beta1 = pair(b1, b1), keep1 = pair(c.keep1, c.keep1), beta2 = pair(b2, b2),
-                   keep2 = pair(c.keep2, c.keep2), root = pair(c.root, c.root), eps = pair(c.eps, c.eps), shrink = pair(decay, decay),
-                   minus = pair(-rate, -rate);
+    // The moments are those of fp32 products and sums, each rounded by itself, and their root is the nearest number: what an
+    // 8-bit state is rounded to then depends on nothing but these, for a fused product would turn one code in a million, and with
+    // it the element's next step.  The root by a Newton step, r - (r^2 - v) / (2 r), from r = v rsqrt(v), whose error of 2^-22 goes
+    // to 2^-45; all of it with v's and r's signs turned, which saves the negations.
+    const uint64_t c_g = pair(c.g, c.g), beta1 = pair(b1, b1), keep1 = pair(c.keep1, c.keep1), minus_beta2 = pair(-b2, -b2),
+                   minus_keep2 = pair(-c.keep2, -c.keep2), minus_root = pair(-c.root, -c.root), eps = pair(c.eps, c.eps), shrink = pair(decay, decay),
+                   minus = pair(-rate, -rate), half = pair(0.5f, 0.5f);
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
-        const uint64_t x = mul2(pair(gf[k], gf[k + 1]), c_g), m2 = fma2(keep1, x, mul2(beta1, pair(mf[k], mf[k + 1])));
-        uint64_t v2 = pair(vf[k], vf[k + 1]);
-        if (BITS == 8) v2 = mul2(v2, v2);
-        v2 = fma2(keep2, mul2(x, x), mul2(beta2, v2));
-        unpair(m2, mf[k], mf[k + 1]);
-        unpair(v2, vf[k], vf[k + 1]);
-        rf[k] = sqrt_fast(vf[k]);
-        rf[k + 1] = sqrt_fast(vf[k + 1]);
+        const uint64_t x = mul2(pair(gf[k], gf[k + 1]), c_g);
+        uint64_t w = pair(vf[k], vf[k + 1]);
+        if (BITS == 8) w = mul2(w, w);
+        sums(mul2(beta1, pair(mf[k], mf[k + 1])), mul2(keep1, x), mf[k], mf[k + 1]);
+        sums(mul2(minus_beta2, w), mul2(minus_keep2, mul2(x, x)), vf[k], vf[k + 1]);     // -v
+        const uint64_t v2 = pair(vf[k], vf[k + 1]);
+        const uint64_t y = pair(rsqrt_fast(-vf[k]), rsqrt_fast(-vf[k + 1])), r = mul2(v2, y);
+        unpair(fma2(fma2(r, r, v2), mul2(half, y), r), rf[k], rf[k + 1]);               // -r
     }
-    const bool tiny = least8(vf) < FLT_MIN;            // zeros mostly, of elements that never had a gradient
+    const bool tiny = largest8s(vf) > -FLT_MIN;        // zeros mostly, of elements that never had a gradient
     if (tiny) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) rf[k] = sqrtf(vf[k]);
+        for (int k = 0; k < 8; ++k) rf[k] = -sqrtf(-vf[k]);
     }
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         float d0, d1;
-        unpair(fma2(pair(rf[k], rf[k + 1]), root, eps), d0, d1);
+        unpair(fma2(pair(rf[k], rf[k + 1]), minus_root, eps), d0, d1);
         const uint64_t u = mul2(pair(mf[k], mf[k + 1]), pair(rcp_fast(d0), rcp_fast(d1)));
         unpair(fma2(minus, u, mul2(pair(pf[k], pf[k + 1]), shrink)), pf[k], pf[k + 1]);
     }
@@ -462,6 +475,8 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
     }
     if (BITS == 32) {
         store8(at.m, PODS_DTYPE_F32, off, n, vectors, from_floats(mf, PODS_DTYPE_F32));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) vf[k] = -vf[k];
         store8(at.v, PODS_DTYPE_F32, off, n, vectors, from_floats(vf, PODS_DTYPE_F32));
         return;
     }
@@ -616,22 +631,16 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
 }
 
 // ---- norm -------------------------------------------------------------------------------------------------------------
-// Squares of four in fp32, everything beyond in fp64; where a sum of four leaves the middle of fp32's range its squares are
-// taken again in fp64, so that neither large nor small gradients are lost.
+// Squares and sums in fp64: exact but for 2^-53 a sum, whatever the gradients' size, so that the clipping factor does not depend on
+// how they are grouped.
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __grid_constant__ T tab, double* parts, uint32_t* status) {
-    double sum = 0.0;
+__global__ void __launch_bounds__(kThreads, 6) pods_grad_norm_kernel(const __grid_constant__ T tab, double* parts, uint32_t* status) {
+    double s4[4] = {0.0, 0.0, 0.0, 0.0};
     auto add = [&](const Raw8& g, int type) {
         float x[8];
         to_floats(g, type, x);
 #pragma unroll
-        for (int h = 0; h < 8; h += 4) {
-            const float q = (x[h] * x[h] + x[h + 1] * x[h + 1]) + (x[h + 2] * x[h + 2] + x[h + 3] * x[h + 3]);
-            if (q > 1e-24f && q < 1e38f) sum += (double)q;
-            else
-#pragma unroll
-                for (int k = h; k < h + 4; ++k) sum += (double)x[k] * (double)x[k];
-        }
+        for (int k = 0; k < 8; ++k) s4[k & 3] = fma((double)x[k], (double)x[k], s4[k & 3]);
     };
     each_stretch(tab, status, [&](const TensorG& t, int64_t base, int tiles) {
         const int type = t.g_type;
@@ -649,6 +658,7 @@ __global__ void __launch_bounds__(kThreads, 8) pods_grad_norm_kernel(const __gri
         for (; k < whole; ++k, i += kTile) add(load8(at, type, i, t.vectors), type);
         for (; k < tiles; ++k, i += kTile) add(gather8(at, type, i, (int)max((int64_t)0, min((int64_t)8, t.n - base - i))), type);
     });
+    double sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
     __shared__ double scratch[kThreads / 32];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(PODS_FULL_MASK, sum, d);
@@ -770,7 +780,7 @@ int norm_launches(const pods_adamw_tensor* t, int32_t n, double* parts, int& use
     for (int from = 0; from < n;) {
         T tab;
         unsigned grid;
-        from = fill(tab, t, from, n, nullptr, most_ctas(8, kMostNormCtas), first, grid);
+        from = fill(tab, t, from, n, nullptr, most_ctas(6, kMostNormCtas), first, grid);
         if (tab.count == 0) continue;
         pods_grad_norm_kernel<<<grid, kThreads, 0, s>>>(tab, parts + used, status);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());

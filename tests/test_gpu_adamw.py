@@ -196,6 +196,23 @@ def test_states_of_both_kinds_in_one_table(binding):
     check_step(both, before, 4, 1e-3)
 
 
+@pytest.mark.parametrize("grad", ["fp32", "bf16"])
+def test_moments_are_those_of_single_roundings_bit_for_bit(binding, grad):
+    """Operations of g, m and v rounded one by one: elementary fp32 operations give the same bits, over enough elements to meet every
+    last place, and so 8-bit states do not depend on how a product and a sum were put together."""
+    n = 1 << 22
+    table = make(binding, [n], "fp32", grad, 32, seed=8)
+    (m, v), g = table.states[0], table.grads[0].float()
+    norm = binding.pods_grad_norm(table)
+    assert norm.item() == torch.sqrt(g.double().square().sum()).float().item()
+    b1, b2 = f32(0.9), f32(0.95)
+    x = g * (1.0 / norm)                               # 1 is max_norm
+    want_m = b1 * m + (1.0 - b1) * x
+    want_v = b2 * v + (1.0 - b2) * (x * x)
+    binding.pods_adamw(table, 3, 1e-3, norm=norm, max_norm=1.0, **SET)
+    assert norm.item() > 1 and torch.equal(m, want_m) and torch.equal(v, want_v)
+
+
 def test_steps_far_below_half_a_unit_keep_their_average(binding):
     """bf16 parameters at 1 (units of 2^-7 above, 2^-8 below) that lose 1e-5 a step: nearest rounding leaves them, random bits keep the
     average.  Of n elements each rounds down with probability 1e-5 * 2^8; six standard deviations."""
