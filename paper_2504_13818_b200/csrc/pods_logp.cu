@@ -791,7 +791,13 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
 // Gradient: rows of up to this many vectors are taken a warp each, unless there are few of them.  Measured, a warp each against a
 // CTA each: bf16 V = 1000 81 : 310 us (100000 rows), V = 4000 116 : 157 us (40000), 6.0 : 3.3 us (300); V = 8000 115 : 111 us (20000).
 constexpr int kWarpVecs = 512;
-constexpr int kRowsVecs = 1024;        // log-probabilities: the same
+// Log-probabilities of many rows: up to kRowsVecs vectors a warp each, beyond them the pipeline.  Measured, a warp each against
+// the pipeline: bf16 V = 1000 51 : 390 us (100000 rows), V = 8000 63 : 90 us (20000), V = 16000 65.3 : 65.7 us (10000), fp16
+// V = 32000 78 : 71 us (6007).
+constexpr int kRowsVecs = 1024;
+// The pipeline in groups of four warps for shares of up to this many vectors; sixteen warps a row against it: V = 16000 79 : 66 us,
+// V = 32000 74 : 71 us, V = 50257 64 : 60 us (3000 rows), but 20 : 22 us of 700 rows, which leave a group one or two.
+constexpr int kGroupVecs = 8192;
 // Rows of up to kCtaVecs vectors, up to kFewRows of them an SM, get a CTA each.  Measured, a CTA each against what takes more of
 // them: bf16 V = 1000 3.5 : 4.1 us (37 rows), 4.5 : 5.3 (1200), 20.8 : 17.2 (20000); V = 8000 3.7 : 7.7, 11.9 : 11.6, 116 : 64;
 // V = 32000 5.4 : 6.2, 21.3 : 21.0, 67 : 59 (5000).
@@ -830,6 +836,7 @@ int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
         return launch_rows<DT, ENT>(a, dev, batch, ctas < 3 * sms ? (int)ctas : 3 * sms, stream);
     }
     // the cluster size with the shortest longest share: rounds of rows times the vectors of a share and what a row costs beside
+    // (V = 151936, one CTA a row against what is chosen: 32.4 : 31.0 us of 512 rows, 12.3 : 10.6 of 64, 11.0 : 6.4 of one)
     int best = 1;
     int64_t least = INT64_MAX;
     for (int cl = 1; cl <= 8; cl *= 2) {
