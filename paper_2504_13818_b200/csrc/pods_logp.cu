@@ -802,7 +802,6 @@ constexpr int kGroupVecs = 8192;
 // them: bf16 V = 1000 3.5 : 4.1 us (37 rows), 4.5 : 5.3 (1200), 20.8 : 17.2 (20000); V = 8000 3.7 : 7.7, 11.9 : 11.6, 116 : 64;
 // V = 32000 5.4 : 6.2, 21.3 : 21.0, 67 : 59 (5000).
 constexpr int kFewRows = 8, kCtaVecs = 4096;
-constexpr int kGroupVecs = 8192;       // shares of up to this many vectors are taken by groups of four warps
 
 template <int DT, bool ENT>
 int launch_rows(const FwdArgs& a, int dev, int batch, int grid, cudaStream_t stream) {
