@@ -251,9 +251,8 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 // Codes of eight numbers in a block of scale k.  A number times 2^(127 - k) 2^-120 has e4m3's exponent where fp32 keeps its
 // own, and e4m3's smallest numbers are fp32's: for all of them the code lies above the lowest 20 bits, and 16 random bits and a
 // half (a number that is on the grid stays) added there carry into it with the probability that keeps the average.  Four bits
-// further up the code is the highest byte: one multiply-add makes it, and bytes are picked, so that the integer pipe, which is
-// the busiest, has little to do.   The 16 random
-// bits go to bytes 1 and 2, the half to byte 0.
+// further up the code is the highest byte: one multiply-add makes it, and bytes are picked, so that the integer pipe has little to
+// do.  The 16 random bits go to bytes 1 and 2, the half to byte 0.
 template <bool ROOT>
 __device__ __forceinline__ uint2 to_codes(float (&x)[8], uint32_t k, const uint32_t (&word)[8]) {
     float f = __uint_as_float((134u - k) << 23);
@@ -308,6 +307,14 @@ __device__ __forceinline__ float largest8s(const float (&x)[8]) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
     asm("max.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
     return fmaxf(a, b);
+}
+
+__device__ __forceinline__ float least8s(const float (&x)[8]) {
+    float a, b;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
+    return fminf(a, b);
 }
 
 struct Coefs {
@@ -431,8 +438,9 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
         const uint64_t y = pair(rsqrt_fast(-vf[k]), rsqrt_fast(-vf[k + 1])), r = mul2(v2, y);
         unpair(fma2(fma2(r, r, v2), mul2(half, y), r), rf[k], rf[k + 1]);               // -r
     }
-    const bool tiny = largest8s(vf) > -FLT_MIN;        // zeros mostly, of elements that never had a gradient
-    if (tiny) {
+    // zeros mostly, of elements that never had a gradient; squares that overflowed
+    const bool tiny = largest8s(vf) > -FLT_MIN;
+    if (tiny || least8s(vf) < -FLT_MAX) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) rf[k] = -sqrtf(-vf[k]);
     }

@@ -277,6 +277,27 @@ def test_norms_of_tiny_and_huge_gradients(binding, scale):
     assert abs(binding.pods_grad_norm(g).item() - want) <= 4 * U * want
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_gradients_whose_square_overflows_or_vanishes(binding, bits):
+    """v infinite: the step is 0; v 0 beside a first moment: the step is the moment over eps."""
+    table = make(binding, [4096 + 64], "fp32", "fp32", bits, warm=False, decay=0.0)
+    p, g = table.params[0], table.grads[0]
+    g[5], g[4100] = 1e20, -3e30
+    g[64:96] = 1e-30
+    before = p.clone()
+    binding.pods_adamw(table, 1, 1e-2, beta1=0.5, beta2=0.5, eps=1e-8)
+    assert p[5] == before[5] and p[4100] == before[4100] and torch.isfinite(p).all()
+    # m-hat = 1e-30 over eps: 1e-24 of a step
+    assert torch.equal(p[64:96], before[64:96])
+    moved = torch.ones(p.numel(), dtype=torch.bool)
+    moved[[5, 4100]] = False
+    moved[64:96] = False
+    assert ((p - before).abs()[moved.cuda()] <= 1.001e-2).all() and ((p - before).abs()[moved.cuda()] > 0.9e-2).float().mean() > 0.99
+    if bits == 32:
+        m, v = table.states[0]
+        assert m[5].item() == f32(0.5e20) and v[5] == torch.inf and (v[64:96] == 0).all()
+
+
 def test_norm_of_nothing(binding):
     assert binding.pods_grad_norm([]).item() == 0
     assert binding.pods_grad_norm([torch.zeros(0, device="cuda"), torch.zeros(7, device="cuda", dtype=torch.float16)]).item() == 0
