@@ -301,22 +301,6 @@ __device__ __forceinline__ float rcp_fast(float x) {       // off by 2^-23 at mo
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float largest8s(const float (&x)[8]) {
-    float a, b;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
-    return fmaxf(a, b);
-}
-
-__device__ __forceinline__ float least8s(const float (&x)[8]) {
-    float a, b;
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(x[0]), "f"(x[1]), "f"(x[2]));
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(b) : "f"(x[3]), "f"(x[4]), "f"(x[5]));
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(x[6]), "f"(x[7]));
-    return fminf(a, b);
-}
-
 struct Coefs {
     float g, beta1, beta2, keep1, keep2, lr, step, root, eps;
 };
@@ -438,11 +422,13 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
         const uint64_t y = pair(rsqrt_fast(-vf[k]), rsqrt_fast(-vf[k + 1])), r = mul2(v2, y);
         unpair(fma2(fma2(r, r, v2), mul2(half, y), r), rf[k], rf[k + 1]);               // -r
     }
-    // zeros mostly, of elements that never had a gradient; squares that overflowed
-    const bool tiny = largest8s(vf) > -FLT_MIN;
-    if (tiny || least8s(vf) < -FLT_MAX) {
+    // no root came of a v of 0 (elements that never had a gradient, mostly), below the normal numbers, infinite or NaN
+    float top = largest8(rf);
+    const bool odd = !(top <= FLT_MAX);
+    if (odd) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) rf[k] = -sqrtf(-vf[k]);
+        top = largest8(rf);
     }
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
@@ -492,13 +478,14 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (k >= n) mf[k] = rf[k] = 0.0f;
+        top = largest8(rf);
     }
-    uint32_t scales = block_scale(largest8(mf)) | block_scale(largest8(rf)) << 16;     // larger numbers have larger scales
+    uint32_t scales = block_scale(largest8(mf)) | block_scale(top) << 16;     // larger numbers have larger scales
     scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 1));
     scales = __vmaxu2(scales, __shfl_xor_sync(PODS_FULL_MASK, scales, 2));
     const uint32_t mk = scales & 0xffffu, rk = scales >> 16;
     uint32_t zero_x = 0, zero_y = 0;                   // bytes of the roots that are 0
-    if (tiny || !fast) {
+    if (odd || !fast) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             zero_x |= rf[k] == 0.0f ? 0xffu << (8 * k) : 0u;
@@ -507,7 +494,7 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
     }
     store_codes(at.m, off, n, fast, to_codes<false>(mf, mk, word));
     uint2 rc = to_codes<true>(rf, rk, word);
-    if (tiny || !fast) {
+    if (odd || !fast) {
         rc.x &= ~zero_x;
         rc.y &= ~zero_y;
     }
