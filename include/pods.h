@@ -447,7 +447,7 @@ int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t dtype, cons
 /*
  * One tensor of pods_grad_norm and pods_adamw.  The array of them is in HOST memory and is read during the call only; every
  * pointer in it is [dev].  Tensors are dense; n elements, each pointer aligned to its element type (vectors are used where all of
- * a tensor's pointers lie on four elements' boundaries).  No two may overlap.
+ * a tensor's pointers lie on 16-byte boundaries, those of 8-bit states on 8-byte ones).  No two may overlap.
  *   state_bits 32: m, v fp32 [n], the first moment and the second.
  *   state_bits 8:  m, v uint8 [n], e4m3 numbers; m_scale, v_scale uint8 [(n + 31) / 32], the exponent k of each block of 32
  *                  elements: an element is its number times 2^(k - 127).  v holds the ROOT of the second moment.  All bytes 0 is
