@@ -492,7 +492,7 @@ int pods_grad_norm(const pods_adamw_tensor* tensors /*host*/, int32_t n, float s
  *   step_dev [dev] int64, lr_dev [dev] fp32, or NULL: read on the device instead of step and lr, for captured graphs
  *   norm [dev] fp32 or NULL, as pods_grad_norm left it with the same scale.  A norm that is NaN or infinite leaves every tensor
  *          as it was and raises PODS_STATUS_NONFINITE_GRAD.
- * Betas in [0, 1), eps >= 0.  A gradient that is no number makes its element no number, and its block's 8-bit states; so does
+ * Betas in [0, 1), eps 0 or in [FLT_MIN, 2^126] (with 0, an element that never had a gradient becomes 0/0, NaN).  A gradient that is no number makes its element no number, and its block's 8-bit states; so does
  * one whose square overflows, but that it leaves the parameter where an infinite v puts it.
  */
 int pods_adamw(const pods_adamw_tensor* tensors /*host*/, int32_t n, int64_t step, const int64_t* step_dev, float lr,

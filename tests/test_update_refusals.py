@@ -101,9 +101,9 @@ def adamw(lib, e=None, n=1, step=1, lr=0.1, beta1=0.9, beta2=0.99, eps=1e-8, sca
 
 @pytest.mark.parametrize("want,kw", [
     (INVALID, dict(n=-1)), (INVALID, dict(step=0)), (INVALID, dict(lr=nan)), (INVALID, dict(beta1=1.0)), (INVALID, dict(beta2=-0.1)),
-    (INVALID, dict(beta1=nan)), (INVALID, dict(eps=-1.0)), (INVALID, dict(eps=inf)), (INVALID, dict(scale=inf)), (INVALID, dict(max_norm=1.0)),
+    (INVALID, dict(beta1=nan)), (INVALID, dict(eps=-1.0)), (INVALID, dict(eps=inf)), (INVALID, dict(eps=1e-38)), (INVALID, dict(eps=1e38)), (INVALID, dict(scale=inf)), (INVALID, dict(max_norm=1.0)),
     (INVALID, dict(max_norm=-1.0)), (INVALID, dict(max_norm=nan, norm=F)), (INVALID, dict(norm=at(2))), (INVALID, dict(step_dev=at(4))),
-    (UNSUPPORTED, dict(flags=2)), (0, dict(n=0))])
+    (UNSUPPORTED, dict(flags=2)), (0, dict(n=0)), (0, dict(n=0, eps=0.0)), (0, dict(n=0, eps=2.0 ** -126)), (0, dict(n=0, eps=2.0 ** 126))])
 def test_adamw_refuses_settings_on_the_host(lib, want, kw):
     assert adamw(lib, **kw) == want
 
