@@ -13,12 +13,15 @@
 #include <type_traits>
 
 #include "pods_logp.cuh"
+#include "row_plan.cuh"
 
 namespace {
 
 using namespace pods_row;
 using pods_logp::FwdArgs;
 using pods_logp::GradArgs;
+using pods_logp::kBatch;
+using pods_logp::kFewRows;
 
 constexpr int kThreads = 256;
 constexpr int kBlockVecs = 4;          // vectors a thread takes at once
@@ -251,7 +254,6 @@ __device__ __forceinline__ uint4 nothing() {           // a vector of -inf
 // lanes sum a row: a reduction over the warp for each row, its logarithms and the chain to its token's logit would cost more
 // than 1000 logits do.  bf16, 20000 rows of 8000 logits 63 us (5.1 TB/s), 100000 of 1000 51 us (3.9 TB/s); the exponentials' pipe is
 // busy 71 % of the first.
-constexpr int kBatch = 8;
 constexpr int kAhead = 3;              // blocks a warp holds
 
 template <bool ENT>
@@ -796,17 +798,6 @@ __global__ void __launch_bounds__(kThreads) pods_logp_grad_kernel(const GradArgs
 // Gradient: rows of up to this many vectors are taken a warp each, unless there are few of them.  Measured, a warp each against a
 // CTA each: bf16 V = 1000 81 : 310 us (100000 rows), V = 4000 116 : 157 us (40000), 6.0 : 3.3 us (300); V = 8000 115 : 111 us (20000).
 constexpr int kWarpVecs = 512;
-// Log-probabilities of many rows: up to kRowsVecs vectors a warp each, beyond them the pipeline.  Measured, a warp each against
-// the pipeline: bf16 V = 1000 51 : 390 us (100000 rows), V = 8000 63 : 90 us (20000), V = 16000 65.3 : 65.7 us (10000), fp16
-// V = 32000 78 : 71 us (6007).
-constexpr int kRowsVecs = 1024;
-// The pipeline in groups of four warps for shares of up to this many vectors; sixteen warps a row against it: V = 16000 79 : 66 us,
-// V = 32000 74 : 71 us, V = 50257 64 : 60 us (3000 rows), but 20 : 22 us of 700 rows, which leave a group one or two.
-constexpr int kGroupVecs = 8192;
-// Rows of up to kCtaVecs vectors, up to kFewRows of them an SM, get a CTA each.  Measured, a CTA each against what takes more of
-// them: bf16 V = 1000 3.5 : 4.1 us (37 rows), 4.5 : 5.3 (1200), 20.8 : 17.2 (20000); V = 8000 3.7 : 7.7, 11.9 : 11.6, 116 : 64;
-// V = 32000 5.4 : 6.2, 21.3 : 21.0, 67 : 59 (5000).
-constexpr int kFewRows = 8, kCtaVecs = 4096;
 
 template <int DT, bool ENT>
 int launch_rows(const FwdArgs& a, int dev, int batch, int grid, cudaStream_t stream) {
@@ -827,33 +818,19 @@ int launch_fwd(const FwdArgs& a, cudaStream_t stream) {
     int dev;
     const int sms = pods_logp::device_sms(dev);
     if (dev < 0) return PODS_ERR_UNSUPPORTED;
-    if (nvec <= kCtaVecs && a.T <= kFewRows * sms) {
+    const pods_logp::RowPlan plan = pods_logp::plan_rows(a.T, nvec, sms);
+    if (plan.kernel == pods_logp::kRowEach) {
         const int threads = nvec <= 128 ? 32 : nvec <= 256 ? 64 : nvec <= 512 ? 128 : kThreads;
         pods_logp_row_kernel<DT, ENT><<<(unsigned)a.T, threads, 0, stream>>>(a);
         PODS_RETURN_IF_CUDA_ERROR(cudaGetLastError());
         return PODS_OK;
     }
-    if (nvec <= kRowsVecs) {
-        const int64_t per = a.T / ((int64_t)sms * 24);
-        const int batch = (int)(per < 1 ? 1 : per > kBatch ? kBatch : per);
-        const int64_t ctas = (a.T + (int64_t)batch * (kThreads / 32) - 1) / ((int64_t)batch * (kThreads / 32));
-        return launch_rows<DT, ENT>(a, dev, batch, ctas < 3 * sms ? (int)ctas : 3 * sms, stream);
+    if (plan.kernel == pods_logp::kRowsWarp) {
+        const int64_t per_cta = (int64_t)plan.batch * (kThreads / 32), ctas = (a.T + per_cta - 1) / per_cta;
+        return launch_rows<DT, ENT>(a, dev, plan.batch, ctas < 3 * sms ? (int)ctas : 3 * sms, stream);
     }
-    // the cluster size with the shortest longest share: rounds of rows times the vectors of a share and what a row costs beside
-    // (V = 151936, one CTA a row against what is chosen: 32.4 : 31.0 us of 512 rows, 12.3 : 10.6 of 64, 11.0 : 6.4 of one)
-    int best = 1;
-    int64_t least = INT64_MAX;
-    for (int cl = 1; cl <= 8; cl *= 2) {
-        const int64_t n = cl == 1 ? sms : cl == 2 ? sms / 2 : (sms - 16) / cl;         // clusters at once; larger ones leave SMs empty
-        const int64_t cost = (a.T + n - 1) / n * (nvec / cl + (cl == 1 ? 1000 : 1250));
-        if (cost < least) {
-            least = cost;
-            best = cl;
-        }
-    }
-    // groups of four warps want several rows each
-    return nvec / best <= kGroupVecs && a.T * best >= 16 * (int64_t)sms ? launch_row_clusters<pods_logp_pipe_kernel<DT, ENT, 4>>(a, a.T, best, Pipe<4>::threads, kStageBytes + sizeof(PipeCtrl<4>), stream)
-                                     : launch_row_clusters<pods_logp_pipe_kernel<DT, ENT, 16>>(a, a.T, best, Pipe<16>::threads, kStageBytes + sizeof(PipeCtrl<16>), stream);
+    return plan.warps == 4 ? launch_row_clusters<pods_logp_pipe_kernel<DT, ENT, 4>>(a, a.T, plan.cluster, Pipe<4>::threads, kStageBytes + sizeof(PipeCtrl<4>), stream)
+                           : launch_row_clusters<pods_logp_pipe_kernel<DT, ENT, 16>>(a, a.T, plan.cluster, Pipe<16>::threads, kStageBytes + sizeof(PipeCtrl<16>), stream);
 }
 
 template <int DT, bool ENT>
