@@ -45,3 +45,20 @@ def test_devices_and_parts_of_them(plan, sms):
                     assert 1 <= batch <= 8 and V * esize <= 1024 * 16 + 15
                 else:
                     assert kernel == ROW_EACH and T <= 8 * sms and V * esize <= 4096 * 16 + 15
+
+
+def test_the_sizes_tested_on_the_gpu_reach_every_kernel(plan):
+    """On 148 SMs; a limit that moves has to take the sizes of these tests along."""
+    from test_gpu_logp_many_rows import SHAPES
+    seen = set()
+    for name, dtype, T, V, _ in SHAPES:
+        kernel, batch, warps, cluster = plan(T, V, 4 if dtype == "fp32" else 2)
+        got = "rows" if kernel == ROWS_WARP else "pipe%d" % warps if kernel == ROWS_PIPE else "row"
+        assert name == got + (" x%d" % cluster if cluster > 1 else ""), (T, V, dtype)
+        seen.add((name, dtype) if kernel == ROWS_WARP else name)
+        if kernel == ROWS_WARP:
+            seen.add("batch of 1" if batch == 1 else "batch of 8" if batch == 8 else "batch between")
+        elif T > 32 * 148 // cluster:
+            seen.add("more rows than a look at the mask, " + ("one CTA" if cluster == 1 else "a cluster"))
+    assert seen >= {("rows", "bf16"), ("rows", "fp16"), ("rows", "fp32"), "batch of 1", "batch of 8", "batch between", "pipe4", "pipe16", "pipe16 x2",
+                    "pipe16 x4", "pipe16 x8", "more rows than a look at the mask, one CTA", "more rows than a look at the mask, a cluster"}
