@@ -380,8 +380,8 @@ int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype, const int
  *   mask   [dev] uint8 [T] or NULL: rows with mask 0 are not read and their outputs are left as they were
  *   logp   [dev] fp32 [T]    lse [dev] fp64 [T] or NULL (64 bits, so that pods_logp_grad_chunk loses nothing on logits far from
  *          0; sums themselves are to fp32's precision)    entropy [dev] fp32 [T] or NULL
- * -inf marks an id without probability.  A row with NaN or +inf gets NaN throughout (PODS_STATUS_NONFINITE_LOGIT), one of -inf
- * alone lse -inf and NaN otherwise (PODS_STATUS_EMPTY_ROW).  temperature: finite, at least FLT_MIN.  V above PODS_MAX_ROW_V, T
+ * -inf marks an id without probability (a large negative number does it too, at the same cost).  A row with NaN or +inf gets NaN
+ * throughout (PODS_STATUS_NONFINITE_LOGIT), one of -inf alone lse -inf and NaN otherwise (PODS_STATUS_EMPTY_ROW).  temperature: finite, at least FLT_MIN.  V above PODS_MAX_ROW_V, T
  * above 2^24 or an unknown dtype returns PODS_ERR_UNSUPPORTED.  No workspace.
  */
 int pods_logp_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* tokens, const uint8_t* mask, int64_t T,

@@ -32,11 +32,11 @@ constexpr int kNoRef = -(1 << 28);
 constexpr double kExponentialsLow = 3.5e-8 * 1.4426950408889634;
 constexpr int kFar = 1 << 22;          // references from here on leave fp32 too few fractional bits: the row is taken in fp64
 
-// A part of a row: S and U relative to 2^R.  R == kNoRef: nothing but -inf so far.
+// A part of a row: S and U relative to 2^R.  R == kNoRef: nothing above -kFar so far.
 struct Part {
     double s, u;
     int R;
-    int bad;                           // 1: NaN or +inf, 2: far
+    int bad;                           // 1: NaN or +inf, 2: far above 0
 };
 
 __device__ __forceinline__ double pow2_int(int n) {    // n <= 0
@@ -106,7 +106,7 @@ struct Sums {
         float bs, bu;
         add_all(q, c, c_lo, bs, bu);
         if (!(bs < kSumLimit) || (fresh && !(bs > 1.0f / kSumLimit))) {
-            // rare: the reference lies far from the first block or below a later one; NaN, +inf, nothing but -inf
+            // rare: the reference lies far from the first block or below a later one; NaN, +inf, nothing but ids ruled out
             float m = -INFINITY;
 #pragma unroll
             for (int k = 0; k < N; ++k) m = max_nan(m, El::vec_max(q[k]));
@@ -115,8 +115,8 @@ struct Sums {
             if (!(m < INFINITY)) bad |= 1;
             else if (m > -INFINITY) {
                 const float top = ceilf(m * c);
-                if (!(fabsf(top) < (float)kFar)) bad |= 2;
-                else {
+                if (!(top < (float)kFar)) bad |= 2;
+                else if (top > -(float)kFar) {         // below: nothing so far, see finish_rows
                     const int to = (int)top;
                     if (to > R) {
                         const float f = R - to < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + R - to) << 23);
@@ -180,8 +180,11 @@ __device__ __forceinline__ float token_logit(const FwdArgs& a, int64_t t) {
 // A warp's lanes each hold the sums of a row of their own (t < 0: none), and its token's logit: writes the rows' outputs.
 template <int DT, bool ENT>
 __device__ __forceinline__ void finish_rows(const FwdArgs& a, int64_t t, Part p, float z, int lane) {
-    // far, or nothing above 2^kNoRef: fp64 tells huge negative logits from a row of -inf
-    const bool far = t >= 0 && (p.bad == 2 || (p.bad == 0 && p.R == kNoRef));
+    // far, or nothing near 0: a thread leaves out blocks below -kFar (ids ruled out by a large negative number), which are nothing beside
+    // a reference above -kFar / 2; without one fp64 also tells huge negative logits from a row of -inf.  2048 bf16 rows of 151936 logits
+    // with nine in ten at the type's lowest value: 117 us spread, 126 us in one stretch ahead of the others (106 us without; 7500 us if
+    // such a block sends its row to fp64).
+    const bool far = t >= 0 && (p.bad == 2 || (p.bad == 0 && p.R < -kFar / 2));
     float top = 0.0f;
     for (unsigned todo = __ballot_sync(PODS_FULL_MASK, far); todo != 0; todo &= todo - 1) {
         const int who = __ffs(todo) - 1;
