@@ -80,6 +80,7 @@ struct Step {
     const float* norm;
     uint64_t seed;
     int stochastic;
+    uint32_t least_ms, least_vs, fold_vs;  // block scales that may go into the betas: from least_ms on; fold_vs from least_vs on
     uint32_t* status;
 };
 
@@ -392,17 +393,20 @@ __device__ __forceinline__ void adamw_tile(const Loaded<BITS>& d, const Tensor32
         codes_to_floats(d.mc, mf);
         codes_to_floats(d.vc, vf);
     }
-    // the blocks' scales, powers of two, go into the betas: the same numbers as if they had gone into the codes, as long as their
-    // square is a normal number
+    // the blocks' scales, powers of two, go into the betas: the same numbers as if they had gone into the codes, as long as the square
+    // of the second and both products are normal numbers
     float b1 = c.beta1, b2 = c.beta2;
     if (BITS == 8) {
-        const float s = __uint_as_float(d.vs << 23);
-        b1 *= __uint_as_float(d.ms << 23);
-        if (d.vs - 65u < 125u) {
-            b2 *= s * s;
+        const float s1 = __uint_as_float(d.ms << 23), s2 = __uint_as_float(d.vs << 23);
+        if (d.ms >= a.least_ms && d.vs - a.least_vs < a.fold_vs) {
+            b1 *= s1;
+            b2 *= s2 * s2;
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) vf[k] *= s;
+            for (int k = 0; k < 8; ++k) {
+                mf[k] *= s1;
+                vf[k] *= s2;
+            }
         }
     }
     // The moments are those of fp32 products and sums, each rounded by itself, and their root is the nearest number: what an
@@ -527,7 +531,7 @@ constexpr int kCtas8 = 4, kCtas32 = 3;                 // an SM
 
 // Eight consecutive elements a thread, since a block of 32 is then four lanes' (four: 2.1 ms), and a run of tiles a CTA, since the
 // tensor is looked up once a stretch.  32-bit states: HBM bounds it, 1.42 ms of 303 M fp32 weights with bf16 copy and gradients
-// (6.0 TB/s).  8-bit states: instruction issue (77 % of the cycles), 685 us of 311 M bf16 weights with fp32 gradients (5.5 TB/s), 658
+// (6.0 TB/s).  8-bit states: instruction issue (77 % of the cycles), 705 us of 311 M bf16 weights with fp32 gradients (5.35 TB/s), 658
 // with bf16 gradients (4.8 TB/s); loads a tile ahead in registers took 731 where copies to shared memory took
 // 701.
 template <typename T, int PT, int GT, int BITS>
@@ -867,6 +871,13 @@ extern "C" int pods_adamw(const pods_adamw_tensor* tensors, int32_t n, int64_t s
     a.norm = norm;
     a.seed = seed;
     a.stochastic = (flags & PODS_ADAMW_STOCHASTIC) ? 1 : 0;
+    // beta = f 2^e with f in [1/2, 1): its product with a power of two is normal from 2^(-125 - e) on
+    int e1, e2;
+    frexpf(beta1, &e1);
+    frexpf(beta2, &e2);
+    a.least_ms = (uint32_t)max(2 - e1, 1);
+    a.least_vs = (uint32_t)max((130 - e2) / 2, 65);
+    a.fold_vs = a.least_vs < 190u ? 190u - a.least_vs : 0u;
     a.status = status;
     cudaStream_t s = pods_stream(stream);
     // a launch for each kind of tensor; sets have one or two
