@@ -1,5 +1,6 @@
-"""pods_logp_chunk's kernels for many rows, its finite masks, and the optimiser's smallest states once more on the checked build of the
-library: computed indices are compared with their extents, and a violation raises PODS_STATUS_INTERNAL, which those tests reject."""
+"""pods_logp_chunk's kernels for many rows, its finite masks, the optimiser's smallest states and full tables once more on the checked
+build of the library: computed indices are compared with their extents, and a violation raises PODS_STATUS_INTERNAL, which those tests
+reject."""
 import os
 import subprocess
 import sys
@@ -13,7 +14,8 @@ pytestmark = pytest.mark.gpu
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-@pytest.mark.parametrize("tests", ["tests/test_gpu_logp_many_rows.py", "tests/test_gpu_logp_finite_masks.py", "tests/test_gpu_adamw_small_states.py"])
+@pytest.mark.parametrize("tests", ["tests/test_gpu_logp_many_rows.py", "tests/test_gpu_logp_finite_masks.py", "tests/test_gpu_adamw_small_states.py",
+                                   "tests/test_gpu_adamw_tables.py"])
 def test_on_the_checked_build(tests):
     lib = cuda_build.CHECKED_LIB
     sources = cuda_build.SOURCES + cuda_build.HEADERS
