@@ -34,7 +34,7 @@ struct Tensor32 {
     void* copy;
     int64_t n, first;                  // elements; the number of the first one among all of the call
     uint32_t tile0;                    // tiles of this launch ahead of it
-    uint8_t g_type, copy_type;
+    uint8_t copy_type;
     uint8_t vectors;                   // 2: eight elements of every buffer lie on their boundary (32 bytes of fp32), 1: 16 bytes, 0: neither
     float decay, lr_scale;
 };
@@ -188,9 +188,8 @@ __device__ __forceinline__ void store8(void* base, int type, uint32_t i, int n, 
 }
 
 // ---- e4m3 blocks: a block of 32 is held by four lanes -----------------------------------------------------------------------
-__device__ __forceinline__ uint2 load_codes(const void* base, uint32_t i, int n, bool fast) {
+__device__ __forceinline__ uint2 gather_codes(const void* base, uint32_t i, int n) {
     const uint8_t* at = static_cast<const uint8_t*>(base) + i;
-    if (fast) return *reinterpret_cast<const uint2*>(at);
     uint2 r = make_uint2(0, 0);
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -316,9 +315,10 @@ struct Loaded {
 };
 
 // `off`: elements into the stretch; left: elements of the tensor from the tile's first on.  PT, GT: types of parameter and gradient.
-// FAST: whole tiles of tensors on the vectors' boundaries.
+// FAST: whole tiles of tensors on the vectors' boundaries (those with 8-bit states go through shared memory, see ask_tile).
 template <int PT, int GT, int BITS, bool FAST>
 __device__ __forceinline__ void load_tile(Loaded<BITS>& d, const Tensor8& at, int vectors, uint32_t off, int left) {
+    static_assert(BITS == 32 || !FAST);
     const int n = FAST ? 8 : left - (int)threadIdx.x * 8;         // the thread's elements and those behind
     constexpr bool fast = FAST;
     if (fast) {
@@ -332,8 +332,8 @@ __device__ __forceinline__ void load_tile(Loaded<BITS>& d, const Tensor8& at, in
         d.m = fast ? load8(at.m, PODS_DTYPE_F32, off, vectors) : gather8(at.m, PODS_DTYPE_F32, off, n);
         d.v = fast ? load8(at.v, PODS_DTYPE_F32, off, vectors) : gather8(at.v, PODS_DTYPE_F32, off, n);
     } else {
-        d.mc = load_codes(at.m, off, n, fast);
-        d.vc = load_codes(at.v, off, n, fast);
+        d.mc = gather_codes(at.m, off, n);
+        d.vc = gather_codes(at.v, off, n);
         d.ms = n > 0 ? at.m_scale[off >> 5] : 0;
         d.vs = n > 0 ? at.v_scale[off >> 5] : 0;
     }
@@ -593,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? kCtas8 : kCtas32) pods_a
         const uint64_t first = (uint64_t)(t.first + base);
         uint32_t off = threadIdx.x * 8;
         int k = 0;
-        if (BITS == 8) {                               // the next tile is on its way while one is worked on
+        if constexpr (BITS == 8) {                     // the next tile is on its way while one is worked on
             extern __shared__ __align__(16) unsigned char smem[];
             Ahead<PT, GT>* const ahead = reinterpret_cast<Ahead<PT, GT>*>(smem);
             uint32_t ms = 0, vs = 0;
@@ -732,7 +732,7 @@ void enter(TensorG& d, const pods_adamw_tensor& x, int64_t) {
         if (pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? 16 * level : 16)) d.vectors = (uint8_t)level;
 }
 void enter(Tensor32& d, const pods_adamw_tensor& x, int64_t first) {
-    d = {x.param, x.grad, x.m, x.v, x.copy, x.n, first, 0, (uint8_t)x.grad_type, (uint8_t)x.copy_type, 0, x.weight_decay, x.lr_scale};
+    d = {x.param, x.grad, x.m, x.v, x.copy, x.n, first, 0, (uint8_t)x.copy_type, 0, x.weight_decay, x.lr_scale};
     for (int level = 1; level <= 2; ++level) {
         const size_t f = 16 * level;
         if (pods_aligned(x.grad, x.grad_type == PODS_DTYPE_F32 ? f : 16) && pods_aligned(x.param, x.param_type == PODS_DTYPE_F32 ? f : 16) &&

@@ -889,7 +889,7 @@ extern "C" int pods_logp_chunk(const void* logits, int64_t ldl, int32_t dtype, c
     a.mask = mask;
     a.T = T;
     a.V = V;
-    pods_logp::set_temperature(a, temperature);
+    a.c64 = pods_logp::set_temperature(a, temperature);
     a.logp = logp;
     a.lse = lse;
     a.entropy = entropy;

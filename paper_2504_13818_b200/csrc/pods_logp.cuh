@@ -36,24 +36,24 @@ struct GradArgs {
     int64_t T;
     int32_t V;
     int32_t n_seg, seg;
-    double inv_tau, c64;               // c64 = log2 e / temperature, c + c_lo the same in two fp32 numbers
-    float c, c_lo;
+    double inv_tau;
+    float c, c_lo;                     // their sum is log2 e / temperature
     void* dlogits;
     int64_t ldd;
     uint32_t* status;
 };
 
-// Exponents of temperatures so cold that the scale overflows are taken in fp64, as those of huge logits are.
+// Sets the scales of a call; returns log2 e / temperature, which is at most 1.3e38 (temperatures are normal numbers).
 template <typename Args>
-void set_temperature(Args& a, float temperature) {
+double set_temperature(Args& a, float temperature) {
     a.inv_tau = 1.0 / (double)temperature;
     const double c = 1.4426950408889634074 / (double)temperature;
-    a.c64 = c;
-    a.c = c > 3e38 ? 3e38f : (float)c;
+    a.c = (float)c;
     if ((double)a.c > c) a.c = nextafterf(a.c, 0.0f);
     // above 0, so that -inf times it is -inf as -inf times c is
-    const float lo = c > 3e38 ? 0.0f : (float)(c - (double)a.c), least = a.c * 0x1p-48f;
+    const float lo = (float)(c - (double)a.c), least = a.c * 0x1p-48f;
     a.c_lo = lo > least ? lo : least > 1e-45f ? least : 1e-45f;
+    return c;
 }
 
 // The current device and its SMs (asked once a device).

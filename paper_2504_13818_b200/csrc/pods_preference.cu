@@ -361,7 +361,7 @@ extern "C" int pods_preference_fwd_bwd(const void* logits, int64_t ldl, int32_t 
         f.T = T;
         f.V = V;
         f.fill = 1;
-        pods_logp::set_temperature(f, temperature);
+        f.c64 = pods_logp::set_temperature(f, temperature);
         f.logp = logp;
         f.logp64 = logp64;
         f.lse = lse;
