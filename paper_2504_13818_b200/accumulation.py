@@ -115,20 +115,22 @@ def _step_rows(step, ranges, logits_step):
     return row_lo, row_hi
 
 
-def logp_step(step, ranges, logits_step, tokens, mask, logp, lse, temperature=1.0, status=None):
+def logp_step(step, ranges, logits_step, tokens, mask, logp, lse, temperature=1.0, status=None, entropy=None):
     """Accumulation step `step` of an objective on log-probabilities: `pods_logp_chunk` over the step's rows, into the
-    batch-wide logp [T] and lse [T] (fp64).  After the last step `pods_preference` takes logp as it is."""
+    batch-wide logp [T], lse [T] (fp64) and, where given, entropy [T].  After the last step `pods_preference` takes logp as
+    it is."""
     lo, hi = _step_rows(step, ranges, logits_step)
     binding.pods_logp_chunk(logits_step, tokens[lo:hi], temperature=temperature, mask=None if mask is None else mask[lo:hi],
-                            logp=logp[lo:hi], lse=lse[lo:hi], status=status)
+                            logp=logp[lo:hi], lse=lse[lo:hi], entropy=None if entropy is None else entropy[lo:hi], status=status)
 
 
-def logp_grad_step(step, ranges, logits_step, tokens, lse, dlogp, dlogits_step, temperature=1.0, status=None):
+def logp_grad_step(step, ranges, logits_step, tokens, lse, dlogp, dlogits_step, temperature=1.0, status=None, entropy=None, dentropy=None):
     """The step's logits once more (its forward pass made them again, or kept them): `pods_logp_grad_chunk` with the
-    batch-wide lse and dlogp; ``dlogits_step`` may be ``logits_step``."""
+    batch-wide lse and dlogp, and with entropy and dentropy for an entropy bonus; ``dlogits_step`` may be ``logits_step``."""
     lo, hi = _step_rows(step, ranges, logits_step)
     return binding.pods_logp_grad_chunk(logits_step, tokens[lo:hi], lse[lo:hi], dlogp[lo:hi], temperature=temperature,
-                                        dlogits=dlogits_step, status=status)
+                                        entropy=None if entropy is None else entropy[lo:hi],
+                                        dentropy=None if dentropy is None else dentropy[lo:hi], dlogits=dlogits_step, status=status)
 
 
 def update(table, step, lr, max_norm=1.0, grad_scale=1.0, status=None, **settings):
