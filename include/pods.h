@@ -381,8 +381,8 @@ int pods_distill_chunk(const void* logits, int64_t ldl, int32_t dtype, const int
  *   logp   [dev] fp32 [T]    lse [dev] fp64 [T] or NULL (64 bits, so that pods_logp_grad_chunk loses nothing on logits far from
  *          0; sums themselves are to fp32's precision)    entropy [dev] fp32 [T] or NULL
  * -inf marks an id without probability (a large negative number does it too, at the same cost).  A row with NaN or +inf gets NaN
- * throughout (PODS_STATUS_NONFINITE_LOGIT), one of -inf alone lse -inf and NaN otherwise (PODS_STATUS_EMPTY_ROW).  temperature: finite, at least FLT_MIN.  V above PODS_MAX_ROW_V, T
- * above 2^24 or an unknown dtype returns PODS_ERR_UNSUPPORTED.  No workspace.
+ * throughout (PODS_STATUS_NONFINITE_LOGIT), one of -inf alone lse -inf and NaN otherwise (PODS_STATUS_EMPTY_ROW).  temperature:
+ * finite, at least FLT_MIN.  V above PODS_MAX_ROW_V, T above 2^24 or an unknown dtype returns PODS_ERR_UNSUPPORTED.  No workspace.
  */
 int pods_logp_chunk(const void* logits, int64_t ldl, int32_t dtype, const int32_t* tokens, const uint8_t* mask, int64_t T,
                     int32_t V, float temperature, float* logp, double* lse, float* entropy, uint32_t* status, void* stream);
@@ -412,9 +412,10 @@ size_t pods_preference_workspace_bytes(int64_t M, int64_t P);
  *   l_p = loss_p(h_p) + nll (1 / |o_c|) sum_t mask_t (-logp_t)                                       t of rollout c
  * sum_p w_p l_p is ADDED to *loss_acc, w_p = pair_weight[p] or 1 / the number of pairs in use, and
  *   dlogp[t] = grad_scale mask_t d(sum_p w_p l_p) / d logp_t        (0 for rows that belong to no rollout)
- * A rollout may stand in any number of pairs.  A pair with an id of -1 is unused, one with another id outside [0,M) raises
- * PODS_STATUS_INDEX_RANGE and is unused too: its pair_loss is 0.  A pair of weight 0 leaves nothing in the loss or in dlogp.  A
- * log-probability of -inf makes scores and losses infinite or NaN as the formulas do; masked ones are not read.
+ * A rollout may stand in any number of pairs; its pairs should lie together in the list, for the list is read from the first of them
+ * to the last (a shuffled list costs time in the product of M and P).  A pair with an id of -1 is unused, one with another id outside
+ * [0,M) raises PODS_STATUS_INDEX_RANGE and is unused too: its pair_loss is 0.  A pair of weight 0 leaves nothing in the loss or in
+ * dlogp.  A log-probability of -inf makes scores and losses infinite or NaN as the formulas do; masked ones are not read.
  *   logp, ref_logp (NULL: 0), mask (NULL: ones), dlogp: [dev] arrays of T (fp32, fp32, uint8, fp32 out)
  *   cu_seqlens [dev] int64 [M+1]    pairs [dev] int32 [P,2]    pair_weight [dev] fp32 [P] or NULL
  *   margin_pair [dev] fp32 [P], or NULL: margin holds for every pair    label_smoothing in [0, 1/2), sigmoid only
@@ -472,8 +473,8 @@ typedef struct {
 size_t pods_grad_norm_workspace_bytes(int32_t n);
 
 /*
- * pods_grad_norm - norm [dev] fp32 scalar = |scale| sqrt(sum over all tensors of their squared gradients) (fp64 beyond a few
- * terms, fixed order).  Reads grad, n and grad_type of each entry.  A norm that is NaN or infinite raises
+ * pods_grad_norm - norm [dev] fp32 scalar = |scale| sqrt(sum over all tensors of their squared gradients) (squares and sums in
+ * fp64, fixed order).  Reads grad, n and grad_type of each entry.  A norm that is NaN or infinite raises
  * PODS_STATUS_NONFINITE_GRAD.  workspace [dev], 8-byte aligned.
  */
 int pods_grad_norm(const pods_adamw_tensor* tensors /*host*/, int32_t n, float scale, float* norm, void* workspace,

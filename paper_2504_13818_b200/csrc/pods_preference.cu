@@ -4,7 +4,8 @@
 // A pair's slope is known only when both of its rollouts have been summed, and a token's coefficient only when every pair of
 // its rollout has its slope: three phases with a barrier between them, which one thread-block cluster takes in one launch
 // (a few MB at most are read: 8 bytes a token; latency bounds it).  Sums are fp64 in a fixed order.  A rollout's coefficient
-// is summed over the stretch of the list that holds its first to its last pair, in the list's order.
+// is summed over the stretch of the list that holds its first to its last pair, in the list's order: pairs that lie together cost little
+// (65536 rollouts of 20 tokens, as many pairs in order 1.6 ms), shuffled ones the product of rollouts and pairs (69 ms).
 #include <float.h>
 
 #include "pods_logp.cuh"
@@ -217,7 +218,7 @@ int launch_preference(const PrefArgs& a, cudaStream_t stream) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     // one CTA where it has warps and tokens enough for itself: its barriers cost less than a cluster's (32 rollouts of 188 tokens
-    // 8.3 : 9.1 us; a cluster for 128 of 500 18 us, for 1024 of 500 and 4096 pairs 136)
+    // 8.3 : 9.1 us; a cluster for 128 of 500 18.5 us, for 1024 of 500 and 4096 pairs 135)
     const int size = a.M <= 2 * kThreads / 32 && a.P <= kThreads && a.T <= 16384 ? 1 : kCluster;
     attr[0].val.clusterDim.x = (unsigned)size;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
