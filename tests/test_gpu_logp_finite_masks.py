@@ -51,7 +51,7 @@ def test_values(binding, dtype, T, V):
     assert binding.read_status(status) == 0
 
 
-def shortest(f, n=5):
+def shortest(f, n=12):
     """Device time of a call, the shortest of n."""
     f()
     times = []
